@@ -62,7 +62,8 @@ enum {
   TEMPO_ERR_NULL = -1,        /* a required pointer is NULL                      */
   TEMPO_ERR_SHAPE = -2,       /* a size is not positive or not a multiple of 128 */
   TEMPO_ERR_UNSUPPORTED = -3, /* a size exceeds a documented limit               */
-  TEMPO_ERR_CUDA = -4         /* a CUDA call (launch, tensor-map encode) failed  */
+  TEMPO_ERR_CUDA = -4,        /* a CUDA call (launch, tensor-map encode) failed  */
+  TEMPO_ERR_ALIGN = -5        /* a pointer is not aligned as its comment asks    */
 };
 
 enum {
@@ -71,7 +72,8 @@ enum {
                                   claimed twice: the entry counts as absent / zero                   */
   TEMPO_STATUS_CAPACITY = 4,   /* padded rows exceed M_cap: rows that do not fit are dropped         */
   TEMPO_STATUS_TIMEOUT = 8,    /* a bounded device wait expired; the outputs of that call are invalid */
-  TEMPO_STATUS_BAD_SCALE = 16  /* tempo_pack_weights met a weight scale that is not a power of two   */
+  TEMPO_STATUS_BAD_SCALE = 16, /* tempo_pack_weights met a weight scale that is not a power of two   */
+  TEMPO_STATUS_BAD_LOGIT = 32  /* tempo_route met a logit that is not finite: chosen last, weight 0   */
 };
 
 int tempo_version(void);
@@ -304,6 +306,81 @@ int tempo_permute_pad_bf16(const tempo_shape* shape, const void* x_bf16, const i
 int tempo_grouped_ffn_bf16(const tempo_shape* shape, const void* a_bf16, const void* packed,
                            const int32_t* inst_off, const int32_t* m_pad, void* h_bf16, void* y_bf16,
                            uint32_t* status, void* workspace, void* stream);
+
+/*
+ * Norms around the block, for every row count from one token up.  One kernel each, every operand read once.
+ *   tempo_norm_in    x  = norm(r) * w + b
+ *   tempo_norm_out   r' = r_scale * r + y_scale * g (.) (norm(y) * post_w + post_b)
+ *                    x' = norm(r') * next_w + next_b           (the next block's input, from the 32-bit r')
+ * norm(v) = v / sqrt(mean(v^2) + eps) (TEMPO_NORM_RMS) or the same of v - mean(v) (TEMPO_NORM_LAYER), sums in 32 bits.
+ *   y, x, x' bf16; r, r' bf16 or f32 (stream_f32); weights and biases bf16 or f32 (param_f32), [d]; the gate bf16 or f32
+ *   (gate_f32), element (t, c) at gate[t * gate_row + c * gate_col]: pitches (0, 1) are a gate per channel, (1, 0) per
+ *   token, (d, 1) per element; both 0 one number.
+ *   Optional (NULL): b, post_w (y is not normed), post_b, gate (1), next_b, n_valid, and x' with next_w.
+ *   Rows are d elements at pitches ld_* >= d (elements); rows t >= n_valid are neither read nor written.  r' may be r and
+ *   x' may be y (same address and pitch).  Any d from 1 to 16384; rows that 16-byte (8-, 4-byte) vectors do not divide
+ *   or align run with narrower loads.  Pointers need the alignment of their element (TEMPO_ERR_ALIGN).
+ */
+enum { TEMPO_NORM_RMS = 0, TEMPO_NORM_LAYER = 1 };
+typedef struct {
+  int32_t T, d;
+  int32_t kind;                             /* TEMPO_NORM_RMS or TEMPO_NORM_LAYER */
+  int32_t stream_f32, param_f32, gate_f32;  /* 0: bf16, 1: f32 */
+  int64_t ld_y, ld_r, ld_r_out, ld_x;       /* row pitches in elements (tempo_norm_in: ld_r and ld_x only) */
+  int64_t gate_row, gate_col;
+  float eps, r_scale, y_scale;
+} tempo_norm;
+int tempo_norm_in(const tempo_norm* args, const void* r, const void* w, const void* b, const int32_t* n_valid, void* x_bf16,
+                  void* stream);
+int tempo_norm_out(const tempo_norm* args, const void* y_bf16, const void* r, const void* post_w, const void* post_b,
+                   const void* gate, const void* next_w, const void* next_b, const int32_t* n_valid, void* r_out,
+                   void* x_bf16, void* stream);
+
+/*
+ * The router: what tempo_count_dispatch and tempo_few_ffn take as topk_ids and topk_w.  One kernel.
+ *   logits[t, e] = sum_c x[t, c] * w_router[e, c], bf16 x bf16 with 32-bit accumulation
+ *   p[t, e] = softmax(logits[t])_e (TEMPO_ROUTE_SOFTMAX) or 1 / (1 + exp(-logits[t, e])) (TEMPO_ROUTE_SIGMOID)
+ *   ids[t, :] = the k experts with the largest logits, or with the largest p + bias where a bias is given, in falling
+ *               order; ties go to the lowest expert
+ *   w[t, s] = p[t, ids[t, s]], divided by its sum over s if `renormalise`, times `scale`
+ * A logit that is not finite is chosen after every finite one, with weight 0 (TEMPO_STATUS_BAD_LOGIT); so is, without the
+ * status bit, an expert whose bias is not finite (-inf takes an expert out).  The k ids of a token are always distinct.
+ * Rows t >= n_valid get ids -1 and weights 0.
+ *   in   x bf16 [T, d], w_router bf16 [E, d] (16-byte aligned), bias f32 [E] or NULL, n_valid or NULL
+ *   out  topk_ids i32 [T, k], topk_w f32 [T, k]
+ * k <= E (TEMPO_ERR_SHAPE), E <= 512 (TEMPO_ERR_UNSUPPORTED).  G_max, R_max, f, M_cap are not used, but checked.
+ */
+enum { TEMPO_ROUTE_SOFTMAX = 0, TEMPO_ROUTE_SIGMOID = 1 };
+int tempo_route(const tempo_shape* shape, int32_t score, int32_t renormalise, float scale, const void* x_bf16,
+                const void* w_router_bf16, const float* bias, const int32_t* n_valid, int32_t* topk_ids, float* topk_w,
+                uint32_t* status, void* stream);
+
+/*
+ * Steps 1 to 4 for a few tokens (T <= 64, T*k <= 1024) in one kernel; with tempo_route a whole layer is two kernels.
+ *   out[t, :] = sum_s topk_w[t, s] * W2_e (silu(Wgate_e x_t) (.) (Wup_e x_t)),  e = topk_ids[t, s]
+ * over the experts that replica_map puts on this rank; of several replicas the first column with a slot is used.  Each
+ * chosen expert's weights are read once; no 128-row padding, no quota table.  `packed` is the blob of tempo_pack_weights
+ * (tempo_pack_weights_bf16 for the _bf16 call).  Unlike steps 2 and 3, x and H are not rounded to 8 bits: both enter the
+ * products as two e4m3 terms (8 significant bits; x exactly), in the _bf16 call as bf16 (x) and two bf16 terms (H).
+ * A value of x that is not finite makes its own token's output NaN.  Rows without a local expert and rows t >= n_valid
+ * are zero.  An id outside [0, E) of a live row is ignored (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token
+ * counts twice.  Results do not depend on timing; nothing is summed with atomics.
+ *   in   x bf16 [T, d] (16-byte aligned), topk_ids i32 [T, k], topk_w f32 [T, k], n_valid or NULL,
+ *        replica_map i32 [E, R_max], packed (256-byte aligned)
+ *   out  out bf16 [T, d] (16-byte aligned)
+ *   workspace  tempo_few_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves
+ *        it ready for the next.  One workspace serves every call on one stream with the same G_max, d and f and with T and k
+ *        no larger than those it was sized for.  After TEMPO_STATUS_TIMEOUT zero it again.  Calls that may overlap
+ *        on the GPU need a workspace each.
+ * The kernel's CTAs (one per SM) wait for each other, bounded as in tempo_grouped_ffn.
+ */
+int tempo_few_workspace_bytes(const tempo_shape* shape /*[host]*/, size_t* bytes /*[host]*/);
+int tempo_few_ffn(const tempo_shape* shape, const void* x_bf16, const int32_t* topk_ids, const float* topk_w,
+                  const int32_t* n_valid, const int32_t* replica_map, const void* packed, void* out_bf16, uint32_t* status,
+                  void* workspace, void* stream);
+int tempo_few_ffn_bf16(const tempo_shape* shape, const void* x_bf16, const int32_t* topk_ids, const float* topk_w,
+                       const int32_t* n_valid, const int32_t* replica_map, const void* packed, void* out_bf16,
+                       uint32_t* status, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

@@ -15,7 +15,9 @@ import torch
 _LIB_PATH = os.environ.get("TEMPO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtempo.so")
 
 TEMPO_OK = 0
-STATUS_BAD_ID, STATUS_BAD_TABLE, STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_BAD_SCALE = 1, 2, 4, 8, 16
+STATUS_BAD_ID, STATUS_BAD_TABLE, STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_BAD_SCALE, STATUS_BAD_LOGIT = 1, 2, 4, 8, 16, 32
+NORM_RMS, NORM_LAYER = 0, 1
+ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 
 EXPORTS = (
     "tempo_version", "tempo_status_string", "tempo_m_cap_bound", "tempo_sf_bytes", "tempo_workspace_bytes",
@@ -25,11 +27,18 @@ EXPORTS = (
     "tempo_token_sf_bytes", "tempo_quantize_tokens", "tempo_grouped_ffn_gather", "tempo_unpermute_combine",
     "tempo_count_dispatch_masked", "tempo_permute_pad_masked", "tempo_grouped_ffn_masked",
     "tempo_packed_weight_bytes_bf16", "tempo_pack_weights_bf16", "tempo_permute_pad_bf16", "tempo_grouped_ffn_bf16",
+    "tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_workspace_bytes", "tempo_few_ffn", "tempo_few_ffn_bf16",
 )
 
 
 class TempoShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "G_max", "R_max", "d", "f", "M_cap")]
+
+
+class TempoNorm(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("T", "d", "kind", "stream_f32", "param_f32", "gate_f32")]
+                + [(n, ctypes.c_int64) for n in ("ld_y", "ld_r", "ld_r_out", "ld_x", "gate_row", "gate_col")]
+                + [(n, ctypes.c_float) for n in ("eps", "r_scale", "y_scale")])
 
 
 class TempoError(RuntimeError):
@@ -261,6 +270,117 @@ def tempo_grouped_ffn_bf16(shape, a_bf16, packed, inst_off, m_pad, h_bf16, y_bf1
                                        _ptr(h_bf16, torch.bfloat16), _ptr(y_bf16, torch.bfloat16),
                                        _ptr(status, torch.int32), _ptr(workspace, torch.uint8), _stream()),
            "tempo_grouped_ffn_bf16")
+
+
+# ---- norms around the block, the router, the layer for a few tokens ------------------------------
+
+_BF16_F32 = (torch.bfloat16, torch.float32)
+
+
+def _rows(t, what, T, d, dtypes):
+    """Pointer and row pitch of a [T, d] tensor whose rows are contiguous (the rows themselves may be strided)."""
+    if not t.is_cuda:
+        raise TempoError("expected a CUDA tensor (the library has no CPU path)")
+    if t.dtype not in dtypes:
+        raise TempoError(f"{what}: expected dtype {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.dim() != 2 or tuple(t.shape) != (T, d):
+        raise TempoError(f"{what}: expected shape ({T}, {d}), got {tuple(t.shape)}")
+    if d > 1 and t.stride(1) != 1:
+        raise TempoError(f"{what}: expected contiguous rows")
+    pitch = t.stride(0) if T > 1 else max(t.stride(0), d)
+    if pitch < d:
+        raise TempoError(f"{what}: rows overlap")
+    return ctypes.c_void_p(t.data_ptr()), pitch
+
+
+def _params(d, **tensors):
+    """Weights and biases [d] of one dtype, bf16 or f32 -> (pointers by name, is f32)."""
+    given = {n: t for n, t in tensors.items() if t is not None}
+    if len({t.dtype for t in given.values()}) > 1:
+        raise TempoError("weights and biases must have one dtype")
+    ptrs = {n: ctypes.c_void_p(0) for n in tensors}
+    f32 = False
+    for n, t in given.items():
+        if t.dtype not in _BF16_F32:
+            raise TempoError(f"{n}: expected dtype torch.bfloat16 or torch.float32, got {t.dtype}")
+        if tuple(t.shape) != (d,):
+            raise TempoError(f"{n}: expected shape ({d},), got {tuple(t.shape)}")
+        ptrs[n], f32 = _ptr(t), t.dtype == torch.float32
+    return ptrs, f32
+
+
+def tempo_norm_in(r, w, x_out, b=None, kind=NORM_RMS, eps=1e-6, n_valid=None):
+    """x_out = norm(r) * w + b, row by row.  r [T, d] bf16 or f32, x_out [T, d] bf16 (rows may be strided), w, b [d]."""
+    T, d = r.shape
+    ptrs, f32 = _params(d, w=w, b=b)
+    pr, ld_r = _rows(r, "r", T, d, _BF16_F32)
+    px, ld_x = _rows(x_out, "x_out", T, d, (torch.bfloat16,))
+    a = TempoNorm(T=T, d=d, kind=kind, stream_f32=r.dtype == torch.float32, param_f32=f32, ld_r=ld_r, ld_x=ld_x, eps=eps)
+    _check(_lib.tempo_norm_in(ctypes.byref(a), pr, ptrs["w"], ptrs["b"], _ptr(n_valid, torch.int32), px, _stream()),
+           "tempo_norm_in")
+
+
+def tempo_norm_out(y, r, r_out, post_w=None, post_b=None, gate=None, next_w=None, next_b=None, x_out=None, kind=NORM_RMS,
+                   eps=1e-6, r_scale=1.0, y_scale=1.0, n_valid=None):
+    """r_out = r_scale * r + y_scale * gate * (norm(y) * post_w + post_b);  x_out = norm(r_out) * next_w + next_b.
+
+    y, x_out bf16, r and r_out bf16 or f32, all [T, d] (rows may be strided; r_out may be r, x_out may be y); the gate
+    bf16 or f32 of any shape that broadcasts to [T, d]; weights and biases [d] of one dtype."""
+    T, d = r.shape
+    ptrs, f32 = _params(d, post_w=post_w, post_b=post_b, next_w=next_w, next_b=next_b)
+    py, ld_y = _rows(y, "y", T, d, (torch.bfloat16,))
+    pr, ld_r = _rows(r, "r", T, d, _BF16_F32)
+    po, ld_ro = _rows(r_out, "r_out", T, d, (r.dtype,))
+    px, ld_x = (ctypes.c_void_p(0), 0) if x_out is None else _rows(x_out, "x_out", T, d, (torch.bfloat16,))
+    a = TempoNorm(T=T, d=d, kind=kind, stream_f32=r.dtype == torch.float32, param_f32=f32, ld_y=ld_y, ld_r=ld_r,
+                  ld_r_out=ld_ro, ld_x=ld_x, eps=eps, r_scale=r_scale, y_scale=y_scale)
+    pg = ctypes.c_void_p(0)
+    if gate is not None:
+        if not gate.is_cuda:
+            raise TempoError("expected a CUDA tensor (the library has no CPU path)")
+        if gate.dtype not in _BF16_F32:
+            raise TempoError(f"gate: expected dtype torch.bfloat16 or torch.float32, got {gate.dtype}")
+        try:
+            full = gate.expand(T, d)
+        except RuntimeError:
+            raise TempoError(f"gate: shape {tuple(gate.shape)} does not broadcast to ({T}, {d})") from None
+        a.gate_row, a.gate_col = full.stride()
+        a.gate_f32 = gate.dtype == torch.float32
+        pg = ctypes.c_void_p(gate.data_ptr())
+    _check(_lib.tempo_norm_out(ctypes.byref(a), py, pr, ptrs["post_w"], ptrs["post_b"], pg, ptrs["next_w"], ptrs["next_b"],
+                               _ptr(n_valid, torch.int32), po, px, _stream()), "tempo_norm_out")
+
+
+def tempo_route(shape, x_bf16, w_router, bias, n_valid, topk_ids, topk_w, status, score=ROUTE_SOFTMAX, renormalise=True,
+                scale=1.0):
+    f32 = torch.float32
+    _check(_lib.tempo_route(ctypes.byref(shape), ctypes.c_int32(score), ctypes.c_int32(bool(renormalise)),
+                            ctypes.c_float(scale), _ptr(x_bf16, torch.bfloat16), _ptr(w_router, torch.bfloat16),
+                            _ptr(bias, f32), _ptr(n_valid, torch.int32), _ptr(topk_ids, torch.int32), _ptr(topk_w, f32),
+                            _ptr(status, torch.int32), _stream()), "tempo_route")
+
+
+def tempo_few_workspace_bytes(shape: TempoShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.tempo_few_workspace_bytes(ctypes.byref(shape), ctypes.byref(out)), "tempo_few_workspace_bytes")
+    return out.value
+
+
+def _few(fn, what, shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
+    i32, u8 = torch.int32, torch.uint8
+    _check(fn(ctypes.byref(shape), _ptr(x_bf16, torch.bfloat16), _ptr(topk_ids, i32), _ptr(topk_w, torch.float32),
+              _ptr(n_valid, i32), _ptr(replica_map, i32), _ptr(packed, u8), _ptr(out_bf16, torch.bfloat16),
+              _ptr(status, i32), _ptr(workspace, u8), _stream()), what)
+
+
+def tempo_few_ffn(shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
+    _few(_lib.tempo_few_ffn, "tempo_few_ffn", shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16,
+         status, workspace)
+
+
+def tempo_few_ffn_bf16(shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
+    _few(_lib.tempo_few_ffn_bf16, "tempo_few_ffn_bf16", shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed,
+         out_bf16, status, workspace)
 
 
 # ------------------------------------------------------------------------------------------------

@@ -154,6 +154,7 @@ const char* tempo_status_string(int code) {
     case TEMPO_ERR_SHAPE: return "a size is not positive or not a multiple of 128";
     case TEMPO_ERR_UNSUPPORTED: return "a size exceeds a documented limit";
     case TEMPO_ERR_CUDA: return "a CUDA call failed";
+    case TEMPO_ERR_ALIGN: return "a pointer is not aligned as its comment asks";
     default: return "unknown code";
   }
 }
@@ -443,6 +444,168 @@ int tempo_unpermute_combine(const tempo_shape* s, const void* y_bf16, const int3
   CombineParams p{s->T, s->k, s->d, static_cast<const __nv_bfloat16*>(y_bf16), pair_row, topk_w, n_valid,
                   static_cast<__nv_bfloat16*>(out_bf16)};
   return launch_combine(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+// ---- norms around the block ----------------------------------------------------------------------------
+static bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+static int check_norm(const tempo_norm* s) {
+  if (s == nullptr) return TEMPO_ERR_NULL;
+  if (s->T <= 0 || s->d <= 0) return TEMPO_ERR_SHAPE;
+  if (s->kind != TEMPO_NORM_RMS && s->kind != TEMPO_NORM_LAYER) return TEMPO_ERR_UNSUPPORTED;
+  if (s->d > 16384) return TEMPO_ERR_UNSUPPORTED;
+  return TEMPO_OK;
+}
+
+// The widest vector (elements) that the width, every pitch and every pointer of the launch allow.
+static int norm_vec(const NormParams& p) {
+  for (int vec = 8; vec > 1; vec /= 2) {
+    const size_t b16 = 2 * vec, f32 = vec >= 4 ? 16 : 4 * vec;
+    const size_t rs = p.stream_f32 ? f32 : b16, ps = p.param_f32 ? f32 : b16;
+    bool ok = p.d % vec == 0 && aligned(p.r, rs) && p.ld_r % vec == 0 && aligned(p.x, b16) && (!p.x || p.ld_x % vec == 0);
+    ok = ok && aligned(p.next_w, ps) && aligned(p.next_b, ps) && aligned(p.post_w, ps) && aligned(p.post_b, ps);
+    if (p.y != nullptr) ok = ok && aligned(p.y, b16) && p.ld_y % vec == 0 && aligned(p.r_out, rs) && p.ld_r_out % vec == 0;
+    if (ok) return vec;
+  }
+  return 1;
+}
+
+static int run_norm(NormParams& p, cudaStream_t stream) {
+  const int sms = sm_count();
+  if (sms <= 0) return TEMPO_ERR_CUDA;
+  const int vec = norm_vec(p);
+  const size_t gs = p.gate_f32 ? (vec >= 4 ? 16 : 4 * vec) : 2 * vec;
+  p.gate_vec = p.gate != nullptr && p.gate_col == 1 && p.gate_row % vec == 0 && aligned(p.gate, gs) ? 1 : 0;
+  return launch_norm(p, vec, sms, stream) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+int tempo_norm_in(const tempo_norm* s, const void* r, const void* w, const void* b, const int32_t* n_valid, void* x_bf16,
+                  void* stream) {
+  const int rc = check_norm(s);
+  if (rc != TEMPO_OK) return rc;
+  if (!r || !w || !x_bf16) return TEMPO_ERR_NULL;
+  if (s->ld_r < s->d || s->ld_x < s->d) return TEMPO_ERR_SHAPE;
+  if (!aligned(r, s->stream_f32 ? 4 : 2) || !aligned(w, s->param_f32 ? 4 : 2) || !aligned(b, s->param_f32 ? 4 : 2) ||
+      !aligned(x_bf16, 2))
+    return TEMPO_ERR_ALIGN;
+  NormParams p{};
+  p.T = s->T; p.d = s->d; p.layer = s->kind == TEMPO_NORM_LAYER;
+  p.stream_f32 = s->stream_f32; p.param_f32 = s->param_f32;
+  p.r = r; p.next_w = w; p.next_b = b; p.n_valid = n_valid;
+  p.x = static_cast<__nv_bfloat16*>(x_bf16);
+  p.ld_r = s->ld_r; p.ld_x = s->ld_x; p.eps = s->eps;
+  return run_norm(p, static_cast<cudaStream_t>(stream));
+}
+
+int tempo_norm_out(const tempo_norm* s, const void* y_bf16, const void* r, const void* post_w, const void* post_b,
+                   const void* gate, const void* next_w, const void* next_b, const int32_t* n_valid, void* r_out,
+                   void* x_bf16, void* stream) {
+  const int rc = check_norm(s);
+  if (rc != TEMPO_OK) return rc;
+  if (!y_bf16 || !r || !r_out || (x_bf16 && !next_w) || (post_b && !post_w)) return TEMPO_ERR_NULL;
+  if (s->ld_y < s->d || s->ld_r < s->d || s->ld_r_out < s->d || (x_bf16 && s->ld_x < s->d)) return TEMPO_ERR_SHAPE;
+  if (gate && (s->gate_row < 0 || s->gate_col < 0)) return TEMPO_ERR_SHAPE;
+  const size_t rs = s->stream_f32 ? 4 : 2, ps = s->param_f32 ? 4 : 2;
+  if (!aligned(y_bf16, 2) || !aligned(r, rs) || !aligned(r_out, rs) || !aligned(x_bf16, 2) || !aligned(post_w, ps) ||
+      !aligned(post_b, ps) || !aligned(next_w, ps) || !aligned(next_b, ps) || !aligned(gate, s->gate_f32 ? 4 : 2))
+    return TEMPO_ERR_ALIGN;
+  NormParams p{};
+  p.T = s->T; p.d = s->d; p.layer = s->kind == TEMPO_NORM_LAYER;
+  p.stream_f32 = s->stream_f32; p.param_f32 = s->param_f32; p.gate_f32 = s->gate_f32;
+  p.y = static_cast<const __nv_bfloat16*>(y_bf16);
+  p.r = r; p.post_w = post_w; p.post_b = post_b; p.gate = gate;
+  p.next_w = x_bf16 ? next_w : nullptr; p.next_b = x_bf16 ? next_b : nullptr; p.n_valid = n_valid;
+  p.r_out = r_out; p.x = static_cast<__nv_bfloat16*>(x_bf16);
+  p.ld_y = s->ld_y; p.ld_r = s->ld_r; p.ld_r_out = s->ld_r_out; p.ld_x = s->ld_x;
+  p.gate_row = s->gate_row; p.gate_col = s->gate_col;
+  p.eps = s->eps; p.r_scale = s->r_scale; p.y_scale = s->y_scale;
+  return run_norm(p, static_cast<cudaStream_t>(stream));
+}
+
+// ---- router ----------------------------------------------------------------------------------------------
+int tempo_route(const tempo_shape* s, int32_t score, int32_t renormalise, float scale, const void* x_bf16,
+                const void* w_router_bf16, const float* bias, const int32_t* n_valid, int32_t* topk_ids, float* topk_w,
+                uint32_t* status, void* stream) {
+  const int rc = check_shape(s);
+  if (rc != TEMPO_OK) return rc;
+  if (!x_bf16 || !w_router_bf16 || !topk_ids || !topk_w || !status) return TEMPO_ERR_NULL;
+  if (s->k > s->E) return TEMPO_ERR_SHAPE;
+  if (s->E > 512 || (score != TEMPO_ROUTE_SOFTMAX && score != TEMPO_ROUTE_SIGMOID)) return TEMPO_ERR_UNSUPPORTED;
+  if (!aligned(x_bf16, 16) || !aligned(w_router_bf16, 16) || !aligned(topk_ids, 4) || !aligned(topk_w, 4) || !aligned(bias, 4))
+    return TEMPO_ERR_ALIGN;
+  const int sms = sm_count();
+  if (sms <= 0) return TEMPO_ERR_CUDA;
+  const RoutePlan plan = route_plan(s->T, s->E, s->d, sms);
+  CUtensorMap tmX, tmW;      // bf16 matrices seen as bytes: 2d per row
+  if (!make_map(&tmX, x_bf16, s->T, 2ull * s->d, plan.x_box)) return TEMPO_ERR_CUDA;
+  if (!make_map(&tmW, w_router_bf16, s->E, 2ull * s->d, plan.w_box)) return TEMPO_ERR_CUDA;
+  RouteParams p{};
+  p.T = s->T; p.k = s->k; p.E = s->E; p.Kb = s->d / 64;
+  p.sigmoid = score == TEMPO_ROUTE_SIGMOID; p.renormalise = renormalise != 0; p.scale = scale;
+  p.bias = bias; p.n_valid = n_valid; p.ids = topk_ids; p.w = topk_w; p.status = status;
+  return launch_route(tmX, tmW, p, plan, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+// ---- the layer's experts for a few tokens ---------------------------------------------------------------
+static int check_few(const tempo_shape* s, int sms) {
+  const int rc = check_shape(s);
+  if (rc != TEMPO_OK) return rc;
+  if (s->T > kFewMaxT || s->T * s->k > kFewMaxPairs) return TEMPO_ERR_UNSUPPORTED;
+  // run arithmetic in 32 bits: (blocks of the larger product) * CTAs, bf16 blocks (64 values) being the more
+  const long long A = s->G_max < s->T * s->k ? s->G_max : s->T * s->k;
+  const long long b1 = A * (s->f / 128) * (s->d / 64), b2 = A * ((s->d + 255) / 256) * (s->f / 64);
+  if (((b1 > b2 ? b1 : b2) + 1) * sms > 0xffffffffll) return TEMPO_ERR_UNSUPPORTED;
+  return TEMPO_OK;
+}
+
+int tempo_few_workspace_bytes(const tempo_shape* s, size_t* bytes) {
+  if (bytes == nullptr) return TEMPO_ERR_NULL;
+  const int rc = check_few(s, kFewMaxSms);
+  if (rc != TEMPO_OK) return rc;
+  *bytes = few_layout(s->T, s->k, s->G_max, s->d, s->f, kFewMaxSms).total;
+  return TEMPO_OK;
+}
+
+static int run_few(bool bf16, const tempo_shape* s, const void* x, const int32_t* ids, const float* w, const int32_t* n_valid,
+                   const int32_t* replica_map, const void* packed, void* out, uint32_t* status, void* workspace, void* stream) {
+  const int rc = check_few(s, kFewMaxSms);
+  if (rc != TEMPO_OK) return rc;
+  if (!x || !ids || !w || !replica_map || !packed || !out || !status || !workspace) return TEMPO_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(packed, 256) || !aligned(out, 16) || !aligned(workspace, 256) || !aligned(ids, 4) ||
+      !aligned(w, 4) || !aligned(replica_map, 4))
+    return TEMPO_ERR_ALIGN;
+  const int sms = min(sm_count(), kFewMaxSms);
+  if (sms <= 0) return TEMPO_ERR_CUDA;
+  const PackLayout L = bf16 ? pack_layout_bf16(s->G_max, s->d, s->f) : pack_layout(s->G_max, s->d, s->f);
+  const FewLayout F = few_layout(s->T, s->k, s->G_max, s->d, s->f, kFewMaxSms);
+  const uint8_t* blob = static_cast<const uint8_t*>(packed);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const int kblock = bf16 ? 64 : 128;
+  FewParams p{};
+  p.T = s->T; p.k = s->k; p.E = s->E; p.R = s->R_max; p.G = s->G_max; p.d = s->d;
+  p.Kb1 = s->d / kblock; p.Kb2 = s->f / kblock; p.NT1 = L.NT1; p.NT2 = L.NT2; p.J1 = L.J1; p.J2 = L.J2;
+  p.ids = ids; p.w = w; p.n_valid = n_valid; p.replica_map = replica_map;
+  p.x = static_cast<const __nv_bfloat16*>(x);
+  p.w13 = blob + L.off_w13; p.w2 = blob + L.off_w2; p.sf13 = blob + L.off_sf13; p.sf2 = blob + L.off_sf2;
+  p.leave = reinterpret_cast<unsigned long long*>(ws + F.off_leave);
+  p.counters = reinterpret_cast<int32_t*>(ws + F.off_counters);
+  p.counter_ints = F.counter_ints;
+  p.x_img = ws + F.off_x; p.h_img = ws + F.off_h;
+  p.gu_part = reinterpret_cast<float*>(ws + F.off_gu); p.y_part = reinterpret_cast<float*>(ws + F.off_y);
+  p.out = static_cast<__nv_bfloat16*>(out); p.status = status; p.wait_ns = kDefaultWaitNs;
+  return launch_few(p, bf16, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+int tempo_few_ffn(const tempo_shape* s, const void* x_bf16, const int32_t* topk_ids, const float* topk_w,
+                  const int32_t* n_valid, const int32_t* replica_map, const void* packed, void* out_bf16, uint32_t* status,
+                  void* workspace, void* stream) {
+  return run_few(false, s, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace, stream);
+}
+
+int tempo_few_ffn_bf16(const tempo_shape* s, const void* x_bf16, const int32_t* topk_ids, const float* topk_w,
+                       const int32_t* n_valid, const int32_t* replica_map, const void* packed, void* out_bf16,
+                       uint32_t* status, void* workspace, void* stream) {
+  return run_few(true, s, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,684 @@
+// The experts of an MoE layer for a few tokens, one persistent kernel:
+//   out[t] = sum_s w[t,s] * W2_e (silu(Wg_e x_t) (.) (Wu_e x_t)),  e = ids[t,s], experts of this rank only.
+//
+// With a few tokens the layer is bound by the bytes of the chosen experts' weights (3 d f per expert), so everything
+// here serves one weight stream that starts early, never stops and is the same length on every SM:
+//   - The weights are the M side of the tensor-core product and the tokens the N side: a 32 KB tile of the packed blob
+//     (256 weight rows x 128 bytes of K, already in the shared-memory image) is the A operand of two M 128
+//     instructions, and N is the number of token columns, a multiple of 16.  No row of a tile is padding.
+//   - The blocks (tiles of 32 KB) of all chosen experts' gate/up matrices are dealt to the CTAs as equal contiguous
+//     runs, whatever expert or column block they belong to; a column block that spans CTAs is summed by the CTA that
+//     finishes it last, from 32-bit partials in the workspace, in the order of the runs.  The down matrices likewise.
+//   - A CTA's ring goes on with down weights while the other CTAs still finish H.
+//   - Activations are not rounded to 8 bits.  fp8 weights: a bf16 value has 8 significant bits, an e4m3 value 4, so
+//     x = 2^eps (q1 + q2 / 16) with two e4m3 terms is x itself for everything within 2^-13 of the block's largest value
+//     (and within 2^-22 of that value below), and each token takes two columns whose block scales differ by 2^4; the
+//     two sums are added in 32 bits.  H is split the same way: 8 bits like a bf16 rounding, with 0.4 of its mean error.
+//     bf16 weights: x as it is, H as two bf16 terms (16 bits).
+// A value of x or H that is not finite becomes a NaN code: its token's output is NaN, no other token's.
+//
+// Phases of a CTA (one per SM, 384 threads): warps 4-11 write their share of the x operand image to the workspace while
+// warps 0-3 build the expert lists; warp 0 streams weight tiles, warp 2 token tiles (they wait for the image, then for
+// H), warp 1 issues the MMAs, warps 4-11 drain the accumulators: gate/up partials or H, then down partials; at the end
+// the CTAs that worked on a 256-column block of the output share its weighted sum out among them.  Nothing is summed
+// with atomics, so results do not depend on timing.
+//
+// Counters in the workspace come in two sets: a launch counts in one and zeroes the other for the next launch; which
+// one is told by a launch count that every CTA bumps once as it leaves.  Every wait is bounded (FewParams::wait_ns).
+#include <cuda_fp16.h>
+
+#include "ffn_common.cuh"
+
+namespace tempo {
+
+constexpr int kFewThreads = 384;
+constexpr int kFewRing = 8;                 // most stages
+constexpr int kFewBudget = 222 * 1024;      // dynamic shared memory: ring, then the lists
+
+// ---- small helpers --------------------------------------------------------------------------------
+__device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+// Barrier of n threads that tells every one of them whether `ok` held in all.
+__device__ __forceinline__ bool bar_all(int id, int n, bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %3, 0;\n\t"
+      "barrier.cta.red.and.pred q, %1, %2, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"(id), "r"(n), "r"(ok ? 1u : 0u) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ bool few_poll(const int32_t* flag, int want, volatile int* abort_flag, unsigned long long limit_ns) {
+  unsigned long long t0 = 0;
+  for (uint32_t it = 0; ld_acquire(flag) < want; ++it) {
+    if ((it & 63u) == 63u) {
+      if (*abort_flag) return false;
+      const unsigned long long now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > limit_ns) { *abort_flag = 1; return false; }
+    }
+  }
+  return true;
+}
+
+// Run of CTA c when B blocks are dealt to C CTAs, and the CTA that block b falls to (products below 2^32, checked on
+// the host).
+__device__ __forceinline__ uint32_t run_begin(uint32_t c, uint32_t C, uint32_t B) { return c * B / C; }
+__device__ __forceinline__ uint32_t run_owner(uint32_t b, uint32_t C, uint32_t B) { return ((b + 1) * C - 1) / B; }
+
+struct FewSeg { int a, nt, kb0, kb1; uint32_t line; };
+// Segments of a CTA's run: the parts of lines (one expert's column block, Kb blocks long) that it covers.
+struct FewIter {
+  uint32_t b, e, Kb;
+  int inner, by_expert;                    // lines: a * inner + nt (gate/up) or nt * inner + a (down)
+  __device__ FewIter(uint32_t b_, uint32_t e_, uint32_t Kb_, int inner_, int by_expert_)
+      : b(b_), e(e_), Kb(Kb_), inner(inner_), by_expert(by_expert_) {}
+  __device__ bool next(FewSeg& s) {
+    if (b >= e) return false;
+    s.line = b / Kb;
+    s.kb0 = static_cast<int>(b - s.line * Kb);
+    const uint32_t n = min(Kb - s.kb0, e - b);
+    s.kb1 = s.kb0 + static_cast<int>(n);
+    const int q = static_cast<int>(s.line) / inner, r = static_cast<int>(s.line) % inner;
+    s.a = by_expert ? q : r;
+    s.nt = by_expert ? r : q;
+    b += n;
+    return true;
+  }
+};
+
+// Block exponent of the two-term split: 2^eps * 448 covers the block, and eps - 4 is still a valid scale.
+__device__ __forceinline__ int split_exponent(float amax) { return max(pow2_scale_exponent(amax), -122); }
+// (v, v') -> two e4m3 codes of the first and of the second term; a value that is not finite gives NaN codes.
+__device__ __forceinline__ void split_e4m3(float a, float b, float inv, uint32_t& q1, uint32_t& q2) {
+  a *= inv;
+  b *= inv;
+  q1 = cvt_e4m3x2(a, b);
+  uint32_t h;                                                   // the codes as two f16 values (exact)
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(q1)));
+  const __half2 hh = *reinterpret_cast<const __half2*>(&h);
+  q2 = cvt_e4m3x2((a - __low2float(hh)) * 16.f, (b - __high2float(hh)) * 16.f);
+  if (!isfinite(a)) { q1 |= 0x7fu; }
+  if (!isfinite(b)) { q1 |= 0x7f00u; }
+}
+
+__device__ __forceinline__ uint32_t few_idesc_fp8(int n, int sf_id) {     // weights: A (scale id = K-block % 4), tokens: B (id 0)
+  return (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(kTileM >> 4) << 24) |
+         (static_cast<uint32_t>(sf_id) << 29);
+}
+__device__ __forceinline__ uint32_t few_idesc_bf16(int n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
+}
+
+struct FewLists {                          // in dynamic shared memory behind the ring
+  unsigned long long* mask;                // [G]  tokens of each instance slot, bit t
+  uint16_t* act;                           // [A]  instance slot of the a-th active expert (ascending)
+  uint16_t* off;                           // [A+1] (token, expert) pairs before it
+  uint16_t* hrow;                          // [A]  operand rows of H before it
+  int16_t* s2a;                            // [G]  inverse of act
+  int16_t* pslot;                          // [T*k] slot of each pair, -1: none on this rank
+};
+__host__ __device__ inline size_t few_list_bytes(int G, int P) {
+  const int A = G < P ? G : P;
+  return static_cast<size_t>(G) * 8 + ((static_cast<size_t>(A) + 1) * 2 + 7) / 8 * 8 * 3 + (static_cast<size_t>(G) * 2 + 7) / 8 * 8 +
+         (static_cast<size_t>(P) * 2 + 7) / 8 * 8;
+}
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t s_full[kFewRing];
+  __shared__ __align__(8) uint64_t s_empty[kFewRing];
+  __shared__ __align__(8) uint64_t s_acc_full[2];
+  __shared__ __align__(8) uint64_t s_acc_empty[2];
+  __shared__ uint32_t s_tmem_base;
+  __shared__ int s_abort_storage, s_A, s_finish;
+  __shared__ uint32_t s_amax[2][2][4][8];  // [chunk parity][group][warp][token]
+  volatile int* s_abort = &s_abort_storage;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t C = gridDim.x, cta = blockIdx.x;
+  const int T = p.T, k = p.k, G = p.G, P = T * k, A_cap = min(G, P);
+  constexpr int kTerms = kBf16 ? 1 : 2;    // columns per token of the gate/up product
+  FewLists L;
+  {
+    uint8_t* q = smem_raw + (smem_base - smem_u32(smem_raw)) + p.stages * p.stage_bytes;
+    const size_t act_bytes = ((static_cast<size_t>(A_cap) + 1) * 2 + 7) / 8 * 8;
+    L.mask = reinterpret_cast<unsigned long long*>(q); q += static_cast<size_t>(G) * 8;
+    L.act = reinterpret_cast<uint16_t*>(q); q += act_bytes;
+    L.off = reinterpret_cast<uint16_t*>(q); q += act_bytes;
+    L.hrow = reinterpret_cast<uint16_t*>(q); q += act_bytes;
+    L.s2a = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(G) * 2 + 7) / 8 * 8;
+    L.pslot = reinterpret_cast<int16_t*>(q);
+  }
+  pdl_trigger();
+  // prologue that needs nothing from the previous kernel
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&s_full[s]), 2); mbar_init(smem_u32(&s_empty[s]), 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&s_acc_full[s]), 1); mbar_init(smem_u32(&s_acc_empty[s]), 8); }
+    s_abort_storage = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem_base)),
+                 "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  for (int i = tid; i < G; i += kFewThreads) L.mask[i] = 0ull;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = s_tmem_base;
+  pdl_wait();
+  int nv = T;
+  if (p.n_valid != nullptr) nv = max(0, min(*p.n_valid, T));
+  // launch count: every CTA of every earlier launch has bumped it, those of this one that have left as well
+  const unsigned long long launch = *reinterpret_cast<volatile const unsigned long long*>(p.leave) / C;
+  int32_t* cnt = p.counters + (launch & 1ull) * p.counter_ints;
+  int32_t* cnt_next = p.counters + ((launch & 1ull) ^ 1ull) * p.counter_ints;
+  int32_t *x_done = cnt, *h_done = cnt + 32, *y_cnt = cnt + 64, *line_cnt = cnt + 64 + p.NT2;
+  const int T8 = (T + 7) & ~7;
+  const int R1 = kBf16 ? (T + 15) & ~15 : 2 * T8;                   // operand rows of x: MMA columns of gate/up
+  const uint32_t x_block = R1 * 128 + (kBf16 ? 0 : 512);           // one K-block of the x image, scale atom behind it
+  const int units = p.Kb1 * nv;
+  const int x_want = min(static_cast<int>(C), (units + 7) / 8);
+
+  if (warp < 4) {
+    // ---- expert lists (128 threads) ----------------------------------------------------------------
+    bool bad = false;
+    for (int i = tid; i < P; i += 128) {
+      int slot = -1;
+      const int t = i / k;
+      if (t < nv) {
+        const int id = p.ids[i];
+        if (id >= 0 && id < p.E) {
+          for (int r = 0; r < p.R && slot < 0; ++r) {              // the first replica on this rank
+            const int v = p.replica_map[id * p.R + r];
+            if (v >= 0 && v < G) slot = v;
+          }
+        } else {
+          bad = true;
+        }
+      }
+      L.pslot[i] = static_cast<int16_t>(slot);
+      if (slot >= 0) atomicOr(&L.mask[slot], 1ull << t);           // the union of bits: no order
+    }
+    if (bad && cta == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_ID));
+    bar_sync(1, 128);
+    if (warp == 0) {
+      int a0 = 0, o0 = 0, h0 = 0;
+      for (int base = 0; base < G; base += 32) {
+        const int i = base + lane;
+        const int n = i < G ? __popcll(L.mask[i]) : 0;
+        const uint32_t on = __ballot_sync(0xffffffffu, n > 0);
+        if (on == 0) continue;
+        int po = n, ph = 2 * ((n + 7) & ~7);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int u = __shfl_up_sync(0xffffffffu, po, o), v = __shfl_up_sync(0xffffffffu, ph, o);
+          if (lane >= o) { po += u; ph += v; }
+        }
+        if (n > 0) {
+          const int a = a0 + __popc(on & ((1u << lane) - 1u));
+          L.act[a] = static_cast<uint16_t>(i);
+          L.off[a] = static_cast<uint16_t>(o0 + po - n);
+          L.hrow[a] = static_cast<uint16_t>(h0 + ph - 2 * ((n + 7) & ~7));
+          L.s2a[i] = static_cast<int16_t>(a);
+        }
+        a0 += __popc(on);
+        o0 += __shfl_sync(0xffffffffu, po, 31);
+        h0 += __shfl_sync(0xffffffffu, ph, 31);
+      }
+      if (lane == 0) { s_A = a0; L.off[a0] = static_cast<uint16_t>(o0); }
+    }
+    bar_sync(1, 128);
+    bar_arrive(2, kFewThreads);                                     // the lists, for the epilogue warps
+  } else {
+    // ---- this CTA's share of the x operand image: one (K-block, token) per warp and turn --------------
+    for (int u = static_cast<int>(cta) * 8 + warp - 4; u < units; u += static_cast<int>(C) * 8) {
+      const int kb = u / nv, t = u - kb * nv;
+      uint8_t* blk = p.x_img + static_cast<size_t>(kb) * x_block;
+      if constexpr (kBf16) {
+        const uint32_t v = *reinterpret_cast<const uint32_t*>(p.x + static_cast<size_t>(t) * p.d + kb * 64 + lane * 2);
+        *reinterpret_cast<uint32_t*>(blk + t * 128 + (((lane >> 2) ^ (t & 7)) << 4) + (lane & 3) * 4) = v;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(p.x + static_cast<size_t>(t) * p.d + kb * 128 + lane * 4);
+        uint32_t m = max(max(v.x & 0x7fffu, (v.x >> 16) & 0x7fffu), max(v.y & 0x7fffu, (v.y >> 16) & 0x7fffu));
+        m = __reduce_max_sync(0xffffffffu, m);                      // bits of a bf16 magnitude order like its value
+        const int eps = split_exponent(__uint_as_float(m << 16));
+        const float inv = pow2_neg(eps);
+        uint32_t a1, a2, b1, b2;
+        split_e4m3(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), inv, a1, a2);
+        split_e4m3(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u), inv, b1, b2);
+        const int r1 = t, r2 = T8 + t;
+        const int at = (lane >> 2), in = (lane & 3) * 4;
+        *reinterpret_cast<uint32_t*>(blk + r1 * 128 + ((at ^ (r1 & 7)) << 4) + in) = a1 | (b1 << 16);
+        *reinterpret_cast<uint32_t*>(blk + r2 * 128 + ((at ^ (r2 & 7)) << 4) + in) = a2 | (b2 << 16);
+        if (lane < 2) {                                             // scale byte: word of the row, byte 0
+          const int r = lane == 0 ? r1 : r2;
+          blk[R1 * 128 + (r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(eps + 127 - 4 * lane);
+        }
+      }
+    }
+    bar_sync(3, 256);
+    if (tid == 128 && static_cast<int>(cta) < x_want) {
+      __threadfence();
+      atomicAdd(x_done, 1);
+    }
+    for (int i = static_cast<int>(cta) * 256 + tid - 128; i < p.counter_ints; i += static_cast<int>(C) * 256) cnt_next[i] = 0;
+    bar_sync(2, kFewThreads);
+  }
+  const int A = s_A;
+  const uint32_t B1 = static_cast<uint32_t>(A) * p.NT1 * p.Kb1, B2 = static_cast<uint32_t>(A) * p.NT2 * p.Kb2;
+  // Down: at least a third of a line per CTA, so that a line's partial sums are at most kFewSplit (short phases only:
+  // those blocks are in the ring before H is complete anyway).
+  // Never more CTAs than blocks: every run has one.
+  const uint32_t C1 = max(1u, min(C, B1)), C2 = max(1u, min(min(C, B2), 3u * A * p.NT2));
+  const uint32_t g0 = cta < C1 ? run_begin(cta, C1, B1) : 0u, g1 = cta < C1 ? run_begin(cta + 1, C1, B1) : 0u;
+  const uint32_t d0 = cta < C2 ? run_begin(cta, C2, B2) : 0u, d1 = cta < C2 ? run_begin(cta + 1, C2, B2) : 0u;
+
+  if (warp == 0) {
+    // ---- weight producer ---------------------------------------------------------------------------
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      FewSeg s;
+      for (int ph = 0; ph < 2; ++ph) {
+        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
+        const int NT = ph == 0 ? p.NT1 : p.NT2, Kb = ph == 0 ? p.Kb1 : p.Kb2, J = ph == 0 ? p.J1 : p.J2;
+        const uint8_t* wt = ph == 0 ? p.w13 : p.w2;
+        const uint8_t* sf = ph == 0 ? p.sf13 : p.sf2;
+        while (ok && it.next(s)) {
+          const size_t tile = static_cast<size_t>(L.act[s.a]) * NT + s.nt;
+          const uint8_t* src = wt + tile * Kb * kBBytes;
+          const uint8_t* sf_src = sf + tile * J * kSfbBytes;
+#pragma unroll 1
+          for (int kb = s.kb0; kb < s.kb1; ++kb) {
+            if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+            const uint32_t full = smem_u32(&s_full[stage]), sA = smem_base + stage * p.stage_bytes;
+            const bool with_sf = !kBf16 && ((kb & 3) == 0 || kb == s.kb0);
+            mbar_arrive_expect_tx(full, kBBytes + (with_sf ? kSfbBytes : 0));
+            bulk_load_stream(sA, src + static_cast<size_t>(kb) * kBBytes, kBBytes, full);
+            if (with_sf) bulk_load(sA + kBBytes, sf_src + static_cast<size_t>(kb >> 2) * kSfbBytes, kSfbBytes, full);
+            if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    }
+  } else if (warp == 2) {
+    // ---- token producer: x image, then H image -------------------------------------------------------
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      FewSeg s;
+      for (int ph = 0; ph < 2; ++ph) {
+        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
+        if (it.b >= it.e) continue;
+        ok = ok && few_poll(ph == 0 ? x_done : h_done, ph == 0 ? x_want : A * p.NT1, s_abort, p.wait_ns);
+        asm volatile("fence.proxy.async;" ::: "memory");            // ordinary stores before the bulk copies below
+        while (ok && it.next(s)) {
+          uint32_t bytes = x_block;
+          const uint8_t* src = p.x_img;
+          if (ph == 1) {
+            const int rows = 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
+            bytes = rows * 128 + (kBf16 ? 0 : 512);
+            src = p.h_img + static_cast<size_t>(p.Kb2) * (static_cast<size_t>(L.hrow[s.a]) * 128 + (kBf16 ? 0 : 512) * static_cast<size_t>(s.a));
+          }
+#pragma unroll 1
+          for (int kb = s.kb0; kb < s.kb1; ++kb) {
+            if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+            const uint32_t full = smem_u32(&s_full[stage]);
+            mbar_arrive_expect_tx(full, bytes);
+            bulk_load(smem_base + stage * p.stage_bytes + kBBytes + kSfbBytes, src + static_cast<size_t>(kb) * bytes, bytes, full);
+            if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---- MMA issuer ------------------------------------------------------------------------------------
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0, n_seg = 0, n_sf = 0, n_blk = 0;
+      bool ok = true;
+      FewSeg s;
+      for (int ph = 0; ph < 2; ++ph) {
+        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
+        while (ok && it.next(s)) {
+          const int N = ph == 0 ? R1 : 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
+          const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+          ++n_seg;
+          if (!mbar_wait(smem_u32(&s_acc_empty[slot]), (use & 1u) ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t acc = tmem_base + slot * 128u;
+#pragma unroll 1
+          for (int kb = s.kb0; kb < s.kb1; ++kb) {
+            if (!mbar_wait(smem_u32(&s_full[stage]), phase, s_abort, p.wait_ns)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sA = smem_base + stage * p.stage_bytes, sSF = sA + kBBytes, sB = sSF + kSfbBytes;
+            const uint64_t da = smem_desc_sw128(sA), db = smem_desc_sw128(sB);
+            const uint32_t accumulate = kb > s.kb0 ? 1u : 0u;
+            if constexpr (kBf16) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                  tc_mma_bf16(acc + h * N, da + h * ((kTileM * 128) >> 4) + 2u * ks, db + 2u * ks, few_idesc_bf16(N),
+                              accumulate | (ks != 0 ? 1u : 0u));
+            } else {
+              if ((kb & 3) == 0 || kb == s.kb0) {
+                ++n_sf;
+                const uint32_t t = tmem_base + kSfCol0 + 8u * (n_sf & 1u);
+                tc_cp_sf(t, smem_desc_sf(sSF));
+                tc_cp_sf(t + 4, smem_desc_sf(sSF + 512));
+              }
+              ++n_blk;
+              const uint32_t sfa = tmem_base + kSfCol0 + 8u * (n_sf & 1u), sfb = tmem_base + kSfCol0 + 16u + 4u * (n_blk & 1u);
+              tc_cp_sf(sfb, smem_desc_sf(sB + N * 128));
+              const uint32_t idesc = few_idesc_fp8(N, kb & 3);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                  tc_mma_mxf8(acc + h * N, da + h * ((kTileM * 128) >> 4) + 2u * ks, db + 2u * ks, idesc, sfa + 4u * h, sfb,
+                              accumulate | (ks != 0 ? 1u : 0u));
+            }
+            tc_commit(smem_u32(&s_empty[stage]));
+            if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+          }
+          if (ok) tc_commit(smem_u32(&s_acc_full[slot]));
+        }
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- epilogue: two groups of four warps; a thread owns row `row` of both 128-row halves of a tile ------
+    const int g = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane, et = tid - 128;
+    const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
+    uint32_t n_seg = 0, par = 0;
+    bool ok = true;
+    FewSeg s;
+    FewIter it1(g0, g1, p.Kb1, p.NT1, 1);
+    while (ok && it1.next(s)) {
+      const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+      ++n_seg;
+      ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t acc = tmem_base + slot * 128u + lanes;
+      const unsigned long long mask = L.mask[L.act[s.a]];
+      const bool whole = s.kb0 == 0 && s.kb1 == p.Kb1;
+      if (!whole) {
+        // partial sums of both halves: [slot of the run][token][half][row]
+        float* dst = p.gu_part + (static_cast<size_t>(cta) * 2 + (s.kb0 > 0 ? 0 : 1)) * T * 256 + row;
+        for (int ch = g; ch * 8 < T; ch += 2) {
+          const uint32_t m8 = static_cast<uint32_t>(mask >> (8 * ch)) & 0xffu;
+          if (m8 == 0) continue;
+          uint32_t v[2][kTerms][8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < kTerms; ++j) tmem_ld8(acc + h * R1 + j * T8 + ch * 8, v[h][j]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (m8 >> i & 1u) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float f = __uint_as_float(v[h][0][i]);
+                if constexpr (kTerms == 2) f += __uint_as_float(v[h][1][i]);
+                __stcg(dst + (ch * 8 + i) * 256 + h * 128, f);
+              }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
+        bar_sync(3, 256);
+        if (et == 0) {
+          __threadfence();
+          const int n = s.kb1 - s.kb0;
+          const int before = atomicAdd(line_cnt + s.line, n);
+          __threadfence();
+          s_finish = before + n == p.Kb1 ? 1 : 0;
+        }
+        bar_sync(3, 256);
+        if (s_finish == 0) continue;                                // another CTA finishes this column block
+      }
+      // H of this (expert, 128-column block): SwiGLU, the two-term split, straight into the operand image
+      const uint32_t c_lo = run_owner(s.line * p.Kb1, C1, B1), c_hi = run_owner(s.line * p.Kb1 + p.Kb1 - 1, C1, B1);
+      const int n_col = L.off[s.a + 1] - L.off[s.a], C8 = (n_col + 7) & ~7;
+      uint8_t* himg = p.h_img + static_cast<size_t>(p.Kb2) * (static_cast<size_t>(L.hrow[s.a]) * 128 + (kBf16 ? 0 : 512) * static_cast<size_t>(s.a));
+      for (int ch = g; ch * 8 < T; ch += 2) {
+        const uint32_t m8 = static_cast<uint32_t>(mask >> (8 * ch)) & 0xffu;
+        if (m8 == 0) continue;
+        float gu[2][8];
+        if (whole) {
+          uint32_t v[2][kTerms][8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < kTerms; ++j) tmem_ld8(acc + h * R1 + j * T8 + ch * 8, v[h][j]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              gu[h][i] = __uint_as_float(v[h][0][i]);
+              if constexpr (kTerms == 2) gu[h][i] += __uint_as_float(v[h][1][i]);
+            }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gu[h][i] = 0.f;
+          for (uint32_t c = c_lo; c <= c_hi; ++c) {                 // in the order of the runs
+            const int part = run_begin(c, C1, B1) > s.line * p.Kb1 ? 0 : 1;
+            const float* src = p.gu_part + (static_cast<size_t>(c) * 2 + part) * T * 256 + row;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (m8 >> i & 1u) {
+                gu[0][i] += __ldcg(src + (ch * 8 + i) * 256);
+                gu[1][i] += __ldcg(src + (ch * 8 + i) * 256 + 128);
+              }
+          }
+        }
+        const int col0 = __popcll(mask & ((1ull << (8 * ch)) - 1ull));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gu[0][i] = __fdividef(gu[0][i], 1.f + __expf(-gu[0][i])) * gu[1][i];
+        if constexpr (kBf16) {
+          uint8_t* blk = himg + static_cast<size_t>(s.nt * 2 + (row >> 6)) * (2 * C8 * 128);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (m8 >> i & 1u) {
+              const int col = col0 + __popc(m8 & ((1u << i) - 1u)), r2 = C8 + col, ii = row & 63;
+              const __nv_bfloat16 hi = __float2bfloat16_rn(gu[0][i]);
+              const float hf = __bfloat162float(hi);
+              const __nv_bfloat16 lo = __float2bfloat16_rn(isfinite(hf) ? gu[0][i] - hf : 0.f);
+              *reinterpret_cast<__nv_bfloat16*>(blk + col * 128 + (((ii >> 3) ^ (col & 7)) << 4) + (ii & 7) * 2) = hi;
+              *reinterpret_cast<__nv_bfloat16*>(blk + r2 * 128 + (((ii >> 3) ^ (r2 & 7)) << 4) + (ii & 7) * 2) = lo;
+            }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(gu[0][i]) & 0x7fffffffu);
+            if (lane == i) s_amax[par][g][quad][i] = m;
+          }
+          bar_sync(4 + g, 128);
+          uint8_t* blk = himg + static_cast<size_t>(s.nt) * (2 * C8 * 128 + 512);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (m8 >> i & 1u) {
+              const uint32_t m = max(max(s_amax[par][g][0][i], s_amax[par][g][1][i]), max(s_amax[par][g][2][i], s_amax[par][g][3][i]));
+              const int eps = split_exponent(__uint_as_float(m));
+              uint32_t q1, q2;
+              split_e4m3(gu[0][i], 0.f, pow2_neg(eps), q1, q2);
+              const int col = col0 + __popc(m8 & ((1u << i) - 1u)), r2 = C8 + col;
+              blk[col * 128 + (((row >> 4) ^ (col & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q1);
+              blk[r2 * 128 + (((row >> 4) ^ (r2 & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q2);
+              if (row < 2) {
+                const int r = row == 0 ? col : r2;
+                blk[2 * C8 * 128 + (r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(eps + 127 - 4 * row);
+              }
+            }
+          par ^= 1u;
+        }
+      }
+      if (whole) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
+      }
+      bar_sync(3, 256);
+      if (et == 0) {
+        __threadfence();
+        atomicAdd(h_done, 1);
+      }
+    }
+    // ---- down: partial sums of (256 output columns, expert), one row of Y per (token, expert) pair -----------
+    FewIter it2(d0, d1, p.Kb2, A, 0);
+    int pend_nt = -1, pend = 0;                                     // blocks of column block pend_nt not yet published
+    while (ok && it2.next(s)) {
+      if (s.nt != pend_nt && pend > 0) {
+        bar_sync(3, 256);
+        if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
+        pend = 0;
+      }
+      const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+      ++n_seg;
+      ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
+      if (!ok) break;
+      tc_fence_after();
+      const int u0 = L.off[s.a], n_col = L.off[s.a + 1] - u0, C8 = (n_col + 7) & ~7;
+      const uint32_t acc = tmem_base + slot * 128u + lanes + g * (2 * C8);
+      const int j = static_cast<int>(cta - run_owner(s.line * p.Kb2, C2, B2));
+      const int n = s.nt * 256 + g * 128 + row;
+      float* dst = p.y_part + (static_cast<size_t>(j) * P + u0) * p.d + n;
+      for (int ch = 0; ch * 8 < n_col; ++ch) {
+        uint32_t v0[8], v1[8];
+        tmem_ld8(acc + ch * 8, v0);
+        tmem_ld8(acc + C8 + ch * 8, v1);
+        tmem_wait_ld();
+        if (n < p.d) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (ch * 8 + i < n_col)
+              __stcg(dst + static_cast<size_t>(ch * 8 + i) * p.d, __uint_as_float(v0[i]) + __uint_as_float(v1[i]));
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
+      pend_nt = s.nt;
+      pend += s.kb1 - s.kb0;
+    }
+    if (pend > 0) {
+      bar_sync(3, 256);
+      if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
+    }
+    // ---- weighted sums: the CTAs of a column block share its (token, 4 columns) items --------------------------
+    if (A == 0) {
+      uint4* out = reinterpret_cast<uint4*>(p.out);
+      for (size_t i = static_cast<size_t>(cta) * 256 + et; i < static_cast<size_t>(T) * p.d / 8; i += static_cast<size_t>(C) * 256)
+        out[i] = make_uint4(0, 0, 0, 0);
+    } else if (ok && d1 > d0) {
+      const uint32_t per_nt = static_cast<uint32_t>(A) * p.Kb2;
+      const int nt_lo = static_cast<int>(d0 / per_nt), nt_hi = static_cast<int>((d1 - 1) / per_nt);
+      for (int nt = nt_lo; ok && nt <= nt_hi; ++nt) {
+        bool seen = true;
+        if (et == 0) seen = few_poll(y_cnt + nt, static_cast<int>(per_nt), s_abort, p.wait_ns);
+        ok = bar_all(3, 256, seen);
+        if (!ok) break;
+        const uint32_t c_lo = run_owner(nt * per_nt, C2, B2), c_hi = run_owner((nt + 1) * per_nt - 1, C2, B2);
+        const int parts = static_cast<int>(c_hi - c_lo + 1);
+        for (int i = static_cast<int>(cta - c_lo) * 256 + et; i < T * 64; i += parts * 256) {
+          const int t = i >> 6, col = nt * 256 + (i & 63) * 4;
+          if (col >= p.d) continue;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (t < nv) {
+            for (int q = 0; q < k; ++q) {
+              const int sl = L.pslot[t * k + q];
+              if (sl < 0) continue;
+              const int a = L.s2a[sl];
+              const int u = L.off[a] + __popcll(L.mask[sl] & ((1ull << t) - 1ull));
+              const uint32_t b = (static_cast<uint32_t>(nt) * A + a) * p.Kb2;
+              const int splits = static_cast<int>(run_owner(b + p.Kb2 - 1, C2, B2) - run_owner(b, C2, B2)) + 1;
+              const float w = p.w[t * k + q];
+              float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+              for (int j = 0; j < splits; ++j) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(p.y_part + (static_cast<size_t>(j) * P + u) * p.d + col));
+                y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+              }
+              acc.x = fmaf(w, y.x, acc.x); acc.y = fmaf(w, y.y, acc.y); acc.z = fmaf(w, y.z, acc.z); acc.w = fmaf(w, y.w, acc.w);
+            }
+          }
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+          *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(t) * p.d + col) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+      }
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0) atomicAdd(p.leave, 1ull);
+  if (*s_abort) {
+    if (tid == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_TIMEOUT));
+    for (int i = 0; i < 50; ++i) __nanosleep(1000);      // let copies and MMAs in flight drain
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+static size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
+
+FewLayout few_layout(int T, int k, int G, int d, int f, int num_sms) {
+  FewLayout L;
+  const size_t P = static_cast<size_t>(T) * k, A = P < static_cast<size_t>(G) ? P : static_cast<size_t>(G);
+  const int NT1 = f / 128, NT2 = (d + 255) / 256;
+  // the widest of both weight types: rows of 128 bytes per K-block of 64 (bf16) or 128 (fp8) values
+  const size_t T16 = (static_cast<size_t>(T) + 15) / 16 * 16;
+  L.counter_ints = 64 + NT2 + G * NT1;
+  L.off_leave = 0;
+  L.off_counters = 256;
+  L.off_x = align256(L.off_counters + 2 * sizeof(int32_t) * static_cast<size_t>(L.counter_ints));
+  L.off_h = align256(L.off_x + static_cast<size_t>(d / 64) * T16 * 128 + static_cast<size_t>(d / 128) * 512);
+  const size_t h_rows = 2 * (P + 7 * A);                 // every expert's columns rounded up to 8, two terms
+  L.off_gu = align256(L.off_h + static_cast<size_t>(f / 64) * (h_rows * 128 + 512 * A));
+  L.off_y = align256(L.off_gu + static_cast<size_t>(num_sms) * 2 * T * 256 * 4);
+  L.total = align256(L.off_y + static_cast<size_t>(kFewSplit) * P * d * 4);
+  return L;
+}
+
+template <bool kBf16>
+static cudaError_t launch_few_t(FewParams p, int num_sms, cudaStream_t stream) {
+  static std::atomic<unsigned long long> smem_set{0};
+  const int T8 = (p.T + 7) & ~7, T16 = (p.T + 15) & ~15;
+  // columns: gate/up R1 (all tokens), down twice the tokens of an expert rounded up to 8
+  const int rows = kBf16 ? max(T16, 2 * T8) : 2 * T8;
+  p.stage_bytes = (kBBytes + kSfbBytes + rows * 128 + 512 + 1023) / 1024 * 1024;
+  p.slots = rows <= 64 ? 2 : 1;
+  const size_t lists = few_list_bytes(p.G, p.T * p.k);
+  p.stages = min(kFewRing, static_cast<int>((kFewBudget - 1024 - lists) / p.stage_bytes));
+  const size_t smem = 1024 + static_cast<size_t>(p.stages) * p.stage_bytes + lists;
+  cudaError_t e = smem_limit_once(few_kernel<kBf16>, kFewBudget, smem_set);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(few_kernel<kBf16>, dim3(num_sms), dim3(kFewThreads), smem, stream, p);
+}
+
+cudaError_t launch_few(const FewParams& p, bool bf16, int num_sms, cudaStream_t stream) {
+  return bf16 ? launch_few_t<true>(p, num_sms, stream) : launch_few_t<false>(p, num_sms, stream);
+}
+
+}  // namespace tempo

@@ -137,5 +137,74 @@ cudaError_t launch_ffn(const CUtensorMap& tmA1, const CUtensorMap& tmA2, const C
 cudaError_t launch_ffn_gather(const CUtensorMap& tmA2, const CUtensorMap& tmY, const FfnParams& p, int num_sms,
                               cudaStream_t stream);
 
+// ---- around the block, and the layer for a few tokens -------------------------------------------------
+struct NormParams {
+  int T, d, layer;           // layer: subtract the row's mean
+  int stream_f32, param_f32, gate_f32, gate_vec;   // gate_vec: the gate's row can be read with the row's vectors
+  const __nv_bfloat16* y;    // NULL: the norm before a block
+  const void* r;
+  const void* post_w;
+  const void* post_b;
+  const void* gate;
+  const void* next_w;
+  const void* next_b;
+  const int32_t* n_valid;
+  void* r_out;
+  __nv_bfloat16* x;
+  size_t ld_y, ld_r, ld_r_out, ld_x, gate_row, gate_col;
+  float eps, r_scale, y_scale;
+};
+cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream);
+
+struct RoutePlan {
+  int E16, tile_rows, x_box, w_box, w_boxes, stage_bytes, stages, splits, ctas;
+};
+struct RouteParams {
+  int T, k, E, Kb;           // Kb = d / 64
+  int sigmoid, renormalise;
+  float scale;
+  const float* bias;
+  const int32_t* n_valid;
+  int32_t* ids;
+  float* w;
+  uint32_t* status;
+  int E16, tile_rows, x_box, w_box, w_boxes, stage_bytes, stages, splits, tmem_cols;   // from the plan
+};
+RoutePlan route_plan(int T, int E, int d, int num_sms);
+cudaError_t launch_route(const CUtensorMap& tmX, const CUtensorMap& tmW, RouteParams p, const RoutePlan& r, cudaStream_t stream);
+
+constexpr int kFewMaxT = 64, kFewMaxPairs = 1024;
+constexpr int kFewMaxSms = 160;      // the workspace is sized for so many CTAs, whatever the device
+constexpr int kFewSplit = 4;         // most partial sums of a (256 output columns, expert) line of the down product
+struct FewLayout {
+  int counter_ints;                  // of one of the two counter sets
+  size_t off_leave, off_counters, off_x, off_h, off_gu, off_y, total;
+};
+struct FewParams {
+  int T, k, E, R, G, d;
+  int Kb1, Kb2, NT1, NT2, J1, J2;    // K-blocks, column blocks and scale atoms of the gate/up and the down product
+  const int32_t* ids;
+  const float* w;
+  const int32_t* n_valid;
+  const int32_t* replica_map;
+  const __nv_bfloat16* x;
+  const uint8_t* w13;
+  const uint8_t* w2;
+  const uint8_t* sf13;
+  const uint8_t* sf2;
+  unsigned long long* leave;
+  int32_t* counters;
+  int counter_ints;
+  uint8_t* x_img;
+  uint8_t* h_img;
+  float* gu_part;
+  float* y_part;
+  __nv_bfloat16* out;
+  uint32_t* status;
+  unsigned long long wait_ns;
+  int stages, stage_bytes, slots;    // set by the launcher
+};
+FewLayout few_layout(int T, int k, int G, int d, int f, int num_sms);
+cudaError_t launch_few(const FewParams& p, bool bf16, int num_sms, cudaStream_t stream);
 
 }  // namespace tempo
