@@ -34,6 +34,10 @@ namespace tempo {
 constexpr int kFewThreads = 384;
 constexpr int kFewRing = 8;                 // most stages
 constexpr int kFewBudget = 222 * 1024;      // dynamic shared memory: ring, then the lists
+constexpr uint32_t kFewFlight = 3;     // weight tiles of a CTA on their way at a time
+constexpr int kFewRun = 8;                  // fewest blocks of a gate/up line that are worth a CTA of their own
+constexpr int kFewBatch = 4;                // token columns that an epilogue group takes at a time
+constexpr int kFewHalf = 8;                 // fewest gate/up blocks per CTA of a half
 
 // ---- small helpers --------------------------------------------------------------------------------
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
@@ -49,10 +53,12 @@ __device__ __forceinline__ bool bar_all(int id, int n, bool ok) {
       : "=r"(r) : "r"(id), "r"(n), "r"(ok ? 1u : 0u) : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr) : "memory");
+__device__ __forceinline__ void tmem_ld1(uint32_t taddr, uint32_t& r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ bool few_poll(const int32_t* flag, int want, volatile int* abort_flag, unsigned long long limit_ns) {
   unsigned long long t0 = 0;
@@ -72,23 +78,60 @@ __device__ __forceinline__ bool few_poll(const int32_t* flag, int want, volatile
 __device__ __forceinline__ uint32_t run_begin(uint32_t c, uint32_t C, uint32_t B) { return c * B / C; }
 __device__ __forceinline__ uint32_t run_owner(uint32_t b, uint32_t C, uint32_t B) { return ((b + 1) * C - 1) / B; }
 
-struct FewSeg { int a, nt, kb0, kb1; uint32_t line; };
-// Segments of a CTA's run: the parts of lines (one expert's column block, Kb blocks long) that it covers.
+// One of the four phases of a launch: gate/up of the first half of the active experts, of the second half, then down of
+// the first and of the second.  While a half's H is being summed and published the other half's weights stream.
+struct FewPhase {
+  int a0, an;                              // its active experts
+  uint32_t B, C;                           // blocks, CTAs that they are dealt to
+  uint32_t b, e;                           // this CTA's run
+  int line, kb0, q, r;                     // where the run begins: line, K-block in it, line / inner, line % inner
+};
+__device__ __forceinline__ void few_phase(FewPhase& f, const FewParams& p, int ph, int A, uint32_t ctas, uint32_t cta) {
+  // two halves where each of them keeps every CTA busy
+  const int A1 = static_cast<uint32_t>(A) * p.NT1 * p.Kb1 >= 2u * kFewHalf * ctas && A >= 2 ? (A + 1) / 2 : A;
+  f.a0 = (ph & 1) ? A1 : 0;
+  f.an = (ph & 1) ? A - A1 : A1;
+  const bool down = ph >= 2;
+  const uint32_t Kb = down ? p.Kb2 : p.Kb1, inner = down ? f.an : p.NT1;
+  const uint32_t lines = static_cast<uint32_t>(f.an) * (down ? p.NT2 : p.NT1);
+  f.B = lines * Kb;
+  // Short phases are dealt to fewer CTAs.  Gate/up: a line is cut only into runs of kFewRun blocks or more (a cut costs
+  // an exchange of partial sums).  Down: into at most kFewSplit partial sums, i.e. a third of a line per CTA.
+  f.C = down ? 3u * lines : max(lines, f.B / kFewRun);
+  f.C = max(1u, min(f.C, min(ctas, f.B)));
+  f.b = cta < f.C ? run_begin(cta, f.C, f.B) : 0u;
+  f.e = cta < f.C ? run_begin(cta + 1, f.C, f.B) : 0u;
+  f.line = f.kb0 = f.q = f.r = 0;
+  if (f.e > f.b) {
+    f.line = static_cast<int>(f.b / Kb);
+    f.kb0 = static_cast<int>(f.b - f.line * Kb);
+    f.q = f.line / static_cast<int>(inner);
+    f.r = f.line % static_cast<int>(inner);
+  }
+}
+// Segments of a CTA's run: the parts of lines (one expert's column block, Kb blocks long) that it covers.  Lines are
+// a * NT1 + nt (gate/up) or nt * an + a (down), a counted within the phase.
 struct FewIter {
-  uint32_t b, e, Kb;
-  int inner, by_expert;                    // lines: a * inner + nt (gate/up) or nt * inner + a (down)
-  __device__ FewIter(uint32_t b_, uint32_t e_, uint32_t Kb_, int inner_, int by_expert_)
-      : b(b_), e(e_), Kb(Kb_), inner(inner_), by_expert(by_expert_) {}
-  __device__ bool next(FewSeg& s) {
-    if (b >= e) return false;
-    s.line = b / Kb;
-    s.kb0 = static_cast<int>(b - s.line * Kb);
-    const uint32_t n = min(Kb - s.kb0, e - b);
-    s.kb1 = s.kb0 + static_cast<int>(n);
-    const int q = static_cast<int>(s.line) / inner, r = static_cast<int>(s.line) % inner;
-    s.a = by_expert ? q : r;
-    s.nt = by_expert ? r : q;
-    b += n;
+  int left, Kb, inner, a0, q, r;
+  bool down;
+  int a, nt, kb0, kb1, line;               // the segment
+  __device__ FewIter(const FewParams& p, const FewPhase& f, bool down_) {
+    down = down_;
+    left = static_cast<int>(f.e - f.b);
+    Kb = down ? p.Kb2 : p.Kb1;
+    inner = down ? f.an : p.NT1;
+    a0 = f.a0; q = f.q; r = f.r - 1; line = f.line - 1;
+    kb1 = f.kb0;
+  }
+  __device__ bool next() {
+    if (left <= 0) return false;
+    kb0 = kb1 == Kb ? 0 : kb1;             // only the run's first segment may begin inside its line
+    kb1 = min(Kb, kb0 + left);
+    left -= kb1 - kb0;
+    ++line;
+    if (++r == inner) { r = 0; ++q; }
+    a = a0 + (down ? r : q);
+    nt = down ? q : r;
     return true;
   }
 };
@@ -122,24 +165,30 @@ struct FewLists {                          // in dynamic shared memory behind th
   uint16_t* off;                           // [A+1] (token, expert) pairs before it
   uint16_t* hrow;                          // [A]  operand rows of H before it
   int16_t* s2a;                            // [G]  inverse of act
-  int16_t* pslot;                          // [T*k] slot of each pair, -1: none on this rank
+  int16_t* pa;                             // [T*k] active expert of each pair (first its slot), -1: none on this rank
+  int16_t* pu;                             // [T*k] its row of the down partials
+  uint8_t* tok;                            // [T*k] token of each row of the down partials (by expert, then token)
+  float* w;                                // [T*k] routing weights
+  uint8_t* split;                          // [2][A] partial sums per expert of the column block being reduced
 };
 __host__ __device__ inline size_t few_list_bytes(int G, int P) {
-  const int A = G < P ? G : P;
-  return static_cast<size_t>(G) * 8 + ((static_cast<size_t>(A) + 1) * 2 + 7) / 8 * 8 * 3 + (static_cast<size_t>(G) * 2 + 7) / 8 * 8 +
-         (static_cast<size_t>(P) * 2 + 7) / 8 * 8;
+  const size_t A = G < P ? G : P;
+  return static_cast<size_t>(G) * 8 + (2 * (A + 1) + 7) / 8 * 8 * 3 + (2 * static_cast<size_t>(G) + 7) / 8 * 8 +
+         (2 * static_cast<size_t>(P) + 7) / 8 * 8 * 2 + (4 * static_cast<size_t>(P) + 7) / 8 * 8 + (static_cast<size_t>(P) + 7) / 8 * 8 + (2 * A + 7) / 8 * 8;
 }
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_full[kFewRing];
+  __shared__ __align__(8) uint64_t s_full[kFewRing];      // weight tile landed
+  __shared__ __align__(8) uint64_t s_tok[kFewRing];       // token tile landed
   __shared__ __align__(8) uint64_t s_empty[kFewRing];
   __shared__ __align__(8) uint64_t s_acc_full[2];
   __shared__ __align__(8) uint64_t s_acc_empty[2];
   __shared__ uint32_t s_tmem_base;
-  __shared__ int s_abort_storage, s_A, s_finish;
-  __shared__ uint32_t s_amax[2][2][4][8];  // [chunk parity][group][warp][token]
+  __shared__ int s_abort_storage, s_A;
+  __shared__ FewPhase s_phase[4];
+  __shared__ uint32_t s_amax[2][2][4][kFewBatch];  // [batch parity][group][warp][token]
   volatile int* s_abort = &s_abort_storage;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -156,12 +205,20 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     L.off = reinterpret_cast<uint16_t*>(q); q += act_bytes;
     L.hrow = reinterpret_cast<uint16_t*>(q); q += act_bytes;
     L.s2a = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(G) * 2 + 7) / 8 * 8;
-    L.pslot = reinterpret_cast<int16_t*>(q);
+    L.pa = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(P) * 2 + 7) / 8 * 8;
+    L.pu = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(P) * 2 + 7) / 8 * 8;
+    L.w = reinterpret_cast<float*>(q); q += (static_cast<size_t>(P) * 4 + 7) / 8 * 8;
+    L.tok = q; q += (static_cast<size_t>(P) + 7) / 8 * 8;
+    L.split = q;
   }
   pdl_trigger();
   // prologue that needs nothing from the previous kernel
   if (tid == 0) {
-    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&s_full[s]), 2); mbar_init(smem_u32(&s_empty[s]), 1); }
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(smem_u32(&s_full[s]), 1);
+      mbar_init(smem_u32(&s_tok[s]), 1);
+      mbar_init(smem_u32(&s_empty[s]), 1);
+    }
     for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&s_acc_full[s]), 1); mbar_init(smem_u32(&s_acc_empty[s]), 8); }
     s_abort_storage = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -183,7 +240,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
   const unsigned long long launch = *reinterpret_cast<volatile const unsigned long long*>(p.leave) / C;
   int32_t* cnt = p.counters + (launch & 1ull) * p.counter_ints;
   int32_t* cnt_next = p.counters + ((launch & 1ull) ^ 1ull) * p.counter_ints;
-  int32_t *x_done = cnt, *h_done = cnt + 32, *y_cnt = cnt + 64, *line_cnt = cnt + 64 + p.NT2;
+  // h_done: 32 ints per half; part_done: [half][CTA], the partial sums of that CTA's first segment are in the workspace
+  int32_t *x_done = cnt, *h_done = cnt + 32, *y_cnt = cnt + 96, *part_done = cnt + 96 + p.NT2;
   const int T8 = (T + 7) & ~7;
   const int R1 = kBf16 ? (T + 15) & ~15 : 2 * T8;                   // operand rows of x: MMA columns of gate/up
   const uint32_t x_block = R1 * 128 + (kBf16 ? 0 : 512);           // one K-block of the x image, scale atom behind it
@@ -193,22 +251,36 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
   if (warp < 4) {
     // ---- expert lists (128 threads) ----------------------------------------------------------------
     bool bad = false;
-    for (int i = tid; i < P; i += 128) {
-      int slot = -1;
-      const int t = i / k;
-      if (t < nv) {
-        const int id = p.ids[i];
-        if (id >= 0 && id < p.E) {
-          for (int r = 0; r < p.R && slot < 0; ++r) {              // the first replica on this rank
-            const int v = p.replica_map[id * p.R + r];
-            if (v >= 0 && v < G) slot = v;
-          }
-        } else {
-          bad = true;
-        }
+    for (int i0 = tid; i0 < P; i0 += 512) {                          // four pairs per thread: their loads overlap
+      int id[4], slot[4];
+      float w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + 128 * j;
+        const bool live = i < nv * k;
+        id[j] = live ? p.ids[i] : 0;
+        w[j] = live ? p.w[i] : 0.f;
       }
-      L.pslot[i] = static_cast<int16_t>(slot);
-      if (slot >= 0) atomicOr(&L.mask[slot], 1ull << t);           // the union of bits: no order
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool live = i0 + 128 * j < nv * k, good = id[j] >= 0 && id[j] < p.E;
+        bad |= live && !good;
+        slot[j] = live && good ? p.replica_map[id[j] * p.R] : -1;
+        id[j] = live && good ? id[j] : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + 128 * j;
+        if (i >= P) break;
+        int v = slot[j] < G ? slot[j] : -1;
+        for (int r = 1; r < p.R && v < 0 && id[j] >= 0; ++r) {       // the first replica on this rank
+          const int u = p.replica_map[id[j] * p.R + r];
+          if (u < G) v = u;
+        }
+        L.pa[i] = static_cast<int16_t>(v < 0 ? -1 : v);
+        L.w[i] = w[j];
+        if (v >= 0) atomicOr(&L.mask[v], 1ull << (i / k));           // the union of bits: no order
+      }
     }
     if (bad && cta == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_ID));
     bar_sync(1, 128);
@@ -237,6 +309,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
         h0 += __shfl_sync(0xffffffffu, ph, 31);
       }
       if (lane == 0) { s_A = a0; L.off[a0] = static_cast<uint16_t>(o0); }
+      if (lane < 4) few_phase(s_phase[lane], p, lane, a0, C, cta);
     }
     bar_sync(1, 128);
     bar_arrive(2, kFewThreads);                                     // the lists, for the epilogue warps
@@ -276,32 +349,31 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     bar_sync(2, kFewThreads);
   }
   const int A = s_A;
-  const uint32_t B1 = static_cast<uint32_t>(A) * p.NT1 * p.Kb1, B2 = static_cast<uint32_t>(A) * p.NT2 * p.Kb2;
-  // Down: at least a third of a line per CTA, so that a line's partial sums are at most kFewSplit (short phases only:
-  // those blocks are in the ring before H is complete anyway).
-  // Never more CTAs than blocks: every run has one.
-  const uint32_t C1 = max(1u, min(C, B1)), C2 = max(1u, min(min(C, B2), 3u * A * p.NT2));
-  const uint32_t g0 = cta < C1 ? run_begin(cta, C1, B1) : 0u, g1 = cta < C1 ? run_begin(cta + 1, C1, B1) : 0u;
-  const uint32_t d0 = cta < C2 ? run_begin(cta, C2, B2) : 0u, d1 = cta < C2 ? run_begin(cta + 1, C2, B2) : 0u;
 
   if (warp == 0) {
     // ---- weight producer ---------------------------------------------------------------------------
     if (lane == 0) {
       uint32_t stage = 0, phase = 0;
+      uint32_t old_stage = 0, old_phase = 0, issued = 0;            // the block kFewFlight before the next one
       bool ok = true;
-      FewSeg s;
-      for (int ph = 0; ph < 2; ++ph) {
-        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
-        const int NT = ph == 0 ? p.NT1 : p.NT2, Kb = ph == 0 ? p.Kb1 : p.Kb2, J = ph == 0 ? p.J1 : p.J2;
-        const uint8_t* wt = ph == 0 ? p.w13 : p.w2;
-        const uint8_t* sf = ph == 0 ? p.sf13 : p.sf2;
-        while (ok && it.next(s)) {
+#pragma unroll 1
+      for (int ph = 0; ph < 4; ++ph) {
+        const bool down = ph >= 2;
+        FewIter s(p, s_phase[ph], down);
+        const int NT = down ? p.NT2 : p.NT1, Kb = down ? p.Kb2 : p.Kb1, J = down ? p.J2 : p.J1;
+        const uint8_t* wt = down ? p.w2 : p.w13;
+        const uint8_t* sf = down ? p.sf2 : p.sf13;
+        while (ok && s.next()) {
           const size_t tile = static_cast<size_t>(L.act[s.a]) * NT + s.nt;
           const uint8_t* src = wt + tile * Kb * kBBytes;
           const uint8_t* sf_src = sf + tile * J * kSfbBytes;
 #pragma unroll 1
           for (int kb = s.kb0; kb < s.kb1; ++kb) {
             if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+            if (issued++ >= kFewFlight) {
+              if (!mbar_wait(smem_u32(&s_full[old_stage]), old_phase, s_abort, p.wait_ns)) { ok = false; break; }
+              if (++old_stage == static_cast<uint32_t>(p.stages)) { old_stage = 0; old_phase ^= 1u; }
+            }
             const uint32_t full = smem_u32(&s_full[stage]), sA = smem_base + stage * p.stage_bytes;
             const bool with_sf = !kBf16 && ((kb & 3) == 0 || kb == s.kb0);
             mbar_arrive_expect_tx(full, kBBytes + (with_sf ? kSfbBytes : 0));
@@ -317,16 +389,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     if (lane == 0) {
       uint32_t stage = 0, phase = 0;
       bool ok = true;
-      FewSeg s;
-      for (int ph = 0; ph < 2; ++ph) {
-        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
-        if (it.b >= it.e) continue;
-        ok = ok && few_poll(ph == 0 ? x_done : h_done, ph == 0 ? x_want : A * p.NT1, s_abort, p.wait_ns);
+#pragma unroll 1
+      for (int ph = 0; ph < 4; ++ph) {
+        FewIter s(p, s_phase[ph], ph >= 2);
+        if (s.left <= 0) continue;
+        ok = ok && few_poll(ph < 2 ? x_done : h_done + 32 * (ph - 2), ph < 2 ? x_want : s_phase[ph].an * p.NT1, s_abort, p.wait_ns);
         asm volatile("fence.proxy.async;" ::: "memory");            // ordinary stores before the bulk copies below
-        while (ok && it.next(s)) {
+        while (ok && s.next()) {
           uint32_t bytes = x_block;
           const uint8_t* src = p.x_img;
-          if (ph == 1) {
+          if (ph >= 2) {
             const int rows = 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
             bytes = rows * 128 + (kBf16 ? 0 : 512);
             src = p.h_img + static_cast<size_t>(p.Kb2) * (static_cast<size_t>(L.hrow[s.a]) * 128 + (kBf16 ? 0 : 512) * static_cast<size_t>(s.a));
@@ -334,7 +406,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
 #pragma unroll 1
           for (int kb = s.kb0; kb < s.kb1; ++kb) {
             if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
-            const uint32_t full = smem_u32(&s_full[stage]);
+            const uint32_t full = smem_u32(&s_tok[stage]);
             mbar_arrive_expect_tx(full, bytes);
             bulk_load(smem_base + stage * p.stage_bytes + kBBytes + kSfbBytes, src + static_cast<size_t>(kb) * bytes, bytes, full);
             if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
@@ -347,11 +419,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     if (lane == 0) {
       uint32_t stage = 0, phase = 0, n_seg = 0, n_sf = 0, n_blk = 0;
       bool ok = true;
-      FewSeg s;
-      for (int ph = 0; ph < 2; ++ph) {
-        FewIter it(ph == 0 ? g0 : d0, ph == 0 ? g1 : d1, ph == 0 ? p.Kb1 : p.Kb2, ph == 0 ? p.NT1 : A, ph == 0);
-        while (ok && it.next(s)) {
-          const int N = ph == 0 ? R1 : 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
+#pragma unroll 1
+      for (int ph = 0; ph < 4; ++ph) {
+        FewIter s(p, s_phase[ph], ph >= 2);
+        while (ok && s.next()) {
+          const int N = ph < 2 ? R1 : 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
           const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
           ++n_seg;
           if (!mbar_wait(smem_u32(&s_acc_empty[slot]), (use & 1u) ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
@@ -359,7 +431,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
           const uint32_t acc = tmem_base + slot * 128u;
 #pragma unroll 1
           for (int kb = s.kb0; kb < s.kb1; ++kb) {
-            if (!mbar_wait(smem_u32(&s_full[stage]), phase, s_abort, p.wait_ns)) { ok = false; break; }
+            if (!mbar_wait(smem_u32(&s_full[stage]), phase, s_abort, p.wait_ns) ||
+                !mbar_wait(smem_u32(&s_tok[stage]), phase, s_abort, p.wait_ns)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sA = smem_base + stage * p.stage_bytes, sSF = sA + kBBytes, sB = sSF + kSfbBytes;
             const uint64_t da = smem_desc_sw128(sA), db = smem_desc_sw128(sB);
@@ -402,180 +475,167 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
     uint32_t n_seg = 0, par = 0;
     bool ok = true;
-    FewSeg s;
-    FewIter it1(g0, g1, p.Kb1, p.NT1, 1);
-    while (ok && it1.next(s)) {
-      const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
-      ++n_seg;
-      ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t acc = tmem_base + slot * 128u + lanes;
-      const unsigned long long mask = L.mask[L.act[s.a]];
-      const bool whole = s.kb0 == 0 && s.kb1 == p.Kb1;
-      if (!whole) {
-        // partial sums of both halves: [slot of the run][token][half][row]
-        float* dst = p.gu_part + (static_cast<size_t>(cta) * 2 + (s.kb0 > 0 ? 0 : 1)) * T * 256 + row;
-        for (int ch = g; ch * 8 < T; ch += 2) {
-          const uint32_t m8 = static_cast<uint32_t>(mask >> (8 * ch)) & 0xffu;
-          if (m8 == 0) continue;
-          uint32_t v[2][kTerms][8];
+    for (int i = et; i < P; i += 256) {                             // pairs: slot -> active expert, row of its partials
+      const int sl = L.pa[i], t = i / k;
+      const int a = sl < 0 ? -1 : L.s2a[sl];
+      const int u = sl < 0 ? -1 : L.off[a] + __popcll(L.mask[sl] & ((1ull << t) - 1ull));
+      L.pa[i] = static_cast<int16_t>(a);
+      L.pu[i] = static_cast<int16_t>(u);
+      if (u >= 0) L.tok[u] = static_cast<uint8_t>(t);
+    }
+    // ---- gate/up.  The CTA with a line's first block finishes it: its part of the line is the last of its run, while
+    // the other parts are the first segments of the runs after it, done long before except in runs of one line.  So nobody
+    // waits in a circle, and mostly not at all.
+#pragma unroll 1
+    for (int ph = 0; ph < 2; ++ph) {
+      const FewPhase& f = s_phase[ph];
+      FewIter s(p, f, false);
+      while (ok && s.next()) {
+        const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+        ++n_seg;
+        bool seen = mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns);
+        const int last = s.kb0 == 0 && s.kb1 < p.Kb1 ? static_cast<int>(run_owner(s.line * p.Kb1 + p.Kb1 - 1, f.C, f.B)) : static_cast<int>(cta);
+        for (int c = static_cast<int>(cta) + 1 + et; c <= last; c += 256)
+          seen = seen && few_poll(part_done + ph * C + c, 1, s_abort, p.wait_ns);
+        ok = bar_all(3, 256, seen);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t acc = tmem_base + slot * 128u + lanes;
+        const int u0 = L.off[s.a], n_col = L.off[s.a + 1] - u0, C8 = (n_col + 7) & ~7;
+        uint8_t* himg = p.h_img + static_cast<size_t>(p.Kb2) * (static_cast<size_t>(L.hrow[s.a]) * 128 + (kBf16 ? 0 : 512) * static_cast<size_t>(s.a));
+        float* mine = p.gu_part + (static_cast<size_t>(ph) * C + cta) * T * 256 + row;     // [token column][half][row]
+#pragma unroll 1
+        for (int c0 = g * kFewBatch; c0 < n_col; c0 += 2 * kFewBatch) {
+          uint32_t v[kFewBatch][2][kTerms];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int i = 0; i < kFewBatch; ++i) {
+            const uint32_t t = L.tok[u0 + min(c0 + i, n_col - 1)];
 #pragma unroll
-            for (int j = 0; j < kTerms; ++j) tmem_ld8(acc + h * R1 + j * T8 + ch * 8, v[h][j]);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int j = 0; j < kTerms; ++j) tmem_ld1(acc + h * R1 + j * T8 + t, v[i][h][j]);
+          }
           tmem_wait_ld();
+          float gu[kFewBatch][2];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (m8 >> i & 1u) {
+          for (int i = 0; i < kFewBatch; ++i)
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float f = __uint_as_float(v[h][0][i]);
-                if constexpr (kTerms == 2) f += __uint_as_float(v[h][1][i]);
-                __stcg(dst + (ch * 8 + i) * 256 + h * 128, f);
-              }
+            for (int h = 0; h < 2; ++h) {
+              gu[i][h] = __uint_as_float(v[i][h][0]);
+              if constexpr (kTerms == 2) gu[i][h] += __uint_as_float(v[i][h][1]);
             }
+          if (s.kb0 > 0) {                                          // another CTA's line: hand the partial sums over
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i)
+              if (c0 + i < n_col) {
+                __stcg(mine + (c0 + i) * 256, gu[i][0]);
+                __stcg(mine + (c0 + i) * 256 + 128, gu[i][1]);
+              }
+            continue;
+          }
+#pragma unroll 2
+          for (int c = static_cast<int>(cta) + 1; c <= last; ++c) { // the other parts, in the order of the runs
+            const float* src = p.gu_part + (static_cast<size_t>(ph) * C + c) * T * 256 + row;
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i)
+              if (c0 + i < n_col) {
+                gu[i][0] += __ldcg(src + (c0 + i) * 256);
+                gu[i][1] += __ldcg(src + (c0 + i) * 256 + 128);
+              }
+          }
+          // H of this (expert, 128-column block): SwiGLU, the two-term split, straight into the operand image
+#pragma unroll
+          for (int i = 0; i < kFewBatch; ++i) gu[i][0] = __fdividef(gu[i][0], 1.f + __expf(-gu[i][0])) * gu[i][1];
+          if constexpr (kBf16) {
+            uint8_t* blk = himg + static_cast<size_t>(s.nt * 2 + (row >> 6)) * (2 * C8 * 128);
+            const int ii = row & 63;
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i)
+              if (c0 + i < n_col) {
+                const int col = c0 + i, r2 = C8 + col;
+                const __nv_bfloat16 hi = __float2bfloat16_rn(gu[i][0]);
+                const float hf = __bfloat162float(hi);
+                const __nv_bfloat16 lo = __float2bfloat16_rn(isfinite(hf) ? gu[i][0] - hf : 0.f);
+                *reinterpret_cast<__nv_bfloat16*>(blk + col * 128 + (((ii >> 3) ^ (col & 7)) << 4) + (ii & 7) * 2) = hi;
+                *reinterpret_cast<__nv_bfloat16*>(blk + r2 * 128 + (((ii >> 3) ^ (r2 & 7)) << 4) + (ii & 7) * 2) = lo;
+              }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i) {
+              const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(gu[i][0]) & 0x7fffffffu);
+              if (lane == i) s_amax[par][g][quad][i] = m;
+            }
+            bar_sync(4 + g, 128);
+            uint8_t* blk = himg + static_cast<size_t>(s.nt) * (2 * C8 * 128 + 512);
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i)
+              if (c0 + i < n_col) {
+                const uint32_t m = max(max(s_amax[par][g][0][i], s_amax[par][g][1][i]), max(s_amax[par][g][2][i], s_amax[par][g][3][i]));
+                const int eps = split_exponent(__uint_as_float(m));
+                uint32_t q1, q2;
+                split_e4m3(gu[i][0], 0.f, pow2_neg(eps), q1, q2);
+                const int col = c0 + i, r2 = C8 + col;
+                blk[col * 128 + (((row >> 4) ^ (col & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q1);
+                blk[r2 * 128 + (((row >> 4) ^ (r2 & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q2);
+                if (row < 2) {
+                  const int r = row == 0 ? col : r2;
+                  blk[2 * C8 * 128 + (r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(eps + 127 - 4 * row);
+                }
+              }
+            par ^= 1u;
+          }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
         bar_sync(3, 256);
-        if (et == 0) {
+        if (et == 0) {                                              // publish the partial sums, or H
           __threadfence();
-          const int n = s.kb1 - s.kb0;
-          const int before = atomicAdd(line_cnt + s.line, n);
-          __threadfence();
-          s_finish = before + n == p.Kb1 ? 1 : 0;
+          atomicAdd(s.kb0 > 0 ? part_done + ph * C + cta : h_done + 32 * ph, 1);
         }
-        bar_sync(3, 256);
-        if (s_finish == 0) continue;                                // another CTA finishes this column block
-      }
-      // H of this (expert, 128-column block): SwiGLU, the two-term split, straight into the operand image
-      const uint32_t c_lo = run_owner(s.line * p.Kb1, C1, B1), c_hi = run_owner(s.line * p.Kb1 + p.Kb1 - 1, C1, B1);
-      const int n_col = L.off[s.a + 1] - L.off[s.a], C8 = (n_col + 7) & ~7;
-      uint8_t* himg = p.h_img + static_cast<size_t>(p.Kb2) * (static_cast<size_t>(L.hrow[s.a]) * 128 + (kBf16 ? 0 : 512) * static_cast<size_t>(s.a));
-      for (int ch = g; ch * 8 < T; ch += 2) {
-        const uint32_t m8 = static_cast<uint32_t>(mask >> (8 * ch)) & 0xffu;
-        if (m8 == 0) continue;
-        float gu[2][8];
-        if (whole) {
-          uint32_t v[2][kTerms][8];
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < kTerms; ++j) tmem_ld8(acc + h * R1 + j * T8 + ch * 8, v[h][j]);
-          tmem_wait_ld();
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              gu[h][i] = __uint_as_float(v[h][0][i]);
-              if constexpr (kTerms == 2) gu[h][i] += __uint_as_float(v[h][1][i]);
-            }
-        } else {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gu[h][i] = 0.f;
-          for (uint32_t c = c_lo; c <= c_hi; ++c) {                 // in the order of the runs
-            const int part = run_begin(c, C1, B1) > s.line * p.Kb1 ? 0 : 1;
-            const float* src = p.gu_part + (static_cast<size_t>(c) * 2 + part) * T * 256 + row;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (m8 >> i & 1u) {
-                gu[0][i] += __ldcg(src + (ch * 8 + i) * 256);
-                gu[1][i] += __ldcg(src + (ch * 8 + i) * 256 + 128);
-              }
-          }
-        }
-        const int col0 = __popcll(mask & ((1ull << (8 * ch)) - 1ull));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) gu[0][i] = __fdividef(gu[0][i], 1.f + __expf(-gu[0][i])) * gu[1][i];
-        if constexpr (kBf16) {
-          uint8_t* blk = himg + static_cast<size_t>(s.nt * 2 + (row >> 6)) * (2 * C8 * 128);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (m8 >> i & 1u) {
-              const int col = col0 + __popc(m8 & ((1u << i) - 1u)), r2 = C8 + col, ii = row & 63;
-              const __nv_bfloat16 hi = __float2bfloat16_rn(gu[0][i]);
-              const float hf = __bfloat162float(hi);
-              const __nv_bfloat16 lo = __float2bfloat16_rn(isfinite(hf) ? gu[0][i] - hf : 0.f);
-              *reinterpret_cast<__nv_bfloat16*>(blk + col * 128 + (((ii >> 3) ^ (col & 7)) << 4) + (ii & 7) * 2) = hi;
-              *reinterpret_cast<__nv_bfloat16*>(blk + r2 * 128 + (((ii >> 3) ^ (r2 & 7)) << 4) + (ii & 7) * 2) = lo;
-            }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(gu[0][i]) & 0x7fffffffu);
-            if (lane == i) s_amax[par][g][quad][i] = m;
-          }
-          bar_sync(4 + g, 128);
-          uint8_t* blk = himg + static_cast<size_t>(s.nt) * (2 * C8 * 128 + 512);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (m8 >> i & 1u) {
-              const uint32_t m = max(max(s_amax[par][g][0][i], s_amax[par][g][1][i]), max(s_amax[par][g][2][i], s_amax[par][g][3][i]));
-              const int eps = split_exponent(__uint_as_float(m));
-              uint32_t q1, q2;
-              split_e4m3(gu[0][i], 0.f, pow2_neg(eps), q1, q2);
-              const int col = col0 + __popc(m8 & ((1u << i) - 1u)), r2 = C8 + col;
-              blk[col * 128 + (((row >> 4) ^ (col & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q1);
-              blk[r2 * 128 + (((row >> 4) ^ (r2 & 7)) << 4) + (row & 15)] = static_cast<uint8_t>(q2);
-              if (row < 2) {
-                const int r = row == 0 ? col : r2;
-                blk[2 * C8 * 128 + (r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(eps + 127 - 4 * row);
-              }
-            }
-          par ^= 1u;
-        }
-      }
-      if (whole) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
-      }
-      bar_sync(3, 256);
-      if (et == 0) {
-        __threadfence();
-        atomicAdd(h_done, 1);
       }
     }
     // ---- down: partial sums of (256 output columns, expert), one row of Y per (token, expert) pair -----------
-    FewIter it2(d0, d1, p.Kb2, A, 0);
     int pend_nt = -1, pend = 0;                                     // blocks of column block pend_nt not yet published
-    while (ok && it2.next(s)) {
-      if (s.nt != pend_nt && pend > 0) {
-        bar_sync(3, 256);
-        if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
-        pend = 0;
-      }
-      const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
-      ++n_seg;
-      ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
-      if (!ok) break;
-      tc_fence_after();
-      const int u0 = L.off[s.a], n_col = L.off[s.a + 1] - u0, C8 = (n_col + 7) & ~7;
-      const uint32_t acc = tmem_base + slot * 128u + lanes + g * (2 * C8);
-      const int j = static_cast<int>(cta - run_owner(s.line * p.Kb2, C2, B2));
-      const int n = s.nt * 256 + g * 128 + row;
-      float* dst = p.y_part + (static_cast<size_t>(j) * P + u0) * p.d + n;
-      for (int ch = 0; ch * 8 < n_col; ++ch) {
-        uint32_t v0[8], v1[8];
-        tmem_ld8(acc + ch * 8, v0);
-        tmem_ld8(acc + C8 + ch * 8, v1);
-        tmem_wait_ld();
-        if (n < p.d) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (ch * 8 + i < n_col)
-              __stcg(dst + static_cast<size_t>(ch * 8 + i) * p.d, __uint_as_float(v0[i]) + __uint_as_float(v1[i]));
+#pragma unroll 1
+    for (int ph = 2; ph < 4; ++ph) {
+      const FewPhase& f = s_phase[ph];
+      FewIter s(p, f, true);
+      while (ok && s.next()) {
+        if (s.nt != pend_nt && pend > 0) {
+          bar_sync(3, 256);
+          if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
+          pend = 0;
         }
+        const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+        ++n_seg;
+        ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
+        if (!ok) break;
+        tc_fence_after();
+        const int u0 = L.off[s.a], n_col = L.off[s.a + 1] - u0, C8 = (n_col + 7) & ~7;
+        const uint32_t acc = tmem_base + slot * 128u + lanes + g * (2 * C8);
+        const int j = static_cast<int>(cta - run_owner(s.line * p.Kb2, f.C, f.B));
+        const int n = s.nt * 256 + g * 128 + row;
+        float* dst = p.y_part + (static_cast<size_t>(j) * P + u0) * p.d + n;
+#pragma unroll 1
+        for (int c0 = 0; c0 < n_col; c0 += kFewBatch) {
+          uint32_t v0[kFewBatch], v1[kFewBatch];
+          tmem_ld4(acc + c0, v0);
+          tmem_ld4(acc + C8 + c0, v1);
+          tmem_wait_ld();
+          if (n < p.d) {
+#pragma unroll
+            for (int i = 0; i < kFewBatch; ++i)
+              if (c0 + i < n_col)
+                __stcg(dst + static_cast<size_t>(c0 + i) * p.d, __uint_as_float(v0[i]) + __uint_as_float(v1[i]));
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
+        pend_nt = s.nt;
+        pend += s.kb1 - s.kb0;
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
-      pend_nt = s.nt;
-      pend += s.kb1 - s.kb0;
     }
     if (pend > 0) {
       bar_sync(3, 256);
@@ -586,40 +646,60 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       uint4* out = reinterpret_cast<uint4*>(p.out);
       for (size_t i = static_cast<size_t>(cta) * 256 + et; i < static_cast<size_t>(T) * p.d / 8; i += static_cast<size_t>(C) * 256)
         out[i] = make_uint4(0, 0, 0, 0);
-    } else if (ok && d1 > d0) {
-      const uint32_t per_nt = static_cast<uint32_t>(A) * p.Kb2;
-      const int nt_lo = static_cast<int>(d0 / per_nt), nt_hi = static_cast<int>((d1 - 1) / per_nt);
+    } else if (ok) {
+      const FewPhase &f0 = s_phase[2], &f = s_phase[3].an > 0 ? s_phase[3] : s_phase[2];   // f: the last phase that has work
+      const uint32_t per_nt = static_cast<uint32_t>(f.an) * p.Kb2;
+      const int nt_lo = static_cast<int>(f.b / per_nt), nt_hi = f.e > f.b ? static_cast<int>((f.e - 1) / per_nt) : nt_lo - 1;
       for (int nt = nt_lo; ok && nt <= nt_hi; ++nt) {
+        uint8_t* split = L.split + (nt & 1) * A;                    // the other half may still be read
+        for (int a = et; a < A; a += 256) {
+          const FewPhase& h = a < f0.an ? f0 : f;
+          const uint32_t b = (static_cast<uint32_t>(nt) * h.an + a - h.a0) * p.Kb2;
+          split[a] = static_cast<uint8_t>(run_owner(b + p.Kb2 - 1, h.C, h.B) - run_owner(b, h.C, h.B) + 1);
+        }
+        const uint32_t c_lo = run_owner(nt * per_nt, f.C, f.B), c_hi = run_owner((nt + 1) * per_nt - 1, f.C, f.B);
+        const int parts = static_cast<int>(c_hi - c_lo + 1);
         bool seen = true;
-        if (et == 0) seen = few_poll(y_cnt + nt, static_cast<int>(per_nt), s_abort, p.wait_ns);
+        if (et == 0) seen = few_poll(y_cnt + nt, A * p.Kb2, s_abort, p.wait_ns);
         ok = bar_all(3, 256, seen);
         if (!ok) break;
-        const uint32_t c_lo = run_owner(nt * per_nt, C2, B2), c_hi = run_owner((nt + 1) * per_nt - 1, C2, B2);
-        const int parts = static_cast<int>(c_hi - c_lo + 1);
-        for (int i = static_cast<int>(cta - c_lo) * 256 + et; i < T * 64; i += parts * 256) {
+        // Four lanes per (token, 4 columns): lane q takes the slots q, q + 4, ... with all their partials in flight, then
+        // the four sums are added in a fixed tree.
+        const int q = et & 3;
+        const size_t part_pitch = static_cast<size_t>(P) * p.d;
+        for (int i = static_cast<int>(cta - c_lo) * 64 + (et >> 2); i < T * 64; i += parts * 64) {
           const int t = i >> 6, col = nt * 256 + (i & 63) * 4;
-          if (col >= p.d) continue;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (t < nv) {
-            for (int q = 0; q < k; ++q) {
-              const int sl = L.pslot[t * k + q];
-              if (sl < 0) continue;
-              const int a = L.s2a[sl];
-              const int u = L.off[a] + __popcll(L.mask[sl] & ((1ull << t) - 1ull));
-              const uint32_t b = (static_cast<uint32_t>(nt) * A + a) * p.Kb2;
-              const int splits = static_cast<int>(run_owner(b + p.Kb2 - 1, C2, B2) - run_owner(b, C2, B2)) + 1;
-              const float w = p.w[t * k + q];
-              float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-              for (int j = 0; j < splits; ++j) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(p.y_part + (static_cast<size_t>(j) * P + u) * p.d + col));
-                y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
-              }
-              acc.x = fmaf(w, y.x, acc.x); acc.y = fmaf(w, y.y, acc.y); acc.z = fmaf(w, y.z, acc.z); acc.w = fmaf(w, y.w, acc.w);
+          if (col < p.d) {
+#pragma unroll 2
+            for (int s = q; s < k; s += 4) {
+              const int a = L.pa[t * k + s];
+              if (a < 0) continue;
+              const int n = split[a];
+              const float* src = p.y_part + static_cast<size_t>(L.pu[t * k + s]) * p.d + col;
+              float4 v[kFewSplit];
+#pragma unroll
+              for (int j = 0; j < kFewSplit; ++j)
+                v[j] = n > j ? __ldcg(reinterpret_cast<const float4*>(src + j * part_pitch)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              const float w = L.w[t * k + s];
+              acc.x = fmaf(w, v[0].x + v[1].x + v[2].x + v[3].x, acc.x);
+              acc.y = fmaf(w, v[0].y + v[1].y + v[2].y + v[3].y, acc.y);
+              acc.z = fmaf(w, v[0].z + v[1].z + v[2].z + v[3].z, acc.z);
+              acc.w = fmaf(w, v[0].w + v[1].w + v[2].w + v[3].w, acc.w);
             }
           }
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
-          *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(t) * p.d + col) =
-              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) {
+            acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
+            acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
+            acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
+            acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
+          }
+          if (q == 0 && col < p.d) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+            *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(t) * p.d + col) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+          }
         }
       }
     }
@@ -646,10 +726,10 @@ static size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255);
 FewLayout few_layout(int T, int k, int G, int d, int f, int num_sms) {
   FewLayout L;
   const size_t P = static_cast<size_t>(T) * k, A = P < static_cast<size_t>(G) ? P : static_cast<size_t>(G);
-  const int NT1 = f / 128, NT2 = (d + 255) / 256;
+  const int NT2 = (d + 255) / 256;
   // the widest of both weight types: rows of 128 bytes per K-block of 64 (bf16) or 128 (fp8) values
   const size_t T16 = (static_cast<size_t>(T) + 15) / 16 * 16;
-  L.counter_ints = 64 + NT2 + G * NT1;
+  L.counter_ints = 96 + NT2 + 2 * num_sms;
   L.off_leave = 0;
   L.off_counters = 256;
   L.off_x = align256(L.off_counters + 2 * sizeof(int32_t) * static_cast<size_t>(L.counter_ints));
