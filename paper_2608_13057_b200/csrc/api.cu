@@ -587,7 +587,7 @@ static int run_few(bool bf16, const tempo_shape* s, const void* x, const int32_t
   p.ids = ids; p.w = w; p.n_valid = n_valid; p.replica_map = replica_map;
   p.x = static_cast<const __nv_bfloat16*>(x);
   p.w13 = blob + L.off_w13; p.w2 = blob + L.off_w2; p.sf13 = blob + L.off_sf13; p.sf2 = blob + L.off_sf2;
-  p.leave = reinterpret_cast<unsigned long long*>(ws + F.off_leave);
+  p.leave = reinterpret_cast<unsigned int*>(ws + F.off_leave);
   p.counters = reinterpret_cast<int32_t*>(ws + F.off_counters);
   p.counter_ints = F.counter_ints;
   p.x_img = ws + F.off_x; p.h_img = ws + F.off_h;

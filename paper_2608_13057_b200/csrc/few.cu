@@ -24,7 +24,7 @@
 // with atomics, so results do not depend on timing.
 //
 // Counters in the workspace come in two sets: a launch counts in one and zeroes the other for the next launch; which
-// one is told by a launch count that every CTA bumps once as it leaves.  Every wait is bounded (FewParams::wait_ns).
+// one is told by a count, modulo twice the grid, that every CTA bumps once as it leaves.  Every wait is bounded (FewParams::wait_ns).
 #include <cuda_fp16.h>
 
 #include "ffn_common.cuh"
@@ -159,35 +159,57 @@ __device__ __forceinline__ uint32_t few_idesc_bf16(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
 }
 
+// Shared-memory descriptor of a K-major operand in the 128-byte swizzle (rows of 128 bytes, groups of 8 rows 1024 bytes
+// apart): only its low word differs from tile to tile.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void few_mma_fp8(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 da, {%1, %7};\n\tmov.b64 db, {%2, %7};\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], da, db, %3, [%5], [%6], p;\n\t}"
+      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(kDescHi) : "memory");
+}
+__device__ __forceinline__ void few_mma_bf16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+}
+
 struct FewLists {                          // in dynamic shared memory behind the ring
   unsigned long long* mask;                // [G]  tokens of each instance slot, bit t
   uint16_t* act;                           // [A]  instance slot of the a-th active expert (ascending)
   uint16_t* off;                           // [A+1] (token, expert) pairs before it
   uint16_t* hrow;                          // [A]  operand rows of H before it
   int16_t* s2a;                            // [G]  inverse of act
-  int16_t* pa;                             // [T*k] active expert of each pair (first its slot), -1: none on this rank
+  int16_t* pa;                             // [T*k] slot of each pair, -1: none on this rank; then see below
   int16_t* pu;                             // [T*k] its row of the down partials
   uint8_t* tok;                            // [T*k] token of each row of the down partials (by expert, then token)
   float* w;                                // [T*k] routing weights
+  int16_t* first;                          // [E]  first replica column of every expert (-1: not a slot)
   uint8_t* split;                          // [2][A] partial sums per expert of the column block being reduced
 };
-__host__ __device__ inline size_t few_list_bytes(int G, int P) {
+__host__ __device__ inline size_t few_list_bytes(int G, int P, int E) {
   const size_t A = G < P ? G : P;
   return static_cast<size_t>(G) * 8 + (2 * (A + 1) + 7) / 8 * 8 * 3 + (2 * static_cast<size_t>(G) + 7) / 8 * 8 +
-         (2 * static_cast<size_t>(P) + 7) / 8 * 8 * 2 + (4 * static_cast<size_t>(P) + 7) / 8 * 8 + (static_cast<size_t>(P) + 7) / 8 * 8 + (2 * A + 7) / 8 * 8;
+         (2 * static_cast<size_t>(P) + 7) / 8 * 8 * 2 + (4 * static_cast<size_t>(P) + 7) / 8 * 8 + (static_cast<size_t>(P) + 7) / 8 * 8 + (2 * static_cast<size_t>(E) + 7) / 8 * 8 + (2 * A + 7) / 8 * 8;
 }
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_full[kFewRing];      // weight tile landed
-  __shared__ __align__(8) uint64_t s_tok[kFewRing];       // token tile landed
-  __shared__ __align__(8) uint64_t s_empty[kFewRing];
+  __shared__ __align__(16) uint64_t s_bars[3 * kFewRing];
+  uint64_t *s_full = s_bars, *s_tok = s_bars + kFewRing, *s_empty = s_bars + 2 * kFewRing;   // weight tile, token tile landed; free
   __shared__ __align__(8) uint64_t s_acc_full[2];
   __shared__ __align__(8) uint64_t s_acc_empty[2];
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort_storage, s_A;
   __shared__ FewPhase s_phase[4];
+  __shared__ int s_local[kFewMaxT];        // pairs on this rank of each token
   __shared__ uint32_t s_amax[2][2][4][kFewBatch];  // [batch parity][group][warp][token]
   volatile int* s_abort = &s_abort_storage;
 
@@ -209,6 +231,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     L.pu = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(P) * 2 + 7) / 8 * 8;
     L.w = reinterpret_cast<float*>(q); q += (static_cast<size_t>(P) * 4 + 7) / 8 * 8;
     L.tok = q; q += (static_cast<size_t>(P) + 7) / 8 * 8;
+    L.first = reinterpret_cast<int16_t*>(q); q += (static_cast<size_t>(p.E) * 2 + 7) / 8 * 8;
     L.split = q;
   }
   pdl_trigger();
@@ -234,12 +257,29 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
   tc_fence_after();
   const uint32_t tmem_base = s_tmem_base;
   pdl_wait();
-  int nv = T;
-  if (p.n_valid != nullptr) nv = max(0, min(*p.n_valid, T));
-  // launch count: every CTA of every earlier launch has bumped it, those of this one that have left as well
-  const unsigned long long launch = *reinterpret_cast<volatile const unsigned long long*>(p.leave) / C;
-  int32_t* cnt = p.counters + (launch & 1ull) * p.counter_ints;
-  int32_t* cnt_next = p.counters + ((launch & 1ull) ^ 1ull) * p.counter_ints;
+  const uint32_t left = *reinterpret_cast<volatile const uint32_t*>(p.leave);
+  const int n_valid = p.n_valid != nullptr ? *p.n_valid : T;
+  // The first pairs and the replica map's first column are requested before anything waits for what was just read: one
+  // memory latency for all of it.
+  int id[4];
+  float w[4];
+  if (warp < 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      id[j] = tid + 128 * j < P ? p.ids[tid + 128 * j] : 0;
+      w[j] = tid + 128 * j < P ? p.w[tid + 128 * j] : 0.f;
+    }
+#pragma unroll 4
+    for (int e = tid; e < p.E; e += 128) {
+      const int v = p.replica_map[e * p.R];
+      L.first[e] = static_cast<int16_t>(v >= 0 && v < G ? v : -1);
+    }
+  }
+  const int nv = max(0, min(n_valid, T));
+  // CTAs count modulo 2 C as they leave: a launch finds the count in [0, C) or in [C, 2 C), with those of its own CTAs
+  // that have left already
+  int32_t* cnt = p.counters + (left >= C ? p.counter_ints : 0);
+  int32_t* cnt_next = p.counters + (left >= C ? 0 : p.counter_ints);
   // h_done: 32 ints per half; part_done: [half][CTA], the partial sums of that CTA's first segment are in the workspace
   int32_t *x_done = cnt, *h_done = cnt + 32, *y_cnt = cnt + 96, *part_done = cnt + 96 + p.NT2;
   const int T8 = (T + 7) & ~7;
@@ -250,30 +290,22 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
 
   if (warp < 4) {
     // ---- expert lists (128 threads) ----------------------------------------------------------------
+    bar_sync(1, 128);
     bool bad = false;
-    for (int i0 = tid; i0 < P; i0 += 512) {                          // four pairs per thread: their loads overlap
-      int id[4], slot[4];
-      float w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = i0 + 128 * j;
-        const bool live = i < nv * k;
-        id[j] = live ? p.ids[i] : 0;
-        w[j] = live ? p.w[i] : 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool live = i0 + 128 * j < nv * k, good = id[j] >= 0 && id[j] < p.E;
-        bad |= live && !good;
-        slot[j] = live && good ? p.replica_map[id[j] * p.R] : -1;
-        id[j] = live && good ? id[j] : -1;
-      }
+    for (int i0 = tid; i0 < P; i0 += 512) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = i0 + 128 * j;
         if (i >= P) break;
-        int v = slot[j] < G ? slot[j] : -1;
-        for (int r = 1; r < p.R && v < 0 && id[j] >= 0; ++r) {       // the first replica on this rank
+        const bool live = i < nv * k;
+        if (i0 >= 512) {
+          id[j] = p.ids[i];
+          w[j] = p.w[i];
+        }
+        const bool good = id[j] >= 0 && id[j] < p.E;
+        bad |= live && !good;
+        int v = live && good ? L.first[id[j]] : -1;
+        for (int r = 1; r < p.R && v < 0 && live && good; ++r) {     // else the first replica on this rank
           const int u = p.replica_map[id[j] * p.R + r];
           if (u < G) v = u;
         }
@@ -309,7 +341,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
         h0 += __shfl_sync(0xffffffffu, ph, 31);
       }
       if (lane == 0) { s_A = a0; L.off[a0] = static_cast<uint16_t>(o0); }
-      if (lane < 4) few_phase(s_phase[lane], p, lane, a0, C, cta);
+    } else if (warp == 1) {                                         // the runs need the number of experts only
+      int n = 0;
+      for (int base = 0; base < G; base += 32) n += __popc(__ballot_sync(0xffffffffu, base + lane < G && L.mask[base + lane] != 0ull));
+      if (lane < 4) few_phase(s_phase[lane], p, lane, n, C, cta);
     }
     bar_sync(1, 128);
     bar_arrive(2, kFewThreads);                                     // the lists, for the epilogue warps
@@ -417,7 +452,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
   } else if (warp == 1) {
     // ---- MMA issuer ------------------------------------------------------------------------------------
     if (lane == 0) {
-      uint32_t stage = 0, phase = 0, n_seg = 0, n_sf = 0, n_blk = 0;
+      uint32_t stage = 0, phase = 0, n_seg = 0;
+      // One thread issues everything, so what it computes per block counts: descriptors are a low word plus a constant.
+      const uint32_t bars = smem_u32(s_bars), desc_lo = ((smem_base >> 4) & 0x3fffu) | (1u << 16), desc_step = p.stage_bytes >> 4;
+      uint32_t sf_slot = tmem_base + kSfCol0, tok_slot = tmem_base + kSfCol0 + 16u;      // two of each, used in turn
       bool ok = true;
 #pragma unroll 1
       for (int ph = 0; ph < 4; ++ph) {
@@ -428,41 +466,37 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
           ++n_seg;
           if (!mbar_wait(smem_u32(&s_acc_empty[slot]), (use & 1u) ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t acc = tmem_base + slot * 128u;
+          const uint32_t acc = tmem_base + slot * 128u, acc2 = acc + N;
+          const uint32_t idesc0 = kBf16 ? few_idesc_bf16(N) : few_idesc_fp8(N, 0);
+          uint32_t accumulate = 0;
 #pragma unroll 1
           for (int kb = s.kb0; kb < s.kb1; ++kb) {
-            if (!mbar_wait(smem_u32(&s_full[stage]), phase, s_abort, p.wait_ns) ||
-                !mbar_wait(smem_u32(&s_tok[stage]), phase, s_abort, p.wait_ns)) { ok = false; break; }
+            if (!mbar_wait(bars + 8 * stage, phase, s_abort, p.wait_ns) ||
+                !mbar_wait(bars + 8 * (kFewRing + stage), phase, s_abort, p.wait_ns)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t sA = smem_base + stage * p.stage_bytes, sSF = sA + kBBytes, sB = sSF + kSfbBytes;
-            const uint64_t da = smem_desc_sw128(sA), db = smem_desc_sw128(sB);
-            const uint32_t accumulate = kb > s.kb0 ? 1u : 0u;
+            const uint32_t da = desc_lo + stage * desc_step, db = da + ((kBBytes + kSfbBytes) >> 4), da2 = da + ((kTileM * 128) >> 4);
             if constexpr (kBf16) {
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
+              for (int ks = 0; ks < 4; ++ks) few_mma_bf16(acc, da + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                  tc_mma_bf16(acc + h * N, da + h * ((kTileM * 128) >> 4) + 2u * ks, db + 2u * ks, few_idesc_bf16(N),
-                              accumulate | (ks != 0 ? 1u : 0u));
+              for (int ks = 0; ks < 4; ++ks) few_mma_bf16(acc2, da2 + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
             } else {
-              if ((kb & 3) == 0 || kb == s.kb0) {
-                ++n_sf;
-                const uint32_t t = tmem_base + kSfCol0 + 8u * (n_sf & 1u);
-                tc_cp_sf(t, smem_desc_sf(sSF));
-                tc_cp_sf(t + 4, smem_desc_sf(sSF + 512));
+              const uint32_t sSF = smem_base + stage * p.stage_bytes + kBBytes;
+              if ((kb & 3) == 0 || accumulate == 0) {
+                sf_slot ^= 8u;
+                tc_cp_sf(sf_slot, smem_desc_sf(sSF));
+                tc_cp_sf(sf_slot + 4, smem_desc_sf(sSF + 512));
               }
-              ++n_blk;
-              const uint32_t sfa = tmem_base + kSfCol0 + 8u * (n_sf & 1u), sfb = tmem_base + kSfCol0 + 16u + 4u * (n_blk & 1u);
-              tc_cp_sf(sfb, smem_desc_sf(sB + N * 128));
-              const uint32_t idesc = few_idesc_fp8(N, kb & 3);
+              tok_slot ^= 4u;
+              tc_cp_sf(tok_slot, smem_desc_sf(sSF + kSfbBytes + N * 128));
+              const uint32_t idesc = idesc0 | static_cast<uint32_t>(kb & 3) << 29;
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
+              for (int ks = 0; ks < 4; ++ks) few_mma_fp8(acc, da + 2 * ks, db + 2 * ks, idesc, sf_slot, tok_slot, ks == 0 ? accumulate : 1u);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                  tc_mma_mxf8(acc + h * N, da + h * ((kTileM * 128) >> 4) + 2u * ks, db + 2u * ks, idesc, sfa + 4u * h, sfb,
-                              accumulate | (ks != 0 ? 1u : 0u));
+              for (int ks = 0; ks < 4; ++ks) few_mma_fp8(acc2, da2 + 2 * ks, db + 2 * ks, idesc, sf_slot + 4, tok_slot, ks == 0 ? accumulate : 1u);
             }
-            tc_commit(smem_u32(&s_empty[stage]));
+            accumulate = 1;
+            tc_commit(bars + 8 * (2 * kFewRing + stage));
             if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
           }
           if (ok) tc_commit(smem_u32(&s_acc_full[slot]));
@@ -475,13 +509,20 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
     uint32_t n_seg = 0, par = 0;
     bool ok = true;
-    for (int i = et; i < P; i += 256) {                             // pairs: slot -> active expert, row of its partials
-      const int sl = L.pa[i], t = i / k;
-      const int a = sl < 0 ? -1 : L.s2a[sl];
-      const int u = sl < 0 ? -1 : L.off[a] + __popcll(L.mask[sl] & ((1ull << t) - 1ull));
-      L.pa[i] = static_cast<int16_t>(a);
-      L.pu[i] = static_cast<int16_t>(u);
-      if (u >= 0) L.tok[u] = static_cast<uint8_t>(t);
+    if (et < T) {                                                   // a token's pairs on this rank, packed to the front
+      const int t = et;
+      int n = 0;
+      for (int q = 0; q < k; ++q) {
+        const int sl = L.pa[t * k + q];
+        if (sl < 0) continue;
+        const int a = L.s2a[sl], u = L.off[a] + __popcll(L.mask[sl] & ((1ull << t) - 1ull));
+        L.pa[t * k + n] = static_cast<int16_t>(a);                  // active expert, row of its partials, weight
+        L.pu[t * k + n] = static_cast<int16_t>(u);
+        L.w[t * k + n] = L.w[t * k + q];
+        L.tok[u] = static_cast<uint8_t>(t);
+        ++n;
+      }
+      s_local[t] = n;
     }
     // ---- gate/up.  The CTA with a line's first block finishes it: its part of the line is the last of its run, while
     // the other parts are the first segments of the runs after it, done long before except in runs of one line.  So nobody
@@ -650,57 +691,75 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       const FewPhase &f0 = s_phase[2], &f = s_phase[3].an > 0 ? s_phase[3] : s_phase[2];   // f: the last phase that has work
       const uint32_t per_nt = static_cast<uint32_t>(f.an) * p.Kb2;
       const int nt_lo = static_cast<int>(f.b / per_nt), nt_hi = f.e > f.b ? static_cast<int>((f.e - 1) / per_nt) : nt_lo - 1;
-      for (int nt = nt_lo; ok && nt <= nt_hi; ++nt) {
-        uint8_t* split = L.split + (nt & 1) * A;                    // the other half may still be read
-        for (int a = et; a < A; a += 256) {
+      bool seen = true;
+      for (int nt = nt_lo + et; nt <= nt_hi; nt += 256) seen = seen && few_poll(y_cnt + nt, A * p.Kb2, s_abort, p.wait_ns);
+      const size_t part_pitch = static_cast<size_t>(P) * p.d;
+      for (int nt0 = nt_lo; nt0 <= nt_hi; nt0 += 2) {               // (almost every CTA has one or two column blocks)
+        const int two = min(2, nt_hi - nt0 + 1);
+        for (int i = et; i < two * A; i += 256) {
+          const int a = i % A, nt = nt0 + i / A;
           const FewPhase& h = a < f0.an ? f0 : f;
           const uint32_t b = (static_cast<uint32_t>(nt) * h.an + a - h.a0) * p.Kb2;
-          split[a] = static_cast<uint8_t>(run_owner(b + p.Kb2 - 1, h.C, h.B) - run_owner(b, h.C, h.B) + 1);
+          L.split[i] = static_cast<uint8_t>(run_owner(b + p.Kb2 - 1, h.C, h.B) - run_owner(b, h.C, h.B) + 1);
         }
-        const uint32_t c_lo = run_owner(nt * per_nt, f.C, f.B), c_hi = run_owner((nt + 1) * per_nt - 1, f.C, f.B);
-        const int parts = static_cast<int>(c_hi - c_lo + 1);
-        bool seen = true;
-        if (et == 0) seen = few_poll(y_cnt + nt, A * p.Kb2, s_abort, p.wait_ns);
         ok = bar_all(3, 256, seen);
         if (!ok) break;
-        // Four lanes per (token, 4 columns): lane q takes the slots q, q + 4, ... with all their partials in flight, then
-        // the four sums are added in a fixed tree.
-        const int q = et & 3;
-        const size_t part_pitch = static_cast<size_t>(P) * p.d;
-        for (int i = static_cast<int>(cta - c_lo) * 64 + (et >> 2); i < T * 64; i += parts * 64) {
-          const int t = i >> 6, col = nt * 256 + (i & 63) * 4;
+        // This CTA's share of each block's (token, 4 columns) items.  With few items four lanes share one (lane q takes the
+        // token's pairs q, q + 4, ..., then the four sums are added in a fixed tree); two pairs' partials are in flight.
+        int from[2], n_item[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const uint32_t c_lo = run_owner((nt0 + m) * per_nt, f.C, f.B), c_hi = run_owner((nt0 + m + 1) * per_nt - 1, f.C, f.B);
+          const uint32_t parts = c_hi - c_lo + 1, me = cta - c_lo;
+          from[m] = m < two ? static_cast<int>(run_begin(me, parts, T * 64)) : 0;
+          n_item[m] = m < two ? static_cast<int>(run_begin(me + 1, parts, T * 64)) - from[m] : 0;
+        }
+        const int items = n_item[0] + n_item[1];
+        const int lanes_per = items * 4 <= 512 ? 4 : 1, q = et & (lanes_per - 1), groups = 256 / lanes_per;
+        for (int i0 = 0; i0 < items; i0 += groups) {                // the same number of turns for every lane of a warp
+          const int i = i0 + et / lanes_per;
+          const int m = i >= n_item[0] ? 1 : 0, it = (m ? i - n_item[0] + from[1] : i + from[0]);
+          const int t = it >> 6, col = (nt0 + m) * 256 + (it & 63) * 4;
+          const bool on = i < items && col < p.d;
+          const uint8_t* split = L.split + m * A;
+          const int n_pair = on ? s_local[t] : 0;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (col < p.d) {
-#pragma unroll 2
-            for (int s = q; s < k; s += 4) {
-              const int a = L.pa[t * k + s];
-              if (a < 0) continue;
-              const int n = split[a];
-              const float* src = p.y_part + static_cast<size_t>(L.pu[t * k + s]) * p.d + col;
-              float4 v[kFewSplit];
+#pragma unroll 1
+          for (int s = q; s < n_pair; s += 2 * lanes_per) {
+            float4 v[2][kFewSplit];
+            float w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int at = t * k + min(s + h * lanes_per, n_pair - 1);
+              const int n = s + h * lanes_per < n_pair ? split[L.pa[at]] : 0;
+              w[h] = L.w[at];
+              const float* src = p.y_part + static_cast<size_t>(L.pu[at]) * p.d + col;
 #pragma unroll
               for (int j = 0; j < kFewSplit; ++j)
-                v[j] = n > j ? __ldcg(reinterpret_cast<const float4*>(src + j * part_pitch)) : make_float4(0.f, 0.f, 0.f, 0.f);
-              const float w = L.w[t * k + s];
-              acc.x = fmaf(w, v[0].x + v[1].x + v[2].x + v[3].x, acc.x);
-              acc.y = fmaf(w, v[0].y + v[1].y + v[2].y + v[3].y, acc.y);
-              acc.z = fmaf(w, v[0].z + v[1].z + v[2].z + v[3].z, acc.z);
-              acc.w = fmaf(w, v[0].w + v[1].w + v[2].w + v[3].w, acc.w);
+                v[h][j] = n > j ? __ldcg(reinterpret_cast<const float4*>(src + j * part_pitch)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              if (n == 0) w[h] = 0.f;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              acc.x = fmaf(w[h], v[h][0].x + v[h][1].x + v[h][2].x + v[h][3].x, acc.x);
+              acc.y = fmaf(w[h], v[h][0].y + v[h][1].y + v[h][2].y + v[h][3].y, acc.y);
+              acc.z = fmaf(w[h], v[h][0].z + v[h][1].z + v[h][2].z + v[h][3].z, acc.z);
+              acc.w = fmaf(w[h], v[h][0].w + v[h][1].w + v[h][2].w + v[h][3].w, acc.w);
             }
           }
-#pragma unroll
-          for (int o = 1; o < 4; o <<= 1) {
+          for (int o = 1; o < lanes_per; o <<= 1) {
             acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
             acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
             acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
             acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
           }
-          if (q == 0 && col < p.d) {
+          if (on && q == 0) {
             const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
             *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(t) * p.d + col) =
                 make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
           }
         }
+        if (nt0 + 2 <= nt_hi) bar_sync(3, 256);                     // before the table is written again
       }
     }
   }
@@ -708,7 +767,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (tid == 0) atomicAdd(p.leave, 1ull);
+  if (tid == 0) atomicInc(p.leave, 2 * C - 1);
   if (*s_abort) {
     if (tid == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_TIMEOUT));
     for (int i = 0; i < 50; ++i) __nanosleep(1000);      // let copies and MMAs in flight drain
@@ -749,7 +808,7 @@ static cudaError_t launch_few_t(FewParams p, int num_sms, cudaStream_t stream) {
   const int rows = kBf16 ? max(T16, 2 * T8) : 2 * T8;
   p.stage_bytes = (kBBytes + kSfbBytes + rows * 128 + 512 + 1023) / 1024 * 1024;
   p.slots = rows <= 64 ? 2 : 1;
-  const size_t lists = few_list_bytes(p.G, p.T * p.k);
+  const size_t lists = few_list_bytes(p.G, p.T * p.k, p.E);
   p.stages = min(kFewRing, static_cast<int>((kFewBudget - 1024 - lists) / p.stage_bytes));
   const size_t smem = 1024 + static_cast<size_t>(p.stages) * p.stage_bytes + lists;
   cudaError_t e = smem_limit_once(few_kernel<kBf16>, kFewBudget, smem_set);

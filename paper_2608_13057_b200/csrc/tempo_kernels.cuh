@@ -192,7 +192,7 @@ struct FewParams {
   const uint8_t* w2;
   const uint8_t* sf13;
   const uint8_t* sf2;
-  unsigned long long* leave;
+  unsigned int* leave;
   int32_t* counters;
   int counter_ints;
   uint8_t* x_img;
