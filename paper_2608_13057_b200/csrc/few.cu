@@ -27,7 +27,7 @@
 // one is told by a count, modulo twice the grid, that every CTA bumps once as it leaves.  Every wait is bounded (FewParams::wait_ns).
 #include <cuda_fp16.h>
 
-#include "ffn_common.cuh"
+#include "mma_warp.cuh"
 
 namespace tempo {
 
@@ -157,27 +157,6 @@ __device__ __forceinline__ uint32_t few_idesc_fp8(int n, int sf_id) {     // wei
 }
 __device__ __forceinline__ uint32_t few_idesc_bf16(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
-}
-
-// Shared-memory descriptor of a K-major operand in the 128-byte swizzle (rows of 128 bytes, groups of 8 rows 1024 bytes
-// apart): only its low word differs from tile to tile.
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ void few_mma_fp8(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                            uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "mov.b64 da, {%1, %7};\n\tmov.b64 db, {%2, %7};\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], da, db, %3, [%5], [%6], p;\n\t}"
-      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(kDescHi) : "memory");
-}
-__device__ __forceinline__ void few_mma_bf16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
-      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
 }
 
 struct FewLists {                          // in dynamic shared memory behind the ring
@@ -451,56 +430,57 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     }
   } else if (warp == 1) {
     // ---- MMA issuer ------------------------------------------------------------------------------------
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0, n_seg = 0;
-      // One thread issues everything, so what it computes per block counts: descriptors are a low word plus a constant.
-      const uint32_t bars = smem_u32(s_bars), desc_lo = ((smem_base >> 4) & 0x3fffu) | (1u << 16), desc_step = p.stage_bytes >> 4;
-      uint32_t sf_slot = tmem_base + kSfCol0, tok_slot = tmem_base + kSfCol0 + 16u;      // two of each, used in turn
-      bool ok = true;
+    const uint32_t leader = elect_one();
+    const uint32_t bars = smem_u32(s_bars), desc0 = desc_lo_sw128(smem_base), desc_step = p.stage_bytes >> 4;
+    uint32_t sf_slot = tmem_base + kSfCol0, tok_slot = tmem_base + kSfCol0 + 16u;        // two of each, used in turn
+    uint32_t stage = 0, phase = 0, n_seg = 0;
+    bool ok = true;
 #pragma unroll 1
-      for (int ph = 0; ph < 4; ++ph) {
-        FewIter s(p, s_phase[ph], ph >= 2);
-        while (ok && s.next()) {
-          const int N = ph < 2 ? R1 : 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7);
-          const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
-          ++n_seg;
-          if (!mbar_wait(smem_u32(&s_acc_empty[slot]), (use & 1u) ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+    for (int ph = 0; ph < 4 && ok; ++ph) {
+      FewIter s(p, s_phase[ph], ph >= 2);
+      while (ok && warp_uniform(s.next()) != 0) {
+        const int N = warp_uniform(ph < 2 ? R1 : 2 * ((L.off[s.a + 1] - L.off[s.a] + 7) & ~7));
+        const int kb0 = warp_uniform(s.kb0), kb1 = warp_uniform(s.kb1);
+        const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
+        ++n_seg;
+        if (!mbar_wait_warp(smem_u32(&s_acc_empty[slot]), (use & 1u) ^ 1u, s_abort, p.wait_ns)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t acc = tmem_base + slot * 128u, acc2 = acc + N;
+        const uint32_t idesc0 = kBf16 ? few_idesc_bf16(N) : few_idesc_fp8(N, 0);
+        uint32_t accumulate = 0;
+#pragma unroll 1
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!mbar_wait_warp(bars + 8 * stage, phase, s_abort, p.wait_ns) ||
+              !mbar_wait_warp(bars + 8 * (kFewRing + stage), phase, s_abort, p.wait_ns)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t acc = tmem_base + slot * 128u, acc2 = acc + N;
-          const uint32_t idesc0 = kBf16 ? few_idesc_bf16(N) : few_idesc_fp8(N, 0);
-          uint32_t accumulate = 0;
-#pragma unroll 1
-          for (int kb = s.kb0; kb < s.kb1; ++kb) {
-            if (!mbar_wait(bars + 8 * stage, phase, s_abort, p.wait_ns) ||
-                !mbar_wait(bars + 8 * (kFewRing + stage), phase, s_abort, p.wait_ns)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t da = desc_lo + stage * desc_step, db = da + ((kBBytes + kSfbBytes) >> 4), da2 = da + ((kTileM * 128) >> 4);
-            if constexpr (kBf16) {
+          const uint32_t da = desc0 + stage * desc_step, db = da + ((kBBytes + kSfbBytes) >> 4), da2 = da + ((kTileM * 128) >> 4);
+          if constexpr (kBf16) {
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) few_mma_bf16(acc, da + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
+            for (int ks = 0; ks < 4; ++ks) warp_mma_bf16(leader, acc, da + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) few_mma_bf16(acc2, da2 + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
-            } else {
-              const uint32_t sSF = smem_base + stage * p.stage_bytes + kBBytes;
-              if ((kb & 3) == 0 || accumulate == 0) {
-                sf_slot ^= 8u;
-                tc_cp_sf(sf_slot, smem_desc_sf(sSF));
-                tc_cp_sf(sf_slot + 4, smem_desc_sf(sSF + 512));
-              }
-              tok_slot ^= 4u;
-              tc_cp_sf(tok_slot, smem_desc_sf(sSF + kSfbBytes + N * 128));
-              const uint32_t idesc = idesc0 | static_cast<uint32_t>(kb & 3) << 29;
-#pragma unroll
-              for (int ks = 0; ks < 4; ++ks) few_mma_fp8(acc, da + 2 * ks, db + 2 * ks, idesc, sf_slot, tok_slot, ks == 0 ? accumulate : 1u);
-#pragma unroll
-              for (int ks = 0; ks < 4; ++ks) few_mma_fp8(acc2, da2 + 2 * ks, db + 2 * ks, idesc, sf_slot + 4, tok_slot, ks == 0 ? accumulate : 1u);
+            for (int ks = 0; ks < 4; ++ks) warp_mma_bf16(leader, acc2, da2 + 2 * ks, db + 2 * ks, idesc0, ks == 0 ? accumulate : 1u);
+          } else {
+            const uint32_t sSF = smem_base + stage * p.stage_bytes + kBBytes;
+            if ((kb & 3) == 0 || accumulate == 0) {
+              sf_slot ^= 8u;
+              warp_cp_sf(leader, sf_slot, sSF);
+              warp_cp_sf(leader, sf_slot + 4, sSF + 512);
             }
-            accumulate = 1;
-            tc_commit(bars + 8 * (2 * kFewRing + stage));
-            if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+            tok_slot ^= 4u;
+            warp_cp_sf(leader, tok_slot, sSF + kSfbBytes + N * 128);
+            const uint32_t idesc = idesc0 | static_cast<uint32_t>(kb & 3) << 29;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              warp_mma_fp8(leader, acc, da + 2 * ks, db + 2 * ks, idesc, sf_slot, tok_slot, ks == 0 ? accumulate : 1u);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              warp_mma_fp8(leader, acc2, da2 + 2 * ks, db + 2 * ks, idesc, sf_slot + 4, tok_slot, ks == 0 ? accumulate : 1u);
           }
-          if (ok) tc_commit(smem_u32(&s_acc_full[slot]));
+          accumulate = 1;
+          warp_commit(leader, bars + 8 * (2 * kFewRing + stage));
+          if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
         }
+        if (ok) warp_commit(leader, smem_u32(&s_acc_full[slot]));
       }
     }
   } else if (warp >= 4) {

@@ -11,7 +11,7 @@
 // break ties towards the lowest index.  Logits, scores and weights stay in 32 bits.
 //
 // A logit that is not finite counts as minus infinity: it is chosen after every finite one, with weight 0.
-#include "ffn_common.cuh"
+#include "mma_warp.cuh"
 
 namespace tempo {
 
@@ -169,27 +169,30 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
       for (int c = 0; c < p.w_boxes; ++c) tma_load_2d(sW + c * p.w_box * 128, &tmW, full, kb * kBlockK, c * p.w_box);
       if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
     }
-  } else if (work && warp == 1 && lane == 0) {
-    uint32_t stage = 0, phase = 0;
+  } else if (work && warp == 1) {
+    const uint32_t leader = elect_one();
+    const uint32_t full0 = smem_u32(s_full), empty0 = smem_u32(s_empty), desc0 = desc_lo_sw128(smem_base), desc_step = p.stage_bytes >> 4;
+    uint32_t stage = 0, phase = 0, accumulate = 0;
     bool ok = true;
     for (int kb = kb0; kb < kb1; ++kb) {
-      if (!mbar_wait(smem_u32(&s_full[stage]), phase, s_abort, kDefaultWaitNs)) { ok = false; break; }
+      if (!mbar_wait_warp(full0 + 8 * stage, phase, s_abort, kDefaultWaitNs)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t sX = smem_base + stage * p.stage_bytes, sW = sX + kABytes;
-      const uint64_t da = smem_desc_sw128(sX);
+      const uint32_t da = desc0 + stage * desc_step;
+      uint32_t db = da + (kABytes >> 4), acc = tmem_base;
       for (int c = 0; c < p.w_boxes; ++c) {
         const int n = min(p.w_box, p.E16 - c * p.w_box);
-        const uint64_t db = smem_desc_sw128(sW + c * p.w_box * 128);
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) |
                                (static_cast<uint32_t>(kTileM >> 4) << 24);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          tc_mma_bf16(tmem_base + c * p.w_box, da + 2u * ks, db + 2u * ks, idesc, (kb > kb0 || ks != 0) ? 1u : 0u);
+        for (int ks = 0; ks < 4; ++ks) warp_mma_bf16(leader, acc, da + 2 * ks, db + 2 * ks, idesc, ks == 0 ? accumulate : 1u);
+        db += (p.w_box * 128) >> 4;
+        acc += p.w_box;
       }
-      tc_commit(smem_u32(&s_empty[stage]));
+      accumulate = 1;
+      warp_commit(leader, empty0 + 8 * stage);
       if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
     }
-    if (ok) tc_commit(smem_u32(&s_acc));
+    if (ok) warp_commit(leader, smem_u32(&s_acc));
   }
   __syncwarp();
   // Partial logits to shared memory: lane = token row of the warp's quadrant, so a column of 32 rows is one
