@@ -7,15 +7,15 @@
 // (tokens x 64 and experts x 64 bf16 values, 128-byte swizzle), tcgen05.mma.kind::f16 (M 128, N = experts) into tensor
 // memory, the partial logits to shared memory; then the CTAs share the tile's tokens out, and a warp sums a token's S
 // partials in rank order (the same bits every time) over distributed shared memory and picks its experts:
-// every lane holds E/32 logits, k rounds of a warp-wide maximum on order-preserving integer keys take the best left and
-// break ties towards the lowest index.  Logits, scores and weights stay in 32 bits.
+// every lane holds up to 16 logits, and rounds of a warp-wide maximum on order-preserving integer keys take the best left;
+// ties go to the lowest index.  Logits, scores and weights stay in 32 bits.
 //
 // A logit that is not finite counts as minus infinity: it is chosen after every finite one, with weight 0.
 #include "mma_warp.cuh"
 
 namespace tempo {
 
-constexpr int kRouteThreads = 256;
+constexpr int kRouteThreads = 512;
 constexpr int kRouteMaxStages = 8;
 constexpr int kRouteRing = 200 * 1024;
 
@@ -31,7 +31,12 @@ __device__ __forceinline__ uint32_t map_peer(uint32_t addr, uint32_t rank) {
 }
 __device__ __forceinline__ float ld_peer(uint32_t addr) {
   float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
 // Larger floats have larger keys; finite values only, never 0 or 1.
@@ -39,89 +44,229 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t u = __float_as_uint(v + 0.f);           // -0 and +0 tie
   return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
+constexpr uint32_t kLeastFinite = 0x00800000u;           // key of the lowest finite value (that of -inf is the one below)
+__device__ __forceinline__ float from_key(uint32_t k) {
+  return __uint_as_float(k ^ ((k >> 31) != 0 ? 0x80000000u : 0xffffffffu));
+}
+// Expert of a lane's j-th logit: four neighbours per 16-byte load, 128 to a warp.
+__device__ __forceinline__ int expert_of(int j, int lane) { return 128 * (j >> 2) + 4 * lane + (j & 3); }
 // Rounded step by step, without contraction: the choice among biased scores must not depend on how the compiler fuses.
 __device__ __forceinline__ float sigmoid_rn(float l) { return __fdiv_rn(1.f, __fadd_rn(1.f, expf(-l))); }
 
-struct RouteRow {
-  const RouteParams* p;
-  float mx, sum;
-  __device__ float score(float l) const {
-    if (!isfinite(l)) return 0.f;
-    return p->sigmoid ? sigmoid_rn(l) : __fdiv_rn(expf(l - mx), sum);
-  }
-};
-
-// One warp, one token: J logits per lane (expert lane + 32 j).
+// Descending order of a lane's J keys (J = 4, 8, 16: odd-even merge network, 5, 19 or 63 exchanges).
 template <int J>
-__device__ __forceinline__ void pick(const RouteParams& p, int t, const float (&l)[J], int lane) {
-  RouteRow row{&p, 0.f, 1.f};
-  bool bad = false;
+__device__ __forceinline__ void sort_keys(uint32_t (&v)[J]) {
 #pragma unroll
-  for (int j = 0; j < J; ++j) bad |= lane + 32 * j < p.E && !isfinite(l[j]);
-  if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_LOGIT));
-  if (!p.sigmoid) {
-    uint32_t m = 0;
+  for (int w = 1; w < J; w *= 2)
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      if (lane + 32 * j < p.E && isfinite(l[j])) m = max(m, order_key(l[j]));
-    m = __reduce_max_sync(0xffffffffu, m);
-    row.mx = m == 0 ? 0.f : __uint_as_float(m ^ ((m >> 31) != 0 ? 0x80000000u : 0xffffffffu));
-    float s = 0.f;
+    for (int q = w; q >= 1; q /= 2)
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      if (lane + 32 * j < p.E && isfinite(l[j])) s += expf(l[j] - row.mx);
+      for (int j = q % w; j + q < J; j += 2 * q)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    row.sum = s > 0.f ? s : 1.f;
+        for (int i = 0; i < q; ++i)
+          if (j + i + q < J && (j + i) / (2 * w) == (j + i + q) / (2 * w)) {
+            const uint32_t a = v[j + i], b = v[j + i + q];
+            v[j + i] = max(a, b);
+            v[j + i + q] = min(a, b);
+          }
+}
+
+__device__ __forceinline__ float exact_score(const RouteParams& p, float l, float mx, float sum) {
+  return p.sigmoid ? sigmoid_rn(l) : __fdiv_rn(expf(l - mx), sum);
+}
+// The logit of expert `id` (every lane asks for its own), from the lane that holds it; an index into the registers would
+// put them into local memory.
+template <int J>
+__device__ __forceinline__ float lane_logit(const float (&l)[J], int id) {
+  float r = 0.f;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const float v = __shfl_sync(0xffffffffu, l[j], (id >> 2) & 31);
+    if (j == ((id >> 7) << 2 | (id & 3))) r = v;
   }
+  return r;
+}
+// Whether two candidates' keys (both of finite scores, a >= b) may stand in the wrong order.  Without a bias the scores are
+// the logits and only the cut bits are open; a biased score is off by less than 2^-19 of its terms, which are below 1 + |a|.
+__device__ __forceinline__ bool too_near(const RouteParams& p, uint32_t a, uint32_t b, uint32_t mask) {
+  const float fa = from_key(a & ~mask), fb = from_key(b & ~mask);
+  return (a & ~mask) - (b & ~mask) <= mask + 1u || (p.bias != nullptr && fa - fb <= 0x1p-17f * (1.f + fabsf(fa)));
+}
+// The exact choice among all experts: k rounds of a warp-wide maximum on exact keys, ties to the lowest expert.  Lane s < k
+// gets the s-th, and whether its score is finite.
+template <int J>
+__device__ __forceinline__ void choose_exact(const RouteParams& p, const float (&l)[J], const float (&bias)[J], float mx, float sum,
+                                             int lane, int& my_id, bool& my_fine) {
   uint32_t key[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const int e = lane + 32 * j;
-    key[j] = 0;
-    if (e < p.E) {
-      float v = l[j];
-      if (p.bias != nullptr) v = isfinite(v) ? __fadd_rn(row.score(v), __ldg(p.bias + e)) : v;
-      key[j] = isfinite(v) ? order_key(v) : 1u;
-    }
+    float v = l[j];
+    if (p.bias != nullptr && isfinite(v)) v = __fadd_rn(exact_score(p, v, mx, sum), bias[j]);   // bias -inf: taken out
+    key[j] = expert_of(j, lane) >= p.E ? 0u : isfinite(v) ? order_key(v) : 1u;
   }
-  int my_id = 0;
-  float my_l = 0.f;
+#pragma unroll 1
   for (int s = 0; s < p.k; ++s) {
-    uint32_t best = 0;
-    int bj = 0;
-    float bl = 0.f;
+    uint32_t best = key[0];
+#pragma unroll
+    for (int j = 1; j < J; ++j) best = max(best, key[j]);
+    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+    int jj = J;
+#pragma unroll
+    for (int j = J - 1; j >= 0; --j)
+      if (key[j] == top) jj = j;
+    const uint32_t mine = best == top ? static_cast<uint32_t>(expert_of(jj, lane)) : 0xffffffffu;
+    const uint32_t e = __reduce_min_sync(0xffffffffu, mine);
+    if (lane == s) { my_id = static_cast<int>(e); my_fine = top > 1; }
+    const int gone = mine == e ? jj : J;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (key[j] > best) { best = key[j]; bj = j; bl = l[j]; }
-    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-    const uint32_t e = __reduce_min_sync(0xffffffffu, best == top ? static_cast<uint32_t>(lane + 32 * bj) : 0xffffffffu);
-    const float el = __shfl_sync(0xffffffffu, bl, static_cast<int>(e & 31u));
-    if (lane == s) { my_id = static_cast<int>(e); my_l = el; }
-    if (static_cast<uint32_t>(lane) == (e & 31u)) {
+      if (j == gone) key[j] = 0;
+  }
+}
+
+// Sum of a token's partial logits over the cluster's CTAs, in rank order.
+template <int JJ>
+__device__ __forceinline__ void gather(const RouteParams& p, uint32_t row_addr, int lane, float (&l)[4 * JJ]) {
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (j == static_cast<int>(e >> 5)) key[j] = 0;
+  for (int j = 0; j < 4 * JJ; ++j) l[j] = 0.f;
+  // kAhead CTAs' partials are requested before any is added
+  constexpr int kAhead = JJ == 1 ? 8 : JJ == 2 ? 4 : 2;
+#pragma unroll 1
+  for (int q0 = 0; q0 < p.splits; q0 += kAhead) {
+    float4 v[kAhead][JJ];
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (q0 + q < p.splits) {
+        const uint32_t peer = map_peer(row_addr, q0 + q);
+#pragma unroll
+        for (int j = 0; j < JJ; ++j) v[q][j] = ld_peer4(peer + 4u * min(128 * j + 4 * lane, p.E16 - 4));
+      }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (q0 + q < p.splits) {
+#pragma unroll
+        for (int j = 0; j < JJ; ++j) {
+          l[4 * j] += v[q][j].x; l[4 * j + 1] += v[q][j].y;
+          l[4 * j + 2] += v[q][j].z; l[4 * j + 3] += v[q][j].w;
+        }
+      }
+  }
+}
+
+// One warp, one token: J logits per lane.
+//
+// Candidates, a few more than k, are found on keys that carry the expert: the upper bits of the order-preserving key of the
+// score, the lower bits count the experts down.  A lane sorts its keys once; a round is then a warp-wide maximum of the
+// lanes' first keys, and the winner moves its list up.  The upper bits leave out the score's last 7 to 9 bits, and a biased
+// score comes from the fast exponential and division.  Where neighbours among the first k + 1 are nearer than that can be
+// off, the candidates are ordered again by exact keys, a lane each (one or two tokens in 100 on normal logits); where even the
+// last candidate is that near to the k-th, or a logit is not finite, all experts are.
+template <int J>
+__device__ __forceinline__ void pick(const RouteParams& p, int t, const float (&l)[J], const float (&bias)[J], int lane) {
+  constexpr int kBits = J == 4 ? 7 : J == 8 ? 8 : 9;
+  constexpr uint32_t kMask = (1u << kBits) - 1u;
+  float zero = 0.f;                                      // stays 0 while every logit is finite
+#pragma unroll
+  for (int j = 0; j < J; ++j) zero = fmaf(l[j], 0.f, zero);
+  const bool bad = __any_sync(0xffffffffu, zero != 0.f);   // NaN != 0
+  if (bad && lane == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_LOGIT));
+  // Softmax: the row's maximum and sum, where a weight or a biased key needs them (renormalised weights without a bias
+  // do not: the sum cancels, and the first expert chosen has the maximum).
+  const bool whole = !p.sigmoid && (!p.renormalise || p.bias != nullptr);
+  float mx = 0.f, sum = 1.f;
+  if (whole) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (expert_of(j, lane) < p.E && isfinite(l[j])) m = max(m, order_key(l[j]));
+    m = __reduce_max_sync(0xffffffffu, m);
+    mx = m == 0 ? 0.f : from_key(m);
+    float v = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (expert_of(j, lane) < p.E && isfinite(l[j])) v += expf(l[j] - mx);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    sum = v > 0.f ? v : 1.f;
+  }
+  int id = 0;
+  bool fine = false;                                     // finite logit, finite bias
+  bool again = bad || p.k == 32;                         // 32 choices leave no lane for the first left out
+  uint32_t mine = 0;                                     // lane s: the s-th candidate (0: there are no more experts)
+  const int m = min(p.k + 4, 32);
+  if (!again) {
+    const float inv_sum = 1.f / sum;
+    uint32_t key[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float v = l[j];
+      if (p.bias != nullptr) v = (p.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __expf(v - mx) * inv_sum) + bias[j];
+      key[j] = expert_of(j, lane) >= p.E ? 0u : (order_key(v) & ~kMask) | (kMask - static_cast<uint32_t>(expert_of(j, lane)));
     }
-  }
-  float w = 0.f;
-  if (lane < p.k) {
-    w = row.score(my_l);
-    if (p.bias != nullptr && !isfinite(__ldg(p.bias + my_id))) w = 0.f;   // an expert that the bias takes out
-  }
-  if (p.renormalise) {
-    float s = w;
+    sort_keys<J>(key);
+#pragma unroll 1
+    for (int s = 0; s < m; ++s) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
+      if (lane == s) mine = top;
+      const bool won = key[0] == top;                    // keys differ, except the zeros
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    w = s > 0.f ? __fdiv_rn(w, s) : 0.f;
+      for (int j = 0; j + 1 < J; ++j) key[j] = won ? key[j + 1] : key[j];
+      key[J - 1] = won ? 0u : key[J - 1];
+    }
+    id = static_cast<int>(kMask - (mine & kMask));
+    fine = mine >= kLeastFinite;
+    const uint32_t below = __shfl_down_sync(0xffffffffu, mine, 1);
+    again = __any_sync(0xffffffffu, lane < p.k && below >= kLeastFinite && too_near(p, mine, below, kMask));
+  }
+  float el = lane_logit<J>(l, id);
+  if (again) {
+    const uint32_t kth = __shfl_sync(0xffffffffu, mine, p.k - 1), last = __shfl_sync(0xffffffffu, mine, m - 1);
+    if (!bad && m > p.k && (last < kLeastFinite || !too_near(p, kth, last, kMask))) {
+      uint32_t exact = 0;
+      if (mine != 0) {
+        float v = el;
+        if (p.bias != nullptr) {
+          const float b = __ldg(p.bias + id);
+          v = isfinite(b) ? __fadd_rn(exact_score(p, v, mx, sum), b) : b;
+        }
+        exact = isfinite(v) ? order_key(v) : 1u;
+      }
+      int rank = 0;
+      for (int s = 0; s < m; ++s) {
+        const uint32_t o = __shfl_sync(0xffffffffu, exact, s);
+        const int oid = __shfl_sync(0xffffffffu, id, s);
+        rank += o > exact || (o == exact && oid < id) ? 1 : 0;
+      }
+      const uint32_t self = static_cast<uint32_t>(id) | (exact > 1u ? 0x80000000u : 0u);
+      uint32_t got = 0;
+      for (int s = 0; s < m; ++s) {
+        const int r = __shfl_sync(0xffffffffu, rank, s);
+        const uint32_t v = __shfl_sync(0xffffffffu, self, s);
+        if (r == lane) got = v;
+      }
+      id = static_cast<int>(got & 0x7fffffffu);
+      fine = (got >> 31) != 0;
+    } else {
+      choose_exact<J>(p, l, bias, mx, sum, lane, id, fine);
+    }
+    el = lane_logit<J>(l, id);
+  }
+  if (!whole) mx = __shfl_sync(0xffffffffu, el, 0);
+  float w = 0.f;
+  if (lane < p.k && fine) w = exact_score(p, el, mx, sum);
+  if (p.renormalise) {
+    float v = w;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    w = v > 0.f ? __fdiv_rn(w, v) : 0.f;
   }
   if (lane < p.k) {
-    p.ids[static_cast<size_t>(t) * p.k + lane] = my_id;
+    p.ids[static_cast<size_t>(t) * p.k + lane] = id;
     p.w[static_cast<size_t>(t) * p.k + lane] = w * p.scale;
   }
 }
 
-template <int J>
+template <int JJ>
 __global__ void __launch_bounds__(kRouteThreads, 1)
 route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const RouteParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -159,15 +304,23 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
   const int live = max(0, min(p.tile_rows, nv - t0));   // the same in every CTA of the cluster
   const int kb0 = static_cast<int>(rank) * p.Kb / S, kb1 = (static_cast<int>(rank) + 1) * p.Kb / S;
   const bool work = live > 0 && kb1 > kb0;
-  if (work && warp == 0 && lane == 0) {
-    uint32_t stage = 0, phase = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (!mbar_wait(smem_u32(&s_empty[stage]), phase ^ 1u, s_abort, kDefaultWaitNs)) break;
+  if (work && warp == 0) {
+    // The ring is empty at first: one lane per stage issues its loads (one thread takes 0.2 us per block).
+    auto load = [&](int kb, uint32_t stage) {
       const uint32_t full = smem_u32(&s_full[stage]), sX = smem_base + stage * p.stage_bytes, sW = sX + kABytes;
       mbar_arrive_expect_tx(full, p.x_box * 128 + p.w_boxes * p.w_box * 128);
       tma_load_2d(sX, &tmX, full, kb * kBlockK, t0);
       for (int c = 0; c < p.w_boxes; ++c) tma_load_2d(sW + c * p.w_box * 128, &tmW, full, kb * kBlockK, c * p.w_box);
-      if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+    };
+    if (lane < p.stages && kb0 + lane < kb1) load(kb0 + lane, lane);
+    __syncwarp();
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      for (int kb = kb0 + p.stages; kb < kb1; ++kb) {
+        if (!mbar_wait(smem_u32(&s_empty[stage]), phase, s_abort, kDefaultWaitNs)) break;
+        load(kb, stage);
+        if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
+      }
     }
   } else if (work && warp == 1) {
     const uint32_t leader = elect_one();
@@ -195,18 +348,28 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
     if (ok) warp_commit(leader, smem_u32(&s_acc));
   }
   __syncwarp();
-  // Partial logits to shared memory: lane = token row of the warp's quadrant, so a column of 32 rows is one
-  // conflict-free store (the pitch is odd).  The ring is free: every MMA that read it has completed.
+  // Partial logits to shared memory: lane = token row of the warp's quadrant; 16-byte stores at a pitch of 4 words more than
+  // a multiple of 32 touch every bank once per eight lanes, and so do the reads along a row.  The ring is free: every MMA
+  // that read it has completed.
   float* logits = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)));
-  const int pitch = p.E16 + 1;
-  const int row = (warp & 3) * 32 + lane;
+  const uint32_t logits_addr = smem_u32(logits);
+  const int pitch = p.pitch;
+  constexpr int J = 4 * JJ, kWarps = kRouteThreads / 32;
   bool have = work;
   if (work) {
     have = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_acc), 0, s_abort, kDefaultWaitNs));
     tc_fence_after();
   }
+  float bias[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int e = 128 * (j / 4) + 4 * lane + j % 4;
+    const float b = p.bias != nullptr && e < p.E ? __ldg(p.bias + e) : 0.f;
+    bias[j] = isfinite(b) ? b : -INFINITY;               // a bias that is not finite takes its expert out
+  }
   if ((warp & 3) * 32 < live) {
-    for (int c = (warp >> 2) * 16; c < p.E16; c += 32) {
+    const int row = (warp & 3) * 32 + lane;
+    for (int c = (warp >> 2) * 16; c < p.E16; c += 16 * (kRouteThreads / 128)) {
       uint32_t v[16];
       if (have) {
         asm volatile(
@@ -221,32 +384,26 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
       }
       if (row < live) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) logits[row * pitch + c + i] = __uint_as_float(v[i]);
+        for (int i = 0; i < 16; i += 4)
+          st_shared_v4(logits_addr + 4u * (row * pitch + c + i), make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]));
       }
     }
   }
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  // The tile's tokens are dealt to the cluster's CTAs and their warps.
-  const uint32_t logits_addr = smem_u32(logits);
-  for (int r = static_cast<int>(rank) + S * warp; r < p.tile_rows && t0 + r < p.T; r += S * (kRouteThreads / 32)) {
+  // The tokens are dealt to the cluster's CTAs and their warps.
+  for (int r = static_cast<int>(rank) + S * warp; r < p.tile_rows && t0 + r < p.T; r += S * kWarps) {
+    const int t = t0 + r;
     if (r >= live) {                                     // a padding row
       if (lane < p.k) {
-        p.ids[static_cast<size_t>(t0 + r) * p.k + lane] = -1;
-        p.w[static_cast<size_t>(t0 + r) * p.k + lane] = 0.f;
+        p.ids[static_cast<size_t>(t) * p.k + lane] = -1;
+        p.w[static_cast<size_t>(t) * p.k + lane] = 0.f;
       }
       continue;
     }
     float l[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) l[j] = 0.f;
-    for (int q = 0; q < S; ++q) {
-      const uint32_t src = map_peer(logits_addr, q) + static_cast<uint32_t>(r * pitch + lane) * 4u;
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (lane + 32 * j < p.E) l[j] += ld_peer(src + 128u * j);
-    }
-    pick<J>(p, t0 + r, l, lane);
+    gather<JJ>(p, logits_addr + 4u * static_cast<uint32_t>(r * pitch), lane, l);
+    pick<J>(p, t, l, bias, lane);
   }
   // nobody leaves while a peer may still read its logits
   __syncwarp();
@@ -263,11 +420,11 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
   }
 }
 
-template <int J>
+template <int JJ>
 static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW, const RouteParams& p, int ctas,
                                   size_t smem, cudaStream_t stream) {
   static std::atomic<unsigned long long> smem_set{0};
-  cudaError_t e = smem_limit_once(route_kernel<J>, 227 * 1024 - 1024, smem_set);
+  cudaError_t e = smem_limit_once(route_kernel<JJ>, 227 * 1024 - 1024, smem_set);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
@@ -282,19 +439,20 @@ static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, route_kernel<J>, tmX, tmW, p);
+  return cudaLaunchKernelEx(&cfg, route_kernel<JJ>, tmX, tmW, p);
 }
 
 RoutePlan route_plan(int T, int E, int d, int num_sms) {
   RoutePlan r;
   r.E16 = (E + 15) / 16 * 16;
+  const int Kb = d / 64;
   r.tile_rows = E <= 256 ? 128 : 64;
   r.x_box = min(r.tile_rows, (T + 7) / 8 * 8);
   r.w_box = min(r.E16, 256);
   r.w_boxes = (r.E16 + 255) / 256;
   r.stage_bytes = kABytes + r.w_boxes * r.w_box * 128;
   r.stages = min(kRouteMaxStages, kRouteRing / r.stage_bytes);
-  const int tiles = (T + r.tile_rows - 1) / r.tile_rows, Kb = d / 64;
+  const int tiles = (T + r.tile_rows - 1) / r.tile_rows;
   r.splits = 1;
   while (r.splits < 8 && 2 * r.splits * tiles <= num_sms && 2 * r.splits <= Kb) r.splits *= 2;
   r.ctas = tiles * r.splits;
@@ -310,17 +468,15 @@ cudaError_t launch_route(const CUtensorMap& tmX, const CUtensorMap& tmW, RoutePa
   p.stage_bytes = r.stage_bytes;
   p.stages = r.stages;
   p.splits = r.splits;
+  p.pitch = (r.E16 + 31) / 32 * 32 + 4;
   p.tmem_cols = 32;
   while (p.tmem_cols < r.E16) p.tmem_cols *= 2;
   const size_t ring = static_cast<size_t>(r.stages) * r.stage_bytes;
-  const size_t table = static_cast<size_t>(r.tile_rows) * (r.E16 + 1) * 4;
+  const size_t table = static_cast<size_t>(r.tile_rows) * p.pitch * 4;
   const size_t smem = (ring > table ? ring : table) + 1024;
-  const int J = (p.E + 31) / 32;
-  if (J <= 1) return launch_route_t<1>(tmX, tmW, p, r.ctas, smem, stream);
-  if (J <= 2) return launch_route_t<2>(tmX, tmW, p, r.ctas, smem, stream);
-  if (J <= 4) return launch_route_t<4>(tmX, tmW, p, r.ctas, smem, stream);
-  if (J <= 8) return launch_route_t<8>(tmX, tmW, p, r.ctas, smem, stream);
-  return launch_route_t<16>(tmX, tmW, p, r.ctas, smem, stream);
+  if (p.E <= 128) return launch_route_t<1>(tmX, tmW, p, r.ctas, smem, stream);
+  if (p.E <= 256) return launch_route_t<2>(tmX, tmW, p, r.ctas, smem, stream);
+  return launch_route_t<4>(tmX, tmW, p, r.ctas, smem, stream);
 }
 
 }  // namespace tempo

@@ -168,7 +168,7 @@ struct RouteParams {
   int32_t* ids;
   float* w;
   uint32_t* status;
-  int E16, tile_rows, x_box, w_box, w_boxes, stage_bytes, stages, splits, tmem_cols;   // from the plan
+  int E16, tile_rows, x_box, w_box, w_boxes, stage_bytes, stages, splits, tmem_cols, pitch;   // from the plan
 };
 RoutePlan route_plan(int T, int E, int d, int num_sms);
 cudaError_t launch_route(const CUtensorMap& tmX, const CUtensorMap& tmW, RouteParams p, const RoutePlan& r, cudaStream_t stream);
