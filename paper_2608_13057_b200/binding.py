@@ -374,10 +374,13 @@ def tempo_norm_out(y, r, r_out, post_w=None, post_b=None, gate=None, next_w=None
         g32 = gate.dtype is _F32
         if not g32 and gate.dtype is not _BF16:
             raise TempoError(f"gate: expected dtype {_BF16} or {_F32}, got {gate.dtype}")
-        try:
-            gate_row, gate_col = gate.expand(shape).stride()
-        except RuntimeError:
-            raise TempoError(f"gate: shape {tuple(gate.shape)} does not broadcast to {tuple(shape)}") from None
+        if gate.dim() == 2 and gate.shape == (T, 1):                # one per token, the shape that needs no broadcast view
+            gate_row = gate.stride(0)
+        else:
+            try:
+                gate_row, gate_col = gate.expand(shape).stride()
+            except RuntimeError:
+                raise TempoError(f"gate: shape {tuple(gate.shape)} does not broadcast to {tuple(shape)}") from None
         pg = gate.data_ptr()
     a = _NORM.pack(T, d, kind, dtype is _F32, ptype is _F32, g32, ld_y, ld_r, ld_ro, ld_x, gate_row, gate_col, eps, r_scale,
                    y_scale)

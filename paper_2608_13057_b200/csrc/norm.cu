@@ -25,6 +25,10 @@ __device__ __forceinline__ void load_bf16_stream(const __nv_bfloat16* p, uint32_
   }
 }
 
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
 template <int VEC>
 __device__ __forceinline__ void widen(const uint32_t (&u)[(VEC + 1) / 2], float (&v)[VEC]) {
 #pragma unroll
@@ -128,114 +132,216 @@ __device__ __forceinline__ float cta_sum(float v, float (&s_part)[2][32], int sl
   return t;
 }
 
-// v (CH chunks of VEC values of this thread; those beyond the row are zero) -> normed in place, without weights.
+// Two 32-bit operations per instruction: with bf16 operands a row costs more instructions than bytes, so the arithmetic is
+// done on pairs (the issue slots, not HBM, bounded the scalar form: 35 instructions an element, 0.65 issued per clock).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 r, a, b;\n\tmov.b64 {%0, %1}, r;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 r, a, b;\n\tmov.b64 {%0, %1}, r;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 r, a, b, c;\n\tmov.b64 {%0, %1}, r;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+// A thread's values of a row: CH chunks of VEC neighbours, as pairs.  kSplit (rows that no vector divides or aligns): a
+// chunk is two single elements, blockDim.x columns apart, so that a warp still reads neighbours; the second may lie beyond the
+// row when the first does not.
 template <int VEC, int CH>
-__device__ __forceinline__ void norm_row(float (&v)[CH][VEC], const bool (&on)[CH], int layer, float inv_d, float eps,
-                                         float (&s_part)[2][32], int& slot, int warps) {
+struct RowVals { float2 v[CH][VEC / 2]; };
+template <int CH>
+struct Cols {
+  int col[CH];
+  bool on[CH], on2[CH];      // first, second element of a split chunk inside the row
+  int nt;                    // distance of a split chunk's elements
+};
+template <int VEC, int CH, bool kSplit, bool kFull>
+__device__ __forceinline__ void set_cols(Cols<CH>& k, int d) {
+  k.nt = static_cast<int>(blockDim.x);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    k.col[c] = kSplit ? 2 * c * k.nt + static_cast<int>(threadIdx.x) : (c * k.nt + static_cast<int>(threadIdx.x)) * VEC;
+    k.on[c] = kFull || k.col[c] < d;
+    k.on2[c] = kSplit ? k.col[c] + k.nt < d : k.on[c];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void to_pairs(const float (&f)[VEC], float2 (&v)[VEC / 2]) {
+#pragma unroll
+  for (int i = 0; i < VEC / 2; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+}
+template <int VEC, bool kSplit>
+__device__ __forceinline__ void load_bf16_chunk(const __nv_bfloat16* p, uint32_t (&u)[VEC / 2], int nt, bool on2) {
+  if constexpr (kSplit) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    u[0] = q[0] | (on2 ? static_cast<uint32_t>(q[nt]) << 16 : 0u);
+  } else {
+    load_bf16_stream<VEC>(p, u);
+  }
+}
+template <int VEC, bool kSplit>
+__device__ __forceinline__ void load_f32_chunk(const float* p, float (&f)[VEC], int nt, bool on2) {
+  if constexpr (kSplit) {
+    f[0] = p[0];
+    f[1] = on2 ? p[nt] : 0.f;
+  } else {
+    load_f32_stream<VEC>(p, f);
+  }
+}
+template <int VEC, bool kSplit>
+__device__ __forceinline__ void store_bf16_chunk(__nv_bfloat16* p, const float2 (&v)[VEC / 2], int nt, bool on2) {
+  if constexpr (kSplit) {
+    p[0] = __float2bfloat16_rn(v[0].x);
+    if (on2) p[nt] = __float2bfloat16_rn(v[0].y);
+  } else {
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    store_bf16<VEC>(p, f);
+  }
+}
+template <int VEC, bool kSplit>
+__device__ __forceinline__ void store_f32_chunk(float* p, const float2 (&v)[VEC / 2], int nt, bool on2) {
+  if constexpr (kSplit) {
+    p[0] = v[0].x;
+    if (on2) p[nt] = v[0].y;
+  } else {
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    store_f32<VEC>(p, f);
+  }
+}
+
+// v -> normed in place, without weights and without the final factor, which is returned: 1 / sqrt(mean square + eps).
+// Values beyond the row are zero and stay so; kFull: there are none.
+template <int VEC, int CH, bool kSplit, bool kFull>
+__device__ __forceinline__ float norm_row(RowVals<VEC, CH>& a, const Cols<CH>& k, int layer, float inv_d, float eps,
+                                          float (&s_part)[2][32], int& slot) {
+  const int warps = k.nt >> 5;
   if (layer) {
-    float s = 0.f;
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) s += v[c][i];
-    const float mean = cta_sum(s, s_part, slot, warps) * inv_d;
+      for (int i = 0; i < VEC / 2; ++i) s = add2(s, a.v[c][i]);
+    const float mean = cta_sum(s.x + s.y, s_part, slot, warps) * inv_d;
     slot ^= 1;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
+      if (kFull || k.on[c]) {
+        const float2 m = make_float2(-mean, !kSplit || k.on2[c] ? -mean : 0.f);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[c][i] = on[c] ? v[c][i] - mean : 0.f;
+        for (int i = 0; i < VEC / 2; ++i) a.v[c][i] = add2(a.v[c][i], m);
+      }
   }
-  float q = 0.f;
+  float2 q = make_float2(0.f, 0.f);
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) q = fmaf(v[c][i], v[c][i], q);
-  const float ms = cta_sum(q, s_part, slot, warps) * inv_d;
+    for (int i = 0; i < VEC / 2; ++i) q = fma2(a.v[c][i], a.v[c][i], q);
+  const float ms = cta_sum(q.x + q.y, s_part, slot, warps) * inv_d;
   slot ^= 1;
-  const float r = 1.f / sqrtf(ms + eps);
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[c][i] *= r;
+  return 1.f / sqrtf(ms + eps);
 }
 
-// kF32: the residual stream is f32.  p.y == NULL: the norm before a block.
-template <int VEC, int CH, bool kF32>
-__global__ void __launch_bounds__(VEC * CH >= 32 ? 512 : 1024) norm_kernel(const NormParams p) {
-  __shared__ float s_part[2][32];
-  const int t = blockIdx.x, nt = blockDim.x, warps = nt >> 5;
-  pdl_trigger();
-  pdl_wait();
-  if (p.n_valid != nullptr && t >= *p.n_valid) return;
+// v *= the parameter, or += it.
+template <int VEC, int CH, bool kSplit, bool kFull, bool kAdd>
+__device__ __forceinline__ void apply_param(RowVals<VEC, CH>& a, const void* base, size_t at, int is_f32, const Cols<CH>& k) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if (!kFull && !k.on[c]) continue;
+    float f[VEC];
+    float2 w[VEC / 2];
+    if constexpr (kSplit) {
+      float f0[1], f1[1] = {0.f};
+      load_param<1>(base, at + k.col[c], is_f32, f0);
+      if (k.on2[c]) load_param<1>(base, at + k.col[c] + k.nt, is_f32, f1);
+      f[0] = f0[0];
+      f[1] = f1[0];
+    } else {
+      load_param<VEC>(base, at + k.col[c], is_f32, f);
+    }
+    to_pairs<VEC>(f, w);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) a.v[c][i] = kAdd ? add2(a.v[c][i], w[i]) : mul2(a.v[c][i], w[i]);
+  }
+}
+template <int VEC, int CH>
+__device__ __forceinline__ void scale_row(RowVals<VEC, CH>& a, float f) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) a.v[c][i] = mul2(a.v[c][i], make_float2(f, f));
+}
+
+// Everything between a row's loads and its stores.  yu: the block's output (kOut); ru or r: the stream; zero beyond the row.
+template <int VEC, int CH, bool kSplit, bool kF32, bool kOut, bool kFull>
+__device__ __forceinline__ void finish_row(const NormParams& p, size_t row, const Cols<CH>& k, const uint32_t (&yu)[CH][VEC / 2],
+                                           const uint32_t (&ru)[CH][VEC / 2], RowVals<VEC, CH>& r, float (&s_part)[2][32], int& slot) {
   const float inv_d = 1.f / static_cast<float>(p.d);
-  int col[CH];
-  bool on[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    col[c] = (c * nt + static_cast<int>(threadIdx.x)) * VEC;
-    on[c] = col[c] < p.d;                               // d is a multiple of VEC
-  }
-  const size_t row = static_cast<size_t>(t);
-  uint32_t yu[CH][(VEC + 1) / 2], ru[CH][(VEC + 1) / 2];
-  float v[CH][VEC], rf[CH][VEC];
-  int slot = 0;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if constexpr (kF32) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) rf[c][i] = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < (VEC + 1) / 2; ++i) yu[c][i] = ru[c][i] = 0u;
-    if (!on[c]) continue;
-    if (p.y != nullptr) load_bf16_stream<VEC>(p.y + row * p.ld_y + col[c], yu[c]);
-    if constexpr (kF32) load_f32_stream<VEC>(static_cast<const float*>(p.r) + row * p.ld_r + col[c], rf[c]);
-    else load_bf16_stream<VEC>(static_cast<const __nv_bfloat16*>(p.r) + row * p.ld_r + col[c], ru[c]);
-  }
-  if (p.y != nullptr) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) widen<VEC>(yu[c], v[c]);
-    if (p.post_w != nullptr) norm_row<VEC, CH>(v, on, p.layer, inv_d, p.eps, s_part, slot, warps);
-    float gt = 1.f;
-    if (p.gate != nullptr && p.gate_col == 0) {         // one gate for the row
-      float g1[1];
-      load_param<1>(p.gate, row * p.gate_row, p.gate_f32, g1);
-      gt = g1[0];
-    }
-    const float ys = p.y_scale * gt;
+  RowVals<VEC, CH> a;
+  float f[VEC];
+  if constexpr (kOut) {
+    float ys = p.y_scale;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      if (!on[c]) continue;
-      float w[VEC];
-      if (p.post_w != nullptr) {
-        load_param<VEC>(p.post_w, col[c], p.param_f32, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[c][i] *= w[i];
-        if (p.post_b != nullptr) {
-          load_param<VEC>(p.post_b, col[c], p.param_f32, w);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) v[c][i] += w[i];
-        }
+      widen<VEC>(yu[c], f);
+      to_pairs<VEC>(f, a.v[c]);
+    }
+    if (p.post_w != nullptr) {
+      const float inv = norm_row<VEC, CH, kSplit, kFull>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+      apply_param<VEC, CH, kSplit, kFull, false>(a, p.post_w, 0, p.param_f32, k);
+      if (p.post_b != nullptr) {
+        scale_row<VEC, CH>(a, inv);
+        apply_param<VEC, CH, kSplit, kFull, true>(a, p.post_b, 0, p.param_f32, k);
+      } else {
+        ys *= inv;
       }
-      if (p.gate != nullptr && p.gate_col != 0) {
-        if (p.gate_vec) {
-          load_param<VEC>(p.gate, row * p.gate_row + col[c], p.gate_f32, w);
-        } else {
+    }
+    if (p.gate != nullptr) {
+      if (p.gate_col == 0) {                            // one gate for the row
+        float g1[1];
+        load_param<1>(p.gate, row * p.gate_row, p.gate_f32, g1);
+        ys *= g1[0];
+      } else if (p.gate_vec) {
+        apply_param<VEC, CH, kSplit, kFull, false>(a, p.gate, row * p.gate_row, p.gate_f32, k);
+      } else {                                          // columns at a pitch of their own
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          if (!kFull && !k.on[c]) continue;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
+            if (kSplit && i == 1 && !k.on2[c]) continue;
             float g1[1];
-            load_param<1>(p.gate, row * p.gate_row + static_cast<size_t>(col[c] + i) * p.gate_col, p.gate_f32, g1);
-            w[i] = g1[0];
+            load_param<1>(p.gate, row * p.gate_row + static_cast<size_t>(k.col[c] + (kSplit ? i * k.nt : i)) * p.gate_col, p.gate_f32, g1);
+            (i & 1 ? a.v[c][i / 2].y : a.v[c][i / 2].x) *= g1[0];
           }
         }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[c][i] *= w[i];
       }
-      if constexpr (!kF32) widen<VEC>(ru[c], rf[c]);
+    }
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[c][i] = fmaf(ys, v[c][i], p.r_scale * rf[c][i]);
-      if constexpr (kF32) store_f32<VEC>(static_cast<float*>(p.r_out) + row * p.ld_r_out + col[c], v[c]);
-      else store_bf16<VEC>(static_cast<__nv_bfloat16*>(p.r_out) + row * p.ld_r_out + col[c], v[c]);
+    for (int c = 0; c < CH; ++c) {
+      if constexpr (!kF32) {
+        widen<VEC>(ru[c], f);
+        to_pairs<VEC>(f, r.v[c]);
+      }
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i)
+        a.v[c][i] = fma2(a.v[c][i], make_float2(ys, ys), mul2(r.v[c][i], make_float2(p.r_scale, p.r_scale)));
+      if (kFull || k.on[c]) {
+        if constexpr (kF32) store_f32_chunk<VEC, kSplit>(static_cast<float*>(p.r_out) + row * p.ld_r_out + k.col[c], a.v[c], k.nt, k.on2[c]);
+        else store_bf16_chunk<VEC, kSplit>(static_cast<__nv_bfloat16*>(p.r_out) + row * p.ld_r_out + k.col[c], a.v[c], k.nt, k.on2[c]);
+      }
     }
     if (p.x == nullptr) return;
   } else {
@@ -243,44 +349,148 @@ __global__ void __launch_bounds__(VEC * CH >= 32 ? 512 : 1024) norm_kernel(const
     for (int c = 0; c < CH; ++c) {
       if constexpr (kF32) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[c][i] = rf[c][i];
+        for (int i = 0; i < VEC / 2; ++i) a.v[c][i] = r.v[c][i];
       } else {
-        widen<VEC>(ru[c], v[c]);
+        widen<VEC>(ru[c], f);
+        to_pairs<VEC>(f, a.v[c]);
       }
     }
   }
-  norm_row<VEC, CH>(v, on, p.layer, inv_d, p.eps, s_part, slot, warps);
+  const float inv = norm_row<VEC, CH, kSplit, kFull>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+  apply_param<VEC, CH, kSplit, kFull, false>(a, p.next_w, 0, p.param_f32, k);
+  scale_row<VEC, CH>(a, inv);
+  if (p.next_b != nullptr) apply_param<VEC, CH, kSplit, kFull, true>(a, p.next_b, 0, p.param_f32, k);
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (kFull || k.on[c]) store_bf16_chunk<VEC, kSplit>(p.x + row * p.ld_x + k.col[c], a.v[c], k.nt, k.on2[c]);
+}
+
+// One row per CTA.  kOut: the norm after a block (p.y), else the norm before one.  kF32: the residual stream is f32.
+template <int VEC, int CH, bool kSplit, bool kF32, bool kOut, bool kFull>
+__global__ void __launch_bounds__(VEC * CH >= 32 ? 512 : 1024) norm_kernel(const NormParams p) {
+  __shared__ float s_part[2][32];
+  const int t = blockIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  if (p.n_valid != nullptr && t >= *p.n_valid) return;
+  Cols<CH> k;
+  set_cols<VEC, CH, kSplit, kFull>(k, p.d);
+  const size_t row = static_cast<size_t>(t);
+  uint32_t yu[CH][VEC / 2], ru[CH][VEC / 2];
+  RowVals<VEC, CH> r;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if (!on[c]) continue;
-    float w[VEC];
-    load_param<VEC>(p.next_w, col[c], p.param_f32, w);
+    float rf[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[c][i] *= w[i];
-    if (p.next_b != nullptr) {
-      load_param<VEC>(p.next_b, col[c], p.param_f32, w);
+    for (int i = 0; i < VEC; ++i) rf[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[c][i] += w[i];
+    for (int i = 0; i < VEC / 2; ++i) yu[c][i] = ru[c][i] = 0u;
+    if (kFull || k.on[c]) {
+      if constexpr (kOut) load_bf16_chunk<VEC, kSplit>(p.y + row * p.ld_y + k.col[c], yu[c], k.nt, k.on2[c]);
+      if constexpr (kF32) load_f32_chunk<VEC, kSplit>(static_cast<const float*>(p.r) + row * p.ld_r + k.col[c], rf, k.nt, k.on2[c]);
+      else load_bf16_chunk<VEC, kSplit>(static_cast<const __nv_bfloat16*>(p.r) + row * p.ld_r + k.col[c], ru[c], k.nt, k.on2[c]);
     }
-    store_bf16<VEC>(p.x + row * p.ld_x + col[c], v[c]);
+    if constexpr (kF32) to_pairs<VEC>(rf, r.v[c]);
+  }
+  int slot = 0;
+  finish_row<VEC, CH, kSplit, kF32, kOut, kFull>(p, row, k, yu, ru, r, s_part, slot);
+}
+
+// Several rows per CTA (bf16 stream, VEC = 8): the next row is on its way while this one is summed and written.  Every
+// thread copies its own columns of the next row to its own words of shared memory (cp.async, 16 bytes each) and reads only
+// those back, so the copies need no barrier; two buffers.  64 registers: two CTAs of 448 threads to an SM at d = 7168, where
+// the compiler's own choice leaves one.
+template <int CH, bool kOut, bool kFull>
+__global__ void __maxnreg__(64) norm_rows_kernel(const NormParams p) {
+  extern __shared__ uint4 s_row[];                      // [buffer][y, r][chunk][thread]
+  __shared__ float s_part[2][32];
+  constexpr int VEC = 8, kR = kOut ? 1 : 0, kStreams = kR + 1;
+  pdl_trigger();
+  pdl_wait();
+  int rows = p.T;
+  if (p.n_valid != nullptr) rows = max(0, min(*p.n_valid, p.T));
+  Cols<CH> k;
+  set_cols<VEC, CH, false, kFull>(k, p.d);
+  const int nt = k.nt, tid = threadIdx.x;
+  auto fetch = [&](int t, int buf) {
+    if (t < rows) {
+      const size_t row = static_cast<size_t>(t);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        if (!kFull && !k.on[c]) continue;
+        uint4* dst = s_row + (buf * kStreams * CH + c) * nt + tid;
+        if constexpr (kOut) copy16(dst, p.y + row * p.ld_y + k.col[c]);
+        copy16(dst + kR * CH * nt, static_cast<const __nv_bfloat16*>(p.r) + row * p.ld_r + k.col[c]);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int slot = 0, buf = 0;
+  fetch(blockIdx.x, 0);
+  for (int t = blockIdx.x; t < rows; t += gridDim.x, buf ^= 1) {
+    fetch(t + gridDim.x, buf ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    uint32_t yu[CH][4], ru[CH][4];
+    RowVals<VEC, CH> r;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const uint4* src = s_row + (buf * kStreams * CH + c) * nt + tid;
+      uint4 a = make_uint4(0, 0, 0, 0), b = a;
+      if (kFull || k.on[c]) {
+        if constexpr (kOut) a = src[0];
+        b = src[kR * CH * nt];
+      }
+      yu[c][0] = a.x; yu[c][1] = a.y; yu[c][2] = a.z; yu[c][3] = a.w;
+      ru[c][0] = b.x; ru[c][1] = b.y; ru[c][2] = b.z; ru[c][3] = b.w;
+    }
+    finish_row<VEC, CH, false, false, kOut, kFull>(p, static_cast<size_t>(t), k, yu, ru, r, s_part, slot);
   }
 }
 
-template <int VEC, int CH>
-static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
+template <int VEC, int CH, bool kSplit, bool kF32, bool kOut>
+static cudaError_t launch_norm_o(const NormParams& p, cudaStream_t stream) {
   const int threads = ((p.d + VEC * CH - 1) / (VEC * CH) + 31) / 32 * 32;
-  if (p.stream_f32) return launch_pdl(norm_kernel<VEC, CH, true>, dim3(p.T), dim3(threads), 0, stream, p);
-  return launch_pdl(norm_kernel<VEC, CH, false>, dim3(p.T), dim3(threads), 0, stream, p);
+  if (VEC == 8 && p.d == VEC * CH * threads)
+    return launch_pdl(norm_kernel<VEC, CH, kSplit, kF32, kOut, VEC == 8>, dim3(p.T), dim3(threads), 0, stream, p);
+  return launch_pdl(norm_kernel<VEC, CH, kSplit, kF32, kOut, false>, dim3(p.T), dim3(threads), 0, stream, p);
 }
 
-// vec: the widest load that every pointer and pitch allows (8, 4, 2 or 1 elements).  Chunks per thread: one where the
-// row count leaves SMs idle (latency), more where they are full.
+template <int CH, bool kOut, bool kFull>
+static cudaError_t launch_rows_f(const NormParams& p, int threads, int num_sms, cudaStream_t stream) {
+  static std::atomic<unsigned long long> smem_set{0};
+  const int smem = 2 * (kOut ? 2 : 1) * CH * threads * 16;
+  cudaError_t e = smem_limit_once(norm_rows_kernel<CH, kOut, kFull>, 128 * 1024, smem_set);
+  if (e != cudaSuccess) return e;
+  const int per_sm = max(1, min(min(32, 65536 / (64 * threads)), 224 * 1024 / (smem + 1280)));   // CTAs that are resident
+  return launch_pdl(norm_rows_kernel<CH, kOut, kFull>, dim3(min(p.T, per_sm * num_sms)), dim3(threads), smem, stream, p);
+}
+template <int CH>
+static cudaError_t launch_rows(const NormParams& p, int num_sms, cudaStream_t stream) {
+  const int threads = ((p.d + 8 * CH - 1) / (8 * CH) + 31) / 32 * 32;
+  const bool full = p.d == 8 * CH * threads;
+  if (p.y) return full ? launch_rows_f<CH, true, true>(p, threads, num_sms, stream) : launch_rows_f<CH, true, false>(p, threads, num_sms, stream);
+  return full ? launch_rows_f<CH, false, true>(p, threads, num_sms, stream) : launch_rows_f<CH, false, false>(p, threads, num_sms, stream);
+}
+
+template <int VEC, int CH, bool kSplit = false>
+static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
+  if (p.stream_f32)
+    return p.y ? launch_norm_o<VEC, CH, kSplit, true, true>(p, stream) : launch_norm_o<VEC, CH, kSplit, true, false>(p, stream);
+  return p.y ? launch_norm_o<VEC, CH, kSplit, false, true>(p, stream) : launch_norm_o<VEC, CH, kSplit, false, false>(p, stream);
+}
+
+// vec: the widest load that every pointer and pitch allows (8, 4, 2 or 1 elements).
+//   Fewer than two rows per SM: one chunk per thread, the shortest chain (one row of 4096: 2.5 us with one, 2.9 with two).
+//   More: the kernel with several rows per CTA where a CTA gets few of them or they are wide (d = 7168: 600 rows 7.6 us
+//   against 10.9, 8192 rows 87 against 102; 1024 rows of 4096: 6.8 against 9.4), else one row per CTA, whose CTAs' phases mix
+//   (8192 rows of 2048: 24.1 us against 25.7; 2048 of 4096: 14.9 against 15.7).  An f32 stream has half as many elements to
+//   its bytes and needs the registers: one row per CTA, four chunks (8192 rows of 7168: 123 us against 161).
 cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream) {
-  const bool full = p.T >= 2 * num_sms;
   if (vec == 8) {
-    if (full && p.d > 2048) return launch_norm_t<8, 4>(p, stream);
-    if (p.d > 8192 || (full && p.d > 512)) return launch_norm_t<8, 2>(p, stream);
-    return launch_norm_t<8, 1>(p, stream);
+    if (p.T < 2 * num_sms) return p.d > 8192 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
+    if (!p.stream_f32 && p.d >= 1024 && (p.d > 4096 || p.T < 10 * num_sms)) return launch_rows<2>(p, num_sms, stream);
+    if (p.d > 4096 || (p.stream_f32 && p.d > 2048)) return launch_norm_t<8, 4>(p, stream);
+    return p.d > 512 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
   }
   if (vec == 4) {
     if (p.d <= 4096) return launch_norm_t<4, 1>(p, stream);
@@ -290,8 +500,8 @@ cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t 
     if (p.d <= 4096) return launch_norm_t<2, 2>(p, stream);
     return launch_norm_t<2, 8>(p, stream);
   }
-  if (p.d <= 4096) return launch_norm_t<1, 4>(p, stream);
-  return launch_norm_t<1, 16>(p, stream);
+  if (p.d <= 4096) return launch_norm_t<2, 2, true>(p, stream);
+  return launch_norm_t<2, 8, true>(p, stream);
 }
 
 }  // namespace tempo
