@@ -296,30 +296,37 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     if (bad && cta == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_ID));
     bar_sync(1, 128);
     if (warp == 0) {
-      int a0 = 0, o0 = 0, h0 = 0;
-      for (int base = 0; base < G; base += 32) {
-        const int i = base + lane;
-        const int n = i < G ? __popcll(L.mask[i]) : 0;
-        const uint32_t on = __ballot_sync(0xffffffffu, n > 0);
-        if (on == 0) continue;
-        int po = n, ph = 2 * ((n + 7) & ~7);
+      // 128 slots per turn, four neighbours to a lane; experts, pairs and operand rows before a slot in one 64-bit scan
+      unsigned long long before = 0;                                // 16 bits each: experts, pairs, rows
+      for (int base = 0; base < G; base += 128) {
+        unsigned long long n4[4], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = base + 4 * lane + q, n = i < G ? __popcll(L.mask[i]) : 0;
+          n4[q] = n == 0 ? 0ull : 1ull | static_cast<unsigned long long>(n) << 16 | static_cast<unsigned long long>(2 * ((n + 7) & ~7)) << 32;
+          sum += n4[q];
+        }
+        unsigned long long incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const int u = __shfl_up_sync(0xffffffffu, po, o), v = __shfl_up_sync(0xffffffffu, ph, o);
-          if (lane >= o) { po += u; ph += v; }
+          const unsigned long long u = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += u;
         }
-        if (n > 0) {
-          const int a = a0 + __popc(on & ((1u << lane) - 1u));
-          L.act[a] = static_cast<uint16_t>(i);
-          L.off[a] = static_cast<uint16_t>(o0 + po - n);
-          L.hrow[a] = static_cast<uint16_t>(h0 + ph - 2 * ((n + 7) & ~7));
-          L.s2a[i] = static_cast<int16_t>(a);
+        unsigned long long at = before + incl - sum;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (n4[q] != 0) {
+            const int a = static_cast<int>(at & 0xffff), i = base + 4 * lane + q;
+            L.act[a] = static_cast<uint16_t>(i);
+            L.off[a] = static_cast<uint16_t>(at >> 16);
+            L.hrow[a] = static_cast<uint16_t>(at >> 32);
+            L.s2a[i] = static_cast<int16_t>(a);
+          }
+          at += n4[q];
         }
-        a0 += __popc(on);
-        o0 += __shfl_sync(0xffffffffu, po, 31);
-        h0 += __shfl_sync(0xffffffffu, ph, 31);
+        before += __shfl_sync(0xffffffffu, incl, 31);
       }
-      if (lane == 0) { s_A = a0; L.off[a0] = static_cast<uint16_t>(o0); }
+      if (lane == 0) { s_A = static_cast<int>(before & 0xffff); L.off[before & 0xffff] = static_cast<uint16_t>(before >> 16); }
     } else if (warp == 1) {                                         // the runs need the number of experts only
       int n = 0;
       for (int base = 0; base < G; base += 32) n += __popc(__ballot_sync(0xffffffffu, base + lane < G && L.mask[base + lane] != 0ull));
@@ -514,8 +521,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       while (ok && s.next()) {
         const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
         ++n_seg;
-        bool seen = mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns);
         const int last = s.kb0 == 0 && s.kb1 < p.Kb1 ? static_cast<int>(run_owner(s.line * p.Kb1 + p.Kb1 - 1, f.C, f.B)) : static_cast<int>(cta);
+        bool seen = mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns);
         for (int c = static_cast<int>(cta) + 1 + et; c <= last; c += 256)
           seen = seen && few_poll(part_done + ph * C + c, 1, s_abort, p.wait_ns);
         ok = bar_all(3, 256, seen);
@@ -630,12 +637,12 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
         }
         const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
         ++n_seg;
+        const int j = static_cast<int>(cta - run_owner(s.line * p.Kb2, f.C, f.B));
         ok = bar_all(3, 256, mbar_wait(smem_u32(&s_acc_full[slot]), use & 1u, s_abort, p.wait_ns));
         if (!ok) break;
         tc_fence_after();
         const int u0 = L.off[s.a], n_col = L.off[s.a + 1] - u0, C8 = (n_col + 7) & ~7;
         const uint32_t acc = tmem_base + slot * 128u + lanes + g * (2 * C8);
-        const int j = static_cast<int>(cta - run_owner(s.line * p.Kb2, f.C, f.B));
         const int n = s.nt * 256 + g * 128 + row;
         float* dst = p.y_part + (static_cast<size_t>(j) * P + u0) * p.d + n;
 #pragma unroll 1
@@ -671,21 +678,17 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       const FewPhase &f0 = s_phase[2], &f = s_phase[3].an > 0 ? s_phase[3] : s_phase[2];   // f: the last phase that has work
       const uint32_t per_nt = static_cast<uint32_t>(f.an) * p.Kb2;
       const int nt_lo = static_cast<int>(f.b / per_nt), nt_hi = f.e > f.b ? static_cast<int>((f.e - 1) / per_nt) : nt_lo - 1;
-      bool seen = true;
-      for (int nt = nt_lo + et; nt <= nt_hi; nt += 256) seen = seen && few_poll(y_cnt + nt, A * p.Kb2, s_abort, p.wait_ns);
       const size_t part_pitch = static_cast<size_t>(P) * p.d;
       for (int nt0 = nt_lo; nt0 <= nt_hi; nt0 += 2) {               // (almost every CTA has one or two column blocks)
+        // What the wait does not need is computed before it: partials per expert, and this CTA's share of each block's
+        // (token, 4 columns) items.
         const int two = min(2, nt_hi - nt0 + 1);
         for (int i = et; i < two * A; i += 256) {
-          const int a = i % A, nt = nt0 + i / A;
+          const int m = i >= A ? 1 : 0, a = i - m * A, nt = nt0 + m;
           const FewPhase& h = a < f0.an ? f0 : f;
           const uint32_t b = (static_cast<uint32_t>(nt) * h.an + a - h.a0) * p.Kb2;
           L.split[i] = static_cast<uint8_t>(run_owner(b + p.Kb2 - 1, h.C, h.B) - run_owner(b, h.C, h.B) + 1);
         }
-        ok = bar_all(3, 256, seen);
-        if (!ok) break;
-        // This CTA's share of each block's (token, 4 columns) items.  With few items four lanes share one (lane q takes the
-        // token's pairs q, q + 4, ..., then the four sums are added in a fixed tree); two pairs' partials are in flight.
         int from[2], n_item[2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -694,6 +697,12 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
           from[m] = m < two ? static_cast<int>(run_begin(me, parts, T * 64)) : 0;
           n_item[m] = m < two ? static_cast<int>(run_begin(me + 1, parts, T * 64)) - from[m] : 0;
         }
+        bool seen = true;
+        if (et < two) seen = few_poll(y_cnt + nt0 + et, A * p.Kb2, s_abort, p.wait_ns);
+        ok = bar_all(3, 256, seen);
+        if (!ok) break;
+        // With few items four lanes share one (lane q takes the token's pairs q, q + 4, ..., then the four sums are added in
+        // a fixed tree); two pairs' partials are in flight.
         const int items = n_item[0] + n_item[1];
         const int lanes_per = items * 4 <= 512 ? 4 : 1, q = et & (lanes_per - 1), groups = 256 / lanes_per;
         for (int i0 = 0; i0 < items; i0 += groups) {                // the same number of turns for every lane of a warp

@@ -420,12 +420,26 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
   }
 }
 
+constexpr int kRouteSmem = 226 * 1024;      // the most a launch asks for
+
 template <int JJ>
 static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW, const RouteParams& p, int ctas,
                                   size_t smem, cudaStream_t stream) {
   static std::atomic<unsigned long long> smem_set{0};
-  cudaError_t e = smem_limit_once(route_kernel<JJ>, 227 * 1024 - 1024, smem_set);
+  cudaError_t e = smem_limit_once(route_kernel<JJ>, kRouteSmem, smem_set);
   if (e != cudaSuccess) return e;
+  if (p.splits > 8) {
+    static std::atomic<unsigned long long> wide_set{0};
+    int dev = 0;
+    e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+    if (bit == 0 || !(wide_set.load(std::memory_order_acquire) & bit)) {
+      e = cudaFuncSetAttribute(route_kernel<JJ>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      if (bit != 0) wide_set.fetch_or(bit, std::memory_order_release);
+    }
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(kRouteThreads);
@@ -442,6 +456,37 @@ static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW
   return cudaLaunchKernelEx(&cfg, route_kernel<JJ>, tmX, tmW, p);
 }
 
+// Clusters of 16 CTAs (one per SM) that this device runs at once; 0 where it refuses them.  Asked once per device.
+static int wide_clusters() {
+  static std::atomic<int> cached[64];                   // 0: not asked yet, else the answer + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  const int known = cached[dev].load(std::memory_order_acquire);
+  if (known != 0) return known - 1;
+  int n = 0;
+  if (cudaFuncSetAttribute(route_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRouteSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(route_kernel<1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    (void)cudaGetLastError();
+  } else {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(kRouteThreads);
+    cfg.dynamicSmemBytes = kRouteSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 16;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, route_kernel<1>, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();                          // a refused query must not poison the next launch
+      n = 0;
+    }
+  }
+  cached[dev].store(n + 1, std::memory_order_release);
+  return n;
+}
+
 RoutePlan route_plan(int T, int E, int d, int num_sms) {
   RoutePlan r;
   r.E16 = (E + 15) / 16 * 16;
@@ -455,6 +500,7 @@ RoutePlan route_plan(int T, int E, int d, int num_sms) {
   const int tiles = (T + r.tile_rows - 1) / r.tile_rows;
   r.splits = 1;
   while (r.splits < 8 && 2 * r.splits * tiles <= num_sms && 2 * r.splits <= Kb) r.splits *= 2;
+  if (r.splits == 8 && Kb >= 32 && tiles <= wide_clusters()) r.splits = 16;
   r.ctas = tiles * r.splits;
   return r;
 }
