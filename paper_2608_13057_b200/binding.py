@@ -8,10 +8,15 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import Optional
 
 import torch
+
+try:
+    from . import _marshal                      # needs torch's libraries: imported after torch
+except ImportError as e:
+    raise ImportError(f"the extension module _marshal is missing or does not load ({e}): build it with "
+                      "__graft_entry__.build() (python -m paper_2608_13057_b200.build); there is no fallback path") from e
 
 _LIB_PATH = os.environ.get("TEMPO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtempo.so")
 
@@ -268,89 +273,17 @@ def tempo_grouped_ffn_bf16(shape, a_bf16, packed, inst_off, m_pad, h_bf16, y_bf1
 
 
 # ---- norms around the block, the router, the layer for a few tokens ------------------------------
-# With one token a kernel of this section takes a few microseconds, less than careless marshalling: pointers go as
-# plain integers through fixed argtypes, and every property of a tensor is asked for once.
+# With one token a kernel of this section takes a few microseconds, less than ctypes marshalling from Python: the
+# extension module _marshal (csrc/marshal.cpp) checks the tensors and calls the same library's C entry points.
 
-_F32, _BF16, _I32, _U8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
-_NORM = struct.Struct("6i6q3f4x")                       # tempo_norm
-_NO_PITCH = (0, 0)
-_vp, _ci, _cf = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
-_lib.tempo_norm_in.argtypes = [ctypes.c_char_p] + [_vp] * 6
-_lib.tempo_norm_out.argtypes = [ctypes.c_char_p] + [_vp] * 11
-_lib.tempo_route.argtypes = [_vp, _ci, _ci, _cf] + [_vp] * 8
-_lib.tempo_few_ffn.argtypes = _lib.tempo_few_ffn_bf16.argtypes = [_vp] * 11
-
-
-def _addr(t, dtype, what):
-    """Address of a contiguous CUDA tensor of the given type; None stays None (a NULL pointer)."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        _ptr(t, dtype)                                  # says what is wrong
-        raise TempoError(f"{what}: unusable tensor")
-    return t.data_ptr()
-
-
-def _raw_stream():
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-
-
-def _rows(t, what, shape, dtype):
-    """Address and row pitch of a [T, d] tensor whose rows are contiguous (the rows themselves may be strided)."""
-    if not t.is_cuda:
-        raise TempoError("expected a CUDA tensor (the library has no CPU path)")
-    if t.dtype is not dtype:
-        raise TempoError(f"{what}: expected dtype {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise TempoError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    pitch, step = t.stride()
-    if step != 1 and shape[1] > 1:
-        raise TempoError(f"{what}: expected contiguous rows")
-    if pitch < shape[1]:
-        if shape[0] > 1:
-            raise TempoError(f"{what}: rows overlap")
-        pitch = shape[1]
-    return t.data_ptr(), pitch
-
-
-def _param(t, what, d, dtype):
-    """Address of a weight or bias [d] of the call's parameter type."""
-    if t is None:
-        return None
-    if t.dtype is not dtype:
-        raise TempoError(f"{what}: weights and biases are bf16 or f32, all of one dtype; got {t.dtype} beside {dtype}")
-    if t.shape != (d,):
-        raise TempoError(f"{what}: expected shape ({d},), got {tuple(t.shape)}")
-    return _addr(t, dtype, what)
-
-
-def _stream_type(r):
-    if r.dim() != 2:
-        raise TempoError(f"r: expected 2 dimensions, got {r.dim()}")
-    dtype = r.dtype
-    if dtype is not _BF16 and dtype is not _F32:
-        raise TempoError(f"r: expected dtype {_BF16} or {_F32}, got {dtype}")
-    return dtype
-
-
-def _param_type(*params):
-    for t in params:
-        if t is not None:
-            if t.dtype is not _BF16 and t.dtype is not _F32:
-                raise TempoError(f"weights and biases: expected dtype {_BF16} or {_F32}, got {t.dtype}")
-            return t.dtype
-    return _BF16
+_marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
+                            ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",
+                             "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16")))
 
 
 def tempo_norm_in(r, w, x_out, b=None, kind=NORM_RMS, eps=1e-6, n_valid=None):
     """x_out = norm(r) * w + b, row by row.  r [T, d] bf16 or f32, x_out [T, d] bf16 (rows may be strided), w, b [d]."""
-    dtype, ptype, shape = _stream_type(r), _param_type(w, b), r.shape
-    T, d = shape
-    pr, ld_r = _rows(r, "r", shape, dtype)
-    px, ld_x = _rows(x_out, "x_out", shape, _BF16)
-    a = _NORM.pack(T, d, kind, dtype is _F32, ptype is _F32, 0, 0, ld_r, 0, ld_x, 0, 0, eps, 1.0, 1.0)
-    rc = _lib.tempo_norm_in(a, pr, _param(w, "w", d, ptype), _param(b, "b", d, ptype), _addr(n_valid, _I32, "n_valid"), px,
-                            _raw_stream())
+    rc = _marshal.norm_in(r, w, x_out, b, kind, eps, n_valid)
     if rc:
         _check(rc, "tempo_norm_in")
 
@@ -361,42 +294,15 @@ def tempo_norm_out(y, r, r_out, post_w=None, post_b=None, gate=None, next_w=None
 
     y, x_out bf16, r and r_out bf16 or f32, all [T, d] (rows may be strided; r_out may be r, x_out may be y); the gate
     bf16 or f32 of any shape that broadcasts to [T, d]; weights and biases [d] of one dtype."""
-    dtype, ptype, shape = _stream_type(r), _param_type(post_w, post_b, next_w, next_b), r.shape
-    T, d = shape
-    py, ld_y = _rows(y, "y", shape, _BF16)
-    pr, ld_r = _rows(r, "r", shape, dtype)
-    po, ld_ro = _rows(r_out, "r_out", shape, dtype)
-    px, ld_x = (None, 0) if x_out is None else _rows(x_out, "x_out", shape, _BF16)
-    pg, g32, (gate_row, gate_col) = None, False, _NO_PITCH
-    if gate is not None:
-        if not gate.is_cuda:
-            raise TempoError("expected a CUDA tensor (the library has no CPU path)")
-        g32 = gate.dtype is _F32
-        if not g32 and gate.dtype is not _BF16:
-            raise TempoError(f"gate: expected dtype {_BF16} or {_F32}, got {gate.dtype}")
-        if gate.dim() == 2 and gate.shape == (T, 1):                # one per token, the shape that needs no broadcast view
-            gate_row = gate.stride(0)
-        else:
-            try:
-                gate_row, gate_col = gate.expand(shape).stride()
-            except RuntimeError:
-                raise TempoError(f"gate: shape {tuple(gate.shape)} does not broadcast to {tuple(shape)}") from None
-        pg = gate.data_ptr()
-    a = _NORM.pack(T, d, kind, dtype is _F32, ptype is _F32, g32, ld_y, ld_r, ld_ro, ld_x, gate_row, gate_col, eps, r_scale,
-                   y_scale)
-    rc = _lib.tempo_norm_out(a, py, pr, _param(post_w, "post_w", d, ptype), _param(post_b, "post_b", d, ptype), pg,
-                             _param(next_w, "next_w", d, ptype), _param(next_b, "next_b", d, ptype),
-                             _addr(n_valid, _I32, "n_valid"), po, px, _raw_stream())
+    rc = _marshal.norm_out(y, r, r_out, post_w, post_b, gate, next_w, next_b, x_out, kind, eps, r_scale, y_scale, n_valid)
     if rc:
         _check(rc, "tempo_norm_out")
 
 
 def tempo_route(shape, x_bf16, w_router, bias, n_valid, topk_ids, topk_w, status, score=ROUTE_SOFTMAX, renormalise=True,
                 scale=1.0):
-    rc = _lib.tempo_route(ctypes.addressof(shape), score, bool(renormalise), scale, _addr(x_bf16, _BF16, "x"),
-                          _addr(w_router, _BF16, "w_router"), _addr(bias, _F32, "bias"), _addr(n_valid, _I32, "n_valid"),
-                          _addr(topk_ids, _I32, "topk_ids"), _addr(topk_w, _F32, "topk_w"), _addr(status, _I32, "status"),
-                          _raw_stream())
+    rc = _marshal.route(ctypes.addressof(shape), x_bf16, w_router, bias, n_valid, topk_ids, topk_w, status, score, renormalise,
+                        scale)
     if rc:
         _check(rc, "tempo_route")
 
@@ -407,23 +313,18 @@ def tempo_few_workspace_bytes(shape: TempoShape) -> int:
     return out.value
 
 
-def _few(fn, what, shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
-    rc = fn(ctypes.addressof(shape), _addr(x_bf16, _BF16, "x"), _addr(topk_ids, _I32, "topk_ids"),
-            _addr(topk_w, _F32, "topk_w"), _addr(n_valid, _I32, "n_valid"), _addr(replica_map, _I32, "replica_map"),
-            _addr(packed, _U8, "packed"), _addr(out_bf16, _BF16, "out"), _addr(status, _I32, "status"),
-            _addr(workspace, _U8, "workspace"), _raw_stream())
-    if rc:
-        _check(rc, what)
-
-
 def tempo_few_ffn(shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
-    _few(_lib.tempo_few_ffn, "tempo_few_ffn", shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16,
-         status, workspace)
+    rc = _marshal.few(False, ctypes.addressof(shape), x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status,
+                      workspace)
+    if rc:
+        _check(rc, "tempo_few_ffn")
 
 
 def tempo_few_ffn_bf16(shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace):
-    _few(_lib.tempo_few_ffn_bf16, "tempo_few_ffn_bf16", shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed,
-         out_bf16, status, workspace)
+    rc = _marshal.few(True, ctypes.addressof(shape), x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status,
+                      workspace)
+    if rc:
+        _check(rc, "tempo_few_ffn_bf16")
 
 
 # ------------------------------------------------------------------------------------------------

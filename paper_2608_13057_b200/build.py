@@ -1,9 +1,11 @@
-"""Builds libtempo.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libtempo.so (the C-ABI CUDA library, nvcc for sm_100a) and _marshal (the Python module that marshals the short
+calls, the host compiler against torch's headers) in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
@@ -13,15 +15,42 @@ SOURCES = ["api.cu", "dispatch.cu", "dispatch_sampled.cu", "permute.cu", "ffn.cu
            "norm.cu", "route.cu", "few.cu"]
 
 
+MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+HEADER = os.path.join(ROOT, "include", "tempo.h")
+
+
 def _stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
     t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "tempo.h")]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [HEADER]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_marshal(force: bool = False) -> str:
+    """The extension links torch's libraries by name only: importing torch first loads them."""
+    if not force and os.path.exists(MARSHAL_PATH) and \
+            os.path.getmtime(MARSHAL_PATH) >= max(os.path.getmtime(MARSHAL_SRC), os.path.getmtime(HEADER)):
+        return MARSHAL_PATH
+    import torch
+    base = os.path.dirname(os.path.abspath(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"),
+           "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"],
+           "-o", MARSHAL_PATH, MARSHAL_SRC, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("the host compiler failed building _marshal")
+    return MARSHAL_PATH
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_marshal(force)
     if not force and not _stale():
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

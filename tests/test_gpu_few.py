@@ -278,7 +278,7 @@ def test_refusals(B):
     for kw in (dict(x=x), dict(x=xc.float()), dict(ids=ic.long()), dict(w=None), dict(ws=None), dict(m=None), dict(out=out.t()),
                dict(shape=B.make_shape(65, 2, 2, 2, 1, 128, 128, 128)), dict(shape=B.make_shape(64, 17, 20, 2, 1, 128, 128, 128)),
                dict(shape=B.make_shape(4, 2, 2, 2, 1, 192, 128, 128)), dict(shape=B.make_shape(0, 2, 2, 2, 1, 128, 128, 128)),
-               dict(ws=ws[16:]), dict(packed=L.packed[16:]),
+               dict(ws=ws[16:]), dict(packed=L.packed[16:]), dict(ws=ws[:-256]), dict(packed=L.packed[:-1024]), dict(x=xc[:3]),
                dict(x=torch.zeros(4 * 128 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(4, 128))):
         with pytest.raises(B.TempoError):
             call(**kw)
