@@ -1,0 +1,72 @@
+"""One mixture-of-experts layer of a served model on one rank: the norm before the block, the router, this rank's experts,
+and the norm after it with the block's gate, the residual sum and the next block's norm.
+
+Batches of up to FEW_TOKENS tokens run in four kernels (norm, router, few-token experts, norm); larger ones take the
+four-step block between the norms (dispatch, permute, grouped FFN, combine).  Both read the same packed weights.  Marshalling
+and buffers only; every step runs in the library's kernels."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+# The few-token kernel takes at most 64 tokens and is the faster form of all of them: 16 experts of d = 4096, f = 1536 on a
+# rank, top-8 of 128: 56 us against 76 of the four-step block at 64 tokens, 27 against 46 at 8, 14 against 29 at 1 (either way
+# every chosen expert's weights are read once; the block pads each instance to 128 rows and runs four kernels).
+FEW_TOKENS = 64
+
+
+class MoELayer:
+    """Weights of one layer and the buffers of its calls.
+
+    max_tokens   largest batch (rows of the buffers)
+    w_router     bf16 [E, d]; bias f32 [E] or None; score B.ROUTE_SOFTMAX or B.ROUTE_SIGMOID
+    replica_map  i32 [E, R]; quota i32 [E, R] or None (uniform over an expert's replicas; the few-token path uses the first)
+    packed       the blob of tempo_pack_weights (fp8)
+    norm_w, post_w, next_w   weights [d] of the norm before the block, after it (None: not normed) and of the next block
+    """
+
+    def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
+                 quota=None, gate=None, kind=B.NORM_RMS, eps=1e-6, score=B.ROUTE_SOFTMAX, renormalise=True, scale=1.0,
+                 r_scale=1.0, y_scale=1.0):
+        E, d = w_router.shape
+        dev = w_router.device
+        self.k, self.E, self.G_max, self.R, self.d, self.f = k, E, G_max, replica_map.shape[1], d, f
+        self.w_router, self.bias, self.replica_map, self.packed = w_router, bias, replica_map, packed
+        self.quota = torch.zeros_like(replica_map) if quota is None else quota
+        self.norm_w, self.post_w, self.next_w, self.gate = norm_w, post_w, next_w, gate
+        self.kind, self.eps, self.r_scale, self.y_scale = kind, eps, r_scale, y_scale
+        self.score, self.renormalise, self.scale = score, renormalise, scale
+        bf16 = dict(dtype=torch.bfloat16, device=dev)
+        self.x = torch.empty(max_tokens, d, **bf16)
+        self.y = torch.empty(max_tokens, d, **bf16)
+        self.topk_ids = torch.empty(max_tokens, k, dtype=torch.int32, device=dev)
+        self.topk_w = torch.empty(max_tokens, k, dtype=torch.float32, device=dev)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        few = B.make_shape(min(max_tokens, FEW_TOKENS), k, E, G_max, self.R, d, f, 128)
+        self.workspace = torch.zeros(B.tempo_few_workspace_bytes(few), dtype=torch.uint8, device=dev)
+        self.block = B.RankBuffers(max_tokens, k, E, G_max, self.R, d, f, device=dev) if max_tokens > FEW_TOKENS else None
+        if self.block is not None:                       # the block reads this layer's tables and tensors
+            self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
+            self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
+            self.block.out, self.block.status = self.y, self.status
+
+    def forward(self, r, r_out, x_next=None):
+        """r_out = the residual stream after the block; x_next = its norm for the next block (with next_w).  r, r_out [T, d]
+        bf16 or f32 (r_out may be r), x_next bf16.  Enqueues kernels only: the call can be captured in a CUDA graph."""
+        T = r.shape[0]
+        if T > self.x.shape[0]:
+            raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.x.shape[0]}")
+        x, y, ids, w = self.x[:T], self.y[:T], self.topk_ids[:T], self.topk_w[:T]
+        shape = B.make_shape(T, self.k, self.E, self.G_max, self.R, self.d, self.f, 128)
+        B.tempo_norm_in(r, self.norm_w, x, kind=self.kind, eps=self.eps)
+        B.tempo_route(shape, x, self.w_router, self.bias, None, ids, w, self.status, score=self.score,
+                      renormalise=self.renormalise, scale=self.scale)
+        if T <= FEW_TOKENS:
+            B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
+        else:
+            self.block.n_valid.fill_(T)
+            self.block.run_block()
+        B.tempo_norm_out(y, r, r_out, post_w=self.post_w, gate=self.gate, next_w=self.next_w if x_next is not None else None,
+                         x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale, y_scale=self.y_scale)
+        return r_out
