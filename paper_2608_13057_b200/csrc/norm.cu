@@ -480,14 +480,17 @@ static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
 }
 
 // vec: the widest load that every pointer and pitch allows (8, 4, 2 or 1 elements).
-//   Fewer than two rows per SM: one chunk per thread, the shortest chain (one row of 4096: 2.5 us with one, 2.9 with two).
+//   Fewer than two rows per SM: one chunk per thread, the shortest chain (one row of 4096: 2.4 us with one, 2.6 with two, 3.2
+//   with four; 203 rows 3.9, 4.3, 5.4), unless two CTAs of that many threads do not fit an SM and there are more rows than SMs
+//   (290 rows of 7168: 5.4 us with one, 4.0 with two).
 //   More: the kernel with several rows per CTA where a CTA gets few of them or they are wide (d = 7168: 600 rows 7.6 us
 //   against 10.9, 8192 rows 87 against 102; 1024 rows of 4096: 6.8 against 9.4), else one row per CTA, whose CTAs' phases mix
 //   (8192 rows of 2048: 24.1 us against 25.7; 2048 of 4096: 14.9 against 15.7).  An f32 stream has half as many elements to
 //   its bytes and needs the registers: one row per CTA, four chunks (8192 rows of 7168: 123 us against 161).
 cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream) {
   if (vec == 8) {
-    if (p.T < 2 * num_sms) return p.d > 8192 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
+    if (p.T < 2 * num_sms)
+      return p.d > 8192 || (p.T > num_sms && p.d > 4096) ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
     if (!p.stream_f32 && p.d >= 1024 && (p.d > 4096 || p.T < 10 * num_sms)) return launch_rows<2>(p, num_sms, stream);
     if (p.d > 4096 || (p.stream_f32 && p.d > 2048)) return launch_norm_t<8, 4>(p, stream);
     return p.d > 512 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);

@@ -39,10 +39,10 @@ __device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
-// Larger floats have larger keys; finite values only, never 0 or 1.
+// Larger floats have larger keys, never 0 or 1 (-0 before +0: callers add +0, or a bias, so that the two tie).
 __device__ __forceinline__ uint32_t order_key(float v) {
-  const uint32_t u = __float_as_uint(v + 0.f);           // -0 and +0 tie
-  return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
+  const uint32_t u = __float_as_uint(v);
+  return u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);
 }
 constexpr uint32_t kLeastFinite = 0x00800000u;           // key of the lowest finite value (that of -inf is the one below)
 __device__ __forceinline__ float from_key(uint32_t k) {
@@ -102,7 +102,7 @@ __device__ __forceinline__ void choose_exact(const RouteParams& p, const float (
   for (int j = 0; j < J; ++j) {
     float v = l[j];
     if (p.bias != nullptr && isfinite(v)) v = __fadd_rn(exact_score(p, v, mx, sum), bias[j]);   // bias -inf: taken out
-    key[j] = expert_of(j, lane) >= p.E ? 0u : isfinite(v) ? order_key(v) : 1u;
+    key[j] = expert_of(j, lane) >= p.E ? 0u : isfinite(v) ? order_key(v + 0.f) : 1u;
   }
 #pragma unroll 1
   for (int s = 0; s < p.k; ++s) {
@@ -153,7 +153,7 @@ __device__ __forceinline__ void gather(const RouteParams& p, uint32_t row_addr, 
   }
 }
 
-// One warp, one token: J logits per lane.
+// One warp, NR tokens at once (the chains of dependent steps overlap): J logits of each per lane.
 //
 // Candidates, a few more than k, are found on keys that carry the expert: the upper bits of the order-preserving key of the
 // score, the lower bits count the experts down.  A lane sorts its keys once; a round is then a warp-wide maximum of the
@@ -161,112 +161,122 @@ __device__ __forceinline__ void gather(const RouteParams& p, uint32_t row_addr, 
 // score comes from the fast exponential and division.  Where neighbours among the first k + 1 are nearer than that can be
 // off, the candidates are ordered again by exact keys, a lane each (one or two tokens in 100 on normal logits); where even the
 // last candidate is that near to the k-th, or a logit is not finite, all experts are.
-template <int J>
-__device__ __forceinline__ void pick(const RouteParams& p, int t, const float (&l)[J], const float (&bias)[J], int lane) {
+template <int J, int NR>
+__device__ __forceinline__ void pick(const RouteParams& p, const int (&t)[NR], const bool (&on)[NR], const float (&l)[NR][J],
+                                     const float (&bias)[J], int lane) {
   constexpr int kBits = J == 4 ? 7 : J == 8 ? 8 : 9;
   constexpr uint32_t kMask = (1u << kBits) - 1u;
-  float zero = 0.f;                                      // stays 0 while every logit is finite
-#pragma unroll
-  for (int j = 0; j < J; ++j) zero = fmaf(l[j], 0.f, zero);
-  const bool bad = __any_sync(0xffffffffu, zero != 0.f);   // NaN != 0
-  if (bad && lane == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_LOGIT));
   // Softmax: the row's maximum and sum, where a weight or a biased key needs them (renormalised weights without a bias
   // do not: the sum cancels, and the first expert chosen has the maximum).
   const bool whole = !p.sigmoid && (!p.renormalise || p.bias != nullptr);
-  float mx = 0.f, sum = 1.f;
-  if (whole) {
-    uint32_t m = 0;
+  const int m = min(p.k + 2, 32);
+  bool bad[NR];
+  float mx[NR], sum[NR];
+  uint32_t key[NR][J], mine[NR];                         // mine, lane s: the s-th candidate
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      if (expert_of(j, lane) < p.E && isfinite(l[j])) m = max(m, order_key(l[j]));
-    m = __reduce_max_sync(0xffffffffu, m);
-    mx = m == 0 ? 0.f : from_key(m);
-    float v = 0.f;
+  for (int n = 0; n < NR; ++n) {
+    float zero = 0.f;                                    // stays 0 while every logit is finite
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      if (expert_of(j, lane) < p.E && isfinite(l[j])) v += expf(l[j] - mx);
+    for (int j = 0; j < J; ++j) zero = fmaf(l[n][j], 0.f, zero);
+    bad[n] = __any_sync(0xffffffffu, zero != 0.f);       // NaN != 0
+    mx[n] = 0.f;
+    sum[n] = 1.f;
+    mine[n] = 0;
+    if (whole) {
+      uint32_t top = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    sum = v > 0.f ? v : 1.f;
-  }
-  int id = 0;
-  bool fine = false;                                     // finite logit, finite bias
-  bool again = bad || p.k == 32;                         // 32 choices leave no lane for the first left out
-  uint32_t mine = 0;                                     // lane s: the s-th candidate (0: there are no more experts)
-  const int m = min(p.k + 4, 32);
-  if (!again) {
-    const float inv_sum = 1.f / sum;
-    uint32_t key[J];
+      for (int j = 0; j < J; ++j)
+        if (expert_of(j, lane) < p.E && isfinite(l[n][j])) top = max(top, order_key(l[n][j]));
+      top = __reduce_max_sync(0xffffffffu, top);
+      mx[n] = top == 0 ? 0.f : from_key(top);
+      float v = 0.f;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (expert_of(j, lane) < p.E && isfinite(l[n][j])) v += expf(l[n][j] - mx[n]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      sum[n] = v > 0.f ? v : 1.f;
+    }
+    const float inv_sum = 1.f / sum[n];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      float v = l[j];
-      if (p.bias != nullptr) v = (p.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __expf(v - mx) * inv_sum) + bias[j];
-      key[j] = expert_of(j, lane) >= p.E ? 0u : (order_key(v) & ~kMask) | (kMask - static_cast<uint32_t>(expert_of(j, lane)));
+      float v = l[n][j];
+      if (p.bias != nullptr) v = p.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __expf(v - mx[n]) * inv_sum;
+      key[n][j] = (order_key(v + bias[j]) & ~kMask) | (kMask - static_cast<uint32_t>(expert_of(j, lane)));
     }
-    sort_keys<J>(key);
+    sort_keys<J>(key[n]);
+  }
 #pragma unroll 1
-    for (int s = 0; s < m; ++s) {
-      const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
-      if (lane == s) mine = top;
-      const bool won = key[0] == top;                    // keys differ, except the zeros
+  for (int s = 0; s < m; ++s) {
+    uint32_t top[NR];
 #pragma unroll
-      for (int j = 0; j + 1 < J; ++j) key[j] = won ? key[j + 1] : key[j];
-      key[J - 1] = won ? 0u : key[J - 1];
+    for (int n = 0; n < NR; ++n) top[n] = __reduce_max_sync(0xffffffffu, key[n][0]);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      if (lane == s) mine[n] = top[n];
+      const bool won = key[n][0] == top[n];              // keys differ, except the zeros of lists that have run out
+#pragma unroll
+      for (int j = 0; j + 1 < J; ++j) key[n][j] = won ? key[n][j + 1] : key[n][j];
+      key[n][J - 1] = won ? 0u : key[n][J - 1];
     }
-    id = static_cast<int>(kMask - (mine & kMask));
-    fine = mine >= kLeastFinite;
-    const uint32_t below = __shfl_down_sync(0xffffffffu, mine, 1);
-    again = __any_sync(0xffffffffu, lane < p.k && below >= kLeastFinite && too_near(p, mine, below, kMask));
   }
-  float el = lane_logit<J>(l, id);
-  if (again) {
-    const uint32_t kth = __shfl_sync(0xffffffffu, mine, p.k - 1), last = __shfl_sync(0xffffffffu, mine, m - 1);
-    if (!bad && m > p.k && (last < kLeastFinite || !too_near(p, kth, last, kMask))) {
-      uint32_t exact = 0;
-      if (mine != 0) {
-        float v = el;
-        if (p.bias != nullptr) {
-          const float b = __ldg(p.bias + id);
-          v = isfinite(b) ? __fadd_rn(exact_score(p, v, mx, sum), b) : b;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    if (bad[n] && lane == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_LOGIT));
+    int id = static_cast<int>(kMask - (mine[n] & kMask));
+    bool fine = mine[n] >= kLeastFinite;                 // finite logit, finite bias
+    const uint32_t below = __shfl_down_sync(0xffffffffu, mine[n], 1);
+    const bool near = __any_sync(0xffffffffu, lane < p.k && lane + 1 < m && below >= kLeastFinite && too_near(p, mine[n], below, kMask));
+    float el = lane_logit<J>(l[n], id);
+    if (near || bad[n] || p.k == 32) {                   // 32 choices leave no lane for the first left out
+      const uint32_t kth = __shfl_sync(0xffffffffu, mine[n], p.k - 1), last = __shfl_sync(0xffffffffu, mine[n], m - 1);
+      if (!bad[n] && m > p.k && (last < kLeastFinite || !too_near(p, kth, last, kMask))) {
+        uint32_t exact = 0;
+        if (id < p.E && lane < m) {
+          float v = el;
+          if (p.bias != nullptr) {
+            const float b = __ldg(p.bias + id);
+            v = isfinite(b) ? __fadd_rn(exact_score(p, v, mx[n], sum[n]), b) : b;
+          }
+          exact = isfinite(v) ? order_key(v + 0.f) : 1u;
         }
-        exact = isfinite(v) ? order_key(v) : 1u;
+        int rank = 0;
+        for (int s = 0; s < m; ++s) {
+          const uint32_t o = __shfl_sync(0xffffffffu, exact, s);
+          const int oid = __shfl_sync(0xffffffffu, id, s);
+          rank += o > exact || (o == exact && oid < id) ? 1 : 0;
+        }
+        const uint32_t self = static_cast<uint32_t>(id) | (exact > 1u ? 0x80000000u : 0u);
+        uint32_t got = 0;
+        for (int s = 0; s < m; ++s) {
+          const int r = __shfl_sync(0xffffffffu, rank, s);
+          const uint32_t v = __shfl_sync(0xffffffffu, self, s);
+          if (r == lane) got = v;
+        }
+        id = static_cast<int>(got & 0x7fffffffu);
+        fine = (got >> 31) != 0;
+      } else {
+        choose_exact<J>(p, l[n], bias, mx[n], sum[n], lane, id, fine);
       }
-      int rank = 0;
-      for (int s = 0; s < m; ++s) {
-        const uint32_t o = __shfl_sync(0xffffffffu, exact, s);
-        const int oid = __shfl_sync(0xffffffffu, id, s);
-        rank += o > exact || (o == exact && oid < id) ? 1 : 0;
-      }
-      const uint32_t self = static_cast<uint32_t>(id) | (exact > 1u ? 0x80000000u : 0u);
-      uint32_t got = 0;
-      for (int s = 0; s < m; ++s) {
-        const int r = __shfl_sync(0xffffffffu, rank, s);
-        const uint32_t v = __shfl_sync(0xffffffffu, self, s);
-        if (r == lane) got = v;
-      }
-      id = static_cast<int>(got & 0x7fffffffu);
-      fine = (got >> 31) != 0;
-    } else {
-      choose_exact<J>(p, l, bias, mx, sum, lane, id, fine);
+      el = lane_logit<J>(l[n], id);
     }
-    el = lane_logit<J>(l, id);
-  }
-  if (!whole) mx = __shfl_sync(0xffffffffu, el, 0);
-  float w = 0.f;
-  if (lane < p.k && fine) w = exact_score(p, el, mx, sum);
-  if (p.renormalise) {
-    float v = w;
+    const float top_l = whole ? mx[n] : __shfl_sync(0xffffffffu, el, 0);
+    float w = 0.f;
+    if (lane < p.k && fine) w = exact_score(p, el, top_l, sum[n]);
+    if (p.renormalise) {
+      float v = w;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    w = v > 0.f ? __fdiv_rn(w, v) : 0.f;
-  }
-  if (lane < p.k) {
-    p.ids[static_cast<size_t>(t) * p.k + lane] = id;
-    p.w[static_cast<size_t>(t) * p.k + lane] = w * p.scale;
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      w = v > 0.f ? __fdiv_rn(w, v) : 0.f;
+    }
+    if (lane < p.k && on[n]) {
+      p.ids[static_cast<size_t>(t[n]) * p.k + lane] = id;
+      p.w[static_cast<size_t>(t[n]) * p.k + lane] = w * p.scale;
+    }
   }
 }
 
-template <int JJ>
+template <int JJ, int NR>
 __global__ void __launch_bounds__(kRouteThreads, 1)
 route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const RouteParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -365,7 +375,7 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
   for (int j = 0; j < J; ++j) {
     const int e = 128 * (j / 4) + 4 * lane + j % 4;
     const float b = p.bias != nullptr && e < p.E ? __ldg(p.bias + e) : 0.f;
-    bias[j] = isfinite(b) ? b : -INFINITY;               // a bias that is not finite takes its expert out
+    bias[j] = e < p.E && isfinite(b) ? b : -INFINITY;    // a bias that is not finite takes its expert out, as one that is not there
   }
   if ((warp & 3) * 32 < live) {
     const int row = (warp & 3) * 32 + lane;
@@ -391,19 +401,27 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
   }
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  // The tokens are dealt to the cluster's CTAs and their warps.
-  for (int r = static_cast<int>(rank) + S * warp; r < p.tile_rows && t0 + r < p.T; r += S * kWarps) {
-    const int t = t0 + r;
-    if (r >= live) {                                     // a padding row
-      if (lane < p.k) {
-        p.ids[static_cast<size_t>(t) * p.k + lane] = -1;
-        p.w[static_cast<size_t>(t) * p.k + lane] = 0.f;
+  // The tokens are dealt to the cluster's CTAs and their warps, NR at a time.
+  const int step = S * kWarps;
+  for (int r0 = static_cast<int>(rank) + S * warp; r0 < p.tile_rows && t0 + r0 < p.T; r0 += NR * step) {
+    int t[NR];
+    bool on[NR];
+    float l[NR][J];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = r0 + n * step;
+      t[n] = t0 + r;
+      on[n] = r < live;
+      if (!on[n] && r < p.tile_rows && t[n] < p.T && lane < p.k) {       // a padding row
+        p.ids[static_cast<size_t>(t[n]) * p.k + lane] = -1;
+        p.w[static_cast<size_t>(t[n]) * p.k + lane] = 0.f;
       }
-      continue;
     }
-    float l[J];
-    gather<JJ>(p, logits_addr + 4u * static_cast<uint32_t>(r * pitch), lane, l);
-    pick<J>(p, t, l, bias, lane);
+    if (!on[0]) continue;                                // rows beyond it are padding too
+#pragma unroll
+    for (int n = 0; n < NR; ++n)                         // a row that is not there repeats the first
+      gather<JJ>(p, logits_addr + 4u * static_cast<uint32_t>((on[n] ? r0 + n * step : r0) * pitch), lane, l[n]);
+    pick<J, NR>(p, t, on, l, bias, lane);
   }
   // nobody leaves while a peer may still read its logits
   __syncwarp();
@@ -422,11 +440,11 @@ route_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CU
 
 constexpr int kRouteSmem = 226 * 1024;      // the most a launch asks for
 
-template <int JJ>
+template <int JJ, int NR>
 static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW, const RouteParams& p, int ctas,
                                   size_t smem, cudaStream_t stream) {
   static std::atomic<unsigned long long> smem_set{0};
-  cudaError_t e = smem_limit_once(route_kernel<JJ>, kRouteSmem, smem_set);
+  cudaError_t e = smem_limit_once(route_kernel<JJ, NR>, kRouteSmem, smem_set);
   if (e != cudaSuccess) return e;
   if (p.splits > 8) {
     static std::atomic<unsigned long long> wide_set{0};
@@ -435,7 +453,7 @@ static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW
     if (e != cudaSuccess) return e;
     const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
     if (bit == 0 || !(wide_set.load(std::memory_order_acquire) & bit)) {
-      e = cudaFuncSetAttribute(route_kernel<JJ>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      e = cudaFuncSetAttribute(route_kernel<JJ, NR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return e;
       if (bit != 0) wide_set.fetch_or(bit, std::memory_order_release);
     }
@@ -453,7 +471,7 @@ static cudaError_t launch_route_t(const CUtensorMap& tmX, const CUtensorMap& tmW
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, route_kernel<JJ>, tmX, tmW, p);
+  return cudaLaunchKernelEx(&cfg, route_kernel<JJ, NR>, tmX, tmW, p);
 }
 
 // Clusters of 16 CTAs (one per SM) that this device runs at once; 0 where it refuses them.  Asked once per device.
@@ -464,8 +482,8 @@ static int wide_clusters() {
   const int known = cached[dev].load(std::memory_order_acquire);
   if (known != 0) return known - 1;
   int n = 0;
-  if (cudaFuncSetAttribute(route_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRouteSmem) != cudaSuccess ||
-      cudaFuncSetAttribute(route_kernel<1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+  if (cudaFuncSetAttribute(route_kernel<1, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRouteSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(route_kernel<1, 1>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
     (void)cudaGetLastError();
   } else {
     cudaLaunchConfig_t cfg = {};
@@ -478,7 +496,7 @@ static int wide_clusters() {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, route_kernel<1>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, route_kernel<1, 1>, &cfg) != cudaSuccess) {
       (void)cudaGetLastError();                          // a refused query must not poison the next launch
       n = 0;
     }
@@ -520,9 +538,11 @@ cudaError_t launch_route(const CUtensorMap& tmX, const CUtensorMap& tmW, RoutePa
   const size_t ring = static_cast<size_t>(r.stages) * r.stage_bytes;
   const size_t table = static_cast<size_t>(r.tile_rows) * p.pitch * 4;
   const size_t smem = (ring > table ? ring : table) + 1024;
-  if (p.E <= 128) return launch_route_t<1>(tmX, tmW, p, r.ctas, smem, stream);
-  if (p.E <= 256) return launch_route_t<2>(tmX, tmW, p, r.ctas, smem, stream);
-  return launch_route_t<4>(tmX, tmW, p, r.ctas, smem, stream);
+  // two tokens per warp at a time where every warp has at least two (16 logits per lane leave no registers for it)
+  const bool two = min(r.tile_rows, p.T) / r.splits >= 2 * (kRouteThreads / 32);
+  if (p.E <= 128) return two ? launch_route_t<1, 2>(tmX, tmW, p, r.ctas, smem, stream) : launch_route_t<1, 1>(tmX, tmW, p, r.ctas, smem, stream);
+  if (p.E <= 256) return two ? launch_route_t<2, 2>(tmX, tmW, p, r.ctas, smem, stream) : launch_route_t<2, 1>(tmX, tmW, p, r.ctas, smem, stream);
+  return launch_route_t<4, 1>(tmX, tmW, p, r.ctas, smem, stream);
 }
 
 }  // namespace tempo
