@@ -532,15 +532,17 @@ static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
 //   Fewer than two rows per SM: one chunk per thread, the shortest chain (one row of 4096: 2.4 us with one, 2.6 with two, 3.2
 //   with four; 203 rows 3.9, 4.3, 5.4), unless two CTAs of that many threads do not fit an SM and there are more rows than SMs
 //   (290 rows of 7168: 5.4 us with one, 4.0 with two).
-//   More: the kernel with several rows per CTA where a CTA gets few of them or they are wide (d = 7168: 600 rows 7.6 us
-//   against 10.9, 8192 rows 87 against 102; 1024 rows of 4096: 6.8 against 9.4), else one row per CTA, whose CTAs' phases mix
-//   (8192 rows of 2048: 24.1 us against 25.7; 2048 of 4096: 14.9 against 15.7).  An f32 stream has half as many elements to
-//   its bytes and needs the registers: one row per CTA, four chunks (8192 rows of 7168: 123 us against 161).
+//   More: the kernel with several rows per CTA where the parameter folds (4096 rows of 4096 23.3 us against 28.9, before a block
+//   12.7 against 14.6), or a CTA gets few rows or wide ones (600 rows of 7168: 7.6 us against 10.9, 8192 rows 87 against 102); else
+//   one row per CTA, whose CTAs' phases mix (8192 rows of 2048, two parameters after the first norm: 24.1 us against 25.7),
+//   and below d = 1024, unless 512 columns leave no thread idle (8192 rows of 512: 7.9 us against 9.7; of 1000: 18.0 against 15.1).
+//   An f32 stream has half as many elements to its bytes and needs the registers: one row per CTA, four chunks (8192 rows of
+//   7168: 123 us against 161).
 cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream) {
   if (vec == 8) {
     if (p.T < 2 * num_sms)
       return p.d > 8192 || (p.T > num_sms && p.d > 4096) ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
-    if (!p.stream_f32 && p.d >= 1024 && (p.d > 4096 || p.T < 10 * num_sms || p.y == nullptr || folds(p))) return launch_rows<2>(p, num_sms, stream);
+    if (!p.stream_f32 && (p.d >= 1024 || p.d == 512) && (p.d > 4096 || p.T < 10 * num_sms || p.y == nullptr || folds(p))) return launch_rows<2>(p, num_sms, stream);
     if (p.d > 4096 || (p.stream_f32 && p.d > 2048)) return launch_norm_t<8, 4>(p, stream);
     return p.d > 512 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
   }
