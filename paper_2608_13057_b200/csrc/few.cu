@@ -41,6 +41,10 @@ constexpr int kFewHalf = 8;                 // fewest gate/up blocks per CTA of 
 
 // ---- small helpers --------------------------------------------------------------------------------
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+// Adds to a counter after everything this thread has seen written (a barrier before it makes that the CTA's writes).
+__device__ __forceinline__ void add_release(int32_t* p, int v) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 // Barrier of n threads that tells every one of them whether `ok` held in all.
 __device__ __forceinline__ bool bar_all(int id, int n, bool ok) {
@@ -290,7 +294,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
         }
         L.pa[i] = static_cast<int16_t>(v < 0 ? -1 : v);
         L.w[i] = w[j];
-        if (v >= 0) atomicOr(&L.mask[v], 1ull << (i / k));           // the union of bits: no order
+        if (v >= 0) {                                                // the union of bits: no order
+          const int t = i / k;
+          atomicOr(reinterpret_cast<uint32_t*>(&L.mask[v]) + (t >> 5), 1u << (t & 31));   // (low word first)
+        }
       }
     }
     if (bad && cta == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_BAD_ID));
@@ -362,10 +369,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       }
     }
     bar_sync(3, 256);
-    if (tid == 128 && static_cast<int>(cta) < x_want) {
-      __threadfence();
-      atomicAdd(x_done, 1);
-    }
+    if (tid == 128 && static_cast<int>(cta) < x_want) add_release(x_done, 1);
     for (int i = static_cast<int>(cta) * 256 + tid - 128; i < p.counter_ints; i += static_cast<int>(C) * 256) cnt_next[i] = 0;
     bar_sync(2, kFewThreads);
   }
@@ -617,10 +621,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_acc_empty[slot]));
         bar_sync(3, 256);
-        if (et == 0) {                                              // publish the partial sums, or H
-          __threadfence();
-          atomicAdd(s.kb0 > 0 ? part_done + ph * C + cta : h_done + 32 * ph, 1);
-        }
+        if (et == 0) add_release(s.kb0 > 0 ? part_done + ph * C + cta : h_done + 32 * ph, 1);   // the partial sums, or H
       }
     }
     // ---- down: partial sums of (256 output columns, expert), one row of Y per (token, expert) pair -----------
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
       while (ok && s.next()) {
         if (s.nt != pend_nt && pend > 0) {
           bar_sync(3, 256);
-          if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
+          if (et == 0) add_release(y_cnt + pend_nt, pend);
           pend = 0;
         }
         const uint32_t slot = p.slots == 2 ? n_seg & 1u : 0u, use = p.slots == 2 ? n_seg >> 1 : n_seg;
@@ -667,7 +668,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
     }
     if (pend > 0) {
       bar_sync(3, 256);
-      if (et == 0) { __threadfence(); atomicAdd(y_cnt + pend_nt, pend); }
+      if (et == 0) add_release(y_cnt + pend_nt, pend);
     }
     // ---- weighted sums: the CTAs of a column block share its (token, 4 columns) items --------------------------
     if (A == 0) {
