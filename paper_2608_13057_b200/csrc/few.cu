@@ -565,14 +565,24 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
               }
             continue;
           }
-#pragma unroll 2
-          for (int c = static_cast<int>(cta) + 1; c <= last; ++c) { // the other parts, in the order of the runs
-            const float* src = p.gu_part + (static_cast<size_t>(ph) * C + c) * T * 256 + row;
+          for (int ca = static_cast<int>(cta) + 1; ca <= last; ca += 3) {   // the other parts, three in flight, in the order of the runs
+            float v3[3][kFewBatch][2];
 #pragma unroll
-            for (int i = 0; i < kFewBatch; ++i)
-              if (c0 + i < n_col) {
-                gu[i][0] += __ldcg(src + (c0 + i) * 256);
-                gu[i][1] += __ldcg(src + (c0 + i) * 256 + 128);
+            for (int m = 0; m < 3; ++m) {
+              const float* src = p.gu_part + (static_cast<size_t>(ph) * C + min(ca + m, last)) * T * 256 + row;
+#pragma unroll
+              for (int i = 0; i < kFewBatch; ++i) {
+                const bool on = ca + m <= last && c0 + i < n_col;
+                v3[m][i][0] = on ? __ldcg(src + (c0 + i) * 256) : 0.f;
+                v3[m][i][1] = on ? __ldcg(src + (c0 + i) * 256 + 128) : 0.f;
+              }
+            }
+#pragma unroll
+            for (int m = 0; m < 3; ++m)
+#pragma unroll
+              for (int i = 0; i < kFewBatch; ++i) {
+                gu[i][0] += v3[m][i][0];
+                gu[i][1] += v3[m][i][1];
               }
           }
           // H of this (expert, 128-column block): SwiGLU, the two-term split, straight into the operand image
