@@ -318,8 +318,8 @@ int tempo_grouped_ffn_bf16(const tempo_shape* shape, const void* a_bf16, const v
  *   token, (d, 1) per element; both 0 one number.
  *   Optional (NULL): b, post_w (y is not normed), post_b, gate (1), next_b, n_valid, and x' with next_w.
  *   Rows are d elements at pitches ld_* >= d (elements); rows t >= n_valid are neither read nor written.  r' may be r and
- *   x' may be y (same address and pitch).  Any d from 1 to 16384; rows that 16-byte (8-, 4-byte) vectors do not divide
- *   or align run with narrower loads.  Pointers need the alignment of their element (TEMPO_ERR_ALIGN).
+ *   x' may be y (same address and pitch).  Any d from 1 to 16384; rows that 16-byte vectors do not divide or
+ *   align take 8-byte ones, or go through shared memory (bf16), or run with narrower loads.  Pointers need the alignment of their element (TEMPO_ERR_ALIGN).
  */
 enum { TEMPO_NORM_RMS = 0, TEMPO_NORM_LAYER = 1 };
 typedef struct {

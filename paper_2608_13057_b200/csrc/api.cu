@@ -474,8 +474,11 @@ static int run_norm(NormParams& p, cudaStream_t stream) {
   const int sms = sm_count();
   if (sms <= 0) return TEMPO_ERR_CUDA;
   const int vec = norm_vec(p);
-  const size_t gs = p.gate_f32 ? (vec >= 4 ? 16 : 4 * vec) : 2 * vec;
-  p.gate_vec = p.gate != nullptr && p.gate_col == 1 && p.gate_row % vec == 0 && aligned(p.gate, gs) ? 1 : 0;
+  p.shift = norm_shifts(p, vec);
+  const int pv = p.shift ? 8 : vec;
+  const size_t gs = p.gate_f32 ? (pv >= 4 ? 16 : 4 * pv) : 2 * pv;
+  p.gate_vec = p.gate != nullptr && p.gate_col == 1 && p.gate_row % pv == 0 && aligned(p.gate, gs) ? 1 : 0;
+  p.param_vec = aligned(p.next_w, 16) && aligned(p.next_b, 16) && aligned(p.post_w, 16) && aligned(p.post_b, 16);
   return launch_norm(p, vec, sms, stream) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
 }
 

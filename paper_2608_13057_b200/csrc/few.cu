@@ -7,15 +7,25 @@
 //     (256 weight rows x 128 bytes of K, already in the shared-memory image) is the A operand of two M 128
 //     instructions, and N is the number of token columns, a multiple of 16.  No row of a tile is padding.
 //   - The blocks (tiles of 32 KB) of all chosen experts' gate/up matrices are dealt to the CTAs as equal contiguous
-//     runs, whatever expert or column block they belong to; a column block that spans CTAs is summed by the CTA that
-//     finishes it last, from 32-bit partials in the workspace, in the order of the runs.  The down matrices likewise.
-//   - A CTA's ring goes on with down weights while the other CTAs still finish H.
+//     runs, whatever expert or column block they belong to; a gate/up column block that spans CTAs is summed by the CTA
+//     that has its first block (that one ends its run there, so it is the last thing it does), from the others' 32-bit
+//     partial sums in the workspace, in the order of the runs.  The down matrices are dealt in the same way.
+//   - With enough blocks the experts are taken in two halves (gate/up 1, gate/up 2, down 1, down 2): while one half's H
+//     is summed and published the other half's weights stream, and the ring goes on with down weights all the same
+//     (one token of 8 experts, 4096 x 1536: 34.0 us in halves, 35.6 us without).
 //   - Activations are not rounded to 8 bits.  fp8 weights: a bf16 value has 8 significant bits, an e4m3 value 4, so
 //     x = 2^eps (q1 + q2 / 16) with two e4m3 terms is x itself for everything within 2^-13 of the block's largest value
 //     (and within 2^-22 of that value below), and each token takes two columns whose block scales differ by 2^4; the
 //     two sums are added in 32 bits.  H is split the same way: 8 bits like a bf16 rounding, with 0.4 of its mean error.
 //     bf16 weights: x as it is, H as two bf16 terms (16 bits).
 // A value of x or H that is not finite becomes a NaN code: its token's output is NaN, no other token's.
+//
+// What bounds it: the weight stream.  Measured, each against the chosen weights' bytes at the rate of a plain copy: one
+// token of 8 experts, d 4096, f 1536, fp8: 31.8 us against 23.1; 64 tokens over 16 experts of the same: 55.3 against
+// 46.2 (305 MB read from memory for 302 MB of weights); 11 tokens over 41 experts, d 2048, f 1024, bf16: 106.7 against
+// 110.3 (a stream that only reads runs above the copy's rate).  What stays above the stream, about 9 us, is latency: the
+// expert lists and the first tiles, 4 us; the last half's H, about 2 us beside the down weights; the sum over experts, 3 us.
+// With few bytes that latency is all there is: 11.4 us for 5 tokens at d 256, f 512.
 //
 // Phases of a CTA (one per SM, 384 threads): warps 4-11 write their share of the x operand image to the workspace while
 // warps 0-3 build the expert lists; warp 0 streams weight tiles, warp 2 token tiles (they wait for the image, then for
@@ -34,9 +44,15 @@ namespace tempo {
 constexpr int kFewThreads = 384;
 constexpr int kFewRing = 8;                 // most stages
 constexpr int kFewBudget = 222 * 1024;      // dynamic shared memory: ring, then the lists
-constexpr uint32_t kFewFlight = 3;     // weight tiles of a CTA on their way at a time
-constexpr int kFewRun = 8;                  // fewest blocks of a gate/up line that are worth a CTA of their own
-constexpr int kFewBatch = 4;                // token columns that an epilogue group takes at a time
+// Weight tiles of a CTA on their way at a time: 96 KB per SM cover the memory's latency at its full rate; 2 leave gaps, and
+// with 4 the CTAs that a line is shared by drift apart (both slower on every size measured).
+constexpr uint32_t kFewFlight = 3;
+// Fewest blocks of a gate/up line that are worth a CTA of their own (2, 4 and 16 were slower where a phase has few blocks,
+// and make no difference where it has many).
+constexpr int kFewRun = 8;
+// Token columns that an epilogue group takes at a time.  8 would serve many tokens on one expert (64: 34.5 us, not 35.6), but
+// their registers cost every other size 0.2 to 0.5 us.
+constexpr int kFewBatch = 4;
 constexpr int kFewHalf = 8;                 // fewest gate/up blocks per CTA of a half
 
 // ---- small helpers --------------------------------------------------------------------------------

@@ -6,6 +6,10 @@
 // the row, each a shuffle tree in a warp and a fixed-order sum over the warps (32-bit, the same bits every time); the
 // centred square sum is taken after the mean from the registers, not as a difference of two large sums.
 // x' is taken from the 32-bit r', not from its rounding to the stream's type.
+// Bound by the bytes: 8192 x 7168 with a gate per channel reads y and r and writes r' and x', 470 MB, in 79.7 us, 90 % of a
+// copy's rate in long runs (two copies of the same bytes take 78.3 us); one row is the latency of a launch and a load, 2.4 us.
+// Rows at odd addresses are bound by instructions (49 a column and thread, 60 % of the issue slots): 4096 x 5001 in 50 us of 25.
+// Which kernel a shape gets, and the figures behind that, stand at the launcher below.
 #include "tempo_kernels.cuh"
 
 namespace tempo {
@@ -25,6 +29,10 @@ __device__ __forceinline__ void load_bf16_stream(const __nv_bfloat16* p, uint32_
   }
 }
 
+// The first n bytes of 16, the rest zero.
+__device__ __forceinline__ void copy16_part(void* dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(n) : "memory");
+}
 __device__ __forceinline__ void copy16(void* dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
@@ -153,7 +161,8 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
-// A thread's values of a row: CH chunks of VEC neighbours, as pairs.  kSplit (rows that no vector divides or aligns): a
+// A thread's values of a row: CH chunks of VEC neighbours, as pairs.  kSplit (rows that no vector divides or aligns, where they do
+// not go through shared memory): a
 // chunk is two single elements, blockDim.x columns apart, so that a warp still reads neighbours; the second may lie beyond the
 // row when the first does not.
 template <int VEC, int CH>
@@ -162,6 +171,7 @@ template <int CH>
 struct Cols {
   int col[CH];
   bool on[CH], on2[CH];      // first, second element of a split chunk inside the row
+  int n[CH];                 // elements of a chunk inside the row (at most VEC)
   int nt;                    // distance of a split chunk's elements
 };
 template <int VEC, int CH, bool kSplit, bool kFull>
@@ -172,6 +182,7 @@ __device__ __forceinline__ void set_cols(Cols<CH>& k, int d) {
     k.col[c] = kSplit ? 2 * c * k.nt + static_cast<int>(threadIdx.x) : (c * k.nt + static_cast<int>(threadIdx.x)) * VEC;
     k.on[c] = kFull || k.col[c] < d;
     k.on2[c] = kSplit ? k.col[c] + k.nt < d : k.on[c];
+    k.n[c] = max(0, min(VEC, d - k.col[c]));
   }
 }
 template <int VEC>
@@ -222,9 +233,110 @@ __device__ __forceinline__ void store_f32_chunk(float* p, const float2 (&v)[VEC 
   }
 }
 
+// ---- rows at any alignment (kShift) ---------------------------------------------------------------
+// A row that starts h elements (0 to 7) past a 16-byte boundary: its granule g (16 aligned bytes) holds the columns 8 g - h to
+// 8 g - h + 7, so a thread's eight columns lie in two granules, and a granule's in the columns of two threads.
+__device__ __forceinline__ int row_shift(const __nv_bfloat16* row) { return static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1) & 7; }
+
+// u[c] = eight elements from element `off` (0 to 7, the same for the CTA) of the 16-byte words first + c * nt and the next one
+// on; a word before `base` is not needed and not read.
+template <int CH, int K>
+__device__ __forceinline__ void windows_at(const uint4* base, const uint4* first, int nt, uint32_t sh, uint32_t (&u)[CH][4]) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const uint4* q = first + c * nt;
+    const uint4 lo = *(c == 0 && q < base ? base : q), hi = q[1];
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[c][i] = __funnelshift_r(w[K + i], w[K + i + 1], sh);
+  }
+}
+template <int CH>
+__device__ __forceinline__ void windows(const uint4* base, int first, int nt, int off, uint32_t (&u)[CH][4]) {
+  const uint4* q = base + first;
+  const uint32_t sh = (off & 1) * 16;
+  switch (off >> 1) {
+    case 0:
+      if (off == 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const uint4 w = q[c * nt];
+          u[c][0] = w.x; u[c][1] = w.y; u[c][2] = w.z; u[c][3] = w.w;
+        }
+      } else {
+        windows_at<CH, 0>(base, q, nt, sh, u);
+      }
+      break;
+    case 1: windows_at<CH, 1>(base, q, nt, sh, u); break;
+    case 2: windows_at<CH, 2>(base, q, nt, sh, u); break;
+    default: windows_at<CH, 3>(base, q, nt, sh, u);
+  }
+}
+// A thread's columns of a row whose granules are in shared memory, zero beyond the row.
+template <int CH>
+__device__ __forceinline__ void load_shifted(const uint4* granules, int h, const Cols<CH>& k, uint32_t (&u)[CH][4]) {
+  windows<CH>(granules, threadIdx.x, k.nt, h, u);
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (k.n[c] < 8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[c][i] = 2 * i + 1 < k.n[c] ? u[c][i] : 2 * i < k.n[c] ? u[c][i] & 0xffffu : 0u;
+    }
+}
+// A thread's columns to shared memory, rounded, where store_shifted takes them from.
+template <int CH>
+__device__ __forceinline__ void stage_row(uint4* stage, const Cols<CH>& k, const RowVals<8, CH>& a) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(a.v[c][i].x, a.v[c][i].y);
+      u[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    stage[c * k.nt + threadIdx.x] = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+}
+// Writes a staged row (after a barrier): whole granules, and the row's two edges by element.
+template <int CH>
+__device__ __forceinline__ void store_shifted(__nv_bfloat16* row, const uint4* stage, const Cols<CH>& k, int d) {
+  const int h = row_shift(row), tid = threadIdx.x;
+  uint32_t u[CH][4];
+  windows<CH>(stage, tid - (h > 0), k.nt, (8 - h) & 7, u);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int a = k.col[c] - h;                         // the granule's first column
+    if (a >= 0 && a + 8 <= d) {
+      __stcs(reinterpret_cast<uint4*>(row + a), make_uint4(u[c][0], u[c][1], u[c][2], u[c][3]));
+    } else if (a < d) {
+      uint16_t* q = reinterpret_cast<uint16_t*>(row) + a;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (a + i >= 0 && a + i < d) q[i] = static_cast<uint16_t>(u[c][i / 2] >> (16 * (i & 1)));
+    }
+  }
+  if (tid < h) {                                        // the granule behind the last thread's
+    const int col = 8 * CH * k.nt - h + tid;
+    if (col < d) reinterpret_cast<uint16_t*>(row)[col] = reinterpret_cast<const uint16_t*>(stage)[col];
+  }
+}
+// Eight neighbours of a parameter, n of them inside the row; `vec`: they can be read in 16-byte loads.
+__device__ __forceinline__ void load_param_part(const void* base, size_t at, int is_f32, bool vec, int n, float (&v)[8]) {
+  if (vec && n == 8) {
+    load_param<8>(base, at, is_f32, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float f[1] = {0.f};
+      if (i < n) load_param<1>(base, at + i, is_f32, f);
+      v[i] = f[0];
+    }
+  }
+}
+
 // v -> normed in place, without weights and without the final factor, which is returned: 1 / sqrt(mean square + eps).
 // Values beyond the row are zero and stay so; kFull: there are none.
-template <int VEC, int CH, bool kSplit, bool kFull>
+template <int VEC, int CH, bool kSplit, bool kFull, bool kShift>
 __device__ __forceinline__ float norm_row(RowVals<VEC, CH>& a, const Cols<CH>& k, int layer, float inv_d, float eps,
                                           float (&s_part)[2][32], int& slot) {
   const int warps = k.nt >> 5;
@@ -242,6 +354,13 @@ __device__ __forceinline__ float norm_row(RowVals<VEC, CH>& a, const Cols<CH>& k
         const float2 m = make_float2(-mean, !kSplit || k.on2[c] ? -mean : 0.f);
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i) a.v[c][i] = add2(a.v[c][i], m);
+        if (kShift && k.n[c] < VEC) {
+#pragma unroll
+          for (int i = 0; i < VEC / 2; ++i) {
+            if (2 * i >= k.n[c]) a.v[c][i].x = 0.f;
+            if (2 * i + 1 >= k.n[c]) a.v[c][i].y = 0.f;
+          }
+        }
       }
   }
   float2 q = make_float2(0.f, 0.f);
@@ -255,8 +374,9 @@ __device__ __forceinline__ float norm_row(RowVals<VEC, CH>& a, const Cols<CH>& k
 }
 
 // v *= the parameter, or += it.
-template <int VEC, int CH, bool kSplit, bool kFull, bool kAdd>
-__device__ __forceinline__ void apply_param(RowVals<VEC, CH>& a, const void* base, size_t at, int is_f32, const Cols<CH>& k) {
+template <int VEC, int CH, bool kSplit, bool kFull, bool kShift, bool kAdd>
+__device__ __forceinline__ void apply_param(RowVals<VEC, CH>& a, const void* base, size_t at, int is_f32, const Cols<CH>& k,
+                                            [[maybe_unused]] bool vec) {
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     if (!kFull && !k.on[c]) continue;
@@ -268,6 +388,8 @@ __device__ __forceinline__ void apply_param(RowVals<VEC, CH>& a, const void* bas
       if (k.on2[c]) load_param<1>(base, at + k.col[c] + k.nt, is_f32, f1);
       f[0] = f0[0];
       f[1] = f1[0];
+    } else if constexpr (kShift) {
+      load_param_part(base, at + k.col[c], is_f32, vec, k.n[c], f);
     } else {
       load_param<VEC>(base, at + k.col[c], is_f32, f);
     }
@@ -301,10 +423,11 @@ __device__ __forceinline__ void scale_row(RowVals<VEC, CH>& a, float f) {
 // Everything between a row's loads and its stores.  yu: the block's output (kOut); ru or r: the stream; zero beyond the row.
 // kFold: the parameter that follows the first norm, the same for every row, comes from `fold` in 32 bits (this thread's words:
 // [chunk][pair of float4][thread]): post_w, times a gate per channel, or next_w in the norm before a block.
-template <int VEC, int CH, bool kSplit, bool kF32, bool kOut, bool kFull, bool kFold = false>
+template <int VEC, int CH, bool kSplit, bool kF32, bool kOut, bool kFull, bool kFold = false, bool kShift = false>
 __device__ __forceinline__ void finish_row(const NormParams& p, size_t row, const Cols<CH>& k, const uint32_t (&yu)[CH][VEC / 2],
                                            const uint32_t (&ru)[CH][VEC / 2], RowVals<VEC, CH>& r, float (&s_part)[2][32], int& slot,
-                                           const float4* fold = nullptr) {
+                                           const float4* fold = nullptr, [[maybe_unused]] uint4* stage_r = nullptr,
+                                           [[maybe_unused]] uint4* stage_x = nullptr) {
   const float inv_d = 1.f / static_cast<float>(p.d);
   RowVals<VEC, CH> a;
   float f[VEC];
@@ -316,14 +439,14 @@ __device__ __forceinline__ void finish_row(const NormParams& p, size_t row, cons
       to_pairs<VEC>(f, a.v[c]);
     }
     if constexpr (kFold) {
-      ys *= norm_row<VEC, CH, kSplit, kFull>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+      ys *= norm_row<VEC, CH, kSplit, kFull, kShift>(a, k, p.layer, inv_d, p.eps, s_part, slot);
       apply_fold<VEC, CH, kFull>(a, fold, k);
     } else if (p.post_w != nullptr) {
-      const float inv = norm_row<VEC, CH, kSplit, kFull>(a, k, p.layer, inv_d, p.eps, s_part, slot);
-      apply_param<VEC, CH, kSplit, kFull, false>(a, p.post_w, 0, p.param_f32, k);
+      const float inv = norm_row<VEC, CH, kSplit, kFull, kShift>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+      apply_param<VEC, CH, kSplit, kFull, kShift, false>(a, p.post_w, 0, p.param_f32, k, p.param_vec);
       if (p.post_b != nullptr) {
         scale_row<VEC, CH>(a, inv);
-        apply_param<VEC, CH, kSplit, kFull, true>(a, p.post_b, 0, p.param_f32, k);
+        apply_param<VEC, CH, kSplit, kFull, kShift, true>(a, p.post_b, 0, p.param_f32, k, p.param_vec);
       } else {
         ys *= inv;
       }
@@ -335,14 +458,14 @@ __device__ __forceinline__ void finish_row(const NormParams& p, size_t row, cons
         ys *= g1[0];
       } else if (kFold) {                               // in the folded parameter
       } else if (p.gate_vec) {
-        apply_param<VEC, CH, kSplit, kFull, false>(a, p.gate, row * p.gate_row, p.gate_f32, k);
+        apply_param<VEC, CH, kSplit, kFull, kShift, false>(a, p.gate, row * p.gate_row, p.gate_f32, k, true);
       } else {                                          // columns at a pitch of their own
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           if (!kFull && !k.on[c]) continue;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            if (kSplit && i == 1 && !k.on2[c]) continue;
+            if ((kSplit && i == 1 && !k.on2[c]) || (kShift && i >= k.n[c])) continue;
             float g1[1];
             load_param<1>(p.gate, row * p.gate_row + static_cast<size_t>(k.col[c] + (kSplit ? i * k.nt : i)) * p.gate_col, p.gate_f32, g1);
             (i & 1 ? a.v[c][i / 2].y : a.v[c][i / 2].x) *= g1[0];
@@ -359,10 +482,16 @@ __device__ __forceinline__ void finish_row(const NormParams& p, size_t row, cons
 #pragma unroll
       for (int i = 0; i < VEC / 2; ++i)
         a.v[c][i] = fma2(a.v[c][i], make_float2(ys, ys), mul2(r.v[c][i], make_float2(p.r_scale, p.r_scale)));
-      if (kFull || k.on[c]) {
+      if (!kShift && (kFull || k.on[c])) {
         if constexpr (kF32) store_f32_chunk<VEC, kSplit>(static_cast<float*>(p.r_out) + row * p.ld_r_out + k.col[c], a.v[c], k.nt, k.on2[c]);
         else store_bf16_chunk<VEC, kSplit>(static_cast<__nv_bfloat16*>(p.r_out) + row * p.ld_r_out + k.col[c], a.v[c], k.nt, k.on2[c]);
       }
+    }
+    if constexpr (kShift) {
+      if (p.post_w == nullptr || k.nt == 32) __syncthreads();   // every thread has read y: its words take r'
+      stage_row<CH>(stage_r, k, a);
+      if (p.x == nullptr || k.nt == 32) __syncthreads();
+      if (p.x == nullptr) store_shifted<CH>(static_cast<__nv_bfloat16*>(p.r_out) + row * p.ld_r_out, stage_r, k, p.d);
     }
     if (p.x == nullptr) return;
   } else {
@@ -377,14 +506,23 @@ __device__ __forceinline__ void finish_row(const NormParams& p, size_t row, cons
       }
     }
   }
-  const float inv = norm_row<VEC, CH, kSplit, kFull>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+  const float inv = norm_row<VEC, CH, kSplit, kFull, kShift>(a, k, p.layer, inv_d, p.eps, s_part, slot);
+  // a barrier (in the sum) lies behind: r' is staged, and every thread has read r
+  if constexpr (kShift && kOut) store_shifted<CH>(static_cast<__nv_bfloat16*>(p.r_out) + row * p.ld_r_out, stage_r, k, p.d);
   if constexpr (kFold && !kOut) apply_fold<VEC, CH, kFull>(a, fold, k);
-  else apply_param<VEC, CH, kSplit, kFull, false>(a, p.next_w, 0, p.param_f32, k);
+  else apply_param<VEC, CH, kSplit, kFull, kShift, false>(a, p.next_w, 0, p.param_f32, k, p.param_vec);
   scale_row<VEC, CH>(a, inv);
-  if (p.next_b != nullptr) apply_param<VEC, CH, kSplit, kFull, true>(a, p.next_b, 0, p.param_f32, k);
+  if (p.next_b != nullptr) apply_param<VEC, CH, kSplit, kFull, kShift, true>(a, p.next_b, 0, p.param_f32, k, p.param_vec);
+  if constexpr (kShift) {
+    if (k.nt == 32) __syncwarp();
+    stage_row<CH>(stage_x, k, a);
+    __syncthreads();
+    store_shifted<CH>(p.x + row * p.ld_x, stage_x, k, p.d);
+  } else {
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
-    if (kFull || k.on[c]) store_bf16_chunk<VEC, kSplit>(p.x + row * p.ld_x + k.col[c], a.v[c], k.nt, k.on2[c]);
+    for (int c = 0; c < CH; ++c)
+      if (kFull || k.on[c]) store_bf16_chunk<VEC, kSplit>(p.x + row * p.ld_x + k.col[c], a.v[c], k.nt, k.on2[c]);
+  }
 }
 
 // One row per CTA.  kOut: the norm after a block (p.y), else the norm before one.  kF32: the residual stream is f32.
@@ -487,6 +625,78 @@ __global__ void __maxnreg__(64) norm_rows_kernel(const NormParams p) {
   }
 }
 
+// Rows of bf16 at any pitch, width and alignment.  As norm_rows_kernel, but a row is copied as the 16-byte granules that it
+// has in memory; a thread's eight columns come from two of them, and the results go back through the same shared memory and out
+// in whole granules, single elements at the row's two edges alone (two more barriers per row).
+template <int CH, bool kOut, bool kFold>
+__global__ void __maxnreg__(64) norm_shift_kernel(const NormParams p) {
+  extern __shared__ uint4 s_row[];                      // [buffer][y, r][granule], then the folded parameters
+  __shared__ float s_part[2][32];
+  constexpr int kR = kOut ? 1 : 0, kStreams = kR + 1;
+  pdl_trigger();
+  pdl_wait();
+  int rows = p.T;
+  if (p.n_valid != nullptr) rows = max(0, min(*p.n_valid, p.T));
+  Cols<CH> k;
+  set_cols<8, CH, false, false>(k, p.d);
+  const int nt = k.nt, tid = threadIdx.x, pitch = CH * nt + 1;
+  auto fetch_row = [&](const __nv_bfloat16* base, size_t ld, int t, uint4* dst) {
+    const size_t at = static_cast<size_t>(t) * ld;
+    const __nv_bfloat16* row = base + at;
+    const int h = row_shift(row);
+#pragma unroll
+    for (int c = 0; c <= CH; ++c) {
+      const int g = c * nt + tid, a = 8 * g - h;        // granule, its first column
+      if ((c == CH && tid > 0) || a >= p.d) continue;
+      // The columns before the row's first are the end of the row before, or what lies between the two; the granule
+      // that begins before the first row of all is read by element.
+      if (a >= 0 || at >= static_cast<size_t>(h)) {
+        copy16_part(dst + g, row + a, static_cast<uint32_t>(min(16, 2 * (p.d - a))));
+      } else {
+        uint16_t* e = reinterpret_cast<uint16_t*>(dst + g);
+        for (int i = h; i < min(8, h + p.d); ++i) e[i] = reinterpret_cast<const uint16_t*>(row)[i - h];
+      }
+    }
+  };
+  auto fetch = [&](int t, int buf) {
+    if (t < rows) {
+      if constexpr (kOut) fetch_row(p.y, p.ld_y, t, s_row + buf * kStreams * pitch);
+      fetch_row(static_cast<const __nv_bfloat16*>(p.r), p.ld_r, t, s_row + (buf * kStreams + kR) * pitch);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int slot = 0, buf = 0;
+  fetch(blockIdx.x, 0);
+  float4* fold = reinterpret_cast<float4*>(s_row + 2 * kStreams * pitch) + tid;
+  if constexpr (kFold) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (!k.on[c]) continue;
+      float w[8], g[8];
+      load_param_part(kOut ? p.post_w : p.next_w, k.col[c], p.param_f32, p.param_vec, k.n[c], w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = 1.f;
+      if (kOut && p.gate != nullptr && p.gate_col != 0) load_param_part(p.gate, k.col[c], p.gate_f32, p.gate_vec, k.n[c], g);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        fold[(2 * c + h) * nt] = make_float4(w[4 * h] * g[4 * h], w[4 * h + 1] * g[4 * h + 1], w[4 * h + 2] * g[4 * h + 2], w[4 * h + 3] * g[4 * h + 3]);
+    }
+  }
+  for (int t = blockIdx.x; t < rows; t += gridDim.x, buf ^= 1) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();                                    // every thread's copies of row t are here, and row t - grid was read
+    fetch(t + gridDim.x, buf ^ 1);
+    uint32_t yu[CH][4], ru[CH][4];
+    RowVals<8, CH> r;
+    const size_t row = static_cast<size_t>(t);
+    uint4* in_y = s_row + buf * kStreams * pitch;
+    uint4* in_r = in_y + kR * pitch;
+    if constexpr (kOut) load_shifted<CH>(in_y, row_shift(p.y + row * p.ld_y), k, yu);
+    load_shifted<CH>(in_r, row_shift(static_cast<const __nv_bfloat16*>(p.r) + row * p.ld_r), k, ru);
+    finish_row<8, CH, false, false, kOut, false, kFold, true>(p, row, k, yu, ru, r, s_part, slot, fold, in_y, in_r);
+  }
+}
+
 template <int VEC, int CH, bool kSplit, bool kF32, bool kOut>
 static cudaError_t launch_norm_o(const NormParams& p, cudaStream_t stream) {
   const int threads = ((p.d + VEC * CH - 1) / (VEC * CH) + 31) / 32 * 32;
@@ -498,7 +708,8 @@ static cudaError_t launch_norm_o(const NormParams& p, cudaStream_t stream) {
 // Whether the norm after a block has one parameter between its first norm and the sum: post_w, alone or with a gate per token
 // or per channel.
 static bool folds(const NormParams& p) {
-  return p.post_w != nullptr && p.post_b == nullptr && (p.gate == nullptr || p.gate_col == 0 || (p.gate_vec && p.gate_row == 0));
+  return p.post_w != nullptr && p.post_b == nullptr &&
+         (p.gate == nullptr || p.gate_col == 0 || (p.gate_row == 0 && (p.shift ? p.gate_col == 1 : p.gate_vec != 0)));
 }
 
 template <int CH, bool kOut, bool kFull, bool kFold>
@@ -521,12 +732,37 @@ static cudaError_t launch_rows(const NormParams& p, int num_sms, cudaStream_t st
   return p.d == 8 * CH * threads ? launch_rows_t<CH, true>(p, threads, num_sms, stream) : launch_rows_t<CH, false>(p, threads, num_sms, stream);
 }
 
+template <int CH, bool kOut, bool kFold>
+static cudaError_t launch_shift_f(const NormParams& p, int num_sms, cudaStream_t stream) {
+  static std::atomic<unsigned long long> smem_set{0};
+  const int threads = ((p.d + 8 * CH - 1) / (8 * CH) + 31) / 32 * 32;
+  const int smem = (2 * (kOut ? 2 : 1) * (CH * threads + 1) + (kFold ? 2 * CH * threads : 0)) * 16;
+  cudaError_t e = smem_limit_once(norm_shift_kernel<CH, kOut, kFold>, 200 * 1024, smem_set);
+  if (e != cudaSuccess) return e;
+  const int per_sm = max(1, min(min(32, 65536 / (64 * threads)), 224 * 1024 / (smem + 1280)));   // CTAs that are resident
+  return launch_pdl(norm_shift_kernel<CH, kOut, kFold>, dim3(min(p.T, per_sm * num_sms)), dim3(threads), smem, stream, p);
+}
+template <int CH>
+static cudaError_t launch_shift(const NormParams& p, int num_sms, cudaStream_t stream) {
+  if (p.y == nullptr) return launch_shift_f<CH, false, true>(p, num_sms, stream);
+  return folds(p) ? launch_shift_f<CH, true, true>(p, num_sms, stream) : launch_shift_f<CH, true, false>(p, num_sms, stream);
+}
+
+template <int VEC, int CH, bool kSplit>
+static cudaError_t launch_norm_f32(const NormParams& p, cudaStream_t stream) {
+  return p.y ? launch_norm_o<VEC, CH, kSplit, true, true>(p, stream) : launch_norm_o<VEC, CH, kSplit, true, false>(p, stream);
+}
 template <int VEC, int CH, bool kSplit = false>
 static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
-  if (p.stream_f32)
-    return p.y ? launch_norm_o<VEC, CH, kSplit, true, true>(p, stream) : launch_norm_o<VEC, CH, kSplit, true, false>(p, stream);
+  if (p.stream_f32) return launch_norm_f32<VEC, CH, kSplit>(p, stream);
   return p.y ? launch_norm_o<VEC, CH, kSplit, false, true>(p, stream) : launch_norm_o<VEC, CH, kSplit, false, false>(p, stream);
 }
+
+// Rows of bf16 that only loads of one or two elements fit: through shared memory in 16-byte pieces (8192 rows of 7168 at a pitch
+// of 7171: 117 us, element by element 383; 4096 of 5001 50 against 101, of 5002 50 against 59; one row of 4001 4.1 against
+// 4.4), not rows so short that most of a warp idles (3000 of 257: 7.3 against 6.5; 8192 of 511: 17.5 against 19.0).
+// Four elements at a time keep their own loads (4096 of 5004: 38.4 us, through shared memory 50).
+bool norm_shifts(const NormParams& p, int vec) { return !p.stream_f32 && vec <= 2 && p.d >= 384; }
 
 // vec: the widest load that every pointer and pitch allows (8, 4, 2 or 1 elements).
 //   Fewer than two rows per SM: one chunk per thread, the shortest chain (one row of 4096: 2.4 us with one, 2.6 with two, 3.2
@@ -538,6 +774,8 @@ static cudaError_t launch_norm_t(const NormParams& p, cudaStream_t stream) {
 //   and below d = 1024, unless 512 columns leave no thread idle (8192 rows of 512: 7.9 us against 9.7; of 1000: 18.0 against 15.1).
 //   An f32 stream has half as many elements to its bytes and needs the registers: one row per CTA, four chunks (8192 rows of
 //   7168: 123 us against 161).
+//   p.shift: one chunk per thread for few or short rows (515 rows of 1021: 3.3 us against 3.7, after a block 5.6 against 7.0),
+//   two for the rest (8192 rows of 1021 10.7 us against 14.8; 4096 of 2048 at a pitch of 2051 20.4 against 22.9).
 cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream) {
   if (vec == 8) {
     if (p.T < 2 * num_sms)
@@ -546,16 +784,16 @@ cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t 
     if (p.d > 4096 || (p.stream_f32 && p.d > 2048)) return launch_norm_t<8, 4>(p, stream);
     return p.d > 512 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
   }
+  if (p.shift) {
+    if (p.d > 8192 || (p.T > num_sms && p.d > 1024) || (p.T > 10 * num_sms && p.d > 512)) return launch_shift<2>(p, num_sms, stream);
+    return launch_shift<1>(p, num_sms, stream);
+  }
   if (vec == 4) {
     if (p.d <= 4096) return launch_norm_t<4, 1>(p, stream);
     return launch_norm_t<4, 4>(p, stream);
   }
-  if (vec == 2) {
-    if (p.d <= 4096) return launch_norm_t<2, 2>(p, stream);
-    return launch_norm_t<2, 8>(p, stream);
-  }
-  if (p.d <= 4096) return launch_norm_t<2, 2, true>(p, stream);
-  return launch_norm_t<2, 8, true>(p, stream);
+  if (p.d <= 4096) return vec == 2 ? launch_norm_t<2, 2>(p, stream) : launch_norm_t<2, 2, true>(p, stream);
+  return vec == 2 ? launch_norm_f32<2, 8, false>(p, stream) : launch_norm_f32<2, 8, true>(p, stream);
 }
 
 }  // namespace tempo

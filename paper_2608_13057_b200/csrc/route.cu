@@ -5,10 +5,19 @@
 // shared memory) and splits the reduction over d between its CTAs: with few tokens that spreads the router's weights
 // over S SMs, with many tokens it brings the number of CTAs up to the number of SMs.  Per CTA: a ring of TMA tiles
 // (tokens x 64 and experts x 64 bf16 values, 128-byte swizzle), tcgen05.mma.kind::f16 (M 128, N = experts) into tensor
-// memory, the partial logits to shared memory; then the CTAs share the tile's tokens out, and a warp sums a token's S
-// partials in rank order (the same bits every time) over distributed shared memory and picks its experts:
-// every lane holds up to 16 logits, and rounds of a warp-wide maximum on order-preserving integer keys take the best left;
-// ties go to the lowest index.  Logits, scores and weights stay in 32 bits.
+// memory, the partial logits to shared memory; then the CTAs share the tile's tokens out, and a warp sums its tokens' S
+// partials in rank order (the same bits every time) over distributed shared memory and picks their experts: every lane
+// holds up to 16 logits as order-preserving integer keys whose low bits carry the expert, sorted in the lane; rounds of a
+// warp-wide integer maximum take the k best and two more, and only where two of those are closer than the bits that
+// the expert took are they put in order by their full values.  Ties go to the lowest index.  Logits, scores and
+// weights stay in 32 bits, and every step that decides between experts is rounded singly.
+//
+// S: few tokens take a split as wide as a cluster goes (16 where the device runs such clusters), since the weights' way
+// from memory to one SM is the time; many tokens take the split that fills the SMs.  What bounds it, as measured: one
+// token of d 4096, 128 experts 5.5 us, of which a launch alone is 2.3, the rest a chain of latencies (tiles, tensor cores,
+// cluster barrier, 8 rounds); 8192 tokens of d 7168, 256 experts 40 us, 18.6 by the operations at the library rate: the
+// main loop runs at 85 % of it per SM on 128 of 148 SMs (24 us: tiles of 128 tokens come in whole numbers), the sum and the
+// choice (integer instructions of all warps) take the rest.
 //
 // A logit that is not finite counts as minus infinity: it is chosen after every finite one, with weight 0.
 #include "mma_warp.cuh"

@@ -141,6 +141,8 @@ cudaError_t launch_ffn_gather(const CUtensorMap& tmA2, const CUtensorMap& tmY, c
 struct NormParams {
   int T, d, layer;           // layer: subtract the row's mean
   int stream_f32, param_f32, gate_f32, gate_vec;   // gate_vec: the gate's row can be read with the row's vectors
+  bool shift;                // eight columns at a time at any alignment (norm_shifts)
+  bool param_vec;            // the weights and biases can be read in 16-byte loads
   const __nv_bfloat16* y;    // NULL: the norm before a block
   const void* r;
   const void* post_w;
@@ -154,6 +156,7 @@ struct NormParams {
   size_t ld_y, ld_r, ld_r_out, ld_x, gate_row, gate_col;
   float eps, r_scale, y_scale;
 };
+bool norm_shifts(const NormParams& p, int vec);
 cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t stream);
 
 struct RoutePlan {

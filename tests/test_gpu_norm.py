@@ -112,6 +112,47 @@ def test_norms_match_the_formula(B, T, d, pad, shift, kind, f32, pf32, gate):
         assert (whole[keep] == -77.0).all()
 
 
+@pytest.mark.parametrize("T,d,kind,place", [
+    (9, 1, 0, (1, 2, 3, 5)), (11, 7, 1, (7, 0, 6, 1)), (8, 8, 0, (4, 4, 3, 2)), (8, 9, 1, (0, 1, 2, 3)), (16, 255, 0, (5, 6, 7, 0)),
+    (16, 256, 1, (3, 3, 3, 3)), (16, 257, 0, (1, 1, 1, 1)), (350, 2056, 1, (2, 4, 6, 0)), (350, 2311, 0, (0, 0, 0, 0)),
+    (700, 1030, 1, (6, 1, 4, 7)), (310, 8193, 0, (1, 0, 7, 2)), (3, 12345, 1, (4, 7, 2, 5))])
+def test_operands_at_alignments_of_their_own(B, T, d, kind, place):
+    """Rows of bf16 that begin anywhere between two 16-byte boundaries, each operand elsewhere, and the in-place form."""
+    g = torch.Generator(device="cuda").manual_seed(T * 31 + d)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    bf = torch.bfloat16
+    (y, y_all), (r, r_all), (ro, ro_all), (x, x_all) = (strided(T, d, pad, bf, float("nan"), s) for pad, s in zip((0, 3, 1, 2), place))
+    y.copy_(rnd(T, d) * 0.5 + 0.25)
+    r.copy_(rnd(T, d) * 3 + 1)
+    off = torch.empty(d + 1, device="cuda")
+    pw, w, gt = (1 + 0.2 * rnd(d)), off[1:], rnd(1, d)             # one weight that no 16-byte load reaches
+    w.copy_(1 + 0.2 * rnd(d))
+    eps = 1e-5
+    outside = []
+    for whole, rows, pad, s in ((ro_all, ro, 1, place[2]), (x_all, x, 2, place[3]), (r_all, r, 3, place[1]), (y_all, y, 0, place[0])):
+        keep = torch.ones_like(whole, dtype=torch.bool)
+        keep[s:].as_strided((T, d), (d + pad, 1)).fill_(False)
+        outside.append((whole, keep))
+    B.tempo_norm_out(y, r, ro, pw, None, gt, w, None, x, kind=kind, eps=eps, r_scale=0.75, y_scale=1.25)
+    n, e = norm64(y, pw, None, kind, eps)
+    n, e = n * gt.double(), e * gt.double().abs()
+    ref = 0.75 * r.double() + 1.25 * n
+    err = 1.25 * e + E32 * (1.25 * n.abs() + 0.75 * r.double().abs())
+    check(ro, ref, err)
+    n, e = norm64(ref, w, None, kind, eps)
+    s = torch.sqrt((((ref - ref.mean(1, keepdim=True)) if kind else ref) ** 2).mean(1, keepdim=True) + eps)
+    check(x, n, e + (2 * err + err.amax(1, keepdim=True)) / s * w.double().abs() * (1 + ref.abs().amax(1, keepdim=True) / s))
+    first, second = ro.clone(), x.clone()
+    B.tempo_norm_in(r, w, x, kind=kind, eps=eps)
+    n, e = norm64(r, w, None, kind, eps)
+    check(x, n, e)
+    B.tempo_norm_out(y, r, r, pw, None, gt, w, None, y, kind=kind, eps=eps, r_scale=0.75, y_scale=1.25)
+    torch.cuda.synchronize()
+    assert torch.equal(r, first) and torch.equal(y, second)
+    for whole, keep in outside:                                    # nothing around or between the rows is written
+        assert torch.isnan(whole[keep]).all()
+
+
 def test_optional_operands(B):
     T, d = 5, 640
     y, r = torch.randn(T, d, device="cuda").bfloat16(), torch.randn(T, d, device="cuda").bfloat16()
