@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libtempo.so.  Argument marshalling only: every step runs in the CUDA kernels.
+"""Thin binding of libtempo.so (ctypes; the extension module _marshal for the norms, the router and the few-token FFN).
+Argument marshalling only: every step runs in the CUDA kernels.
 
 The functions carry the C-ABI names (see include/tempo.h).  Tensors are torch CUDA tensors used as
 device memory; kernels are enqueued on torch's current stream.  There is no CPU fallback: importing
