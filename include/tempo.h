@@ -343,6 +343,7 @@ int tempo_norm_out(const tempo_norm* args, const void* y_bf16, const void* r, co
  *   ids[t, :] = the k experts with the largest logits, or with the largest p + bias where a bias is given, in falling
  *               order; ties go to the lowest expert
  *   w[t, s] = p[t, ids[t, s]], divided by its sum over s if `renormalise`, times `scale`
+ *             (renormalised weights exist however small the scores are, also where no p of the token has a 32-bit value)
  * A logit that is not finite is chosen after every finite one, with weight 0 (TEMPO_STATUS_BAD_LOGIT); so is, without the
  * status bit, an expert whose bias is not finite (-inf takes an expert out).  The k ids of a token are always distinct.
  * Rows t >= n_valid get ids -1 and weights 0.

@@ -83,6 +83,11 @@ __device__ __forceinline__ void sort_keys(uint32_t (&v)[J]) {
 __device__ __forceinline__ float exact_score(const RouteParams& p, float l, float mx, float sum) {
   return p.sigmoid ? sigmoid_rn(l) : __fdiv_rn(expf(l - mx), sum);
 }
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
 // The logit of expert `id` (every lane asks for its own), from the lane that holds it; an index into the registers would
 // put them into local memory.
 template <int J>
@@ -202,8 +207,7 @@ __device__ __forceinline__ void pick(const RouteParams& p, const int (&t)[NR], c
 #pragma unroll
       for (int j = 0; j < J; ++j)
         if (expert_of(j, lane) < p.E && isfinite(l[n][j])) v += expf(l[n][j] - mx[n]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      v = warp_sum(v);
       sum[n] = v > 0.f ? v : 1.f;
     }
     const float inv_sum = 1.f / sum[n];
@@ -273,9 +277,14 @@ __device__ __forceinline__ void pick(const RouteParams& p, const int (&t)[NR], c
     float w = 0.f;
     if (lane < p.k && fine) w = exact_score(p, el, top_l, sum[n]);
     if (p.renormalise) {
-      float v = w;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      float v = warp_sum(w);
+      if (p.sigmoid && v < 0x1p-60f) {                   // (the same in every lane)
+        // Logits below -41, where 1 / (1 + exp(-l)) is exp(l) to 2^-59 of itself; below -87 it has no normal 32-bit value,
+        // while the quotient by the sum has one: exp(l - m) over the sum of those, m the largest logit chosen.
+        const uint32_t m = __reduce_max_sync(0xffffffffu, lane < p.k && fine ? order_key(el) : 0u);
+        w = lane < p.k && fine ? expf(el - from_key(m)) : 0.f;
+        v = warp_sum(w);
+      }
       w = v > 0.f ? __fdiv_rn(w, v) : 0.f;
     }
     if (lane < p.k && on[n]) {
