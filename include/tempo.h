@@ -363,7 +363,7 @@ int tempo_route(const tempo_shape* shape, int32_t score, int32_t renormalise, fl
  * chosen expert's weights are read once; no 128-row padding, no quota table.  `packed` is the blob of tempo_pack_weights
  * (tempo_pack_weights_bf16 for the _bf16 call).  Unlike steps 2 and 3, x and H are not rounded to 8 bits: both enter the
  * products as two e4m3 terms (8 significant bits; x exactly), in the _bf16 call as bf16 (x) and two bf16 terms (H).
- * A value of x or H that is not finite makes its own token's output NaN.  Rows without a local expert and rows t >= n_valid
+ * A value of x or H that is not finite (the _bf16 call: an H beyond bf16's range) makes its own token's output NaN.  Rows without a local expert and rows t >= n_valid
  * are zero.  An id outside [0, E) of a live row is ignored (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token
  * counts twice.  Results do not depend on timing; nothing is summed with atomics.
  *   in   x bf16 [T, d] (16-byte aligned), topk_ids i32 [T, k], topk_w f32 [T, k], n_valid or NULL,

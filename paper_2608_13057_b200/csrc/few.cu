@@ -18,7 +18,8 @@
 //     (and within 2^-22 of that value below), and each token takes two columns whose block scales differ by 2^4; the
 //     two sums are added in 32 bits.  H is split the same way: 8 bits like a bf16 rounding, with 0.4 of its mean error.
 //     bf16 weights: x as it is, H as two bf16 terms (16 bits).
-// A value of x or H that is not finite becomes a NaN code: its token's output is NaN, no other token's.
+// A value of H that is not finite (bf16 weights: beyond bf16's range), and with fp8 weights one of x, becomes a NaN: its
+// token's output is NaN, no other token's.  With bf16 weights an x that is not finite makes H so.
 //
 // What bounds it: the weight stream.  Measured, each against the chosen weights' bytes at the rate of a plain copy: one
 // token of 8 experts, d 4096, f 1536, fp8: 31.8 us against 23.1; 64 tokens over 16 experts of the same: 55.3 against
@@ -611,8 +612,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const FewParams p) 
             for (int i = 0; i < kFewBatch; ++i)
               if (c0 + i < n_col) {
                 const int col = c0 + i, r2 = C8 + col;
-                const __nv_bfloat16 hi = __float2bfloat16_rn(gu[i][0]);
+                // beyond bf16's range: NaN, as the other form's codes (an infinite first term alone would give an infinite output)
+                __nv_bfloat16 hi = __float2bfloat16_rn(gu[i][0]);
                 const float hf = __bfloat162float(hi);
+                if (!isfinite(hf)) hi = __ushort_as_bfloat16(0x7fff);
                 const __nv_bfloat16 lo = __float2bfloat16_rn(isfinite(hf) ? gu[i][0] - hf : 0.f);
                 *reinterpret_cast<__nv_bfloat16*>(blk + col * 128 + (((ii >> 3) ^ (col & 7)) << 4) + (ii & 7) * 2) = hi;
                 *reinterpret_cast<__nv_bfloat16*>(blk + r2 * 128 + (((ii >> 3) ^ (r2 & 7)) << 4) + (ii & 7) * 2) = lo;
