@@ -47,6 +47,11 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
   return t;
 }
 
+// Elements that the C entry reads or writes by the sizes it is given.
+void holds(PyObject* o, int64_t want, const char* what) {
+  if (o != Py_None && THPVariable_Unpack(o).numel() < want) refuse(what, ": expected at least ", want, " elements");
+}
+
 // Address of a contiguous tensor of the given type; None is a NULL pointer.
 void* addr(PyObject* o, at::ScalarType dtype, const char* what) {
   if (o == Py_None) return nullptr;
@@ -54,6 +59,12 @@ void* addr(PyObject* o, at::ScalarType dtype, const char* what) {
   if (!t.is_contiguous()) refuse(what, ": expected a contiguous tensor");
   if (t.scalar_type() != dtype) refuse(what, ": expected dtype ", dtype, ", got ", t.scalar_type());
   return t.data_ptr();
+}
+// Address of a device word: n_valid, status.  An empty tensor has none, and NULL would mean that no count is given.
+void* word(PyObject* o, const char* what) {
+  void* p = addr(o, at::kInt, what);
+  holds(o, 1, what);
+  return p;
 }
 
 bool is_f32(const at::Tensor& t, const char* what) {
@@ -135,7 +146,7 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.param_f32 = f32 > 0;
     a.kind = static_cast<int32_t>(integer(v[4]));
     a.eps = number(v[5]);
-    return g_norm_in(&a, r, w, b, static_cast<const int32_t*>(addr(v[6], at::kInt, "n_valid")), x, stream());
+    return g_norm_in(&a, r, w, b, static_cast<const int32_t*>(word(v[6], "n_valid")), x, stream());
   });
 }
 
@@ -171,7 +182,7 @@ PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.r_scale = number(v[11]);
     a.y_scale = number(v[12]);
     return g_norm_out(&a, y, r, post_w, post_b, gate, next_w, next_b,
-                      static_cast<const int32_t*>(addr(v[13], at::kInt, "n_valid")), r_out, x, stream());
+                      static_cast<const int32_t*>(word(v[13], "n_valid")), r_out, x, stream());
   });
 }
 
@@ -181,11 +192,6 @@ const tempo_shape* shape_at(PyObject* o) {
   return static_cast<const tempo_shape*>(p);
 }
 
-// Rows of a [T, ...] buffer that the C entry reads or writes by the shape's sizes.
-void holds(PyObject* o, int64_t want, const char* what) {
-  if (o != Py_None && THPVariable_Unpack(o).numel() < want) refuse(what, ": expected at least ", want, " elements");
-}
-
 // (shape address, x, w_router, bias, n_valid, topk_ids, topk_w, status, score, renormalise, scale)
 PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
@@ -193,10 +199,10 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* x = addr(v[1], at::kBFloat16, "x");
     void* wr = addr(v[2], at::kBFloat16, "w_router");
     void* bias = addr(v[3], at::kFloat, "bias");
-    void* nv = addr(v[4], at::kInt, "n_valid");
+    void* nv = word(v[4], "n_valid");
     void* ids = addr(v[5], at::kInt, "topk_ids");
     void* w = addr(v[6], at::kFloat, "topk_w");
-    void* status = addr(v[7], at::kInt, "status");
+    void* status = word(v[7], "status");
     if (s != nullptr && s->T > 0 && s->d > 0 && s->E > 0 && s->k > 0) {
       const int64_t T = s->T;
       holds(v[1], T * s->d, "x");
@@ -218,11 +224,11 @@ PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* x = addr(v[2], at::kBFloat16, "x");
     void* ids = addr(v[3], at::kInt, "topk_ids");
     void* w = addr(v[4], at::kFloat, "topk_w");
-    void* nv = addr(v[5], at::kInt, "n_valid");
+    void* nv = word(v[5], "n_valid");
     void* map = addr(v[6], at::kInt, "replica_map");
     void* packed = addr(v[7], at::kByte, "packed");
     void* out = addr(v[8], at::kBFloat16, "out");
-    void* status = addr(v[9], at::kInt, "status");
+    void* status = word(v[9], "status");
     void* workspace = addr(v[10], at::kByte, "workspace");
     if (s != nullptr && s->T > 0 && s->d > 0 && s->E > 0 && s->k > 0 && s->R_max > 0) {
       const int64_t T = s->T;
