@@ -276,6 +276,7 @@ def tempo_grouped_ffn_bf16(shape, a_bf16, packed, inst_off, m_pad, h_bf16, y_bf1
 # ---- norms around the block, the router, the layer for a few tokens ------------------------------
 # With one token a kernel of this section takes a few microseconds, less than ctypes marshalling from Python: the
 # extension module _marshal (csrc/marshal.cpp) checks the tensors and calls the same library's C entry points.
+# Every operand is on the current device.
 
 _marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
                             ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",

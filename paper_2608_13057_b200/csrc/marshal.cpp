@@ -4,6 +4,7 @@
 // library that is called is the one it loaded.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -45,6 +46,22 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) refuse("expected a CUDA tensor (the library has no CPU path)");
   return t;
+}
+
+// The tensors among a call's arguments are on one device, and that is the current one: the kernel goes to its current stream.
+void one_device(PyObject* const* v, Py_ssize_t n) {
+  int dev = -1;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (v[i] == Py_None || PyLong_Check(v[i]) || PyFloat_Check(v[i]) || !THPVariable_Check(v[i])) continue;
+    const at::Tensor& t = THPVariable_Unpack(v[i]);
+    if (!t.is_cuda()) refuse("expected a CUDA tensor (the library has no CPU path)");
+    const int d = t.get_device();
+    if (dev >= 0 && d != dev) refuse("operands on cuda:", dev, " and cuda:", d);
+    dev = d;
+  }
+  if (dev < 0) return;
+  const int current = c10::cuda::current_device();
+  if (dev != current) refuse("operands on cuda:", dev, ", but the current device is cuda:", current);
 }
 
 // Elements that the C entry reads or writes by the sizes it is given.
@@ -136,6 +153,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F f) {
 // (r, w, x_out, b, kind, eps, n_valid)
 PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> int {
+    one_device(v, n);
     tempo_norm a{};
     stream_shape(v[0], a);
     int f32 = -1;
@@ -153,6 +171,7 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // (y, r, r_out, post_w, post_b, gate, next_w, next_b, x_out, kind, eps, r_scale, y_scale, n_valid)
 PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 14, [&]() -> int {
+    one_device(v, n);
     tempo_norm a{};
     stream_shape(v[1], a);
     const at::ScalarType dtype = a.stream_f32 ? at::kFloat : at::kBFloat16;
@@ -195,6 +214,7 @@ const tempo_shape* shape_at(PyObject* o) {
 // (shape address, x, w_router, bias, n_valid, topk_ids, topk_w, status, score, renormalise, scale)
 PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
+    one_device(v, n);
     const tempo_shape* s = shape_at(v[0]);
     void* x = addr(v[1], at::kBFloat16, "x");
     void* wr = addr(v[2], at::kBFloat16, "w_router");
@@ -220,6 +240,7 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // (bf16, shape address, x, topk_ids, topk_w, n_valid, replica_map, packed, out, status, workspace)
 PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
+    one_device(v, n);
     const tempo_shape* s = shape_at(v[1]);
     void* x = addr(v[2], at::kBFloat16, "x");
     void* ids = addr(v[3], at::kInt, "topk_ids");

@@ -1,7 +1,9 @@
 """Counts and status words without an element are refused: they have no address, and a count without one would mean that every
-row is live."""
+row is live.  Operands on another device than the current one (fakes without memory) are refused too."""
 import pytest
 import torch
+
+from tests.test_marshal_operands import CALLS, fakes
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +51,10 @@ def test_empty_counts_and_status_words(B):
             assert "expected at least 1 elements" in str(e), (name, str(e))
     torch.cuda.synchronize()
     assert not accepted and (out == 5).all()
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_operands_on_another_device_than_the_current_one(B, name):
+    operands, call = CALLS[name]
+    with pytest.raises(B.TempoError, match="operands on cuda:1, but the current device is cuda:0"):
+        call(B, B.make_shape(4, 2, 8, 2, 1, 128, 128, 128), fakes(*operands))
