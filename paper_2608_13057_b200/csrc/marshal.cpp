@@ -125,15 +125,22 @@ void stream_shape(PyObject* o, tempo_norm& a) {
   a.d = static_cast<int32_t>(t.size(1));
 }
 
+// Numbers and flags are converted before a tensor is looked at: the conversion may run Python code and may fail.
 float number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Refused("");
   return static_cast<float>(v);
 }
-long integer(PyObject* o) {
+int32_t integer(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) throw Refused("");
-  return v;
+  if (v < INT32_MIN || v > INT32_MAX) refuse("expected a 32-bit integer, got ", static_cast<int64_t>(v));
+  return static_cast<int32_t>(v);
+}
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Refused("");
+  return v != 0;
 }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
@@ -153,8 +160,10 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F f) {
 // (r, w, x_out, b, kind, eps, n_valid)
 PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> int {
-    one_device(v, n);
     tempo_norm a{};
+    a.kind = integer(v[4]);
+    a.eps = number(v[5]);
+    one_device(v, n);
     stream_shape(v[0], a);
     int f32 = -1;
     void* r = rows(v[0], a.stream_f32 ? at::kFloat : at::kBFloat16, "r", a.T, a.d, a.ld_r);
@@ -162,8 +171,6 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* x = rows(v[2], at::kBFloat16, "x_out", a.T, a.d, a.ld_x);
     const void* b = param(v[3], "b", a.d, f32);
     a.param_f32 = f32 > 0;
-    a.kind = static_cast<int32_t>(integer(v[4]));
-    a.eps = number(v[5]);
     return g_norm_in(&a, r, w, b, static_cast<const int32_t*>(word(v[6], "n_valid")), x, stream());
   });
 }
@@ -171,8 +178,12 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // (y, r, r_out, post_w, post_b, gate, next_w, next_b, x_out, kind, eps, r_scale, y_scale, n_valid)
 PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 14, [&]() -> int {
-    one_device(v, n);
     tempo_norm a{};
+    a.kind = integer(v[9]);
+    a.eps = number(v[10]);
+    a.r_scale = number(v[11]);
+    a.y_scale = number(v[12]);
+    one_device(v, n);
     stream_shape(v[1], a);
     const at::ScalarType dtype = a.stream_f32 ? at::kFloat : at::kBFloat16;
     int f32 = -1;
@@ -196,10 +207,6 @@ PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const void* next_b = param(v[7], "next_b", a.d, f32);
     void* x = v[8] == Py_None ? nullptr : rows(v[8], at::kBFloat16, "x_out", a.T, a.d, a.ld_x);
     a.param_f32 = f32 > 0;
-    a.kind = static_cast<int32_t>(integer(v[9]));
-    a.eps = number(v[10]);
-    a.r_scale = number(v[11]);
-    a.y_scale = number(v[12]);
     return g_norm_out(&a, y, r, post_w, post_b, gate, next_w, next_b,
                       static_cast<const int32_t*>(word(v[13], "n_valid")), r_out, x, stream());
   });
@@ -214,8 +221,11 @@ const tempo_shape* shape_at(PyObject* o) {
 // (shape address, x, w_router, bias, n_valid, topk_ids, topk_w, status, score, renormalise, scale)
 PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
-    one_device(v, n);
     const tempo_shape* s = shape_at(v[0]);
+    const int32_t score = integer(v[8]);
+    const bool renormalise = truth(v[9]);
+    const float scale = number(v[10]);
+    one_device(v, n);
     void* x = addr(v[1], at::kBFloat16, "x");
     void* wr = addr(v[2], at::kBFloat16, "w_router");
     void* bias = addr(v[3], at::kFloat, "bias");
@@ -231,7 +241,7 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
       holds(v[5], T * s->k, "topk_ids");
       holds(v[6], T * s->k, "topk_w");
     }
-    return g_route(s, static_cast<int32_t>(integer(v[8])), static_cast<int32_t>(PyObject_IsTrue(v[9])), number(v[10]), x, wr,
+    return g_route(s, score, renormalise, scale, x, wr,
                    static_cast<const float*>(bias), static_cast<const int32_t*>(nv), static_cast<int32_t*>(ids),
                    static_cast<float*>(w), static_cast<uint32_t*>(status), stream());
   });
@@ -240,8 +250,9 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // (bf16, shape address, x, topk_ids, topk_w, n_valid, replica_map, packed, out, status, workspace)
 PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
-    one_device(v, n);
+    const bool bf16 = truth(v[0]);
     const tempo_shape* s = shape_at(v[1]);
+    one_device(v, n);
     void* x = addr(v[2], at::kBFloat16, "x");
     void* ids = addr(v[3], at::kInt, "topk_ids");
     void* w = addr(v[4], at::kFloat, "topk_w");
@@ -259,7 +270,6 @@ PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
       holds(v[6], static_cast<int64_t>(s->E) * s->R_max, "replica_map");
       holds(v[8], T * s->d, "out");
     }
-    const int bf16 = PyObject_IsTrue(v[0]) ? 1 : 0;
     size_t bytes = 0;                                   // a shape that these refuse, the call refuses too
     if (g_few_bytes(s, &bytes) == TEMPO_OK) holds(v[10], static_cast<int64_t>(bytes), "workspace");
     if (g_packed_bytes[bf16](s, &bytes) == TEMPO_OK) holds(v[7], static_cast<int64_t>(bytes), "packed");

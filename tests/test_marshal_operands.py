@@ -1,5 +1,6 @@
 """The extension module that marshals the short calls, without a GPU: operands on several devices are refused before an address
 is taken, and an argument that cannot be converted raises its own error.  Tensors of two GPUs are fakes without memory."""
+import ctypes
 from unittest import mock
 
 import pytest
@@ -44,3 +45,24 @@ def test_operands_on_two_devices(B, name, operand):
     s = B.make_shape(4, 2, 8, 2, 1, 128, 128, 128)
     with pytest.raises(B.TempoError, match="cuda:0 and cuda:1|cuda:1 and cuda:0"):
         CALLS[name][1](B, s, fakes(operand))
+
+
+class Unsure:
+    def __bool__(self):
+        raise ZeroDivisionError("neither")
+
+
+def test_arguments_that_cannot_be_converted_raise_their_own_error(B):
+    from paper_2608_13057_b200 import _marshal
+    s, o = B.make_shape(4, 2, 8, 2, 1, 128, 128, 128), fakes()
+    with pytest.raises(ZeroDivisionError):
+        B.tempo_route(s, o["x"], o["wr"], None, None, o["ids"], o["tw"], o["st"], renormalise=Unsure())
+    with pytest.raises(ZeroDivisionError):
+        _marshal.few(Unsure(), ctypes.addressof(s), *(o[n] for n in ("x", "ids", "tw", "n_valid", "rmap", "packed", "ro", "st", "ws")))
+    with pytest.raises(TypeError):
+        B.tempo_norm_in(o["r"], o["w"], o["x"], eps="small")
+    for kind in (2 ** 32, -2 ** 31 - 1, 2 ** 80):                   # 2^32 is not NORM_RMS
+        with pytest.raises((B.TempoError, OverflowError), match="32-bit|too large"):
+            B.tempo_norm_in(o["r"], o["w"], o["x"], kind=kind)
+        with pytest.raises((B.TempoError, OverflowError), match="32-bit|too large"):
+            B.tempo_route(s, o["x"], o["wr"], None, None, o["ids"], o["tw"], o["st"], score=kind)
