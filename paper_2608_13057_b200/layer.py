@@ -1,9 +1,9 @@
 """One mixture-of-experts layer of a served model on one rank: the norm before the block, the router, this rank's experts,
 and the norm after it with the block's gate, the residual sum and the next block's norm.
 
-Batches of up to FEW_TOKENS tokens run in four kernels (norm, router, few-token experts, norm); larger ones take the
-four-step block between the norms (dispatch, permute, grouped FFN, combine).  Both read the same packed weights.  Marshalling
-and buffers only; every step runs in the library's kernels."""
+Batches of up to `few_tokens` (FEW_TOKENS, fewer above 16 choices per token) run in four kernels (norm, router, few-token
+experts, norm); larger ones take the four-step block between the norms (dispatch, permute, grouped FFN, combine).  Both read
+the same packed weights.  Marshalling and buffers only; every step runs in the library's kernels."""
 from __future__ import annotations
 
 import torch
@@ -14,6 +14,7 @@ from . import binding as B
 # rank, top-8 of 128: 56 us against 76 of the four-step block at 64 tokens, 27 against 46 at 8, 14 against 29 at 1 (either way
 # every chosen expert's weights are read once; the block pads each instance to 128 rows and runs four kernels).
 FEW_TOKENS = 64
+FEW_PAIRS = 1024            # and at most so many (token, expert) pairs: fewer tokens above 16 choices each
 
 
 class MoELayer:
@@ -43,9 +44,10 @@ class MoELayer:
         self.topk_ids = torch.empty(max_tokens, k, dtype=torch.int32, device=dev)
         self.topk_w = torch.empty(max_tokens, k, dtype=torch.float32, device=dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
-        few = B.make_shape(min(max_tokens, FEW_TOKENS), k, E, G_max, self.R, d, f, 128)
+        self.few_tokens = min(FEW_TOKENS, FEW_PAIRS // max(k, 1))
+        few = B.make_shape(min(max_tokens, self.few_tokens), k, E, G_max, self.R, d, f, 128)
         self.workspace = torch.zeros(B.tempo_few_workspace_bytes(few), dtype=torch.uint8, device=dev)
-        self.block = B.RankBuffers(max_tokens, k, E, G_max, self.R, d, f, device=dev) if max_tokens > FEW_TOKENS else None
+        self.block = B.RankBuffers(max_tokens, k, E, G_max, self.R, d, f, device=dev) if max_tokens > self.few_tokens else None
         if self.block is not None:                       # the block reads this layer's tables and tensors
             self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
@@ -62,7 +64,7 @@ class MoELayer:
         B.tempo_norm_in(r, self.norm_w, x, kind=self.kind, eps=self.eps)
         B.tempo_route(shape, x, self.w_router, self.bias, None, ids, w, self.status, score=self.score,
                       renormalise=self.renormalise, scale=self.scale)
-        if T <= FEW_TOKENS:
+        if T <= self.few_tokens:
             B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
             self.block.n_valid.fill_(T)

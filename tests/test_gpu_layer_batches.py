@@ -1,0 +1,68 @@
+"""layer.MoELayer at the sizes between its two paths: more than 16 choices per token, batches smaller than the buffers.
+Tolerances as in test_gpu_layer."""
+import pytest
+import torch
+
+from tests.test_gpu_layer import _fp8
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2608_13057_b200 import binding
+    return binding
+
+
+class Case:
+    """A seeded layer of G local experts and its definition in 64 bits."""
+
+    def __init__(self, B, max_tokens, k, E, G, d=256, f=256, **kw):
+        from paper_2608_13057_b200.layer import MoELayer
+        g = torch.Generator().manual_seed(k * 100 + E)
+        self.B, self.k, self.G, self.d, self.f, self.kw = B, k, G, d, f, kw
+        w13, s13, self.w13 = _fp8(torch.randn(G, 2 * f, d, generator=g) * 0.05)
+        w2, s2, self.w2 = _fp8(torch.randn(G, d, f, generator=g) * 0.05)
+        shape = B.make_shape(1, k, E, G, 1, d, f, 128)
+        packed = torch.empty(B.tempo_packed_weight_bytes(shape), dtype=torch.uint8, device="cuda")
+        B.tempo_pack_weights(shape, w13.cuda(), s13.cuda(), w2.cuda(), s2.cuda(), packed, torch.zeros(1, dtype=torch.int32, device="cuda"))
+        rmap = torch.full((E, 1), -1, dtype=torch.int32)
+        rmap[:G, 0] = torch.arange(G, dtype=torch.int32)
+        self.w_router = (torch.randn(E, d, generator=g) * 0.2).bfloat16()
+        self.norm_w = (1 + 0.1 * torch.randn(d, generator=g)).bfloat16()
+        self.layer = MoELayer(max_tokens, k, G, f, self.w_router.cuda(), rmap.cuda(), packed, self.norm_w.cuda(), **kw)
+
+    def definition(self, r):
+        r = r.double()
+        x = (r / torch.sqrt((r * r).mean(1, keepdim=True) + 1e-6) * self.norm_w.double()).float().bfloat16().double()
+        w, ids = torch.topk(torch.softmax(x @ self.w_router.double().t(), 1), self.k, dim=1)
+        w = w / w.sum(1, keepdim=True)
+        y = torch.zeros_like(x)
+        for e in range(self.G):
+            t, j = torch.nonzero(ids == e, as_tuple=True)
+            if t.numel():
+                gate, up = (x[t] @ self.w13[e].t()).chunk(2, 1)
+                y.index_add_(0, t, (gate * torch.sigmoid(gate) * up) @ self.w2[e].t() * w[t, j][:, None])
+        return y, ids
+
+    def check(self, T, few, seed=0):
+        r = torch.randn(T, self.d, generator=torch.Generator().manual_seed(seed * 1000 + T))
+        out = torch.empty(T, self.d, device="cuda")
+        self.layer.forward(r.cuda(), out)
+        torch.cuda.synchronize()
+        assert int(self.layer.status.item()) == 0
+        ref, ids = self.definition(r)
+        upd = out.double().cpu() - r.double()
+        err = float((upd - ref).norm() / ref.norm())
+        assert err < (5e-3 if few else 6e-2), (T, err)
+        return ids
+
+
+@pytest.mark.parametrize("k,max_tokens,few", [(17, 64, 60), (20, 64, 51), (32, 40, 32), (32, 300, 32), (16, 64, 64)])
+def test_more_than_sixteen_choices(B, k, max_tokens, few):
+    """The few-token kernel takes 1024 (token, expert) pairs: fewer than 64 tokens above 16 choices each."""
+    c = Case(B, max_tokens, k, 40, 24)
+    for T in sorted({1, few - 1, few, min(few + 1, max_tokens), max_tokens}):
+        c.check(T, T <= few)

@@ -1,0 +1,41 @@
+"""layer.MoELayer on the host: which calls a batch makes and with which shapes.  The library's calls are recorded, not made."""
+import pytest
+import torch
+
+
+@pytest.fixture
+def L(monkeypatch):
+    from paper_2608_13057_b200 import build
+    build.build()
+    from paper_2608_13057_b200 import binding, layer
+    calls = []
+    for name in ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16", "tempo_count_dispatch",
+                 "tempo_permute_pad", "tempo_permute_pad_bf16", "tempo_grouped_ffn", "tempo_grouped_ffn_bf16",
+                 "tempo_unpermute_combine"):
+        monkeypatch.setattr(binding, name, lambda *a, name=name, **kw: calls.append((name, a, kw)))
+    layer.calls = calls
+    return layer
+
+
+def make(L, max_tokens, k, **kw):
+    E, d, f = 40, 128, 128
+    w = torch.ones(d, dtype=torch.bfloat16)
+    return L.MoELayer(max_tokens, k, 3, f, torch.zeros(E, d, dtype=torch.bfloat16), torch.full((E, 1), -1, dtype=torch.int32),
+                      torch.zeros(1, dtype=torch.uint8), w, post_w=w, next_w=w, **kw)
+
+
+def forward(L, layer, T, *a, **kw):
+    L.calls.clear()
+    r = torch.zeros(T, 128)
+    layer.forward(r, r, *a, **kw)
+    return {name: (a, kw) for name, a, kw in L.calls}
+
+
+@pytest.mark.parametrize("k,few", [(1, 64), (16, 64), (17, 60), (20, 51), (32, 32)])
+def test_the_few_token_kernel_gets_the_batches_that_it_takes(L, k, few):
+    for max_tokens in (1, few, few + 1, 64, 200):
+        layer = make(L, max_tokens, k)
+        for T in {1, few - 1, few, few + 1, 64, 200}:
+            if T <= max_tokens:
+                got = forward(L, layer, T)
+                assert ("tempo_few_ffn" in got) == (T <= few) and ("tempo_grouped_ffn" in got) == (T > few)
