@@ -379,9 +379,16 @@ class RankBuffers:
         torch.cuda.synchronize()
         return self.packed
 
-    def run_block(self, packed=None):
-        """One pass of the whole hot path: the four C-ABI steps, enqueued back to back."""
-        s = self.shape
+    def shape_for(self, T):
+        """The shape of a batch of T <= self.T rows at the front of these buffers."""
+        if not 0 < T <= self.T:
+            raise TempoError(f"a batch of {T} rows does not fit buffers of {self.T}")
+        args = (T, self.k, self.E, self.G_max, self.R_max, self.d, self.f)
+        return make_shape(*args, min(self.M_cap, tempo_m_cap_bound(make_shape(*args, 128))))
+
+    def run_block(self, packed=None, T=None):
+        """One pass of the whole hot path: the four C-ABI steps, enqueued back to back.  T: the first T rows only."""
+        s = self.shape if T is None else self.shape_for(T)
         packed = self.packed if packed is None else packed
         tempo_count_dispatch(s, self.topk_ids, self.n_valid, self.replica_map, self.quota, self.cum_counts,
                              self.counts, self.inst_count, self.inst_off, self.pair_row, self.row_pair,

@@ -51,7 +51,7 @@ class MoELayer:
         if self.block is not None:                       # the block reads this layer's tables and tensors
             self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
-            self.block.out, self.block.status = self.y, self.status
+            self.block.out, self.block.status, self.block.n_valid = self.y, self.status, None
 
     def forward(self, r, r_out, x_next=None):
         """r_out = the residual stream after the block; x_next = its norm for the next block (with next_w).  r, r_out [T, d]
@@ -67,8 +67,7 @@ class MoELayer:
         if T <= self.few_tokens:
             B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
-            self.block.n_valid.fill_(T)
-            self.block.run_block()
+            self.block.run_block(T=T)
         B.tempo_norm_out(y, r, r_out, post_w=self.post_w, gate=self.gate, next_w=self.next_w if x_next is not None else None,
                          x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale, y_scale=self.y_scale)
         return r_out

@@ -66,3 +66,12 @@ def test_more_than_sixteen_choices(B, k, max_tokens, few):
     c = Case(B, max_tokens, k, 40, 24)
     for T in sorted({1, few - 1, few, min(few + 1, max_tokens), max_tokens}):
         c.check(T, T <= few)
+
+
+def test_batches_smaller_than_the_buffers(B):
+    """Above the few-token limit a batch of T rows runs as T rows: what lies behind them is not written."""
+    c = Case(B, 1200, 3, 12, 7)
+    for T in (1200, 65, 300, 1199, 70, 66):
+        c.layer.y.fill_(float("nan"))
+        c.check(T, False)
+        assert torch.isnan(c.layer.y[T:]).all() and not torch.isnan(c.layer.y[:T]).any()

@@ -39,3 +39,17 @@ def test_the_few_token_kernel_gets_the_batches_that_it_takes(L, k, few):
             if T <= max_tokens:
                 got = forward(L, layer, T)
                 assert ("tempo_few_ffn" in got) == (T <= few) and ("tempo_grouped_ffn" in got) == (T > few)
+
+
+def test_the_block_runs_at_the_size_of_the_batch(L):
+    layer = make(L, 1000, 4)
+    for T in (65, 1000, 300):
+        got = forward(L, layer, T)
+        for name in ("tempo_count_dispatch", "tempo_permute_pad", "tempo_grouped_ffn", "tempo_unpermute_combine"):
+            s = got[name][0][0]
+            assert s.T == T and s.M_cap == -(-4 * T // 128) * 128 + 3 * 128 <= layer.block.M_cap
+        assert got["tempo_count_dispatch"][0][2] is None and got["tempo_unpermute_combine"][0][4] is None   # every row is live
+    with pytest.raises(Exception, match="1001"):
+        forward(L, layer, 1001)
+    with pytest.raises(Exception, match="0 rows"):
+        layer.block.shape_for(0)
