@@ -25,11 +25,14 @@ class MoELayer:
     replica_map  i32 [E, R]; quota i32 [E, R] or None (uniform over an expert's replicas; the few-token path uses the first)
     packed       the blob of tempo_pack_weights (fp8)
     norm_w, post_w, next_w   weights [d] of the norm before the block, after it (None: not normed) and of the next block
+    count        every batch's pairs per expert are written to `counts` (i32 [E]) and added to `cum_counts` (u32 counters in
+                 an i32 tensor, mod 2^32), which the dispatch solver works from.  The block counts as it dispatches; a
+                 few-token batch takes one more kernel for it, the block's first step (6 us).  Without it both are None.
     """
 
     def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
                  quota=None, gate=None, kind=B.NORM_RMS, eps=1e-6, score=B.ROUTE_SOFTMAX, renormalise=True, scale=1.0,
-                 r_scale=1.0, y_scale=1.0):
+                 r_scale=1.0, y_scale=1.0, count=False):
         E, d = w_router.shape
         dev = w_router.device
         self.k, self.E, self.G_max, self.R, self.d, self.f = k, E, G_max, replica_map.shape[1], d, f
@@ -52,6 +55,14 @@ class MoELayer:
             self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
             self.block.out, self.block.status, self.block.n_valid = self.y, self.status, None
+        self.counts = self.cum_counts = None
+        if count:
+            i32 = dict(dtype=torch.int32, device=dev)
+            self.counts, self.cum_counts = torch.zeros(E, **i32), torch.zeros(E, **i32)
+            if self.block is not None:
+                self.block.counts, self.block.cum_counts = self.counts, self.cum_counts
+            cap = B.tempo_m_cap_bound(few)               # the dispatch of a few-token batch, of which only the counts are used
+            self.few_dispatch = [torch.empty(n, **i32) for n in (G_max, G_max + 1, few.T * k, cap, cap // 128, 1)]
 
     def forward(self, r, r_out, x_next=None):
         """r_out = the residual stream after the block; x_next = its norm for the next block (with next_w).  r, r_out [T, d]
@@ -65,6 +76,10 @@ class MoELayer:
         B.tempo_route(shape, x, self.w_router, self.bias, None, ids, w, self.status, score=self.score,
                       renormalise=self.renormalise, scale=self.scale)
         if T <= self.few_tokens:
+            if self.counts is not None:
+                shape.M_cap = B.tempo_m_cap_bound(shape)
+                B.tempo_count_dispatch(shape, ids, None, self.replica_map, self.quota, self.cum_counts, self.counts,
+                                       *self.few_dispatch, self.status)
             B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
             self.block.run_block(T=T)

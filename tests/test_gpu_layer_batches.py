@@ -75,3 +75,16 @@ def test_batches_smaller_than_the_buffers(B):
         c.layer.y.fill_(float("nan"))
         c.check(T, False)
         assert torch.isnan(c.layer.y[T:]).all() and not torch.isnan(c.layer.y[:T]).any()
+
+
+@pytest.mark.parametrize("max_tokens", [40, 300])
+def test_counts_of_every_batch(B, max_tokens):
+    c = Case(B, max_tokens, 3, 12, 7, count=True)
+    total = torch.zeros(12, dtype=torch.int64)
+    for i, T in enumerate((1, 40, 7, 64, 65, 300, 2)):
+        if T > max_tokens:
+            continue
+        ids = c.check(T, T <= 64, seed=i)
+        n = torch.bincount(ids.reshape(-1), minlength=12)
+        total += n
+        assert torch.equal(c.layer.counts.cpu().long(), n) and torch.equal(c.layer.cum_counts.cpu().long(), total)

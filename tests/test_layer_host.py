@@ -53,3 +53,17 @@ def test_the_block_runs_at_the_size_of_the_batch(L):
         forward(L, layer, 1001)
     with pytest.raises(Exception, match="0 rows"):
         layer.block.shape_for(0)
+
+
+@pytest.mark.parametrize("max_tokens", [20, 200])
+def test_counts_come_from_every_batch(L, max_tokens):
+    layer = make(L, max_tokens, 4, count=True)
+    for T in (1, 20, 65, 200):
+        if T <= max_tokens:
+            a = forward(L, layer, T)["tempo_count_dispatch"][0]
+            assert a[0].T == T and a[0].M_cap == -(-4 * T // 128) * 128 + 3 * 128
+            assert a[5] is layer.cum_counts and a[6] is layer.counts and a[-2].numel() == 1
+            assert a[9].numel() >= 4 * T and a[10].numel() >= a[0].M_cap and a[11].numel() >= a[0].M_cap // 128
+            assert a[7].numel() == 3 and a[8].numel() == 4
+    layer = make(L, max_tokens, 4)
+    assert layer.counts is None and layer.cum_counts is None and "tempo_count_dispatch" not in forward(L, layer, 20)
