@@ -24,7 +24,8 @@ class MoELayer:
     w_router     bf16 [E, d]; bias f32 [E] or None; score B.ROUTE_SOFTMAX or B.ROUTE_SIGMOID
     replica_map  i32 [E, R]; quota i32 [E, R] or None (uniform over an expert's replicas; the few-token path uses the first)
     packed       the blob of tempo_pack_weights (fp8)
-    norm_w, post_w, next_w   weights [d] of the norm before the block, after it (None: not normed) and of the next block
+    norm_w, post_w, next_w   weights [d] of the norm before the block, after it (None: not normed) and of the next block;
+                 norm_b, post_b, next_b their biases or None; kind B.NORM_RMS or B.NORM_LAYER
     count        every batch's pairs per expert are written to `counts` (i32 [E]) and added to `cum_counts` (u32 counters in
                  an i32 tensor, mod 2^32), which the dispatch solver works from.  The block counts as it dispatches; a
                  few-token batch takes one more kernel for it, the block's first step (6 us).  Without it both are None.
@@ -32,13 +33,14 @@ class MoELayer:
 
     def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
                  quota=None, gate=None, kind=B.NORM_RMS, eps=1e-6, score=B.ROUTE_SOFTMAX, renormalise=True, scale=1.0,
-                 r_scale=1.0, y_scale=1.0, count=False):
+                 r_scale=1.0, y_scale=1.0, count=False, norm_b=None, post_b=None, next_b=None):
         E, d = w_router.shape
         dev = w_router.device
         self.k, self.E, self.G_max, self.R, self.d, self.f = k, E, G_max, replica_map.shape[1], d, f
         self.w_router, self.bias, self.replica_map, self.packed = w_router, bias, replica_map, packed
         self.quota = torch.zeros_like(replica_map) if quota is None else quota
         self.norm_w, self.post_w, self.next_w, self.gate = norm_w, post_w, next_w, gate
+        self.norm_b, self.post_b, self.next_b = norm_b, post_b, next_b
         self.kind, self.eps, self.r_scale, self.y_scale = kind, eps, r_scale, y_scale
         self.score, self.renormalise, self.scale = score, renormalise, scale
         bf16 = dict(dtype=torch.bfloat16, device=dev)
@@ -72,7 +74,7 @@ class MoELayer:
             raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.x.shape[0]}")
         x, y, ids, w = self.x[:T], self.y[:T], self.topk_ids[:T], self.topk_w[:T]
         shape = B.make_shape(T, self.k, self.E, self.G_max, self.R, self.d, self.f, 128)
-        B.tempo_norm_in(r, self.norm_w, x, kind=self.kind, eps=self.eps)
+        B.tempo_norm_in(r, self.norm_w, x, b=self.norm_b, kind=self.kind, eps=self.eps)
         B.tempo_route(shape, x, self.w_router, self.bias, None, ids, w, self.status, score=self.score,
                       renormalise=self.renormalise, scale=self.scale)
         if T <= self.few_tokens:
@@ -83,6 +85,7 @@ class MoELayer:
             B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
             self.block.run_block(T=T)
-        B.tempo_norm_out(y, r, r_out, post_w=self.post_w, gate=self.gate, next_w=self.next_w if x_next is not None else None,
+        next_w, next_b = (self.next_w, self.next_b) if x_next is not None else (None, None)
+        B.tempo_norm_out(y, r, r_out, post_w=self.post_w, post_b=self.post_b, gate=self.gate, next_w=next_w, next_b=next_b,
                          x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale, y_scale=self.y_scale)
         return r_out

@@ -32,11 +32,19 @@ class Case:
         rmap[:G, 0] = torch.arange(G, dtype=torch.int32)
         self.w_router = (torch.randn(E, d, generator=g) * 0.2).bfloat16()
         self.norm_w = (1 + 0.1 * torch.randn(d, generator=g)).bfloat16()
-        self.layer = MoELayer(max_tokens, k, G, f, self.w_router.cuda(), rmap.cuda(), packed, self.norm_w.cuda(), **kw)
+        self.layer = MoELayer(max_tokens, k, G, f, self.w_router.cuda(), rmap.cuda(), packed, self.norm_w.cuda(),
+                              **{n: v.cuda() if torch.is_tensor(v) else v for n, v in kw.items()})
+
+    def norm(self, v, w, b):
+        if w is None:
+            return v
+        if self.kw.get("kind"):
+            v = v - v.mean(1, keepdim=True)
+        v = v / torch.sqrt((v * v).mean(1, keepdim=True) + 1e-6) * w.double()
+        return v if b is None else v + b.double()
 
     def definition(self, r):
-        r = r.double()
-        x = (r / torch.sqrt((r * r).mean(1, keepdim=True) + 1e-6) * self.norm_w.double()).float().bfloat16().double()
+        x = self.norm(r.double(), self.norm_w, self.kw.get("norm_b")).float().bfloat16().double()
         w, ids = torch.topk(torch.softmax(x @ self.w_router.double().t(), 1), self.k, dim=1)
         w = w / w.sum(1, keepdim=True)
         y = torch.zeros_like(x)
@@ -45,18 +53,21 @@ class Case:
             if t.numel():
                 gate, up = (x[t] @ self.w13[e].t()).chunk(2, 1)
                 y.index_add_(0, t, (gate * torch.sigmoid(gate) * up) @ self.w2[e].t() * w[t, j][:, None])
-        return y, ids
+        return self.norm(y, self.kw.get("post_w"), self.kw.get("post_b")), ids
 
     def check(self, T, few, seed=0):
         r = torch.randn(T, self.d, generator=torch.Generator().manual_seed(seed * 1000 + T))
-        out = torch.empty(T, self.d, device="cuda")
-        self.layer.forward(r.cuda(), out)
+        out, x = torch.empty(T, self.d, device="cuda"), torch.empty(T, self.d, dtype=torch.bfloat16, device="cuda")
+        self.layer.forward(r.cuda(), out, x if "next_w" in self.kw else None)
         torch.cuda.synchronize()
         assert int(self.layer.status.item()) == 0
         ref, ids = self.definition(r)
         upd = out.double().cpu() - r.double()
         err = float((upd - ref).norm() / ref.norm())
         assert err < (5e-3 if few else 6e-2), (T, err)
+        if "next_w" in self.kw:
+            ref = self.norm(r.double() + ref, self.kw["next_w"], self.kw.get("next_b"))
+            assert float((x.double().cpu() - ref).norm() / ref.norm()) < (5e-3 if few else 6e-2)
         return ids
 
 
@@ -88,3 +99,12 @@ def test_counts_of_every_batch(B, max_tokens):
         n = torch.bincount(ids.reshape(-1), minlength=12)
         total += n
         assert torch.equal(c.layer.counts.cpu().long(), n) and torch.equal(c.layer.cum_counts.cpu().long(), total)
+
+
+def test_layer_norms_with_biases(B):
+    g = torch.Generator().manual_seed(4)
+    w = lambda: (1 + 0.1 * torch.randn(256, generator=g)).bfloat16()
+    b = lambda: (0.3 * torch.randn(256, generator=g)).bfloat16()
+    c = Case(B, 200, 3, 12, 7, kind=B.NORM_LAYER, norm_b=b(), post_w=w(), post_b=b(), next_w=w(), next_b=b())
+    for T in (1, 33, 200):
+        c.check(T, T <= 64)

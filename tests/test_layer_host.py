@@ -67,3 +67,15 @@ def test_counts_come_from_every_batch(L, max_tokens):
             assert a[7].numel() == 3 and a[8].numel() == 4
     layer = make(L, max_tokens, 4)
     assert layer.counts is None and layer.cum_counts is None and "tempo_count_dispatch" not in forward(L, layer, 20)
+
+
+def test_biases_reach_the_norms(L):
+    b = [torch.zeros(128, dtype=torch.bfloat16) for _ in range(3)]
+    layer = make(L, 100, 2, norm_b=b[0], post_b=b[1], next_b=b[2])
+    for T in (3, 100):
+        got = forward(L, layer, T, torch.zeros(T, 128, dtype=torch.bfloat16))
+        assert got["tempo_norm_in"][1]["b"] is b[0]
+        kw = got["tempo_norm_out"][1]
+        assert kw["post_b"] is b[1] and kw["next_b"] is b[2] and kw["next_w"] is layer.next_w
+        kw = forward(L, layer, T)["tempo_norm_out"][1]                  # without the next block's input
+        assert kw["post_b"] is b[1] and kw["next_b"] is None and kw["next_w"] is None
