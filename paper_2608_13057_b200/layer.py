@@ -56,7 +56,7 @@ class MoELayer:
         if self.block is not None:                       # the block reads this layer's tables and tensors
             self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
-            self.block.out, self.block.status, self.block.n_valid = self.y, self.status, None
+            self.block.out, self.block.status = self.y, self.status
         self.counts = self.cum_counts = None
         if count:
             i32 = dict(dtype=torch.int32, device=dev)
@@ -66,26 +66,30 @@ class MoELayer:
             cap = B.tempo_m_cap_bound(few)               # the dispatch of a few-token batch, of which only the counts are used
             self.few_dispatch = [torch.empty(n, **i32) for n in (G_max, G_max + 1, few.T * k, cap, cap // 128, 1)]
 
-    def forward(self, r, r_out, x_next=None):
+    def forward(self, r, r_out, x_next=None, gate=None, n_valid=None):
         """r_out = the residual stream after the block; x_next = its norm for the next block (with next_w).  r, r_out [T, d]
-        bf16 or f32 (r_out may be r), x_next bf16.  Enqueues kernels only: the call can be captured in a CUDA graph."""
+        bf16 or f32 (r_out may be r), x_next bf16.  gate: of this batch, e.g. [T, 1] (None: the layer's).  n_valid i32 [1]: rows
+        behind it are padding and stay as they are in r_out and x_next (None: every row is live).  Enqueues kernels only: the
+        call can be captured in a CUDA graph."""
         T = r.shape[0]
         if T > self.x.shape[0]:
             raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.x.shape[0]}")
         x, y, ids, w = self.x[:T], self.y[:T], self.topk_ids[:T], self.topk_w[:T]
         shape = B.make_shape(T, self.k, self.E, self.G_max, self.R, self.d, self.f, 128)
-        B.tempo_norm_in(r, self.norm_w, x, b=self.norm_b, kind=self.kind, eps=self.eps)
-        B.tempo_route(shape, x, self.w_router, self.bias, None, ids, w, self.status, score=self.score,
+        B.tempo_norm_in(r, self.norm_w, x, b=self.norm_b, kind=self.kind, eps=self.eps, n_valid=n_valid)
+        B.tempo_route(shape, x, self.w_router, self.bias, n_valid, ids, w, self.status, score=self.score,
                       renormalise=self.renormalise, scale=self.scale)
         if T <= self.few_tokens:
             if self.counts is not None:
                 shape.M_cap = B.tempo_m_cap_bound(shape)
-                B.tempo_count_dispatch(shape, ids, None, self.replica_map, self.quota, self.cum_counts, self.counts,
+                B.tempo_count_dispatch(shape, ids, n_valid, self.replica_map, self.quota, self.cum_counts, self.counts,
                                        *self.few_dispatch, self.status)
-            B.tempo_few_ffn(shape, x, ids, w, None, self.replica_map, self.packed, y, self.status, self.workspace)
+            B.tempo_few_ffn(shape, x, ids, w, n_valid, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
+            self.block.n_valid = n_valid
             self.block.run_block(T=T)
         next_w, next_b = (self.next_w, self.next_b) if x_next is not None else (None, None)
-        B.tempo_norm_out(y, r, r_out, post_w=self.post_w, post_b=self.post_b, gate=self.gate, next_w=next_w, next_b=next_b,
-                         x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale, y_scale=self.y_scale)
+        B.tempo_norm_out(y, r, r_out, post_w=self.post_w, post_b=self.post_b, gate=self.gate if gate is None else gate,
+                         next_w=next_w, next_b=next_b, x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale,
+                         y_scale=self.y_scale, n_valid=n_valid)
         return r_out

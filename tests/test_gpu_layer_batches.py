@@ -108,3 +108,28 @@ def test_layer_norms_with_biases(B):
     c = Case(B, 200, 3, 12, 7, kind=B.NORM_LAYER, norm_b=b(), post_w=w(), post_b=b(), next_w=w(), next_b=b())
     for T in (1, 33, 200):
         c.check(T, T <= 64)
+
+
+@pytest.mark.parametrize("T,n", [(40, 23), (64, 0), (300, 65), (300, 64), (300, 299), (300, 0)])
+def test_padding_rows_and_a_gate_per_token(B, T, n):
+    """Live rows as the definition has them, the others neither read nor written."""
+    w = torch.ones(256).bfloat16()
+    c = Case(B, 300, 3, 12, 7, post_w=w, next_w=w, count=True)
+    g = torch.Generator().manual_seed(T + n)
+    r, gate = torch.randn(T, 256, generator=g), torch.rand(T, 1, generator=g) + 0.5
+    ref, ids = c.definition(r)
+    rc = r.cuda()
+    rc[n:] = float("nan")
+    out, x = torch.full((T, 256), -7.0, device="cuda"), torch.full((T, 256), -7.0, dtype=torch.bfloat16, device="cuda")
+    c.layer.forward(rc, out, x, gate=gate.cuda(), n_valid=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(c.layer.status.item()) == 0 and (out[n:] == -7).all() and (x[n:] == -7).all()
+    assert torch.equal(c.layer.counts.cpu().long(), torch.bincount(ids[:n].reshape(-1), minlength=12))
+    if n == 0:
+        return
+    tol = 5e-3 if T <= 64 else 6e-2
+    ref = gate.double() * ref
+    upd = out.double().cpu() - r.double()
+    assert float((upd[:n] - ref[:n]).norm() / ref[:n].norm()) < tol
+    ref = c.norm(r.double() + ref, w, None)
+    assert float((x.double().cpu()[:n] - ref[:n]).norm() / ref[:n].norm()) < tol

@@ -79,3 +79,18 @@ def test_biases_reach_the_norms(L):
         assert kw["post_b"] is b[1] and kw["next_b"] is b[2] and kw["next_w"] is layer.next_w
         kw = forward(L, layer, T)["tempo_norm_out"][1]                  # without the next block's input
         assert kw["post_b"] is b[1] and kw["next_b"] is None and kw["next_w"] is None
+
+
+def test_live_rows_and_a_gate_of_the_batch(L):
+    layer = make(L, 100, 2, gate=torch.ones(128), count=True)
+    nv, gate = torch.zeros(1, dtype=torch.int32), torch.ones(100, 1)
+    for T in (3, 100):
+        got = forward(L, layer, T, None, gate[:T], nv)
+        assert got["tempo_norm_in"][1]["n_valid"] is nv and got["tempo_norm_out"][1]["n_valid"] is nv
+        assert got["tempo_route"][0][4] is nv and got["tempo_count_dispatch"][0][2] is nv
+        assert (got["tempo_few_ffn"][0][4] if T == 3 else got["tempo_unpermute_combine"][0][4]) is nv
+        assert got["tempo_norm_out"][1]["gate"].shape == (T, 1)
+        got = forward(L, layer, T)                                     # nothing stays from the call before
+        assert got["tempo_norm_in"][1]["n_valid"] is None and got["tempo_route"][0][4] is None
+        assert got["tempo_count_dispatch"][0][2] is None and got["tempo_norm_out"][1]["gate"] is layer.gate
+        assert (got["tempo_few_ffn"][0][4] if T == 3 else got["tempo_unpermute_combine"][0][4]) is None
