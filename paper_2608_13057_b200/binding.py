@@ -440,9 +440,9 @@ class RankBuffers:
         self.a_bf16 = torch.zeros(self.M_cap, self.d, **dev_kw)
         self.h_bf16 = torch.zeros(self.M_cap, self.f, **dev_kw)
 
-    def run_block_bf16(self, packed=None):
-        """One pass of the block with the bf16 steps 2 and 3."""
-        s = self.shape
+    def run_block_bf16(self, packed=None, T=None):
+        """One pass of the block with the bf16 steps 2 and 3.  T: the first T rows only."""
+        s = self.shape if T is None else self.shape_for(T)
         packed = self.packed_bf16 if packed is None else packed
         tempo_count_dispatch(s, self.topk_ids, self.n_valid, self.replica_map, self.quota, self.cum_counts,
                              self.counts, self.inst_count, self.inst_off, self.pair_row, self.row_pair,

@@ -23,7 +23,7 @@ class MoELayer:
     max_tokens   largest batch (rows of the buffers)
     w_router     bf16 [E, d]; bias f32 [E] or None; score B.ROUTE_SOFTMAX or B.ROUTE_SIGMOID
     replica_map  i32 [E, R]; quota i32 [E, R] or None (uniform over an expert's replicas; the few-token path uses the first)
-    packed       the blob of tempo_pack_weights (fp8)
+    packed       the blob of tempo_pack_weights, or of tempo_pack_weights_bf16 with bf16=True
     norm_w, post_w, next_w   weights [d] of the norm before the block, after it (None: not normed) and of the next block;
                  norm_b, post_b, next_b their biases or None; kind B.NORM_RMS or B.NORM_LAYER
     count        every batch's pairs per expert are written to `counts` (i32 [E]) and added to `cum_counts` (u32 counters in
@@ -33,7 +33,7 @@ class MoELayer:
 
     def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
                  quota=None, gate=None, kind=B.NORM_RMS, eps=1e-6, score=B.ROUTE_SOFTMAX, renormalise=True, scale=1.0,
-                 r_scale=1.0, y_scale=1.0, count=False, norm_b=None, post_b=None, next_b=None):
+                 r_scale=1.0, y_scale=1.0, count=False, norm_b=None, post_b=None, next_b=None, bf16=False):
         E, d = w_router.shape
         dev = w_router.device
         self.k, self.E, self.G_max, self.R, self.d, self.f = k, E, G_max, replica_map.shape[1], d, f
@@ -43,9 +43,9 @@ class MoELayer:
         self.norm_b, self.post_b, self.next_b = norm_b, post_b, next_b
         self.kind, self.eps, self.r_scale, self.y_scale = kind, eps, r_scale, y_scale
         self.score, self.renormalise, self.scale = score, renormalise, scale
-        bf16 = dict(dtype=torch.bfloat16, device=dev)
-        self.x = torch.empty(max_tokens, d, **bf16)
-        self.y = torch.empty(max_tokens, d, **bf16)
+        self.bf16 = bf16
+        self.x = torch.empty(max_tokens, d, dtype=torch.bfloat16, device=dev)
+        self.y = torch.empty_like(self.x)
         self.topk_ids = torch.empty(max_tokens, k, dtype=torch.int32, device=dev)
         self.topk_w = torch.empty(max_tokens, k, dtype=torch.float32, device=dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
@@ -54,7 +54,9 @@ class MoELayer:
         self.workspace = torch.zeros(B.tempo_few_workspace_bytes(few), dtype=torch.uint8, device=dev)
         self.block = B.RankBuffers(max_tokens, k, E, G_max, self.R, d, f, device=dev) if max_tokens > self.few_tokens else None
         if self.block is not None:                       # the block reads this layer's tables and tensors
-            self.block.replica_map, self.block.quota, self.block.packed = self.replica_map, self.quota, packed
+            self.block.replica_map, self.block.quota = self.replica_map, self.quota
+            if bf16:
+                self.block.alloc_bf16()
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
             self.block.out, self.block.status = self.y, self.status
         self.counts = self.cum_counts = None
@@ -84,10 +86,11 @@ class MoELayer:
                 shape.M_cap = B.tempo_m_cap_bound(shape)
                 B.tempo_count_dispatch(shape, ids, n_valid, self.replica_map, self.quota, self.cum_counts, self.counts,
                                        *self.few_dispatch, self.status)
-            B.tempo_few_ffn(shape, x, ids, w, n_valid, self.replica_map, self.packed, y, self.status, self.workspace)
+            ffn = B.tempo_few_ffn_bf16 if self.bf16 else B.tempo_few_ffn
+            ffn(shape, x, ids, w, n_valid, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
             self.block.n_valid = n_valid
-            self.block.run_block(T=T)
+            (self.block.run_block_bf16 if self.bf16 else self.block.run_block)(self.packed, T=T)
         next_w, next_b = (self.next_w, self.next_b) if x_next is not None else (None, None)
         B.tempo_norm_out(y, r, r_out, post_w=self.post_w, post_b=self.post_b, gate=self.gate if gate is None else gate,
                          next_w=next_w, next_b=next_b, x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale,

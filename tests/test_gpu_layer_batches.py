@@ -23,11 +23,16 @@ class Case:
         from paper_2608_13057_b200.layer import MoELayer
         g = torch.Generator().manual_seed(k * 100 + E)
         self.B, self.k, self.G, self.d, self.f, self.kw = B, k, G, d, f, kw
-        w13, s13, self.w13 = _fp8(torch.randn(G, 2 * f, d, generator=g) * 0.05)
-        w2, s2, self.w2 = _fp8(torch.randn(G, d, f, generator=g) * 0.05)
+        w13, w2 = torch.randn(G, 2 * f, d, generator=g) * 0.05, torch.randn(G, d, f, generator=g) * 0.05
         shape = B.make_shape(1, k, E, G, 1, d, f, 128)
-        packed = torch.empty(B.tempo_packed_weight_bytes(shape), dtype=torch.uint8, device="cuda")
-        B.tempo_pack_weights(shape, w13.cuda(), s13.cuda(), w2.cuda(), s2.cuda(), packed, torch.zeros(1, dtype=torch.int32, device="cuda"))
+        if kw.get("bf16"):
+            self.w13, self.w2 = w13.bfloat16().double(), w2.bfloat16().double()
+            packed = torch.empty(B.tempo_packed_weight_bytes_bf16(shape), dtype=torch.uint8, device="cuda")
+            B.tempo_pack_weights_bf16(shape, w13.bfloat16().cuda(), w2.bfloat16().cuda(), packed)
+        else:
+            (q13, s13, self.w13), (q2, s2, self.w2) = _fp8(w13), _fp8(w2)
+            packed = torch.empty(B.tempo_packed_weight_bytes(shape), dtype=torch.uint8, device="cuda")
+            B.tempo_pack_weights(shape, q13.cuda(), s13.cuda(), q2.cuda(), s2.cuda(), packed, torch.zeros(1, dtype=torch.int32, device="cuda"))
         rmap = torch.full((E, 1), -1, dtype=torch.int32)
         rmap[:G, 0] = torch.arange(G, dtype=torch.int32)
         self.w_router = (torch.randn(E, d, generator=g) * 0.2).bfloat16()
@@ -133,3 +138,9 @@ def test_padding_rows_and_a_gate_per_token(B, T, n):
     assert float((upd[:n] - ref[:n]).norm() / ref[:n].norm()) < tol
     ref = c.norm(r.double() + ref, w, None)
     assert float((x.double().cpu()[:n] - ref[:n]).norm() / ref[:n].norm()) < tol
+
+
+def test_bf16_experts(B):
+    c = Case(B, 200, 3, 12, 7, bf16=True)
+    for T in (1, 64, 65, 200):
+        c.check(T, True)                                              # no 8-bit activations on either path

@@ -94,3 +94,13 @@ def test_live_rows_and_a_gate_of_the_batch(L):
         assert got["tempo_norm_in"][1]["n_valid"] is None and got["tempo_route"][0][4] is None
         assert got["tempo_count_dispatch"][0][2] is None and got["tempo_norm_out"][1]["gate"] is layer.gate
         assert (got["tempo_few_ffn"][0][4] if T == 3 else got["tempo_unpermute_combine"][0][4]) is None
+
+
+def test_bf16_experts_on_both_paths(L):
+    layer = make(L, 100, 2, bf16=True)
+    got = forward(L, layer, 3)
+    assert "tempo_few_ffn_bf16" in got and "tempo_few_ffn" not in got
+    got = forward(L, layer, 100)
+    assert "tempo_permute_pad_bf16" in got and "tempo_grouped_ffn" not in got
+    a = got["tempo_grouped_ffn_bf16"][0]
+    assert a[0].T == 100 and a[2] is layer.packed and a[1].dtype == a[5].dtype == torch.bfloat16
