@@ -3,7 +3,8 @@ Argument marshalling only: every step runs in the CUDA kernels.
 
 The functions carry the C-ABI names (see include/tempo.h).  Tensors are torch CUDA tensors used as
 device memory; kernels are enqueued on torch's current stream.  There is no CPU fallback: importing
-this module without the built library, or calling it with CPU tensors, raises.
+this module without the built library, calling it with CPU tensors, or calling one of the entries that need
+_marshal without it, raises.
 """
 from __future__ import annotations
 
@@ -13,11 +14,22 @@ from typing import Optional
 
 import torch
 
+
+class _NoMarshal:
+    """Stands in for an extension module that does not load: every call of it raises what is missing."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"{name} needs the extension module _marshal, which is missing or does not load ({self._why}): build it "
+                          "with __graft_entry__.build() (python -m paper_2608_13057_b200.build); there is no fallback path")
+
+
 try:
     from . import _marshal                      # needs torch's libraries: imported after torch
 except ImportError as e:
-    raise ImportError(f"the extension module _marshal is missing or does not load ({e}): build it with "
-                      "__graft_entry__.build() (python -m paper_2608_13057_b200.build); there is no fallback path") from e
+    _marshal = _NoMarshal(e)
 
 _LIB_PATH = os.environ.get("TEMPO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtempo.so")
 
@@ -278,9 +290,10 @@ def tempo_grouped_ffn_bf16(shape, a_bf16, packed, inst_off, m_pad, h_bf16, y_bf1
 # extension module _marshal (csrc/marshal.cpp) checks the tensors and calls the same library's C entry points.
 # Every operand is on the current device.
 
-_marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
-                            ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",
-                             "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16")))
+if not isinstance(_marshal, _NoMarshal):
+    _marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
+                                ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",
+                                 "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16")))
 
 
 def tempo_norm_in(r, w, x_out, b=None, kind=NORM_RMS, eps=1e-6, n_valid=None):
