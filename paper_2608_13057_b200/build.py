@@ -2,6 +2,8 @@
 calls, the host compiler against torch's headers) in-tree."""
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -28,16 +30,29 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _torch_dir() -> str:
+    return os.path.dirname(os.path.abspath(importlib.util.find_spec("torch").origin))
+
+
+def _marshal_stale(built_for: str) -> bool:
+    """Whether the module is missing, older than its sources or built against another torch, which its own text tells."""
+    if not os.path.exists(MARSHAL_PATH) or \
+            os.path.getmtime(MARSHAL_PATH) < max(os.path.getmtime(MARSHAL_SRC), os.path.getmtime(HEADER)):
+        return True
+    with open(MARSHAL_PATH, "rb") as f:
+        return f"(built for {built_for})".encode() not in f.read()
+
+
 def build_marshal(force: bool = False) -> str:
     """The extension links torch's libraries by name only: importing torch first loads them."""
-    if not force and os.path.exists(MARSHAL_PATH) and \
-            os.path.getmtime(MARSHAL_PATH) >= max(os.path.getmtime(MARSHAL_SRC), os.path.getmtime(HEADER)):
+    base = _torch_dir()
+    built_for = f"torch {importlib.metadata.version('torch')} in {base}"
+    if not force and not _marshal_stale(built_for):
         return MARSHAL_PATH
     import torch
-    base = os.path.dirname(os.path.abspath(torch.__file__))
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DTEMPO_BUILT_FOR="{built_for}"',
            "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"),
            "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
            "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"],

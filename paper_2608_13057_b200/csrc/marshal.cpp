@@ -300,7 +300,7 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 #define TEMPO_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TEMPO_METHOD(bind), TEMPO_METHOD(norm_in), TEMPO_METHOD(norm_out), TEMPO_METHOD(route), TEMPO_METHOD(few),
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the few-microsecond calls.", -1, methods,
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the few-microsecond calls (built for " TEMPO_BUILT_FOR ").", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
