@@ -77,6 +77,7 @@ def main():
         r = torch.randn(T, d, generator=g, device="cuda").bfloat16()
         x_next = torch.empty_like(r)
         side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())       # r is drawn there
         with torch.cuda.stream(side):
             layer.forward(r, torch.empty_like(r), x_next)
         side.synchronize()
