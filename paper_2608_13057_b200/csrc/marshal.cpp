@@ -48,8 +48,8 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
   return t;
 }
 
-// The tensors among a call's arguments are on one device, and that is the current one: the kernel goes to its current stream.
-void one_device(PyObject* const* v, Py_ssize_t n) {
+// The current stream, for operands (the tensors among a call's arguments) that are all on the current device.
+void* current_stream(PyObject* const* v, Py_ssize_t n) {
   int dev = -1;
   for (Py_ssize_t i = 0; i < n; ++i) {
     if (v[i] == Py_None || PyLong_Check(v[i]) || PyFloat_Check(v[i]) || !THPVariable_Check(v[i])) continue;
@@ -59,9 +59,9 @@ void one_device(PyObject* const* v, Py_ssize_t n) {
     if (dev >= 0 && d != dev) refuse("operands on cuda:", dev, " and cuda:", d);
     dev = d;
   }
-  if (dev < 0) return;
   const int current = c10::cuda::current_device();
-  if (dev != current) refuse("operands on cuda:", dev, ", but the current device is cuda:", current);
+  if (dev >= 0 && dev != current) refuse("operands on cuda:", dev, ", but the current device is cuda:", current);
+  return c10::cuda::getCurrentCUDAStream(current).stream();
 }
 
 // Elements that the C entry reads or writes by the sizes it is given.
@@ -142,7 +142,6 @@ bool truth(PyObject* o) {
   if (v < 0) throw Refused("");
   return v != 0;
 }
-void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 template <typename F>
 PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F f) {
@@ -163,7 +162,7 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
     tempo_norm a{};
     a.kind = integer(v[4]);
     a.eps = number(v[5]);
-    one_device(v, n);
+    void* stream = current_stream(v, n);
     stream_shape(v[0], a);
     int f32 = -1;
     void* r = rows(v[0], a.stream_f32 ? at::kFloat : at::kBFloat16, "r", a.T, a.d, a.ld_r);
@@ -171,7 +170,7 @@ PyObject* norm_in(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* x = rows(v[2], at::kBFloat16, "x_out", a.T, a.d, a.ld_x);
     const void* b = param(v[3], "b", a.d, f32);
     a.param_f32 = f32 > 0;
-    return g_norm_in(&a, r, w, b, static_cast<const int32_t*>(word(v[6], "n_valid")), x, stream());
+    return g_norm_in(&a, r, w, b, static_cast<const int32_t*>(word(v[6], "n_valid")), x, stream);
   });
 }
 
@@ -183,7 +182,7 @@ PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.eps = number(v[10]);
     a.r_scale = number(v[11]);
     a.y_scale = number(v[12]);
-    one_device(v, n);
+    void* stream = current_stream(v, n);
     stream_shape(v[1], a);
     const at::ScalarType dtype = a.stream_f32 ? at::kFloat : at::kBFloat16;
     int f32 = -1;
@@ -208,7 +207,7 @@ PyObject* norm_out(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* x = v[8] == Py_None ? nullptr : rows(v[8], at::kBFloat16, "x_out", a.T, a.d, a.ld_x);
     a.param_f32 = f32 > 0;
     return g_norm_out(&a, y, r, post_w, post_b, gate, next_w, next_b,
-                      static_cast<const int32_t*>(word(v[13], "n_valid")), r_out, x, stream());
+                      static_cast<const int32_t*>(word(v[13], "n_valid")), r_out, x, stream);
   });
 }
 
@@ -225,7 +224,7 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const int32_t score = integer(v[8]);
     const bool renormalise = truth(v[9]);
     const float scale = number(v[10]);
-    one_device(v, n);
+    void* stream = current_stream(v, n);
     void* x = addr(v[1], at::kBFloat16, "x");
     void* wr = addr(v[2], at::kBFloat16, "w_router");
     void* bias = addr(v[3], at::kFloat, "bias");
@@ -243,7 +242,7 @@ PyObject* route(PyObject*, PyObject* const* v, Py_ssize_t n) {
     }
     return g_route(s, score, renormalise, scale, x, wr,
                    static_cast<const float*>(bias), static_cast<const int32_t*>(nv), static_cast<int32_t*>(ids),
-                   static_cast<float*>(w), static_cast<uint32_t*>(status), stream());
+                   static_cast<float*>(w), static_cast<uint32_t*>(status), stream);
   });
 }
 
@@ -252,7 +251,7 @@ PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> int {
     const bool bf16 = truth(v[0]);
     const tempo_shape* s = shape_at(v[1]);
-    one_device(v, n);
+    void* stream = current_stream(v, n);
     void* x = addr(v[2], at::kBFloat16, "x");
     void* ids = addr(v[3], at::kInt, "topk_ids");
     void* w = addr(v[4], at::kFloat, "topk_w");
@@ -275,7 +274,7 @@ PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (g_packed_bytes[bf16](s, &bytes) == TEMPO_OK) holds(v[7], static_cast<int64_t>(bytes), "packed");
     return g_few[bf16](s, x, static_cast<const int32_t*>(ids), static_cast<const float*>(w),
                        static_cast<const int32_t*>(nv), static_cast<const int32_t*>(map), packed, out,
-                       static_cast<uint32_t*>(status), workspace, stream());
+                       static_cast<uint32_t*>(status), workspace, stream);
   });
 }
 
