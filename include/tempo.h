@@ -318,8 +318,9 @@ int tempo_grouped_ffn_bf16(const tempo_shape* shape, const void* a_bf16, const v
  *   token, (d, 1) per element; both 0 one number.
  *   Optional (NULL): b, post_w (y is not normed), post_b, gate (1), next_b, n_valid, and x' with next_w.
  *   Rows are d elements at pitches ld_* >= d (elements); rows t >= n_valid are neither read nor written.  r' may be r and
- *   x' may be y (same address and pitch).  Any d from 1 to 16384; rows that 16-byte vectors do not divide or
- *   align take 8-byte ones, or go through shared memory (bf16), or run with narrower loads.  Pointers need the alignment of their element (TEMPO_ERR_ALIGN).
+ *   x' may be y (same address and pitch).  Any d from 1 to 16384; rows that 16-byte vectors do not divide or align take
+ *   8-byte ones, or go through shared memory (bf16), or run with narrower loads.  Pointers need the alignment of their element
+ *   (TEMPO_ERR_ALIGN).
  */
 enum { TEMPO_NORM_RMS = 0, TEMPO_NORM_LAYER = 1 };
 typedef struct {
@@ -361,10 +362,13 @@ int tempo_route(const tempo_shape* shape, int32_t score, int32_t renormalise, fl
  *   out[t, :] = sum_s topk_w[t, s] * W2_e (silu(Wgate_e x_t) (.) (Wup_e x_t)),  e = topk_ids[t, s]
  * over the experts that replica_map puts on this rank; of several replicas the first column with a slot is used.  Each
  * chosen expert's weights are read once; no 128-row padding, no quota table.  `packed` is the blob of tempo_pack_weights
- * (tempo_pack_weights_bf16 for the _bf16 call).  Unlike steps 2 and 3, x and H are not rounded to 8 bits: both enter the
- * products as two e4m3 terms (8 significant bits; x exactly), in the _bf16 call as bf16 (x) and two bf16 terms (H).
- * A value of x or H that is not finite (the _bf16 call: an H beyond bf16's range) makes its own token's output NaN.  Rows without a local expert and rows t >= n_valid
- * are zero.  An id outside [0, E) of a live row is ignored (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token
+ * (tempo_pack_weights_bf16 for the _bf16 call).  Unlike in steps 2 and 3, x and H are not single 8-bit codes: both enter the
+ * products as two e4m3 terms under a power-of-two scale for each 128 values.  That is x itself where it lies within 2^-13 of
+ * the 128 values' largest, within 2^-22 of that largest below, and H rounded to 8 significant bits in the same way.  In the
+ * _bf16 call x enters as it is and H as two bf16 terms (16 bits).  Sums are in 32 bits, silu uses the fast exponential and
+ * division (2^-19 of its value for gates within +-8).
+ * A value of x or H that is not finite (the _bf16 call: an H beyond bf16's range) makes its own token's output NaN.  Rows
+ * without a local expert and rows t >= n_valid are zero.  An id outside [0, E) of a live row is ignored (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token
  * counts twice.  Results do not depend on timing; nothing is summed with atomics.
  *   in   x bf16 [T, d] (16-byte aligned), topk_ids i32 [T, k], topk_w f32 [T, k], n_valid or NULL,
  *        replica_map i32 [E, R_max], packed (256-byte aligned)

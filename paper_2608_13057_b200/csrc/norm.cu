@@ -1,5 +1,6 @@
-// The norms around a block.  One row of the residual stream per CTA, held in registers from the first load to the last
-// store, so every operand is read once and every result written once:
+// The norms around a block.  A row of the residual stream is held in a CTA's registers from its first load to its last store
+// (one row per CTA, or several one after the other with the next in flight), so every operand is read once and every result
+// written once:
 //   tempo_norm_in    x  = norm(r) * w + b
 //   tempo_norm_out   r' = r_scale * r + y_scale * g (.) (norm(y) * post_w + post_b),  x' = norm(r') * next_w + next_b
 // norm(v) = v / sqrt(mean(v^2) + eps), or the same of v - mean(v).  The mean and the mean square are two sums over
@@ -8,7 +9,9 @@
 // x' is taken from the 32-bit r', not from its rounding to the stream's type.
 // Bound by the bytes: 8192 x 7168 with a gate per channel reads y and r and writes r' and x', 470 MB, in 79.7 us, 90 % of a
 // copy's rate in long runs (two copies of the same bytes take 78.3 us); one row is the latency of a launch and a load, 2.4 us.
-// Rows at odd addresses are bound by instructions (49 a column and thread, 60 % of the issue slots): 4096 x 5001 in 50 us of 25.
+// Rows of bf16 at odd addresses go through shared memory on their way in and out, and that staging is what bounds them (49
+// instructions a column and thread, 60 % of the issue slots, four to six barriers a row): 4096 x 5001 in 50 us of 25.  Short rows
+// in batches are bound by what each row's CTA of one or two warps does before and behind its loads: 8192 x 512 in 7.9 us of 5.1.
 // Which kernel a shape gets, and the figures behind that, stand at the launcher below.
 #include "tempo_kernels.cuh"
 
@@ -771,7 +774,8 @@ bool norm_shifts(const NormParams& p, int vec) { return !p.stream_f32 && vec <= 
 //   More: the kernel with several rows per CTA where the parameter folds (4096 rows of 4096 23.3 us against 28.9, before a block
 //   12.7 against 14.6), or a CTA gets few rows or wide ones (600 rows of 7168: 7.6 us against 10.9, 8192 rows 87 against 102); else
 //   one row per CTA, whose CTAs' phases mix (8192 rows of 2048, two parameters after the first norm: 24.1 us against 25.7),
-//   and below d = 1024, unless 512 columns leave no thread idle (8192 rows of 512: 7.9 us against 9.7; of 1000: 18.0 against 15.1).
+//   and below d = 1024, unless the columns fill whole warps and leave no thread idle (multiples of 512; 8192 rows of 512: 7.9 us
+//   against 9.7; of 1000: 18.0 against 15.1).
 //   An f32 stream has half as many elements to its bytes and needs the registers: one row per CTA, four chunks (8192 rows of
 //   7168: 123 us against 161).
 //   p.shift: one chunk per thread for few or short rows (515 rows of 1021: 3.3 us against 3.7, after a block 5.6 against 7.0),
@@ -780,7 +784,7 @@ cudaError_t launch_norm(const NormParams& p, int vec, int num_sms, cudaStream_t 
   if (vec == 8) {
     if (p.T < 2 * num_sms)
       return p.d > 8192 || (p.T > num_sms && p.d > 4096) ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
-    if (!p.stream_f32 && (p.d >= 1024 || p.d == 512) && (p.d > 4096 || p.T < 10 * num_sms || p.y == nullptr || folds(p))) return launch_rows<2>(p, num_sms, stream);
+    if (!p.stream_f32 && (p.d >= 1024 || p.d % 512 == 0) && (p.d > 4096 || p.T < 10 * num_sms || p.y == nullptr || folds(p))) return launch_rows<2>(p, num_sms, stream);
     if (p.d > 4096 || (p.stream_f32 && p.d > 2048)) return launch_norm_t<8, 4>(p, stream);
     return p.d > 512 ? launch_norm_t<8, 2>(p, stream) : launch_norm_t<8, 1>(p, stream);
   }

@@ -29,6 +29,8 @@ class MoELayer:
     count        every batch's pairs per expert are written to `counts` (i32 [E]) and added to `cum_counts` (u32 counters in
                  an i32 tensor, mod 2^32), which the dispatch solver works from.  The block counts as it dispatches; a
                  few-token batch takes one more kernel for it, the block's first step (6 us).  Without it both are None.
+
+    A layer has one set of buffers and one workspace: its calls must follow one another on one stream (or be ordered by events).
     """
 
     def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
