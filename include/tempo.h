@@ -368,8 +368,9 @@ int tempo_route(const tempo_shape* shape, int32_t score, int32_t renormalise, fl
  * _bf16 call x enters as it is and H as two bf16 terms (16 bits).  Sums are in 32 bits, silu uses the fast exponential and
  * division (2^-19 of its value for gates within +-8).
  * A value of x or H that is not finite (the _bf16 call: an H beyond bf16's range) makes its own token's output NaN.  Rows
- * without a local expert and rows t >= n_valid are zero.  An id outside [0, E) of a live row is ignored (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token
- * counts twice.  Results do not depend on timing; nothing is summed with atomics.
+ * without a local expert and rows t >= n_valid are zero.  An id outside [0, E) of a live row is ignored
+ * (TEMPO_STATUS_BAD_ID).  An expert listed twice for a token counts twice.  Results do not depend on timing; nothing is
+ * summed with atomics.
  *   in   x bf16 [T, d] (16-byte aligned), topk_ids i32 [T, k], topk_w f32 [T, k], n_valid or NULL,
  *        replica_map i32 [E, R_max], packed (256-byte aligned)
  *   out  out bf16 [T, d] (16-byte aligned)

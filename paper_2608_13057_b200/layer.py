@@ -31,6 +31,8 @@ class MoELayer:
                  few-token batch takes one more kernel for it, the block's first step (6 us).  Without it both are None.
 
     A layer has one set of buffers and one workspace: its calls must follow one another on one stream (or be ordered by events).
+    `status` collects the STATUS_* bits of every call.  After STATUS_TIMEOUT zero `workspace` and, where there is one,
+    `block.workspace`.
     """
 
     def __init__(self, max_tokens, k, G_max, f, w_router, replica_map, packed, norm_w, post_w=None, next_w=None, bias=None,
@@ -58,7 +60,10 @@ class MoELayer:
         if self.block is not None:                       # the block reads this layer's tables and tensors
             self.block.replica_map, self.block.quota = self.replica_map, self.quota
             if bf16:
+                self.block.packed_bf16 = packed
                 self.block.alloc_bf16()
+            else:
+                self.block.packed = packed
             self.block.x, self.block.topk_ids, self.block.topk_w = self.x, self.topk_ids, self.topk_w
             self.block.out, self.block.status = self.y, self.status
         self.counts = self.cum_counts = None
@@ -92,7 +97,7 @@ class MoELayer:
             ffn(shape, x, ids, w, n_valid, self.replica_map, self.packed, y, self.status, self.workspace)
         else:
             self.block.n_valid = n_valid
-            (self.block.run_block_bf16 if self.bf16 else self.block.run_block)(self.packed, T=T)
+            (self.block.run_block_bf16 if self.bf16 else self.block.run_block)(T=T)
         next_w, next_b = (self.next_w, self.next_b) if x_next is not None else (None, None)
         B.tempo_norm_out(y, r, r_out, post_w=self.post_w, post_b=self.post_b, gate=self.gate if gate is None else gate,
                          next_w=next_w, next_b=next_b, x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale,

@@ -32,7 +32,8 @@ class Case:
         else:
             (q13, s13, self.w13), (q2, s2, self.w2) = _fp8(w13), _fp8(w2)
             packed = torch.empty(B.tempo_packed_weight_bytes(shape), dtype=torch.uint8, device="cuda")
-            B.tempo_pack_weights(shape, q13.cuda(), s13.cuda(), q2.cuda(), s2.cuda(), packed, torch.zeros(1, dtype=torch.int32, device="cuda"))
+            st = torch.zeros(1, dtype=torch.int32, device="cuda")
+            B.tempo_pack_weights(shape, q13.cuda(), s13.cuda(), q2.cuda(), s2.cuda(), packed, st)
         rmap = torch.full((E, 1), -1, dtype=torch.int32)
         rmap[:G, 0] = torch.arange(G, dtype=torch.int32)
         self.w_router = (torch.randn(E, d, generator=g) * 0.2).bfloat16()
