@@ -73,7 +73,9 @@ enum {
   TEMPO_STATUS_CAPACITY = 4,   /* padded rows exceed M_cap: rows that do not fit are dropped         */
   TEMPO_STATUS_TIMEOUT = 8,    /* a bounded device wait expired; the outputs of that call are invalid */
   TEMPO_STATUS_BAD_SCALE = 16, /* tempo_pack_weights met a weight scale that is not a power of two   */
-  TEMPO_STATUS_BAD_LOGIT = 32  /* tempo_route met a logit that is not finite: chosen last, weight 0   */
+  TEMPO_STATUS_BAD_LOGIT = 32, /* tempo_route met a logit that is not finite: chosen last, weight 0   */
+  TEMPO_STATUS_BAD_INDEX = 64, /* a position, slot, page, length or row range outside what it points into */
+  TEMPO_STATUS_BAD_VALUE = 128 /* tempo_kv_append met a key or value that is not finite                   */
 };
 
 int tempo_version(void);
@@ -387,6 +389,87 @@ int tempo_few_ffn(const tempo_shape* shape, const void* x_bf16, const int32_t* t
 int tempo_few_ffn_bf16(const tempo_shape* shape, const void* x_bf16, const int32_t* topk_ids, const float* topk_w,
                        const int32_t* n_valid, const int32_t* replica_map, const void* packed, void* out_bf16,
                        uint32_t* status, void* workspace, void* stream);
+
+/*
+ * The attention half of a layer, between the projections: norm and rotation of each head, a paged cache of keys and values
+ * held in 4 bits, and attention over it.
+ *
+ * The cache.  n_pages pages of page_size tokens (16, 32, 64, 128 or 256), Hkv heads of D = 64 or 128 elements.  32 neighbouring
+ * elements of a head and token are a group: 4-bit codes c, a scale s and a zero point z, element = s * (c - z).  s has four
+ * significant bits (an fp16 number whose upper byte, sign bit shifted out, is stored: 2^-17 to 768), z is 0 to 15, so that every
+ * element is exact in fp16.  For a group of values x
+ *     s = the least such number >= (max(x, 0) - min(x, 0)) / 15, at most 768    z = rint(-min(x, 0) / s)
+ *     c = rint(x / s) + z, clamped to [0, 15]                                   (s = 0 for a group of zeros)
+ * Memory: page, head, key or value, then units of 16 tokens: 8 D bytes of codes and D bytes of (s, 16 z) byte pairs.  In a unit
+ * of keys, token t has bytes [t D/2, (t+1) D/2) of codes, element 2i in the low half of byte i, and D/32 byte pairs.  In a unit
+ * of values two tokens 2p, 2p+1 share 32-bit words: word i of the pair holds elements 4i to 4i+3 of the even token in its low
+ * half and of the odd one in its high half; their byte pairs follow each other group by group.
+ *   tempo_cache_bytes [host]   9 D * page_size / 8 * Hkv * n_pages; the cache is 16-byte aligned, and needs no initial value
+ */
+typedef struct {
+  int32_t n_pages, page_size, Hkv, D;
+} tempo_cache;
+int tempo_cache_bytes(const tempo_cache* shape /*[host]*/, size_t* bytes /*[host]*/);
+
+/*
+ *   tempo_qk_rotate   q' = rot(norm(q) * q_w, position), k' = rot(norm(k) * k_w, position), head by head, in one pass
+ *   tempo_kv_append   the same, with k' and v going into the cache (row t to token slots[t] % page_size of page
+ *                     slots[t] / page_size).  k' is not rounded before it is quantised, and is computed in 64 bits: the codes are
+ *                     those of the formula also where a value lies next to a border between two of them.
+ *   tempo_kv_read     rows of the cache back as fp16, exactly: k[i], v[i] = token slots[i]
+ * norm(x) = x / sqrt(mean(x^2) + eps) over the D elements of a head; without q_w (k_w) that operand is not normed.
+ * rot turns the pairs (i, i + rot/2), or with `interleaved` (2i, 2i+1), i < rot/2, of the first `rot` elements by
+ * (cos, sin) = cos_sin[position, i], cos_sin[position, rot/2 + i]; the others pass.  rot = 0: no rotation, no table.
+ *   q, q' bf16 [T, Hq, D], k, k', v bf16 [T, Hkv, D]: heads of D contiguous elements at row and head pitches ld_*, hd_*
+ *   (elements), any alignment; q' may be q and k' may be k (same address and pitches).  A tensor without heads (Hq = 0, or
+ *   Hkv = 0 in tempo_qk_rotate) is not touched.  q_w, k_w bf16 or f32 (w_f32) [D]; positions i32 [T]; cos_sin f32 [n_pos, rot];
+ *   slots i32 [T]; n_valid (or NULL: T): rows t >= n_valid are neither read nor written.
+ * A position outside the table uses its nearest row, a slot beyond the cache is skipped (TEMPO_STATUS_BAD_INDEX); a slot below
+ * zero is skipped without a status bit (tempo_kv_read: zeros are returned for both).  Slots of one call are distinct.  A token
+ * with a key or value that is not finite is marked in its head's key scales (TEMPO_STATUS_BAD_VALUE): what attends to it becomes
+ * NaN, and nothing else does; its values that are not finite are stored as 0.
+ * D: multiples of 8 up to 256 for tempo_qk_rotate; rot even and at most D.
+ */
+typedef struct {
+  int32_t T, Hq, Hkv, D, rot, interleaved, n_pos;
+  int32_t w_f32;                            /* 0: bf16, 1: f32 */
+  int64_t ld_q, hd_q, ld_k, hd_k, ld_v, hd_v, ld_q_out, hd_q_out, ld_k_out, hd_k_out;
+  float eps;
+} tempo_heads;
+int tempo_qk_rotate(const tempo_heads* args, const void* q_bf16, const void* k_bf16, const void* q_w, const void* k_w,
+                    const int32_t* positions, const float* cos_sin, const int32_t* n_valid, void* q_out_bf16, void* k_out_bf16,
+                    uint32_t* status, void* stream);
+int tempo_kv_append(const tempo_heads* args, const tempo_cache* shape, const void* q_bf16, const void* k_bf16, const void* v_bf16,
+                    const void* q_w, const void* k_w, const int32_t* positions, const float* cos_sin, const int32_t* slots,
+                    const int32_t* n_valid, void* q_out_bf16, void* cache, uint32_t* status, void* stream);
+int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* slots, int32_t n, void* k_f16, void* v_f16,
+                  uint32_t* status, void* stream);
+
+/*
+ * Attention over the cache.  Sequence b has lens[b] tokens in the cache, token t at page page_table[b, t / page_size], and
+ * queries q[q_start[b]] to q[q_start[b+1] - 1], which are its newest tokens (already appended): query i of n sees the tokens
+ * t <= lens[b] - n + i.
+ *     out[i, h] = sum_t softmax_t(scale * <q[i, h], K[t, h / (Hq / Hkv)]>) V[t, h / (Hq / Hkv)]
+ * A query that sees no token gets zeros.  K and V enter as they are (fp16 products, sums in 32 bits), q exactly up to 2^-24 of
+ * its head's largest element; softmax weights are rounded to fp16 before they meet V, statistics are in 32 bits.
+ *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), 16-byte aligned rows (address and
+ *   pitches); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
+ *   max_q [host] is the most queries of a sequence: a hint for the choice of kernels, any value gives the same result within rounding.
+ *   Rows before q_start[0] and from q_start[B] on are left as they are.  Hq is a multiple of Hkv; B <= 2048.
+ *   workspace  tempo_attend_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves it
+ *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.
+ * A length beyond the page table counts as its end, rows outside q as none, both with TEMPO_STATUS_BAD_INDEX; a page outside
+ * the cache that holds tokens of a sequence makes the outputs that see it NaN (TEMPO_STATUS_BAD_INDEX).  Results do not depend on timing.
+ */
+typedef struct {
+  int32_t B, T, Hq, max_q, max_pages;
+  int64_t ld_q, hd_q, ld_out, hd_out;
+  float scale;
+} tempo_attention;
+int tempo_attend_workspace_bytes(const tempo_cache* shape /*[host]*/, int32_t Hq, size_t* bytes /*[host]*/);
+int tempo_attend(const tempo_attention* args, const tempo_cache* shape, const void* q_bf16, const void* cache,
+                 const int32_t* page_table, const int32_t* lens, const int32_t* q_start, void* out_bf16, uint32_t* status,
+                 void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

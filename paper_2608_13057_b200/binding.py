@@ -1,4 +1,5 @@
-"""Thin binding of libtempo.so (ctypes; the extension module _marshal for the norms, the router and the few-token FFN).
+"""Thin binding of libtempo.so (ctypes; the extension module _marshal for the norms, the router, the few-token FFN and
+the attention half of a layer).
 Argument marshalling only: every step runs in the CUDA kernels.
 
 The functions carry the C-ABI names (see include/tempo.h).  Tensors are torch CUDA tensors used as
@@ -35,6 +36,7 @@ _LIB_PATH = os.environ.get("TEMPO_LIB") or os.path.join(os.path.dirname(os.path.
 
 TEMPO_OK = 0
 STATUS_BAD_ID, STATUS_BAD_TABLE, STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_BAD_SCALE, STATUS_BAD_LOGIT = 1, 2, 4, 8, 16, 32
+STATUS_BAD_INDEX, STATUS_BAD_VALUE = 64, 128
 NORM_RMS, NORM_LAYER = 0, 1
 ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 
@@ -47,11 +49,16 @@ EXPORTS = (
     "tempo_count_dispatch_masked", "tempo_permute_pad_masked", "tempo_grouped_ffn_masked",
     "tempo_packed_weight_bytes_bf16", "tempo_pack_weights_bf16", "tempo_permute_pad_bf16", "tempo_grouped_ffn_bf16",
     "tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_workspace_bytes", "tempo_few_ffn", "tempo_few_ffn_bf16",
+    "tempo_cache_bytes", "tempo_qk_rotate", "tempo_kv_append", "tempo_kv_read", "tempo_attend_workspace_bytes", "tempo_attend",
 )
 
 
 class TempoShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "G_max", "R_max", "d", "f", "M_cap")]
+
+
+class TempoCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "Hkv", "D")]
 
 
 class TempoError(RuntimeError):
@@ -293,7 +300,9 @@ def tempo_grouped_ffn_bf16(shape, a_bf16, packed, inst_off, m_pad, h_bf16, y_bf1
 if not isinstance(_marshal, _NoMarshal):
     _marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
                                 ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",
-                                 "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16")))
+                                 "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16",
+                                 "tempo_qk_rotate", "tempo_kv_append", "tempo_kv_read", "tempo_attend", "tempo_cache_bytes",
+                                 "tempo_attend_workspace_bytes")))
 
 
 def tempo_norm_in(r, w, x_out, b=None, kind=NORM_RMS, eps=1e-6, n_valid=None):
@@ -340,6 +349,66 @@ def tempo_few_ffn_bf16(shape, x_bf16, topk_ids, topk_w, n_valid, replica_map, pa
                       workspace)
     if rc:
         _check(rc, "tempo_few_ffn_bf16")
+
+
+# ---- the attention half of a layer: norm and rotation of heads, the 4-bit paged cache, attention over it ------
+
+def make_cache(n_pages, page_size, Hkv, D) -> TempoCache:
+    """The shape of a cache: pages of 16, 32, 64, 128 or 256 tokens, Hkv heads of D = 64 or 128."""
+    return TempoCache(n_pages, page_size, Hkv, D)
+
+
+def tempo_cache_bytes(cache_shape: TempoCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.tempo_cache_bytes(ctypes.byref(cache_shape), ctypes.byref(out)), "tempo_cache_bytes")
+    return out.value
+
+
+def tempo_qk_rotate(q, k, positions, cos_sin, q_out, k_out, status, q_w=None, k_w=None, eps=1e-6, interleaved=False, n_valid=None):
+    """q_out = rot(norm(q) * q_w), k_out = rot(norm(k) * k_w), head by head.
+
+    q, q_out bf16 [T, Hq, D], k, k_out bf16 [T, Hkv, D] (heads contiguous, any pitches; an output may be its input); q or k may
+    be None.  positions i32 [T] and cos_sin f32 [positions, rot] (cos, then sin), or both None: no rotation.  q_w, k_w [D] of
+    one dtype, or None: not normed."""
+    rc = _marshal.qk_rotate(q, k, positions, cos_sin, q_out, k_out, status, q_w, k_w, eps, interleaved, n_valid)
+    if rc:
+        _check(rc, "tempo_qk_rotate")
+
+
+def tempo_kv_append(cache_shape, k, v, slots, cache, status, k_w=None, positions=None, cos_sin=None, q=None, q_w=None, q_out=None,
+                    eps=1e-6, interleaved=False, n_valid=None):
+    """k (normed and rotated as tempo_qk_rotate does) and v, bf16 [T, Hkv, D], to the tokens slots i32 [T] of the cache; q, if
+    given, to q_out in the same pass."""
+    rc = _marshal.kv_append(ctypes.addressof(cache_shape), k, v, slots, cache, status, k_w, positions, cos_sin, q, q_w, q_out, eps,
+                            interleaved, n_valid)
+    if rc:
+        _check(rc, "tempo_kv_append")
+
+
+def tempo_kv_read(cache_shape, cache, slots, k_out, v_out, status):
+    """The tokens slots i32 [n] of the cache as fp16 [n, Hkv, D] (exact)."""
+    rc = _marshal.kv_read(ctypes.addressof(cache_shape), cache, slots, k_out, v_out, status)
+    if rc:
+        _check(rc, "tempo_kv_read")
+
+
+def tempo_attend_workspace_bytes(cache_shape: TempoCache, Hq: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.tempo_attend_workspace_bytes(ctypes.byref(cache_shape), ctypes.c_int32(Hq), ctypes.byref(out)),
+           "tempo_attend_workspace_bytes")
+    return out.value
+
+
+def tempo_attend(cache_shape, q, cache, page_table, lens, out, status, workspace, scale=None, q_start=None, max_q=1):
+    """out[i] = attention of q[i] over its sequence's cached tokens, up to its own.
+
+    q, out bf16 [T, Hq, D]; page_table i32 [B, pages], lens i32 [B]; q_start i32 [B + 1]: the queries of sequence b are rows
+    q_start[b] to q_start[b + 1] - 1, its newest tokens (None: one query per sequence).  scale: None is D ** -0.5.  max_q: the
+    most queries of a sequence, for the choice of kernels."""
+    rc = _marshal.attend(ctypes.addressof(cache_shape), q, cache, page_table, lens, out, status, workspace,
+                         cache_shape.D ** -0.5 if scale is None else scale, q_start, max_q)
+    if rc:
+        _check(rc, "tempo_attend")
 
 
 # ------------------------------------------------------------------------------------------------

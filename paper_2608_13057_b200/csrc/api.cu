@@ -611,4 +611,140 @@ int tempo_few_ffn_bf16(const tempo_shape* s, const void* x_bf16, const int32_t* 
   return run_few(true, s, x_bf16, topk_ids, topk_w, n_valid, replica_map, packed, out_bf16, status, workspace, stream);
 }
 
+// ---- the attention half of a layer ------------------------------------------------------------------------
+static int check_cache(const tempo_cache* c) {
+  if (c == nullptr) return TEMPO_ERR_NULL;
+  if (c->n_pages <= 0 || c->Hkv <= 0) return TEMPO_ERR_SHAPE;
+  if ((c->D != 64 && c->D != 128) || c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return TEMPO_ERR_UNSUPPORTED;
+  if (static_cast<long long>(c->n_pages) * c->page_size > 0x7fffffffll || c->Hkv > 65536) return TEMPO_ERR_UNSUPPORTED;
+  return TEMPO_OK;
+}
+
+int tempo_cache_bytes(const tempo_cache* c, size_t* bytes) {
+  if (bytes == nullptr) return TEMPO_ERR_NULL;
+  const int rc = check_cache(c);
+  if (rc != TEMPO_OK) return rc;
+  *bytes = 9ull * c->D * c->page_size / 8 * c->Hkv * c->n_pages;
+  return TEMPO_OK;
+}
+
+static bool vectors8(const void* p, int64_t ld, int64_t hd) { return aligned(p, 16) && ld % 8 == 0 && hd % 8 == 0; }
+
+// Heads of D elements at these pitches; those of an output do not overlap (rows of heads, or heads of rows).
+static bool pitches(int64_t ld, int64_t hd) { return ld >= 0 && hd >= 0 && ld < (1ll << 40) && hd < (1ll << 40); }
+static bool apart(int64_t ld, int64_t hd, int64_t T, int64_t H, int D) {
+  return pitches(ld, hd) && (H == 1 || hd >= D) && (T == 1 || ld >= D) && (H == 1 || T == 1 || ld >= (H - 1) * hd + D || hd >= (T - 1) * ld + D);
+}
+
+static int check_heads(const tempo_heads* a, bool append) {
+  if (a == nullptr) return TEMPO_ERR_NULL;
+  if (a->T <= 0 || a->Hq < 0 || a->Hkv < 0 || a->Hq + static_cast<int64_t>(a->Hkv) == 0 || (append && a->Hkv == 0)) return TEMPO_ERR_SHAPE;
+  if (a->D <= 0 || a->D % 8 || a->rot < 0 || a->rot > a->D || a->rot % 2 || (a->rot > 0 && a->n_pos <= 0)) return TEMPO_ERR_SHAPE;
+  if (a->D > 256 || a->Hq > 65536 || a->Hkv > 65536 || (a->interleaved != 0 && a->interleaved != 1)) return TEMPO_ERR_UNSUPPORTED;
+  if (a->Hq > 0 && (!pitches(a->ld_q, a->hd_q) || !apart(a->ld_q_out, a->hd_q_out, a->T, a->Hq, a->D))) return TEMPO_ERR_SHAPE;
+  if (a->Hkv > 0 && !pitches(a->ld_k, a->hd_k)) return TEMPO_ERR_SHAPE;
+  if (append && !pitches(a->ld_v, a->hd_v)) return TEMPO_ERR_SHAPE;
+  if (!append && a->Hkv > 0 && !apart(a->ld_k_out, a->hd_k_out, a->T, a->Hkv, a->D)) return TEMPO_ERR_SHAPE;
+  return TEMPO_OK;
+}
+
+static int run_heads(const tempo_heads* a, const tempo_cache* c, const void* q, const void* k, const void* v, const void* q_w,
+                     const void* k_w, const int32_t* positions, const float* cos_sin, const int32_t* slots, const int32_t* n_valid,
+                     void* q_out, void* k_out, void* cache, uint32_t* status, void* stream) {
+  const bool append = c != nullptr;
+  if (!status || (a->Hq > 0 && (!q || !q_out)) || (a->Hkv > 0 && !k) || (a->rot > 0 && (!positions || !cos_sin))) return TEMPO_ERR_NULL;
+  if (append ? !v || !slots || !cache : a->Hkv > 0 && !k_out) return TEMPO_ERR_NULL;
+  const size_t ws = a->w_f32 ? 4 : 2;
+  if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_out, 2) || !aligned(k_out, 2) || !aligned(q_w, ws) ||
+      !aligned(k_w, ws) || !aligned(positions, 4) || !aligned(cos_sin, 4) || !aligned(slots, 4) || !aligned(n_valid, 4) ||
+      !aligned(cache, 16) || !aligned(status, 4))
+    return TEMPO_ERR_ALIGN;
+  HeadsParams p{};
+  p.T = a->T; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.rot = a->rot; p.interleaved = a->interleaved; p.n_pos = a->n_pos;
+  p.w_f32 = a->w_f32;
+  p.q_vec = vectors8(q, a->ld_q, a->hd_q); p.k_vec = vectors8(k, a->ld_k, a->hd_k); p.v_vec = vectors8(v, a->ld_v, a->hd_v);
+  p.q_out_vec = vectors8(q_out, a->ld_q_out, a->hd_q_out); p.k_out_vec = vectors8(k_out, a->ld_k_out, a->hd_k_out);
+  p.w_vec = aligned(q_w, 16) && aligned(k_w, 16);
+  p.rot_vec = aligned(cos_sin, 16) && a->rot % (a->interleaved ? 8 : 16) == 0;
+  p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);
+  p.q_w = q_w; p.k_w = k_w; p.positions = positions; p.cos_sin = cos_sin; p.n_valid = n_valid;
+  p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out);
+  p.ld_q = a->ld_q; p.hd_q = a->hd_q; p.ld_k = a->ld_k; p.hd_k = a->hd_k; p.ld_v = a->ld_v; p.hd_v = a->hd_v;
+  p.ld_q_out = a->ld_q_out; p.hd_q_out = a->hd_q_out; p.ld_k_out = a->ld_k_out; p.hd_k_out = a->hd_k_out;
+  p.eps = a->eps; p.status = status;
+  if (append) {
+    p.n_pages = c->n_pages; p.page_size = c->page_size; p.slots = slots; p.cache = static_cast<uint8_t*>(cache);
+  }
+  return launch_heads(p, append, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+int tempo_qk_rotate(const tempo_heads* a, const void* q, const void* k, const void* q_w, const void* k_w, const int32_t* positions,
+                    const float* cos_sin, const int32_t* n_valid, void* q_out, void* k_out, uint32_t* status, void* stream) {
+  const int rc = check_heads(a, false);
+  if (rc != TEMPO_OK) return rc;
+  return run_heads(a, nullptr, q, k, nullptr, q_w, k_w, positions, cos_sin, nullptr, n_valid, q_out, k_out, nullptr, status, stream);
+}
+
+int tempo_kv_append(const tempo_heads* a, const tempo_cache* c, const void* q, const void* k, const void* v, const void* q_w,
+                    const void* k_w, const int32_t* positions, const float* cos_sin, const int32_t* slots, const int32_t* n_valid,
+                    void* q_out, void* cache, uint32_t* status, void* stream) {
+  int rc = check_cache(c);
+  if (rc == TEMPO_OK) rc = check_heads(a, true);
+  if (rc != TEMPO_OK) return rc;
+  if (a->D != c->D || a->Hkv != c->Hkv) return TEMPO_ERR_SHAPE;
+  return run_heads(a, c, q, k, v, q_w, k_w, positions, cos_sin, slots, n_valid, q_out, nullptr, cache, status, stream);
+}
+
+int tempo_kv_read(const tempo_cache* c, const void* cache, const int32_t* slots, int32_t n, void* k, void* v, uint32_t* status,
+                  void* stream) {
+  const int rc = check_cache(c);
+  if (rc != TEMPO_OK) return rc;
+  if (n <= 0) return TEMPO_ERR_SHAPE;
+  if (!cache || !slots || !k || !v || !status) return TEMPO_ERR_NULL;
+  if (!aligned(cache, 16) || !aligned(slots, 4) || !aligned(k, 16) || !aligned(v, 16) || !aligned(status, 4)) return TEMPO_ERR_ALIGN;
+  KvReadParams p{n, c->n_pages, c->page_size, c->Hkv, static_cast<const uint8_t*>(cache), slots, static_cast<__half*>(k),
+                 static_cast<__half*>(v), status};
+  return launch_kv_read(p, c->D, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+int tempo_attend_workspace_bytes(const tempo_cache* c, int32_t Hq, size_t* bytes) {
+  if (bytes == nullptr) return TEMPO_ERR_NULL;
+  const int rc = check_cache(c);
+  if (rc != TEMPO_OK) return rc;
+  if (Hq <= 0 || Hq % c->Hkv) return TEMPO_ERR_SHAPE;
+  *bytes = attend_layout(c->D).total;
+  return TEMPO_OK;
+}
+
+int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, const void* cache, const int32_t* page_table,
+                 const int32_t* lens, const int32_t* q_start, void* out, uint32_t* status, void* workspace, void* stream) {
+  const int rc = check_cache(c);
+  if (rc != TEMPO_OK) return rc;
+  if (a == nullptr || !q || !cache || !page_table || !lens || !out || !status || !workspace) return TEMPO_ERR_NULL;
+  if (a->B <= 0 || a->T <= 0 || a->Hq <= 0 || a->Hq % c->Hkv || a->max_pages <= 0 || a->max_q <= 0 || (!q_start && a->B != a->T))
+    return TEMPO_ERR_SHAPE;
+  if (!pitches(a->ld_q, a->hd_q) || !apart(a->ld_out, a->hd_out, a->T, a->Hq, c->D)) return TEMPO_ERR_SHAPE;
+  if (a->B > kAttendMaxB || a->Hq > 65536 || static_cast<long long>(a->max_pages) * c->page_size > 0x7fffff00ll ||
+      static_cast<long long>(a->T) * (a->Hq / c->Hkv) > 0x7fffff00ll)
+    return TEMPO_ERR_UNSUPPORTED;
+  if (!vectors8(q, a->ld_q, a->hd_q) || !vectors8(out, a->ld_out, a->hd_out) || !aligned(cache, 16) || !aligned(page_table, 4) ||
+      !aligned(lens, 4) || !aligned(q_start, 4) || !aligned(status, 4) || !aligned(workspace, 256))
+    return TEMPO_ERR_ALIGN;
+  const int sms = min(sm_count(), kAttendMaxSms);
+  if (sms <= 0) return TEMPO_ERR_CUDA;
+  const AttendLayout L = attend_layout(c->D);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  AttendParams p{};
+  p.B = a->B; p.T = a->T; p.Hkv = c->Hkv; p.group = a->Hq / c->Hkv;
+  p.max_pages = a->max_pages; p.page_size = c->page_size; p.n_pages = c->n_pages;
+  p.q = static_cast<const __nv_bfloat16*>(q); p.cache = static_cast<const uint8_t*>(cache);
+  p.page_table = page_table; p.lens = lens; p.q_start = q_start; p.out = static_cast<__nv_bfloat16*>(out);
+  p.ld_q = a->ld_q; p.hd_q = a->hd_q; p.ld_out = a->ld_out; p.hd_out = a->hd_out;
+  p.scale_log2 = a->scale * 1.4426950408889634f; p.status = status;
+  p.counters = reinterpret_cast<unsigned int*>(ws + L.off_counters);
+  p.stats = reinterpret_cast<float*>(ws + L.off_stats); p.part = reinterpret_cast<float*>(ws + L.off_out);
+  p.wait_ns = kDefaultWaitNs;
+  return launch_attend(p, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
 }  // extern "C"

@@ -1,0 +1,629 @@
+// Attention over the 4-bit paged cache (tempo_attend).
+//
+//   out[i, h] = sum_t p[t] V[t] / sum_t p[t],  p[t] = exp(scale <q, K[t]> - m),  t <= the query's own position
+//
+// A key head's queries (the heads of its group, and the new tokens of the sequence) are the rows of one item, 16 rows to an item;
+// each cached byte is read once for all of them.  One pass over the tokens with the running maximum and sum.
+//
+// Bound by the cache's bytes, which one SM takes in at 23 bytes a clock: that leaves 2.8 instruction slots of a lane for each
+// cached element.  So codes go from shared memory to registers and are decoded there into the B operands of the
+// matrix instruction (m16n8k16, 32-bit sums), at 11 instructions for 8 elements; a decoded copy in shared memory for the
+// tensor-memory form of the instruction would move 2 bytes per element in and 2 out, 184 bytes a clock where the SM has 128.
+// The order of a sum over d or t is free, so that a lane's 16-byte load is what it needs: of keys 32 neighbouring elements
+// (one group: one scale) of one token, of values 16 neighbouring elements of two tokens side by side in a word's halves.
+//
+// Work is dealt in tiles of 32 tokens: the tiles of all items in one row, cut into equal runs, one for each warp of the
+// launch, whatever the lengths.  A warp streams its run through a ring of its own (bulk copies, one barrier per stage) and
+// waits for nobody; parts of items that were cut are joined in shared memory after the CTA's last tile, and across CTAs by the one
+// that arrives last, in a fixed order.
+#include "cache.cuh"
+#include "ffn_common.cuh"
+
+namespace tempo {
+
+namespace {
+
+constexpr int kWarps = 12, kTile = 32, kRows = 16;
+constexpr float kBias = 7.0f, kSlack = 8.0f;      // weights are 2^(x - m + 7); m is raised once x exceeds it by more than 8
+
+struct Item {                 // rows [row0, row0 + 16) of a sequence and key head, and its tiles
+  int64_t begin;              // number of its first tile in the launch
+  int tiles, b, h, row0;
+  int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
+};
+
+struct Span { int len, q0, n; };
+__device__ __forceinline__ Span span_of(const AttendParams& p, int b, bool tell) {
+  Span s;
+  const int len = p.lens[b], most = p.max_pages * p.page_size;
+  s.len = min(max(len, 0), most);
+  int q0 = b, q1 = b + 1;
+  if (p.q_start != nullptr) { q0 = p.q_start[b]; q1 = p.q_start[b + 1]; }
+  s.q0 = min(max(q0, 0), p.T);
+  s.n = max(min(max(q1, 0), p.T) - s.q0, 0);
+  if (tell && (s.len != len || s.q0 != q0 || s.q0 + s.n != q1)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+  return s;
+}
+
+// Tiles that the rows [row0, row0 + 16) see: at least one, so that rows without a token are written too.
+__device__ __forceinline__ int tiles_of(const AttendParams& p, const Span& s, int row0) {
+  const int last = min(row0 + kRows, s.n * p.group) - 1;
+  const int seen = s.len - s.n + last / p.group + 1;
+  return max(1, (seen + kTile - 1) / kTile);
+}
+
+__device__ __forceinline__ Item item_at(const AttendParams& p, const int64_t* before, int64_t x) {
+  int lo = 0, hi = p.B - 1;
+  while (lo < hi) {                                  // the last sequence with before[b] <= x and tiles
+    const int mid = (lo + hi + 1) >> 1;
+    if (before[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  Item it;
+  const Span s = span_of(p, lo, false);
+  it.b = lo; it.len = s.len; it.q0 = s.q0; it.n = s.n;
+  const int64_t per_head = (before[lo + 1] - before[lo]) / p.Hkv;
+  int64_t rest = x - before[lo];
+  it.h = static_cast<int>(rest / per_head);
+  rest -= it.h * per_head;
+  it.row0 = 0;
+  for (;;) {
+    it.tiles = tiles_of(p, s, it.row0);
+    if (rest < it.tiles) break;
+    rest -= it.tiles;
+    it.row0 += kRows;
+  }
+  it.begin = x - rest;
+  return it;
+}
+
+struct Part {                 // a cut item's share of one warp
+  Item item;
+  int valid;
+};
+
+template <int D>
+struct AttendSmem {
+  static constexpr int kStageBytes = 2 * 2 * CacheUnit<D>::kBytes;   // keys and values of two units
+  static constexpr int kStages = D == 64 ? 4 : 2;
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
+  static constexpr int kBars = kRing, kParts = kBars + kWarps * kStages * 8;
+  static constexpr int kRecords = kParts + kWarps * kPart;
+  static constexpr int kBefore = kRecords + kWarps * 2 * static_cast<int>(sizeof(Part));
+  static_assert(kRing >= kWarps * kPart, "the second parts take the ring's place");
+  static_assert(kRing >= kAttendMaxSms * kRows * 4 + kRows * 4, "so do the weights of a join");
+  static int bytes(int B) { return kBefore + (B + 1) * 8; }
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void lds64(uint32_t a, uint32_t (&v)[2]) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
+template <int W>
+__device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&v)[W]) {
+  if constexpr (W == 4) lds128(a, v); else lds64(a, v);
+}
+
+// Float4 number q (of D / 4) of a row in a part: rotated so that the eight lanes of a store's phase meet eight bank groups.
+__device__ __forceinline__ int part_at(int row, int q) { return q ^ ((((row & 1) << 2) | ((q >> 3) & 3)) & 7); }
+
+// A warp's running state of one item.
+template <int D>
+struct Running {
+  static constexpr int kN = D / 8;                   // 8-column tiles of O
+  uint32_t q[D / 16][4];                             // A operands: rows lane / 4 and + 8
+  float f[2];                                        // score = f * (sum of products), in units of log2
+  int limit[2], least;                               // last token that each row sees; the least over the 16 rows
+  float m[2], l[2];
+  float o[kN][4];
+};
+
+template <int D>
+__device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it, Running<D>& s) {
+  constexpr int W = D / 32;                          // 8-element words of a lane
+  const int lane = threadIdx.x & 31, j = lane & 3;
+  const int rows = it.n * p.group;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int row = it.row0 + lane / 4 + 8 * half;
+    const bool in = row < rows;
+    const int qi = row / p.group, head = it.h * p.group + row % p.group;
+    s.limit[half] = in ? it.len - it.n + qi : it.len - 1;
+    float x[W][8];
+    float top = 0.0f;
+    bool odd = false;
+    const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + (in ? qi : 0)) * p.ld_q + static_cast<size_t>(in ? head : 0) * p.hd_q + j * (D / 4);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const uint4 u = in ? __ldg(reinterpret_cast<const uint4*>(src) + w) : make_uint4(0, 0, 0, 0);
+      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[w][i] = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
+        top = fmaxf(top, fabsf(x[w][i]));
+        odd = odd || !isfinite(x[w][i]);
+      }
+    }
+#pragma unroll
+    for (int d = 1; d <= 2; d *= 2) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      odd = __shfl_xor_sync(0xffffffffu, static_cast<int>(odd), d) != 0 || odd;
+    }
+    // the row times a power of two, its largest element in [256, 512): fp16 holds 2^-33 of it
+    const int e = top > 0.0f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -110), 119) : 0;
+    const float up = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    s.f[half] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.scale_log2;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {                  // the pairs (n, n + 4) of decode8, two to a matrix instruction
+        s.q[2 * w + u][half] = as_u32(__floats2half2_rn(x[w][2 * u] * up, x[w][2 * u + 4] * up));
+        s.q[2 * w + u][half + 2] = as_u32(__floats2half2_rn(x[w][2 * u + 1] * up, x[w][2 * u + 5] * up));
+      }
+    s.m[half] = -INFINITY;
+    s.l[half] = 0.0f;
+  }
+  s.least = it.len - it.n + it.row0 / p.group;
+#pragma unroll
+  for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][0] = s.o[i][1] = s.o[i][2] = s.o[i][3] = 0.0f; }
+}
+
+// One tile: tokens [t0, t0 + 32) of the item at `stage`.  `absent`: bits of its two units whose page is not in the cache.
+template <int D>
+__device__ __forceinline__ void run_tile(Running<D>& s, uint32_t stage, int t0, int len, uint32_t absent) {
+  using U = CacheUnit<D>;
+  constexpr int W = D / 32;
+  const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
+  float c[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                      // scores of the tokens 8 i to 8 i + 7
+    c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.0f;
+    const uint32_t unit = stage + (i / 2) * 2 * U::kBytes;
+    const int at = (i & 1) * 8 + g;
+    uint32_t w[W];
+    lds_words<W>(unit + at * U::kKeyRow + j * (D / 8), w);
+    const uint32_t params = lds16(unit + U::kCodes + at * U::kKeyParams + (D == 128 ? j : j / 2) * 2) * 0x10001u;
+    uint32_t sc, b;
+    group_params(params, sc, b);
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      uint32_t v[4];
+      decode8(w[x], sc, b, v);
+      mma_f16(c[i], s.q[2 * x], v[0], v[1]);
+      mma_f16(c[i], s.q[2 * x + 1], v[2], v[3]);
+    }
+  }
+  if (absent != 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (absent >> (i / 2) & 1) c[i][0] = c[i][1] = c[i][2] = c[i][3] = __uint_as_float(0x7fc00000u);
+  }
+  float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) c[i][x] *= s.f[x / 2];
+  if (t0 + kTile - 1 > s.least) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (t0 + 8 * i + 2 * j + (x & 1) > s.limit[x / 2]) c[i][x] = -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top[x / 2] = fmaxf(top[x / 2], c[i][x]);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+  }
+  // a maximum that has grown little stays: weights up to 2^15 are in fp16's range, and O is left alone
+  if (__any_sync(0xffffffffu, top[0] > s.m[0] + kSlack || top[1] > s.m[1] + kSlack)) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float m = top[r] > s.m[r] + kSlack ? top[r] : s.m[r];
+      const float k = m == s.m[r] ? 1.0f : exp2_fast(s.m[r] - m);
+      s.m[r] = m;
+      s.l[r] *= k;
+#pragma unroll
+      for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][2 * r] *= k; s.o[i][2 * r + 1] *= k; }
+    }
+  }
+  uint32_t a[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const float m = s.m[r] == -INFINITY ? 0.0f : s.m[r] - kBias;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 w = __floats2half2_rn(exp2_fast(c[i][2 * r] - m), exp2_fast(c[i][2 * r + 1] - m));
+      a[i / 2][(i & 1) * 2 + r] = as_u32(w);
+      const float2 back = __half22float2(w);         // the sum is that of the weights as they meet V
+      s.l[r] += back.x + back.y;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {                      // unit k: tokens 16 k + 2 j, + 1 and 16 k + 8 + 2 j, + 1
+    const uint32_t unit = stage + (k * 2 + 1) * U::kBytes;
+    uint32_t w[2][W], sc[2], b[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int pair = 4 * x + j;
+      lds_words<W>(unit + pair * U::kPairRow + g * (D / 8), w[x]);
+      uint32_t params = lds32(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4);
+      const int left = len - (t0 + 16 * k + 2 * pair);           // tokens of the pair that exist: what lies behind may be anything
+      if (left < 2) params &= left == 1 ? 0xffffu : 0u;
+      group_params(params, sc[x], b[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      uint32_t v0[4], v1[4];
+      decode8(w[0][x], sc[0], b[0], v0);
+      decode8(w[1][x], sc[1], b[1], v1);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) mma_f16(s.o[4 * x + n], a[k], v0[n], v1[n]);
+    }
+  }
+}
+
+// Sums over the four lanes of a row.
+template <int D>
+__device__ __forceinline__ void close_sums(Running<D>& s) {
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    s.l[r] += __shfl_xor_sync(0xffffffffu, s.l[r], 1);
+    s.l[r] += __shfl_xor_sync(0xffffffffu, s.l[r], 2);
+  }
+}
+
+__device__ __forceinline__ __nv_bfloat16* out_row(const AttendParams& p, const Item& it, int row) {
+  const int r = it.row0 + row;
+  return p.out + static_cast<size_t>(it.q0 + r / p.group) * p.ld_out + static_cast<size_t>(it.h * p.group + r % p.group) * p.hd_out;
+}
+
+// A whole item's result from the registers.  Lane (g, j) has, of the rows g and g + 8, the elements j D/4 to (j+1) D/4 - 1: O tile i
+// holds element i of each of the eight runs of D / 8.
+template <int D>
+__device__ __forceinline__ void store_item(const AttendParams& p, const Item& it, Running<D>& s) {
+  const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
+  close_sums(s);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (it.row0 + g + 8 * r >= it.n * p.group) continue;
+    const float k = s.l[r] == 0.0f ? 0.0f : 1.0f / s.l[r];
+    uint4* dst = reinterpret_cast<uint4*>(out_row(p, it, g + 8 * r) + j * (D / 4));
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 0; i < Running<D>::kN; i += 8) {
+        uint32_t v[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(s.o[i + 2 * x][2 * r + y] * k, s.o[i + 2 * x + 1][2 * r + y] * k);
+          v[x] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        dst[(y * Running<D>::kN + i) / 8] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void keep_part(Running<D>& s, uint8_t* part) {
+  const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
+  close_sums(s);
+  float4* o = reinterpret_cast<float4*>(part);
+  float2* stat = reinterpret_cast<float2*>(part + kRows * D * 4);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int row = g + 8 * r;
+    if (j == 0) stat[row] = make_float2(s.m[r], s.l[r]);
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 0; i < Running<D>::kN; i += 4) {
+        const int q = j * (D / 16) + (y * Running<D>::kN + i) / 4;
+        o[row * (D / 4) + part_at(row, q)] =
+            make_float4(s.o[i][2 * r + y], s.o[i + 1][2 * r + y], s.o[i + 2][2 * r + y], s.o[i + 3][2 * r + y]);
+      }
+  }
+}
+
+__device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 v, float k) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x * k, v.y * k), b = __floats2bfloat162_rn(v.z * k, v.w * k);
+  *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+struct Segment {              // neighbouring parts of one item in this CTA
+  int first, more;            // record of the first part, and how many warps follow with their first parts
+  int slot, cta0, ctas;       // -1: the item is whole; else where its part goes, and the CTAs that share the item
+  int last;                   // this CTA is the last of them to arrive
+};
+
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  using S = AttendSmem<D>;
+  using U = CacheUnit<D>;
+  __shared__ int64_t warp_sum[kWarps];
+  __shared__ Segment segments[kWarps + 1];
+  __shared__ int n_segments, abort_flag;
+  int64_t* before = reinterpret_cast<int64_t*>(smem + S::kBefore);
+  Part* records = reinterpret_cast<Part*>(smem + S::kRecords);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t bars = smem_u32(smem + S::kBars) + warp * S::kStages * 8;
+  const uint32_t ring = smem_u32(smem) + warp * S::kStages * S::kStageBytes;
+
+  pdl_trigger();
+  if (lane < S::kStages) mbar_init(bars + 8 * lane, 1);
+  if (tid == 0) { abort_flag = 0; n_segments = 0; }
+  if (lane < 2) records[2 * warp + lane].valid = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  pdl_wait();
+
+  // tiles before each sequence
+  int64_t total = 0;
+  for (int b0 = 0; b0 < p.B; b0 += kWarps * 32) {
+    const int b = b0 + tid;
+    int64_t mine = 0;
+    if (b < p.B) {
+      const Span s = span_of(p, b, blockIdx.x == 0);
+      for (int row0 = 0; row0 < s.n * p.group; row0 += kRows) mine += tiles_of(p, s, row0);
+      mine *= p.Hkv;
+    }
+    int64_t run = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, run, d);
+      if (lane >= d) run += up;
+    }
+    if (lane == 31) warp_sum[warp] = run;
+    __syncthreads();
+    int64_t base = total;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) base += warp_sum[w];
+      total += warp_sum[w];
+    }
+    if (b < p.B) before[b + 1] = base + run;
+    if (b == 0) before[0] = 0;
+    __syncthreads();
+  }
+  if (total == 0) return;
+
+  const int64_t runs = min(total, static_cast<int64_t>(gridDim.x) * kWarps);
+  const auto run_begin = [&](int64_t r) { return r * total / runs; };
+  const auto run_of = [&](int64_t x) { return ((x + 1) * runs - 1) / total; };
+  const int64_t run0 = static_cast<int64_t>(blockIdx.x) * kWarps;
+  if (run0 >= runs) return;
+  const int64_t cta_begin = run_begin(run0), cta_end = run_begin(min(run0 + kWarps, runs));
+
+  if (run0 + warp < runs) {
+    const int64_t begin = run_begin(run0 + warp), end = run_begin(run0 + warp + 1);
+    Item ahead = item_at(p, before, begin);          // the item of the next tile to be requested
+    int64_t asked = begin;
+    uint32_t absent_bits = 0;                        // two bits per stage
+    const auto request = [&](int stage) {
+      if (asked >= ahead.begin + ahead.tiles) ahead = item_at(p, before, asked);
+      const int unit = static_cast<int>(asked - ahead.begin) * 2 + (lane >> 1);     // lanes 0 to 3: (unit, keys or values)
+      const bool wanted = lane < 4 && unit * kUnit < ahead.len;
+      int page = 0;
+      bool there = true;
+      if (wanted) {
+        page = p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + unit * kUnit / p.page_size];
+        there = page >= 0 && page < p.n_pages;
+        if (!there) { page = 0; atomicOr(p.status, TEMPO_STATUS_BAD_INDEX); }
+      }
+      const uint32_t want = __ballot_sync(0xffffffffu, wanted), gone = __ballot_sync(0xffffffffu, !there);
+      absent_bits = (absent_bits & ~(3u << (2 * stage))) | ((gone & 1u) | (gone >> 1 & 2u)) << (2 * stage);
+      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, __popc(want) * U::kBytes);
+      __syncwarp();
+      if (wanted)
+        bulk_load(ring + stage * S::kStageBytes + lane * U::kBytes,
+                  p.cache + unit_offset<D>(page, ahead.h, lane & 1, unit * kUnit % p.page_size, p.Hkv, p.page_size), U::kBytes,
+                  bars + 8 * stage);
+      ++asked;
+    };
+    for (int st = 0; st < S::kStages && asked < end; ++st) request(st);
+
+    Item it = item_at(p, before, begin);
+    Running<D> s;
+    begin_item<D>(p, it, s);
+    int64_t x = begin;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool fine = true, late = false;
+    while (x < end) {
+      fine = mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns);
+      fine = __all_sync(0xffffffffu, fine);
+      if (!fine) break;
+      run_tile<D>(s, ring + stage * S::kStageBytes, static_cast<int>(x - it.begin) * kTile, it.len, absent_bits >> (2 * stage) & 3u);
+      __syncwarp();
+      if (asked < end) request(stage);
+      ++x;
+      if (x == it.begin + it.tiles || x == end) {
+        const bool whole = it.begin >= begin && x == it.begin + it.tiles;
+        if (whole) {
+          store_item<D>(p, it, s);
+        } else {
+          // The run's first item keeps its part beside the ring.  A last one that is another waits until every warp of the CTA
+          // has left the ring, and takes its place.
+          const int at = it.begin <= begin ? 0 : 1;
+          if (at == 0) keep_part<D>(s, smem + S::kParts + warp * S::kPart);
+          else late = true;
+          if (lane == 0) { records[2 * warp + at].item = it; records[2 * warp + at].valid = 1; }
+        }
+        if (x == end) break;
+        it = item_at(p, before, x);
+        begin_item<D>(p, it, s);
+      }
+      if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+    }
+    if (!fine) {                                     // let what was requested arrive before the memory goes
+      if (lane == 0) atomicOr(p.status, TEMPO_STATUS_TIMEOUT);
+      volatile int none = 0;
+      for (int st = 0; st < S::kStages; ++st) mbar_wait(bars + 8 * st, phase ^ (st < stage ? 1u : 0u), &none, p.wait_ns);
+    }
+    __syncthreads();
+    if (late) keep_part<D>(s, smem + warp * S::kPart);
+  } else {
+    __syncthreads();
+  }
+  __syncthreads();
+
+  // Which parts belong together: those of neighbouring warps with one item.
+  if (warp == 0) {
+    const int w = lane >> 1;
+    bool leads = w < kWarps && records[lane].valid != 0;
+    int more = 0;
+    if (leads) {
+      const int64_t begin = records[lane].item.begin;
+      const auto same = [&](int r) { return records[r].valid != 0 && records[r].item.begin == begin; };
+      if ((lane & 1) == 0 && w > 0 && (same(lane - 1) || same(lane - 2))) leads = false;
+      while (leads && w + 1 + more < kWarps && same(2 * (w + 1 + more))) ++more;
+    }
+    const uint32_t all = __ballot_sync(0xffffffffu, leads);
+    if (leads) {
+      const Item& it = records[lane].item;
+      Segment& g = segments[__popc(all & ((1u << lane) - 1u))];
+      g.first = lane;
+      g.more = more;
+      g.slot = it.begin >= cta_begin && it.begin + it.tiles <= cta_end ? -1 : it.begin <= cta_begin ? 0 : 1;
+      g.cta0 = static_cast<int>(run_of(it.begin) / kWarps);
+      g.ctas = static_cast<int>(run_of(it.begin + it.tiles - 1) / kWarps) - g.cta0 + 1;
+    }
+    if (lane == 0) n_segments = __popc(all);
+  }
+  __syncthreads();
+
+  constexpr int kQuads = kRows * D / 4;
+  const int segs = n_segments;
+  for (int task = tid; task < segs * kQuads; task += kWarps * 32) {
+    const Segment& g = segments[task / kQuads];
+    const int row = task % kQuads / (D / 4), q = task % (D / 4);
+    const int w0 = g.first >> 1;
+    const auto part = [&](int i) -> const uint8_t* {
+      return (i == 0 && (g.first & 1)) ? smem + w0 * S::kPart : smem + S::kParts + (w0 + i) * S::kPart;
+    };
+    float m = -INFINITY;
+    for (int i = 0; i <= g.more; ++i) m = fmaxf(m, reinterpret_cast<const float2*>(part(i) + kRows * D * 4)[row].x);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i <= g.more; ++i) {
+      const float2 st = reinterpret_cast<const float2*>(part(i) + kRows * D * 4)[row];
+      const float4 v = reinterpret_cast<const float4*>(part(i))[row * (D / 4) + part_at(row, q)];
+      const float k = exp2_fast(st.x - ref);
+      l += st.y * k;
+      o.x += v.x * k; o.y += v.y * k; o.z += v.z * k; o.w += v.w * k;
+    }
+    if (g.slot < 0) {
+      const Item& it = records[g.first].item;
+      if (it.row0 + row < it.n * p.group) store4(out_row(p, it, row) + 4 * q, o, l == 0.0f ? 0.0f : 1.0f / l);
+    } else {
+      const size_t at = (static_cast<size_t>(blockIdx.x) * 2 + g.slot) * kRows + row;
+      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q, o);
+      if (q == 0) __stcg(reinterpret_cast<float2*>(p.stats) + at, make_float2(m, l));
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  if (tid < segs && segments[tid].slot >= 0) {
+    Segment& g = segments[tid];
+    g.last = atomicAdd(p.counters + g.cta0, 1u) == static_cast<unsigned>(g.ctas) - 1u;
+    if (g.last) p.counters[g.cta0] = 0;
+  }
+  __syncthreads();
+
+  // Items shared with other CTAs, by the last of them: the parts in the order of the CTAs, whoever it is.
+  float* weights = reinterpret_cast<float*>(smem);
+  for (int i = 0; i < segs; ++i) {
+    const Segment g = segments[i];
+    if (g.slot < 0 || !g.last) continue;
+    __threadfence();
+    const Item it = records[g.first].item;
+    const int64_t begin0 = run_begin(static_cast<int64_t>(g.cta0) * kWarps);
+    const auto row_at = [&](int c, int row) {
+      return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 && it.begin > begin0 ? 1 : 0)) * kRows + row;
+    };
+    for (int row = warp; row < kRows; row += kWarps) {
+      float m = -INFINITY;
+      for (int c = lane; c < g.ctas; c += 32) m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(p.stats) + row_at(c, row)).x);
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      const float ref = m == -INFINITY ? 0.0f : m;
+      float l = 0.0f;
+      for (int c = lane; c < g.ctas; c += 32) {
+        const float2 st = __ldcg(reinterpret_cast<const float2*>(p.stats) + row_at(c, row));
+        const float k = exp2_fast(st.x - ref);
+        weights[c * kRows + row] = k;
+        l += st.y * k;
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+      if (lane == 0) weights[kAttendMaxSms * kRows + row] = l;
+    }
+    __syncthreads();
+    for (int task = tid; task < kQuads; task += kWarps * 32) {
+      const int row = task / (D / 4), q = task % (D / 4);
+      float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+      for (int c = 0; c < g.ctas; ++c) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + row_at(c, row) * D) + q);
+        const float k = weights[c * kRows + row];
+        o.x += v.x * k; o.y += v.y * k; o.z += v.z * k; o.w += v.w * k;
+      }
+      const float l = weights[kAttendMaxSms * kRows + row];
+      if (it.row0 + row < it.n * p.group) store4(out_row(p, it, row) + 4 * q, o, l == 0.0f ? 0.0f : 1.0f / l);
+    }
+    __syncthreads();
+  }
+}
+
+template <int D>
+cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
+  using S = AttendSmem<D>;
+  static_assert(S::kBefore + (kAttendMaxB + 1) * 8 + 1024 <= 227 * 1024, "shared memory of one SM");
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = smem_limit_once(attend_kernel<D>, S::bytes(kAttendMaxB), done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attend_kernel<D>, dim3(num_sms), dim3(kWarps * 32), S::bytes(p.B), stream, p);
+}
+
+}  // namespace
+
+AttendLayout attend_layout(int D) {
+  const auto round = [](size_t v) { return (v + 255) / 256 * 256; };
+  AttendLayout L;
+  L.off_counters = 0;
+  L.off_stats = round(kAttendMaxSms * sizeof(unsigned int));
+  L.off_out = L.off_stats + round(static_cast<size_t>(kAttendMaxSms) * 2 * kRows * 8);
+  L.total = L.off_out + static_cast<size_t>(kAttendMaxSms) * 2 * kRows * D * 4;
+  return L;
+}
+
+cudaError_t launch_attend(const AttendParams& p, int D, int num_sms, cudaStream_t stream) {
+  return D == 64 ? launch_attend_as<64>(p, num_sms, stream) : launch_attend_as<128>(p, num_sms, stream);
+}
+
+}  // namespace tempo

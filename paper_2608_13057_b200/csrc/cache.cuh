@@ -1,0 +1,47 @@
+// The 4-bit paged cache: where a token's codes and scales lie, and how codes become fp16 values (see tempo.h).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "tempo_kernels.cuh"
+
+namespace tempo {
+
+constexpr int kUnit = 16;          // tokens of a unit, the smallest piece of the cache that is contiguous for a head
+constexpr int kGroup = 32;         // elements that share a scale and a zero point
+constexpr uint32_t kMarked = 0xff; // scale byte of a marked token: read as fp16 it is NaN
+
+template <int D>
+struct CacheUnit {
+  static constexpr int kCodes = kUnit * D / 2, kParams = kUnit * D / 16, kBytes = kCodes + kParams;
+  static constexpr int kKeyRow = D / 2, kKeyParams = D / 16;      // of a token
+  static constexpr int kPairRow = D, kPairParams = D / 8;         // of two tokens' values
+};
+
+// First byte of the unit that holds token `at` of a page.  kv: 0 keys, 1 values.
+template <int D>
+__host__ __device__ __forceinline__ size_t unit_offset(int64_t page, int head, int kv, int at, int Hkv, int page_size) {
+  return ((static_cast<size_t>(page) * Hkv + head) * 2 + kv) * (static_cast<size_t>(page_size / kUnit) * CacheUnit<D>::kBytes) +
+         static_cast<size_t>(at / kUnit) * CacheUnit<D>::kBytes;
+}
+
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+__device__ __forceinline__ uint32_t as_u32(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+
+// Two groups' (s, 16 z) byte pairs in the halves of p: s and -s (64 + z) as fp16, both exact (4 and 11 significant bits).
+__device__ __forceinline__ void group_params(uint32_t p, uint32_t& s, uint32_t& b) {
+  s = (p & 0x00ff00ffu) << 7;
+  b = as_u32(__hmul2(as_half2(s), as_half2(((p >> 8) & 0x00f000f0u) | 0xd400d400u)));
+}
+
+// A word of eight codes -> four pairs, pair n of the codes n and n + 4 (bits 4n and 4n + 16).  A code in bits 4 to 7 under the
+// exponent of 64 is the fp16 number 64 + c; one fused step takes it to s (64 + c) - s (64 + z) = s (c - z), which has 8
+// significant bits: nothing is rounded.  11 instructions for 8 elements.
+__device__ __forceinline__ void decode8(uint32_t w, uint32_t s, uint32_t b, uint32_t (&v)[4]) {
+  const uint32_t c[4] = {w << 4, w, w >> 4, w >> 8};
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+    v[n] = as_u32(__hfma2(as_half2((c[n] & 0x00f000f0u) | 0x54005400u), as_half2(s), as_half2(b)));
+}
+
+}  // namespace tempo

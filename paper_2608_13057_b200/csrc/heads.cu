@@ -1,0 +1,372 @@
+// Norm and rotation of each head of queries and keys, the append of keys and values to the 4-bit paged cache, and the way back.
+//   tempo_qk_rotate  x' = rot(norm(x) * w, position) for q and k
+//   tempo_kv_append  the same for q; k' and v quantised into the cache in the same pass
+//   tempo_kv_read    rows of the cache as fp16
+// A head is held by D / 8 neighbouring lanes, eight elements (16 bytes) each, so every operand is read once and every result
+// written once; the sum of squares and a group's extremes are shuffles inside the head, and the other element of a rotated
+// pair comes from its lane.  Bound by the bytes for a prompt, by one launch and one load-sum-load-store chain for a token.
+// k' on its way into the cache is computed in 64 bits (about 150 instructions for eight elements, on a pipe that does half
+// the rate of the 32-bit one): a code is then the formula's also next to a border between two codes, whatever order a sum is
+// taken in, and a cache filled here equals one filled elsewhere.
+#include "cache.cuh"
+
+namespace tempo {
+
+namespace {
+
+__device__ __forceinline__ uint4 load8(const __nv_bfloat16* p, bool vec) {
+  uint4 u;
+  if (vec) {
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p) : "memory");
+  } else {
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = h[2 * i] | (static_cast<uint32_t>(h[2 * i + 1]) << 16);
+    u = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+  return u;
+}
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8], bool vec) {
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+    v[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  if (vec) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]);
+  } else {
+    uint16_t* h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
+  }
+}
+
+__device__ __forceinline__ void widen8(uint4 u, float (&x)[8]) {
+  const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
+}
+
+__device__ __forceinline__ void weights8(const void* w, int f32, bool vec, int e, float (&x)[8]) {
+  if (f32) {
+    const float* p = static_cast<const float*>(w) + e;
+    if (vec) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
+    }
+  } else {
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(w) + e;
+    if (vec) {
+      widen8(__ldg(reinterpret_cast<const uint4*>(p)), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+    }
+  }
+}
+
+__device__ __forceinline__ float weight1(const void* w, int f32, int e) {
+  return f32 ? __ldg(static_cast<const float*>(w) + e) : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[e]);
+}
+
+template <typename R>
+__device__ __forceinline__ R inverse_root(R v);
+template <>
+__device__ __forceinline__ float inverse_root<float>(float v) { return rsqrtf(v); }
+template <>
+__device__ __forceinline__ double inverse_root<double>(double v) { return rsqrt(v); }
+
+// One operand of the launch: queries or keys.
+struct Operand {
+  const __nv_bfloat16* x;
+  size_t ld, hd;
+  const void* w;
+  bool vec;
+};
+
+// A lane's eight elements of norm(x) * w turned by the row's angles, in R.  `e` is the lane's first element, beyond D for a
+// lane without one; every lane of the warp takes part in the shuffles.  The loads from x are done when this returns.
+template <int LPH, typename R>
+__device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, size_t at, int e, bool live, const float* angles,
+                                       uint4 raw, R (&y)[8]) {
+  const int lane = threadIdx.x & 31, half = p.rot / 2;
+  const bool mine = live && e < p.D;
+  float x[8], w[8];
+  widen8(raw, x);
+  R r = R(1);
+  if (o.w != nullptr) {
+    R ss = R(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss += R(x[i]) * R(x[i]);
+#pragma unroll
+    for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+    r = inverse_root<R>(ss / R(p.D) + R(p.eps));
+    if (mine) weights8(o.w, p.w_f32, p.w_vec, e, w);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = o.w != nullptr ? R(x[i]) * r * R(w[i]) : R(x[i]);
+  if (p.rot == 0) return;
+
+  if (p.interleaved) {
+    if (!mine || e >= p.rot) return;
+    float c[4], s[4];
+    const float* t = angles + e / 2;
+    if (p.rot_vec) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(t)), b = __ldg(reinterpret_cast<const float4*>(t + half));
+      c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w; s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = e + 2 * i < p.rot;
+        c[i] = in ? __ldg(t + i) : 1.0f;
+        s[i] = in ? __ldg(t + half + i) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (e + 2 * i >= p.rot) continue;                 // unturned elements pass as they are
+      const R a = y[2 * i], b = y[2 * i + 1];
+      y[2 * i] = a * R(c[i]) - b * R(s[i]);
+      y[2 * i + 1] = b * R(c[i]) + a * R(s[i]);
+    }
+    return;
+  }
+
+  if (p.rot_vec) {                                      // rot / 2 is a multiple of 8: the other elements are one lane's eight
+    const bool turn = mine && e < p.rot, first = e < half;
+    const int from = turn ? (first ? lane + half / 8 : lane - half / 8) : lane;
+    uint4 u;
+    u.x = __shfl_sync(0xffffffffu, raw.x, from);
+    u.y = __shfl_sync(0xffffffffu, raw.y, from);
+    u.z = __shfl_sync(0xffffffffu, raw.z, from);
+    u.w = __shfl_sync(0xffffffffu, raw.w, from);
+    if (!turn) return;
+    widen8(u, x);
+    const int eo = first ? e + half : e - half;
+    if (o.w != nullptr) weights8(o.w, p.w_f32, p.w_vec, eo, w);
+    const float4* t = reinterpret_cast<const float4*>(angles + (first ? e : eo));
+    const float4* u4 = reinterpret_cast<const float4*>(angles + half + (first ? e : eo));
+    float c[8], s[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 a = __ldg(t + i), b = __ldg(u4 + i);
+      c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
+      s[4 * i] = b.x; s[4 * i + 1] = b.y; s[4 * i + 2] = b.z; s[4 * i + 3] = b.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const R other = o.w != nullptr ? R(x[i]) * r * R(w[i]) : R(x[i]);
+      y[i] = first ? y[i] * R(c[i]) - other * R(s[i]) : y[i] * R(c[i]) + other * R(s[i]);
+    }
+    return;
+  }
+  // Any even rot: the other elements one by one.
+  if (mine) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (e + i >= p.rot) continue;
+      const bool first = e + i < half;
+      const int eo = first ? e + i + half : e + i - half, a = first ? e + i : eo;
+      const float xo = __bfloat162float(*(o.x + at + eo));
+      const R other = o.w != nullptr ? R(xo) * r * R(weight1(o.w, p.w_f32, eo)) : R(xo);
+      const R c = R(__ldg(angles + a)), s = R(__ldg(angles + half + a));
+      y[i] = first ? y[i] * c - other * s : y[i] * c + other * s;
+    }
+  }
+}
+
+__device__ __forceinline__ const float* angles_of(const HeadsParams& p, int t, bool live) {
+  if (p.rot == 0 || !live) return p.cos_sin;
+  const int at = p.positions[t];
+  const int in = min(max(at, 0), p.n_pos - 1);
+  if (in != at) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+  return p.cos_sin + static_cast<size_t>(in) * p.rot;
+}
+
+// rint(x / s) exactly, ties to even, from the rounded product with 1 / s: the remainder decides (x - n s is exact: x has at
+// most 8 bits in R = float, and s has 4).
+template <typename R>
+__device__ __forceinline__ R divide_rint(R x, R s, R inverse) {
+  R n = rint(x * inverse);
+  const R rest = fma(-n, s, x), h = R(0.5) * s;
+  const bool odd = n * R(0.5) != rint(n * R(0.5));
+  if (rest > h || (rest == h && odd)) n += R(1);
+  else if (rest < -h || (rest == -h && odd)) n -= R(1);
+  return n;
+}
+
+// Eight elements of a group that four neighbouring lanes share -> a word of eight codes, and the group's (s, 16 z) byte pair.
+template <typename R>
+__device__ __forceinline__ uint32_t quantise8(const R (&y)[8], uint32_t& params) {
+  double lo = 0.0, hi = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { lo = fmin(lo, static_cast<double>(y[i])); hi = fmax(hi, static_cast<double>(y[i])); }
+#pragma unroll
+  for (int d = 1; d <= 2; d *= 2) {
+    lo = fmin(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+    hi = fmax(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+  }
+  const double step = (hi - lo) / 15.0;
+  // four significant bits, rounded up: a multiple of 2^(exponent - 3), at least of 2^-17
+  const int exponent = max(static_cast<int>((__double2hiint(step) >> 20) & 0x7ff) - 1023 - 3, -17);
+  const double up = __hiloint2double((1023 + exponent) << 20, 0), down = __hiloint2double((1023 - exponent) << 20, 0);
+  const double s = fmin(ceil(step * down) * up, 768.0);
+  params = 0;
+  if (s == 0.0) return 0;
+  const double inverse = 1.0 / s;
+  const double z = fmin(divide_rint<double>(-lo, s, inverse), 15.0);
+  params = (static_cast<uint32_t>(__half_as_ushort(__double2half(s))) >> 7) | (static_cast<uint32_t>(z) << 12);
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const R c = fmin(fmax(divide_rint<R>(y[i], static_cast<R>(s), static_cast<R>(inverse)) + static_cast<R>(z), R(0)), R(15));
+    word |= static_cast<uint32_t>(static_cast<int>(c)) << (4 * i);
+  }
+  return word;
+}
+
+template <int LPH, bool APPEND>
+__global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ HeadsParams p) {
+  constexpr int HPW = 32 / LPH;                          // heads of a warp
+  pdl_trigger();
+  pdl_wait();
+  const int n = p.n_valid != nullptr ? min(max(*p.n_valid, 0), p.T) : p.T;
+  const int lane = threadIdx.x & 31, e = (lane % LPH) * 8;
+  const int64_t warp = static_cast<int64_t>(blockIdx.x) * (blockDim.x / 32) + (threadIdx.x >> 5);
+  const int64_t k_warps = (static_cast<int64_t>(p.T) * p.Hkv + HPW - 1) / HPW;
+  const bool keys = warp < k_warps;                      // the keys, which take longest, begin first
+  const int H = keys ? p.Hkv : p.Hq;
+  if (H == 0) return;
+  const int64_t item = (keys ? warp : warp - k_warps) * HPW + lane / LPH;
+  const int64_t row = item / H;
+  const int h = static_cast<int>(item - row * H);
+  const bool live = row < n;
+  const int t = live ? static_cast<int>(row) : 0;
+  const Operand o = keys ? Operand{p.k, p.ld_k, p.hd_k, p.k_w, p.k_vec} : Operand{p.q, p.ld_q, p.hd_q, p.q_w, p.q_vec};
+  const size_t at = t * o.ld + h * o.hd;
+  const bool mine = live && e < p.D;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+
+  if (APPEND && keys) {
+    uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
+    const uint4 raw_v = mine ? load8(p.v + t * p.ld_v + h * p.hd_v + e, p.v_vec) : zero;
+    const int slot = live ? p.slots[t] : -1;
+    double y[8];
+    turned<LPH, double>(p, o, at, e, live, angles_of(p, t, live), raw, y);
+    float v[8];
+    widen8(raw_v, v);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (!isfinite(y[i])) { y[i] = 0.0; bad = true; }
+      if (!isfinite(v[i])) { v[i] = 0.0f; bad = true; }
+    }
+    const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
+    bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
+    uint32_t pk, pv;
+    const uint32_t wk = quantise8<double>(y, pk), wv = quantise8<float>(v, pv);
+    if (bad) pk |= kMarked;
+    if (!live) return;
+    if (slot < 0 || slot >= p.n_pages * p.page_size) {
+      if (slot >= 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+      return;
+    }
+    if (bad) atomicOr(p.status, TEMPO_STATUS_BAD_VALUE);
+    using U = CacheUnit<LPH * 8>;
+    const int page = slot / p.page_size, in_page = slot % p.page_size, in_unit = in_page % kUnit;
+    uint8_t* uk = p.cache + unit_offset<LPH * 8>(page, h, 0, in_page, p.Hkv, p.page_size);
+    uint8_t* uv = p.cache + unit_offset<LPH * 8>(page, h, 1, in_page, p.Hkv, p.page_size);
+    *reinterpret_cast<uint32_t*>(uk + in_unit * U::kKeyRow + e / 2) = wk;
+    uint16_t* pair = reinterpret_cast<uint16_t*>(uv + (in_unit / 2) * U::kPairRow + e) + (in_unit & 1);
+    pair[0] = static_cast<uint16_t>(wv);
+    pair[2] = static_cast<uint16_t>(wv >> 16);
+    if (e % kGroup == 0) {
+      *reinterpret_cast<uint16_t*>(uk + U::kCodes + in_unit * U::kKeyParams + e / kGroup * 2) = static_cast<uint16_t>(pk);
+      *reinterpret_cast<uint16_t*>(uv + U::kCodes + (in_unit / 2) * U::kPairParams + e / kGroup * 4 + (in_unit & 1) * 2) =
+          static_cast<uint16_t>(pv);
+    }
+    return;
+  }
+
+  const uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
+  float y[8];
+  turned<LPH, float>(p, o, at, e, live, angles_of(p, t, live), raw, y);
+  __syncwarp();                                          // in place: every load of the warp's heads comes before the stores
+  if (!mine) return;
+  if (keys) store8(p.k_out + t * p.ld_k_out + h * p.hd_k_out + e, y, p.k_out_vec);
+  else store8(p.q_out + t * p.ld_q_out + h * p.hd_q_out + e, y, p.q_out_vec);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ KvReadParams p) {
+  constexpr int LPH = D / 8;
+  using U = CacheUnit<D>;
+  pdl_trigger();
+  pdl_wait();
+  const int64_t item = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) / LPH;
+  const int e = (threadIdx.x % LPH) * 8;
+  const int64_t i = item / p.Hkv;
+  const int h = static_cast<int>(item - i * p.Hkv);
+  if (i >= p.n) return;
+  const int slot = p.slots[i];
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  if (slot >= 0 && slot < p.n_pages * p.page_size) {
+    const int page = slot / p.page_size, in_page = slot % p.page_size, in_unit = in_page % kUnit;
+    const uint8_t* uk = p.cache + unit_offset<D>(page, h, 0, in_page, p.Hkv, p.page_size);
+    const uint8_t* uv = p.cache + unit_offset<D>(page, h, 1, in_page, p.Hkv, p.page_size);
+    const uint16_t* pair = reinterpret_cast<const uint16_t*>(uv + (in_unit / 2) * U::kPairRow + e) + (in_unit & 1);
+    const uint32_t words[2] = {*reinterpret_cast<const uint32_t*>(uk + in_unit * U::kKeyRow + e / 2),
+                               pair[0] | (static_cast<uint32_t>(pair[2]) << 16)};
+    const uint32_t params[2] = {
+        *reinterpret_cast<const uint16_t*>(uk + U::kCodes + in_unit * U::kKeyParams + e / kGroup * 2),
+        *reinterpret_cast<const uint16_t*>(uv + U::kCodes + (in_unit / 2) * U::kPairParams + e / kGroup * 4 + (in_unit & 1) * 2)};
+    uint4* out[2] = {&k, &v};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      uint32_t s, b, pairs[4];
+      group_params(params[j] * 0x10001u, s, b);
+      decode8(words[j], s, b, pairs);                    // codes (n, n + 4)
+      *out[j] = make_uint4(__byte_perm(pairs[0], pairs[1], 0x5410), __byte_perm(pairs[2], pairs[3], 0x5410),
+                           __byte_perm(pairs[0], pairs[1], 0x7632), __byte_perm(pairs[2], pairs[3], 0x7632));
+    }
+  } else if (slot >= 0) {
+    atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+  }
+  const size_t at = (static_cast<size_t>(i) * p.Hkv + h) * D + e;
+  *reinterpret_cast<uint4*>(p.k + at) = k;
+  *reinterpret_cast<uint4*>(p.v + at) = v;
+}
+
+template <int LPH, bool APPEND>
+cudaError_t launch_heads_as(const HeadsParams& p, cudaStream_t stream) {
+  constexpr int HPW = 32 / LPH;
+  const int64_t warps = (static_cast<int64_t>(p.T) * p.Hkv + HPW - 1) / HPW + (static_cast<int64_t>(p.T) * p.Hq + HPW - 1) / HPW;
+  const int64_t blocks = (warps + 7) / 8;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  return launch_pdl(heads_kernel<LPH, APPEND>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_heads(const HeadsParams& p, bool append, cudaStream_t stream) {
+  if (append) return p.D == 64 ? launch_heads_as<8, true>(p, stream) : launch_heads_as<16, true>(p, stream);
+  if (p.D <= 64) return launch_heads_as<8, false>(p, stream);
+  if (p.D <= 128) return launch_heads_as<16, false>(p, stream);
+  return launch_heads_as<32, false>(p, stream);
+}
+
+cudaError_t launch_kv_read(const KvReadParams& p, int D, cudaStream_t stream) {
+  const int64_t blocks = (static_cast<int64_t>(p.n) * p.Hkv * (D / 8) + 255) / 256;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  return D == 64 ? launch_pdl(kv_read_kernel<64>, grid, dim3(256), 0, stream, p)
+                 : launch_pdl(kv_read_kernel<128>, grid, dim3(256), 0, stream, p);
+}
+
+}  // namespace tempo

@@ -1,5 +1,5 @@
 // Python module _marshal: argument marshalling of the calls whose kernels take a few microseconds (the norms, the router,
-// the few-token layer).  It checks tensors and calls the C entry points, nothing else; the Python wrappers in binding.py
+// the few-token layer, the attention half of a layer).  It checks tensors and calls the C entry points, nothing else; the Python wrappers in binding.py
 // document the arguments.  The addresses of the C functions and the exception class come from binding.py at import, so the
 // library that is called is the one it loaded.
 #include <Python.h>
@@ -22,6 +22,12 @@ decltype(&tempo_route) g_route = nullptr;
 decltype(&tempo_few_ffn) g_few[2] = {nullptr, nullptr};               // fp8, bf16 weights
 decltype(&tempo_few_workspace_bytes) g_few_bytes = nullptr;
 decltype(&tempo_packed_weight_bytes) g_packed_bytes[2] = {nullptr, nullptr};
+decltype(&tempo_qk_rotate) g_qk_rotate = nullptr;
+decltype(&tempo_kv_append) g_kv_append = nullptr;
+decltype(&tempo_kv_read) g_kv_read = nullptr;
+decltype(&tempo_attend) g_attend = nullptr;
+decltype(&tempo_cache_bytes) g_cache_bytes = nullptr;
+decltype(&tempo_attend_workspace_bytes) g_attend_bytes = nullptr;
 
 struct Refused : std::runtime_error { using std::runtime_error::runtime_error; };
 
@@ -278,12 +284,167 @@ PyObject* few(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// ---- the attention half of a layer ----
+
+// Sizes and pitches of a tensor [T, H, D] whose heads are contiguous; T, H or D below zero take the tensor's.
+struct Heads { void* at; int64_t ld, hd; };
+Heads heads(PyObject* o, const char* what, int32_t& T, int32_t& H, int32_t& D) {
+  const at::Tensor& t = tensor(o, what);
+  if (t.scalar_type() != at::kBFloat16) refuse(what, ": expected dtype ", at::kBFloat16, ", got ", t.scalar_type());
+  if (t.dim() != 3) refuse(what, ": expected 3 dimensions [T, heads, D], got ", t.sizes());
+  if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX || t.size(2) > INT32_MAX) refuse(what, ": shape ", t.sizes(), " is too large");
+  const int32_t s[3] = {static_cast<int32_t>(t.size(0)), static_cast<int32_t>(t.size(1)), static_cast<int32_t>(t.size(2))};
+  int32_t* const want[3] = {&T, &H, &D};
+  for (int i = 0; i < 3; ++i) {
+    if (*want[i] < 0) *want[i] = s[i];
+    else if (*want[i] != s[i]) refuse(what, ": expected shape [", T, ", ", H, ", ", D, "], got ", t.sizes());
+  }
+  if (D > 1 && t.stride(2) != 1) refuse(what, ": expected contiguous heads");
+  return {t.data_ptr(), t.stride(0), t.stride(1)};
+}
+
+struct Turn {                 // what qk_rotate and kv_append have in common
+  tempo_heads a{};
+  const void *q_w = nullptr, *k_w = nullptr, *positions = nullptr, *cos_sin = nullptr, *n_valid = nullptr;
+  void* status = nullptr;
+  void read(PyObject* q_w_o, PyObject* k_w_o, PyObject* positions_o, PyObject* cos_sin_o, PyObject* n_valid_o, PyObject* status_o) {
+    int f32 = -1;
+    q_w = param(q_w_o, "q_w", a.D, f32);
+    k_w = param(k_w_o, "k_w", a.D, f32);
+    a.w_f32 = f32 > 0;
+    n_valid = word(n_valid_o, "n_valid");
+    status = word(status_o, "status");
+    if (status == nullptr) refuse("status: expected a tensor");
+    if ((cos_sin_o == Py_None) != (positions_o == Py_None)) refuse("positions and cos_sin come together");
+    if (cos_sin_o == Py_None) return;
+    cos_sin = addr(cos_sin_o, at::kFloat, "cos_sin");
+    const at::Tensor& t = THPVariable_Unpack(cos_sin_o);
+    if (t.dim() != 2 || t.size(0) < 1 || t.size(0) > INT32_MAX || t.size(1) > a.D) refuse("cos_sin: expected shape [positions, at most ", a.D, "], got ", t.sizes());
+    a.n_pos = static_cast<int32_t>(t.size(0));
+    a.rot = static_cast<int32_t>(t.size(1));
+    positions = addr(positions_o, at::kInt, "positions");
+    holds(positions_o, a.T, "positions");
+  }
+};
+
+const tempo_cache* cache_at(PyObject* o) {
+  void* p = PyLong_AsVoidPtr(o);
+  if (p == nullptr && PyErr_Occurred()) throw Refused("");
+  return static_cast<const tempo_cache*>(p);
+}
+void* cache_of(PyObject* o, const tempo_cache* c) {
+  void* p = addr(o, at::kByte, "cache");
+  size_t bytes = 0;                                     // a shape that this refuses, the call refuses too
+  if (g_cache_bytes(c, &bytes) == TEMPO_OK) holds(o, static_cast<int64_t>(bytes), "cache");
+  return p;
+}
+
+// (q, k, positions, cos_sin, q_out, k_out, status, q_w, k_w, eps, interleaved, n_valid)
+PyObject* qk_rotate(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded(n, 12, [&]() -> int {
+    Turn t;
+    t.a.eps = number(v[9]);
+    t.a.interleaved = truth(v[10]);
+    void* stream = current_stream(v, n);
+    int32_t T = -1, Hq = -1, Hkv = -1, D = -1;
+    Heads q{}, k{}, qo{}, ko{};
+    if (v[0] != Py_None) { q = heads(v[0], "q", T, Hq, D); qo = heads(v[4], "q_out", T, Hq, D); }
+    if (v[1] != Py_None) { k = heads(v[1], "k", T, Hkv, D); ko = heads(v[5], "k_out", T, Hkv, D); }
+    if (T < 0) refuse("expected q, k or both");
+    t.a.T = T; t.a.Hq = Hq < 0 ? 0 : Hq; t.a.Hkv = Hkv < 0 ? 0 : Hkv; t.a.D = D;
+    t.a.ld_q = q.ld; t.a.hd_q = q.hd; t.a.ld_k = k.ld; t.a.hd_k = k.hd;
+    t.a.ld_q_out = qo.ld; t.a.hd_q_out = qo.hd; t.a.ld_k_out = ko.ld; t.a.hd_k_out = ko.hd;
+    t.read(v[7], v[8], v[2], v[3], v[11], v[6]);
+    return g_qk_rotate(&t.a, q.at, k.at, t.q_w, t.k_w, static_cast<const int32_t*>(t.positions), static_cast<const float*>(t.cos_sin),
+                       static_cast<const int32_t*>(t.n_valid), qo.at, ko.at, static_cast<uint32_t*>(t.status), stream);
+  });
+}
+
+// (cache shape address, k, v, slots, cache, status, k_w, positions, cos_sin, q, q_w, q_out, eps, interleaved, n_valid)
+PyObject* kv_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded(n, 15, [&]() -> int {
+    const tempo_cache* c = cache_at(v[0]);
+    Turn t;
+    t.a.eps = number(v[12]);
+    t.a.interleaved = truth(v[13]);
+    void* stream = current_stream(v, n);
+    int32_t T = -1, Hq = -1, Hkv = -1, D = -1;
+    const Heads k = heads(v[1], "k", T, Hkv, D), x = heads(v[2], "v", T, Hkv, D);
+    Heads q{}, qo{};
+    if (v[9] != Py_None) { q = heads(v[9], "q", T, Hq, D); qo = heads(v[11], "q_out", T, Hq, D); }
+    t.a.T = T; t.a.Hq = Hq < 0 ? 0 : Hq; t.a.Hkv = Hkv; t.a.D = D;
+    t.a.ld_q = q.ld; t.a.hd_q = q.hd; t.a.ld_k = k.ld; t.a.hd_k = k.hd; t.a.ld_v = x.ld; t.a.hd_v = x.hd;
+    t.a.ld_q_out = qo.ld; t.a.hd_q_out = qo.hd;
+    t.read(v[10], v[6], v[7], v[8], v[14], v[5]);
+    void* slots = addr(v[3], at::kInt, "slots");
+    holds(v[3], T, "slots");
+    void* cache = cache_of(v[4], c);
+    return g_kv_append(&t.a, c, q.at, k.at, x.at, t.q_w, t.k_w, static_cast<const int32_t*>(t.positions),
+                       static_cast<const float*>(t.cos_sin), static_cast<const int32_t*>(slots), static_cast<const int32_t*>(t.n_valid),
+                       qo.at, cache, static_cast<uint32_t*>(t.status), stream);
+  });
+}
+
+// (cache shape address, cache, slots, k_out, v_out, status)
+PyObject* kv_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> int {
+    const tempo_cache* c = cache_at(v[0]);
+    void* stream = current_stream(v, n);
+    void* cache = cache_of(v[1], c);
+    void* slots = addr(v[2], at::kInt, "slots");
+    void* k = addr(v[3], at::kHalf, "k_out");
+    void* x = addr(v[4], at::kHalf, "v_out");
+    void* status = word(v[5], "status");
+    const int64_t rows = slots == nullptr ? 0 : THPVariable_Unpack(v[2]).numel();
+    if (rows > INT32_MAX) refuse("slots: too many rows");
+    if (c != nullptr && c->Hkv > 0 && c->D > 0) {
+      holds(v[3], rows * c->Hkv * c->D, "k_out");
+      holds(v[4], rows * c->Hkv * c->D, "v_out");
+    }
+    return g_kv_read(c, cache, static_cast<const int32_t*>(slots), static_cast<int32_t>(rows), k, x, static_cast<uint32_t*>(status), stream);
+  });
+}
+
+// (cache shape address, q, cache, page_table, lens, out, status, workspace, scale, q_start, max_q)
+PyObject* attend(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> int {
+    const tempo_cache* c = cache_at(v[0]);
+    tempo_attention a{};
+    a.scale = number(v[8]);
+    a.max_q = integer(v[10]);
+    void* stream = current_stream(v, n);
+    int32_t T = -1, Hq = -1, D = c == nullptr ? -1 : c->D;
+    const Heads q = heads(v[1], "q", T, Hq, D), out = heads(v[5], "out", T, Hq, D);
+    void* cache = cache_of(v[2], c);
+    void* table = addr(v[3], at::kInt, "page_table");
+    void* lens = addr(v[4], at::kInt, "lens");
+    void* status = word(v[6], "status");
+    void* workspace = addr(v[7], at::kByte, "workspace");
+    void* q_start = addr(v[9], at::kInt, "q_start");
+    if (table == nullptr || lens == nullptr) refuse("page_table and lens: expected tensors");
+    const at::Tensor& pt = THPVariable_Unpack(v[3]);
+    if (pt.dim() != 2 || pt.size(0) > INT32_MAX || pt.size(1) > INT32_MAX) refuse("page_table: expected shape [sequences, pages], got ", pt.sizes());
+    a.B = static_cast<int32_t>(pt.size(0));
+    a.max_pages = static_cast<int32_t>(pt.size(1));
+    holds(v[4], a.B, "lens");
+    holds(v[9], static_cast<int64_t>(a.B) + 1, "q_start");
+    a.T = T; a.Hq = Hq;
+    a.ld_q = q.ld; a.hd_q = q.hd; a.ld_out = out.ld; a.hd_out = out.hd;
+    size_t bytes = 0;
+    if (g_attend_bytes(c, Hq, &bytes) == TEMPO_OK) holds(v[7], static_cast<int64_t>(bytes), "workspace");
+    return g_attend(&a, c, q.at, cache, static_cast<const int32_t*>(table), static_cast<const int32_t*>(lens),
+                    static_cast<const int32_t*>(q_start), out.at, static_cast<uint32_t*>(status), workspace, stream);
+  });
+}
+
 // (exception class, address of each C function below)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
   void** const at[] = {reinterpret_cast<void**>(&g_norm_in), reinterpret_cast<void**>(&g_norm_out), reinterpret_cast<void**>(&g_route),
                        reinterpret_cast<void**>(&g_few[0]), reinterpret_cast<void**>(&g_few[1]),
                        reinterpret_cast<void**>(&g_few_bytes), reinterpret_cast<void**>(&g_packed_bytes[0]),
-                       reinterpret_cast<void**>(&g_packed_bytes[1])};
+                       reinterpret_cast<void**>(&g_packed_bytes[1]), reinterpret_cast<void**>(&g_qk_rotate),
+                       reinterpret_cast<void**>(&g_kv_append), reinterpret_cast<void**>(&g_kv_read), reinterpret_cast<void**>(&g_attend),
+                       reinterpret_cast<void**>(&g_cache_bytes), reinterpret_cast<void**>(&g_attend_bytes)};
   constexpr Py_ssize_t want = 1 + sizeof(at) / sizeof(at[0]);
   if (n != want) return PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
   for (Py_ssize_t i = 1; i < want; ++i) {
@@ -298,6 +459,7 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 
 #define TEMPO_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TEMPO_METHOD(bind), TEMPO_METHOD(norm_in), TEMPO_METHOD(norm_out), TEMPO_METHOD(route), TEMPO_METHOD(few),
+                         TEMPO_METHOD(qk_rotate), TEMPO_METHOD(kv_append), TEMPO_METHOD(kv_read), TEMPO_METHOD(attend),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the few-microsecond calls (built for " TEMPO_BUILT_FOR ").", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -210,4 +210,63 @@ struct FewParams {
 FewLayout few_layout(int T, int k, int G, int d, int f, int num_sms);
 cudaError_t launch_few(const FewParams& p, bool bf16, int num_sms, cudaStream_t stream);
 
+// ---- the attention half of a layer ---------------------------------------------------------------------
+struct HeadsParams {
+  int T, Hq, Hkv, D, rot, interleaved, n_pos, w_f32;
+  bool q_vec, k_vec, v_vec, q_out_vec, k_out_vec, w_vec;   // eight elements can be read or written as 16 bytes
+  bool rot_vec;              // a lane's eight elements turn with one other lane's (or among themselves), angles in 16-byte loads
+  const __nv_bfloat16* q;
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
+  const void* q_w;
+  const void* k_w;
+  const int32_t* positions;
+  const float* cos_sin;
+  const int32_t* n_valid;
+  __nv_bfloat16* q_out;
+  __nv_bfloat16* k_out;
+  size_t ld_q, hd_q, ld_k, hd_k, ld_v, hd_v, ld_q_out, hd_q_out, ld_k_out, hd_k_out;
+  float eps;
+  uint32_t* status;
+  int n_pages, page_size;    // append only, as all below
+  const int32_t* slots;
+  uint8_t* cache;
+};
+cudaError_t launch_heads(const HeadsParams& p, bool append, cudaStream_t stream);
+
+struct KvReadParams {
+  int n, n_pages, page_size, Hkv;
+  const uint8_t* cache;
+  const int32_t* slots;
+  __half* k;
+  __half* v;
+  uint32_t* status;
+};
+cudaError_t launch_kv_read(const KvReadParams& p, int D, cudaStream_t stream);
+
+constexpr int kAttendMaxB = 2048;
+constexpr int kAttendMaxSms = 160;   // the workspace is sized for so many CTAs, whatever the device
+struct AttendLayout {
+  size_t off_counters, off_stats, off_out, total;
+};
+AttendLayout attend_layout(int D);
+struct AttendParams {
+  int B, T, Hkv, group;      // group: query heads of a key head
+  int max_pages, page_size, n_pages;
+  const __nv_bfloat16* q;
+  const uint8_t* cache;
+  const int32_t* page_table;
+  const int32_t* lens;
+  const int32_t* q_start;
+  __nv_bfloat16* out;
+  size_t ld_q, hd_q, ld_out, hd_out;
+  float scale_log2;          // scale * log2(e)
+  uint32_t* status;
+  unsigned int* counters;    // arrivals of the CTAs that share an item, by the first of them; zero between calls
+  float* stats;              // [CTA][2][rows][2]: maximum and sum of a part of an item
+  float* part;               // [CTA][2][rows][D]
+  unsigned long long wait_ns;
+};
+cudaError_t launch_attend(const AttendParams& p, int D, int num_sms, cudaStream_t stream);
+
 }  // namespace tempo
