@@ -675,7 +675,9 @@ static int run_heads(const tempo_heads* a, const tempo_cache* c, const void* q, 
   if (append) {
     p.n_pages = c->n_pages; p.page_size = c->page_size; p.slots = slots; p.cache = static_cast<uint8_t*>(cache);
   }
-  return launch_heads(p, append, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+  const int sms = sm_count();
+  if (sms <= 0) return TEMPO_ERR_CUDA;
+  return launch_heads(p, append, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
 }
 
 int tempo_qk_rotate(const tempo_heads* a, const void* q, const void* k, const void* q_w, const void* k_w, const int32_t* positions,
@@ -724,6 +726,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   if (a->B <= 0 || a->T <= 0 || a->Hq <= 0 || a->Hq % c->Hkv || a->max_pages <= 0 || a->max_q <= 0 || (!q_start && a->B != a->T))
     return TEMPO_ERR_SHAPE;
   if (!pitches(a->ld_q, a->hd_q) || !apart(a->ld_out, a->hd_out, a->T, a->Hq, c->D)) return TEMPO_ERR_SHAPE;
+  if (!(a->scale > -1e30f && a->scale < 1e30f)) return TEMPO_ERR_UNSUPPORTED;
   if (a->B > kAttendMaxB || a->Hq > 65536 || static_cast<long long>(a->max_pages) * c->page_size > 0x7fffff00ll ||
       static_cast<long long>(a->T) * (a->Hq / c->Hkv) > 0x7fffff00ll)
     return TEMPO_ERR_UNSUPPORTED;
@@ -737,6 +740,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   AttendParams p{};
   p.B = a->B; p.T = a->T; p.Hkv = c->Hkv; p.group = a->Hq / c->Hkv;
   p.max_pages = a->max_pages; p.page_size = c->page_size; p.n_pages = c->n_pages;
+  while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
   p.q = static_cast<const __nv_bfloat16*>(q); p.cache = static_cast<const uint8_t*>(cache);
   p.page_table = page_table; p.lens = lens; p.q_start = q_start; p.out = static_cast<__nv_bfloat16*>(out);
   p.ld_q = a->ld_q; p.hd_q = a->hd_q; p.ld_out = a->ld_out; p.hd_out = a->hd_out;

@@ -23,57 +23,69 @@ namespace tempo {
 
 namespace {
 
-constexpr int kWarps = 12, kTile = 32, kRows = 16;
+constexpr int kWarps = 8, kTile = 64, kUnits = kTile / kUnit, kRows = 16;
 constexpr float kBias = 7.0f, kSlack = 8.0f;      // weights are 2^(x - m + 7); m is raised once x exceeds it by more than 8
 
 struct Item {                 // rows [row0, row0 + 16) of a sequence and key head, and its tiles
-  int64_t begin;              // number of its first tile in the launch
-  int tiles, b, h, row0;
+  int begin, tiles;           // number of its first tile in the launch
+  int b, h, row0;
   int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
 };
 
-struct Span { int len, q0, n; };
-__device__ __forceinline__ Span span_of(const AttendParams& p, int b, bool tell) {
-  Span s;
-  const int len = p.lens[b], most = p.max_pages * p.page_size;
-  s.len = min(max(len, 0), most);
-  int q0 = b, q1 = b + 1;
-  if (p.q_start != nullptr) { q0 = p.q_start[b]; q1 = p.q_start[b + 1]; }
-  s.q0 = min(max(q0, 0), p.T);
-  s.n = max(min(max(q1, 0), p.T) - s.q0, 0);
-  if (tell && (s.len != len || s.q0 != q0 || s.q0 + s.n != q1)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
-  return s;
+__device__ __forceinline__ void span_of(const AttendParams& p, int b, int& len, int& q0, int& n, bool tell = false) {
+  const int given = p.lens[b];
+  len = min(max(given, 0), p.max_pages << p.page_shift);
+  int from = b, to = b + 1;
+  if (p.q_start != nullptr) { from = p.q_start[b]; to = p.q_start[b + 1]; }
+  q0 = min(max(from, 0), p.T);
+  n = max(min(max(to, 0), p.T) - q0, 0);
+  if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
 }
 
 // Tiles that the rows [row0, row0 + 16) see: at least one, so that rows without a token are written too.
-__device__ __forceinline__ int tiles_of(const AttendParams& p, const Span& s, int row0) {
-  const int last = min(row0 + kRows, s.n * p.group) - 1;
-  const int seen = s.len - s.n + last / p.group + 1;
+__device__ __forceinline__ int tiles_of(int len, int n, int group, int row0) {
+  const int last = min(row0 + kRows, n * group) - 1;
+  const int seen = len - n + last / group + 1;
   return max(1, (seen + kTile - 1) / kTile);
 }
 
-__device__ __forceinline__ Item item_at(const AttendParams& p, const int64_t* before, int64_t x) {
+// The item of tile x.  before[b]: tiles before sequence b.
+__device__ __forceinline__ Item item_at(const AttendParams& p, const int* before, int x) {
   int lo = 0, hi = p.B - 1;
-  while (lo < hi) {                                  // the last sequence with before[b] <= x and tiles
+  while (lo < hi) {                                  // the last sequence with before[b] <= x: the one that has tile x
     const int mid = (lo + hi + 1) >> 1;
     if (before[mid] <= x) lo = mid; else hi = mid - 1;
   }
   Item it;
-  const Span s = span_of(p, lo, false);
-  it.b = lo; it.len = s.len; it.q0 = s.q0; it.n = s.n;
-  const int64_t per_head = (before[lo + 1] - before[lo]) / p.Hkv;
-  int64_t rest = x - before[lo];
-  it.h = static_cast<int>(rest / per_head);
+  it.b = lo;
+  span_of(p, lo, it.len, it.q0, it.n);
+  const int per_head = (before[lo + 1] - before[lo]) / p.Hkv;
+  int rest = x - before[lo];
+  it.h = rest / per_head;
   rest -= it.h * per_head;
   it.row0 = 0;
   for (;;) {
-    it.tiles = tiles_of(p, s, it.row0);
+    it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
     if (rest < it.tiles) break;
     rest -= it.tiles;
     it.row0 += kRows;
   }
   it.begin = x - rest;
   return it;
+}
+
+// The one behind it (there is one: the caller has a tile left).
+__device__ __forceinline__ void next_item(const AttendParams& p, Item& it) {
+  it.begin += it.tiles;
+  it.row0 += kRows;
+  if (it.row0 >= it.n * p.group) {
+    it.row0 = 0;
+    if (++it.h == p.Hkv) {
+      it.h = 0;
+      do span_of(p, ++it.b, it.len, it.q0, it.n); while (it.n == 0);
+    }
+  }
+  it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
 }
 
 struct Part {                 // a cut item's share of one warp
@@ -83,7 +95,7 @@ struct Part {                 // a cut item's share of one warp
 
 template <int D>
 struct AttendSmem {
-  static constexpr int kStageBytes = 2 * 2 * CacheUnit<D>::kBytes;   // keys and values of two units
+  static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // keys and values of each unit
   static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
@@ -92,37 +104,27 @@ struct AttendSmem {
   static constexpr int kBefore = kRecords + kWarps * 2 * static_cast<int>(sizeof(Part));
   static_assert(kRing >= kWarps * kPart, "the second parts take the ring's place");
   static_assert(kRing >= kAttendMaxSms * kRows * 4 + kRows * 4, "so do the weights of a join");
-  static int bytes(int B) { return kBefore + (B + 1) * 8; }
+  static int bytes(int B) { return kBefore + (B + 1) * 4; }
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void lds64(uint32_t a, uint32_t (&v)[2]) {
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t lds16(uint32_t a) {
-  uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-  return v;
-}
 template <int W>
-__device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&v)[W]) {
-  if constexpr (W == 4) lds128(a, v); else lds64(a, v);
+__device__ __forceinline__ void load_words(const uint8_t* a, uint32_t (&v)[W]) {
+  if constexpr (W == 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(a);
+    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(a);
+    v[0] = u.x; v[1] = u.y;
+  }
 }
 
 // Float4 number q (of D / 4) of a row in a part: rotated so that the eight lanes of a store's phase meet eight bank groups.
@@ -133,9 +135,10 @@ template <int D>
 struct Running {
   static constexpr int kN = D / 8;                   // 8-column tiles of O
   uint32_t q[D / 16][4];                             // A operands: rows lane / 4 and + 8
-  float f[2];                                        // score = f * (sum of products), in units of log2
+  float f[2];                                        // score = f * (sum of products), in units of log2; above zero
   int limit[2], least;                               // last token that each row sees; the least over the 16 rows
-  float m[2], l[2];
+  float m[2];
+  float l[4];                                        // the sums of the weights, one more column of O: rows in l[0] and l[2]
   float o[kN][4];
 };
 
@@ -170,10 +173,11 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
       odd = __shfl_xor_sync(0xffffffffu, static_cast<int>(odd), d) != 0 || odd;
     }
-    // the row times a power of two, its largest element in [256, 512): fp16 holds 2^-33 of it
+    // the row times a power of two (and the scale's sign), its largest element in [256, 512): fp16 holds 2^-33 of it
     const int e = top > 0.0f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -110), 119) : 0;
-    const float up = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    s.f[half] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.scale_log2;
+    const float up = odd ? __uint_as_float(0x7fc00000u)
+                         : __uint_as_float((static_cast<uint32_t>(127 - e) << 23) | (__float_as_uint(p.scale_log2) & 0x80000000u));
+    s.f[half] = fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * fabsf(p.scale_log2), 1.2e-38f);
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
@@ -182,63 +186,62 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it
         s.q[2 * w + u][half + 2] = as_u32(__floats2half2_rn(x[w][2 * u + 1] * up, x[w][2 * u + 5] * up));
       }
     s.m[half] = -INFINITY;
-    s.l[half] = 0.0f;
   }
   s.least = it.len - it.n + it.row0 / p.group;
+  s.l[0] = s.l[1] = s.l[2] = s.l[3] = 0.0f;
 #pragma unroll
   for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][0] = s.o[i][1] = s.o[i][2] = s.o[i][3] = 0.0f; }
 }
 
-// One tile: tokens [t0, t0 + 32) of the item at `stage`.  `absent`: bits of its two units whose page is not in the cache.
+// One tile: tokens [t0, t0 + 64) of the item at `stage`.  `absent`: bits of its units whose page is not in the cache.
 template <int D>
-__device__ __forceinline__ void run_tile(Running<D>& s, uint32_t stage, int t0, int len, uint32_t absent) {
+__device__ __forceinline__ void run_tile(Running<D>& s, const uint8_t* stage, int t0, int len, uint32_t absent) {
   using U = CacheUnit<D>;
-  constexpr int W = D / 32;
+  constexpr int W = D / 32, kCols = kTile / 8;
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  float c[4][4];
+  float c[kCols][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {                      // scores of the tokens 8 i to 8 i + 7
-    c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.0f;
-    const uint32_t unit = stage + (i / 2) * 2 * U::kBytes;
-    const int at = (i & 1) * 8 + g;
-    uint32_t w[W];
-    lds_words<W>(unit + at * U::kKeyRow + j * (D / 8), w);
-    const uint32_t params = lds16(unit + U::kCodes + at * U::kKeyParams + (D == 128 ? j : j / 2) * 2) * 0x10001u;
-    uint32_t sc, b;
-    group_params(params, sc, b);
+  for (int k = 0; k < kUnits; ++k) {                 // scores of unit k: two chains of matrix instructions side by side
+    const uint8_t* unit = stage + k * 2 * U::kBytes;
+    uint32_t w[2][W], sc[2], b[2];
 #pragma unroll
-    for (int x = 0; x < W; ++x) {
-      uint32_t v[4];
-      decode8(w[x], sc, b, v);
-      mma_f16(c[i], s.q[2 * x], v[0], v[1]);
-      mma_f16(c[i], s.q[2 * x + 1], v[2], v[3]);
+    for (int x = 0; x < 2; ++x) {
+      c[2 * k + x][0] = c[2 * k + x][1] = c[2 * k + x][2] = c[2 * k + x][3] = 0.0f;
+      const int at = x * 8 + g;
+      load_words<W>(unit + at * U::kKeyRow + j * (D / 8), w[x]);
+      group_params(*reinterpret_cast<const uint16_t*>(unit + U::kCodes + at * U::kKeyParams + (D == 128 ? j : j / 2) * 2) * 0x10001u, sc[x], b[x]);
+    }
+#pragma unroll
+    for (int y = 0; y < W; ++y) {
+      uint32_t v[2][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) decode8(w[x][y], sc[x], b[x], v[x]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) mma_f16(c[2 * k + x], s.q[2 * y + u], v[x][2 * u], v[x][2 * u + 1]);
     }
   }
   if (absent != 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kCols; ++i)
       if (absent >> (i / 2) & 1) c[i][0] = c[i][1] = c[i][2] = c[i][3] = __uint_as_float(0x7fc00000u);
   }
-  float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) c[i][x] *= s.f[x / 2];
   if (t0 + kTile - 1 > s.least) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kCols; ++i)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         if (t0 + 8 * i + 2 * j + (x & 1) > s.limit[x / 2]) c[i][x] = -INFINITY;
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) top[x / 2] = fmaxf(top[x / 2], c[i][x]);
+  float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) top[r] = fmaxf(top[r], fmaxf(c[i][2 * r], c[i][2 * r + 1]));
     top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
     top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+    top[r] *= s.f[r];
   }
   // a maximum that has grown little stays: weights up to 2^15 are in fp16's range, and O is left alone
   if (__any_sync(0xffffffffu, top[0] > s.m[0] + kSlack || top[1] > s.m[1] + kSlack)) {
@@ -247,54 +250,42 @@ __device__ __forceinline__ void run_tile(Running<D>& s, uint32_t stage, int t0, 
       const float m = top[r] > s.m[r] + kSlack ? top[r] : s.m[r];
       const float k = m == s.m[r] ? 1.0f : exp2_fast(s.m[r] - m);
       s.m[r] = m;
-      s.l[r] *= k;
+      s.l[2 * r] *= k;
 #pragma unroll
       for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][2 * r] *= k; s.o[i][2 * r + 1] *= k; }
     }
   }
-  uint32_t a[2][4];
+  uint32_t a[kUnits][4];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    const float m = s.m[r] == -INFINITY ? 0.0f : s.m[r] - kBias;
+    const float m = s.m[r] == -INFINITY ? 0.0f : kBias - s.m[r];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __half2 w = __floats2half2_rn(exp2_fast(c[i][2 * r] - m), exp2_fast(c[i][2 * r + 1] - m));
-      a[i / 2][(i & 1) * 2 + r] = as_u32(w);
-      const float2 back = __half22float2(w);         // the sum is that of the weights as they meet V
-      s.l[r] += back.x + back.y;
-    }
+    for (int i = 0; i < kCols; ++i)
+      a[i / 2][(i & 1) * 2 + r] =
+          as_u32(__floats2half2_rn(exp2_fast(fmaf(c[i][2 * r], s.f[r], m)), exp2_fast(fmaf(c[i][2 * r + 1], s.f[r], m))));
   }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {                      // unit k: tokens 16 k + 2 j, + 1 and 16 k + 8 + 2 j, + 1
-    const uint32_t unit = stage + (k * 2 + 1) * U::kBytes;
+  for (int k = 0; k < kUnits; ++k) {                 // unit k: tokens 16 k + 2 j, + 1 and 16 k + 8 + 2 j, + 1
+    const uint8_t* unit = stage + (k * 2 + 1) * U::kBytes;
     uint32_t w[2][W], sc[2], b[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int pair = 4 * x + j;
-      lds_words<W>(unit + pair * U::kPairRow + g * (D / 8), w[x]);
-      uint32_t params = lds32(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4);
+      load_words<W>(unit + pair * U::kPairRow + g * (D / 8), w[x]);
+      uint32_t params = *reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4);
       const int left = len - (t0 + 16 * k + 2 * pair);           // tokens of the pair that exist: what lies behind may be anything
       if (left < 2) params &= left == 1 ? 0xffffu : 0u;
       group_params(params, sc[x], b[x]);
     }
+    mma_f16(s.l, a[k], 0x3c003c00u, 0x3c003c00u);    // times 1: the sum is that of the weights as they meet V
 #pragma unroll
-    for (int x = 0; x < W; ++x) {
+    for (int y = 0; y < W; ++y) {
       uint32_t v0[4], v1[4];
-      decode8(w[0][x], sc[0], b[0], v0);
-      decode8(w[1][x], sc[1], b[1], v1);
+      decode8(w[0][y], sc[0], b[0], v0);
+      decode8(w[1][y], sc[1], b[1], v1);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) mma_f16(s.o[4 * x + n], a[k], v0[n], v1[n]);
+      for (int n = 0; n < 4; ++n) mma_f16(s.o[4 * y + n], a[k], v0[n], v1[n]);
     }
-  }
-}
-
-// Sums over the four lanes of a row.
-template <int D>
-__device__ __forceinline__ void close_sums(Running<D>& s) {
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    s.l[r] += __shfl_xor_sync(0xffffffffu, s.l[r], 1);
-    s.l[r] += __shfl_xor_sync(0xffffffffu, s.l[r], 2);
   }
 }
 
@@ -308,11 +299,10 @@ __device__ __forceinline__ __nv_bfloat16* out_row(const AttendParams& p, const I
 template <int D>
 __device__ __forceinline__ void store_item(const AttendParams& p, const Item& it, Running<D>& s) {
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  close_sums(s);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (it.row0 + g + 8 * r >= it.n * p.group) continue;
-    const float k = s.l[r] == 0.0f ? 0.0f : 1.0f / s.l[r];
+    const float k = s.l[2 * r] == 0.0f ? 0.0f : 1.0f / s.l[2 * r];
     uint4* dst = reinterpret_cast<uint4*>(out_row(p, it, g + 8 * r) + j * (D / 4));
 #pragma unroll
     for (int y = 0; y < 2; ++y)
@@ -332,13 +322,12 @@ __device__ __forceinline__ void store_item(const AttendParams& p, const Item& it
 template <int D>
 __device__ __forceinline__ void keep_part(Running<D>& s, uint8_t* part) {
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  close_sums(s);
   float4* o = reinterpret_cast<float4*>(part);
   float2* stat = reinterpret_cast<float2*>(part + kRows * D * 4);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     const int row = g + 8 * r;
-    if (j == 0) stat[row] = make_float2(s.m[r], s.l[r]);
+    if (j == 0) stat[row] = make_float2(s.m[r], s.l[2 * r]);
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -366,14 +355,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   extern __shared__ __align__(128) uint8_t smem[];
   using S = AttendSmem<D>;
   using U = CacheUnit<D>;
-  __shared__ int64_t warp_sum[kWarps];
+  __shared__ int warp_sum[kWarps];
   __shared__ Segment segments[kWarps + 1];
   __shared__ int n_segments, abort_flag;
-  int64_t* before = reinterpret_cast<int64_t*>(smem + S::kBefore);
+  int* before = reinterpret_cast<int*>(smem + S::kBefore);
   Part* records = reinterpret_cast<Part*>(smem + S::kRecords);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bars = smem_u32(smem + S::kBars) + warp * S::kStages * 8;
-  const uint32_t ring = smem_u32(smem) + warp * S::kStages * S::kStageBytes;
+  const uint8_t* ring = smem + warp * S::kStages * S::kStageBytes;
 
   pdl_trigger();
   if (lane < S::kStages) mbar_init(bars + 8 * lane, 1);
@@ -383,27 +372,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   pdl_wait();
 
   // tiles before each sequence
-  int64_t total = 0;
+  int total = 0;
   for (int b0 = 0; b0 < p.B; b0 += kWarps * 32) {
     const int b = b0 + tid;
-    int64_t mine = 0;
+    int mine = 0;
     if (b < p.B) {
-      const Span s = span_of(p, b, blockIdx.x == 0);
-      for (int row0 = 0; row0 < s.n * p.group; row0 += kRows) mine += tiles_of(p, s, row0);
+      int len, q0, n;
+      span_of(p, b, len, q0, n, blockIdx.x == 0);
+      for (int row0 = 0; row0 < n * p.group; row0 += kRows) mine += tiles_of(len, n, p.group, row0);
       mine *= p.Hkv;
     }
-    int64_t run = mine;
+    int run = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, run, d);
+      const int up = __shfl_up_sync(0xffffffffu, run, d);
       if (lane >= d) run += up;
     }
     if (lane == 31) warp_sum[warp] = run;
     __syncthreads();
-    int64_t base = total;
+    int base = total;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) base += warp_sum[w];
-      total += warp_sum[w];
+      const int v = warp_sum[w];
+      if (w < warp) base += v;
+      total += v;
     }
     if (b < p.B) before[b + 1] = base + run;
     if (b == 0) before[0] = 0;
@@ -411,70 +403,78 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   }
   if (total == 0) return;
 
-  const int64_t runs = min(total, static_cast<int64_t>(gridDim.x) * kWarps);
-  const auto run_begin = [&](int64_t r) { return r * total / runs; };
-  const auto run_of = [&](int64_t x) { return ((x + 1) * runs - 1) / total; };
-  const int64_t run0 = static_cast<int64_t>(blockIdx.x) * kWarps;
+  // Equal runs: the first `longer` of them have one tile more.
+  const int runs = min(total, static_cast<int>(gridDim.x) * kWarps);
+  const int quota = total / runs, longer = total - quota * runs;
+  const auto run_begin = [&](int r) { return r * quota + min(r, longer); };
+  const auto run_of = [&](int x) { return x < longer * (quota + 1) ? x / (quota + 1) : longer + (x - longer * (quota + 1)) / quota; };
+  const int run0 = blockIdx.x * kWarps;
   if (run0 >= runs) return;
-  const int64_t cta_begin = run_begin(run0), cta_end = run_begin(min(run0 + kWarps, runs));
+  const int cta_begin = run_begin(run0), cta_end = run_begin(min(run0 + kWarps, runs));
 
   if (run0 + warp < runs) {
-    const int64_t begin = run_begin(run0 + warp), end = run_begin(run0 + warp + 1);
-    Item ahead = item_at(p, before, begin);          // the item of the next tile to be requested
-    int64_t asked = begin;
-    uint32_t absent_bits = 0;                        // two bits per stage
+    const int begin = run_begin(run0 + warp), end = run_begin(run0 + warp + 1);
+    Item it = item_at(p, before, begin);
+    Item ahead = it;                                 // the item of the next tile to be requested
+    int asked = begin;
+    uint32_t absent_bits = 0;                        // four bits per stage
+    // Lanes 0 to 7 each fetch one unit's keys or values.  The page numbers are read one request ahead.
+    const int my_unit = lane >> 1;
+    const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
+    const auto look = [&](int tile) {                // tile of the item `ahead`
+      const int t = tile * kTile + my_unit * kUnit;
+      return lane < 2 * kUnits && t < ahead.len ? p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + (t >> p.page_shift)] : -1;
+    };
+    int page = look(asked - ahead.begin);
     const auto request = [&](int stage) {
-      if (asked >= ahead.begin + ahead.tiles) ahead = item_at(p, before, asked);
-      const int unit = static_cast<int>(asked - ahead.begin) * 2 + (lane >> 1);     // lanes 0 to 3: (unit, keys or values)
-      const bool wanted = lane < 4 && unit * kUnit < ahead.len;
-      int page = 0;
-      bool there = true;
-      if (wanted) {
-        page = p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + unit * kUnit / p.page_size];
-        there = page >= 0 && page < p.n_pages;
-        if (!there) { page = 0; atomicOr(p.status, TEMPO_STATUS_BAD_INDEX); }
+      const int tile = asked - ahead.begin, t = tile * kTile + my_unit * kUnit;
+      const bool wanted = lane < 2 * kUnits && t < ahead.len;
+      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
+      const uint8_t* src = p.cache + ((static_cast<size_t>(there ? page : 0) * p.Hkv + ahead.h) * 2 + (lane & 1)) * head_bytes +
+                           ((t & (p.page_size - 1)) / kUnit) * U::kBytes;
+      const uint32_t want = __ballot_sync(0xffffffffu, wanted), gone = __ballot_sync(0xffffffffu, wanted && !there);
+      if (gone != 0 || absent_bits != 0) {
+        const uint32_t bits = (gone & 1u) | (gone >> 1 & 2u) | (gone >> 2 & 4u) | (gone >> 3 & 8u);
+        absent_bits = (absent_bits & ~(15u << (4 * stage))) | bits << (4 * stage);
+        if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
-      const uint32_t want = __ballot_sync(0xffffffffu, wanted), gone = __ballot_sync(0xffffffffu, !there);
-      absent_bits = (absent_bits & ~(3u << (2 * stage))) | ((gone & 1u) | (gone >> 1 & 2u)) << (2 * stage);
       if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, __popc(want) * U::kBytes);
       __syncwarp();
-      if (wanted)
-        bulk_load(ring + stage * S::kStageBytes + lane * U::kBytes,
-                  p.cache + unit_offset<D>(page, ahead.h, lane & 1, unit * kUnit % p.page_size, p.Hkv, p.page_size), U::kBytes,
-                  bars + 8 * stage);
-      ++asked;
+      if (wanted) bulk_load(smem_u32(ring + stage * S::kStageBytes + lane * U::kBytes), src, U::kBytes, bars + 8 * stage);
+      if (++asked < end) {
+        if (asked == ahead.begin + ahead.tiles) next_item(p, ahead);
+        page = look(asked - ahead.begin);
+      }
     };
+#pragma unroll 1
     for (int st = 0; st < S::kStages && asked < end; ++st) request(st);
 
-    Item it = item_at(p, before, begin);
     Running<D> s;
     begin_item<D>(p, it, s);
-    int64_t x = begin;
-    int stage = 0;
+    int x = begin, stage = 0;
     uint32_t phase = 0;
     bool fine = true, late = false;
-    while (x < end) {
-      fine = mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns);
-      fine = __all_sync(0xffffffffu, fine);
+#pragma unroll 1
+    while (true) {
+      fine = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns));
       if (!fine) break;
-      run_tile<D>(s, ring + stage * S::kStageBytes, static_cast<int>(x - it.begin) * kTile, it.len, absent_bits >> (2 * stage) & 3u);
+      run_tile<D>(s, ring + stage * S::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (4 * stage) & 15u);
       __syncwarp();
       if (asked < end) request(stage);
       ++x;
       if (x == it.begin + it.tiles || x == end) {
-        const bool whole = it.begin >= begin && x == it.begin + it.tiles;
-        if (whole) {
+        if (it.begin >= begin && x == it.begin + it.tiles) {
           store_item<D>(p, it, s);
         } else {
           // The run's first item keeps its part beside the ring.  A last one that is another waits until every warp of the CTA
           // has left the ring, and takes its place.
           const int at = it.begin <= begin ? 0 : 1;
-          if (at == 0) keep_part<D>(s, smem + S::kParts + warp * S::kPart);
-          else late = true;
           if (lane == 0) { records[2 * warp + at].item = it; records[2 * warp + at].valid = 1; }
+          late = at == 1;
+          if (!late) keep_part<D>(s, smem + S::kParts + warp * S::kPart);
         }
         if (x == end) break;
-        it = item_at(p, before, x);
+        next_item(p, it);
         begin_item<D>(p, it, s);
       }
       if (++stage == S::kStages) { stage = 0; phase ^= 1; }
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     bool leads = w < kWarps && records[lane].valid != 0;
     int more = 0;
     if (leads) {
-      const int64_t begin = records[lane].item.begin;
+      const int begin = records[lane].item.begin;
       const auto same = [&](int r) { return records[r].valid != 0 && records[r].item.begin == begin; };
       if ((lane & 1) == 0 && w > 0 && (same(lane - 1) || same(lane - 2))) leads = false;
       while (leads && w + 1 + more < kWarps && same(2 * (w + 1 + more))) ++more;
@@ -509,8 +509,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       g.first = lane;
       g.more = more;
       g.slot = it.begin >= cta_begin && it.begin + it.tiles <= cta_end ? -1 : it.begin <= cta_begin ? 0 : 1;
-      g.cta0 = static_cast<int>(run_of(it.begin) / kWarps);
-      g.ctas = static_cast<int>(run_of(it.begin + it.tiles - 1) / kWarps) - g.cta0 + 1;
+      g.cta0 = run_of(it.begin) / kWarps;
+      g.ctas = run_of(it.begin + it.tiles - 1) / kWarps - g.cta0 + 1;
     }
     if (lane == 0) n_segments = __popc(all);
   }
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     if (g.slot < 0 || !g.last) continue;
     __threadfence();
     const Item it = records[g.first].item;
-    const int64_t begin0 = run_begin(static_cast<int64_t>(g.cta0) * kWarps);
+    const int begin0 = run_begin(g.cta0 * kWarps);
     const auto row_at = [&](int c, int row) {
       return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 && it.begin > begin0 ? 1 : 0)) * kRows + row;
     };
@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
 template <int D>
 cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
   using S = AttendSmem<D>;
-  static_assert(S::kBefore + (kAttendMaxB + 1) * 8 + 1024 <= 227 * 1024, "shared memory of one SM");
+  static_assert(S::kBefore + (kAttendMaxB + 1) * 4 + 1024 <= 227 * 1024, "shared memory of one SM");
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = smem_limit_once(attend_kernel<D>, S::bytes(kAttendMaxB), done);
   if (e != cudaSuccess) return e;

@@ -82,11 +82,20 @@ __device__ __forceinline__ float inverse_root<float>(float v) { return rsqrtf(v)
 template <>
 __device__ __forceinline__ double inverse_root<double>(double v) { return rsqrt(v); }
 
+// Warps per SM, with a head of each lane group to a warp, from which on a group takes four heads.
+constexpr int kSpread = 64;
+
 // One operand of the launch: queries or keys.
 struct Operand {
   const __nv_bfloat16* x;
   size_t ld, hd;
   const void* w;
+  bool vec;
+};
+
+struct Target {
+  __nv_bfloat16* x;
+  size_t ld, hd;
   bool vec;
 };
 
@@ -231,53 +240,163 @@ __device__ __forceinline__ uint32_t quantise8(const R (&y)[8], uint32_t& params)
   return word;
 }
 
-template <int LPH, bool APPEND>
+// The factors of a lane's eight elements: out[i] = r * (x[i] * a[i] + other[i] * b[i]), weights, cos and sin in them.  They are
+// the same for every head of a token.  Returns whether the lane's elements turn; if not, a is the weight and b unused.
+template <int LPH>
+__device__ __forceinline__ bool factors(const HeadsParams& p, const void* w, int e, const float* angles, float (&a)[8], float (&b)[8]) {
+  const int half = p.rot / 2;
+  float wb[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = wb[i] = 1.0f;
+  if (e >= p.D) return false;
+  if (w != nullptr) weights8(w, p.w_f32, p.w_vec, e, a);
+  if (e >= p.rot) return false;
+  if (p.interleaved) {
+    const float4 c = __ldg(reinterpret_cast<const float4*>(angles + e / 2)), s = __ldg(reinterpret_cast<const float4*>(angles + half + e / 2));
+    const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float w0 = a[2 * i], w1 = a[2 * i + 1];
+      a[2 * i] = w0 * cv[i]; b[2 * i] = -w1 * sv[i];
+      a[2 * i + 1] = w1 * cv[i]; b[2 * i + 1] = w0 * sv[i];
+    }
+    return true;
+  }
+  const bool first = e < half;
+  const int at = first ? e : e - half;
+  if (w != nullptr) weights8(w, p.w_f32, p.w_vec, first ? e + half : at, wb);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float4 c = __ldg(reinterpret_cast<const float4*>(angles + at) + i), s = __ldg(reinterpret_cast<const float4*>(angles + half + at) + i);
+    const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      a[4 * i + x] *= cv[x];
+      b[4 * i + x] = wb[4 * i + x] * (first ? -sv[x] : sv[x]);
+    }
+  }
+  return true;
+}
+
+// NH heads of a token by one group of lanes: their loads are in flight together, the factors are made once.
+template <int LPH, int NH>
+__device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, bool live) {
+  constexpr int HPW = 32 / LPH;
+  const int lane = threadIdx.x & 31, e = (lane % LPH) * 8, half = p.rot / 2;
+  const bool mine = live && e < p.D;
+  uint4 raw[NH];
+#pragma unroll
+  for (int n = 0; n < NH; ++n) {
+    const int h = h0 + n * HPW;
+    raw[n] = mine && h < H ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
+  }
+  const float* angles = angles_of(p, t, live);
+  if (!p.rot_vec) {                                     // any even rot: one head at a time
+#pragma unroll 1
+    for (int n = 0; n < NH; ++n) {
+      const int h = h0 + n * HPW;
+      const bool in = mine && h < H;
+      float y[8];
+      uint4 u = in ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
+      turned<LPH, float>(p, o, t * o.ld + (h < H ? h : 0) * o.hd, e, live && h < H, angles, u, y);
+      __syncwarp();                                     // in place: every load of the warp's heads comes before the stores
+      if (in) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
+    }
+    return;
+  }
+  float a[8], b[8];
+  const bool turn = live && factors<LPH>(p, o.w, e, angles, a, b);
+  const int from = turn && !p.interleaved ? (e < half ? lane + half / 8 : lane - half / 8) : lane;
+#pragma unroll
+  for (int n = 0; n < NH; ++n) {
+    float x[8], y[8];
+    widen8(raw[n], x);
+    float r = 1.0f;
+    if (o.w != nullptr) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+#pragma unroll
+      for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+      r = rsqrtf(ss / static_cast<float>(p.D) + p.eps);
+    }
+    uint4 u = raw[n];
+    if (p.rot != 0 && !p.interleaved) {
+      u.x = __shfl_sync(0xffffffffu, u.x, from);
+      u.y = __shfl_sync(0xffffffffu, u.y, from);
+      u.z = __shfl_sync(0xffffffffu, u.z, from);
+      u.w = __shfl_sync(0xffffffffu, u.w, from);
+    }
+    if (turn) {
+      float z[8];
+      widen8(u, z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = fmaf(x[i], a[i], (p.interleaved ? x[i ^ 1] : z[i]) * b[i]) * r;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = x[i] * a[i] * r;
+    }
+    const int h = h0 + n * HPW;
+    if (mine && h < H) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
+  }
+}
+
+template <int LPH, bool APPEND, int NH>
 __global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ HeadsParams p) {
-  constexpr int HPW = 32 / LPH;                          // heads of a warp
+  constexpr int HPW = 32 / LPH;                          // heads of a warp at a time
   pdl_trigger();
   pdl_wait();
   const int n = p.n_valid != nullptr ? min(max(*p.n_valid, 0), p.T) : p.T;
   const int lane = threadIdx.x & 31, e = (lane % LPH) * 8;
-  const int64_t warp = static_cast<int64_t>(blockIdx.x) * (blockDim.x / 32) + (threadIdx.x >> 5);
-  const int64_t k_warps = (static_cast<int64_t>(p.T) * p.Hkv + HPW - 1) / HPW;
-  const bool keys = warp < k_warps;                      // the keys, which take longest, begin first
+  // the keys, which take longest on their way into the cache, begin first
+  const uint32_t k_blocks = p.k_blocks;
+  const bool keys = blockIdx.x < k_blocks;
   const int H = keys ? p.Hkv : p.Hq;
-  if (H == 0) return;
-  const int64_t item = (keys ? warp : warp - k_warps) * HPW + lane / LPH;
-  const int64_t row = item / H;
-  const int h = static_cast<int>(item - row * H);
-  const bool live = row < n;
-  const int t = live ? static_cast<int>(row) : 0;
+  constexpr int kAhead = APPEND ? 1 : NH;
+  const int step = HPW * (keys ? kAhead : NH);
+  const uint32_t chunks = (H + step - 1) / step;         // of a token's heads
+  const uint32_t warp = (blockIdx.x - (keys ? 0u : k_blocks)) * 8 + (threadIdx.x >> 5);
+  const uint32_t row = warp / chunks;
+  const int h0 = static_cast<int>(warp - row * chunks) * step + lane / LPH;
+  const bool in = row < static_cast<uint32_t>(n);
+  const int t = in ? static_cast<int>(row) : 0;
   const Operand o = keys ? Operand{p.k, p.ld_k, p.hd_k, p.k_w, p.k_vec} : Operand{p.q, p.ld_q, p.hd_q, p.q_w, p.q_vec};
+  if (!APPEND || !keys) {
+    turn_heads<LPH, NH>(p, o, keys ? Target{p.k_out, p.ld_k_out, p.hd_k_out, p.k_out_vec} : Target{p.q_out, p.ld_q_out, p.hd_q_out, p.q_out_vec},
+                        t, h0, H, in);
+    return;
+  }
+
+  const bool live = in && h0 < H;
+  const int h = h0 < H ? h0 : 0;
   const size_t at = t * o.ld + h * o.hd;
   const bool mine = live && e < p.D;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-
-  if (APPEND && keys) {
-    uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
-    const uint4 raw_v = mine ? load8(p.v + t * p.ld_v + h * p.hd_v + e, p.v_vec) : zero;
-    const int slot = live ? p.slots[t] : -1;
-    double y[8];
-    turned<LPH, double>(p, o, at, e, live, angles_of(p, t, live), raw, y);
-    float v[8];
-    widen8(raw_v, v);
-    bool bad = false;
+  uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
+  const uint4 raw_v = mine ? load8(p.v + t * p.ld_v + h * p.hd_v + e, p.v_vec) : zero;
+  const int slot = live ? p.slots[t] : -1;
+  double y[8];
+  turned<LPH, double>(p, o, at, e, live, angles_of(p, t, live), raw, y);
+  float v[8];
+  widen8(raw_v, v);
+  bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (!isfinite(y[i])) { y[i] = 0.0; bad = true; }
-      if (!isfinite(v[i])) { v[i] = 0.0f; bad = true; }
-    }
-    const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
-    bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
-    uint32_t pk, pv;
-    const uint32_t wk = quantise8<double>(y, pk), wv = quantise8<float>(v, pv);
-    if (bad) pk |= kMarked;
-    if (!live) return;
-    if (slot < 0 || slot >= p.n_pages * p.page_size) {
-      if (slot >= 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
-      return;
-    }
-    if (bad) atomicOr(p.status, TEMPO_STATUS_BAD_VALUE);
+  for (int i = 0; i < 8; ++i) {
+    if (!isfinite(y[i])) { y[i] = 0.0; bad = true; }
+    if (!isfinite(v[i])) { v[i] = 0.0f; bad = true; }
+  }
+  const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
+  bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
+  uint32_t pk, pv;
+  const uint32_t wk = quantise8<double>(y, pk), wv = quantise8<float>(v, pv);
+  if (bad) pk |= kMarked;
+  if (!live) return;
+  if (slot < 0 || slot >= p.n_pages * p.page_size) {
+    if (slot >= 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+    return;
+  }
+  if (bad) atomicOr(p.status, TEMPO_STATUS_BAD_VALUE);
+  if constexpr (APPEND) {
     using U = CacheUnit<LPH * 8>;
     const int page = slot / p.page_size, in_page = slot % p.page_size, in_unit = in_page % kUnit;
     uint8_t* uk = p.cache + unit_offset<LPH * 8>(page, h, 0, in_page, p.Hkv, p.page_size);
@@ -291,16 +410,7 @@ __global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ Head
       *reinterpret_cast<uint16_t*>(uv + U::kCodes + (in_unit / 2) * U::kPairParams + e / kGroup * 4 + (in_unit & 1) * 2) =
           static_cast<uint16_t>(pv);
     }
-    return;
   }
-
-  const uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
-  float y[8];
-  turned<LPH, float>(p, o, at, e, live, angles_of(p, t, live), raw, y);
-  __syncwarp();                                          // in place: every load of the warp's heads comes before the stores
-  if (!mine) return;
-  if (keys) store8(p.k_out + t * p.ld_k_out + h * p.hd_k_out + e, y, p.k_out_vec);
-  else store8(p.q_out + t * p.ld_q_out + h * p.hd_q_out + e, y, p.q_out_vec);
 }
 
 template <int D>
@@ -343,22 +453,29 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Kv
   *reinterpret_cast<uint4*>(p.v + at) = v;
 }
 
+template <int LPH, bool APPEND, int NH>
+cudaError_t launch_heads_as(HeadsParams p, cudaStream_t stream) {
+  constexpr int HPW = 32 / LPH, kStep = HPW * (APPEND ? 1 : NH);
+  const int64_t k = (static_cast<int64_t>(p.T) * ((p.Hkv + kStep - 1) / kStep) + 7) / 8;
+  const int64_t q = (static_cast<int64_t>(p.T) * ((p.Hq + HPW * NH - 1) / (HPW * NH)) + 7) / 8;
+  if (k + q > 0x1fffffff) return cudaErrorInvalidValue;          // warps are numbered in 32 bits
+  p.k_blocks = static_cast<uint32_t>(k);
+  return launch_pdl(heads_kernel<LPH, APPEND, NH>, dim3(static_cast<unsigned>(k + q)), dim3(256), 0, stream, p);
+}
+
 template <int LPH, bool APPEND>
-cudaError_t launch_heads_as(const HeadsParams& p, cudaStream_t stream) {
-  constexpr int HPW = 32 / LPH;
-  const int64_t warps = (static_cast<int64_t>(p.T) * p.Hkv + HPW - 1) / HPW + (static_cast<int64_t>(p.T) * p.Hq + HPW - 1) / HPW;
-  const int64_t blocks = (warps + 7) / 8;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_pdl(heads_kernel<LPH, APPEND>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p);
+cudaError_t launch_heads_as(const HeadsParams& p, int num_sms, cudaStream_t stream) {
+  const int64_t warps = static_cast<int64_t>(p.T) * (static_cast<int64_t>(p.Hq) + p.Hkv) / (32 / LPH);
+  return warps > static_cast<int64_t>(num_sms) * kSpread ? launch_heads_as<LPH, APPEND, 4>(p, stream) : launch_heads_as<LPH, APPEND, 1>(p, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_heads(const HeadsParams& p, bool append, cudaStream_t stream) {
-  if (append) return p.D == 64 ? launch_heads_as<8, true>(p, stream) : launch_heads_as<16, true>(p, stream);
-  if (p.D <= 64) return launch_heads_as<8, false>(p, stream);
-  if (p.D <= 128) return launch_heads_as<16, false>(p, stream);
-  return launch_heads_as<32, false>(p, stream);
+cudaError_t launch_heads(const HeadsParams& p, bool append, int num_sms, cudaStream_t stream) {
+  if (append) return p.D == 64 ? launch_heads_as<8, true>(p, num_sms, stream) : launch_heads_as<16, true>(p, num_sms, stream);
+  if (p.D <= 64) return launch_heads_as<8, false>(p, num_sms, stream);
+  if (p.D <= 128) return launch_heads_as<16, false>(p, num_sms, stream);
+  return launch_heads_as<32, false>(p, num_sms, stream);
 }
 
 cudaError_t launch_kv_read(const KvReadParams& p, int D, cudaStream_t stream) {

@@ -231,8 +231,9 @@ struct HeadsParams {
   int n_pages, page_size;    // append only, as all below
   const int32_t* slots;
   uint8_t* cache;
+  uint32_t k_blocks;         // set by the launcher: blocks that take keys
 };
-cudaError_t launch_heads(const HeadsParams& p, bool append, cudaStream_t stream);
+cudaError_t launch_heads(const HeadsParams& p, bool append, int num_sms, cudaStream_t stream);
 
 struct KvReadParams {
   int n, n_pages, page_size, Hkv;
@@ -252,7 +253,7 @@ struct AttendLayout {
 AttendLayout attend_layout(int D);
 struct AttendParams {
   int B, T, Hkv, group;      // group: query heads of a key head
-  int max_pages, page_size, n_pages;
+  int max_pages, page_size, page_shift, n_pages;
   const __nv_bfloat16* q;
   const uint8_t* cache;
   const int32_t* page_table;

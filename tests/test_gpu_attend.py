@@ -144,7 +144,8 @@ def test_bad_pages_lengths_and_values(B, n):
     c.table[2] = c.table[2, :19].repeat(2)[:c.table.shape[1]]
     out = c.run()
     assert int(c.status) == B.STATUS_BAD_INDEX
-    assert out[n:2 * n].isnan().all() and torch.equal(out[:n], good[:n]) and torch.equal(out[3 * n:], good[3 * n:])
+    assert out[n:2 * n].isnan().all()
+    c.check(torch.cat([out[:n], good[n:3 * n], out[3 * n:]]))          # not by bits: where items are cut goes by all the lengths
     assert not out[2 * n:3 * n].isnan().any()
     # a marked token: whoever sees it, of its head
     c = Case(B, [(300, n), (300, n)], 4, 2, 128, 16)
