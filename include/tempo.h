@@ -455,7 +455,7 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), 16-byte aligned rows (address and
  *   pitches); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
  *   max_q [host] is the most queries of a sequence: a hint for the choice of kernels, any value gives the same result within rounding.
- *   Rows before q_start[0] and from q_start[B] on are left as they are.  Hq is a multiple of Hkv; B <= 2048.
+ *   Rows before q_start[0] and from q_start[B] on are left as they are.  Hq is a multiple of Hkv; B <= 1024.
  *   workspace  tempo_attend_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves it
  *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.
  * A length beyond the page table counts as its end, rows outside q as none, both with TEMPO_STATUS_BAD_INDEX; a page outside

@@ -14,7 +14,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libtempo.so")
 SOURCES = ["api.cu", "dispatch.cu", "dispatch_sampled.cu", "permute.cu", "ffn.cu", "combine.cu", "pack.cu",
-           "norm.cu", "route.cu", "few.cu", "heads.cu", "attend.cu"]
+           "norm.cu", "route.cu", "few.cu", "heads.cu", "attend.cu",
+           "attend_many.cu"]
 
 
 MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")

@@ -748,7 +748,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.counters = reinterpret_cast<unsigned int*>(ws + L.off_counters);
   p.stats = reinterpret_cast<float*>(ws + L.off_stats); p.part = reinterpret_cast<float*>(ws + L.off_out);
   p.wait_ns = kDefaultWaitNs;
-  return launch_attend(p, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+  return launch_attend(p, a->max_q, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -16,77 +16,16 @@
 // launch, whatever the lengths.  A warp streams its run through a ring of its own (bulk copies, one barrier per stage) and
 // waits for nobody; parts of items that were cut are joined in shared memory after the CTA's last tile, and across CTAs by the one
 // that arrives last, in a fixed order.
-#include "cache.cuh"
-#include "ffn_common.cuh"
+#include "attend_common.cuh"
 
 namespace tempo {
 
 namespace {
 
 constexpr int kWarps = 8, kTile = 64, kUnits = kTile / kUnit, kRows = 16;
-constexpr float kBias = 7.0f, kSlack = 8.0f;      // weights are 2^(x - m + 7); m is raised once x exceeds it by more than 8
 
-struct Item {                 // rows [row0, row0 + 16) of a sequence and key head, and its tiles
-  int begin, tiles;           // number of its first tile in the launch
-  int b, h, row0;
-  int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
-};
-
-__device__ __forceinline__ void span_of(const AttendParams& p, int b, int& len, int& q0, int& n, bool tell = false) {
-  const int given = p.lens[b];
-  len = min(max(given, 0), p.max_pages << p.page_shift);
-  int from = b, to = b + 1;
-  if (p.q_start != nullptr) { from = p.q_start[b]; to = p.q_start[b + 1]; }
-  q0 = min(max(from, 0), p.T);
-  n = max(min(max(to, 0), p.T) - q0, 0);
-  if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
-}
-
-// Tiles that the rows [row0, row0 + 16) see: at least one, so that rows without a token are written too.
-__device__ __forceinline__ int tiles_of(int len, int n, int group, int row0) {
-  const int last = min(row0 + kRows, n * group) - 1;
-  const int seen = len - n + last / group + 1;
-  return max(1, (seen + kTile - 1) / kTile);
-}
-
-// The item of tile x.  before[b]: tiles before sequence b.
-__device__ __forceinline__ Item item_at(const AttendParams& p, const int* before, int x) {
-  int lo = 0, hi = p.B - 1;
-  while (lo < hi) {                                  // the last sequence with before[b] <= x: the one that has tile x
-    const int mid = (lo + hi + 1) >> 1;
-    if (before[mid] <= x) lo = mid; else hi = mid - 1;
-  }
-  Item it;
-  it.b = lo;
-  span_of(p, lo, it.len, it.q0, it.n);
-  const int per_head = (before[lo + 1] - before[lo]) / p.Hkv;
-  int rest = x - before[lo];
-  it.h = rest / per_head;
-  rest -= it.h * per_head;
-  it.row0 = 0;
-  for (;;) {
-    it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
-    if (rest < it.tiles) break;
-    rest -= it.tiles;
-    it.row0 += kRows;
-  }
-  it.begin = x - rest;
-  return it;
-}
-
-// The one behind it (there is one: the caller has a tile left).
-__device__ __forceinline__ void next_item(const AttendParams& p, Item& it) {
-  it.begin += it.tiles;
-  it.row0 += kRows;
-  if (it.row0 >= it.n * p.group) {
-    it.row0 = 0;
-    if (++it.h == p.Hkv) {
-      it.h = 0;
-      do span_of(p, ++it.b, it.len, it.q0, it.n); while (it.n == 0);
-    }
-  }
-  it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
-}
+using Tiles = Cut<kRows, kTile>;
+using Item = Tiles::Item;
 
 struct Part {                 // a cut item's share of one warp
   Item item;
@@ -110,11 +49,6 @@ struct AttendSmem {
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* a, uint32_t (&v)[W]) {
@@ -173,11 +107,8 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
       odd = __shfl_xor_sync(0xffffffffu, static_cast<int>(odd), d) != 0 || odd;
     }
-    // the row times a power of two (and the scale's sign), its largest element in [256, 512): fp16 holds 2^-33 of it
-    const int e = top > 0.0f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -110), 119) : 0;
-    const float up = odd ? __uint_as_float(0x7fc00000u)
-                         : __uint_as_float((static_cast<uint32_t>(127 - e) << 23) | (__float_as_uint(p.scale_log2) & 0x80000000u));
-    s.f[half] = fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * fabsf(p.scale_log2), 1.2e-38f);
+    float up;
+    row_factors(top, odd, p.scale_log2, up, s.f[half]);
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
@@ -371,50 +302,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_wait();
 
-  // tiles before each sequence
-  int total = 0;
-  for (int b0 = 0; b0 < p.B; b0 += kWarps * 32) {
-    const int b = b0 + tid;
-    int mine = 0;
-    if (b < p.B) {
-      int len, q0, n;
-      span_of(p, b, len, q0, n, blockIdx.x == 0);
-      for (int row0 = 0; row0 < n * p.group; row0 += kRows) mine += tiles_of(len, n, p.group, row0);
-      mine *= p.Hkv;
-    }
-    int run = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const int up = __shfl_up_sync(0xffffffffu, run, d);
-      if (lane >= d) run += up;
-    }
-    if (lane == 31) warp_sum[warp] = run;
-    __syncthreads();
-    int base = total;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const int v = warp_sum[w];
-      if (w < warp) base += v;
-      total += v;
-    }
-    if (b < p.B) before[b + 1] = base + run;
-    if (b == 0) before[0] = 0;
-    __syncthreads();
-  }
+  const int total = Tiles::count_tiles<kWarps>(p, before, warp_sum, blockIdx.x == 0);
   if (total == 0) return;
 
-  // Equal runs: the first `longer` of them have one tile more.
-  const int runs = min(total, static_cast<int>(gridDim.x) * kWarps);
-  const int quota = total / runs, longer = total - quota * runs;
-  const auto run_begin = [&](int r) { return r * quota + min(r, longer); };
-  const auto run_of = [&](int x) { return x < longer * (quota + 1) ? x / (quota + 1) : longer + (x - longer * (quota + 1)) / quota; };
+  const int n_runs = min(total, static_cast<int>(gridDim.x) * kWarps);
+  const Runs runs(total, n_runs);
   const int run0 = blockIdx.x * kWarps;
-  if (run0 >= runs) return;
-  const int cta_begin = run_begin(run0), cta_end = run_begin(min(run0 + kWarps, runs));
+  if (run0 >= n_runs) return;
+  const int cta_begin = runs.begin(run0), cta_end = runs.begin(min(run0 + kWarps, n_runs));
 
-  if (run0 + warp < runs) {
-    const int begin = run_begin(run0 + warp), end = run_begin(run0 + warp + 1);
-    Item it = item_at(p, before, begin);
+  if (run0 + warp < n_runs) {
+    const int begin = runs.begin(run0 + warp), end = runs.begin(run0 + warp + 1);
+    Item it = Tiles::item_at(p, before, begin);
     Item ahead = it;                                 // the item of the next tile to be requested
     int asked = begin;
     uint32_t absent_bits = 0;                        // four bits per stage
@@ -442,7 +341,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       __syncwarp();
       if (wanted) bulk_load(smem_u32(ring + stage * S::kStageBytes + lane * U::kBytes), src, U::kBytes, bars + 8 * stage);
       if (++asked < end) {
-        if (asked == ahead.begin + ahead.tiles) next_item(p, ahead);
+        if (asked == ahead.begin + ahead.tiles) Tiles::next_item(p, ahead);
         page = look(asked - ahead.begin);
       }
     };
@@ -474,7 +373,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
           if (!late) keep_part<D>(s, smem + S::kParts + warp * S::kPart);
         }
         if (x == end) break;
-        next_item(p, it);
+        Tiles::next_item(p, it);
         begin_item<D>(p, it, s);
       }
       if (++stage == S::kStages) { stage = 0; phase ^= 1; }
@@ -509,8 +408,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       g.first = lane;
       g.more = more;
       g.slot = it.begin >= cta_begin && it.begin + it.tiles <= cta_end ? -1 : it.begin <= cta_begin ? 0 : 1;
-      g.cta0 = run_of(it.begin) / kWarps;
-      g.ctas = run_of(it.begin + it.tiles - 1) / kWarps - g.cta0 + 1;
+      g.cta0 = runs.of(it.begin) / kWarps;
+      g.ctas = runs.of(it.begin + it.tiles - 1) / kWarps - g.cta0 + 1;
     }
     if (lane == 0) n_segments = __popc(all);
   }
@@ -562,7 +461,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     if (g.slot < 0 || !g.last) continue;
     __threadfence();
     const Item it = records[g.first].item;
-    const int begin0 = run_begin(g.cta0 * kWarps);
+    const int begin0 = runs.begin(g.cta0 * kWarps);
     const auto row_at = [&](int c, int row) {
       return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 && it.begin > begin0 ? 1 : 0)) * kRows + row;
     };
@@ -617,13 +516,23 @@ AttendLayout attend_layout(int D) {
   AttendLayout L;
   L.off_counters = 0;
   L.off_stats = round(kAttendMaxSms * sizeof(unsigned int));
-  L.off_out = L.off_stats + round(static_cast<size_t>(kAttendMaxSms) * 2 * kRows * 8);
-  L.total = L.off_out + static_cast<size_t>(kAttendMaxSms) * 2 * kRows * D * 4;
+  L.off_out = L.off_stats + round(static_cast<size_t>(kAttendMaxSms) * 2 * kAttendManyRows * 8);
+  L.total = L.off_out + static_cast<size_t>(kAttendMaxSms) * 2 * kAttendManyRows * D * 4;
   return L;
 }
 
-cudaError_t launch_attend(const AttendParams& p, int D, int num_sms, cudaStream_t stream) {
-  return D == 64 ? launch_attend_as<64>(p, num_sms, stream) : launch_attend_as<128>(p, num_sms, stream);
+// Sequences of up to kFewRows rows are this kernel's, longer ones the other's.
+constexpr int kFewRows = 64;
+
+cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream) {
+  const bool many = static_cast<int64_t>(max_q) * p.group > kFewRows;
+  p.rows_above = 0;
+  p.rows_most = many ? kFewRows : INT32_MAX;         // without the other kernel this one takes whatever comes
+  cudaError_t e = D == 64 ? launch_attend_as<64>(p, num_sms, stream) : launch_attend_as<128>(p, num_sms, stream);
+  if (e != cudaSuccess || !many) return e;
+  p.rows_above = kFewRows;
+  p.rows_most = INT32_MAX;
+  return launch_attend_many(p, D, num_sms, stream);
 }
 
 }  // namespace tempo

@@ -1,0 +1,145 @@
+// What the attention kernels share: how work is cut into items and tiles, and how it is dealt.
+//
+// A key head's queries (the heads of its group, and the new tokens of the sequence) are rows; kRows of them are an item.  An item
+// has one tile for each kTile tokens that its last row sees.  The tiles of all items stand in one row, which is cut into runs of
+// equal length whatever the lengths of the sequences.
+#pragma once
+
+#include "cache.cuh"
+#include "ffn_common.cuh"
+
+namespace tempo {
+
+template <int ROWS, int TILE>
+struct Cut {
+  static constexpr int kRows = ROWS, kTile = TILE;
+
+  struct Item {                 // rows [row0, row0 + kRows) of a sequence and key head, and its tiles
+    int begin, tiles;           // number of its first tile in the launch
+    int b, h, row0;
+    int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
+  };
+
+  // A sequence; one whose rows are another launch's has no queries here.
+  static __device__ __forceinline__ void span_of(const AttendParams& p, int b, int& len, int& q0, int& n, bool tell = false) {
+    const int given = p.lens[b];
+    len = min(max(given, 0), p.max_pages << p.page_shift);
+    int from = b, to = b + 1;
+    if (p.q_start != nullptr) { from = p.q_start[b]; to = p.q_start[b + 1]; }
+    q0 = min(max(from, 0), p.T);
+    n = max(min(max(to, 0), p.T) - q0, 0);
+    if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+    if (n * p.group <= p.rows_above || n * p.group > p.rows_most) n = 0;
+  }
+
+  // Tiles that the rows [row0, row0 + kRows) see: at least one, so that rows without a token are written too.
+  static __device__ __forceinline__ int tiles_of(int len, int n, int group, int row0) {
+    const int last = min(row0 + kRows, n * group) - 1;
+    const int seen = len - n + last / group + 1;
+    return max(1, (seen + kTile - 1) / kTile);
+  }
+
+  // The item of tile x.  before[b]: tiles before sequence b.
+  static __device__ __forceinline__ Item item_at(const AttendParams& p, const int* before, int x) {
+    int lo = 0, hi = p.B - 1;
+    while (lo < hi) {                                  // the last sequence with before[b] <= x: the one that has tile x
+      const int mid = (lo + hi + 1) >> 1;
+      if (before[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    Item it;
+    it.b = lo;
+    span_of(p, lo, it.len, it.q0, it.n);
+    const int per_head = (before[lo + 1] - before[lo]) / p.Hkv;
+    int rest = x - before[lo];
+    it.h = rest / per_head;
+    rest -= it.h * per_head;
+    it.row0 = 0;
+    for (;;) {
+      it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
+      if (rest < it.tiles) break;
+      rest -= it.tiles;
+      it.row0 += kRows;
+    }
+    it.begin = x - rest;
+    return it;
+  }
+
+  // The one behind it (there is one: the caller has a tile left).
+  static __device__ __forceinline__ void next_item(const AttendParams& p, Item& it) {
+    it.begin += it.tiles;
+    it.row0 += kRows;
+    if (it.row0 >= it.n * p.group) {
+      it.row0 = 0;
+      if (++it.h == p.Hkv) {
+        it.h = 0;
+        do span_of(p, ++it.b, it.len, it.q0, it.n); while (it.n == 0);
+      }
+    }
+    it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
+  }
+
+  // before[0] to before[B], by a whole CTA of WARPS warps; returns before[B].
+  template <int WARPS>
+  static __device__ __forceinline__ int count_tiles(const AttendParams& p, int* before, int* warp_sum, bool tell) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int total = 0;
+    for (int b0 = 0; b0 < p.B; b0 += WARPS * 32) {
+      const int b = b0 + tid;
+      int mine = 0;
+      if (b < p.B) {
+        int len, q0, n;
+        span_of(p, b, len, q0, n, tell);
+        for (int row0 = 0; row0 < n * p.group; row0 += kRows) mine += tiles_of(len, n, p.group, row0);
+        mine *= p.Hkv;
+      }
+      int run = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int up = __shfl_up_sync(0xffffffffu, run, d);
+        if (lane >= d) run += up;
+      }
+      if (lane == 31) warp_sum[warp] = run;
+      __syncthreads();
+      int base = total;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const int v = warp_sum[w];
+        if (w < warp) base += v;
+        total += v;
+      }
+      if (b < p.B) before[b + 1] = base + run;
+      if (b == 0) before[0] = 0;
+      __syncthreads();
+    }
+    return total;
+  }
+};
+
+// Runs of equal length: the first `longer` of them have one tile more.
+struct Runs {
+  int quota, longer;
+  __device__ __forceinline__ Runs(int total, int runs) : quota(total / runs), longer(total - total / runs * runs) {}
+  __device__ __forceinline__ int begin(int r) const { return r * quota + min(r, longer); }
+  __device__ __forceinline__ int of(int x) const {
+    return x < longer * (quota + 1) ? x / (quota + 1) : longer + (x - longer * (quota + 1)) / quota;
+  }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+constexpr float kBias = 7.0f, kSlack = 8.0f;      // weights are 2^(x - m + 7); m is raised once x exceeds it by more than 8
+
+// A row of queries times a power of two (and the scale's sign), its largest element in [256, 512): fp16 holds 2^-33 of it.
+// `up`: that factor; `f`: a score is f times the sum of products, in units of log2, and f is above zero.
+__device__ __forceinline__ void row_factors(float top, bool odd, float scale_log2, float& up, float& f) {
+  const int e = top > 0.0f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -110), 119) : 0;
+  up = odd ? __uint_as_float(0x7fc00000u)
+           : __uint_as_float((static_cast<uint32_t>(127 - e) << 23) | (__float_as_uint(scale_log2) & 0x80000000u));
+  f = fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * fabsf(scale_log2), 1.2e-38f);
+}
+
+}  // namespace tempo

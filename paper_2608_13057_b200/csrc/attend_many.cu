@@ -1,0 +1,609 @@
+// Attention over the 4-bit paged cache for many queries of a sequence (prompts and their chunks).
+//
+// Rows are queries times the heads of a group, 256 to an item as two tiles of 128; keys come in tiles of 128.  Bound by the
+// matrix products (4 D operations per row and key) and, close behind, by the exponentials (one per row and key, 16 a clock) and by
+// shared memory: of every key tile 128 x D decoded numbers are written once and read by both row tiles.  Roles of the warps:
+//   loader     copies units of 16 cached tokens into a ring of key and value stages
+//   decoders   codes -> fp16 tiles in shared memory in the layout of the matrix instruction, values transposed
+//   issuer     tcgen05.mma: S = Q K^T into tensor memory, O += P V with P read from tensor memory
+//   softmax    a warpgroup for each row tile, a thread for each row: S -> P in place, running maximum and sum
+// While one row tile's weights are made the tensor cores work on the other.  Maxima are raised only when they have grown by
+// more than 8 (in powers of 2), so that O is seldom touched between products.  The order of a sum over d is free: K and Q are stored
+// as the pairs (n, n + 4) in which codes are decoded, V's rows in the order that stores them without bank conflicts.
+// The tiles of all items are dealt to the CTAs in equal runs; items that were cut are joined by the CTA that arrives last.
+#include "attend_common.cuh"
+#include "mma_warp.cuh"
+
+namespace tempo {
+
+namespace {
+
+constexpr int kThreads = 512;                         // four warpgroups: loader, issuer and decoders; decoders; softmax; softmax
+constexpr int kKeys = 128, kRowTile = 128, kRows = 2 * kRowTile;
+static_assert(kRows == kAttendManyRows, "the workspace is sized for it");
+constexpr int kDecoders = 6;                          // warps 2 to 7
+using Tiles = Cut<kRows, kKeys>;
+using Item = Tiles::Item;
+
+template <int D>
+struct ManySmem {
+  static constexpr int kTileBytes = kKeys * D * 2;                       // fp16 keys, values, or one row tile of queries
+  static constexpr int kStageBytes = kKeys / kUnit * CacheUnit<D>::kBytes;
+  static constexpr int kStages = 3;
+  static constexpr int kQ = 0, kK = 2 * kTileBytes, kV = 4 * kTileBytes, kCodes = 6 * kTileBytes;
+  static constexpr int kBefore = kCodes + kStages * kStageBytes;
+  static int bytes(int B) { return kBefore + (B + 1) * 4 + 1024; }       // the tiles start on 1024 bytes
+  static_assert(kBefore + (kAttendMaxB + 1) * 4 + 1024 + 512 <= 227 * 1024, "shared memory of one SM");
+};
+
+struct Bars {
+  uint64_t code_full[3], code_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t s_full[2], p_ready[2], q_full[2], o_done[2], o_free[2];      // of each row tile
+  uint64_t joined;                                                      // all softmax warps
+};
+
+// A CTA's run as pieces of items, the same in every role.
+struct Pieces {
+  Item it;
+  int x, end;
+  bool first;
+  __device__ __forceinline__ Pieces(const Item& it_, int begin, int end_) : it(it_), x(begin), end(end_), first(true) {}
+  __device__ __forceinline__ bool next(const AttendParams& p) {
+    if (!first) {
+      x = it.begin + it.tiles;
+      if (x < end) Tiles::next_item(p, it);
+    }
+    first = false;
+    return x < end;
+  }
+  __device__ __forceinline__ int tile0() const { return x - it.begin; }
+  __device__ __forceinline__ int steps() const { return min(it.begin + it.tiles, end) - x; }
+  __device__ __forceinline__ bool two(int group) const { return it.n * group - it.row0 > kRowTile; }
+};
+
+// Instruction descriptor of kind::f16 with fp16 operands (0 at bits 7 and 10), 32-bit sums, both K-major, 128 rows, N columns.
+template <int N>
+constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(kRowTile >> 4) << 24);
+
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  warp_mma_bf16(leader, d, a_lo, b_lo, idesc, accumulate);               // kind::f16: the types are the descriptor's
+}
+// A from tensor memory.
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, l;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 l, %6, 0;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "@l tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// (a, b) * f + (m, m)
+__device__ __forceinline__ void fma_pair(float& a, float& b, float f, float m) {
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(f), "f"(m));
+}
+__device__ __forceinline__ void add_pair(float& a, float& b, float c, float d) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+
+// Row `row` of a K-major tile in the 128-byte swizzle: blocks of 64 numbers, each of `rows` rows of 128 bytes.
+__device__ __forceinline__ uint32_t chunk_at(uint32_t base, int rows, int row, int block, int chunk) {
+  return base + block * rows * 128 + row * 128 + ((chunk ^ (row & 7)) << 4);
+}
+
+// ---- decoders -----------------------------------------------------------------------------------------
+// Keys of one stage.  A lane takes 32 neighbouring elements of a key: one group, four words, four 16-byte stores.
+template <int D>
+__device__ __forceinline__ void decode_keys(const uint8_t* stage, uint32_t tile, uint32_t absent, int warp) {
+  using U = CacheUnit<D>;
+  constexpr int kParts = D / 32, kPer = 32 / kParts;                     // lanes to a key, keys to a warp
+  const int lane = threadIdx.x & 31, j = lane % kParts;
+#pragma unroll 1
+  for (int task = warp; task < kKeys / kPer; task += kDecoders) {
+    const int key = task * kPer + lane / kParts;
+    const uint8_t* unit = stage + key / kUnit * U::kBytes;
+    const uint4 u = *reinterpret_cast<const uint4*>(unit + key % kUnit * U::kKeyRow + j * 16);
+    uint32_t params = *reinterpret_cast<const uint16_t*>(unit + U::kCodes + key % kUnit * U::kKeyParams + j * 2) * 0x10001u;
+    if (absent >> (key / kUnit) & 1) params |= kMarked * 0x10001u;
+    uint32_t s, b;
+    group_params(params, s, b);
+    const bool turn = D == 128 && (j & 2) != 0;                          // the second block's lanes in another order: no bank twice
+    const uint32_t w[4] = {turn ? u.z : u.x, turn ? u.w : u.y, turn ? u.x : u.z, turn ? u.y : u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t v[4];
+      decode8(w[i], s, b, v);
+      st_shared_v4(chunk_at(tile, kKeys, key, j / 2, 4 * (j & 1) + (turn ? i ^ 2 : i)), make_uint4(v[0], v[1], v[2], v[3]));
+    }
+  }
+}
+
+// Values of one stage, transposed: a lane takes two words (8 elements) of four pairs of tokens and stores, for each element, its
+// eight tokens.  Element 8 x + 4 e + n is row (D / 4) n + (D / 8) e + x of the tile.
+template <int D>
+__device__ __forceinline__ void decode_values(const uint8_t* stage, uint32_t tile, int t0, int len, int warp) {
+  using U = CacheUnit<D>;
+  constexpr int kX = D / 8, kPer = 32 / kX;                              // lanes to eight tokens, eights of tokens to a warp
+  const int lane = threadIdx.x & 31, x = lane % kX;
+#pragma unroll 1
+  for (int task = warp; task < kKeys / 8 / kPer; task += kDecoders) {
+    const int eight = task * kPer + lane / kX;
+    const uint8_t* unit = stage + eight / 2 * U::kBytes;
+    uint32_t v[4][2][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int pair = (eight & 1) * 4 + i;
+      const uint2 w = *reinterpret_cast<const uint2*>(unit + pair * U::kPairRow + x * 8);
+      uint32_t params = *reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + x / 4 * 4);
+      const int left = len - (t0 + 8 * eight + 2 * i);                   // tokens of the pair that exist
+      if (left < 2) params &= left == 1 ? 0xffffu : 0u;
+      uint32_t s, b;
+      group_params(params, s, b);
+      decode8(w.x, s, b, v[i][0]);
+      decode8(w.y, s, b, v[i][1]);
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        st_shared_v4(chunk_at(tile, D, D / 4 * n + kX * e + x, eight / 8, eight % 8),
+                     make_uint4(v[0][e][n], v[1][e][n], v[2][e][n], v[3][e][n]));
+  }
+}
+
+// ---- softmax ------------------------------------------------------------------------------------------
+struct Row {
+  float f, up;
+  int limit;                 // last token the row sees
+  bool in;
+  __nv_bfloat16* out;
+};
+
+// This thread's row of queries into its row tile, as fp16 in the order of the decoded keys.
+template <int D>
+__device__ __forceinline__ Row load_row(const AttendParams& p, const Item& it, int r, uint32_t tile, int row_in_tile) {
+  Row o;
+  const int row = it.row0 + r, qi = row / p.group, head = it.h * p.group + row % p.group;
+  o.in = row < it.n * p.group;
+  o.limit = o.in ? it.len - it.n + qi : it.len - 1;
+  o.out = p.out + static_cast<size_t>(it.q0 + qi) * p.ld_out + static_cast<size_t>(head) * p.hd_out;
+  const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<size_t>(it.q0 + (o.in ? qi : 0)) * p.ld_q +
+                                                    static_cast<size_t>(o.in ? head : 0) * p.hd_q);
+  uint4 u[D / 8];
+  float top = 0.0f;
+  bool odd = false;
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) u[c] = o.in ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    const uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
+      top = fmaxf(top, fabsf(x));
+      odd = odd || !isfinite(x);
+    }
+  }
+  row_factors(top, odd, p.scale_log2, o.up, o.f);
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    const uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16)) * o.up;
+    uint32_t h[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) h[n] = as_u32(__floats2half2_rn(x[n], x[n + 4]));
+    st_shared_v4(chunk_at(tile, kRowTile, row_in_tile, c / 8, c % 8), make_uint4(h[0], h[1], h[2], h[3]));
+  }
+  return o;
+}
+
+// O's column c of a row is element 8 x + 4 e + n, c = (D / 4) n + (D / 8) e + x.
+template <int D>
+__device__ __forceinline__ void store_row(const Row& r, const float (&o)[D], float k) {
+  if (!r.in) return;
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    uint32_t v[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int n = 0; n < 4; n += 2) {
+        const int c = D / 4 * n + D / 8 * e + x;
+        const __nv_bfloat162 h = __floats2bfloat162_rn(o[c] * k, o[c + D / 4] * k);
+        v[2 * e + n / 2] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    reinterpret_cast<uint4*>(r.out)[x] = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_constant__ AttendParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  using S = ManySmem<D>;
+  using U = CacheUnit<D>;
+  __shared__ Bars bars;
+  __shared__ uint32_t s_tmem;
+  __shared__ int abort_flag, s_last, warp_sum[kThreads / 32];
+  __shared__ uint32_t s_absent[S::kStages];
+  const uint32_t raw = smem_u32(smem_raw), pad = (1024 - (raw & 1023)) & 1023;
+  uint8_t* smem = smem_raw + pad;
+  const uint32_t base = raw + pad;
+  int* before = reinterpret_cast<int*>(smem + S::kBefore);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const auto bar = [&](uint64_t& b) { return smem_u32(&b); };
+
+  pdl_trigger();
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < S::kStages; ++i) { mbar_init(bar(bars.code_full[i]), 1); mbar_init(bar(bars.code_empty[i]), kDecoders); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(bars.k_full[i]), kDecoders); mbar_init(bar(bars.k_empty[i]), 1);
+      mbar_init(bar(bars.v_full[i]), kDecoders); mbar_init(bar(bars.v_empty[i]), 1);
+      mbar_init(bar(bars.s_full[i]), 1); mbar_init(bar(bars.p_ready[i]), 4); mbar_init(bar(bars.q_full[i]), 4);
+      mbar_init(bar(bars.o_done[i]), 1); mbar_init(bar(bars.o_free[i]), 4);
+    }
+    mbar_init(bar(bars.joined), 8);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_wait();
+  tc_fence_before();
+  const int total = Tiles::count_tiles<kThreads / 32>(p, before, warp_sum, false);      // also orders what is set up above
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+
+  // Runs of at least kLeast tiles: a shorter one costs more at its joins than it takes off the others.
+  constexpr int kLeast = 4;
+  const int n_runs = min(max(total / kLeast, 1), static_cast<int>(gridDim.x));
+  const bool works = total > 0 && static_cast<int>(blockIdx.x) < n_runs;
+  if (works) {
+    const Runs runs(total, n_runs);
+    const int begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
+    volatile int* abort_at = &abort_flag;
+    const auto wait = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.wait_ns); };
+
+    // 512 threads of 128 registers at launch: 256 of 72 and 256 of 184
+    if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    Pieces pc(Tiles::item_at(p, before, begin), begin, end);
+    if (warp == 0) {
+      // ---- loader: keys, then values of each tile; lanes 0 to 7 a unit each
+      const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
+      int stage = 0;
+      uint32_t phase = 0;
+      bool fine = true;
+      while (fine && pc.next(p)) {
+        for (int i = 0; fine && i < pc.steps(); ++i) {
+          const int t = (pc.tile0() + i) * kKeys + lane * kUnit;
+          const bool wanted = lane < kKeys / kUnit && t < pc.it.len;
+          int page = 0;
+          if (wanted) page = p.page_table[static_cast<size_t>(pc.it.b) * p.max_pages + (t >> p.page_shift)];
+          const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
+          const uint32_t want = __ballot_sync(0xffffffffu, wanted), gone = __ballot_sync(0xffffffffu, wanted && !there);
+          if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+          const uint8_t* src = p.cache + (static_cast<size_t>(there ? page : 0) * p.Hkv + pc.it.h) * 2 * head_bytes +
+                               ((t & (p.page_size - 1)) / kUnit) * U::kBytes;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            fine = wait(bars.code_empty[stage], phase ^ 1);
+            if (!fine) break;
+            if (lane == 0) {
+              s_absent[stage] = gone;
+              mbar_arrive_expect_tx(bar(bars.code_full[stage]), __popc(want) * U::kBytes);
+            }
+            __syncwarp();
+            if (wanted) bulk_load(base + S::kCodes + stage * S::kStageBytes + lane * U::kBytes, src + kv * head_bytes, U::kBytes, bar(bars.code_full[stage]));
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          }
+        }
+      }
+      if (!fine) {                                     // what was requested arrives before the memory goes
+        volatile int none = 0;
+        for (int st = 0; st < S::kStages; ++st) mbar_wait_warp(bar(bars.code_full[st]), phase ^ (st < stage ? 0u : 1u), &none, p.wait_ns);
+      }
+    } else if (warp == 1) {
+      // ---- issuer
+      const uint32_t leader = elect_one();
+      constexpr uint32_t kQk = kIdesc<kKeys>, kPv = kIdesc<D>;
+      const auto s_at = [&](int x) { return tmem + x * kKeys; };
+      const auto o_at = [&](int x) { return tmem + 2 * kKeys + x * D; };
+      const auto product_qk = [&](int x, int buf) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t at = (k / 4) * kKeys * 128 + (k % 4) * 32;
+          mma_ss(leader, s_at(x), desc_lo_sw128(base + S::kQ + x * S::kTileBytes + at), desc_lo_sw128(base + S::kK + buf * S::kTileBytes + at), kQk, k > 0);
+        }
+        warp_commit(leader, bar(bars.s_full[x]));
+      };
+      int t = 0;
+      int done[2] = {0, 0}, seen[2] = {0, 0};          // steps and items of each row tile
+      bool fine = true;
+      while (fine && pc.next(p)) {
+        const int steps = pc.steps(), tiles = pc.two(p.group) ? 2 : 1;
+        fine = wait(bars.k_full[t & 1], t >> 1 & 1);
+        for (int x = 0; fine && x < tiles; ++x) {
+          fine = wait(bars.q_full[x], seen[x] & 1);
+          if (!fine) break;
+          tc_fence_after();
+          product_qk(x, t & 1);
+          if (x == tiles - 1) warp_commit(leader, bar(bars.k_empty[t & 1]));
+        }
+        for (int i = 0; fine && i < steps; ++i) {
+          const int now = t + i, buf = now & 1;
+          fine = wait(bars.v_full[buf], now >> 1 & 1);
+          for (int x = 0; fine && x < tiles; ++x) {
+            fine = wait(bars.p_ready[x], done[x] & 1) && (i > 0 || wait(bars.o_free[x], (seen[x] & 1) ^ 1));
+            if (!fine) break;
+            ++done[x];
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              mma_ts(leader, o_at(x), s_at(x) + k * 8, desc_lo_sw128(base + S::kV + buf * S::kTileBytes + (k / 4) * D * 128 + (k % 4) * 32), kPv,
+                     i > 0 || k > 0);
+            if (i == steps - 1) warp_commit(leader, bar(bars.o_done[x]));
+            if (x == tiles - 1) warp_commit(leader, bar(bars.v_empty[buf]));
+            if (i + 1 < steps) {
+              if (x == 0) fine = wait(bars.k_full[buf ^ 1], (now + 1) >> 1 & 1);
+              if (!fine) break;
+              product_qk(x, buf ^ 1);
+              if (x == tiles - 1) warp_commit(leader, bar(bars.k_empty[buf ^ 1]));
+            }
+          }
+        }
+        for (int x = 0; x < tiles; ++x) ++seen[x];
+        t += steps;
+      }
+    } else {
+      // ---- decoders
+      int stage = 0, t = 0;
+      uint32_t phase = 0;
+      bool fine = true;
+      while (fine && pc.next(p)) {
+        const int steps = pc.steps();
+        for (int i = 0; fine && i < steps; ++i, ++t) {
+          const int buf = t & 1;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            fine = wait(kv == 0 ? bars.k_empty[buf] : bars.v_empty[buf], (t >> 1 & 1) ^ 1) && wait(bars.code_full[stage], phase);
+            if (!fine) break;
+            const uint8_t* codes = smem + S::kCodes + stage * S::kStageBytes;
+            if (kv == 0) decode_keys<D>(codes, base + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
+            else decode_values<D>(codes, base + S::kV + buf * S::kTileBytes, (pc.tile0() + i) * kKeys, pc.it.len, warp - 2);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(bar(kv == 0 ? bars.k_full[buf] : bars.v_full[buf]));
+              mbar_arrive(bar(bars.code_empty[stage]));
+            }
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          }
+        }
+      }
+    }
+    } else {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+      Pieces pc(Tiles::item_at(p, before, begin), begin, end);
+      // ---- softmax: warpgroup x on row tile x, thread by row
+      const int x = (warp - 8) >> 2, row = (warp & 3) * 32 + lane, r = x * kRowTile + row;
+      const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+      const uint32_t s_at = tmem + lanes + x * kKeys, o_at = tmem + lanes + 2 * kKeys + x * D;
+      const uint32_t q_tile = base + S::kQ + x * S::kTileBytes;
+      int done = 0, seen = 0;
+      uint32_t joins = 0;
+      const auto sync_softmax = [&]() {                // a barrier of the softmax warps whose wait ends like any other
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(bars.joined));
+        return wait(bars.joined, joins++ & 1);
+      };
+      bool fine = true;
+      Row mine;
+      const auto load = [&](const Pieces& c) {
+        if (x == 1 && !c.two(p.group)) return;
+        mine = load_row<D>(p, c.it, r, q_tile, row);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(bars.q_full[x]));
+      };
+      bool more = pc.next(p);
+      if (more) load(pc);
+      while (more && fine) {
+        const Item it = pc.it;
+        const int steps = pc.steps(), tile0 = pc.tile0();
+        const bool active = x == 0 || pc.two(p.group);
+        float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+        const Row cur = mine;
+        if (active) {
+          for (int i = 0; i < steps; ++i) {
+            fine = wait(bars.s_full[x], done & 1);
+            if (!fine) break;
+            ++done;
+            tc_fence_after();
+            const int k0 = (tile0 + i) * kKeys;
+            const int see = cur.limit - k0;
+            const bool masked = __any_sync(0xffffffffu, see < kKeys - 1);
+            const auto scores = [&](int b, uint32_t (&c)[32]) {          // 32 of the row's scores; -inf where it does not see
+              tmem_ld32(s_at + 32 * b, c);
+              tmem_wait_ld();
+              if (masked) {
+#pragma unroll
+                for (int v = 0; v < 32; ++v)
+                  if (32 * b + v > see) c[v] = 0xff800000u;
+              }
+            };
+            float top = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              uint32_t c[32];
+              scores(b, c);
+#pragma unroll
+              for (int v = 0; v < 32; v += 2) top = fmaxf(top, fmaxf(__uint_as_float(c[v]), __uint_as_float(c[v + 1])));
+            }
+            top *= cur.f;
+            if (__any_sync(0xffffffffu, top > m + kSlack)) {
+              const float to = top > m + kSlack ? top : m;
+              const float k = to == m ? 1.0f : exp2_fast(m - to);
+              m = to;
+              l0 *= k;
+              l1 *= k;
+              if (i > 0) {                             // S of this step is there: the products into O before it are done
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) {
+                  uint32_t o[32];
+                  tmem_ld32(o_at + 32 * b, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int v = 0; v < 32; ++v) o[v] = __float_as_uint(__uint_as_float(o[v]) * k);
+                  tmem_st32(o_at + 32 * b, o);
+                }
+                tmem_wait_st();
+              }
+            }
+            const float less = m == -INFINITY ? 0.0f : kBias - m;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {              // S's columns 64 h to 64 h + 63 become P's 32 h to 32 h + 31
+              uint32_t w[32];
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                uint32_t c[32];
+                scores(2 * h + y, c);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                  float a = __uint_as_float(c[2 * v]), b = __uint_as_float(c[2 * v + 1]);
+                  fma_pair(a, b, cur.f, less);
+                  a = exp2_fast(a);
+                  b = exp2_fast(b);
+                  add_pair(l0, l1, a, b);
+                  w[16 * y + v] = as_u32(__floats2half2_rn(a, b));
+                }
+              }
+              tmem_st32(s_at + 32 * h, w);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars.p_ready[x]));
+          }
+          if (!fine) break;
+        }
+        more = pc.next(p);
+        if (more) load(pc);                            // the next item's queries: every product with these is done
+
+        const float l = l0 + l1;
+        float o[D];
+        if (active) {
+          fine = wait(bars.o_done[x], seen & 1);
+          if (!fine) break;
+          tc_fence_after();
+#pragma unroll
+          for (int b = 0; b < D / 32; ++b) {
+            uint32_t v[32];
+            tmem_ld32(o_at + 32 * b, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[32 * b + i] = __uint_as_float(v[i]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(bars.o_free[x]));
+          ++seen;
+        }
+        const int first = runs.of(it.begin), ctas = runs.of(it.begin + it.tiles - 1) - first + 1;
+        if (ctas == 1) {
+          if (active) store_row<D>(cur, o, l == 0.0f ? 0.0f : 1.0f / l);
+          continue;
+        }
+        // A cut item: this CTA's part goes to the workspace, four columns of a row to a 16-byte line of 256 rows; the CTA that
+        // arrives last adds the parts up in their order.
+        const auto part_of = [&](int cta) { return static_cast<size_t>(cta) * 2 + (cta == first && it.begin > runs.begin(cta) ? 1 : 0); };
+        float4* parts = reinterpret_cast<float4*>(p.part);
+        float2* stats = reinterpret_cast<float2*>(p.stats);
+        if (active) {
+          const size_t at = part_of(blockIdx.x);
+          __stcg(stats + at * kRows + r, make_float2(m, l));
+#pragma unroll
+          for (int q = 0; q < D / 4; ++q)
+            __stcg(parts + (at * (D / 4) + q) * kRows + r, make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]));
+        }
+        __threadfence();
+        fine = sync_softmax();
+        if (!fine) break;
+        if (tid == kThreads - 1) {
+          const bool last = atomicAdd(p.counters + first, 1u) == static_cast<unsigned>(ctas) - 1u;
+          if (last) p.counters[first] = 0;
+          s_last = last;
+        }
+        fine = sync_softmax();
+        if (!fine) break;
+        if (s_last && active) {
+          __threadfence();
+          float top = -INFINITY;
+          for (int c = 0; c < ctas; ++c) top = fmaxf(top, __ldcg(stats + part_of(first + c) * kRows + r).x);
+          const float ref = top == -INFINITY ? 0.0f : top;
+          float sum = 0.0f;
+#pragma unroll
+          for (int q = 0; q < D; ++q) o[q] = 0.0f;
+          for (int c = 0; c < ctas; ++c) {
+            const size_t at = part_of(first + c);
+            const float2 st = __ldcg(stats + at * kRows + r);
+            const float k = exp2_fast(st.x - ref);
+            sum += st.y * k;
+#pragma unroll
+            for (int q = 0; q < D / 4; ++q) {
+              const float4 v = __ldcg(parts + (at * (D / 4) + q) * kRows + r);
+              o[4 * q] += v.x * k; o[4 * q + 1] += v.y * k; o[4 * q + 2] += v.z * k; o[4 * q + 3] += v.w * k;
+            }
+          }
+          store_row<D>(cur, o, sum == 0.0f ? 0.0f : 1.0f / sum);
+        }
+        fine = sync_softmax();                         // s_last is read before the next item's is written
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (abort_flag) {
+    if (tid == 0) atomicOr(p.status, static_cast<uint32_t>(TEMPO_STATUS_TIMEOUT));
+    for (int i = 0; i < 50; ++i) __nanosleep(1000);    // products in flight drain
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+template <int D>
+cudaError_t launch_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = smem_limit_once(attend_many_kernel<D>, ManySmem<D>::bytes(kAttendMaxB), done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attend_many_kernel<D>, dim3(num_sms), dim3(kThreads), ManySmem<D>::bytes(p.B), stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_many(const AttendParams& p, int D, int num_sms, cudaStream_t stream) {
+  return D == 64 ? launch_as<64>(p, num_sms, stream) : launch_as<128>(p, num_sms, stream);
+}
+
+}  // namespace tempo

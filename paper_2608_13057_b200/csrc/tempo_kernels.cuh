@@ -245,8 +245,9 @@ struct KvReadParams {
 };
 cudaError_t launch_kv_read(const KvReadParams& p, int D, cudaStream_t stream);
 
-constexpr int kAttendMaxB = 2048;
+constexpr int kAttendMaxB = 1024;
 constexpr int kAttendMaxSms = 160;   // the workspace is sized for so many CTAs, whatever the device
+constexpr int kAttendManyRows = 256; // rows of an item in the kernel for many queries
 struct AttendLayout {
   size_t off_counters, off_stats, off_out, total;
 };
@@ -254,6 +255,7 @@ AttendLayout attend_layout(int D);
 struct AttendParams {
   int B, T, Hkv, group;      // group: query heads of a key head
   int max_pages, page_size, page_shift, n_pages;
+  int rows_above, rows_most; // sequences with so many rows (queries times group) are this launch's
   const __nv_bfloat16* q;
   const uint8_t* cache;
   const int32_t* page_table;
@@ -268,6 +270,7 @@ struct AttendParams {
   float* part;               // [CTA][2][rows][D]
   unsigned long long wait_ns;
 };
-cudaError_t launch_attend(const AttendParams& p, int D, int num_sms, cudaStream_t stream);
+cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream);
+cudaError_t launch_attend_many(const AttendParams& p, int D, int num_sms, cudaStream_t stream);
 
 }  // namespace tempo
