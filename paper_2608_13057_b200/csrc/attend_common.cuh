@@ -89,7 +89,15 @@ struct Cut {
       if (b < p.B) {
         int len, q0, n;
         span_of(p, b, len, q0, n, tell);
-        for (int row0 = 0; row0 < n * p.group; row0 += kRows) mine += tiles_of(len, n, p.group, row0);
+        // tiles_of for each row0; the last row's query, (row0 + kRows - 1) / group, is carried along
+        const int step = kRows / p.group, over = kRows - step * p.group;
+        int query = (kRows - 1) / p.group, rest = kRows - 1 - query * p.group;
+        for (int row0 = 0; row0 < n * p.group; row0 += kRows) {
+          mine += max(1, (len - n + min(query, n - 1) + kTile) / kTile);
+          query += step;
+          rest += over;
+          if (rest >= p.group) { rest -= p.group; ++query; }
+        }
         mine *= p.Hkv;
       }
       int run = mine;

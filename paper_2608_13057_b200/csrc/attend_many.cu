@@ -22,6 +22,7 @@ constexpr int kThreads = 512;                         // four warpgroups: loader
 constexpr int kKeys = 128, kRowTile = 128, kRows = 2 * kRowTile;
 static_assert(kRows == kAttendManyRows, "the workspace is sized for it");
 constexpr int kDecoders = 6;                          // warps 2 to 7
+constexpr int kEvery = 4;                             // every fourth pair of exponentials is computed on the FMA pipe
 using Tiles = Cut<kRows, kKeys>;
 using Item = Tiles::Item;
 
@@ -38,7 +39,7 @@ struct ManySmem {
 
 struct Bars {
   uint64_t code_full[3], code_empty[3], k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t s_full[2], p_ready[2], q_full[2], o_done[2], o_free[2];      // of each row tile
+  uint64_t s_full[2], p_ready[2][2], q_full[2], o_done[2], o_free[2];   // of each row tile (P in two halves of 64 keys)
   uint64_t joined;                                                      // all softmax warps
 };
 
@@ -133,7 +134,8 @@ __device__ __forceinline__ void decode_keys(const uint8_t* stage, uint32_t tile,
 }
 
 // Values of one stage, transposed: a lane takes two words (8 elements) of four pairs of tokens and stores, for each element, its
-// eight tokens.  Element 8 x + 4 e + n is row (D / 4) n + (D / 8) e + x of the tile.
+// eight tokens.  Element 8 x + 4 e + n is row 64 (x / 8) + 8 (4 e + n) + x % 8 of the tile: no bank twice in a store, and 64
+// neighbouring rows are 64 neighbouring elements.
 template <int D>
 __device__ __forceinline__ void decode_values(const uint8_t* stage, uint32_t tile, int t0, int len, int warp) {
   using U = CacheUnit<D>;
@@ -160,76 +162,108 @@ __device__ __forceinline__ void decode_values(const uint8_t* stage, uint32_t til
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        st_shared_v4(chunk_at(tile, D, D / 4 * n + kX * e + x, eight / 8, eight % 8),
+        st_shared_v4(chunk_at(tile, D, x / 8 * 64 + (4 * e + n) * 8 + x % 8, eight / 8, eight % 8),
                      make_uint4(v[0][e][n], v[1][e][n], v[2][e][n], v[3][e][n]));
   }
 }
 
 // ---- softmax ------------------------------------------------------------------------------------------
 struct Row {
-  float f, up;
+  float f;                   // a score is f times the sum of products
   int limit;                 // last token the row sees
   bool in;
   __nv_bfloat16* out;
 };
 
-// This thread's row of queries into its row tile, as fp16 in the order of the decoded keys.
+// A warp's 32 rows of queries, from row `r0` of the item on, into their row tile as fp16 in the order of the decoded keys; each lane
+// gets its own row's factors.  D / 8 lanes to a row, so that a load takes whole lines.
 template <int D>
-__device__ __forceinline__ Row load_row(const AttendParams& p, const Item& it, int r, uint32_t tile, int row_in_tile) {
+__device__ __forceinline__ Row load_rows(const AttendParams& p, const Item& it, int r0, uint32_t tile, int row_in_tile0) {
+  constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+  const int lane = threadIdx.x & 31, c = lane % kLanes;
+  const int rows = it.n * p.group;
   Row o;
-  const int row = it.row0 + r, qi = row / p.group, head = it.h * p.group + row % p.group;
-  o.in = row < it.n * p.group;
-  o.limit = o.in ? it.len - it.n + qi : it.len - 1;
-  o.out = p.out + static_cast<size_t>(it.q0 + qi) * p.ld_out + static_cast<size_t>(head) * p.hd_out;
-  const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<size_t>(it.q0 + (o.in ? qi : 0)) * p.ld_q +
-                                                    static_cast<size_t>(o.in ? head : 0) * p.hd_q);
-  uint4 u[D / 8];
-  float top = 0.0f;
-  bool odd = false;
-#pragma unroll
-  for (int c = 0; c < D / 8; ++c) u[c] = o.in ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int c = 0; c < D / 8; ++c) {
-    const uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+  {
+    const int row = it.row0 + r0 + lane, qi = row / p.group;
+    o.in = row < rows;
+    o.limit = o.in ? it.len - it.n + qi : it.len - 1;
+    o.out = p.out + static_cast<size_t>(it.q0 + qi) * p.ld_out + static_cast<size_t>(it.h * p.group + row % p.group) * p.hd_out;
+  }
+  o.f = 1.0f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < 32; i0 += 8 * kAtOnce) {
+    uint4 u[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float x = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
-      top = fmaxf(top, fabsf(x));
-      odd = odd || !isfinite(x);
+      const int row = it.row0 + r0 + i0 + i * kAtOnce + lane / kLanes, qi = row / p.group;
+      u[i] = make_uint4(0, 0, 0, 0);
+      if (i0 + i * kAtOnce < 32 && row < rows)
+        u[i] = __ldg(reinterpret_cast<const uint4*>(p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q +
+                                                    static_cast<size_t>(it.h * p.group + row % p.group) * p.hd_q) + c);
     }
-  }
-  row_factors(top, odd, p.scale_log2, o.up, o.f);
 #pragma unroll
-  for (int c = 0; c < D / 8; ++c) {
-    const uint32_t v[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
-    float x[8];
+    for (int i = 0; i < 8; ++i) {
+      const int at = i0 + i * kAtOnce;                 // of the warp's rows
+      if (at >= 32) break;
+      const uint32_t v[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+      float x[8], top = 0.0f, up, f;
+      int odd = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16)) * o.up;
-    uint32_t h[4];
+      for (int n = 0; n < 8; ++n) {
+        x[n] = __uint_as_float((n & 1) ? (v[n / 2] & 0xffff0000u) : (v[n / 2] << 16));
+        top = fmaxf(top, fabsf(x[n]));
+        odd |= !isfinite(x[n]);
+      }
 #pragma unroll
-    for (int n = 0; n < 4; ++n) h[n] = as_u32(__floats2half2_rn(x[n], x[n + 4]));
-    st_shared_v4(chunk_at(tile, kRowTile, row_in_tile, c / 8, c % 8), make_uint4(h[0], h[1], h[2], h[3]));
+      for (int d = kLanes / 2; d > 0; d /= 2) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        odd |= __shfl_xor_sync(0xffffffffu, odd, d);
+      }
+      row_factors(top, odd != 0, p.scale_log2, up, f);
+      const float given = __shfl_sync(0xffffffffu, f, (lane - at) * kLanes & 31);      // row at + n is the lanes' from n kLanes on
+      if (lane >= at && lane < at + kAtOnce) o.f = given;
+      uint32_t h[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) h[n] = as_u32(__floats2half2_rn(x[n] * up, x[n + 4] * up));
+      st_shared_v4(chunk_at(tile, kRowTile, row_in_tile0 + at + lane / kLanes, c / 8, c % 8), make_uint4(h[0], h[1], h[2], h[3]));
+    }
   }
   return o;
 }
 
-// O's column c of a row is element 8 x + 4 e + n, c = (D / 4) n + (D / 8) e + x.
-template <int D>
-__device__ __forceinline__ void store_row(const Row& r, const float (&o)[D], float k) {
+// Columns [64 y, 64 y + 64) of O in the row's elements 64 y on: column 8 (4 e + n) + x is element 8 x + 4 e + n of them.
+__device__ __forceinline__ void store_half(const Row& r, int y, const float (&o)[64], float k) {
   if (!r.in) return;
 #pragma unroll
-  for (int x = 0; x < D / 8; ++x) {
+  for (int x = 0; x < 8; ++x) {
     uint32_t v[4];
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int n = 0; n < 4; n += 2) {
-        const int c = D / 4 * n + D / 8 * e + x;
-        const __nv_bfloat162 h = __floats2bfloat162_rn(o[c] * k, o[c + D / 4] * k);
-        v[2 * e + n / 2] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-    reinterpret_cast<uint4*>(r.out)[x] = make_uint4(v[0], v[1], v[2], v[3]);
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(o[16 * i + x] * k, o[16 * i + 8 + x] * k);
+      v[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    reinterpret_cast<uint4*>(r.out)[8 * y + x] = make_uint4(v[0], v[1], v[2], v[3]);
   }
+}
+
+// 2^a and 2^b without the special-function unit, which alone would take as long as the products: n the nearest integer, a
+// polynomial of degree 4 for 2^(a - n) (least relative error on [-1/2, 1/2], 2.6e-6), times 2^n.  NaN stays NaN.
+__device__ __forceinline__ void exp2_pair(float& a, float& b) {
+  asm("max.NaN.f32 %0, %0, 0fC2FA0000;\n\tmax.NaN.f32 %1, %1, 0fC2FA0000;" : "+f"(a), "+f"(b));      // -125
+  asm("{\n\t.reg .b64 y, t, n, r, q, c;\n\t.reg .f32 cf;\n\t.reg .b32 t0, t1;\n\t"
+      "mov.b64 y, {%0, %1};\n\t"
+      "mov.f32 cf, 0f4B400000;\n\tmov.b64 c, {cf, cf};\n\tadd.rn.f32x2 t, y, c;\n\t"
+      "mov.f32 cf, 0fCB400000;\n\tmov.b64 c, {cf, cf};\n\tadd.rn.f32x2 n, t, c;\n\t"
+      "mov.f32 cf, 0fBF800000;\n\tmov.b64 c, {cf, cf};\n\tfma.rn.f32x2 r, n, c, y;\n\t"
+      "mov.b64 q, {%2, %2};\n\tmov.b64 c, {%3, %3};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
+      "mov.b64 c, {%4, %4};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
+      "mov.b64 c, {%5, %5};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
+      "mov.b64 c, {%6, %6};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
+      "mov.b64 {t0, t1}, t;\n\tshl.b32 t0, t0, 23;\n\tadd.u32 t0, t0, 0x3f800000;\n\t"
+      "shl.b32 t1, t1, 23;\n\tadd.u32 t1, t1, 0x3f800000;\n\tmov.b64 c, {t0, t1};\n\t"
+      "mul.rn.f32x2 q, q, c;\n\tmov.b64 {%0, %1}, q;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(0.009570101276040077f), "f"(0.05591785907745361f), "f"(0.240247443318367f), "f"(0.6931217908859253f), "f"(0.9999992847442627f));
 }
 
 template <int D>
@@ -259,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(bars.k_full[i]), kDecoders); mbar_init(bar(bars.k_empty[i]), 1);
       mbar_init(bar(bars.v_full[i]), kDecoders); mbar_init(bar(bars.v_empty[i]), 1);
-      mbar_init(bar(bars.s_full[i]), 1); mbar_init(bar(bars.p_ready[i]), 4); mbar_init(bar(bars.q_full[i]), 4);
+      mbar_init(bar(bars.s_full[i]), 1); mbar_init(bar(bars.p_ready[i][0]), 4); mbar_init(bar(bars.p_ready[i][1]), 4); mbar_init(bar(bars.q_full[i]), 4);
       mbar_init(bar(bars.o_done[i]), 1); mbar_init(bar(bars.o_free[i]), 4);
     }
     mbar_init(bar(bars.joined), 8);
@@ -281,9 +315,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     volatile int* abort_at = &abort_flag;
     const auto wait = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.wait_ns); };
 
-    // 512 threads of 128 registers at launch: 256 of 72 and 256 of 184
+    // 512 threads of 128 registers at launch: 256 of 64 and 256 of 192
     if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     Pieces pc(Tiles::item_at(p, before, begin), begin, end);
     if (warp == 0) {
       // ---- loader: keys, then values of each tile; lanes 0 to 7 a unit each
@@ -321,56 +355,76 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
         for (int st = 0; st < S::kStages; ++st) mbar_wait_warp(bar(bars.code_full[st]), phase ^ (st < stage ? 0u : 1u), &none, p.wait_ns);
       }
     } else if (warp == 1) {
-      // ---- issuer
+      // ---- issuer: a warp whose loops are uniform (see mma_warp.cuh)
       const uint32_t leader = elect_one();
       constexpr uint32_t kQk = kIdesc<kKeys>, kPv = kIdesc<D>;
-      const auto s_at = [&](int x) { return tmem + x * kKeys; };
-      const auto o_at = [&](int x) { return tmem + 2 * kKeys + x * D; };
-      const auto product_qk = [&](int x, int buf) {
+      const uint32_t tm = warp_uniform(tmem);
+      const auto product_qk = [&](uint32_t x, uint32_t buf) {
+        const uint32_t s_at = tm + x * kKeys, q = base + S::kQ + x * S::kTileBytes, k0 = base + S::kK + buf * S::kTileBytes;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t at = (k / 4) * kKeys * 128 + (k % 4) * 32;
-          mma_ss(leader, s_at(x), desc_lo_sw128(base + S::kQ + x * S::kTileBytes + at), desc_lo_sw128(base + S::kK + buf * S::kTileBytes + at), kQk, k > 0);
+          mma_ss(leader, s_at, desc_lo_sw128(q + at), desc_lo_sw128(k0 + at), kQk, k > 0);
         }
         warp_commit(leader, bar(bars.s_full[x]));
       };
-      int t = 0;
-      int done[2] = {0, 0}, seen[2] = {0, 0};          // steps and items of each row tile
+      int buf = 0, done0 = 0, done1 = 0, seen0 = 0, seen1 = 0;           // steps and items of each row tile
+      uint32_t turn = 0;                                                 // of the two buffers
       bool fine = true;
-      while (fine && pc.next(p)) {
-        const int steps = pc.steps(), tiles = pc.two(p.group) ? 2 : 1;
-        fine = wait(bars.k_full[t & 1], t >> 1 & 1);
-        for (int x = 0; fine && x < tiles; ++x) {
-          fine = wait(bars.q_full[x], seen[x] & 1);
+      while (fine && warp_uniform(pc.next(p))) {
+        const int steps = warp_uniform(pc.steps());
+        const bool two = warp_uniform(pc.two(p.group)) != 0;
+        fine = wait(bars.k_full[buf], turn) && wait(bars.q_full[0], seen0 & 1);
+        if (!fine) break;
+        tc_fence_after();
+        product_qk(0, buf);
+        if (two) {
+          fine = wait(bars.q_full[1], seen1 & 1);
           if (!fine) break;
           tc_fence_after();
-          product_qk(x, t & 1);
-          if (x == tiles - 1) warp_commit(leader, bar(bars.k_empty[t & 1]));
+          product_qk(1, buf);
         }
-        for (int i = 0; fine && i < steps; ++i) {
-          const int now = t + i, buf = now & 1;
-          fine = wait(bars.v_full[buf], now >> 1 & 1);
-          for (int x = 0; fine && x < tiles; ++x) {
-            fine = wait(bars.p_ready[x], done[x] & 1) && (i > 0 || wait(bars.o_free[x], (seen[x] & 1) ^ 1));
+        warp_commit(leader, bar(bars.k_empty[buf]));
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+          const int next = buf ^ 1;
+          const uint32_t next_turn = turn ^ (buf == 1 ? 1u : 0u);
+          fine = wait(bars.v_full[buf], turn);
+          if (!fine) break;
+#pragma unroll 1
+          for (int x = 0; x < (two ? 2 : 1); ++x) {
+            const uint32_t ready = (x == 0 ? done0++ : done1++) & 1;
+            fine = wait(bars.p_ready[x][0], ready) && (i > 0 || wait(bars.o_free[x], ((x == 0 ? seen0 : seen1) & 1) ^ 1));
             if (!fine) break;
-            ++done[x];
+            tc_fence_after();
+            const uint32_t o_at = tm + 2 * kKeys + x * D, s_at = tm + x * kKeys, v0 = base + S::kV + buf * S::kTileBytes;
+            const uint32_t add = i > 0 ? 1u : 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_ts(leader, o_at, s_at + k * 8, desc_lo_sw128(v0 + k * 32), kPv, k > 0 ? 1u : add);
+            fine = wait(bars.p_ready[x][1], ready);
+            if (!fine) break;
             tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              mma_ts(leader, o_at(x), s_at(x) + k * 8, desc_lo_sw128(base + S::kV + buf * S::kTileBytes + (k / 4) * D * 128 + (k % 4) * 32), kPv,
-                     i > 0 || k > 0);
+            for (int k = 0; k < 4; ++k) mma_ts(leader, o_at, s_at + 32 + k * 8, desc_lo_sw128(v0 + D * 128 + k * 32), kPv, 1u);
+            const bool last = x == (two ? 1 : 0);
             if (i == steps - 1) warp_commit(leader, bar(bars.o_done[x]));
-            if (x == tiles - 1) warp_commit(leader, bar(bars.v_empty[buf]));
+            if (last) warp_commit(leader, bar(bars.v_empty[buf]));
             if (i + 1 < steps) {
-              if (x == 0) fine = wait(bars.k_full[buf ^ 1], (now + 1) >> 1 & 1);
-              if (!fine) break;
-              product_qk(x, buf ^ 1);
-              if (x == tiles - 1) warp_commit(leader, bar(bars.k_empty[buf ^ 1]));
+              if (x == 0) {
+                fine = wait(bars.k_full[next], next_turn);
+                if (!fine) break;
+                tc_fence_after();
+              }
+              product_qk(x, next);
+              if (last) warp_commit(leader, bar(bars.k_empty[next]));
             }
           }
+          if (!fine) break;
+          buf = next;
+          turn = next_turn;
         }
-        for (int x = 0; x < tiles; ++x) ++seen[x];
-        t += steps;
+        ++seen0;
+        if (two) ++seen1;
       }
     } else {
       // ---- decoders
@@ -400,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       }
     }
     } else {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
       Pieces pc(Tiles::item_at(p, before, begin), begin, end);
       // ---- softmax: warpgroup x on row tile x, thread by row
       const int x = (warp - 8) >> 2, row = (warp & 3) * 32 + lane, r = x * kRowTile + row;
@@ -418,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       Row mine;
       const auto load = [&](const Pieces& c) {
         if (x == 1 && !c.two(p.group)) return;
-        mine = load_row<D>(p, c.it, r, q_tile, row);
+        mine = load_rows<D>(p, c.it, r - lane, q_tile, row - lane);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(bars.q_full[x]));
@@ -429,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
         const Item it = pc.it;
         const int steps = pc.steps(), tile0 = pc.tile0();
         const bool active = x == 0 || pc.two(p.group);
-        float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+        float m = -INFINITY, l[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
         const Row cur = mine;
         if (active) {
           for (int i = 0; i < steps; ++i) {
@@ -440,32 +494,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
             const int k0 = (tile0 + i) * kKeys;
             const int see = cur.limit - k0;
             const bool masked = __any_sync(0xffffffffu, see < kKeys - 1);
-            const auto scores = [&](int b, uint32_t (&c)[32]) {          // 32 of the row's scores; -inf where it does not see
-              tmem_ld32(s_at + 32 * b, c);
-              tmem_wait_ld();
-              if (masked) {
+            uint32_t c[4][32];
 #pragma unroll
-                for (int v = 0; v < 32; ++v)
-                  if (32 * b + v > see) c[v] = 0xff800000u;
-              }
-            };
+            for (int b = 0; b < 4; ++b) tmem_ld32(s_at + 32 * b, c[b]);
+            tmem_wait_ld();
+            if (masked) {
+#pragma unroll
+              for (int v = 0; v < 128; ++v)
+                if (v > see) c[v / 32][v % 32] = 0xff800000u;
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              uint32_t c[32];
-              scores(b, c);
-#pragma unroll
-              for (int v = 0; v < 32; v += 2) top = fmaxf(top, fmaxf(__uint_as_float(c[v]), __uint_as_float(c[v + 1])));
-            }
+            for (int v = 0; v < 128; v += 2)
+              top = fmaxf(top, fmaxf(__uint_as_float(c[v / 32][v % 32]), __uint_as_float(c[v / 32][v % 32 + 1])));
             top *= cur.f;
             if (__any_sync(0xffffffffu, top > m + kSlack)) {
               const float to = top > m + kSlack ? top : m;
               const float k = to == m ? 1.0f : exp2_fast(m - to);
               m = to;
-              l0 *= k;
-              l1 *= k;
+              l[0][0] *= k; l[0][1] *= k; l[1][0] *= k; l[1][1] *= k;
               if (i > 0) {                             // S of this step is there: the products into O before it are done
-#pragma unroll
+#pragma unroll 1
                 for (int b = 0; b < D / 32; ++b) {
                   uint32_t o[32];
                   tmem_ld32(o_at + 32 * b, o);
@@ -482,67 +531,69 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
             for (int h = 0; h < 2; ++h) {              // S's columns 64 h to 64 h + 63 become P's 32 h to 32 h + 31
               uint32_t w[32];
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                uint32_t c[32];
-                scores(2 * h + y, c);
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                  float a = __uint_as_float(c[2 * v]), b = __uint_as_float(c[2 * v + 1]);
-                  fma_pair(a, b, cur.f, less);
+              for (int v = 0; v < 32; ++v) {
+                float a = __uint_as_float(c[2 * h + v / 16][v % 16 * 2]), b = __uint_as_float(c[2 * h + v / 16][v % 16 * 2 + 1]);
+                fma_pair(a, b, cur.f, less);
+                if (v % kEvery == kEvery - 1) {
+                  exp2_pair(a, b);
+                } else {
                   a = exp2_fast(a);
                   b = exp2_fast(b);
-                  add_pair(l0, l1, a, b);
-                  w[16 * y + v] = as_u32(__floats2half2_rn(a, b));
                 }
+                add_pair(l[v & 1][0], l[v & 1][1], a, b);
+                w[v] = as_u32(__floats2half2_rn(a, b));
               }
               tmem_st32(s_at + 32 * h, w);
+              tmem_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(bars.p_ready[x][h]));
             }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(bars.p_ready[x]));
           }
           if (!fine) break;
         }
         more = pc.next(p);
         if (more) load(pc);                            // the next item's queries: every product with these is done
 
-        const float l = l0 + l1;
-        float o[D];
-        if (active) {
-          fine = wait(bars.o_done[x], seen & 1);
-          if (!fine) break;
-          tc_fence_after();
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) {
-            uint32_t v[32];
-            tmem_ld32(o_at + 32 * b, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[32 * b + i] = __uint_as_float(v[i]);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(bars.o_free[x]));
-          ++seen;
-        }
+        const float sum = (l[0][0] + l[0][1]) + (l[1][0] + l[1][1]);
         const int first = runs.of(it.begin), ctas = runs.of(it.begin + it.tiles - 1) - first + 1;
-        if (ctas == 1) {
-          if (active) store_row<D>(cur, o, l == 0.0f ? 0.0f : 1.0f / l);
-          continue;
-        }
-        // A cut item: this CTA's part goes to the workspace, four columns of a row to a 16-byte line of 256 rows; the CTA that
-        // arrives last adds the parts up in their order.
+        // A cut item's parts go to the workspace, four columns of a row to a 16-byte line of 256 rows; the CTA that arrives last adds
+        // them up in their order.
         const auto part_of = [&](int cta) { return static_cast<size_t>(cta) * 2 + (cta == first && it.begin > runs.begin(cta) ? 1 : 0); };
         float4* parts = reinterpret_cast<float4*>(p.part);
         float2* stats = reinterpret_cast<float2*>(p.stats);
         if (active) {
+          fine = wait(bars.o_done[x], seen & 1);
+          if (!fine) break;
+          tc_fence_after();
+          const float k = sum == 0.0f ? 0.0f : 1.0f / sum;
           const size_t at = part_of(blockIdx.x);
-          __stcg(stats + at * kRows + r, make_float2(m, l));
+          if (ctas > 1) __stcg(stats + at * kRows + r, make_float2(m, sum));
+#pragma unroll 1
+          for (int y = 0; y < D / 64; ++y) {
+            uint32_t v[2][32];
+            tmem_ld32(o_at + 64 * y, v[0]);
+            tmem_ld32(o_at + 64 * y + 32, v[1]);
+            tmem_wait_ld();
+            if (y == D / 64 - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(bars.o_free[x]));
+            }
+            float o[64];
 #pragma unroll
-          for (int q = 0; q < D / 4; ++q)
-            __stcg(parts + (at * (D / 4) + q) * kRows + r, make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]));
+            for (int i = 0; i < 64; ++i) o[i] = __uint_as_float(v[i / 32][i % 32]);
+            if (ctas == 1) {
+              store_half(cur, y, o, k);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                __stcg(parts + (at * (D / 4) + 16 * y + q) * kRows + r, make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]));
+            }
+          }
+          ++seen;
         }
+        if (ctas == 1) continue;
         __threadfence();
         fine = sync_softmax();
         if (!fine) break;
@@ -555,24 +606,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
         if (!fine) break;
         if (s_last && active) {
           __threadfence();
-          float top = -INFINITY;
+          float top = -INFINITY, all = 0.0f;
           for (int c = 0; c < ctas; ++c) top = fmaxf(top, __ldcg(stats + part_of(first + c) * kRows + r).x);
           const float ref = top == -INFINITY ? 0.0f : top;
-          float sum = 0.0f;
-#pragma unroll
-          for (int q = 0; q < D; ++q) o[q] = 0.0f;
           for (int c = 0; c < ctas; ++c) {
-            const size_t at = part_of(first + c);
-            const float2 st = __ldcg(stats + at * kRows + r);
-            const float k = exp2_fast(st.x - ref);
-            sum += st.y * k;
-#pragma unroll
-            for (int q = 0; q < D / 4; ++q) {
-              const float4 v = __ldcg(parts + (at * (D / 4) + q) * kRows + r);
-              o[4 * q] += v.x * k; o[4 * q + 1] += v.y * k; o[4 * q + 2] += v.z * k; o[4 * q + 3] += v.w * k;
-            }
+            const float2 st = __ldcg(stats + part_of(first + c) * kRows + r);
+            all += st.y * exp2_fast(st.x - ref);
           }
-          store_row<D>(cur, o, sum == 0.0f ? 0.0f : 1.0f / sum);
+#pragma unroll 1
+          for (int y = 0; y < D / 64; ++y) {
+            float o[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) o[i] = 0.0f;
+#pragma unroll 1
+            for (int c = 0; c < ctas; ++c) {
+              const size_t at = part_of(first + c);
+              const float k = exp2_fast(__ldcg(stats + at * kRows + r).x - ref);
+              float4 v[16];
+#pragma unroll
+              for (int q = 0; q < 16; ++q) v[q] = __ldcg(parts + (at * (D / 4) + 16 * y + q) * kRows + r);
+#pragma unroll
+              for (int q = 0; q < 16; ++q) {
+                o[4 * q] += v[q].x * k; o[4 * q + 1] += v[q].y * k; o[4 * q + 2] += v[q].z * k; o[4 * q + 3] += v[q].w * k;
+              }
+            }
+            store_half(cur, y, o, all == 0.0f ? 0.0f : 1.0f / all);
+          }
         }
         fine = sync_softmax();                         // s_last is read before the next item's is written
       }
