@@ -617,6 +617,7 @@ static int check_cache(const tempo_cache* c) {
   if (c->n_pages <= 0 || c->Hkv <= 0) return TEMPO_ERR_SHAPE;
   if ((c->D != 64 && c->D != 128) || c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return TEMPO_ERR_UNSUPPORTED;
   if (static_cast<long long>(c->n_pages) * c->page_size > 0x7fffffffll || c->Hkv > 65536) return TEMPO_ERR_UNSUPPORTED;
+  if (9.0 * c->D * c->page_size / 8 * c->Hkv * c->n_pages > 1e12) return TEMPO_ERR_UNSUPPORTED;   // units are numbered in 32 bits
   return TEMPO_OK;
 }
 

@@ -22,18 +22,17 @@ namespace tempo {
 
 namespace {
 
-constexpr int kWarps = 8, kTile = 64, kUnits = kTile / kUnit, kRows = 16;
-
-using Tiles = Cut<kRows, kTile>;
-using Item = Tiles::Item;
-
-struct Part {                 // a cut item's share of one warp
-  Item item;
-  int valid;
-};
-
-template <int D>
-struct AttendSmem {
+// The kernel's form for items of 8 NR rows.
+template <int D_, int NR_>
+struct Few {
+  static constexpr int D = D_, NR = NR_, kRows = 8 * NR, kTile = 32, kUnits = kTile / kUnit;
+  static constexpr int kWarps = NR == 1 ? 16 : 12;
+  using Tiles = Cut<kRows, kTile>;
+  using Item = typename Tiles::Item;
+  struct Part {               // a cut item's share of one warp
+    Item item;
+    int valid;
+  };
   static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // keys and values of each unit
   static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
@@ -46,9 +45,15 @@ struct AttendSmem {
   static int bytes(int B) { return kBefore + (B + 1) * 4; }
 };
 
-__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of 16-bit numbers, two neighbours of row lane / 4 in each lane, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
 }
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* a, uint32_t (&v)[W]) {
@@ -62,35 +67,34 @@ __device__ __forceinline__ void load_words(const uint8_t* a, uint32_t (&v)[W]) {
 }
 
 // Float4 number q (of D / 4) of a row in a part: rotated so that the eight lanes of a store's phase meet eight bank groups.
-__device__ __forceinline__ int part_at(int row, int q) { return q ^ ((((row & 1) << 2) | ((q >> 3) & 3)) & 7); }
+__device__ __forceinline__ int part_at(int row, int q) { return q ^ (row >> 1 & 3); }
 
-// A warp's running state of one item.
-template <int D>
+// A warp's running state of one item.  Lane (g, j) = (lane / 4, lane % 4) keeps the rows 2 j and 2 j + 1 of each eight.
+template <class F>
 struct Running {
-  static constexpr int kN = D / 8;                   // 8-column tiles of O
-  uint32_t q[D / 16][4];                             // A operands: rows lane / 4 and + 8
-  float f[2];                                        // score = f * (sum of products), in units of log2; above zero
-  int limit[2], least;                               // last token that each row sees; the least over the 16 rows
-  float m[2];
-  float l[4];                                        // the sums of the weights, one more column of O: rows in l[0] and l[2]
-  float o[kN][4];
+  static constexpr int kN = F::D / 16;               // products with 16 elements of a value row
+  uint32_t q[F::NR][F::D / 16][2];                   // B operands of the scores: row g, elements j D/4 to (j+1) D/4 - 1
+  float f[F::NR][2];                                 // score = f * (sum of products), in units of log2; above zero
+  int limit[F::NR][2], least;                        // last token that each row sees; the least over all rows
+  float m[F::NR][2];
+  float l[F::NR][4];                                 // sums of the weights: rows in [0] and [1]
+  float o[F::NR][kN][4];                             // elements g D/8 + 2 i (in [0], [1]) and + 2 i + 1 (in [2], [3])
 };
 
-template <int D>
-__device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it, Running<D>& s) {
-  constexpr int W = D / 32;                          // 8-element words of a lane
-  const int lane = threadIdx.x & 31, j = lane & 3;
+template <class F>
+__device__ __forceinline__ void begin_item(const AttendParams& p, const typename F::Item& it, Running<F>& s) {
+  constexpr int W = F::D / 32;                       // 8-element words of a lane
+  const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
   const int rows = it.n * p.group;
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = it.row0 + lane / 4 + 8 * half;
+  for (int r = 0; r < F::NR; ++r) {
+    const int row = it.row0 + 8 * r + g;
     const bool in = row < rows;
-    const int qi = row / p.group, head = it.h * p.group + row % p.group;
-    s.limit[half] = in ? it.len - it.n + qi : it.len - 1;
+    const int qi = in ? row / p.group : 0, head = in ? it.h * p.group + row - qi * p.group : 0;
     float x[W][8];
     float top = 0.0f;
     bool odd = false;
-    const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + (in ? qi : 0)) * p.ld_q + static_cast<size_t>(in ? head : 0) * p.hd_q + j * (D / 4);
+    const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q + static_cast<size_t>(head) * p.hd_q + j * (F::D / 4);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const uint4 u = in ? __ldg(reinterpret_cast<const uint4*>(src) + w) : make_uint4(0, 0, 0, 0);
@@ -107,167 +111,204 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const Item& it
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
       odd = __shfl_xor_sync(0xffffffffu, static_cast<int>(odd), d) != 0 || odd;
     }
-    float up;
-    row_factors(top, odd, p.scale_log2, up, s.f[half]);
+    float up, f;
+    row_factors(top, odd, p.scale_log2, up, f);
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {                  // the pairs (n, n + 4) of decode8, two to a matrix instruction
-        s.q[2 * w + u][half] = as_u32(__floats2half2_rn(x[w][2 * u] * up, x[w][2 * u + 4] * up));
-        s.q[2 * w + u][half + 2] = as_u32(__floats2half2_rn(x[w][2 * u + 1] * up, x[w][2 * u + 5] * up));
+        s.q[r][2 * w + u][0] = as_u32(__floats2half2_rn(x[w][2 * u] * up, x[w][2 * u + 4] * up));
+        s.q[r][2 * w + u][1] = as_u32(__floats2half2_rn(x[w][2 * u + 1] * up, x[w][2 * u + 5] * up));
       }
-    s.m[half] = -INFINITY;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      s.f[r][y] = __shfl_sync(0xffffffffu, f, (2 * j + y) * 4);
+      const int mine = it.row0 + 8 * r + 2 * j + y;
+      s.limit[r][y] = it.len - it.n + min(mine / p.group, it.n - 1);
+      s.m[r][y] = -INFINITY;
+    }
+    s.l[r][0] = s.l[r][1] = s.l[r][2] = s.l[r][3] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Running<F>::kN; ++i) { s.o[r][i][0] = s.o[r][i][1] = s.o[r][i][2] = s.o[r][i][3] = 0.0f; }
   }
   s.least = it.len - it.n + it.row0 / p.group;
-  s.l[0] = s.l[1] = s.l[2] = s.l[3] = 0.0f;
-#pragma unroll
-  for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][0] = s.o[i][1] = s.o[i][2] = s.o[i][3] = 0.0f; }
 }
 
-// One tile: tokens [t0, t0 + 64) of the item at `stage`.  `absent`: bits of its units whose page is not in the cache.
-template <int D>
-__device__ __forceinline__ void run_tile(Running<D>& s, const uint8_t* stage, int t0, int len, uint32_t absent) {
-  using U = CacheUnit<D>;
-  constexpr int W = D / 32, kCols = kTile / 8;
+// One tile: tokens [t0, t0 + kTile) of the item at `stage`.  `absent`: bits of its units whose page is not in the cache.
+template <class F>
+__device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const uint8_t* stage, int t0, int len, uint32_t absent) {
+  using U = CacheUnit<F::D>;
+  constexpr int D = F::D, W = D / 32, NR = F::NR;
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  float c[kCols][4];
+  float c[F::kUnits][NR][4];                         // scores of the tokens 16 k + g (in [0], [1]) and + 8, rows 2 j and 2 j + 1
+  {
+    uint32_t w[F::kUnits][2][W], sc[F::kUnits][2], b[F::kUnits][2];
 #pragma unroll
-  for (int k = 0; k < kUnits; ++k) {                 // scores of unit k: two chains of matrix instructions side by side
-    const uint8_t* unit = stage + k * 2 * U::kBytes;
-    uint32_t w[2][W], sc[2], b[2];
+    for (int k = 0; k < F::kUnits; ++k) {
+      const uint8_t* unit = stage + k * 2 * U::kBytes;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      c[2 * k + x][0] = c[2 * k + x][1] = c[2 * k + x][2] = c[2 * k + x][3] = 0.0f;
-      const int at = x * 8 + g;
-      load_words<W>(unit + at * U::kKeyRow + j * (D / 8), w[x]);
-      group_params(*reinterpret_cast<const uint16_t*>(unit + U::kCodes + at * U::kKeyParams + (D == 128 ? j : j / 2) * 2) * 0x10001u, sc[x], b[x]);
+      for (int x = 0; x < 2; ++x) {
+        const int at = x * 8 + g;
+        load_words<W>(unit + at * U::kKeyRow + j * (D / 8), w[k][x]);
+        group_params(*reinterpret_cast<const uint16_t*>(unit + U::kCodes + at * U::kKeyParams + (D == 128 ? j : j / 2) * 2) * 0x10001u,
+                     sc[k][x], b[k][x]);
+      }
+#pragma unroll
+      for (int r = 0; r < NR; ++r) c[k][r][0] = c[k][r][1] = c[k][r][2] = c[k][r][3] = 0.0f;
     }
 #pragma unroll
-    for (int y = 0; y < W; ++y) {
-      uint32_t v[2][4];
+    for (int y = 0; y < W; ++y)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) decode8(w[x][y], sc[x], b[x], v[x]);
+      for (int k = 0; k < F::kUnits; ++k) {
+        uint32_t v[2][4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int x = 0; x < 2; ++x) decode8(dc, w[k][x][y], sc[k][x], b[k][x], v[x]);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) mma_f16(c[2 * k + x], s.q[2 * y + u], v[x][2 * u], v[x][2 * u + 1]);
-    }
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            mma_f16(c[k][r], v[0][2 * u], v[1][2 * u], v[0][2 * u + 1], v[1][2 * u + 1], s.q[r][2 * y + u][0], s.q[r][2 * y + u][1]);
+      }
   }
   if (absent != 0) {
 #pragma unroll
-    for (int i = 0; i < kCols; ++i)
-      if (absent >> (i / 2) & 1) c[i][0] = c[i][1] = c[i][2] = c[i][3] = __uint_as_float(0x7fc00000u);
+    for (int k = 0; k < F::kUnits; ++k)
+      if (absent >> k & 1) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) c[k][r][0] = c[k][r][1] = c[k][r][2] = c[k][r][3] = __uint_as_float(0x7fc00000u);
+      }
   }
-  if (t0 + kTile - 1 > s.least) {
+  if (t0 + F::kTile - 1 > s.least) {
 #pragma unroll
-    for (int i = 0; i < kCols; ++i)
+    for (int k = 0; k < F::kUnits; ++k)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        if (t0 + 8 * i + 2 * j + (x & 1) > s.limit[x / 2]) c[i][x] = -INFINITY;
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (t0 + 16 * k + 8 * (x / 2) + g > s.limit[r][x & 1]) c[k][r][x] = -INFINITY;
   }
-  float top[2] = {-INFINITY, -INFINITY};
+  bool raise = false;
+  float top[NR][2];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < NR; ++r)
 #pragma unroll
-    for (int i = 0; i < kCols; ++i) top[r] = fmaxf(top[r], fmaxf(c[i][2 * r], c[i][2 * r + 1]));
-    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-    top[r] *= s.f[r];
-  }
-  // a maximum that has grown little stays: weights up to 2^15 are in fp16's range, and O is left alone
-  if (__any_sync(0xffffffffu, top[0] > s.m[0] + kSlack || top[1] > s.m[1] + kSlack)) {
+    for (int y = 0; y < 2; ++y) {
+      float t = fmaxf(c[0][r][y], c[0][r][y + 2]);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const float m = top[r] > s.m[r] + kSlack ? top[r] : s.m[r];
-      const float k = m == s.m[r] ? 1.0f : exp2_fast(s.m[r] - m);
-      s.m[r] = m;
-      s.l[2 * r] *= k;
-#pragma unroll
-      for (int i = 0; i < Running<D>::kN; ++i) { s.o[i][2 * r] *= k; s.o[i][2 * r + 1] *= k; }
+      for (int k = 1; k < F::kUnits; ++k) t = fmaxf(t, fmaxf(c[k][r][y], c[k][r][y + 2]));
+      top[r][y] = t * s.f[r][y];
+      raise = raise || top[r][y] > s.m[r][y] + kSlack;
     }
+  // A maximum that has grown little stays: weights up to 2^15 are in fp16's range, and O is left alone.
+  if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        float t = top[r][y];
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+        const float m = t > s.m[r][y] + kSlack ? t : s.m[r][y];
+        const float k = m == s.m[r][y] ? 1.0f : exp2_fast(s.m[r][y] - m);
+        s.m[r][y] = m;
+        s.l[r][y] *= k;
+#pragma unroll
+        for (int i = 0; i < Running<F>::kN; ++i) { s.o[r][i][y] *= k; s.o[r][i][y + 2] *= k; }
+      }
   }
-  uint32_t a[kUnits][4];
+  uint32_t w8[F::kUnits][NR][2];                     // B operands of the output: row g, tokens 2 j, + 1 and 8 + 2 j, + 1 of unit k
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const float m = s.m[r] == -INFINITY ? 0.0f : kBias - s.m[r];
+  for (int r = 0; r < NR; ++r) {
+    float less[2];
 #pragma unroll
-    for (int i = 0; i < kCols; ++i)
-      a[i / 2][(i & 1) * 2 + r] =
-          as_u32(__floats2half2_rn(exp2_fast(fmaf(c[i][2 * r], s.f[r], m)), exp2_fast(fmaf(c[i][2 * r + 1], s.f[r], m))));
+    for (int y = 0; y < 2; ++y) less[y] = s.m[r][y] == -INFINITY ? 0.0f : kBias - s.m[r][y];
+#pragma unroll
+    for (int k = 0; k < F::kUnits; ++k)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        w8[k][r][x] = transpose8(as_u32(__floats2half2_rn(exp2_fast(fmaf(c[k][r][2 * x], s.f[r][0], less[0])),
+                                                          exp2_fast(fmaf(c[k][r][2 * x + 1], s.f[r][1], less[1])))));
   }
+  const bool tail = t0 + F::kTile > len;
 #pragma unroll
-  for (int k = 0; k < kUnits; ++k) {                 // unit k: tokens 16 k + 2 j, + 1 and 16 k + 8 + 2 j, + 1
+  for (int k = 0; k < F::kUnits; ++k) {
     const uint8_t* unit = stage + (k * 2 + 1) * U::kBytes;
     uint32_t w[2][W], sc[2], b[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
+    for (int x = 0; x < 2; ++x) {                    // tokens 16 k + 2 pair, + 1
       const int pair = 4 * x + j;
       load_words<W>(unit + pair * U::kPairRow + g * (D / 8), w[x]);
       uint32_t params = *reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4);
-      const int left = len - (t0 + 16 * k + 2 * pair);           // tokens of the pair that exist: what lies behind may be anything
-      if (left < 2) params &= left == 1 ? 0xffffu : 0u;
+      if (tail) {                                    // tokens that do not exist: what lies there may be anything
+        const int left = len - (t0 + 16 * k + 2 * pair);
+        if (left < 2) params &= left == 1 ? 0xffffu : 0u;
+      }
       group_params(params, sc[x], b[x]);
     }
-    mma_f16(s.l, a[k], 0x3c003c00u, 0x3c003c00u);    // times 1: the sum is that of the weights as they meet V
+#pragma unroll
+    for (int r = 0; r < NR; ++r)                     // times 1: the sum is that of the weights as they meet V
+      mma_f16(s.l[r], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, w8[k][r][0], w8[k][r][1]);
 #pragma unroll
     for (int y = 0; y < W; ++y) {
       uint32_t v0[4], v1[4];
-      decode8(w[0][y], sc[0], b[0], v0);
-      decode8(w[1][y], sc[1], b[1], v1);
+      decode8(dc, w[0][y], sc[0], b[0], v0);
+      decode8(dc, w[1][y], sc[1], b[1], v1);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) mma_f16(s.o[4 * y + n], a[k], v0[n], v1[n]);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          mma_f16(s.o[r][2 * y + h], v0[2 * h], v0[2 * h + 1], v1[2 * h], v1[2 * h + 1], w8[k][r][0], w8[k][r][1]);
     }
   }
 }
 
+template <class Item>
 __device__ __forceinline__ __nv_bfloat16* out_row(const AttendParams& p, const Item& it, int row) {
   const int r = it.row0 + row;
   return p.out + static_cast<size_t>(it.q0 + r / p.group) * p.ld_out + static_cast<size_t>(it.h * p.group + r % p.group) * p.hd_out;
 }
 
-// A whole item's result from the registers.  Lane (g, j) has, of the rows g and g + 8, the elements j D/4 to (j+1) D/4 - 1: O tile i
-// holds element i of each of the eight runs of D / 8.
-template <int D>
-__device__ __forceinline__ void store_item(const AttendParams& p, const Item& it, Running<D>& s) {
+// A whole item's result from the registers: of its rows a lane has the elements g D/8 to (g+1) D/8 - 1.
+template <class F>
+__device__ __forceinline__ void store_item(const AttendParams& p, const typename F::Item& it, Running<F>& s) {
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    if (it.row0 + g + 8 * r >= it.n * p.group) continue;
-    const float k = s.l[2 * r] == 0.0f ? 0.0f : 1.0f / s.l[2 * r];
-    uint4* dst = reinterpret_cast<uint4*>(out_row(p, it, g + 8 * r) + j * (D / 4));
+  for (int r = 0; r < F::NR; ++r)
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < 2; ++y) {
+      const int row = 8 * r + 2 * j + y;
+      if (it.row0 + row >= it.n * p.group) continue;
+      const float k = s.l[r][y] == 0.0f ? 0.0f : 1.0f / s.l[r][y];
+      uint4* dst = reinterpret_cast<uint4*>(out_row(p, it, row) + g * (F::D / 8));
 #pragma unroll
-      for (int i = 0; i < Running<D>::kN; i += 8) {
+      for (int i = 0; i < Running<F>::kN; i += 4) {
         uint32_t v[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(s.o[i + 2 * x][2 * r + y] * k, s.o[i + 2 * x + 1][2 * r + y] * k);
+          const __nv_bfloat162 h = __floats2bfloat162_rn(s.o[r][i + x][y] * k, s.o[r][i + x][y + 2] * k);
           v[x] = *reinterpret_cast<const uint32_t*>(&h);
         }
-        dst[(y * Running<D>::kN + i) / 8] = make_uint4(v[0], v[1], v[2], v[3]);
+        dst[i / 4] = make_uint4(v[0], v[1], v[2], v[3]);
       }
-  }
+    }
 }
 
-template <int D>
-__device__ __forceinline__ void keep_part(Running<D>& s, uint8_t* part) {
+template <class F>
+__device__ __forceinline__ void keep_part(Running<F>& s, uint8_t* part) {
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
   float4* o = reinterpret_cast<float4*>(part);
-  float2* stat = reinterpret_cast<float2*>(part + kRows * D * 4);
+  float2* stat = reinterpret_cast<float2*>(part + F::kRows * F::D * 4);
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int row = g + 8 * r;
-    if (j == 0) stat[row] = make_float2(s.m[r], s.l[2 * r]);
+  for (int r = 0; r < F::NR; ++r)
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < 2; ++y) {
+      const int row = 8 * r + 2 * j + y;
+      if (g == 0) stat[row] = make_float2(s.m[r][y], s.l[r][y]);
 #pragma unroll
-      for (int i = 0; i < Running<D>::kN; i += 4) {
-        const int q = j * (D / 16) + (y * Running<D>::kN + i) / 4;
-        o[row * (D / 4) + part_at(row, q)] =
-            make_float4(s.o[i][2 * r + y], s.o[i + 1][2 * r + y], s.o[i + 2][2 * r + y], s.o[i + 3][2 * r + y]);
-      }
-  }
+      for (int i = 0; i < Running<F>::kN; i += 2)
+        o[row * (F::D / 4) + part_at(row, g * (F::D / 32) + i / 2)] =
+            make_float4(s.o[r][i][y], s.o[r][i][y + 2], s.o[r][i + 1][y], s.o[r][i + 1][y + 2]);
+    }
 }
 
 __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 v, float k) {
@@ -281,28 +322,30 @@ struct Segment {              // neighbouring parts of one item in this CTA
   int last;                   // this CTA is the last of them to arrive
 };
 
-template <int D>
-__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p) {
+template <class F>
+__global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p) {
   extern __shared__ __align__(128) uint8_t smem[];
-  using S = AttendSmem<D>;
-  using U = CacheUnit<D>;
+  using Item = typename F::Item;
+  using Tiles = typename F::Tiles;
+  using U = CacheUnit<F::D>;
+  constexpr int D = F::D, kWarps = F::kWarps, kRows = F::kRows, kTile = F::kTile;
   __shared__ int warp_sum[kWarps];
   __shared__ Segment segments[kWarps + 1];
   __shared__ int n_segments, abort_flag;
-  int* before = reinterpret_cast<int*>(smem + S::kBefore);
-  Part* records = reinterpret_cast<Part*>(smem + S::kRecords);
+  int* before = reinterpret_cast<int*>(smem + F::kBefore);
+  typename F::Part* records = reinterpret_cast<typename F::Part*>(smem + F::kRecords);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t bars = smem_u32(smem + S::kBars) + warp * S::kStages * 8;
-  const uint8_t* ring = smem + warp * S::kStages * S::kStageBytes;
+  const uint32_t bars = smem_u32(smem + F::kBars) + warp * F::kStages * 8;
+  const uint8_t* ring = smem + warp * F::kStages * F::kStageBytes;
 
   pdl_trigger();
-  if (lane < S::kStages) mbar_init(bars + 8 * lane, 1);
+  if (lane < F::kStages) mbar_init(bars + 8 * lane, 1);
   if (tid == 0) { abort_flag = 0; n_segments = 0; }
   if (lane < 2) records[2 * warp + lane].valid = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_wait();
 
-  const int total = Tiles::count_tiles<kWarps>(p, before, warp_sum, blockIdx.x == 0);
+  const int total = Tiles::template count_tiles<kWarps>(p, before, warp_sum, blockIdx.x == 0);
   if (total == 0) return;
 
   const int n_runs = min(total, static_cast<int>(gridDim.x) * kWarps);
@@ -316,40 +359,46 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     Item it = Tiles::item_at(p, before, begin);
     Item ahead = it;                                 // the item of the next tile to be requested
     int asked = begin;
-    uint32_t absent_bits = 0;                        // four bits per stage
-    // Lanes 0 to 7 each fetch one unit's keys or values.  The page numbers are read one request ahead.
-    const int my_unit = lane >> 1;
-    const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
+    uint32_t absent_bits = 0;                        // kUnits bits per stage
+    // The first 2 kUnits lanes each fetch one unit's keys or values.  The page numbers are read one request ahead.
+    const int my_unit = lane >> 1, unit_shift = p.page_shift - 4;
     const auto look = [&](int tile) {                // tile of the item `ahead`
       const int t = tile * kTile + my_unit * kUnit;
-      return lane < 2 * kUnits && t < ahead.len ? p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + (t >> p.page_shift)] : -1;
+      return lane < 2 * F::kUnits && t < ahead.len ? p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + (t >> p.page_shift)] : 0;
     };
     int page = look(asked - ahead.begin);
     const auto request = [&](int stage) {
-      const int tile = asked - ahead.begin, t = tile * kTile + my_unit * kUnit;
-      const bool wanted = lane < 2 * kUnits && t < ahead.len;
+      const int tile = asked - ahead.begin, unit = tile * F::kUnits + my_unit;
+      const int units = min(F::kUnits, max(0, (ahead.len - tile * kTile + kUnit - 1) / kUnit));
       const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
-      const uint8_t* src = p.cache + ((static_cast<size_t>(there ? page : 0) * p.Hkv + ahead.h) * 2 + (lane & 1)) * head_bytes +
-                           ((t & (p.page_size - 1)) / kUnit) * U::kBytes;
-      const uint32_t want = __ballot_sync(0xffffffffu, wanted), gone = __ballot_sync(0xffffffffu, wanted && !there);
+      const uint32_t gone = __ballot_sync(0xffffffffu, !there);
+      // units are numbered in 32 bits: a cache has less than 2^32 of them
+      const uint32_t number = (((there ? static_cast<uint32_t>(page) : 0u) * p.Hkv + ahead.h) * 2 + (lane & 1) << unit_shift) +
+                              (unit & ((1 << unit_shift) - 1));
       if (gone != 0 || absent_bits != 0) {
-        const uint32_t bits = (gone & 1u) | (gone >> 1 & 2u) | (gone >> 2 & 4u) | (gone >> 3 & 8u);
-        absent_bits = (absent_bits & ~(15u << (4 * stage))) | bits << (4 * stage);
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < F::kUnits; ++k) bits |= (gone >> 2 * k & 1u) << k;
+        constexpr uint32_t kMask = (1u << F::kUnits) - 1u;
+        absent_bits = (absent_bits & ~(kMask << (F::kUnits * stage))) | bits << (F::kUnits * stage);
         if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
-      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, __popc(want) * U::kBytes);
+      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, units * 2 * U::kBytes);
       __syncwarp();
-      if (wanted) bulk_load(smem_u32(ring + stage * S::kStageBytes + lane * U::kBytes), src, U::kBytes, bars + 8 * stage);
+      if (lane < 2 * units)
+        bulk_load(smem_u32(ring + stage * F::kStageBytes + lane * U::kBytes), p.cache + static_cast<size_t>(number) * U::kBytes, U::kBytes,
+                  bars + 8 * stage);
       if (++asked < end) {
         if (asked == ahead.begin + ahead.tiles) Tiles::next_item(p, ahead);
         page = look(asked - ahead.begin);
       }
     };
 #pragma unroll 1
-    for (int st = 0; st < S::kStages && asked < end; ++st) request(st);
+    for (int st = 0; st < F::kStages && asked < end; ++st) request(st);
 
-    Running<D> s;
-    begin_item<D>(p, it, s);
+    const Decode dc;
+    Running<F> s;
+    begin_item<F>(p, it, s);
     int x = begin, stage = 0;
     uint32_t phase = 0;
     bool fine = true, late = false;
@@ -357,34 +406,34 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     while (true) {
       fine = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns));
       if (!fine) break;
-      run_tile<D>(s, ring + stage * S::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (4 * stage) & 15u);
+      run_tile<F>(s, dc, ring + stage * F::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (F::kUnits * stage));
       __syncwarp();
       if (asked < end) request(stage);
       ++x;
       if (x == it.begin + it.tiles || x == end) {
         if (it.begin >= begin && x == it.begin + it.tiles) {
-          store_item<D>(p, it, s);
+          store_item<F>(p, it, s);
         } else {
           // The run's first item keeps its part beside the ring.  A last one that is another waits until every warp of the CTA
           // has left the ring, and takes its place.
           const int at = it.begin <= begin ? 0 : 1;
           if (lane == 0) { records[2 * warp + at].item = it; records[2 * warp + at].valid = 1; }
           late = at == 1;
-          if (!late) keep_part<D>(s, smem + S::kParts + warp * S::kPart);
+          if (!late) keep_part<F>(s, smem + F::kParts + warp * F::kPart);
         }
         if (x == end) break;
         Tiles::next_item(p, it);
-        begin_item<D>(p, it, s);
+        begin_item<F>(p, it, s);
       }
-      if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+      if (++stage == F::kStages) { stage = 0; phase ^= 1; }
     }
     if (!fine) {                                     // let what was requested arrive before the memory goes
       if (lane == 0) atomicOr(p.status, TEMPO_STATUS_TIMEOUT);
       volatile int none = 0;
-      for (int st = 0; st < S::kStages; ++st) mbar_wait(bars + 8 * st, phase ^ (st < stage ? 1u : 0u), &none, p.wait_ns);
+      for (int st = 0; st < F::kStages; ++st) mbar_wait(bars + 8 * st, phase ^ (st < stage ? 1u : 0u), &none, p.wait_ns);
     }
     __syncthreads();
-    if (late) keep_part<D>(s, smem + warp * S::kPart);
+    if (late) keep_part<F>(s, smem + warp * F::kPart);
   } else {
     __syncthreads();
   }
@@ -422,7 +471,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     const int row = task % kQuads / (D / 4), q = task % (D / 4);
     const int w0 = g.first >> 1;
     const auto part = [&](int i) -> const uint8_t* {
-      return (i == 0 && (g.first & 1)) ? smem + w0 * S::kPart : smem + S::kParts + (w0 + i) * S::kPart;
+      return (i == 0 && (g.first & 1)) ? smem + w0 * F::kPart : smem + F::kParts + (w0 + i) * F::kPart;
     };
     float m = -INFINITY;
     for (int i = 0; i <= g.more; ++i) m = fmaxf(m, reinterpret_cast<const float2*>(part(i) + kRows * D * 4)[row].x);
@@ -499,14 +548,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   }
 }
 
-template <int D>
+template <int D, int NR>
 cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
-  using S = AttendSmem<D>;
-  static_assert(S::kBefore + (kAttendMaxB + 1) * 4 + 1024 <= 227 * 1024, "shared memory of one SM");
+  using F = Few<D, NR>;
+  static_assert(F::kBefore + (kAttendMaxB + 1) * 4 + 1024 <= 227 * 1024, "shared memory of one SM");
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = smem_limit_once(attend_kernel<D>, S::bytes(kAttendMaxB), done);
+  const cudaError_t e = smem_limit_once(attend_kernel<F>, F::bytes(kAttendMaxB), done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend_kernel<D>, dim3(num_sms), dim3(kWarps * 32), S::bytes(p.B), stream, p);
+  return launch_pdl(attend_kernel<F>, dim3(num_sms), dim3(F::kWarps * 32), F::bytes(p.B), stream, p);
+}
+
+// Items of 8 rows where no sequence has more: half the products of items of 16, and registers for 16 warps instead of 12.
+template <int D>
+cudaError_t launch_attend_as(const AttendParams& p, int64_t rows, int num_sms, cudaStream_t stream) {
+  return rows <= 8 ? launch_attend_as<D, 1>(p, num_sms, stream) : launch_attend_as<D, 2>(p, num_sms, stream);
 }
 
 }  // namespace
@@ -525,10 +580,11 @@ AttendLayout attend_layout(int D) {
 constexpr int kFewRows = 64;
 
 cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream) {
-  const bool many = static_cast<int64_t>(max_q) * p.group > kFewRows;
+  const int64_t rows = static_cast<int64_t>(max_q) * p.group;
+  const bool many = rows > kFewRows;
   p.rows_above = 0;
   p.rows_most = many ? kFewRows : INT32_MAX;         // without the other kernel this one takes whatever comes
-  cudaError_t e = D == 64 ? launch_attend_as<64>(p, num_sms, stream) : launch_attend_as<128>(p, num_sms, stream);
+  cudaError_t e = D == 64 ? launch_attend_as<64>(p, rows, num_sms, stream) : launch_attend_as<128>(p, rows, num_sms, stream);
   if (e != cudaSuccess || !many) return e;
   p.rows_above = kFewRows;
   p.rows_most = INT32_MAX;

@@ -109,7 +109,7 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int rows, int row, i
 // ---- decoders -----------------------------------------------------------------------------------------
 // Keys of one stage.  A lane takes 32 neighbouring elements of a key: one group, four words, four 16-byte stores.
 template <int D>
-__device__ __forceinline__ void decode_keys(const uint8_t* stage, uint32_t tile, uint32_t absent, int warp) {
+__device__ __forceinline__ void decode_keys(const Decode& dc, const uint8_t* stage, uint32_t tile, uint32_t absent, int warp) {
   using U = CacheUnit<D>;
   constexpr int kParts = D / 32, kPer = 32 / kParts;                     // lanes to a key, keys to a warp
   const int lane = threadIdx.x & 31, j = lane % kParts;
@@ -127,7 +127,7 @@ __device__ __forceinline__ void decode_keys(const uint8_t* stage, uint32_t tile,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t v[4];
-      decode8(w[i], s, b, v);
+      decode8(dc, w[i], s, b, v);
       st_shared_v4(chunk_at(tile, kKeys, key, j / 2, 4 * (j & 1) + (turn ? i ^ 2 : i)), make_uint4(v[0], v[1], v[2], v[3]));
     }
   }
@@ -137,7 +137,7 @@ __device__ __forceinline__ void decode_keys(const uint8_t* stage, uint32_t tile,
 // eight tokens.  Element 8 x + 4 e + n is row 64 (x / 8) + 8 (4 e + n) + x % 8 of the tile: no bank twice in a store, and 64
 // neighbouring rows are 64 neighbouring elements.
 template <int D>
-__device__ __forceinline__ void decode_values(const uint8_t* stage, uint32_t tile, int t0, int len, int warp) {
+__device__ __forceinline__ void decode_values(const Decode& dc, const uint8_t* stage, uint32_t tile, int t0, int len, int warp) {
   using U = CacheUnit<D>;
   constexpr int kX = D / 8, kPer = 32 / kX;                              // lanes to eight tokens, eights of tokens to a warp
   const int lane = threadIdx.x & 31, x = lane % kX;
@@ -155,8 +155,8 @@ __device__ __forceinline__ void decode_values(const uint8_t* stage, uint32_t til
       if (left < 2) params &= left == 1 ? 0xffffu : 0u;
       uint32_t s, b;
       group_params(params, s, b);
-      decode8(w.x, s, b, v[i][0]);
-      decode8(w.y, s, b, v[i][1]);
+      decode8(dc, w.x, s, b, v[i][0]);
+      decode8(dc, w.y, s, b, v[i][1]);
     }
 #pragma unroll
     for (int n = 0; n < 4; ++n)
@@ -428,6 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       }
     } else {
       // ---- decoders
+      const Decode dc;
       int stage = 0, t = 0;
       uint32_t phase = 0;
       bool fine = true;
@@ -440,8 +441,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
             fine = wait(kv == 0 ? bars.k_empty[buf] : bars.v_empty[buf], (t >> 1 & 1) ^ 1) && wait(bars.code_full[stage], phase);
             if (!fine) break;
             const uint8_t* codes = smem + S::kCodes + stage * S::kStageBytes;
-            if (kv == 0) decode_keys<D>(codes, base + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
-            else decode_values<D>(codes, base + S::kV + buf * S::kTileBytes, (pc.tile0() + i) * kKeys, pc.it.len, warp - 2);
+            if (kv == 0) decode_keys<D>(dc, codes, base + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
+            else decode_values<D>(dc, codes, base + S::kV + buf * S::kTileBytes, (pc.tile0() + i) * kKeys, pc.it.len, warp - 2);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {

@@ -34,17 +34,32 @@ __device__ __forceinline__ void group_params(uint32_t p, uint32_t& s, uint32_t& 
   b = as_u32(__hmul2(as_half2(s), as_half2(((p >> 8) & 0x00f000f0u) | 0xd400d400u)));
 }
 
+// (v & mask) | bits in one instruction: with both as immediates it would be two, and logic is what bounds the decoding.
+__device__ __forceinline__ uint32_t and_or(uint32_t v, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(v), "r"(mask), "r"(bits));
+  return r;
+}
+
+// The constants of decode8, in registers for a whole loop (the compiler cannot see that they are constants).
+struct Decode {
+  uint32_t low, high, m1024, m64, down;
+  __device__ __forceinline__ Decode() {
+    asm volatile("mov.b32 %0, 0x000f000f;\n\tmov.b32 %1, 0x00f000f0;\n\tmov.b32 %2, 0x64006400;\n\tmov.b32 %3, 0x54005400;\n\tmov.b32 %4, 0xe380e380;"
+                 : "=r"(low), "=r"(high), "=r"(m1024), "=r"(m64), "=r"(down));   // down: -960 twice
+  }
+};
+
 // A word of eight codes -> four pairs, pair n of the codes n and n + 4 (bits 4n and 4n + 16).  A code in bits 4 to 7 under the
 // exponent of 64 is the fp16 number 64 + c, one in bits 0 to 3 under the exponent of 1024 is 1024 + c and one exact sum from
 // 64 + c; one fused step takes that to s (64 + c) - s (64 + z) = s (c - z), which has 8 significant bits: nothing is rounded.
 // 11 instructions for 8 elements, 5 of them on the pipe of logic and shifts, which has half the rate of the other one.
-__device__ __forceinline__ void decode8(uint32_t w, uint32_t s, uint32_t b, uint32_t (&v)[4]) {
+__device__ __forceinline__ void decode8(const Decode& k, uint32_t w, uint32_t s, uint32_t b, uint32_t (&v)[4]) {
   const uint32_t t = w >> 8;
-  const __half2 down = as_half2(0xe380e380u);        // -960
-  v[1] = as_u32(__hfma2(as_half2((w & 0x00f000f0u) | 0x54005400u), as_half2(s), as_half2(b)));
-  v[3] = as_u32(__hfma2(as_half2((t & 0x00f000f0u) | 0x54005400u), as_half2(s), as_half2(b)));
-  v[0] = as_u32(__hfma2(__hadd2(as_half2((w & 0x000f000fu) | 0x64006400u), down), as_half2(s), as_half2(b)));
-  v[2] = as_u32(__hfma2(__hadd2(as_half2((t & 0x000f000fu) | 0x64006400u), down), as_half2(s), as_half2(b)));
+  v[1] = as_u32(__hfma2(as_half2(and_or(w, k.high, k.m64)), as_half2(s), as_half2(b)));
+  v[3] = as_u32(__hfma2(as_half2(and_or(t, k.high, k.m64)), as_half2(s), as_half2(b)));
+  v[0] = as_u32(__hfma2(__hadd2(as_half2(and_or(w, k.low, k.m1024)), as_half2(k.down)), as_half2(s), as_half2(b)));
+  v[2] = as_u32(__hfma2(__hadd2(as_half2(and_or(t, k.low, k.m1024)), as_half2(k.down)), as_half2(s), as_half2(b)));
 }
 
 }  // namespace tempo

@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Kv
     for (int j = 0; j < 2; ++j) {
       uint32_t s, b, pairs[4];
       group_params(params[j] * 0x10001u, s, b);
-      decode8(words[j], s, b, pairs);                    // codes (n, n + 4)
+      decode8(Decode(), words[j], s, b, pairs);                    // codes (n, n + 4)
       *out[j] = make_uint4(__byte_perm(pairs[0], pairs[1], 0x5410), __byte_perm(pairs[2], pairs[3], 0x5410),
                            __byte_perm(pairs[0], pairs[1], 0x7632), __byte_perm(pairs[2], pairs[3], 0x7632));
     }
