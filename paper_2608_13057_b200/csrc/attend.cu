@@ -25,23 +25,17 @@ namespace {
 // The kernel's form for items of 8 NR rows.
 template <int D_, int NR_>
 struct Few {
-  static constexpr int D = D_, NR = NR_, kRows = 8 * NR, kTile = 32, kUnits = kTile / kUnit;
-  static constexpr int kWarps = NR == 1 ? 16 : 12;
+  static constexpr int D = D_, NR = NR_, kRows = 8 * NR;
+  static constexpr int kWarps = NR == 1 ? 16 : 8, kTile = NR == 1 ? 32 : 64, kUnits = kTile / kUnit;
   using Tiles = Cut<kRows, kTile>;
   using Item = typename Tiles::Item;
-  struct Part {               // a cut item's share of one warp
-    Item item;
-    int valid;
-  };
   static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // keys and values of each unit
   static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
   static constexpr int kBars = kRing, kParts = kBars + kWarps * kStages * 8;
-  static constexpr int kRecords = kParts + kWarps * kPart;
-  static constexpr int kBefore = kRecords + kWarps * 2 * static_cast<int>(sizeof(Part));
+  static constexpr int kBefore = kParts + kWarps * kPart;
   static_assert(kRing >= kWarps * kPart, "the second parts take the ring's place");
-  static_assert(kRing >= kAttendMaxSms * kRows * 4 + kRows * 4, "so do the weights of a join");
   static int bytes(int B) { return kBefore + (B + 1) * 4; }
 };
 
@@ -316,8 +310,44 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 v, float k) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// Parts of an item one after the other: their sums under the common maximum.
+struct Merged {
+  float m = -INFINITY, l = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  __device__ __forceinline__ float factor() const { return l == 0.0f ? 0.0f : 1.0f / l; }
+};
+// `stat(i)` and `quad(i)` read part i's (m, l) of the row and four of its elements; BATCH parts' loads are in flight together.
+template <int BATCH, typename Stat, typename Quad>
+__device__ __forceinline__ Merged merge(int n, Stat stat, Quad quad) {
+  Merged r;
+  for (int i0 = 0; i0 < n; i0 += BATCH) {
+    float2 st[BATCH];
+    float4 v[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+      if (i0 + i < n) { st[i] = stat(i0 + i); v[i] = quad(i0 + i); }
+    float m = r.m;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+      if (i0 + i < n) m = fmaxf(m, st[i].x);
+    const float ref = m == -INFINITY ? 0.0f : m, before = exp2_fast(r.m - ref);
+    r.m = m;
+    r.l *= before; r.o.x *= before; r.o.y *= before; r.o.z *= before; r.o.w *= before;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+      if (i0 + i < n) {
+        const float k = exp2_fast(st[i].x - ref);
+        r.l += st[i].y * k;
+        r.o.x += v[i].x * k; r.o.y += v[i].y * k; r.o.z += v[i].z * k; r.o.w += v[i].w * k;
+      }
+  }
+  return r;
+}
+
+template <class Item>
 struct Segment {              // neighbouring parts of one item in this CTA
-  int first, more;            // record of the first part, and how many warps follow with their first parts
+  Item item;
+  int warp, late, more;       // the first part is that warp's (its late one or its first), then the first parts of so many warps behind it
   int slot, cta0, ctas;       // -1: the item is whole; else where its part goes, and the CTAs that share the item
   int last;                   // this CTA is the last of them to arrive
 };
@@ -328,12 +358,11 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   using Item = typename F::Item;
   using Tiles = typename F::Tiles;
   using U = CacheUnit<F::D>;
-  constexpr int D = F::D, kWarps = F::kWarps, kRows = F::kRows, kTile = F::kTile;
+  constexpr int D = F::D, kWarps = F::kWarps, kRows = F::kRows, kTile = F::kTile, kUnits = F::kUnits;
   __shared__ int warp_sum[kWarps];
-  __shared__ Segment segments[kWarps + 1];
+  __shared__ Segment<Item> segments[kWarps + 1];
   __shared__ int n_segments, abort_flag;
   int* before = reinterpret_cast<int*>(smem + F::kBefore);
-  typename F::Part* records = reinterpret_cast<typename F::Part*>(smem + F::kRecords);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bars = smem_u32(smem + F::kBars) + warp * F::kStages * 8;
   const uint8_t* ring = smem + warp * F::kStages * F::kStageBytes;
@@ -341,56 +370,64 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   pdl_trigger();
   if (lane < F::kStages) mbar_init(bars + 8 * lane, 1);
   if (tid == 0) { abort_flag = 0; n_segments = 0; }
-  if (lane < 2) records[2 * warp + lane].valid = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_wait();
 
   const int total = Tiles::template count_tiles<kWarps>(p, before, warp_sum, blockIdx.x == 0);
   if (total == 0) return;
 
-  const int n_runs = min(total, static_cast<int>(gridDim.x) * kWarps);
+  // Few tiles go to more CTAs of fewer warps: a warp alone on its scheduler is three times as fast.
+  const int warps = min(kWarps, max(4, (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x)));
+  const int n_runs = min(total, static_cast<int>(gridDim.x) * warps);
   const Runs runs(total, n_runs);
-  const int run0 = blockIdx.x * kWarps;
+  const int run0 = blockIdx.x * warps;
   if (run0 >= n_runs) return;
-  const int cta_begin = runs.begin(run0), cta_end = runs.begin(min(run0 + kWarps, n_runs));
 
-  if (run0 + warp < n_runs) {
+  if (warp < warps && run0 + warp < n_runs) {
     const int begin = runs.begin(run0 + warp), end = runs.begin(run0 + warp + 1);
     Item it = Tiles::item_at(p, before, begin);
-    Item ahead = it;                                 // the item of the next tile to be requested
-    int asked = begin;
+
+    // What is requested next.  The first 2 kUnits lanes each fetch one unit's keys or values, numbered through the whole cache in
+    // 32 bits; the page numbers are read one request ahead.
+    Item ahead = it;
+    int asked = begin, unit, units;                  // this lane's unit of the sequence, and how many it has
+    const int32_t* pages;
+    uint32_t head;
     uint32_t absent_bits = 0;                        // kUnits bits per stage
-    // The first 2 kUnits lanes each fetch one unit's keys or values.  The page numbers are read one request ahead.
-    const int my_unit = lane >> 1, unit_shift = p.page_shift - 4;
-    const auto look = [&](int tile) {                // tile of the item `ahead`
-      const int t = tile * kTile + my_unit * kUnit;
-      return lane < 2 * F::kUnits && t < ahead.len ? p.page_table[static_cast<size_t>(ahead.b) * p.max_pages + (t >> p.page_shift)] : 0;
+    const int unit_shift = p.page_shift - 4, unit_mask = (1 << unit_shift) - 1;
+    const uint32_t page_units = static_cast<uint32_t>(p.Hkv) << (unit_shift + 1);
+    const auto enter = [&]() {
+      unit = (asked - ahead.begin) * kUnits + (lane >> 1);
+      units = (ahead.len + kUnit - 1) / kUnit;
+      pages = p.page_table + static_cast<size_t>(ahead.b) * p.max_pages;
+      head = static_cast<uint32_t>(ahead.h * 2 + (lane & 1)) << unit_shift;
     };
-    int page = look(asked - ahead.begin);
+    const auto look = [&]() { return lane < 2 * kUnits && unit < units ? pages[unit >> unit_shift] : 0; };
+    enter();
+    int page = look();
     const auto request = [&](int stage) {
-      const int tile = asked - ahead.begin, unit = tile * F::kUnits + my_unit;
-      const int units = min(F::kUnits, max(0, (ahead.len - tile * kTile + kUnit - 1) / kUnit));
       const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
       const uint32_t gone = __ballot_sync(0xffffffffu, !there);
-      // units are numbered in 32 bits: a cache has less than 2^32 of them
-      const uint32_t number = (((there ? static_cast<uint32_t>(page) : 0u) * p.Hkv + ahead.h) * 2 + (lane & 1) << unit_shift) +
-                              (unit & ((1 << unit_shift) - 1));
+      const uint32_t number = (there ? static_cast<uint32_t>(page) : 0u) * page_units + head + (unit & unit_mask);
       if (gone != 0 || absent_bits != 0) {
         uint32_t bits = 0;
 #pragma unroll
-        for (int k = 0; k < F::kUnits; ++k) bits |= (gone >> 2 * k & 1u) << k;
-        constexpr uint32_t kMask = (1u << F::kUnits) - 1u;
-        absent_bits = (absent_bits & ~(kMask << (F::kUnits * stage))) | bits << (F::kUnits * stage);
+        for (int k = 0; k < kUnits; ++k) bits |= (gone >> 2 * k & 1u) << k;
+        constexpr uint32_t kMask = (1u << kUnits) - 1u;
+        absent_bits = (absent_bits & ~(kMask << (kUnits * stage))) | bits << (kUnits * stage);
         if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
-      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, units * 2 * U::kBytes);
-      __syncwarp();
-      if (lane < 2 * units)
-        bulk_load(smem_u32(ring + stage * F::kStageBytes + lane * U::kBytes), p.cache + static_cast<size_t>(number) * U::kBytes, U::kBytes,
+      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, max(0, min(kUnits, units - unit)) * 2 * U::kBytes);
+      if (lane < 2 * kUnits && unit < units)
+        bulk_load(smem_u32(ring) + stage * F::kStageBytes + lane * U::kBytes, p.cache + static_cast<size_t>(number) * U::kBytes, U::kBytes,
                   bars + 8 * stage);
+      unit += kUnits;
       if (++asked < end) {
-        if (asked == ahead.begin + ahead.tiles) Tiles::next_item(p, ahead);
-        page = look(asked - ahead.begin);
+        if (asked == ahead.begin + ahead.tiles) {
+          Tiles::next_item(p, ahead);
+          enter();
+        }
+        page = look();
       }
     };
 #pragma unroll 1
@@ -406,7 +443,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     while (true) {
       fine = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns));
       if (!fine) break;
-      run_tile<F>(s, dc, ring + stage * F::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (F::kUnits * stage));
+      run_tile<F>(s, dc, ring + stage * F::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (kUnits * stage));
       __syncwarp();
       if (asked < end) request(stage);
       ++x;
@@ -416,10 +453,20 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
         } else {
           // The run's first item keeps its part beside the ring.  A last one that is another waits until every warp of the CTA
           // has left the ring, and takes its place.
-          const int at = it.begin <= begin ? 0 : 1;
-          if (lane == 0) { records[2 * warp + at].item = it; records[2 * warp + at].valid = 1; }
-          late = at == 1;
+          late = it.begin > begin;
           if (!late) keep_part<F>(s, smem + F::kParts + warp * F::kPart);
+          if (lane == 0 && (it.begin >= begin || warp == 0)) {           // the first of the item's parts in this CTA
+            const int cta_begin = runs.begin(run0), cta_end = runs.begin(min(run0 + warps, n_runs));
+            const int from = runs.of(it.begin), to = runs.of(it.begin + it.tiles - 1);
+            Segment<Item>& g = segments[atomicAdd(&n_segments, 1)];
+            g.item = it;
+            g.warp = warp;
+            g.late = late;
+            g.more = min(to, run0 + warps - 1) - (run0 + warp);
+            g.slot = it.begin >= cta_begin && it.begin + it.tiles <= cta_end ? -1 : it.begin <= cta_begin ? 0 : 1;
+            g.cta0 = from / warps;
+            g.ctas = to / warps - g.cta0 + 1;
+          }
         }
         if (x == end) break;
         Tiles::next_item(p, it);
@@ -439,112 +486,48 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   }
   __syncthreads();
 
-  // Which parts belong together: those of neighbouring warps with one item.
-  if (warp == 0) {
-    const int w = lane >> 1;
-    bool leads = w < kWarps && records[lane].valid != 0;
-    int more = 0;
-    if (leads) {
-      const int begin = records[lane].item.begin;
-      const auto same = [&](int r) { return records[r].valid != 0 && records[r].item.begin == begin; };
-      if ((lane & 1) == 0 && w > 0 && (same(lane - 1) || same(lane - 2))) leads = false;
-      while (leads && w + 1 + more < kWarps && same(2 * (w + 1 + more))) ++more;
-    }
-    const uint32_t all = __ballot_sync(0xffffffffu, leads);
-    if (leads) {
-      const Item& it = records[lane].item;
-      Segment& g = segments[__popc(all & ((1u << lane) - 1u))];
-      g.first = lane;
-      g.more = more;
-      g.slot = it.begin >= cta_begin && it.begin + it.tiles <= cta_end ? -1 : it.begin <= cta_begin ? 0 : 1;
-      g.cta0 = runs.of(it.begin) / kWarps;
-      g.ctas = runs.of(it.begin + it.tiles - 1) / kWarps - g.cta0 + 1;
-    }
-    if (lane == 0) n_segments = __popc(all);
-  }
-  __syncthreads();
-
-  constexpr int kQuads = kRows * D / 4;
+  constexpr int kQuads = kRows * D / 4, kStats = kRows * D * 4;
   const int segs = n_segments;
   for (int task = tid; task < segs * kQuads; task += kWarps * 32) {
-    const Segment& g = segments[task / kQuads];
+    const Segment<Item>& g = segments[task / kQuads];
     const int row = task % kQuads / (D / 4), q = task % (D / 4);
-    const int w0 = g.first >> 1;
-    const auto part = [&](int i) -> const uint8_t* {
-      return (i == 0 && (g.first & 1)) ? smem + w0 * F::kPart : smem + F::kParts + (w0 + i) * F::kPart;
-    };
-    float m = -INFINITY;
-    for (int i = 0; i <= g.more; ++i) m = fmaxf(m, reinterpret_cast<const float2*>(part(i) + kRows * D * 4)[row].x);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = 0; i <= g.more; ++i) {
-      const float2 st = reinterpret_cast<const float2*>(part(i) + kRows * D * 4)[row];
-      const float4 v = reinterpret_cast<const float4*>(part(i))[row * (D / 4) + part_at(row, q)];
-      const float k = exp2_fast(st.x - ref);
-      l += st.y * k;
-      o.x += v.x * k; o.y += v.y * k; o.z += v.z * k; o.w += v.w * k;
-    }
+    const uint8_t* kept = smem + F::kParts + g.warp * F::kPart;
+    const uint8_t* first = g.late ? smem + g.warp * F::kPart : kept;
+    const auto part = [&](int i) { return i == 0 ? first : kept + i * F::kPart; };
+    const Merged r = merge<2>(
+        g.more + 1, [&](int i) { return reinterpret_cast<const float2*>(part(i) + kStats)[row]; },
+        [&](int i) { return reinterpret_cast<const float4*>(part(i))[row * (D / 4) + part_at(row, q)]; });
     if (g.slot < 0) {
-      const Item& it = records[g.first].item;
-      if (it.row0 + row < it.n * p.group) store4(out_row(p, it, row) + 4 * q, o, l == 0.0f ? 0.0f : 1.0f / l);
+      if (g.item.row0 + row < g.item.n * p.group) store4(out_row(p, g.item, row) + 4 * q, r.o, r.factor());
     } else {
       const size_t at = (static_cast<size_t>(blockIdx.x) * 2 + g.slot) * kRows + row;
-      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q, o);
-      if (q == 0) __stcg(reinterpret_cast<float2*>(p.stats) + at, make_float2(m, l));
+      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q, r.o);
+      if (q == 0) __stcg(reinterpret_cast<float2*>(p.stats) + at, make_float2(r.m, r.l));
     }
   }
   __threadfence();
   __syncthreads();
   if (tid < segs && segments[tid].slot >= 0) {
-    Segment& g = segments[tid];
+    Segment<Item>& g = segments[tid];
     g.last = atomicAdd(p.counters + g.cta0, 1u) == static_cast<unsigned>(g.ctas) - 1u;
     if (g.last) p.counters[g.cta0] = 0;
   }
   __syncthreads();
 
   // Items shared with other CTAs, by the last of them: the parts in the order of the CTAs, whoever it is.
-  float* weights = reinterpret_cast<float*>(smem);
   for (int i = 0; i < segs; ++i) {
-    const Segment g = segments[i];
+    const Segment<Item>& g = segments[i];
     if (g.slot < 0 || !g.last) continue;
     __threadfence();
-    const Item it = records[g.first].item;
-    const int begin0 = runs.begin(g.cta0 * kWarps);
-    const auto row_at = [&](int c, int row) {
-      return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 && it.begin > begin0 ? 1 : 0)) * kRows + row;
-    };
-    for (int row = warp; row < kRows; row += kWarps) {
-      float m = -INFINITY;
-      for (int c = lane; c < g.ctas; c += 32) m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(p.stats) + row_at(c, row)).x);
-#pragma unroll
-      for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      const float ref = m == -INFINITY ? 0.0f : m;
-      float l = 0.0f;
-      for (int c = lane; c < g.ctas; c += 32) {
-        const float2 st = __ldcg(reinterpret_cast<const float2*>(p.stats) + row_at(c, row));
-        const float k = exp2_fast(st.x - ref);
-        weights[c * kRows + row] = k;
-        l += st.y * k;
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
-      if (lane == 0) weights[kAttendMaxSms * kRows + row] = l;
-    }
-    __syncthreads();
+    const int begin0 = g.item.begin > runs.begin(g.cta0 * warps) ? 1 : 0;
     for (int task = tid; task < kQuads; task += kWarps * 32) {
       const int row = task / (D / 4), q = task % (D / 4);
-      float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-      for (int c = 0; c < g.ctas; ++c) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + row_at(c, row) * D) + q);
-        const float k = weights[c * kRows + row];
-        o.x += v.x * k; o.y += v.y * k; o.z += v.z * k; o.w += v.w * k;
-      }
-      const float l = weights[kAttendMaxSms * kRows + row];
-      if (it.row0 + row < it.n * p.group) store4(out_row(p, it, row) + 4 * q, o, l == 0.0f ? 0.0f : 1.0f / l);
+      const auto at = [&](int c) { return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 ? begin0 : 0)) * kRows + row; };
+      const Merged r = merge<8>(
+          g.ctas, [&](int c) { return __ldcg(reinterpret_cast<const float2*>(p.stats) + at(c)); },
+          [&](int c) { return __ldcg(reinterpret_cast<const float4*>(p.part + at(c) * D) + q); });
+      if (g.item.row0 + row < g.item.n * p.group) store4(out_row(p, g.item, row) + 4 * q, r.o, r.factor());
     }
-    __syncthreads();
   }
 }
 
