@@ -29,7 +29,7 @@ struct Few {
   static constexpr int kWarps = NR == 1 ? 16 : 8, kTile = NR == 1 ? 32 : 64, kUnits = kTile / kUnit;
   using Tiles = Cut<kRows, kTile>;
   using Item = typename Tiles::Item;
-  static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // keys and values of each unit
+  static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // the keys of its units, then the values
   static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
@@ -139,7 +139,7 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
     uint32_t w[F::kUnits][2][W], sc[F::kUnits][2], b[F::kUnits][2];
 #pragma unroll
     for (int k = 0; k < F::kUnits; ++k) {
-      const uint8_t* unit = stage + k * 2 * U::kBytes;
+      const uint8_t* unit = stage + k * U::kBytes;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int at = x * 8 + g;
@@ -226,7 +226,7 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
   const bool tail = t0 + F::kTile > len;
 #pragma unroll
   for (int k = 0; k < F::kUnits; ++k) {
-    const uint8_t* unit = stage + (k * 2 + 1) * U::kBytes;
+    const uint8_t* unit = stage + (F::kUnits + k) * U::kBytes;
     uint32_t w[2][W], sc[2], b[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {                    // tokens 16 k + 2 pair, + 1
@@ -387,40 +387,45 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     const int begin = runs.begin(run0 + warp), end = runs.begin(run0 + warp + 1);
     Item it = Tiles::item_at(p, before, begin);
 
-    // What is requested next.  The first 2 kUnits lanes each fetch one unit's keys or values, numbered through the whole cache in
-    // 32 bits; the page numbers are read one request ahead.
+    // What is requested next.  A lane fetches the keys or the values of one run of units that lie in one page (each copy costs its
+    // warp about 100 clocks, whatever its size); units are numbered through the whole cache in 32 bits, and the page numbers are
+    // read one request ahead.
     Item ahead = it;
-    int asked = begin, unit, units;                  // this lane's unit of the sequence, and how many it has
+    int asked = begin, unit, units;                  // this lane's first unit of the sequence, and how many the sequence has
     const int32_t* pages;
     uint32_t head;
     uint32_t absent_bits = 0;                        // kUnits bits per stage
     const int unit_shift = p.page_shift - 4, unit_mask = (1 << unit_shift) - 1;
+    const int together = min(kUnits, 1 << unit_shift);                   // units of a run
+    const bool fetches = lane < 2 * kUnits / together;
     const uint32_t page_units = static_cast<uint32_t>(p.Hkv) << (unit_shift + 1);
     const auto enter = [&]() {
-      unit = (asked - ahead.begin) * kUnits + (lane >> 1);
+      unit = (asked - ahead.begin) * kUnits + (lane >> 1) * together;
       units = (ahead.len + kUnit - 1) / kUnit;
       pages = p.page_table + static_cast<size_t>(ahead.b) * p.max_pages;
       head = static_cast<uint32_t>(ahead.h * 2 + (lane & 1)) << unit_shift;
     };
-    const auto look = [&]() { return lane < 2 * kUnits && unit < units ? pages[unit >> unit_shift] : 0; };
+    const auto look = [&]() { return fetches && unit < units ? pages[unit >> unit_shift] : 0; };
     enter();
     int page = look();
     const auto request = [&](int stage) {
+      asm volatile("" : "+r"(page));                 // nothing is computed from it, and so waited for, before this point
       const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
       const uint32_t gone = __ballot_sync(0xffffffffu, !there);
       const uint32_t number = (there ? static_cast<uint32_t>(page) : 0u) * page_units + head + (unit & unit_mask);
       if (gone != 0 || absent_bits != 0) {
         uint32_t bits = 0;
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) bits |= (gone >> 2 * k & 1u) << k;
+        for (int k = 0; k < kUnits; ++k) bits |= (gone >> 2 * (k / together) & 1u) << k;
         constexpr uint32_t kMask = (1u << kUnits) - 1u;
         absent_bits = (absent_bits & ~(kMask << (kUnits * stage))) | bits << (kUnits * stage);
         if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
+      const int mine = min(together, units - unit);
       if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, max(0, min(kUnits, units - unit)) * 2 * U::kBytes);
-      if (lane < 2 * kUnits && unit < units)
-        bulk_load(smem_u32(ring) + stage * F::kStageBytes + lane * U::kBytes, p.cache + static_cast<size_t>(number) * U::kBytes, U::kBytes,
-                  bars + 8 * stage);
+      if (fetches && mine > 0)
+        bulk_load(smem_u32(ring) + stage * F::kStageBytes + ((lane & 1) * kUnits + (lane >> 1) * together) * U::kBytes,
+                  p.cache + static_cast<size_t>(number) * U::kBytes, mine * U::kBytes, bars + 8 * stage);
       unit += kUnits;
       if (++asked < end) {
         if (asked == ahead.begin + ahead.tiles) {
