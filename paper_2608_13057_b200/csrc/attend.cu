@@ -13,8 +13,8 @@
 // (one group: one scale) of one token, of values 16 neighbouring elements of two tokens side by side in a word's halves.
 //
 // Work is dealt in tiles of 32 tokens: the tiles of all items in one row, cut into equal runs, one for each warp of the
-// launch, whatever the lengths.  A warp streams its run through a ring of its own (bulk copies, one barrier per stage) and
-// waits for nobody; parts of items that were cut are joined in shared memory after the CTA's last tile, and across CTAs by the one
+// launch, whatever the lengths.  A warp streams its run through a ring of its own (16-byte asynchronous copies: a bulk copy costs the
+// warp that issues it 200 to 400 clocks, a tenth of a tile) and waits for nobody; parts of items that were cut are joined in shared memory after the CTA's last tile, and across CTAs by the one
 // that arrives last, in a fixed order.
 #include "attend_common.cuh"
 
@@ -26,14 +26,14 @@ namespace {
 template <int D_, int NR_>
 struct Few {
   static constexpr int D = D_, NR = NR_, kRows = 8 * NR;
-  static constexpr int kWarps = NR == 1 ? 16 : 8, kTile = NR == 1 ? 32 : 64, kUnits = kTile / kUnit;
+  static constexpr int kWarps = 8, kTile = 64, kUnits = kTile / kUnit;
   using Tiles = Cut<kRows, kTile>;
   using Item = typename Tiles::Item;
   static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // the keys of its units, then the values
   static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
-  static constexpr int kBars = kRing, kParts = kBars + kWarps * kStages * 8;
+  static constexpr int kParts = kRing;
   static constexpr int kBefore = kParts + kWarps * kPart;
   static_assert(kRing >= kWarps * kPart, "the second parts take the ring's place");
   static int bytes(int B) { return kBefore + (B + 1) * 4; }
@@ -48,6 +48,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
+}
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* a, uint32_t (&v)[W]) {
@@ -75,24 +78,33 @@ struct Running {
   float o[F::NR][kN][4];                             // elements g D/8 + 2 i (in [0], [1]) and + 2 i + 1 (in [2], [3])
 };
 
+// A lane's share of an item's queries, as they are: of row g of each eight the elements j D/4 to (j+1) D/4 - 1.
 template <class F>
-__device__ __forceinline__ void begin_item(const AttendParams& p, const typename F::Item& it, Running<F>& s) {
-  constexpr int W = F::D / 32;                       // 8-element words of a lane
+__device__ __forceinline__ void load_queries(const AttendParams& p, const typename F::Item& it, uint4 (&u)[F::NR][F::D / 32]) {
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  const int rows = it.n * p.group;
 #pragma unroll
   for (int r = 0; r < F::NR; ++r) {
     const int row = it.row0 + 8 * r + g;
-    const bool in = row < rows;
+    const bool in = row < it.n * p.group;
     const int qi = in ? row / p.group : 0, head = in ? it.h * p.group + row - qi * p.group : 0;
+    const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q + static_cast<size_t>(head) * p.hd_q + j * (F::D / 4);
+#pragma unroll
+    for (int w = 0; w < F::D / 32; ++w) u[r][w] = in ? __ldg(reinterpret_cast<const uint4*>(src) + w) : make_uint4(0, 0, 0, 0);
+  }
+}
+
+template <class F>
+__device__ __forceinline__ void begin_item(const AttendParams& p, const typename F::Item& it, const uint4 (&u)[F::NR][F::D / 32], Running<F>& s) {
+  constexpr int W = F::D / 32;                       // 8-element words of a lane
+  const int lane = threadIdx.x & 31, j = lane & 3;
+#pragma unroll
+  for (int r = 0; r < F::NR; ++r) {
     float x[W][8];
     float top = 0.0f;
     bool odd = false;
-    const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q + static_cast<size_t>(head) * p.hd_q + j * (F::D / 4);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const uint4 u = in ? __ldg(reinterpret_cast<const uint4*>(src) + w) : make_uint4(0, 0, 0, 0);
-      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+      const uint32_t v[4] = {u[r][w].x, u[r][w].y, u[r][w].z, u[r][w].w};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[w][i] = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
@@ -110,9 +122,9 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const typename
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {                  // the pairs (n, n + 4) of decode8, two to a matrix instruction
-        s.q[r][2 * w + u][0] = as_u32(__floats2half2_rn(x[w][2 * u] * up, x[w][2 * u + 4] * up));
-        s.q[r][2 * w + u][1] = as_u32(__floats2half2_rn(x[w][2 * u + 1] * up, x[w][2 * u + 5] * up));
+      for (int y = 0; y < 2; ++y) {                  // the pairs (n, n + 4) of decode8, two to a matrix instruction
+        s.q[r][2 * w + y][0] = as_u32(__floats2half2_rn(x[w][2 * y] * up, x[w][2 * y + 4] * up));
+        s.q[r][2 * w + y][1] = as_u32(__floats2half2_rn(x[w][2 * y + 1] * up, x[w][2 * y + 5] * up));
       }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
@@ -361,16 +373,13 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   constexpr int D = F::D, kWarps = F::kWarps, kRows = F::kRows, kTile = F::kTile, kUnits = F::kUnits;
   __shared__ int warp_sum[kWarps];
   __shared__ Segment<Item> segments[kWarps + 1];
-  __shared__ int n_segments, abort_flag;
+  __shared__ int n_segments;
   int* before = reinterpret_cast<int*>(smem + F::kBefore);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t bars = smem_u32(smem + F::kBars) + warp * F::kStages * 8;
   const uint8_t* ring = smem + warp * F::kStages * F::kStageBytes;
 
   pdl_trigger();
-  if (lane < F::kStages) mbar_init(bars + 8 * lane, 1);
-  if (tid == 0) { abort_flag = 0; n_segments = 0; }
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  if (tid == 0) n_segments = 0;
   pdl_wait();
 
   const int total = Tiles::template count_tiles<kWarps>(p, before, warp_sum, blockIdx.x == 0);
@@ -387,25 +396,24 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     const int begin = runs.begin(run0 + warp), end = runs.begin(run0 + warp + 1);
     Item it = Tiles::item_at(p, before, begin);
 
-    // What is requested next.  A lane fetches the keys or the values of one run of units that lie in one page (each copy costs its
-    // warp about 100 clocks, whatever its size); units are numbered through the whole cache in 32 bits, and the page numbers are
-    // read one request ahead.
+    // What is requested next.  A tile's units lie in runs of `together` in one page; a lane keeps the number (through the whole
+    // cache, in 32 bits) of one run's first key unit.  Page numbers are read one request ahead.
     Item ahead = it;
-    int asked = begin, unit, units;                  // this lane's first unit of the sequence, and how many the sequence has
+    int asked = begin, unit, units;                  // the run's first unit in the sequence, and how many the sequence has
     const int32_t* pages;
     uint32_t head;
     uint32_t absent_bits = 0;                        // kUnits bits per stage
     const int unit_shift = p.page_shift - 4, unit_mask = (1 << unit_shift) - 1;
-    const int together = min(kUnits, 1 << unit_shift);                   // units of a run
-    const bool fetches = lane < 2 * kUnits / together;
+    const int together = min(kUnits, 1 << unit_shift), n_parts = kUnits / together;
     const uint32_t page_units = static_cast<uint32_t>(p.Hkv) << (unit_shift + 1);
+    const size_t to_values = static_cast<size_t>(1 << unit_shift) * U::kBytes;
     const auto enter = [&]() {
-      unit = (asked - ahead.begin) * kUnits + (lane >> 1) * together;
+      unit = (asked - ahead.begin) * kUnits + (lane & (n_parts - 1)) * together;
       units = (ahead.len + kUnit - 1) / kUnit;
       pages = p.page_table + static_cast<size_t>(ahead.b) * p.max_pages;
-      head = static_cast<uint32_t>(ahead.h * 2 + (lane & 1)) << unit_shift;
+      head = static_cast<uint32_t>(ahead.h * 2) << unit_shift;
     };
-    const auto look = [&]() { return fetches && unit < units ? pages[unit >> unit_shift] : 0; };
+    const auto look = [&]() { return unit < units ? pages[unit >> unit_shift] : 0; };
     enter();
     int page = look();
     const auto request = [&](int stage) {
@@ -416,16 +424,36 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
       if (gone != 0 || absent_bits != 0) {
         uint32_t bits = 0;
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) bits |= (gone >> 2 * (k / together) & 1u) << k;
+        for (int k = 0; k < kUnits; ++k) bits |= (gone >> (k / together) & 1u) << k;
         constexpr uint32_t kMask = (1u << kUnits) - 1u;
         absent_bits = (absent_bits & ~(kMask << (kUnits * stage))) | bits << (kUnits * stage);
         if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
-      const int mine = min(together, units - unit);
-      if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, max(0, min(kUnits, units - unit)) * 2 * U::kBytes);
-      if (fetches && mine > 0)
-        bulk_load(smem_u32(ring) + stage * F::kStageBytes + ((lane & 1) * kUnits + (lane >> 1) * together) * U::kBytes,
-                  p.cache + static_cast<size_t>(number) * U::kBytes, mine * U::kBytes, bars + 8 * stage);
+      const uint32_t dst = smem_u32(ring) + stage * F::kStageBytes + lane * 16;
+      if (n_parts == 1) {                            // units of the page behind the sequence's last come along
+        constexpr int kRun = kUnits * U::kBytes;
+        const uint8_t* src = p.cache + static_cast<size_t>(number) * U::kBytes + lane * 16;
+#pragma unroll
+        for (int at = 0; at < kRun; at += 512)
+          if (at + 512 <= kRun || at + lane * 16 < kRun) {
+            copy_async_16(dst + at, src + at);
+            copy_async_16(dst + kRun + at, src + to_values + at);
+          }
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < kUnits; ++k) {
+          const int from = k / together, first = __shfl_sync(0xffffffffu, unit, from) + k % together;
+          const uint8_t* src = p.cache + static_cast<size_t>(__shfl_sync(0xffffffffu, number, from) + k % together) * U::kBytes + lane * 16;
+          if (first < units) {
+#pragma unroll
+            for (int at = 0; at < U::kBytes; at += 512)
+              if (at + 512 <= U::kBytes || at + lane * 16 < U::kBytes) {
+                copy_async_16(dst + k * U::kBytes + at, src + at);
+                copy_async_16(dst + (kUnits + k) * U::kBytes + at, src + to_values + at);
+              }
+          }
+        }
+      }
       unit += kUnits;
       if (++asked < end) {
         if (asked == ahead.begin + ahead.tiles) {
@@ -435,22 +463,29 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
         page = look();
       }
     };
-#pragma unroll 1
-    for (int st = 0; st < F::kStages && asked < end; ++st) request(st);
 
     const Decode dc;
     Running<F> s;
-    begin_item<F>(p, it, s);
+    uint4 raw[F::NR][D / 32];
+    load_queries<F>(p, it, raw);                     // asked for before the cache, so as not to queue behind it
+    request(0);
+    cp_async_commit();
+    begin_item<F>(p, it, raw, s);
+#pragma unroll 1
+    for (int st = 1; st < F::kStages; ++st) {
+      if (asked < end) request(st);
+      cp_async_commit();
+    }
     int x = begin, stage = 0;
-    uint32_t phase = 0;
-    bool fine = true, late = false;
+    bool late = false;
 #pragma unroll 1
     while (true) {
-      fine = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, &abort_flag, p.wait_ns));
-      if (!fine) break;
+      cp_async_wait<F::kStages - 1>();               // a group for each tile: all but the newest have arrived
+      __syncwarp();
       run_tile<F>(s, dc, ring + stage * F::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (kUnits * stage));
       __syncwarp();
       if (asked < end) request(stage);
+      cp_async_commit();
       ++x;
       if (x == it.begin + it.tiles || x == end) {
         if (it.begin >= begin && x == it.begin + it.tiles) {
@@ -475,14 +510,10 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
         }
         if (x == end) break;
         Tiles::next_item(p, it);
-        begin_item<F>(p, it, s);
+        load_queries<F>(p, it, raw);
+        begin_item<F>(p, it, raw, s);
       }
-      if (++stage == F::kStages) { stage = 0; phase ^= 1; }
-    }
-    if (!fine) {                                     // let what was requested arrive before the memory goes
-      if (lane == 0) atomicOr(p.status, TEMPO_STATUS_TIMEOUT);
-      volatile int none = 0;
-      for (int st = 0; st < F::kStages; ++st) mbar_wait(bars + 8 * st, phase ^ (st < stage ? 1u : 0u), &none, p.wait_ns);
+      if (++stage == F::kStages) stage = 0;
     }
     __syncthreads();
     if (late) keep_part<F>(s, smem + warp * F::kPart);
