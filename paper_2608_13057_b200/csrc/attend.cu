@@ -26,12 +26,11 @@ namespace {
 template <int D_, int NR_>
 struct Few {
   static constexpr int D = D_, NR = NR_, kRows = 8 * NR;
-  static constexpr int kWarps = 8, kTile = 64, kUnits = kTile / kUnit;
+  static constexpr int kWarps = NR == 2 ? 8 : D == 128 ? 12 : 16, kTile = 64, kUnits = kTile / kUnit;
   using Tiles = Cut<kRows, kTile>;
   using Item = typename Tiles::Item;
   static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // the keys of its units, then the values
-  static constexpr int kStages = D == 64 ? 4 : 2;
-  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kRing = kWarps * kStageBytes;
   static constexpr int kPart = kRows * D * 4 + kRows * 8;            // O, then (m, l) of each row
   static constexpr int kParts = kRing;
   static constexpr int kBefore = kParts + kWarps * kPart;
@@ -140,18 +139,20 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const typename
   s.least = it.len - it.n + it.row0 / p.group;
 }
 
-// One tile: tokens [t0, t0 + kTile) of the item at `stage`.  `absent`: bits of its units whose page is not in the cache.
+// One tile is the tokens [t0, t0 + kTile) of the item, its keys and its values at `stage`.  Here its scores: c[k][r], of the tokens
+// 16 k + g (in [0], [1]) and 16 k + 8 + g, rows 2 j and 2 j + 1 of eight r.  `absent`: bits of its units whose page is not in the cache.
 template <class F>
-__device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const uint8_t* stage, int t0, int len, uint32_t absent) {
+__device__ __forceinline__ void run_keys(const Running<F>& s, const Decode& dc, const uint8_t* stage, int t0, uint32_t absent,
+                                         float (&c)[F::kUnits][F::NR][4]) {
   using U = CacheUnit<F::D>;
   constexpr int D = F::D, W = D / 32, NR = F::NR;
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  float c[F::kUnits][NR][4];                         // scores of the tokens 16 k + g (in [0], [1]) and + 8, rows 2 j and 2 j + 1
-  {
-    uint32_t w[F::kUnits][2][W], sc[F::kUnits][2], b[F::kUnits][2];
 #pragma unroll
-    for (int k = 0; k < F::kUnits; ++k) {
-      const uint8_t* unit = stage + k * U::kBytes;
+  for (int k0 = 0; k0 < F::kUnits; k0 += 2) {        // two units side by side
+    uint32_t w[2][2][W], sc[2][2], b[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint8_t* unit = stage + (k0 + k) * U::kBytes;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int at = x * 8 + g;
@@ -160,12 +161,12 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
                      sc[k][x], b[k][x]);
       }
 #pragma unroll
-      for (int r = 0; r < NR; ++r) c[k][r][0] = c[k][r][1] = c[k][r][2] = c[k][r][3] = 0.0f;
+      for (int r = 0; r < NR; ++r) c[k0 + k][r][0] = c[k0 + k][r][1] = c[k0 + k][r][2] = c[k0 + k][r][3] = 0.0f;
     }
 #pragma unroll
     for (int y = 0; y < W; ++y)
 #pragma unroll
-      for (int k = 0; k < F::kUnits; ++k) {
+      for (int k = 0; k < 2; ++k) {
         uint32_t v[2][4];
 #pragma unroll
         for (int x = 0; x < 2; ++x) decode8(dc, w[k][x][y], sc[k][x], b[k][x], v[x]);
@@ -173,7 +174,7 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < NR; ++r)
-            mma_f16(c[k][r], v[0][2 * u], v[1][2 * u], v[0][2 * u + 1], v[1][2 * u + 1], s.q[r][2 * y + u][0], s.q[r][2 * y + u][1]);
+            mma_f16(c[k0 + k][r], v[0][2 * u], v[1][2 * u], v[0][2 * u + 1], v[1][2 * u + 1], s.q[r][2 * y + u][0], s.q[r][2 * y + u][1]);
       }
   }
   if (absent != 0) {
@@ -193,6 +194,12 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
         for (int x = 0; x < 4; ++x)
           if (t0 + 16 * k + 8 * (x / 2) + g > s.limit[r][x & 1]) c[k][r][x] = -INFINITY;
   }
+}
+
+// Scores to weights, as the B operands of the output: w8[k][r] of row g, tokens 2 j, + 1 and 8 + 2 j, + 1 of unit k.
+template <class F>
+__device__ __forceinline__ void run_weights(Running<F>& s, const float (&c)[F::kUnits][F::NR][4], uint32_t (&w8)[F::kUnits][F::NR][2]) {
+  constexpr int NR = F::NR;
   bool raise = false;
   float top[NR][2];
 #pragma unroll
@@ -222,7 +229,6 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
         for (int i = 0; i < Running<F>::kN; ++i) { s.o[r][i][y] *= k; s.o[r][i][y + 2] *= k; }
       }
   }
-  uint32_t w8[F::kUnits][NR][2];                     // B operands of the output: row g, tokens 2 j, + 1 and 8 + 2 j, + 1 of unit k
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     float less[2];
@@ -235,10 +241,18 @@ __device__ __forceinline__ void run_tile(Running<F>& s, const Decode& dc, const 
         w8[k][r][x] = transpose8(as_u32(__floats2half2_rn(exp2_fast(fmaf(c[k][r][2 * x], s.f[r][0], less[0])),
                                                           exp2_fast(fmaf(c[k][r][2 * x + 1], s.f[r][1], less[1])))));
   }
+}
+
+template <class F>
+__device__ __forceinline__ void run_values(Running<F>& s, const Decode& dc, const uint8_t* stage, int t0, int len,
+                                           const uint32_t (&w8)[F::kUnits][F::NR][2]) {
+  using U = CacheUnit<F::D>;
+  constexpr int D = F::D, W = D / 32, NR = F::NR;
+  const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
   const bool tail = t0 + F::kTile > len;
 #pragma unroll
   for (int k = 0; k < F::kUnits; ++k) {
-    const uint8_t* unit = stage + (F::kUnits + k) * U::kBytes;
+    const uint8_t* unit = stage + k * U::kBytes;
     uint32_t w[2][W], sc[2], b[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {                    // tokens 16 k + 2 pair, + 1
@@ -376,7 +390,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   __shared__ int n_segments;
   int* before = reinterpret_cast<int*>(smem + F::kBefore);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint8_t* ring = smem + warp * F::kStages * F::kStageBytes;
+  const uint8_t* ring = smem + warp * F::kStageBytes;
 
   pdl_trigger();
   if (tid == 0) n_segments = 0;
@@ -397,14 +411,15 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     Item it = Tiles::item_at(p, before, begin);
 
     // What is requested next.  A tile's units lie in runs of `together` in one page; a lane keeps the number (through the whole
-    // cache, in 32 bits) of one run's first key unit.  Page numbers are read one request ahead.
+    // cache, in 32 bits) of one run's first key unit.  Page numbers are read one tile ahead.
     Item ahead = it;
     int asked = begin, unit, units;                  // the run's first unit in the sequence, and how many the sequence has
+    int left;                                        // units from the requested tile's first on
     const int32_t* pages;
-    uint32_t head;
-    uint32_t absent_bits = 0;                        // kUnits bits per stage
+    uint32_t head, number, absent;                   // absent: units of the requested tile whose page is not in the cache
     const int unit_shift = p.page_shift - 4, unit_mask = (1 << unit_shift) - 1;
-    const int together = min(kUnits, 1 << unit_shift), n_parts = kUnits / together;
+    const int together = min(kUnits, 1 << unit_shift), n_parts = kUnits / together, shift_together = min(unit_shift, 2);
+    static_assert(kUnits == 4, "log2 of the largest run");
     const uint32_t page_units = static_cast<uint32_t>(p.Hkv) << (unit_shift + 1);
     const size_t to_values = static_cast<size_t>(1 << unit_shift) * U::kBytes;
     const auto enter = [&]() {
@@ -416,43 +431,17 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     const auto look = [&]() { return unit < units ? pages[unit >> unit_shift] : 0; };
     enter();
     int page = look();
-    const auto request = [&](int stage) {
+    const auto locate = [&]() {                      // the tile `asked`, and a look at the next
       asm volatile("" : "+r"(page));                 // nothing is computed from it, and so waited for, before this point
       const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
       const uint32_t gone = __ballot_sync(0xffffffffu, !there);
-      const uint32_t number = (there ? static_cast<uint32_t>(page) : 0u) * page_units + head + (unit & unit_mask);
-      if (gone != 0 || absent_bits != 0) {
-        uint32_t bits = 0;
+      number = (there ? static_cast<uint32_t>(page) : 0u) * page_units + head + (unit & unit_mask);
+      left = units - __shfl_sync(0xffffffffu, unit, 0);
+      absent = 0;
+      if (gone != 0) {
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) bits |= (gone >> (k / together) & 1u) << k;
-        constexpr uint32_t kMask = (1u << kUnits) - 1u;
-        absent_bits = (absent_bits & ~(kMask << (kUnits * stage))) | bits << (kUnits * stage);
-        if (gone != 0 && lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
-      }
-      const uint32_t dst = smem_u32(ring) + stage * F::kStageBytes + lane * 16;
-      if (n_parts == 1) {                            // units of the page behind the sequence's last come along
-        constexpr int kRun = kUnits * U::kBytes;
-        const uint8_t* src = p.cache + static_cast<size_t>(number) * U::kBytes + lane * 16;
-#pragma unroll
-        for (int at = 0; at < kRun; at += 512)
-          if (at + 512 <= kRun || at + lane * 16 < kRun) {
-            copy_async_16(dst + at, src + at);
-            copy_async_16(dst + kRun + at, src + to_values + at);
-          }
-      } else {
-#pragma unroll 1
-        for (int k = 0; k < kUnits; ++k) {
-          const int from = k / together, first = __shfl_sync(0xffffffffu, unit, from) + k % together;
-          const uint8_t* src = p.cache + static_cast<size_t>(__shfl_sync(0xffffffffu, number, from) + k % together) * U::kBytes + lane * 16;
-          if (first < units) {
-#pragma unroll
-            for (int at = 0; at < U::kBytes; at += 512)
-              if (at + 512 <= U::kBytes || at + lane * 16 < U::kBytes) {
-                copy_async_16(dst + k * U::kBytes + at, src + at);
-                copy_async_16(dst + (kUnits + k) * U::kBytes + at, src + to_values + at);
-              }
-          }
-        }
+        for (int k = 0; k < kUnits; ++k) absent |= (gone >> (k / together) & 1u) << k;
+        if (lane == 0) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
       }
       unit += kUnits;
       if (++asked < end) {
@@ -463,28 +452,60 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
         page = look();
       }
     };
+    const auto request = [&](int kv) {               // keys or values of the tile that was located
+      constexpr int kRun = kUnits * U::kBytes;
+      const uint32_t dst = smem_u32(ring) + kv * kRun + lane * 16;
+      const uint8_t* from = p.cache + kv * to_values;
+      if (n_parts == 1) {                            // units of the page behind the sequence's last come along
+        const uint8_t* src = from + static_cast<size_t>(number) * U::kBytes + lane * 16;
+#pragma unroll
+        for (int at = 0; at < kRun; at += 512)
+          if (at + 512 <= kRun || at + lane * 16 < kRun) copy_async_16(dst + at, src + at);
+      } else {
+#pragma unroll
+        for (int at = 0; at < kRun; at += 512) {
+          const int k = (at + lane * 16) / U::kBytes;                    // the unit of this lane's 16 bytes
+          const uint32_t first = __shfl_sync(0xffffffffu, number, k >> shift_together) + (k & (together - 1));
+          if (k < left && k < kUnits) copy_async_16(dst + at, from + static_cast<size_t>(first) * U::kBytes + (at + lane * 16 - k * U::kBytes));
+        }
+      }
+    };
 
+    // A tile's keys make room for the next one's as soon as its scores are there, its values when its output is: either load has
+    // the other half's work to hide behind.
     const Decode dc;
     Running<F> s;
     uint4 raw[F::NR][D / 32];
     load_queries<F>(p, it, raw);                     // asked for before the cache, so as not to queue behind it
+    locate();
     request(0);
     cp_async_commit();
+    request(1);
+    cp_async_commit();
     begin_item<F>(p, it, raw, s);
-#pragma unroll 1
-    for (int st = 1; st < F::kStages; ++st) {
-      if (asked < end) request(st);
-      cp_async_commit();
-    }
-    int x = begin, stage = 0;
+    int x = begin;
     bool late = false;
 #pragma unroll 1
     while (true) {
-      cp_async_wait<F::kStages - 1>();               // a group for each tile: all but the newest have arrived
+      const int t0 = (x - it.begin) * kTile;
+      const bool more = asked < end;
+      float c[kUnits][F::NR][4];
+      uint32_t w8[kUnits][F::NR][2];
+      cp_async_wait<1>();
       __syncwarp();
-      run_tile<F>(s, dc, ring + stage * F::kStageBytes, (x - it.begin) * kTile, it.len, absent_bits >> (kUnits * stage));
+      run_keys<F>(s, dc, ring, t0, absent, c);
       __syncwarp();
-      if (asked < end) request(stage);
+      if (more) {
+        locate();
+        request(0);
+      }
+      cp_async_commit();
+      run_weights<F>(s, c, w8);
+      cp_async_wait<1>();
+      __syncwarp();
+      run_values<F>(s, dc, ring + kUnits * U::kBytes, t0, it.len, w8);
+      __syncwarp();
+      if (more) request(1);
       cp_async_commit();
       ++x;
       if (x == it.begin + it.tiles || x == end) {
@@ -513,7 +534,6 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
         load_queries<F>(p, it, raw);
         begin_item<F>(p, it, raw, s);
       }
-      if (++stage == F::kStages) stage = 0;
     }
     __syncthreads();
     if (late) keep_part<F>(s, smem + warp * F::kPart);
