@@ -667,6 +667,10 @@ static int run_heads(const tempo_heads* a, const tempo_cache* c, const void* q, 
   p.q_out_vec = vectors8(q_out, a->ld_q_out, a->hd_q_out); p.k_out_vec = vectors8(k_out, a->ld_k_out, a->hd_k_out);
   p.w_vec = aligned(q_w, 16) && aligned(k_w, 16);
   p.rot_vec = aligned(cos_sin, 16) && a->rot % (a->interleaved ? 8 : 16) == 0;
+  const auto quads = [&](const void* x, int64_t ld, int64_t hd) { return aligned(x, 8) && ld % 4 == 0 && hd % 4 == 0; };
+  p.quads = a->rot % 8 == 0 && aligned(cos_sin, 16) && aligned(q_w, 4 * ws) && aligned(k_w, 4 * ws) && quads(q, a->ld_q, a->hd_q) &&
+            quads(q_out, a->ld_q_out, a->hd_q_out) && (append || (quads(k, a->ld_k, a->hd_k) && quads(k_out, a->ld_k_out, a->hd_k_out)));
+  p.inverse_d = 1.0f / a->D;
   p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);
   p.q_w = q_w; p.k_w = k_w; p.positions = positions; p.cos_sin = cos_sin; p.n_valid = n_valid;
   p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out);

@@ -240,104 +240,164 @@ __device__ __forceinline__ uint32_t quantise8(const R (&y)[8], uint32_t& params)
   return word;
 }
 
-// The factors of a lane's eight elements: out[i] = r * (x[i] * a[i] + other[i] * b[i]), weights, cos and sin in them.  They are
-// the same for every head of a token.  Returns whether the lane's elements turn; if not, a is the weight and b unused.
-template <int LPH>
-__device__ __forceinline__ bool factors(const HeadsParams& p, const void* w, int e, const float* angles, float (&a)[8], float (&b)[8]) {
-  const int half = p.rot / 2;
-  float wb[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = wb[i] = 1.0f;
-  if (e >= p.D) return false;
-  if (w != nullptr) weights8(w, p.w_f32, p.w_vec, e, a);
-  if (e >= p.rot) return false;
-  if (p.interleaved) {
-    const float4 c = __ldg(reinterpret_cast<const float4*>(angles + e / 2)), s = __ldg(reinterpret_cast<const float4*>(angles + half + e / 2));
-    const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float w0 = a[2 * i], w1 = a[2 * i + 1];
-      a[2 * i] = w0 * cv[i]; b[2 * i] = -w1 * sv[i];
-      a[2 * i + 1] = w1 * cv[i]; b[2 * i + 1] = w0 * sv[i];
-    }
-    return true;
-  }
-  const bool first = e < half;
-  const int at = first ? e : e - half;
-  if (w != nullptr) weights8(w, p.w_f32, p.w_vec, first ? e + half : at, wb);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float4 c = __ldg(reinterpret_cast<const float4*>(angles + at) + i), s = __ldg(reinterpret_cast<const float4*>(angles + half + at) + i);
-    const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      a[4 * i + x] *= cv[x];
-      b[4 * i + x] = wb[4 * i + x] * (first ? -sv[x] : sv[x]);
-    }
-  }
-  return true;
+// (a, b) * (c, d), and that plus (e, f)
+__device__ __forceinline__ void mul_pair(float& a, float& b, float c, float d) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void fma_pair(float& a, float& b, float c, float d, float e, float f) {
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %5};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d), "f"(e), "f"(f));
 }
 
-// NH heads of a token by one group of lanes: their loads are in flight together, the factors are made once.
-template <int LPH, int NH>
-__device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, bool live) {
-  constexpr int HPW = 32 / LPH;
-  const int lane = threadIdx.x & 31, e = (lane % LPH) * 8, half = p.rot / 2;
-  const bool mine = live && e < p.D;
-  uint4 raw[NH];
-#pragma unroll
-  for (int n = 0; n < NH; ++n) {
-    const int h = h0 + n * HPW;
-    raw[n] = mine && h < H ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
+// Four elements of a row, or four weights.
+__device__ __forceinline__ uint2 load4(const __nv_bfloat16* p) {
+  uint2 u;
+  asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(u.x), "=r"(u.y) : "l"(p) : "memory");
+  return u;
+}
+__device__ __forceinline__ void widen4(uint2 u, float* x) {
+  x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
+  x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void weights4(const void* w, int f32, int e, float* x) {
+  if (f32) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + e));
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  } else {
+    widen4(__ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + e)), x);
   }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* y) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(y[0], y[1]), b = __floats2bfloat162_rn(y[2], y[3]);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// Heads of one token by one group of lanes, h0, h0 + HPW, ... below H, `rounds` times NH of them: NH heads' loads are in flight
+// together, and weights, cos and sin are multiplied once for all.  A lane has two runs of four elements which turn with one another
+// (half pairs: i and i + rot/2) or each in itself, so that nothing is exchanged but the sum of squares:
+//   out[i] = r * (x[i] * a[i] + other[i] * b[i])
+template <int LPH, int NH>
+__device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, int rounds, bool live) {
+  constexpr int HPW = 32 / LPH;
+  const int l = threadIdx.x % LPH, half = p.rot / 2;
   const float* angles = angles_of(p, t, live);
-  if (!p.rot_vec) {                                     // any even rot: one head at a time
+  if (!p.quads) {                                       // any even rot, any alignment: one head at a time
+    const int e = l * 8;
 #pragma unroll 1
-    for (int n = 0; n < NH; ++n) {
+    for (int n = 0; n < NH * rounds; ++n) {
       const int h = h0 + n * HPW;
-      const bool in = mine && h < H;
+      const bool in = live && h < H && e < p.D;
       float y[8];
-      uint4 u = in ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
+      const uint4 u = in ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
       turned<LPH, float>(p, o, t * o.ld + (h < H ? h : 0) * o.hd, e, live && h < H, angles, u, y);
       __syncwarp();                                     // in place: every load of the warp's heads comes before the stores
       if (in) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
     }
     return;
   }
+  const bool mine = live && 8 * l < p.D;
+  const bool turns = 8 * l < p.rot, apart = turns && !p.interleaved;
+  const int e0 = apart ? 4 * l : 8 * l, e1 = apart ? half + 4 * l : 8 * l + 4;
+  const __nv_bfloat16* src = o.x + t * o.ld + h0 * o.hd + e0;
+  __nv_bfloat16* dst = out.x + t * out.ld + h0 * out.hd + e0;
+  const int to = e1 - e0;
+  uint2 raw[NH][2];
+  const auto load = [&](int h) {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      const bool in = mine && h + n * HPW < H;
+      raw[n][0] = in ? load4(src + n * HPW * o.hd) : make_uint2(0, 0);
+      raw[n][1] = in ? load4(src + n * HPW * o.hd + to) : make_uint2(0, 0);
+    }
+  };
+  load(h0);
   float a[8], b[8];
-  const bool turn = live && factors<LPH>(p, o.w, e, angles, a, b);
-  const int from = turn && !p.interleaved ? (e < half ? lane + half / 8 : lane - half / 8) : lane;
 #pragma unroll
-  for (int n = 0; n < NH; ++n) {
-    float x[8], y[8];
-    widen8(raw[n], x);
-    float r = 1.0f;
-    if (o.w != nullptr) {
-      float ss = 0.0f;
+  for (int i = 0; i < 8; ++i) { a[i] = 1.0f; b[i] = 0.0f; }
+  if (mine && o.w != nullptr) { weights4(o.w, p.w_f32, e0, a); weights4(o.w, p.w_f32, e1, a + 4); }
+  if (mine && turns) {
+    const float* at = angles + (apart ? e0 : 4 * l);
+    const float4 c4 = __ldg(reinterpret_cast<const float4*>(at)), s4 = __ldg(reinterpret_cast<const float4*>(at + half));
+    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-      for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-      r = rsqrtf(ss / static_cast<float>(p.D) + p.eps);
+    for (int i = 0; i < 4; ++i) {                       // pair i: elements (i, 4 + i) of the lane's eight, or (2 i, 2 i + 1)
+      const float x0 = p.interleaved ? a[2 * i] : a[i], x1 = p.interleaved ? a[2 * i + 1] : a[4 + i];
+      b[i] = x0 * s[i];                                 // kept by pair until a is no longer needed
+      b[4 + i] = -x1 * s[i];
     }
-    uint4 u = raw[n];
-    if (p.rot != 0 && !p.interleaved) {
-      u.x = __shfl_sync(0xffffffffu, u.x, from);
-      u.y = __shfl_sync(0xffffffffu, u.y, from);
-      u.z = __shfl_sync(0xffffffffu, u.z, from);
-      u.w = __shfl_sync(0xffffffffu, u.w, from);
-    }
-    if (turn) {
-      float z[8];
-      widen8(u, z);
+    float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = fmaf(x[i], a[i], (p.interleaved ? x[i ^ 1] : z[i]) * b[i]) * r;
-    } else {
+    for (int i = 0; i < 8; ++i) f[i] = b[i];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = x[i] * a[i] * r;
+    for (int i = 0; i < 8; ++i) a[i] *= p.interleaved ? c[i / 2] : c[i % 4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)                         // an element's other one: the pair's second for its first, and the reverse
+      b[i] = p.interleaved ? ((i & 1) ? f[i / 2] : f[4 + i / 2]) : (i < 4 ? f[4 + i] : f[i - 4]);
+  }
+#pragma unroll 1
+  for (int round = 0;; ++round) {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      float x[8];
+      widen4(raw[n][0], x);
+      widen4(raw[n][1], x + 4);
+      float r = 1.0f;
+      if (o.w != nullptr) {
+        float s0 = x[0] * x[0], s1 = x[1] * x[1];
+#pragma unroll
+        for (int i = 2; i < 8; i += 2) {
+          float q0 = x[i], q1 = x[i + 1];
+          fma_pair(q0, q1, q0, q1, s0, s1);
+          s0 = q0; s1 = q1;
+        }
+        float ss = s0 + s1;
+#pragma unroll
+        for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+        r = rsqrtf(fmaf(ss, p.inverse_d, p.eps));
+      }
+      float y[8];
+      if (turns) {
+        if (p.interleaved) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            y[i] = x[i + 1]; y[i + 1] = x[i];
+            mul_pair(y[i], y[i + 1], b[i], b[i + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            y[i] = x[i ^ 4]; y[i + 1] = x[(i + 1) ^ 4];
+            mul_pair(y[i], y[i + 1], b[i], b[i + 1]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          float z0 = x[i], z1 = x[i + 1];
+          fma_pair(z0, z1, a[i], a[i + 1], y[i], y[i + 1]);
+          y[i] = z0; y[i + 1] = z1;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          y[i] = x[i]; y[i + 1] = x[i + 1];
+          mul_pair(y[i], y[i + 1], a[i], a[i + 1]);
+        }
+      }
+      if (o.w != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) mul_pair(y[i], y[i + 1], r, r);
+      }
+      if (mine && h0 + n * HPW < H) {
+        store4(dst + n * HPW * out.hd, y);
+        store4(dst + n * HPW * out.hd + to, y + 4);
+      }
     }
-    const int h = h0 + n * HPW;
-    if (mine && h < H) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
+    h0 += NH * HPW;
+    if (round + 1 >= rounds) break;
+    src += NH * HPW * o.hd;
+    dst += NH * HPW * out.hd;
+    load(h0);
   }
 }
 
@@ -352,8 +412,7 @@ __global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ Head
   const uint32_t k_blocks = p.k_blocks;
   const bool keys = blockIdx.x < k_blocks;
   const int H = keys ? p.Hkv : p.Hq;
-  constexpr int kAhead = APPEND ? 1 : NH;
-  const int step = HPW * (keys ? kAhead : NH);
+  const int rounds = keys ? 1 : p.rounds, step = HPW * (APPEND && keys ? 1 : NH * rounds);
   const uint32_t chunks = (H + step - 1) / step;         // of a token's heads
   const uint32_t warp = (blockIdx.x - (keys ? 0u : k_blocks)) * 8 + (threadIdx.x >> 5);
   const uint32_t row = warp / chunks;
@@ -363,7 +422,7 @@ __global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ Head
   const Operand o = keys ? Operand{p.k, p.ld_k, p.hd_k, p.k_w, p.k_vec} : Operand{p.q, p.ld_q, p.hd_q, p.q_w, p.q_vec};
   if (!APPEND || !keys) {
     turn_heads<LPH, NH>(p, o, keys ? Target{p.k_out, p.ld_k_out, p.hd_k_out, p.k_out_vec} : Target{p.q_out, p.ld_q_out, p.hd_q_out, p.q_out_vec},
-                        t, h0, H, in);
+                        t, h0, H, rounds, in);
     return;
   }
 
@@ -454,19 +513,25 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Kv
 }
 
 template <int LPH, bool APPEND, int NH>
-cudaError_t launch_heads_as(HeadsParams p, cudaStream_t stream) {
-  constexpr int HPW = 32 / LPH, kStep = HPW * (APPEND ? 1 : NH);
-  const int64_t k = (static_cast<int64_t>(p.T) * ((p.Hkv + kStep - 1) / kStep) + 7) / 8;
-  const int64_t q = (static_cast<int64_t>(p.T) * ((p.Hq + HPW * NH - 1) / (HPW * NH)) + 7) / 8;
+cudaError_t launch_heads_as(HeadsParams p, int rounds, cudaStream_t stream) {
+  constexpr int HPW = 32 / LPH, kKeys = HPW * (APPEND ? 1 : NH);
+  const int queries = HPW * NH * rounds;
+  const int64_t k = (static_cast<int64_t>(p.T) * ((p.Hkv + kKeys - 1) / kKeys) + 7) / 8;
+  const int64_t q = (static_cast<int64_t>(p.T) * ((p.Hq + queries - 1) / queries) + 7) / 8;
   if (k + q > 0x1fffffff) return cudaErrorInvalidValue;          // warps are numbered in 32 bits
   p.k_blocks = static_cast<uint32_t>(k);
+  p.rounds = rounds;
   return launch_pdl(heads_kernel<LPH, APPEND, NH>, dim3(static_cast<unsigned>(k + q)), dim3(256), 0, stream, p);
 }
 
+// One head to a lane group while there are few warps, then four, then four again and again while every SM keeps kSpread warps.
 template <int LPH, bool APPEND>
 cudaError_t launch_heads_as(const HeadsParams& p, int num_sms, cudaStream_t stream) {
-  const int64_t warps = static_cast<int64_t>(p.T) * (static_cast<int64_t>(p.Hq) + p.Hkv) / (32 / LPH);
-  return warps > static_cast<int64_t>(num_sms) * kSpread ? launch_heads_as<LPH, APPEND, 4>(p, stream) : launch_heads_as<LPH, APPEND, 1>(p, stream);
+  constexpr int HPW = 32 / LPH;
+  const int64_t warps = static_cast<int64_t>(p.T) * (static_cast<int64_t>(p.Hq) + p.Hkv) / HPW, few = static_cast<int64_t>(num_sms) * kSpread;
+  if (warps <= few) return launch_heads_as<LPH, APPEND, 1>(p, 1, stream);
+  const int most = max(1, (p.Hq + 4 * HPW - 1) / (4 * HPW));
+  return launch_heads_as<LPH, APPEND, 4>(p, static_cast<int>(min(static_cast<int64_t>(most), max(static_cast<int64_t>(1), warps / 4 / few))), stream);
 }
 
 }  // namespace

@@ -214,6 +214,7 @@ cudaError_t launch_few(const FewParams& p, bool bf16, int num_sms, cudaStream_t 
 struct HeadsParams {
   int T, Hq, Hkv, D, rot, interleaved, n_pos, w_f32;
   bool q_vec, k_vec, v_vec, q_out_vec, k_out_vec, w_vec;   // eight elements can be read or written as 16 bytes
+  bool quads;                // rows and angles can be read four elements at a time, pairs in fours
   bool rot_vec;              // a lane's eight elements turn with one other lane's (or among themselves), angles in 16-byte loads
   const __nv_bfloat16* q;
   const __nv_bfloat16* k;
@@ -226,12 +227,13 @@ struct HeadsParams {
   __nv_bfloat16* q_out;
   __nv_bfloat16* k_out;
   size_t ld_q, hd_q, ld_k, hd_k, ld_v, hd_v, ld_q_out, hd_q_out, ld_k_out, hd_k_out;
-  float eps;
+  float eps, inverse_d;
   uint32_t* status;
   int n_pages, page_size;    // append only, as all below
   const int32_t* slots;
   uint8_t* cache;
   uint32_t k_blocks;         // set by the launcher: blocks that take keys
+  int rounds;                // and how often a group of lanes takes its number of query heads
 };
 cudaError_t launch_heads(const HeadsParams& p, bool append, int num_sms, cudaStream_t stream);
 
