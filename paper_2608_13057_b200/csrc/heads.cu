@@ -84,6 +84,8 @@ __device__ __forceinline__ double inverse_root<double>(double v) { return rsqrt(
 
 // Warps per SM, with a head of each lane group to a warp, from which on a group takes four heads.
 constexpr int kSpread = 64;
+// Warps per SM that are kept when a group takes four heads again and again.
+constexpr int kRounds = 16;
 
 // One operand of the launch: queries or keys.
 struct Operand {
@@ -524,14 +526,15 @@ cudaError_t launch_heads_as(HeadsParams p, int rounds, cudaStream_t stream) {
   return launch_pdl(heads_kernel<LPH, APPEND, NH>, dim3(static_cast<unsigned>(k + q)), dim3(256), 0, stream, p);
 }
 
-// One head to a lane group while there are few warps, then four, then four again and again while every SM keeps kSpread warps.
+// One head to a lane group while there are few warps, then four, then four again and again up to all of a token's.
 template <int LPH, bool APPEND>
 cudaError_t launch_heads_as(const HeadsParams& p, int num_sms, cudaStream_t stream) {
   constexpr int HPW = 32 / LPH;
   const int64_t warps = static_cast<int64_t>(p.T) * (static_cast<int64_t>(p.Hq) + p.Hkv) / HPW, few = static_cast<int64_t>(num_sms) * kSpread;
   if (warps <= few) return launch_heads_as<LPH, APPEND, 1>(p, 1, stream);
   const int most = max(1, (p.Hq + 4 * HPW - 1) / (4 * HPW));
-  return launch_heads_as<LPH, APPEND, 4>(p, static_cast<int>(min(static_cast<int64_t>(most), max(static_cast<int64_t>(1), warps / 4 / few))), stream);
+  const int chunks = static_cast<int>(min(static_cast<int64_t>(most), (static_cast<int64_t>(num_sms) * kRounds + p.T - 1) / p.T));   // of a token
+  return launch_heads_as<LPH, APPEND, 4>(p, (most + chunks - 1) / chunks, stream);
 }
 
 }  // namespace
