@@ -102,10 +102,11 @@ struct Target {
 };
 
 // A lane's eight elements of norm(x) * w turned by the row's angles, in R.  `e` is the lane's first element, beyond D for a
-// lane without one; every lane of the warp takes part in the shuffles.  The loads from x are done when this returns.
+// lane without one; every lane of the warp takes part in the shuffles.  The loads from x are done when this returns.  amplitude: the
+// most that an element's two products add up to without their signs.
 template <int LPH, typename R>
 __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, size_t at, int e, bool live, const float* angles,
-                                       uint4 raw, R (&y)[8]) {
+                                       uint4 raw, R (&y)[8], float& amplitude) {
   const int lane = threadIdx.x & 31, half = p.rot / 2;
   const bool mine = live && e < p.D;
   float x[8], w[8];
@@ -122,6 +123,9 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, s
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = o.w != nullptr ? R(x[i]) * r * R(w[i]) : R(x[i]);
+  amplitude = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])));
   if (p.rot == 0) return;
 
   if (p.interleaved) {
@@ -143,6 +147,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, s
     for (int i = 0; i < 4; ++i) {
       if (e + 2 * i >= p.rot) continue;                 // unturned elements pass as they are
       const R a = y[2 * i], b = y[2 * i + 1];
+      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(a)) + fabsf(static_cast<float>(b)));
       y[2 * i] = a * R(c[i]) - b * R(s[i]);
       y[2 * i + 1] = b * R(c[i]) + a * R(s[i]);
     }
@@ -173,6 +178,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, s
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const R other = o.w != nullptr ? R(x[i]) * r * R(w[i]) : R(x[i]);
+      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
       y[i] = first ? y[i] * R(c[i]) - other * R(s[i]) : y[i] * R(c[i]) + other * R(s[i]);
     }
     return;
@@ -186,6 +192,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, s
       const int eo = first ? e + i + half : e + i - half, a = first ? e + i : eo;
       const float xo = __bfloat162float(*(o.x + at + eo));
       const R other = o.w != nullptr ? R(xo) * r * R(weight1(o.w, p.w_f32, eo)) : R(xo);
+      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
       const R c = R(__ldg(angles + a)), s = R(__ldg(angles + half + a));
       y[i] = first ? y[i] * c - other * s : y[i] * c + other * s;
     }
@@ -292,7 +299,8 @@ __device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& 
       const bool in = live && h < H && e < p.D;
       float y[8];
       const uint4 u = in ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
-      turned<LPH, float>(p, o, t * o.ld + (h < H ? h : 0) * o.hd, e, live && h < H, angles, u, y);
+      float unused;
+      turned<LPH, float>(p, o, t * o.ld + (h < H ? h : 0) * o.hd, e, live && h < H, angles, u, y, unused);
       __syncwarp();                                     // in place: every load of the warp's heads comes before the stores
       if (in) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
     }
@@ -403,8 +411,59 @@ __device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& 
   }
 }
 
+// The same in 32 bits, for elements that are off by at most `off` (EXACT: not at all, as they came), with `sure`: whether no border
+// was so near that the exact elements might have another scale, zero point or code.
+template <bool EXACT>
+__device__ __forceinline__ uint32_t quantise8_near(const float (&y)[8], float off, uint32_t& params, bool& sure) {
+  float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { lo = fminf(lo, y[i]); hi = fmaxf(hi, y[i]); }
+#pragma unroll
+  for (int d = 1; d <= 2; d *= 2) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+  }
+  const float range = hi - lo, step = range * (1.0f / 15.0f);
+  const int exponent = max(static_cast<int>(__float_as_uint(step) >> 23) - 127 - 3, -17);
+  const float up = __uint_as_float(static_cast<uint32_t>(127 + exponent) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - exponent) << 23);
+  float s = ceilf(step * down) * up;
+  params = 0;
+  if constexpr (EXACT) {                               // 15 s and the difference have few bits: compared as they are
+    sure = range + lo == hi && hi - range == lo && range < 11000.0f;
+    if (15.0f * (s - up) >= range) s -= up;
+    if (15.0f * s < range) s += up;
+  } else {
+    const float doubt = 4.0f * off + 1e-6f * range;    // of the range: both ends, and a few roundings
+    sure = range == 0.0f ? off == 0.0f : range < 15.0f * s - doubt && range > 15.0f * (s - up) + doubt && range < 11000.0f;
+  }
+  if (range == 0.0f || !sure) return 0;
+  const float inverse = __fdividef(1.0f, s);           // s has four significant bits: off by 2^-22 at most
+  // a quotient is off by off / s and a few roundings of at most 16
+  const float border = 0.5f - off * inverse - 8e-6f;
+  const auto nearest = [&](float x) {                  // |x / s| is at most 16
+    const float q = x * inverse, k = (q + 12582912.0f) - 12582912.0f;
+    if constexpr (!EXACT) sure = sure && fabsf(q - k) < border;
+    if constexpr (EXACT) {
+      const float rest = fmaf(-k, s, x), h = 0.5f * s;
+      const bool odd = (__float_as_uint(k + 12582912.0f) & 1u) != 0;
+      if (rest > h || (rest == h && odd)) return k + 1.0f;
+      if (rest < -h || (rest == -h && odd)) return k - 1.0f;
+    }
+    return k;
+  };
+  const float z = fminf(nearest(-lo), 15.0f);
+  params = (static_cast<uint32_t>(__half_as_ushort(__float2half(s))) >> 7) | (static_cast<uint32_t>(z) << 12);
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float c = fminf(fmaxf(nearest(y[i]) + z, 0.0f), 15.0f);
+    word |= (__float_as_uint(c + 8388608.0f) & 15u) << (4 * i);
+  }
+  return word;
+}
+
 template <int LPH, bool APPEND, int NH>
-__global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ HeadsParams p) {
+__global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ HeadsParams p) {
   constexpr int HPW = 32 / LPH;                          // heads of a warp at a time
   pdl_trigger();
   pdl_wait();
@@ -436,20 +495,39 @@ __global__ void __launch_bounds__(256) heads_kernel(const __grid_constant__ Head
   uint4 raw = mine ? load8(o.x + at + e, o.vec) : zero;
   const uint4 raw_v = mine ? load8(p.v + t * p.ld_v + h * p.hd_v + e, p.v_vec) : zero;
   const int slot = live ? p.slots[t] : -1;
-  double y[8];
-  turned<LPH, double>(p, o, at, e, live, angles_of(p, t, live), raw, y);
+  const float* angles = angles_of(p, t, live);
   float v[8];
   widen8(raw_v, v);
+  uint32_t pk, pv, wk, wv;
   bool bad = false;
+  {
+    // In 32 bits first.  An element is off by less than 2^-20 of its amplitude: 2^-22 of the inverse root, half of 12 roundings of
+    // 2^-24 of the sum of squares, five of the products.
+    float y[8], amplitude;
+    turned<LPH, float>(p, o, at, e, live, angles, raw, y, amplitude);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (!isfinite(y[i])) { y[i] = 0.0; bad = true; }
-    if (!isfinite(v[i])) { v[i] = 0.0f; bad = true; }
+    for (int d = 1; d <= 2; d *= 2) amplitude = fmaxf(amplitude, __shfl_xor_sync(0xffffffffu, amplitude, d));
+    bool sure_k, sure_v;
+    wk = quantise8_near<false>(y, amplitude * 0x1p-19f, pk, sure_k);
+    wv = quantise8_near<true>(v, 0.0f, pv, sure_v);
+    bool fine = sure_k && sure_v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fine = fine && isfinite(v[i]) && isfinite(y[i]);
+    if (__any_sync(0xffffffffu, mine && !fine)) {
+      // Some element of the warp is next to a border (1 to 2 warps of 100) or not finite: all of them in 64 bits.
+      double exact[8];
+      turned<LPH, double>(p, o, at, e, live, angles, raw, exact, amplitude);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (!isfinite(exact[i])) { exact[i] = 0.0; bad = true; }
+        if (!isfinite(v[i])) { v[i] = 0.0f; bad = true; }
+      }
+      const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
+      bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
+      wk = quantise8<double>(exact, pk);
+      wv = quantise8<float>(v, pv);
+    }
   }
-  const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
-  bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
-  uint32_t pk, pv;
-  const uint32_t wk = quantise8<double>(y, pk), wv = quantise8<float>(v, pv);
   if (bad) pk |= kMarked;
   if (!live) return;
   if (slot < 0 || slot >= p.n_pages * p.page_size) {
