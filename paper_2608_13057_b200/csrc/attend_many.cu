@@ -22,7 +22,6 @@ constexpr int kThreads = 512;                         // four warpgroups: loader
 constexpr int kKeys = 128, kRowTile = 128, kRows = 2 * kRowTile;
 static_assert(kRows == kAttendManyRows, "the workspace is sized for it");
 constexpr int kDecoders = 6;                          // warps 2 to 7
-constexpr int kEvery = 4;                             // every fourth pair of exponentials is computed on the FMA pipe
 using Tiles = Cut<kRows, kKeys>;
 using Item = Tiles::Item;
 
@@ -91,6 +90,11 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // (a, b) * f + (m, m)
 __device__ __forceinline__ void fma_pair(float& a, float& b, float f, float m) {
   asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
@@ -109,26 +113,32 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int rows, int row, i
 // ---- decoders -----------------------------------------------------------------------------------------
 // Keys of one stage.  A lane takes 32 neighbouring elements of a key: one group, four words, four 16-byte stores.
 template <int D>
-__device__ __forceinline__ void decode_keys(const Decode& dc, const uint8_t* stage, uint32_t tile, uint32_t absent, int warp) {
+__device__ __forceinline__ void decode_keys(const Decode& dc, const uint8_t* stage, uint8_t* tile, uint32_t absent, int warp) {
   using U = CacheUnit<D>;
   constexpr int kParts = D / 32, kPer = 32 / kParts;                     // lanes to a key, keys to a warp
-  const int lane = threadIdx.x & 31, j = lane % kParts;
+  const int lane = threadIdx.x & 31, j = lane % kParts, at = lane / kParts;
+  // Key task * kPer + at is in row at % 8 of its eight whatever the task: the swizzle is the lane's own.  The second block's lanes
+  // store in another order, so that no bank is met twice.
+  const bool turn = D == 128 && (j & 2) != 0;
+  uint8_t* to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    to[i] = tile + j / 2 * kKeys * 128 + at * 128 + (((4 * (j & 1) + (turn ? i ^ 2 : i)) ^ (at & 7)) << 4);
 #pragma unroll 1
   for (int task = warp; task < kKeys / kPer; task += kDecoders) {
-    const int key = task * kPer + lane / kParts;
+    const int key = task * kPer + at;
     const uint8_t* unit = stage + key / kUnit * U::kBytes;
     const uint4 u = *reinterpret_cast<const uint4*>(unit + key % kUnit * U::kKeyRow + j * 16);
     uint32_t params = *reinterpret_cast<const uint16_t*>(unit + U::kCodes + key % kUnit * U::kKeyParams + j * 2) * 0x10001u;
-    if (absent >> (key / kUnit) & 1) params |= kMarked * 0x10001u;
+    if (absent != 0 && (absent >> (key / kUnit) & 1)) params |= kMarked * 0x10001u;
     uint32_t s, b;
     group_params(params, s, b);
-    const bool turn = D == 128 && (j & 2) != 0;                          // the second block's lanes in another order: no bank twice
     const uint32_t w[4] = {turn ? u.z : u.x, turn ? u.w : u.y, turn ? u.x : u.z, turn ? u.y : u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t v[4];
       decode8(dc, w[i], s, b, v);
-      st_shared_v4(chunk_at(tile, kKeys, key, j / 2, 4 * (j & 1) + (turn ? i ^ 2 : i)), make_uint4(v[0], v[1], v[2], v[3]));
+      *reinterpret_cast<uint4*>(to[i] + task * (kPer * 128)) = make_uint4(v[0], v[1], v[2], v[3]);
     }
   }
 }
@@ -137,33 +147,35 @@ __device__ __forceinline__ void decode_keys(const Decode& dc, const uint8_t* sta
 // eight tokens.  Element 8 x + 4 e + n is row 64 (x / 8) + 8 (4 e + n) + x % 8 of the tile: no bank twice in a store, and 64
 // neighbouring rows are 64 neighbouring elements.
 template <int D>
-__device__ __forceinline__ void decode_values(const Decode& dc, const uint8_t* stage, uint32_t tile, int t0, int len, int warp) {
+__device__ __forceinline__ void decode_values(const Decode& dc, const uint8_t* stage, uint8_t* tile, int left, int warp) {
   using U = CacheUnit<D>;
   constexpr int kX = D / 8, kPer = 32 / kX;                              // lanes to eight tokens, eights of tokens to a warp
   const int lane = threadIdx.x & 31, x = lane % kX;
 #pragma unroll 1
   for (int task = warp; task < kKeys / 8 / kPer; task += kDecoders) {
     const int eight = task * kPer + lane / kX;
-    const uint8_t* unit = stage + eight / 2 * U::kBytes;
+    const uint8_t* unit = stage + eight / 2 * U::kBytes + (eight & 1) * 4 * U::kPairRow + x * 8;
+    const uint8_t* unit_params = stage + eight / 2 * U::kBytes + U::kCodes + (eight & 1) * 4 * U::kPairParams + x / 4 * 4;
     uint32_t v[4][2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int pair = (eight & 1) * 4 + i;
-      const uint2 w = *reinterpret_cast<const uint2*>(unit + pair * U::kPairRow + x * 8);
-      uint32_t params = *reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + x / 4 * 4);
-      const int left = len - (t0 + 8 * eight + 2 * i);                   // tokens of the pair that exist
-      if (left < 2) params &= left == 1 ? 0xffffu : 0u;
+      const uint2 w = *reinterpret_cast<const uint2*>(unit + i * U::kPairRow);
+      uint32_t params = *reinterpret_cast<const uint32_t*>(unit_params + i * U::kPairParams);
+      if (left < kKeys) {                                                // tokens of the pair that exist
+        const int here = left - (8 * eight + 2 * i);
+        if (here < 2) params &= here == 1 ? 0xffffu : 0u;
+      }
       uint32_t s, b;
       group_params(params, s, b);
       decode8(dc, w.x, s, b, v[i][0]);
       decode8(dc, w.y, s, b, v[i][1]);
     }
+    uint8_t* to = tile + eight / 8 * D * 128 + (x / 8 * 64 + x % 8) * 128 + (((eight ^ x) & 7) << 4);
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        st_shared_v4(chunk_at(tile, D, x / 8 * 64 + (4 * e + n) * 8 + x % 8, eight / 8, eight % 8),
-                     make_uint4(v[0][e][n], v[1][e][n], v[2][e][n], v[3][e][n]));
+        *reinterpret_cast<uint4*>(to + (4 * e + n) * 1024) = make_uint4(v[0][e][n], v[1][e][n], v[2][e][n], v[3][e][n]);
   }
 }
 
@@ -244,26 +256,6 @@ __device__ __forceinline__ void store_half(const Row& r, int y, const float (&o)
     }
     reinterpret_cast<uint4*>(r.out)[8 * y + x] = make_uint4(v[0], v[1], v[2], v[3]);
   }
-}
-
-// 2^a and 2^b without the special-function unit, which alone would take as long as the products: n the nearest integer, a
-// polynomial of degree 4 for 2^(a - n) (least relative error on [-1/2, 1/2], 2.6e-6), times 2^n.  NaN stays NaN.
-__device__ __forceinline__ void exp2_pair(float& a, float& b) {
-  asm("max.NaN.f32 %0, %0, 0fC2FA0000;\n\tmax.NaN.f32 %1, %1, 0fC2FA0000;" : "+f"(a), "+f"(b));      // -125
-  asm("{\n\t.reg .b64 y, t, n, r, q, c;\n\t.reg .f32 cf;\n\t.reg .b32 t0, t1;\n\t"
-      "mov.b64 y, {%0, %1};\n\t"
-      "mov.f32 cf, 0f4B400000;\n\tmov.b64 c, {cf, cf};\n\tadd.rn.f32x2 t, y, c;\n\t"
-      "mov.f32 cf, 0fCB400000;\n\tmov.b64 c, {cf, cf};\n\tadd.rn.f32x2 n, t, c;\n\t"
-      "mov.f32 cf, 0fBF800000;\n\tmov.b64 c, {cf, cf};\n\tfma.rn.f32x2 r, n, c, y;\n\t"
-      "mov.b64 q, {%2, %2};\n\tmov.b64 c, {%3, %3};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
-      "mov.b64 c, {%4, %4};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
-      "mov.b64 c, {%5, %5};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
-      "mov.b64 c, {%6, %6};\n\tfma.rn.f32x2 q, q, r, c;\n\t"
-      "mov.b64 {t0, t1}, t;\n\tshl.b32 t0, t0, 23;\n\tadd.u32 t0, t0, 0x3f800000;\n\t"
-      "shl.b32 t1, t1, 23;\n\tadd.u32 t1, t1, 0x3f800000;\n\tmov.b64 c, {t0, t1};\n\t"
-      "mul.rn.f32x2 q, q, c;\n\tmov.b64 {%0, %1}, q;\n\t}"
-      : "+f"(a), "+f"(b)
-      : "f"(0.009570101276040077f), "f"(0.05591785907745361f), "f"(0.240247443318367f), "f"(0.6931217908859253f), "f"(0.9999992847442627f));
 }
 
 template <int D>
@@ -441,8 +433,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
             fine = wait(kv == 0 ? bars.k_empty[buf] : bars.v_empty[buf], (t >> 1 & 1) ^ 1) && wait(bars.code_full[stage], phase);
             if (!fine) break;
             const uint8_t* codes = smem + S::kCodes + stage * S::kStageBytes;
-            if (kv == 0) decode_keys<D>(dc, codes, base + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
-            else decode_values<D>(dc, codes, base + S::kV + buf * S::kTileBytes, (pc.tile0() + i) * kKeys, pc.it.len, warp - 2);
+            if (kv == 0) decode_keys<D>(dc, codes, smem + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
+            else decode_values<D>(dc, codes, smem + S::kV + buf * S::kTileBytes, pc.it.len - (pc.tile0() + i) * kKeys, warp - 2);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -504,10 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
               for (int v = 0; v < 128; ++v)
                 if (v > see) c[v / 32][v % 32] = 0xff800000u;
             }
-            float top = -INFINITY;
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int v = 0; v < 128; v += 2)
-              top = fmaxf(top, fmaxf(__uint_as_float(c[v / 32][v % 32]), __uint_as_float(c[v / 32][v % 32 + 1])));
+            for (int v = 0; v < 128; v += 2) tops[v / 2 % 4] = max3(tops[v / 2 % 4], __uint_as_float(c[v / 32][v % 32]), __uint_as_float(c[v / 32][v % 32 + 1]));
+            float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
             top *= cur.f;
             if (__any_sync(0xffffffffu, top > m + kSlack)) {
               const float to = top > m + kSlack ? top : m;
@@ -535,12 +527,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
               for (int v = 0; v < 32; ++v) {
                 float a = __uint_as_float(c[2 * h + v / 16][v % 16 * 2]), b = __uint_as_float(c[2 * h + v / 16][v % 16 * 2 + 1]);
                 fma_pair(a, b, cur.f, less);
-                if (v % kEvery == kEvery - 1) {
-                  exp2_pair(a, b);
-                } else {
-                  a = exp2_fast(a);
-                  b = exp2_fast(b);
-                }
+                a = exp2_fast(a);
+                b = exp2_fast(b);
                 add_pair(l[v & 1][0], l[v & 1][1], a, b);
                 w[v] = as_u32(__floats2half2_rn(a, b));
               }
