@@ -749,6 +749,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.q = static_cast<const __nv_bfloat16*>(q); p.cache = static_cast<const uint8_t*>(cache);
   p.page_table = page_table; p.lens = lens; p.q_start = q_start; p.out = static_cast<__nv_bfloat16*>(out);
   p.ld_q = a->ld_q; p.hd_q = a->hd_q; p.ld_out = a->ld_out; p.hd_out = a->hd_out;
+  p.wide = aligned(q, 32) && a->ld_q % 16 == 0 && a->hd_q % 16 == 0 && aligned(out, 32) && a->ld_out % 16 == 0 && a->hd_out % 16 == 0;
   p.scale_log2 = a->scale * 1.4426950408889634f; p.status = status;
   p.counters = reinterpret_cast<unsigned int*>(ws + L.off_counters);
   p.stats = reinterpret_cast<float*>(ws + L.off_stats); p.part = reinterpret_cast<float*>(ws + L.off_out);

@@ -82,6 +82,25 @@ struct Cut {
   template <int WARPS>
   static __device__ __forceinline__ int count_tiles(const AttendParams& p, int* before, int* warp_sum, bool tell) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (kRows > 16 && p.B <= WARPS) {                  // few long sequences: a warp to each
+      if (warp < p.B) {
+        int len, q0, n, mine = 0;
+        span_of(p, warp, len, q0, n, tell);
+        for (int row0 = lane * kRows; row0 < n * p.group; row0 += 32 * kRows) mine += tiles_of(len, n, p.group, row0);
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+        if (lane == 0) warp_sum[warp] = mine * p.Hkv;
+      }
+      __syncthreads();
+      int total = 0;
+      for (int b = 0; b < p.B; ++b) {
+        if (tid == b) before[b] = total;
+        total += warp_sum[b];
+      }
+      if (tid == 0) before[p.B] = total;
+      __syncthreads();
+      return total;
+    }
     int total = 0;
     for (int b0 = 0; b0 < p.B; b0 += WARPS * 32) {
       const int b = b0 + tid;

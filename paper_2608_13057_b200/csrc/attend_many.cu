@@ -187,74 +187,77 @@ struct Row {
   __nv_bfloat16* out;
 };
 
-// A warp's 32 rows of queries, from row `r0` of the item on, into their row tile as fp16 in the order of the decoded keys; each lane
-// gets its own row's factors.  D / 8 lanes to a row, so that a load takes whole lines.
+// 32 bytes in one access: with a row to a thread every access meets 32 lines, and their number is what it costs.
+__device__ __forceinline__ void load32(const void* src, uint32_t (&v)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(src));
+}
+__device__ __forceinline__ void store32(void* dst, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+// This thread's row of queries into its row tile, as fp16 in the order of the decoded keys.
 template <int D>
-__device__ __forceinline__ Row load_rows(const AttendParams& p, const Item& it, int r0, uint32_t tile, int row_in_tile0) {
-  constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-  const int lane = threadIdx.x & 31, c = lane % kLanes;
-  const int rows = it.n * p.group;
+__device__ __forceinline__ Row load_row(const AttendParams& p, const Item& it, int r, uint32_t tile, int row_in_tile) {
   Row o;
-  {
-    const int row = it.row0 + r0 + lane, qi = row / p.group;
-    o.in = row < rows;
-    o.limit = o.in ? it.len - it.n + qi : it.len - 1;
-    o.out = p.out + static_cast<size_t>(it.q0 + qi) * p.ld_out + static_cast<size_t>(it.h * p.group + row % p.group) * p.hd_out;
+  const int row = it.row0 + r, qi = row / p.group, head = it.h * p.group + row - qi * p.group;
+  o.in = row < it.n * p.group;
+  o.limit = o.in ? it.len - it.n + qi : it.len - 1;
+  o.out = p.out + static_cast<size_t>(it.q0 + qi) * p.ld_out + static_cast<size_t>(head) * p.hd_out;
+  const __nv_bfloat16* src = p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q + static_cast<size_t>(head) * p.hd_q;
+  uint32_t u[D / 16][8];
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    if (o.in && p.wide) {
+      load32(src + 16 * c, u[c]);
+    } else {
+      const uint4 zero = make_uint4(0, 0, 0, 0);
+      const uint4 a = o.in ? __ldg(reinterpret_cast<const uint4*>(src) + 2 * c) : zero, b = o.in ? __ldg(reinterpret_cast<const uint4*>(src) + 2 * c + 1) : zero;
+      u[c][0] = a.x; u[c][1] = a.y; u[c][2] = a.z; u[c][3] = a.w; u[c][4] = b.x; u[c][5] = b.y; u[c][6] = b.z; u[c][7] = b.w;
+    }
   }
-  o.f = 1.0f;
-#pragma unroll 1
-  for (int i0 = 0; i0 < 32; i0 += 8 * kAtOnce) {
-    uint4 u[8];
+  uint32_t most = 0;                                   // the largest magnitudes as integers: infinities and NaN come out on top
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = __vmaxu2(most, u[c][i] & 0x7fff7fffu);
+  most = max(most & 0xffffu, most >> 16);
+  float up;
+  row_factors(__uint_as_float(most << 16), most >= 0x7f80u, p.scale_log2, up, o.f);
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = it.row0 + r0 + i0 + i * kAtOnce + lane / kLanes, qi = row / p.group;
-      u[i] = make_uint4(0, 0, 0, 0);
-      if (i0 + i * kAtOnce < 32 && row < rows)
-        u[i] = __ldg(reinterpret_cast<const uint4*>(p.q + static_cast<size_t>(it.q0 + qi) * p.ld_q +
-                                                    static_cast<size_t>(it.h * p.group + row % p.group) * p.hd_q) + c);
+      const uint32_t v = u[c / 2][4 * (c & 1) + i / 2];
+      x[i] = __uint_as_float((i & 1) ? (v & 0xffff0000u) : (v << 16)) * up;
     }
+    uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int at = i0 + i * kAtOnce;                 // of the warp's rows
-      if (at >= 32) break;
-      const uint32_t v[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
-      float x[8], top = 0.0f, up, f;
-      int odd = 0;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        x[n] = __uint_as_float((n & 1) ? (v[n / 2] & 0xffff0000u) : (v[n / 2] << 16));
-        top = fmaxf(top, fabsf(x[n]));
-        odd |= !isfinite(x[n]);
-      }
-#pragma unroll
-      for (int d = kLanes / 2; d > 0; d /= 2) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        odd |= __shfl_xor_sync(0xffffffffu, odd, d);
-      }
-      row_factors(top, odd != 0, p.scale_log2, up, f);
-      const float given = __shfl_sync(0xffffffffu, f, (lane - at) * kLanes & 31);      // row at + n is the lanes' from n kLanes on
-      if (lane >= at && lane < at + kAtOnce) o.f = given;
-      uint32_t h[4];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) h[n] = as_u32(__floats2half2_rn(x[n] * up, x[n + 4] * up));
-      st_shared_v4(chunk_at(tile, kRowTile, row_in_tile0 + at + lane / kLanes, c / 8, c % 8), make_uint4(h[0], h[1], h[2], h[3]));
-    }
+    for (int n = 0; n < 4; ++n) h[n] = as_u32(__floats2half2_rn(x[n], x[n + 4]));
+    st_shared_v4(chunk_at(tile, kRowTile, row_in_tile, c / 8, c % 8), make_uint4(h[0], h[1], h[2], h[3]));
   }
   return o;
 }
 
 // Columns [64 y, 64 y + 64) of O in the row's elements 64 y on: column 8 (4 e + n) + x is element 8 x + 4 e + n of them.
-__device__ __forceinline__ void store_half(const Row& r, int y, const float (&o)[64], float k) {
+__device__ __forceinline__ void store_half(const Row& r, int y, const float (&o)[64], float k, bool wide) {
   if (!r.in) return;
 #pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    uint32_t v[4];
+  for (int x = 0; x < 8; x += 2) {
+    uint32_t v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(o[16 * i + x] * k, o[16 * i + 8 + x] * k);
+    for (int i = 0; i < 8; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(o[16 * (i % 4) + x + i / 4] * k, o[16 * (i % 4) + 8 + x + i / 4] * k);
       v[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    reinterpret_cast<uint4*>(r.out)[8 * y + x] = make_uint4(v[0], v[1], v[2], v[3]);
+    if (wide) {
+      store32(r.out + 64 * y + 8 * x, v);
+    } else {
+      reinterpret_cast<uint4*>(r.out)[8 * y + x] = make_uint4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<uint4*>(r.out)[8 * y + x + 1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
   }
 }
 
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       Row mine;
       const auto load = [&](const Pieces& c) {
         if (x == 1 && !c.two(p.group)) return;
-        mine = load_rows<D>(p, c.it, r - lane, q_tile, row - lane);
+        mine = load_row<D>(p, c.it, r, q_tile, row);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(bars.q_full[x]));
@@ -573,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
 #pragma unroll
             for (int i = 0; i < 64; ++i) o[i] = __uint_as_float(v[i / 32][i % 32]);
             if (ctas == 1) {
-              store_half(cur, y, o, k);
+              store_half(cur, y, o, k, p.wide);
             } else {
 #pragma unroll
               for (int q = 0; q < 16; ++q)
@@ -619,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
                 o[4 * q] += v[q].x * k; o[4 * q + 1] += v[q].y * k; o[4 * q + 2] += v[q].z * k; o[4 * q + 3] += v[q].w * k;
               }
             }
-            store_half(cur, y, o, all == 0.0f ? 0.0f : 1.0f / all);
+            store_half(cur, y, o, all == 0.0f ? 0.0f : 1.0f / all, p.wide);
           }
         }
         fine = sync_softmax();                         // s_last is read before the next item's is written
