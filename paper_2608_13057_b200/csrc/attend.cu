@@ -336,35 +336,40 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, float4 v, float k) {
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// Parts of an item one after the other: their sums under the common maximum.
+// Parts of an item one after the other: their sums under the common maximum, for eight elements of a row as two quads.
 struct Merged {
   float m = -INFINITY, l = 0.0f;
-  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float4 o[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
   __device__ __forceinline__ float factor() const { return l == 0.0f ? 0.0f : 1.0f / l; }
 };
-// `stat(i)` and `quad(i)` read part i's (m, l) of the row and four of its elements; BATCH parts' loads are in flight together.
+// `stat(i)` and `quad(i, y)` read part i's (m, l) of the row and quad y; BATCH parts' loads are in flight together.
 template <int BATCH, typename Stat, typename Quad>
 __device__ __forceinline__ Merged merge(int n, Stat stat, Quad quad) {
   Merged r;
   for (int i0 = 0; i0 < n; i0 += BATCH) {
     float2 st[BATCH];
-    float4 v[BATCH];
+    float4 v[BATCH][2];
 #pragma unroll
     for (int i = 0; i < BATCH; ++i)
-      if (i0 + i < n) { st[i] = stat(i0 + i); v[i] = quad(i0 + i); }
+      if (i0 + i < n) { st[i] = stat(i0 + i); v[i][0] = quad(i0 + i, 0); v[i][1] = quad(i0 + i, 1); }
     float m = r.m;
 #pragma unroll
     for (int i = 0; i < BATCH; ++i)
       if (i0 + i < n) m = fmaxf(m, st[i].x);
     const float ref = m == -INFINITY ? 0.0f : m, before = exp2_fast(r.m - ref);
     r.m = m;
-    r.l *= before; r.o.x *= before; r.o.y *= before; r.o.z *= before; r.o.w *= before;
+    r.l *= before;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) { r.o[y].x *= before; r.o[y].y *= before; r.o[y].z *= before; r.o[y].w *= before; }
 #pragma unroll
     for (int i = 0; i < BATCH; ++i)
       if (i0 + i < n) {
         const float k = exp2_fast(st[i].x - ref);
         r.l += st[i].y * k;
-        r.o.x += v[i].x * k; r.o.y += v[i].y * k; r.o.z += v[i].z * k; r.o.w += v[i].w * k;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          r.o[y].x += v[i][y].x * k; r.o[y].y += v[i][y].y * k; r.o[y].z += v[i][y].z * k; r.o[y].w += v[i][y].w * k;
+        }
       }
   }
   return r;
@@ -542,22 +547,28 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   }
   __syncthreads();
 
-  constexpr int kQuads = kRows * D / 4, kStats = kRows * D * 4;
+  // Two quads of a row, q and q + D / 8, to a thread.
+  constexpr int kTasks = kRows * D / 8, kStats = kRows * D * 4;
   const int segs = n_segments;
-  for (int task = tid; task < segs * kQuads; task += kWarps * 32) {
-    const Segment<Item>& g = segments[task / kQuads];
-    const int row = task % kQuads / (D / 4), q = task % (D / 4);
+  for (int task = tid; task < segs * kTasks; task += kWarps * 32) {
+    const Segment<Item>& g = segments[task / kTasks];
+    const int row = task % kTasks / (D / 8), q = task % (D / 8);
     const uint8_t* kept = smem + F::kParts + g.warp * F::kPart;
     const uint8_t* first = g.late ? smem + g.warp * F::kPart : kept;
     const auto part = [&](int i) { return i == 0 ? first : kept + i * F::kPart; };
     const Merged r = merge<2>(
         g.more + 1, [&](int i) { return reinterpret_cast<const float2*>(part(i) + kStats)[row]; },
-        [&](int i) { return reinterpret_cast<const float4*>(part(i))[row * (D / 4) + part_at(row, q)]; });
+        [&](int i, int y) { return reinterpret_cast<const float4*>(part(i))[row * (D / 4) + part_at(row, q + y * (D / 8))]; });
     if (g.slot < 0) {
-      if (g.item.row0 + row < g.item.n * p.group) store4(out_row(p, g.item, row) + 4 * q, r.o, r.factor());
+      if (g.item.row0 + row < g.item.n * p.group) {
+        __nv_bfloat16* dst = out_row(p, g.item, row) + 4 * q;
+        store4(dst, r.o[0], r.factor());
+        store4(dst + D / 2, r.o[1], r.factor());
+      }
     } else {
       const size_t at = (static_cast<size_t>(blockIdx.x) * 2 + g.slot) * kRows + row;
-      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q, r.o);
+      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q, r.o[0]);
+      __stcg(reinterpret_cast<float4*>(p.part + at * D) + q + D / 8, r.o[1]);
       if (q == 0) __stcg(reinterpret_cast<float2*>(p.stats) + at, make_float2(r.m, r.l));
     }
   }
@@ -576,13 +587,17 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
     if (g.slot < 0 || !g.last) continue;
     __threadfence();
     const int begin0 = g.item.begin > runs.begin(g.cta0 * warps) ? 1 : 0;
-    for (int task = tid; task < kQuads; task += kWarps * 32) {
-      const int row = task / (D / 4), q = task % (D / 4);
+    for (int task = tid; task < kTasks; task += kWarps * 32) {
+      const int row = task / (D / 8), q = task % (D / 8);
       const auto at = [&](int c) { return (static_cast<size_t>(g.cta0 + c) * 2 + (c == 0 ? begin0 : 0)) * kRows + row; };
       const Merged r = merge<8>(
           g.ctas, [&](int c) { return __ldcg(reinterpret_cast<const float2*>(p.stats) + at(c)); },
-          [&](int c) { return __ldcg(reinterpret_cast<const float4*>(p.part + at(c) * D) + q); });
-      if (g.item.row0 + row < g.item.n * p.group) store4(out_row(p, g.item, row) + 4 * q, r.o, r.factor());
+          [&](int c, int y) { return __ldcg(reinterpret_cast<const float4*>(p.part + at(c) * D) + q + y * (D / 8)); });
+      if (g.item.row0 + row < g.item.n * p.group) {
+        __nv_bfloat16* dst = out_row(p, g.item, row) + 4 * q;
+        store4(dst, r.o[0], r.factor());
+        store4(dst + D / 2, r.o[1], r.factor());
+      }
     }
   }
 }
@@ -615,8 +630,9 @@ AttendLayout attend_layout(int D) {
   return L;
 }
 
-// Sequences of up to kFewRows rows are this kernel's, longer ones the other's.
-constexpr int kFewRows = 64;
+// Sequences of up to kFewRows rows are this kernel's, longer ones the other's.  128 keys of a head take this one 1300 clocks of an SM
+// for each 16 rows and the other 4000 for any number up to 128.
+constexpr int kFewRows = 48;
 
 cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(max_q) * p.group;
