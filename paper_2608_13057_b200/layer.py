@@ -1,7 +1,10 @@
-"""One mixture-of-experts layer of a served model on one rank: the norm before the block, the router, this rank's experts,
-and the norm after it with the block's gate, the residual sum and the next block's norm.
+"""The two halves of a served model's layer on one rank.
 
-Batches of up to `few_tokens` (FEW_TOKENS, fewer above 16 choices per token) run in four kernels (norm, router, few-token
+MoELayer: the norm before the block, the router, this rank's experts, and the norm after it with the block's gate, the residual
+sum and the next block's norm.  Attention: what lies between the projections, norm and rotation of the heads, the append to a paged
+cache held in 4 bits, and attention over it.
+
+MoELayer's batches of up to `few_tokens` (FEW_TOKENS, fewer above 16 choices per token) run in four kernels (norm, router, few-token
 experts, norm); larger ones take the four-step block between the norms (dispatch, permute, grouped FFN, combine).  Both read
 the same packed weights.  Marshalling and buffers only; every step runs in the library's kernels."""
 from __future__ import annotations
@@ -103,3 +106,56 @@ class MoELayer:
                          next_w=next_w, next_b=next_b, x_out=x_next, kind=self.kind, eps=self.eps, r_scale=self.r_scale,
                          y_scale=self.y_scale, n_valid=n_valid)
         return r_out
+
+
+class Attention:
+    """One layer's 4-bit cache of keys and values, and the buffers of its calls.
+
+    n_pages, page_size   the cache: pages of 16, 32, 64, 128 or 256 tokens
+    Hq, Hkv, D           query heads, key heads (a divisor of Hq), elements of a head (64 or 128)
+    max_tokens           largest batch (rows of the buffers)
+    cos_sin              f32 [positions, rot]: cos, then sin, of rot / 2 pairs' angles; None: heads are not rotated
+    q_w, k_w             weights [D] of the heads' RMS norms (one dtype) or None: not normed
+    interleaved          pairs are neighbours instead of (i, i + rot / 2)
+    scale                of the scores; None: D ** -0.5
+
+    A layer has one query buffer and one workspace: its calls must follow one another on one stream (or be ordered by events).
+    `status` collects the STATUS_* bits of every call.
+    """
+
+    def __init__(self, n_pages, page_size, Hq, Hkv, D, max_tokens, cos_sin=None, q_w=None, k_w=None, eps=1e-6, interleaved=False,
+                 scale=None, device="cuda"):
+        self.Hq, self.Hkv, self.D, self.eps, self.interleaved, self.scale = Hq, Hkv, D, eps, interleaved, scale
+        self.cos_sin, self.q_w, self.k_w = cos_sin, q_w, k_w
+        self.shape = B.make_cache(n_pages, page_size, Hkv, D)
+        u8 = dict(dtype=torch.uint8, device=device)
+        self.cache = torch.empty(B.tempo_cache_bytes(self.shape), **u8)
+        self.workspace = torch.zeros(B.tempo_attend_workspace_bytes(self.shape, Hq), **u8)
+        self.q = torch.empty(max_tokens, Hq, D, dtype=torch.bfloat16, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def forward(self, qkv, positions, slots, page_table, lens, out, q_start=None, max_q=1, n_valid=None):
+        """out = attention of this batch's tokens, which are appended to the cache first.
+
+        qkv bf16 [T, (Hq + 2 Hkv) * D]: a projection's rows (queries, keys, values); out bf16 [T, Hq, D] or [T, Hq * D].
+        positions, slots i32 [T]: of the rotation, and where in the cache (page * page_size + offset; below zero: not appended).
+        page_table i32 [B, pages], lens i32 [B]: the sequences with this batch's tokens; q_start i32 [B + 1]: their rows (None: one
+        each), max_q the most of one.  n_valid i32 [1]: rows behind it are not appended.  Enqueues kernels only: the call can be
+        captured in a CUDA graph."""
+        T = qkv.shape[0]
+        if T > self.q.shape[0]:
+            raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.q.shape[0]}")
+        q, k, v = qkv.unflatten(1, (-1, self.D)).split([self.Hq, self.Hkv, self.Hkv], dim=1)
+        turned = self.q[:T]
+        turn = dict(positions=positions, cos_sin=self.cos_sin) if self.cos_sin is not None else {}
+        B.tempo_kv_append(self.shape, k, v, slots, self.cache, self.status, k_w=self.k_w, q=q, q_w=self.q_w, q_out=turned, eps=self.eps,
+                          interleaved=self.interleaved, n_valid=n_valid, **turn)
+        B.tempo_attend(self.shape, turned, self.cache, page_table, lens, out.view(T, self.Hq, self.D), self.status, self.workspace,
+                       scale=self.scale, q_start=q_start, max_q=max_q)
+        return out
+
+    def read(self, slots):
+        """The cache's tokens at slots i32 [n] as fp16 [n, Hkv, D] keys and values: to move a sequence, or to keep its prefix."""
+        k, v = (torch.empty(slots.shape[0], self.Hkv, self.D, dtype=torch.float16, device=self.cache.device) for _ in range(2))
+        B.tempo_kv_read(self.shape, self.cache, slots, k, v, self.status)
+        return k, v

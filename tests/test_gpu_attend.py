@@ -204,3 +204,31 @@ def test_another_stream_and_a_graph(B):
     c.spans = [(l - 30, n) for l, n in c.spans]
     c.k, c.v = [k[:-30] for k in c.k], [v[:-30] for v in c.v]
     c.check(out)
+
+
+@pytest.mark.parametrize("n", [1, 100])
+def test_a_missing_page_anywhere_in_a_tile(B, n):
+    c = Case(B, [(300, n)], 4, 2, 64, 16)
+    c.run()
+    for page in range(10):
+        table = c.table.clone()
+        c.table[0, page] = -1
+        out = c.run()
+        first = max(0, page * 16 - (300 - n))                          # the first query that sees a token of it
+        assert out[first:].isnan().all() and not out[:first].isnan().any()
+        c.table.copy_(table)
+    assert int(c.status) == B.STATUS_BAD_INDEX
+
+
+def test_as_many_sequences_as_there_may_be(B):
+    spans = [(1 + 13 * b % 97, 1) for b in range(1020)] + [(90, 90), (5, 0), (333, 20), (64, 64)]
+    c = Case(B, spans, 4, 1, 64, 16)
+    c.check(c.run())
+    assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 3.0])
+def test_scales(B, scale):
+    c = Case(B, [(200, 70), (45, 2)], 4, 2, 64, 16)
+    c.scale = scale
+    c.check(c.run())

@@ -229,3 +229,21 @@ def test_offsets_beyond_32_bits(B):
     (kb, vb), _ = _read(B, shape, cache, slots)
     assert torch.equal(kb.to(torch.float64), R.cached(k)) and torch.equal(vb.to(torch.float64), R.cached(v))
     assert int((cache != 0).sum()) <= 4 * Hkv * 2 * 72
+
+
+@pytest.mark.parametrize("D,norm,pairs", [(128, True, "half"), (64, False, "next"), (128, False, "half")])
+def test_codes_of_many_keys_are_the_formulas(B, D, norm, pairs):
+    """A few of a million elements lie so near a border that 32 bits would not tell on which side."""
+    g = _gen(D + norm)
+    T, Hkv = 4000, 8
+    k = (_rand(g, T, Hkv, D) * (0.01 + 4 * torch.rand(T, Hkv, 1, generator=g, device=DEV))).to(torch.bfloat16)
+    v = _rand(g, T, Hkv, D).to(torch.bfloat16)
+    w = (1 + 0.3 * _rand(g, D)).to(torch.bfloat16) if norm else None
+    cs = _table(g, D)
+    pos = torch.randint(0, 97, (T,), generator=g, device=DEV, dtype=torch.int32)
+    shape, cache = _cache(B, T // 16, 16, Hkv, D)
+    slots = torch.randperm(T, generator=g, device=DEV).to(torch.int32)
+    B.tempo_kv_append(shape, k, v, slots, cache, _status(), k_w=w, positions=pos, cos_sin=cs, interleaved=pairs == "next")
+    (kb, vb), _ = _read(B, shape, cache, slots)
+    assert torch.equal(kb.to(torch.float64), R.cached(R.turn(k, w, pos, cs, interleaved=pairs == "next")))
+    assert torch.equal(vb.to(torch.float64), R.cached(v))
