@@ -102,11 +102,11 @@ struct Target {
 };
 
 // A lane's eight elements of norm(x) * w turned by the row's angles, in R.  `e` is the lane's first element, beyond D for a
-// lane without one; every lane of the warp takes part in the shuffles.  The loads from x are done when this returns.  amplitude: the
-// most that an element's two products add up to without their signs.
+// lane without one; every lane of the warp takes part in the exchanges (`stage`: 32 places of the warp's own in shared memory).
+// amplitude: the most that an element's two products add up to without their signs.
 template <int LPH, typename R>
-__device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, size_t at, int e, bool live, const float* angles,
-                                       uint4 raw, R (&y)[8], float& amplitude) {
+__device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, int e, bool live, const float* angles, uint4 raw, uint4* stage,
+                                       R (&y)[8], float& amplitude) {
   const int lane = threadIdx.x & 31, half = p.rot / 2;
   const bool mine = live && e < p.D;
   float x[8], w[8];
@@ -183,20 +183,24 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, s
     }
     return;
   }
-  // Any even rot: the other elements one by one.
+  // Any even rot: the other elements one by one, through shared memory.
+  stage[lane] = raw;
+  __syncwarp();
+  const __nv_bfloat16* head = reinterpret_cast<const __nv_bfloat16*>(stage + lane / LPH * LPH);
   if (mine) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (e + i >= p.rot) continue;
       const bool first = e + i < half;
       const int eo = first ? e + i + half : e + i - half, a = first ? e + i : eo;
-      const float xo = __bfloat162float(*(o.x + at + eo));
+      const float xo = __bfloat162float(head[eo]);
       const R other = o.w != nullptr ? R(xo) * r * R(weight1(o.w, p.w_f32, eo)) : R(xo);
       amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
       const R c = R(__ldg(angles + a)), s = R(__ldg(angles + half + a));
       y[i] = first ? y[i] * c - other * s : y[i] * c + other * s;
     }
   }
+  __syncwarp();
 }
 
 __device__ __forceinline__ const float* angles_of(const HeadsParams& p, int t, bool live) {
@@ -282,28 +286,90 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* y) {
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// The same for any even rot and any alignment (see turn_heads): a lane has eight neighbouring elements, and where pairs are half a
+// rotation apart their other elements come through shared memory.
+template <int LPH, int NH>
+__device__ __forceinline__ void turn_any(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, int rounds, bool live,
+                                         const float* angles, uint4* stage) {
+  constexpr int HPW = 32 / LPH;
+  const int lane = threadIdx.x & 31, e = lane % LPH * 8, half = p.rot / 2;
+  const bool mine = live && e < p.D;
+  uint4 raw[NH];
+  const auto load = [&]() {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      const int h = h0 + n * HPW;
+      raw[n] = mine && h < H ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  load();
+  float a[8], b[8];
+  int others[8];                                        // below zero: the element does not turn
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = e + i;
+    const bool turns = mine && at < p.rot, first = p.interleaved ? (i & 1) == 0 : at < half;
+    a[i] = mine && o.w != nullptr ? weight1(o.w, p.w_f32, at) : 1.0f;
+    b[i] = 0.0f;
+    others[i] = -1;
+    if (turns) {
+      const int pair = p.interleaved ? at / 2 : first ? at : at - half, other = p.interleaved ? at ^ 1 : first ? at + half : at - half;
+      const float c = __ldg(angles + pair), s = __ldg(angles + half + pair);
+      const float w = o.w != nullptr ? weight1(o.w, p.w_f32, other) : 1.0f;
+      a[i] *= c;
+      b[i] = first ? -w * s : w * s;
+      others[i] = other;
+    }
+  }
+  const __nv_bfloat16* head = reinterpret_cast<const __nv_bfloat16*>(stage + lane / LPH * LPH);
+#pragma unroll 1
+  for (int round = 0;; ++round) {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      float x[8], z[8];
+      widen8(raw[n], x);
+      float r = 1.0f;
+      if (o.w != nullptr) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+#pragma unroll
+        for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+        r = rsqrtf(fmaf(ss, p.inverse_d, p.eps));
+      }
+      if (p.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = others[i] >= 0 ? x[i ^ 1] : 0.0f;
+      } else {
+        stage[lane] = raw[n];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = others[i] >= 0 ? __bfloat162float(head[others[i]]) : 0.0f;
+        __syncwarp();
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], a[i], z[i] * b[i]) * r;
+      const int h = h0 + n * HPW;
+      if (mine && h < H) store8(out.x + t * out.ld + h * out.hd + e, x, out.vec);
+    }
+    h0 += NH * HPW;
+    if (round + 1 >= rounds) break;
+    load();
+  }
+}
+
 // Heads of one token by one group of lanes, h0, h0 + HPW, ... below H, `rounds` times NH of them: NH heads' loads are in flight
 // together, and weights, cos and sin are multiplied once for all.  A lane has two runs of four elements which turn with one another
 // (half pairs: i and i + rot/2) or each in itself, so that nothing is exchanged but the sum of squares:
 //   out[i] = r * (x[i] * a[i] + other[i] * b[i])
 template <int LPH, int NH>
-__device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, int rounds, bool live) {
+__device__ __forceinline__ void turn_heads(const HeadsParams& p, const Operand& o, const Target& out, int t, int h0, int H, int rounds, bool live,
+                                           uint4* stage) {
   constexpr int HPW = 32 / LPH;
   const int l = threadIdx.x % LPH, half = p.rot / 2;
   const float* angles = angles_of(p, t, live);
-  if (!p.quads) {                                       // any even rot, any alignment: one head at a time
-    const int e = l * 8;
-#pragma unroll 1
-    for (int n = 0; n < NH * rounds; ++n) {
-      const int h = h0 + n * HPW;
-      const bool in = live && h < H && e < p.D;
-      float y[8];
-      const uint4 u = in ? load8(o.x + t * o.ld + h * o.hd + e, o.vec) : make_uint4(0, 0, 0, 0);
-      float unused;
-      turned<LPH, float>(p, o, t * o.ld + (h < H ? h : 0) * o.hd, e, live && h < H, angles, u, y, unused);
-      __syncwarp();                                     // in place: every load of the warp's heads comes before the stores
-      if (in) store8(out.x + t * out.ld + h * out.hd + e, y, out.vec);
-    }
+  if (!p.quads) {
+    turn_any<LPH, NH>(p, o, out, t, h0, H, rounds, live, angles, stage);
     return;
   }
   const bool mine = live && 8 * l < p.D;
@@ -465,6 +531,8 @@ __device__ __forceinline__ uint32_t quantise8_near(const float (&y)[8], float of
 template <int LPH, bool APPEND, int NH>
 __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ HeadsParams p) {
   constexpr int HPW = 32 / LPH;                          // heads of a warp at a time
+  __shared__ uint4 stages[8][32];
+  uint4* stage = stages[threadIdx.x >> 5];
   pdl_trigger();
   pdl_wait();
   const int n = p.n_valid != nullptr ? min(max(*p.n_valid, 0), p.T) : p.T;
@@ -483,7 +551,7 @@ __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ H
   const Operand o = keys ? Operand{p.k, p.ld_k, p.hd_k, p.k_w, p.k_vec} : Operand{p.q, p.ld_q, p.hd_q, p.q_w, p.q_vec};
   if (!APPEND || !keys) {
     turn_heads<LPH, NH>(p, o, keys ? Target{p.k_out, p.ld_k_out, p.hd_k_out, p.k_out_vec} : Target{p.q_out, p.ld_q_out, p.hd_q_out, p.q_out_vec},
-                        t, h0, H, rounds, in);
+                        t, h0, H, rounds, in, stage);
     return;
   }
 
@@ -504,7 +572,7 @@ __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ H
     // In 32 bits first.  An element is off by less than 2^-20 of its amplitude: 2^-22 of the inverse root, half of 12 roundings of
     // 2^-24 of the sum of squares, five of the products.
     float y[8], amplitude;
-    turned<LPH, float>(p, o, at, e, live, angles, raw, y, amplitude);
+    turned<LPH, float>(p, o, e, live, angles, raw, stage, y, amplitude);
 #pragma unroll
     for (int d = 1; d <= 2; d *= 2) amplitude = fmaxf(amplitude, __shfl_xor_sync(0xffffffffu, amplitude, d));
     bool sure_k, sure_v;
@@ -516,7 +584,7 @@ __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ H
     if (__any_sync(0xffffffffu, mine && !fine)) {
       // Some element of the warp is next to a border (1 to 2 warps of 100) or not finite: all of them in 64 bits.
       double exact[8];
-      turned<LPH, double>(p, o, at, e, live, angles, raw, exact, amplitude);
+      turned<LPH, double>(p, o, e, live, angles, raw, stage, exact, amplitude);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (!isfinite(exact[i])) { exact[i] = 0.0; bad = true; }
