@@ -61,6 +61,21 @@ struct Pieces {
   __device__ __forceinline__ bool two(int group) const { return it.n * group - it.row0 > kRowTile; }
 };
 
+constexpr int kLeast = 4, kSnap = 3;
+
+// Where run r begins, and in which item: its equal share of the tiles, or the border of an item that is near.  So an item [b, e) is cut
+// at the equal shares in (b + kSnap, e - kSnap), and nowhere else.
+__device__ __forceinline__ int snapped(const AttendParams& p, const int* before, const Runs& runs, int r, int n_runs, int total, Item& it) {
+  const int x = r >= n_runs ? total : runs.begin(r);
+  if (x == total) return total;
+  it = Tiles::item_at(p, before, x);
+  if (x - it.begin <= kSnap) return it.begin;
+  if (it.begin + it.tiles - x > kSnap) return x;
+  if (it.begin + it.tiles < total) Tiles::next_item(p, it);
+  else it.begin += it.tiles;
+  return it.begin;
+}
+
 // Instruction descriptor of kind::f16 with fp16 operands (0 at bits 7 and 10), 32-bit sums, both K-major, 128 rows, N columns.
 template <int N>
 constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(kRowTile >> 4) << 24);
@@ -300,20 +315,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
   tc_fence_after();
   const uint32_t tmem = s_tmem;
 
-  // Runs of at least kLeast tiles: a shorter one costs more at its joins than it takes off the others.
-  constexpr int kLeast = 4;
+  // Runs of kLeast tiles and more, and none that leaves a part of kSnap tiles or less of an item: writing and joining the parts of an
+  // item takes as long as six tiles.
   const int n_runs = min(max(total / kLeast, 1), static_cast<int>(gridDim.x));
   const bool works = total > 0 && static_cast<int>(blockIdx.x) < n_runs;
   if (works) {
     const Runs runs(total, n_runs);
-    const int begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
+    Item start, behind;                                // the items that the run begins in, and that the next one begins in
+    const int begin = snapped(p, before, runs, blockIdx.x, n_runs, total, start), end = snapped(p, before, runs, blockIdx.x + 1, n_runs, total, behind);
     volatile int* abort_at = &abort_flag;
     const auto wait = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.wait_ns); };
 
     // 512 threads of 128 registers at launch: 256 of 64 and 256 of 192
     if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    Pieces pc(Tiles::item_at(p, before, begin), begin, end);
+    Pieces pc(start, begin, end);
     if (warp == 0) {
       // ---- loader: keys, then values of each tile; lanes 0 to 7 a unit each
       const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
@@ -451,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     }
     } else {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-      Pieces pc(Tiles::item_at(p, before, begin), begin, end);
+      Pieces pc(start, begin, end);
       // ---- softmax: warpgroup x on row tile x, thread by row
       const int x = (warp - 8) >> 2, row = (warp & 3) * 32 + lane, r = x * kRowTile + row;
       const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -548,10 +564,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
         if (more) load(pc);                            // the next item's queries: every product with these is done
 
         const float sum = (l[0][0] + l[0][1]) + (l[1][0] + l[1][1]);
-        const int first = runs.of(it.begin), ctas = runs.of(it.begin + it.tiles - 1) - first + 1;
+        const int first = runs.of(it.begin + kSnap), ctas = max(0, runs.of(it.begin + it.tiles - kSnap - 1) - first) + 1;
         // A cut item's parts go to the workspace, four columns of a row to a 16-byte line of 256 rows; the CTA that arrives last adds
         // them up in their order.
-        const auto part_of = [&](int cta) { return static_cast<size_t>(cta) * 2 + (cta == first && it.begin > runs.begin(cta) ? 1 : 0); };
+        const auto part_of = [&](int cta) { return static_cast<size_t>(cta) * 2 + (cta == first ? 1 : 0); };
         float4* parts = reinterpret_cast<float4*>(p.part);
         float2* stats = reinterpret_cast<float2*>(p.stats);
         if (active) {
