@@ -211,44 +211,48 @@ __device__ __forceinline__ const float* angles_of(const HeadsParams& p, int t, b
   return p.cos_sin + static_cast<size_t>(in) * p.rot;
 }
 
-// rint(x / s) exactly, ties to even, from the rounded product with 1 / s: the remainder decides (x - n s is exact: x has at
-// most 8 bits in R = float, and s has 4).
-template <typename R>
-__device__ __forceinline__ R divide_rint(R x, R s, R inverse) {
-  R n = rint(x * inverse);
-  const R rest = fma(-n, s, x), h = R(0.5) * s;
-  const bool odd = n * R(0.5) != rint(n * R(0.5));
-  if (rest > h || (rest == h && odd)) n += R(1);
-  else if (rest < -h || (rest == -h && odd)) n -= R(1);
-  return n;
-}
-
 // Eight elements of a group that four neighbouring lanes share -> a word of eight codes, and the group's (s, 16 z) byte pair.
-template <typename R>
-__device__ __forceinline__ uint32_t quantise8(const R (&y)[8], uint32_t& params) {
+// Elements in 64 bits, as sums of two floats; a quotient's nearest integer comes from 32 bits and is set right by its remainder.
+__device__ __forceinline__ uint32_t quantise8(const double (&y)[8], uint32_t& params) {
   double lo = 0.0, hi = 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { lo = fmin(lo, static_cast<double>(y[i])); hi = fmax(hi, static_cast<double>(y[i])); }
+  for (int i = 0; i < 8; ++i) { lo = y[i] < lo ? y[i] : lo; hi = y[i] > hi ? y[i] : hi; }
 #pragma unroll
   for (int d = 1; d <= 2; d *= 2) {
-    lo = fmin(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-    hi = fmax(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    const double l = __shfl_xor_sync(0xffffffffu, lo, d), h = __shfl_xor_sync(0xffffffffu, hi, d);
+    lo = l < lo ? l : lo;
+    hi = h > hi ? h : hi;
   }
-  const double step = (hi - lo) / 15.0;
-  // four significant bits, rounded up: a multiple of 2^(exponent - 3), at least of 2^-17
-  const int exponent = max(static_cast<int>((__double2hiint(step) >> 20) & 0x7ff) - 1023 - 3, -17);
-  const double up = __hiloint2double((1023 + exponent) << 20, 0), down = __hiloint2double((1023 - exponent) << 20, 0);
-  const double s = fmin(ceil(step * down) * up, 768.0);
+  const double range = hi - lo;
   params = 0;
-  if (s == 0.0) return 0;
-  const double inverse = 1.0 / s;
-  const double z = fmin(divide_rint<double>(-lo, s, inverse), 15.0);
-  params = (static_cast<uint32_t>(__half_as_ushort(__double2half(s))) >> 7) | (static_cast<uint32_t>(z) << 12);
+  if (range == 0.0) return 0;
+  float s = 768.0f;
+  if (range <= 15.0 * 768.0) {
+    // four significant bits, rounded up: a multiple of 2^(exponent - 3), at least of 2^-17; 32 bits may miss it by one
+    const float step = static_cast<float>(range) * (1.0f / 15.0f);
+    const int exponent = max(static_cast<int>(__float_as_uint(step) >> 23) - 127 - 3, -17);
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + exponent) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - exponent) << 23);
+    s = ceilf(step * down) * up;
+    if (15.0 * static_cast<double>(s - up) >= range) s -= up;
+    if (15.0 * static_cast<double>(s) < range) s += s >= 16.0f * up ? 2.0f * up : up;
+  }
+  const float inverse = 1.0f / s, h = 0.5f * s;
+  const auto nearest = [&](double x) {
+    const float a = static_cast<float>(x), b = static_cast<float>(x - static_cast<double>(a));
+    const float k = (fminf(fmaxf(a * inverse, -1e5f), 1e5f) + 12582912.0f) - 12582912.0f;
+    const float above = fmaf(-k, s, a) - h, below = fmaf(-k, s, a) + h;            // exact where it matters, next to a border
+    const bool odd = (__float_as_uint(k + 12582912.0f) & 1u) != 0;
+    if (above > -b || (above == -b && odd)) return k + 1.0f;
+    if (below < -b || (below == -b && odd)) return k - 1.0f;
+    return k;
+  };
+  const float z = fminf(nearest(-lo), 15.0f);
+  params = (static_cast<uint32_t>(__half_as_ushort(__float2half(s))) >> 7) | (static_cast<uint32_t>(z) << 12);
   uint32_t word = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const R c = fmin(fmax(divide_rint<R>(y[i], static_cast<R>(s), static_cast<R>(inverse)) + static_cast<R>(z), R(0)), R(15));
-    word |= static_cast<uint32_t>(static_cast<int>(c)) << (4 * i);
+    const float c = fminf(fmaxf(nearest(y[i]) + z, 0.0f), 15.0f);
+    word |= (__float_as_uint(c + 8388608.0f) & 15u) << (4 * i);
   }
   return word;
 }
@@ -503,9 +507,9 @@ __device__ __forceinline__ uint32_t quantise8_near(const float (&y)[8], float of
     sure = range == 0.0f ? off == 0.0f : range < 15.0f * s - doubt && range > 15.0f * (s - up) + doubt && range < 11000.0f;
   }
   if (range == 0.0f || !sure) return 0;
-  const float inverse = __fdividef(1.0f, s);           // s has four significant bits: off by 2^-22 at most
-  // a quotient is off by off / s and a few roundings of at most 16
-  const float border = 0.5f - off * inverse - 8e-6f;
+  const float inverse = 1.0f / s;
+  // a quotient is off by off / s and two roundings of at most 16
+  const float border = 0.5f - off * inverse - 2.5e-6f;
   const auto nearest = [&](float x) {                  // |x / s| is at most 16
     const float q = x * inverse, k = (q + 12582912.0f) - 12582912.0f;
     if constexpr (!EXACT) sure = sure && fabsf(q - k) < border;
@@ -569,20 +573,20 @@ __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ H
   uint32_t pk, pv, wk, wv;
   bool bad = false;
   {
-    // In 32 bits first.  An element is off by less than 2^-20 of its amplitude: 2^-22 of the inverse root, half of 12 roundings of
-    // 2^-24 of the sum of squares, five of the products.
+    // In 32 bits first.  An element is off by less than 15 * 2^-24 of its amplitude: 4 of the inverse root, half of 13 of the sum of
+    // squares under it, 4 of the products.
     float y[8], amplitude;
     turned<LPH, float>(p, o, e, live, angles, raw, stage, y, amplitude);
 #pragma unroll
     for (int d = 1; d <= 2; d *= 2) amplitude = fmaxf(amplitude, __shfl_xor_sync(0xffffffffu, amplitude, d));
     bool sure_k, sure_v;
-    wk = quantise8_near<false>(y, amplitude * 0x1p-19f, pk, sure_k);
+    wk = quantise8_near<false>(y, amplitude * 0x1p-20f, pk, sure_k);
     wv = quantise8_near<true>(v, 0.0f, pv, sure_v);
     bool fine = sure_k && sure_v;
 #pragma unroll
     for (int i = 0; i < 8; ++i) fine = fine && isfinite(v[i]) && isfinite(y[i]);
     if (__any_sync(0xffffffffu, mine && !fine)) {
-      // Some element of the warp is next to a border (1 to 2 warps of 100) or not finite: all of them in 64 bits.
+      // Some element of the warp is next to a border (one warp of 150) or not finite: all of them in 64 bits.
       double exact[8];
       turned<LPH, double>(p, o, e, live, angles, raw, stage, exact, amplitude);
 #pragma unroll
@@ -592,8 +596,10 @@ __global__ void __launch_bounds__(256, 4) heads_kernel(const __grid_constant__ H
       }
       const uint32_t head_lanes = (LPH == 32 ? 0xffffffffu : ((1u << LPH) - 1u)) << (lane / LPH * LPH);
       bad = (__ballot_sync(0xffffffffu, bad) & head_lanes) != 0;
-      wk = quantise8<double>(exact, pk);
-      wv = quantise8<float>(v, pv);
+      wk = quantise8(exact, pk);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) exact[i] = v[i];
+      wv = quantise8(exact, pv);
     }
   }
   if (bad) pk |= kMarked;
