@@ -414,8 +414,8 @@ int tempo_cache_bytes(const tempo_cache* shape /*[host]*/, size_t* bytes /*[host
 /*
  *   tempo_qk_rotate   q' = rot(norm(q) * q_w, position), k' = rot(norm(k) * k_w, position), head by head, in one pass
  *   tempo_kv_append   the same, with k' and v going into the cache (row t to token slots[t] % page_size of page
- *                     slots[t] / page_size).  k' is not rounded before it is quantised, and is computed in 64 bits: the codes are
- *                     those of the formula also where a value lies next to a border between two of them.
+ *                     slots[t] / page_size).  k' is not rounded before it is quantised: the codes are those of the formula in 64
+ *                     bits, also where a value lies next to a border between two of them.
  *   tempo_kv_read     rows of the cache back as fp16, exactly: k[i], v[i] = token slots[i]
  * norm(x) = x / sqrt(mean(x^2) + eps) over the D elements of a head; without q_w (k_w) that operand is not normed.
  * rot turns the pairs (i, i + rot/2), or with `interleaved` (2i, 2i+1), i < rot/2, of the first `rot` elements by
@@ -450,16 +450,19 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  * queries q[q_start[b]] to q[q_start[b+1] - 1], which are its newest tokens (already appended): query i of n sees the tokens
  * t <= lens[b] - n + i.
  *     out[i, h] = sum_t softmax_t(scale * <q[i, h], K[t, h / (Hq / Hkv)]>) V[t, h / (Hq / Hkv)]
- * A query that sees no token gets zeros.  K and V enter as they are (fp16 products, sums in 32 bits), q exactly up to 2^-24 of
- * its head's largest element; softmax weights are rounded to fp16 before they meet V, statistics are in 32 bits.
- *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), 16-byte aligned rows (address and
- *   pitches); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
+ * A query that sees no token gets zeros.  K and V enter as they are (fp16 products, sums in 32 bits), and so does q where it lies
+ * within 2^-25 of its head's largest element (within 2^-33 of that largest below); softmax weights are rounded to fp16 before they
+ * meet V, and statistics are in 32 bits.  A query that is not finite makes its own head's output NaN.
+ *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), addresses and pitches 16-byte aligned
+ *   (TEMPO_ERR_ALIGN; with 32 bytes prompts are read and written in fewer accesses); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
  *   max_q [host] is the most queries of a sequence: a hint for the choice of kernels, any value gives the same result within rounding.
  *   Rows before q_start[0] and from q_start[B] on are left as they are.  Hq is a multiple of Hkv; B <= 1024.
  *   workspace  tempo_attend_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves it
- *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.
+ *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.  After
+ *        TEMPO_STATUS_TIMEOUT (waits inside a CTA are bounded as in tempo_grouped_ffn) zero it again.
  * A length beyond the page table counts as its end, rows outside q as none, both with TEMPO_STATUS_BAD_INDEX; a page outside
- * the cache that holds tokens of a sequence makes the outputs that see it NaN (TEMPO_STATUS_BAD_INDEX).  Results do not depend on timing.
+ * the cache that holds tokens of a sequence makes the outputs that see them NaN (TEMPO_STATUS_BAD_INDEX).  Results do not depend
+ * on timing; where long items are cut, and so the last bits of a result, goes by the lengths of all sequences of the call.
  */
 typedef struct {
   int32_t B, T, Hq, max_q, max_pages;

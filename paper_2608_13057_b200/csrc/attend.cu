@@ -1,28 +1,36 @@
-// Attention over the 4-bit paged cache (tempo_attend).
+// Attention over the 4-bit paged cache (tempo_attend) for few queries of a sequence; attend_many.cu has the other kernel.
 //
 //   out[i, h] = sum_t p[t] V[t] / sum_t p[t],  p[t] = exp(scale <q, K[t]> - m),  t <= the query's own position
 //
-// A key head's queries (the heads of its group, and the new tokens of the sequence) are the rows of one item, 16 rows to an item;
-// each cached byte is read once for all of them.  One pass over the tokens with the running maximum and sum.
+// A key head's queries (the heads of its group, and the new tokens of the sequence) are the rows of an item, 8 or 16 of them; a
+// cached byte is read once for all.  One pass over the tokens with the running maximum and sum; 32-bit statistics, weights rounded
+// to fp16 where they meet V (their sum is that of the rounded ones).
 //
-// Bound by the cache's bytes, which one SM takes in at 23 bytes a clock: that leaves 2.8 instruction slots of a lane for each
-// cached element.  So codes go from shared memory to registers and are decoded there into the B operands of the
-// matrix instruction (m16n8k16, 32-bit sums), at 11 instructions for 8 elements; a decoded copy in shared memory for the
-// tensor-memory form of the instruction would move 2 bytes per element in and 2 out, 184 bytes a clock where the SM has 128.
-// The order of a sum over d or t is free, so that a lane's 16-byte load is what it needs: of keys 32 neighbouring elements
-// (one group: one scale) of one token, of values 16 neighbouring elements of two tokens side by side in a word's halves.
+// An SM takes in the cache at 23 bytes a clock, which leaves 2.8 instruction slots of a lane for an element.  So codes go from
+// shared memory to registers and are decoded there into operands of the matrix instruction (m16n8k16, 32-bit sums) at 11
+// instructions for 8 elements; a decoded copy in shared memory for tcgen05 would move 2 bytes of an element in and 2 out, 184 bytes
+// a clock where the SM has 128.  Keys and values are the 16-row operand, so that 8 queries cost half the products of 16.  The order
+// of a sum over d or t is free: a lane's 16-byte load is what it needs, of keys 32 neighbouring elements (one group: one scale) of a
+// token, of values 16 neighbouring elements of two tokens side by side in a word's halves.
+// What bounds it: 64 sequences of up to 8192 tokens (16 rows; 193 MB) take 64.2 us, 46 % of a copy's rate, of which about 12 are
+// start and end; 16 tokens of a head cost a scheduler 330 instructions in 650 clocks with its two warps, 129 of them on the pipe of
+// logic, 121 on the one of fp16 sums, 34 matrix instructions of 8 clocks.  2 sequences of 131072 (4 rows; 245 MB) 58.4 us, 64 %:
+// 289 instructions, 17 matrix instructions.  One sequence of 1500: 9.7 us, a chain of latencies (tiles counted 1, queries and first
+// page 2, one tile 2.5, merges 1, arrival and join 2.5 us).
 //
-// Work is dealt in tiles of 32 tokens: the tiles of all items in one row, cut into equal runs, one for each warp of the
-// launch, whatever the lengths.  A warp streams its run through a ring of its own (16-byte asynchronous copies: a bulk copy costs the
-// warp that issues it 200 to 400 clocks, a tenth of a tile) and waits for nobody; parts of items that were cut are joined in shared memory after the CTA's last tile, and across CTAs by the one
-// that arrives last, in a fixed order.
+// Work is dealt in tiles of 64 tokens: the tiles of all items in one row, cut into equal runs, one for each warp of the launch,
+// whatever the lengths.  A warp streams its run through a tile of shared memory of its own (16-byte asynchronous copies: a bulk copy
+// costs the warp that issues it 200 to 400 clocks, a tenth of a tile) and waits for nobody; parts of items that were cut are joined in
+// shared memory after the CTA's last tile, and across CTAs by the one that arrives last, in a fixed order.
 #include "attend_common.cuh"
 
 namespace tempo {
 
 namespace {
 
-// The kernel's form for items of 8 NR rows.
+// The kernel's form for items of 8 NR rows.  Warps: as many as have their registers without a spill, which would go to L2 (shared memory
+// leaves no L1): 16 rows and 12 warps took 88 us where 8 take 64 (64 x 8192); 8 rows and 12 warps 57, 16 warps 61, 8 warps 61
+// (2 x 131072), for D = 64 16 warps 22.5 and 12 warps 27 (37 x 2999).
 template <int D_, int NR_>
 struct Few {
   static constexpr int D = D_, NR = NR_, kRows = 8 * NR;

@@ -1,8 +1,6 @@
-// Attention over the 4-bit paged cache for many queries of a sequence (prompts and their chunks).
+// Attention over the 4-bit paged cache for many queries of a sequence (prompts and their chunks; see attend.cu for the formula).
 //
-// Rows are queries times the heads of a group, 256 to an item as two tiles of 128; keys come in tiles of 128.  Bound by the
-// matrix products (4 D operations per row and key) and, close behind, by the exponentials (one per row and key, 16 a clock) and by
-// shared memory: of every key tile 128 x D decoded numbers are written once and read by both row tiles.  Roles of the warps:
+// Rows are queries times the heads of a group, 256 to an item as two tiles of 128; keys come in tiles of 128.  Roles of the warps:
 //   loader     copies units of 16 cached tokens into a ring of key and value stages
 //   decoders   codes -> fp16 tiles in shared memory in the layout of the matrix instruction, values transposed
 //   issuer     tcgen05.mma: S = Q K^T into tensor memory, O += P V with P read from tensor memory
@@ -11,6 +9,13 @@
 // more than 8 (in powers of 2), so that O is seldom touched between products.  The order of a sum over d is free: K and Q are stored
 // as the pairs (n, n + 4) in which codes are decoded, V's rows in the order that stores them without bank conflicts.
 // The tiles of all items are dealt to the CTAs in equal runs; items that were cut are joined by the CTA that arrives last.
+//
+// What bounds it: a step of 256 rows and 128 keys takes 2900 to 3600 clocks.  Its products alone, with the operands as they lie, take
+// 2460 (2048 at the nominal rate; Q K^T with both operands in shared memory reads 128 bytes a clock, all that there is), its
+// exponentials 2048 on the special-function units, and the softmax and decoding instructions 1400 of a scheduler's slots.  Two
+// chunks of 2048 queries over 6144 tokens, 64 heads of 128: 492 us, 1012 TFLOP/s, of which the row tiles' starts and ends are
+// about 70 us.  Left out because they were slower (2 x 32768 tokens, 256 queries each, 339 us now): a quarter of the
+// exponentials as polynomials on the FMA pipe 408 against 369, two threads to a row 436 against 369.
 #include "attend_common.cuh"
 #include "mma_warp.cuh"
 
