@@ -460,6 +460,7 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  *   workspace  tempo_attend_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves it
  *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.  After
  *        TEMPO_STATUS_TIMEOUT (waits inside a CTA are bounded as in tempo_grouped_ffn) zero it again.
+ * A sequence with more than 10^9 / B tiles of scores (16 or 256 rows by 64 or 128 tokens) is left out (TEMPO_STATUS_CAPACITY).
  * A length beyond the page table counts as its end, rows outside q as none, both with TEMPO_STATUS_BAD_INDEX; a page outside
  * the cache that holds tokens of a sequence makes the outputs that see them NaN (TEMPO_STATUS_BAD_INDEX).  Results do not depend
  * on timing; where long items are cut, and so the last bits of a result, goes by the lengths of all sequences of the call.

@@ -30,6 +30,12 @@ struct Cut {
     n = max(min(max(to, 0), p.T) - q0, 0);
     if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
     if (n * p.group <= p.rows_above || n * p.group > p.rows_most) n = 0;
+    // Tiles are numbered in 32 bits: a sequence whose bound of them would not leave room for B like it is not taken.
+    const float tiles = (static_cast<float>(n * p.group) / kRows + 1.0f) * (static_cast<float>(len) / kTile + 1.0f) * p.Hkv;
+    if (n > 0 && tiles * p.B > 1e9f) {
+      n = 0;
+      atomicOr(p.status, TEMPO_STATUS_CAPACITY);
+    }
   }
 
   // Tiles that the rows [row0, row0 + kRows) see: at least one, so that rows without a token are written too.

@@ -664,8 +664,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
   }
 }
 
+// The warps' split of registers draws on those that the block was launched with: with fewer of them it would wait for good.
+template <int D>
+bool registers_suffice() {
+  cudaFuncAttributes a;
+  return cudaFuncGetAttributes(&a, attend_many_kernel<D>) == cudaSuccess && a.numRegs * kThreads >= 256 * 64 + 256 * 192;
+}
+
 template <int D>
 cudaError_t launch_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
+  static const bool fits = registers_suffice<D>();
+  if (!fits) return cudaErrorInvalidConfiguration;
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = smem_limit_once(attend_many_kernel<D>, ManySmem<D>::bytes(kAttendMaxB), done);
   if (e != cudaSuccess) return e;

@@ -300,7 +300,7 @@ Heads heads(PyObject* o, const char* what, int32_t& T, int32_t& H, int32_t& D) {
     else if (*want[i] != s[i]) refuse(what, ": expected shape [", T, ", ", H, ", ", D, "], got ", t.sizes());
   }
   if (D > 1 && t.stride(2) != 1) refuse(what, ": expected contiguous heads");
-  return {t.data_ptr(), t.stride(0), t.stride(1)};
+  return {t.data_ptr(), T > 1 ? t.stride(0) : 0, H > 1 ? t.stride(1) : 0};       // a pitch of one row says nothing
 }
 
 struct Turn {                 // what qk_rotate and kv_append have in common

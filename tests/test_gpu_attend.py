@@ -220,6 +220,45 @@ def test_a_missing_page_anywhere_in_a_tile(B, n):
     assert int(c.status) == B.STATUS_BAD_INDEX
 
 
+def test_pages_beyond_4_gib_of_the_cache(B):
+    D, Hkv, page, n = 128, 8, 256, 300
+    shape = B.make_cache(4 * 2 ** 30 // (9 * D * page // 8 * Hkv) + 40, page, Hkv, D)
+    assert B.tempo_cache_bytes(shape) > 2 ** 32
+    c = Case(B, [(700, 1), (400, n)], 16, Hkv, D, page)
+    c.shape, c.cache = shape, torch.zeros(B.tempo_cache_bytes(shape), dtype=torch.uint8, device=DEV)
+    c.table[:] = shape.n_pages - 1 - torch.arange(c.table.numel(), dtype=torch.int32, device=DEV).view(c.table.shape)
+    for b, (l, _) in enumerate(c.spans):
+        k, v = (torch.randn(l, Hkv, D, device=DEV).to(torch.bfloat16) for _ in range(2))
+        t = torch.arange(l, device=DEV)
+        B.tempo_kv_append(shape, k, v, (c.table[b][t // page] * page + t % page).to(torch.int32), c.cache, c.status)
+        c.k[b], c.v[b] = R.cached(k), R.cached(v)
+    c.check(c.run())
+    assert int(c.status) == 0
+
+
+def test_one_row_at_any_pitch(B):
+    c = Case(B, [(77, 1)], 4, 2, 64, 16)
+    want = c.run()
+    row = torch.zeros(2, 4 * 64 + 3, dtype=torch.bfloat16, device=DEV)
+    row[0, :256] = c.q.flatten()
+    q = row[:1, :256].unflatten(1, (4, 64))
+    out = torch.zeros(3, 261, dtype=torch.bfloat16, device=DEV)
+    assert torch.equal(c.run(q=q, out=out[:1, :256].unflatten(1, (4, 64)))[0], want[0])
+    assert not out[1:].any() and not out[0, 256:].any()
+
+
+@pytest.mark.parametrize("max_q", [1, 4])
+def test_more_tiles_than_are_numbered(B, max_q):
+    """A sequence that would need more is left out and told; the others are served."""
+    c = Case(B, [(90, 3), (2000, 2000)], 4, 2, 64, 256)
+    good = c.run()
+    c.table = c.table[:, :1].repeat(1, 2 ** 20)                         # 2^28 tokens, all in one page
+    c.lens[1] = 2 ** 28
+    out = c.run(max_q=max_q)
+    assert int(c.status) == B.STATUS_CAPACITY and (out[3:] == 5.0).all()
+    c.check(torch.cat([out[:3], good[3:]]))
+
+
 def test_as_many_sequences_as_there_may_be(B):
     spans = [(1 + 13 * b % 97, 1) for b in range(1020)] + [(90, 90), (5, 0), (333, 20), (64, 64)]
     c = Case(B, spans, 4, 1, 64, 16)
