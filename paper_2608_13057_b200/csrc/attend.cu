@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
       unit += kUnits;
       if (++asked < end) {
         if (asked == ahead.begin + ahead.tiles) {
-          Tiles::next_item(p, ahead);
+          Tiles::next_item(p, before, ahead);
           enter();
         }
         page = look();
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
           }
         }
         if (x == end) break;
-        Tiles::next_item(p, it);
+        Tiles::next_item(p, before, it);
         load_queries<F>(p, it, raw);
         begin_item<F>(p, it, raw, s);
       }

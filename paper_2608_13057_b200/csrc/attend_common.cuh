@@ -30,12 +30,14 @@ struct Cut {
     n = max(min(max(to, 0), p.T) - q0, 0);
     if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
     if (n * p.group <= p.rows_above || n * p.group > p.rows_most) n = 0;
-    // Tiles are numbered in 32 bits: a sequence whose bound of them would not leave room for B like it is not taken.
+  }
+
+  // Tiles are numbered in 32 bits: a sequence whose bound of them would not leave room for B like it is not taken.
+  static __device__ __forceinline__ bool too_many(const AttendParams& p, int len, int n) {
     const float tiles = (static_cast<float>(n * p.group) / kRows + 1.0f) * (static_cast<float>(len) / kTile + 1.0f) * p.Hkv;
-    if (n > 0 && tiles * p.B > 1e9f) {
-      n = 0;
-      atomicOr(p.status, TEMPO_STATUS_CAPACITY);
-    }
+    if (n == 0 || tiles * p.B <= 1e9f) return false;
+    atomicOr(p.status, TEMPO_STATUS_CAPACITY);
+    return true;
   }
 
   // Tiles that the rows [row0, row0 + kRows) see: at least one, so that rows without a token are written too.
@@ -71,14 +73,15 @@ struct Cut {
   }
 
   // The one behind it (there is one: the caller has a tile left).
-  static __device__ __forceinline__ void next_item(const AttendParams& p, Item& it) {
+  static __device__ __forceinline__ void next_item(const AttendParams& p, const int* before, Item& it) {
     it.begin += it.tiles;
     it.row0 += kRows;
     if (it.row0 >= it.n * p.group) {
       it.row0 = 0;
       if (++it.h == p.Hkv) {
         it.h = 0;
-        do span_of(p, ++it.b, it.len, it.q0, it.n); while (it.n == 0);
+        do ++it.b; while (before[it.b + 1] == before[it.b]);
+        span_of(p, it.b, it.len, it.q0, it.n);
       }
     }
     it.tiles = tiles_of(it.len, it.n, p.group, it.row0);
@@ -92,6 +95,7 @@ struct Cut {
       if (warp < p.B) {
         int len, q0, n, mine = 0;
         span_of(p, warp, len, q0, n, tell);
+        if (too_many(p, len, n)) n = 0;
         for (int row0 = lane * kRows; row0 < n * p.group; row0 += 32 * kRows) mine += tiles_of(len, n, p.group, row0);
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, d);
@@ -114,6 +118,7 @@ struct Cut {
       if (b < p.B) {
         int len, q0, n;
         span_of(p, b, len, q0, n, tell);
+        if (too_many(p, len, n)) n = 0;
         // tiles_of for each row0; the last row's query, (row0 + kRows - 1) / group, is carried along
         const int step = kRows / p.group, over = kRows - step * p.group;
         int query = (kRows - 1) / p.group, rest = kRows - 1 - query * p.group;

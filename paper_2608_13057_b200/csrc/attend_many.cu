@@ -52,11 +52,13 @@ struct Pieces {
   Item it;
   int x, end;
   bool first;
-  __device__ __forceinline__ Pieces(const Item& it_, int begin, int end_) : it(it_), x(begin), end(end_), first(true) {}
+  const int* before;
+  __device__ __forceinline__ Pieces(const Item& it_, int begin, int end_, const int* before_)
+      : it(it_), x(begin), end(end_), first(true), before(before_) {}
   __device__ __forceinline__ bool next(const AttendParams& p) {
     if (!first) {
       x = it.begin + it.tiles;
-      if (x < end) Tiles::next_item(p, it);
+      if (x < end) Tiles::next_item(p, before, it);
     }
     first = false;
     return x < end;
@@ -76,7 +78,7 @@ __device__ __forceinline__ int snapped(const AttendParams& p, const int* before,
   it = Tiles::item_at(p, before, x);
   if (x - it.begin <= kSnap) return it.begin;
   if (it.begin + it.tiles - x > kSnap) return x;
-  if (it.begin + it.tiles < total) Tiles::next_item(p, it);
+  if (it.begin + it.tiles < total) Tiles::next_item(p, before, it);
   else it.begin += it.tiles;
   return it.begin;
 }
@@ -334,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     // 512 threads of 128 registers at launch: 256 of 64 and 256 of 192
     if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    Pieces pc(start, begin, end);
+    Pieces pc(start, begin, end, before);
     if (warp == 0) {
       // ---- loader: keys, then values of each tile; lanes 0 to 7 a unit each
       const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     }
     } else {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-      Pieces pc(start, begin, end);
+      Pieces pc(start, begin, end, before);
       // ---- softmax: warpgroup x on row tile x, thread by row
       const int x = (warp - 8) >> 2, row = (warp & 3) * 32 + lane, r = x * kRowTile + row;
       const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
