@@ -22,6 +22,8 @@
 // whatever the lengths.  A warp streams its run through a tile of shared memory of its own (16-byte asynchronous copies: a bulk copy
 // costs the warp that issues it 200 to 400 clocks, a tenth of a tile) and waits for nobody; parts of items that were cut are joined in
 // shared memory after the CTA's last tile, and across CTAs by the one that arrives last, in a fixed order.
+#include <algorithm>
+
 #include "attend_common.cuh"
 
 namespace tempo {
@@ -640,18 +642,23 @@ AttendLayout attend_layout(int D) {
 
 // Sequences of up to kFewRows rows are this kernel's, longer ones the other's.  128 keys of a head take this one 1300 clocks of an SM
 // for each 16 rows and the other 4000 for any number up to 128.
+// That counts where every SM has work.  Where there is little, the other one's items of 256 rows leave most SMs idle and its start and
+// end cost 12 us: up to kFewPairs pairs of a row and a token in all, were every token of the batch in a sequence as long as this one,
+// they are this kernel's too.  Both sides at 64 heads or fewer, this one first: 128 queries over 128 tokens (0.5 M pairs) 12 and 39 us,
+// 3 x 40 over 700 (1.3 M) 15 and 29, 2 x 64 over 200 (1.6 M) 19 and 39, 2 x 5 over 9000 (2.9 M) 16 and 28, 100 over 2000 (3.2 M) 26
+// and 30; 512 over 512 (8.4 M) 37 and 36, 8 x 16 over 2000 (16 M) 41 and 31, 300 over 5000 (32 M) 97 and 49.
 constexpr int kFewRows = 48;
+constexpr int64_t kFewPairs = 4 << 20;
 
 cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream) {
-  const int64_t rows = static_cast<int64_t>(max_q) * p.group;
-  const bool many = rows > kFewRows;
-  p.rows_above = 0;
-  p.rows_most = many ? kFewRows : INT32_MAX;         // without the other kernel this one takes whatever comes
-  cudaError_t e = D == 64 ? launch_attend_as<64>(p, rows, num_sms, stream) : launch_attend_as<128>(p, rows, num_sms, stream);
-  if (e != cudaSuccess || !many) return e;
-  p.rows_above = kFewRows;
-  p.rows_most = INT32_MAX;
-  return launch_attend_many(p, D, num_sms, stream);
+  const int64_t rows = static_cast<int64_t>(max_q) * p.group, heads = static_cast<int64_t>(p.group) * p.Hkv;
+  const int64_t longest = static_cast<int64_t>(p.max_pages) << p.page_shift;
+  p.rows_few = kFewRows;
+  p.len_few = static_cast<int>(kFewPairs / std::max<int64_t>(p.T * heads, 1));
+  const bool many = rows > kFewRows && longest > p.len_few;
+  if (!many) p.len_few = INT32_MAX;                    // without the other kernel this one takes whatever comes
+  const cudaError_t e = D == 64 ? launch_attend_as<64>(p, rows, num_sms, stream) : launch_attend_as<128>(p, rows, num_sms, stream);
+  return e != cudaSuccess || !many ? e : launch_attend_many(p, D, num_sms, stream);
 }
 
 }  // namespace tempo

@@ -13,6 +13,7 @@ namespace tempo {
 template <int ROWS, int TILE>
 struct Cut {
   static constexpr int kRows = ROWS, kTile = TILE;
+  static constexpr bool kMany = ROWS == kAttendManyRows;
 
   struct Item {                 // rows [row0, row0 + kRows) of a sequence and key head, and its tiles
     int begin, tiles;           // number of its first tile in the launch
@@ -20,7 +21,7 @@ struct Cut {
     int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
   };
 
-  // A sequence; one whose rows are another launch's has no queries here.
+  // A sequence; one that is the other kernel's has no queries here.
   static __device__ __forceinline__ void span_of(const AttendParams& p, int b, int& len, int& q0, int& n, bool tell = false) {
     const int given = p.lens[b];
     len = min(max(given, 0), p.max_pages << p.page_shift);
@@ -29,7 +30,7 @@ struct Cut {
     q0 = min(max(from, 0), p.T);
     n = max(min(max(to, 0), p.T) - q0, 0);
     if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
-    if (n * p.group <= p.rows_above || n * p.group > p.rows_most) n = 0;
+    if ((n * p.group <= p.rows_few || len <= p.len_few) == kMany) n = 0;
   }
 
   // Tiles are numbered in 32 bits: a sequence whose bound of them would not leave room for B like it is not taken.

@@ -258,7 +258,7 @@ struct AttendParams {
   int B, T, Hkv, group;      // group: query heads of a key head
   int max_pages, page_size, page_shift, n_pages;
   bool wide;                 // rows of q and out can be read and written 32 bytes at a time
-  int rows_above, rows_most; // sequences with so many rows (queries times group) are this launch's
+  int rows_few, len_few;    // sequences of up to so many rows (queries times group) or tokens are the few-query kernel's
   const __nv_bfloat16* q;
   const uint8_t* cache;
   const int32_t* page_table;
