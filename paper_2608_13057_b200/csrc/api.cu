@@ -752,6 +752,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.wide = aligned(q, 32) && a->ld_q % 16 == 0 && a->hd_q % 16 == 0 && aligned(out, 32) && a->ld_out % 16 == 0 && a->hd_out % 16 == 0;
   p.scale_log2 = a->scale * 1.4426950408889634f; p.status = status;
   p.counters = reinterpret_cast<unsigned int*>(ws + L.off_counters);
+  p.groups = reinterpret_cast<unsigned int*>(ws + L.off_groups);
   p.stats = reinterpret_cast<float*>(ws + L.off_stats); p.part = reinterpret_cast<float*>(ws + L.off_out);
   p.wait_ns = kDefaultWaitNs;
   return launch_attend(p, a->max_q, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;

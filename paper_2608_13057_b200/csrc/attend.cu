@@ -634,7 +634,8 @@ AttendLayout attend_layout(int D) {
   const auto round = [](size_t v) { return (v + 255) / 256 * 256; };
   AttendLayout L;
   L.off_counters = 0;
-  L.off_stats = round(kAttendMaxSms * sizeof(unsigned int));
+  L.off_groups = round(kAttendMaxSms * sizeof(unsigned int));
+  L.off_stats = L.off_groups + round(kAttendMaxSms * 2 * sizeof(unsigned int));
   L.off_out = L.off_stats + round(static_cast<size_t>(kAttendMaxSms) * 2 * kAttendManyRows * 8);
   L.total = L.off_out + static_cast<size_t>(kAttendMaxSms) * 2 * kAttendManyRows * D * 4;
   return L;

@@ -8,7 +8,8 @@
 // While one row tile's weights are made the tensor cores work on the other.  Maxima are raised only when they have grown by
 // more than 8 (in powers of 2), so that O is seldom touched between products.  The order of a sum over d is free: K and Q are stored
 // as the pairs (n, n + 4) in which codes are decoded, V's rows in the order that stores them without bank conflicts.
-// The tiles of all items are dealt to the CTAs in equal runs; items that were cut are joined by the CTA that arrives last.
+// The tiles of all items are dealt to the CTAs in equal runs; items that were cut are joined by the CTA that arrives last, those
+// of many parts in groups first.
 //
 // What bounds it: a step of 256 rows and 128 keys takes 2900 to 3600 clocks.  Its products alone, with the operands as they lie, take
 // 2460 (2048 at the nominal rate; Q K^T with both operands in shared memory reads 128 bytes a clock, all that there is), its
@@ -609,46 +610,69 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
           ++seen;
         }
         if (ctas == 1) continue;
-        __threadfence();
-        fine = sync_softmax();
-        if (!fine) break;
-        if (tid == kThreads - 1) {
-          const bool last = atomicAdd(p.counters + first, 1u) == static_cast<unsigned>(ctas) - 1u;
-          if (last) p.counters[first] = 0;
-          s_last = last;
-        }
-        fine = sync_softmax();
-        if (!fine) break;
-        if (s_last && active) {
+        // Of many parts, groups first, each by its own last CTA: a CTA reads 64 bytes a clock at best, 2000 clocks for a part of two row
+        // tiles.  18 parts (16 queries over 16384 tokens, 64 heads on 8) 49 -> 43 us, 37 (64 queries over 65536, 16 heads of 64 on 2) 65 ->
+        // 56; 6 or 7 are joined sooner at once (300 queries over 5000 tokens 49 against 53).
+        int group = ctas;
+        if (ctas > 12)
+          for (group = 4; group * group < ctas;) ++group;
+        const int lead = (static_cast<int>(blockIdx.x) - first) / group * group;
+#pragma unroll 1
+        for (int level = 0; level < 2; ++level) {
+          const int from = first + (level == 0 ? lead : 0), stride = level == 0 ? 1 : group;
+          const int count = level == 0 ? min(group, ctas - lead) : (ctas + group - 1) / group;
+          const bool ends = level == 1 || group == ctas;
           __threadfence();
-          float top = -INFINITY, all = 0.0f;
-          for (int c = 0; c < ctas; ++c) top = fmaxf(top, __ldcg(stats + part_of(first + c) * kRows + r).x);
-          const float ref = top == -INFINITY ? 0.0f : top;
-          for (int c = 0; c < ctas; ++c) {
-            const float2 st = __ldcg(stats + part_of(first + c) * kRows + r);
-            all += st.y * exp2_fast(st.x - ref);
+          fine = sync_softmax();
+          if (!fine) break;
+          if (tid == kThreads - 1) {
+            unsigned* counter = ends ? p.counters + first : p.groups + part_of(from);
+            const bool last = atomicAdd(counter, 1u) == static_cast<unsigned>(count) - 1u;
+            if (last) *counter = 0;
+            s_last = last;
           }
+          fine = sync_softmax();
+          if (!fine) break;
+          const bool go = s_last != 0;
+          if (go && active) {
+            __threadfence();
+            float top = -INFINITY, all = 0.0f;
+            for (int c = 0; c < count; ++c) top = fmaxf(top, __ldcg(stats + part_of(from + c * stride) * kRows + r).x);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            for (int c = 0; c < count; ++c) {
+              const float2 st = __ldcg(stats + part_of(from + c * stride) * kRows + r);
+              all += st.y * exp2_fast(st.x - ref);
+            }
 #pragma unroll 1
-          for (int y = 0; y < D / 64; ++y) {
-            float o[64];
+            for (int y = 0; y < D / 64; ++y) {
+              float o[64];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) o[i] = 0.0f;
+              for (int i = 0; i < 64; ++i) o[i] = 0.0f;
 #pragma unroll 1
-            for (int c = 0; c < ctas; ++c) {
-              const size_t at = part_of(first + c);
-              const float k = exp2_fast(__ldcg(stats + at * kRows + r).x - ref);
-              float4 v[16];
+              for (int c = 0; c < count; ++c) {
+                const size_t at = part_of(from + c * stride);
+                const float k = exp2_fast(__ldcg(stats + at * kRows + r).x - ref);
+                float4 v[16];
 #pragma unroll
-              for (int q = 0; q < 16; ++q) v[q] = __ldcg(parts + (at * (D / 4) + 16 * y + q) * kRows + r);
+                for (int q = 0; q < 16; ++q) v[q] = __ldcg(parts + (at * (D / 4) + 16 * y + q) * kRows + r);
 #pragma unroll
-              for (int q = 0; q < 16; ++q) {
-                o[4 * q] += v[q].x * k; o[4 * q + 1] += v[q].y * k; o[4 * q + 2] += v[q].z * k; o[4 * q + 3] += v[q].w * k;
+                for (int q = 0; q < 16; ++q) {
+                  o[4 * q] += v[q].x * k; o[4 * q + 1] += v[q].y * k; o[4 * q + 2] += v[q].z * k; o[4 * q + 3] += v[q].w * k;
+                }
+              }
+              if (ends) {
+                store_half(cur, y, o, all == 0.0f ? 0.0f : 1.0f / all, p.wide);
+              } else {                                 // in the place of the group's first part, whose elements are this thread's
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                  __stcg(parts + (part_of(from) * (D / 4) + 16 * y + q) * kRows + r, make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]));
               }
             }
-            store_half(cur, y, o, all == 0.0f ? 0.0f : 1.0f / all, p.wide);
+            if (!ends) __stcg(stats + part_of(from) * kRows + r, make_float2(top, all));
           }
+          fine = sync_softmax();                       // s_last is read before it is written again
+          if (!fine || !go || ends) break;
         }
-        fine = sync_softmax();                         // s_last is read before the next item's is written
       }
     }
   }

@@ -251,7 +251,7 @@ constexpr int kAttendMaxB = 1024;
 constexpr int kAttendMaxSms = 160;   // the workspace is sized for so many CTAs, whatever the device
 constexpr int kAttendManyRows = 256; // rows of an item in the kernel for many queries
 struct AttendLayout {
-  size_t off_counters, off_stats, off_out, total;
+  size_t off_counters, off_groups, off_stats, off_out, total;
 };
 AttendLayout attend_layout(int D);
 struct AttendParams {
@@ -269,6 +269,7 @@ struct AttendParams {
   float scale_log2;          // scale * log2(e)
   uint32_t* status;
   unsigned int* counters;    // arrivals of the CTAs that share an item, by the first of them; zero between calls
+  unsigned int* groups;      // and of a group among them, by the place of its first part
   float* stats;              // [CTA][2][rows][2]: maximum and sum of a part of an item
   float* part;               // [CTA][2][rows][D]
   unsigned long long wait_ns;

@@ -53,3 +53,13 @@ def test_little_and_much_in_one_batch(B, D, page):
     for _ in range(2):
         c.check(c.run())
     assert int(c.status) == 0 and not c.work[:640].any()
+
+
+@pytest.mark.parametrize("spans,Hq,Hkv,D", [([(30000, 16)], 64, 8, 128), ([(150000, 9)], 16, 1, 64), ([(40000, 40), (9000, 30)], 16, 1, 128)])
+def test_items_of_many_parts(B, spans, Hq, Hkv, D):
+    """Few items of many tokens: the parts of one are joined in groups."""
+    c = Case(B.binding, spans, Hq, Hkv, D, 256)
+    out = c.run()
+    c.check(out)
+    assert torch.equal(out, c.run())
+    assert int(c.status) == 0 and not c.work[:2048].any()
