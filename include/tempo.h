@@ -417,7 +417,8 @@ int tempo_cache_bytes(const tempo_cache* shape /*[host]*/, size_t* bytes /*[host
  *                     slots[t] / page_size).  k' is not rounded before it is quantised: the codes are those of the formula in 64
  *                     bits, also where a value lies next to a border between two of them.
  *   tempo_kv_read     rows of the cache back as fp16, exactly: k[i], v[i] = token slots[i]
- * norm(x) = x / sqrt(mean(x^2) + eps) over the D elements of a head; without q_w (k_w) that operand is not normed.
+ * norm(x) = x / sqrt(mean(x^2) + eps) over the D elements of a head, whatever their size (squares may leave the range of 32 bits);
+ * without q_w (k_w) that operand is not normed.
  * rot turns the pairs (i, i + rot/2), or with `interleaved` (2i, 2i+1), i < rot/2, of the first `rot` elements by
  * (cos, sin) = cos_sin[position, i], cos_sin[position, rot/2 + i]; the others pass.  rot = 0: no rotation, no table.
  *   q, q' bf16 [T, Hq, D], k, k', v bf16 [T, Hkv, D]: heads of D contiguous elements at row and head pitches ld_*, hd_*
