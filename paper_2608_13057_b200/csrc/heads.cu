@@ -138,7 +138,10 @@ __device__ __forceinline__ Target target_of(const HeadsParams& p, bool keys) {
 // A lane's eight elements of norm(x) * w turned by the row's angles, in R.  `e` is the lane's first element, beyond D for a
 // lane without one; every lane of the warp takes part in the exchanges (`stage`: 32 places of the warp's own in shared memory).
 // amplitude: the most that an element's two products add up to without their signs; infinite where the sum of squares is not one that
-// 32 bits give, so that nothing is taken for near.
+// 32 bits give, so that nothing is taken for near, and at least kLeast where an element that enters is not zero: its products may have
+// vanished in 32 bits.
+constexpr float kLeast = 1.2e-38f;
+__device__ __forceinline__ float least_of(uint4 raw) { return ((raw.x | raw.y | raw.z | raw.w) & 0x7fff7fffu) != 0 ? kLeast : 0.0f; }
 template <int LPH, typename R>
 __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, int e, bool live, const float* angles, uint4 raw, uint4* stage,
                                        R (&y)[8], float& amplitude) {
@@ -147,7 +150,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
   float x[8], w[8];
   widen8(raw, x);
   R r = R(1);
-  amplitude = 0.0f;
+  amplitude = least_of(raw);
   if (o.w != nullptr) {
     R ss = R(0);
 #pragma unroll
@@ -156,7 +159,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
     for (int d = LPH / 2; d > 0; d /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
     const R mean = ss / R(p.D) + R(p.eps);
     r = inverse_root<R>(mean);
-    if constexpr (sizeof(R) == 4) amplitude = in_range(mean) ? 0.0f : INFINITY;
+    if constexpr (sizeof(R) == 4) amplitude = in_range(mean) ? amplitude : INFINITY;
     if (mine) weights8(o.w, p.w_f32, p.w_vec, e, w);
   }
 #pragma unroll
@@ -201,6 +204,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
     u.w = __shfl_sync(0xffffffffu, raw.w, from);
     if (!turn) return;
     widen8(u, x);
+    amplitude = fmaxf(amplitude, least_of(u));
     const int eo = first ? e + half : e - half;
     if (o.w != nullptr) weights8(o.w, p.w_f32, p.w_vec, eo, w);
     const float4* t = reinterpret_cast<const float4*>(angles + (first ? e : eo));
@@ -231,6 +235,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
       const bool first = e + i < half;
       const int eo = first ? e + i + half : e + i - half, a = first ? e + i : eo;
       const float xo = __bfloat162float(head[eo]);
+      if (xo != 0.0f) amplitude = fmaxf(amplitude, kLeast);
       const R other = o.w != nullptr ? R(xo) * r * R(weight1(o.w, p.w_f32, eo)) : R(xo);
       amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
       const R c = R(__ldg(angles + a)), s = R(__ldg(angles + half + a));

@@ -78,3 +78,18 @@ def test_append_normed_keys_of_any_size(B, sizes, eps, D, rot, pairs):
         B.tempo_kv_append(shape, k[:, h:h + 1], v[:, h:h + 1], slots, cache, st, k_w=w, positions=pos, cos_sin=cs, eps=eps,
                           interleaved=pairs == "next")
         assert torch.equal(_read(B, shape, cache, slots)[0][0], kb[:, h:h + 1])
+
+
+def test_append_keys_and_weights_so_small_that_their_product_vanishes(B):
+    """Products below 32-bit floats' range: a group of them has a scale (the least one) in 64 bits, a group of zeros has none."""
+    D, T = 64, 12
+    k = torch.zeros(T, 1, D, dtype=torch.bfloat16, device=DEV)
+    k[::2] = 9e-41
+    k[1] = 1.0
+    w = torch.full((D,), 1e-10, device=DEV)
+    shape, cache = _cache(B, 1, 16, 1, D, fill=0)
+    slots, st = torch.arange(T, device=DEV, dtype=torch.int32), _status()
+    B.tempo_kv_append(shape, k, k, slots, cache, st, k_w=w)
+    scales = cache[8 * D:8 * D + 2 * T * (D // 32)].view(T, D // 32, 2)[:, :, 0]
+    want = (k[:, 0].view(T, D // 32, 32) != 0).any(2)
+    assert torch.equal(scales != 0, want) and (scales[::2] == 1).all() and int(st) == 0
