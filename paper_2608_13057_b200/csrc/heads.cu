@@ -135,6 +135,13 @@ __device__ __forceinline__ Target target_of(const HeadsParams& p, bool keys) {
   return keys ? Target{p.k_out, p.ld_k_out, p.hd_k_out, p.k_out_vec} : Target{p.q_out, p.ld_q_out, p.hd_q_out, p.q_out_vec};
 }
 
+// a * c + b * s, and what the two add up to without their signs into `amplitude`: angle tables need not be of unit length.
+template <typename R>
+__device__ __forceinline__ R turned_by(R a, R b, float s, float c, float& amplitude) {
+  amplitude = fmaxf(amplitude, fmaf(fabsf(static_cast<float>(a)), fabsf(c), fabsf(static_cast<float>(b) * s)));
+  return a * R(c) + b * R(s);
+}
+
 // A lane's eight elements of norm(x) * w turned by the row's angles, in R.  `e` is the lane's first element, beyond D for a
 // lane without one; every lane of the warp takes part in the exchanges (`stage`: 32 places of the warp's own in shared memory).
 // amplitude: the most that an element's two products add up to without their signs; infinite where the sum of squares is not one that
@@ -187,9 +194,8 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
     for (int i = 0; i < 4; ++i) {
       if (e + 2 * i >= p.rot) continue;                 // unturned elements pass as they are
       const R a = y[2 * i], b = y[2 * i + 1];
-      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(a)) + fabsf(static_cast<float>(b)));
-      y[2 * i] = a * R(c[i]) - b * R(s[i]);
-      y[2 * i + 1] = b * R(c[i]) + a * R(s[i]);
+      y[2 * i] = turned_by(a, b, -s[i], c[i], amplitude);
+      y[2 * i + 1] = turned_by(b, a, s[i], c[i], amplitude);
     }
     return;
   }
@@ -219,8 +225,7 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const R other = o.w != nullptr ? R(x[i]) * r * R(w[i]) : R(x[i]);
-      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
-      y[i] = first ? y[i] * R(c[i]) - other * R(s[i]) : y[i] * R(c[i]) + other * R(s[i]);
+      y[i] = turned_by(y[i], other, first ? -s[i] : s[i], c[i], amplitude);
     }
     return;
   }
@@ -237,9 +242,8 @@ __device__ __forceinline__ void turned(const HeadsParams& p, const Operand& o, i
       const float xo = __bfloat162float(head[eo]);
       if (xo != 0.0f) amplitude = fmaxf(amplitude, kLeast);
       const R other = o.w != nullptr ? R(xo) * r * R(weight1(o.w, p.w_f32, eo)) : R(xo);
-      amplitude = fmaxf(amplitude, fabsf(static_cast<float>(y[i])) + fabsf(static_cast<float>(other)));
-      const R c = R(__ldg(angles + a)), s = R(__ldg(angles + half + a));
-      y[i] = first ? y[i] * c - other * s : y[i] * c + other * s;
+      const float s = __ldg(angles + half + a);
+      y[i] = turned_by(y[i], other, first ? -s : s, __ldg(angles + a), amplitude);
     }
   }
   __syncwarp();

@@ -1,4 +1,5 @@
-"""Heads whose squares leave the range of 32-bit floats: tempo_qk_rotate and tempo_kv_append against the formulas in 64 bits."""
+"""Heads whose squares leave the range of 32-bit floats, and angle tables that are not of unit length: tempo_qk_rotate and
+tempo_kv_append against the formulas in 64 bits."""
 import pytest
 import torch
 
@@ -93,3 +94,48 @@ def test_append_keys_and_weights_so_small_that_their_product_vanishes(B):
     scales = cache[8 * D:8 * D + 2 * T * (D // 32)].view(T, D // 32, 2)[:, :, 0]
     want = (k[:, 0].view(T, D // 32, 32) != 0).any(2)
     assert torch.equal(scales != 0, want) and (scales[::2] == 1).all() and int(st) == 0
+
+
+@pytest.mark.parametrize("size", [1.35, 50.0, 0.02])
+@pytest.mark.parametrize("D,rot,norm,pairs", [(128, 128, True, "half"), (64, 64, False, "next"), (128, 96, True, "next"), (64, 50, True, "half")])
+def test_codes_with_tables_of_other_lengths(B, size, D, rot, norm, pairs):
+    """cos and sin multiplied by a factor, as a caller may do to scale the scores of long contexts."""
+    g = _gen(D + rot + norm)
+    T, Hkv = 4000, 8
+    k = (_rand(g, T, Hkv, D) * (0.01 + 4 * torch.rand(T, Hkv, 1, generator=g, device=DEV))).to(torch.bfloat16)
+    v = _rand(g, T, Hkv, D).to(torch.bfloat16)
+    w = (1 + 0.3 * _rand(g, D)).to(torch.bfloat16) if norm else None
+    cs = _table(g, rot) * size
+    pos = torch.randint(0, 97, (T,), generator=g, device=DEV, dtype=torch.int32)
+    shape, cache = _cache(B, T // 16, 16, Hkv, D)
+    slots = torch.randperm(T, generator=g, device=DEV).to(torch.int32)
+    st = _status()
+    B.tempo_kv_append(shape, k, v, slots, cache, st, k_w=w, positions=pos, cos_sin=cs, interleaved=pairs == "next")
+    (kb, vb), _ = _read(B, shape, cache, slots)
+    assert torch.equal(kb.double(), R.cached(R.turn(k, w, pos, cs, interleaved=pairs == "next")))
+    assert torch.equal(vb.double(), R.cached(v)) and int(st) == 0
+
+
+@pytest.mark.parametrize("size", [1.0, 30.0, 1000.0])
+@pytest.mark.parametrize("D,rot,norm,pairs", [(128, 128, True, "half"), (128, 128, False, "half"), (64, 64, False, "next"), (64, 60, False, "next"),
+                                              (64, 50, False, "half")])
+def test_codes_where_the_products_of_a_pair_cancel(B, size, D, rot, norm, pairs):
+    """Equal elements turned by an eighth of a circle: half of the results are small, and off by what their products are."""
+    g = _gen(D + rot + norm)
+    T, Hkv = 4000, 4
+    one = _rand(g, T, Hkv, rot // 2).to(torch.bfloat16)
+    k = _rand(g, T, Hkv, D).to(torch.bfloat16)
+    k[:, :, :rot] = one.repeat_interleave(2, 2) if pairs == "next" else torch.cat([one, one], 2)
+    if pairs == "next":                                                 # both results of a pair share a group: the sums are made small too
+        k[:, :, 1:rot:2] *= torch.where(torch.rand(T, Hkv, 1, generator=g, device=DEV) < 0.5, 1.0, -1.0).to(torch.bfloat16)
+    w = torch.full((D,), 1.25, device=DEV) if norm else None
+    a = torch.pi / 4 + 0.003 * _rand(g, 97, rot // 2).double()
+    cs = (size * torch.cat([a.cos(), a.sin()], 1)).float()
+    pos = torch.randint(0, 97, (T,), generator=g, device=DEV, dtype=torch.int32)
+    shape, cache = _cache(B, T // 16, 16, Hkv, D)
+    slots = torch.randperm(T, generator=g, device=DEV).to(torch.int32)
+    st = _status()
+    B.tempo_kv_append(shape, k, k, slots, cache, st, k_w=w, positions=pos, cos_sin=cs, interleaved=pairs == "next")
+    (kb, vb), _ = _read(B, shape, cache, slots)
+    assert torch.equal(kb.double(), R.cached(R.turn(k, w, pos, cs, interleaved=pairs == "next")))
+    assert torch.equal(vb.double(), R.cached(k)) and int(st) == 0
