@@ -463,7 +463,8 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  *        TEMPO_STATUS_TIMEOUT (waits inside a CTA are bounded as in tempo_grouped_ffn) zero it again.
  * A sequence with more than 10^9 / B tiles of scores (16 or 256 rows by 64 or 128 tokens) is left out (TEMPO_STATUS_CAPACITY).
  * A length beyond the page table counts as its end, rows outside q as none, both with TEMPO_STATUS_BAD_INDEX; a page outside
- * the cache that holds tokens of a sequence makes the outputs that see them NaN (TEMPO_STATUS_BAD_INDEX).  Results do not depend
+ * the cache that holds tokens of a sequence makes the outputs that see them NaN (TEMPO_STATUS_BAD_INDEX).  What lies in tokens that a
+ * query does not see says nothing in its output, whatever it is, also where the token was never appended.  Results do not depend
  * on timing; where long items are cut, and so the last bits of a result, goes by the lengths of all sequences of the call.
  */
 typedef struct {

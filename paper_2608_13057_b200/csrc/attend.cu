@@ -253,13 +253,26 @@ __device__ __forceinline__ void run_weights(Running<F>& s, const float (&c)[F::k
   }
 }
 
+// Values of a tile of which some row does not see all, before they are decoded.
 template <class F>
-__device__ __forceinline__ void run_values(Running<F>& s, const Decode& dc, const uint8_t* stage, int t0, int len,
-                                           const uint32_t (&w8)[F::kUnits][F::NR][2]) {
+__device__ __forceinline__ void mend_values(uint8_t* stage, int t0, int len) {
+  using U = CacheUnit<F::D>;
+  constexpr int kWords = U::kParams / 4, kPair = U::kPairParams / 4;     // of a unit, of two tokens
+#pragma unroll
+  for (int k = 0; k < F::kUnits; ++k)
+#pragma unroll
+    for (int i = threadIdx.x & 31; i < kWords; i += 32) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(stage + k * U::kBytes + U::kCodes) + i;
+      *w = edge_params(*w, len - (t0 + 16 * k + 2 * (i / kPair)));
+    }
+  __syncwarp();
+}
+
+template <class F>
+__device__ __forceinline__ void run_values(Running<F>& s, const Decode& dc, const uint8_t* stage, const uint32_t (&w8)[F::kUnits][F::NR][2]) {
   using U = CacheUnit<F::D>;
   constexpr int D = F::D, W = D / 32, NR = F::NR;
   const int lane = threadIdx.x & 31, g = lane / 4, j = lane & 3;
-  const bool tail = t0 + F::kTile > len;
 #pragma unroll
   for (int k = 0; k < F::kUnits; ++k) {
     const uint8_t* unit = stage + k * U::kBytes;
@@ -268,12 +281,7 @@ __device__ __forceinline__ void run_values(Running<F>& s, const Decode& dc, cons
     for (int x = 0; x < 2; ++x) {                    // tokens 16 k + 2 pair, + 1
       const int pair = 4 * x + j;
       load_words<W>(unit + pair * U::kPairRow + g * (D / 8), w[x]);
-      uint32_t params = *reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4);
-      if (tail) {                                    // tokens that do not exist: what lies there may be anything
-        const int left = len - (t0 + 16 * k + 2 * pair);
-        if (left < 2) params &= left == 1 ? 0xffffu : 0u;
-      }
-      group_params(params, sc[x], b[x]);
+      group_params(*reinterpret_cast<const uint32_t*>(unit + U::kCodes + pair * U::kPairParams + (D == 128 ? g / 2 : g / 4) * 4), sc[x], b[x]);
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r)                     // times 1: the sum is that of the weights as they meet V
@@ -405,7 +413,7 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   __shared__ int n_segments;
   int* before = reinterpret_cast<int*>(smem + F::kBefore);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint8_t* ring = smem + warp * F::kStageBytes;
+  uint8_t* ring = smem + warp * F::kStageBytes;
 
   pdl_trigger();
   if (tid == 0) n_segments = 0;
@@ -518,7 +526,8 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
       run_weights<F>(s, c, w8);
       cp_async_wait<1>();
       __syncwarp();
-      run_values<F>(s, dc, ring + kUnits * U::kBytes, t0, it.len, w8);
+      if (t0 + kTile - 1 > s.least) mend_values<F>(ring + kUnits * U::kBytes, t0, it.len);
+      run_values<F>(s, dc, ring + kUnits * U::kBytes, w8);
       __syncwarp();
       if (more) request(1);
       cp_async_commit();

@@ -168,9 +168,9 @@ __device__ __forceinline__ void decode_keys(const Decode& dc, const uint8_t* sta
 
 // Values of one stage, transposed: a lane takes two words (8 elements) of four pairs of tokens and stores, for each element, its
 // eight tokens.  Element 8 x + 4 e + n is row 64 (x / 8) + 8 (4 e + n) + x % 8 of the tile: no bank twice in a store, and 64
-// neighbouring rows are 64 neighbouring elements.
+// neighbouring rows are 64 neighbouring elements.  `left`: tokens that exist from the tile's first on; `edge`: some row does not see all.
 template <int D>
-__device__ __forceinline__ void decode_values(const Decode& dc, const uint8_t* stage, uint8_t* tile, int left, int warp) {
+__device__ __forceinline__ void decode_values(const Decode& dc, uint8_t* stage, uint8_t* tile, int left, bool edge, int warp) {
   using U = CacheUnit<D>;
   constexpr int kX = D / 8, kPer = 32 / kX;                              // lanes to eight tokens, eights of tokens to a warp
   const int lane = threadIdx.x & 31, x = lane % kX;
@@ -178,18 +178,19 @@ __device__ __forceinline__ void decode_values(const Decode& dc, const uint8_t* s
   for (int task = warp; task < kKeys / 8 / kPer; task += kDecoders) {
     const int eight = task * kPer + lane / kX;
     const uint8_t* unit = stage + eight / 2 * U::kBytes + (eight & 1) * 4 * U::kPairRow + x * 8;
-    const uint8_t* unit_params = stage + eight / 2 * U::kBytes + U::kCodes + (eight & 1) * 4 * U::kPairParams + x / 4 * 4;
+    uint8_t* eight_params = stage + eight / 2 * U::kBytes + U::kCodes + (eight & 1) * 4 * U::kPairParams;
+    const uint8_t* unit_params = eight_params + x / 4 * 4;
+    if (edge) {                                                          // a word of byte pairs to each lane, which all read
+      uint32_t* w = reinterpret_cast<uint32_t*>(eight_params) + x;
+      *w = edge_params(*w, left - (8 * eight + 2 * (x / (D / 32))));
+      __syncwarp();
+    }
     uint32_t v[4][2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint2 w = *reinterpret_cast<const uint2*>(unit + i * U::kPairRow);
-      uint32_t params = *reinterpret_cast<const uint32_t*>(unit_params + i * U::kPairParams);
-      if (left < kKeys) {                                                // tokens of the pair that exist
-        const int here = left - (8 * eight + 2 * i);
-        if (here < 2) params &= here == 1 ? 0xffffu : 0u;
-      }
       uint32_t s, b;
-      group_params(params, s, b);
+      group_params(*reinterpret_cast<const uint32_t*>(unit_params + i * U::kPairParams), s, b);
       decode8(dc, w.x, s, b, v[i][0]);
       decode8(dc, w.y, s, b, v[i][1]);
     }
@@ -452,16 +453,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       uint32_t phase = 0;
       bool fine = true;
       while (fine && pc.next(p)) {
-        const int steps = pc.steps();
+        const int steps = pc.steps(), least = pc.it.len - pc.it.n + pc.it.row0 / p.group;   // the last token that every row sees
         for (int i = 0; fine && i < steps; ++i, ++t) {
-          const int buf = t & 1;
+          const int buf = t & 1, k0 = (pc.tile0() + i) * kKeys;
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             fine = wait(kv == 0 ? bars.k_empty[buf] : bars.v_empty[buf], (t >> 1 & 1) ^ 1) && wait(bars.code_full[stage], phase);
             if (!fine) break;
-            const uint8_t* codes = smem + S::kCodes + stage * S::kStageBytes;
+            uint8_t* codes = smem + S::kCodes + stage * S::kStageBytes;
             if (kv == 0) decode_keys<D>(dc, codes, smem + S::kK + buf * S::kTileBytes, s_absent[stage], warp - 2);
-            else decode_values<D>(dc, codes, smem + S::kV + buf * S::kTileBytes, pc.it.len - (pc.tile0() + i) * kKeys, warp - 2);
+            else decode_values<D>(dc, codes, smem + S::kV + buf * S::kTileBytes, pc.it.len - k0, k0 + kKeys - 1 > least, warp - 2);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {

@@ -34,6 +34,14 @@ __device__ __forceinline__ void group_params(uint32_t p, uint32_t& s, uint32_t& 
   b = as_u32(__hmul2(as_half2(s), as_half2(((p >> 8) & 0x00f000f0u) | 0xd400d400u)));
 }
 
+// The byte pairs of two tokens' values, `left` of which (and more behind them) exist: what lies in the others may be anything.  Nor
+// need a token that exists have been written: a scale is at most 768, which is the most that the append stores, since an infinite one or a
+// NaN would reach the rows that do not see the token as 0 * NaN.
+__device__ __forceinline__ uint32_t edge_params(uint32_t p, int left) {
+  p = (p & 0xff00ff00u) | __vminu2(p & 0x00ff00ffu, 0x00c400c4u);
+  return left >= 2 ? p : left == 1 ? p & 0xffffu : 0u;
+}
+
 // (v & mask) | bits in one instruction: with both as immediates it would be two, and logic is what bounds the decoding.
 __device__ __forceinline__ uint32_t and_or(uint32_t v, uint32_t mask, uint32_t bits) {
   uint32_t r;
