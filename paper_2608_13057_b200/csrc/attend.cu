@@ -83,6 +83,7 @@ struct Running {
   float f[F::NR][2];                                 // score = f * (sum of products), in units of log2; above zero
   int limit[F::NR][2], least;                        // last token that each row sees; the least over all rows
   float m[F::NR][2];
+  bool far;                                          // far_scores of some row of the warp
   float l[F::NR][4];                                 // sums of the weights: rows in [0] and [1]
   float o[F::NR][kN][4];                             // elements g D/8 + 2 i (in [0], [1]) and + 2 i + 1 (in [2], [3])
 };
@@ -147,6 +148,7 @@ __device__ __forceinline__ void begin_item(const AttendParams& p, const typename
     for (int i = 0; i < Running<F>::kN; ++i) { s.o[r][i][0] = s.o[r][i][1] = s.o[r][i][2] = s.o[r][i][3] = 0.0f; }
   }
   s.least = it.len - it.n + it.row0 / p.group;
+  s.far = false;
 }
 
 // One tile is the tokens [t0, t0 + kTile) of the item, its keys and its values at `stage`.  Here its scores: c[k][r], of the tokens
@@ -208,7 +210,7 @@ __device__ __forceinline__ void run_keys(const Running<F>& s, const Decode& dc, 
 
 // Scores to weights, as the B operands of the output: w8[k][r] of row g, tokens 2 j, + 1 and 8 + 2 j, + 1 of unit k.
 template <class F>
-__device__ __forceinline__ void run_weights(Running<F>& s, const float (&c)[F::kUnits][F::NR][4], uint32_t (&w8)[F::kUnits][F::NR][2]) {
+__device__ __forceinline__ void run_weights(Running<F>& s, float (&c)[F::kUnits][F::NR][4], uint32_t (&w8)[F::kUnits][F::NR][2]) {
   constexpr int NR = F::NR;
   bool raise = false;
   float top[NR][2];
@@ -224,6 +226,7 @@ __device__ __forceinline__ void run_weights(Running<F>& s, const float (&c)[F::k
     }
   // A maximum that has grown little stays: weights up to 2^15 are in fp16's range, and O is left alone.
   if (__any_sync(0xffffffffu, raise)) {
+    bool far = false;
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -234,23 +237,40 @@ __device__ __forceinline__ void run_weights(Running<F>& s, const float (&c)[F::k
         const float m = t > s.m[r][y] + kSlack ? t : s.m[r][y];
         const float k = m == s.m[r][y] ? 1.0f : exp2_fast(s.m[r][y] - m);
         s.m[r][y] = m;
+        far = far || far_scores(m);
         s.l[r][y] *= k;
 #pragma unroll
         for (int i = 0; i < Running<F>::kN; ++i) { s.o[r][i][y] *= k; s.o[r][i][y + 2] *= k; }
       }
+    s.far = __any_sync(0xffffffffu, far);
+  }
+  float f[NR][2], less[NR][2];
+#pragma unroll
+  for (int r = 0; r < NR; ++r)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) { f[r][y] = s.f[r][y]; less[r][y] = s.m[r][y] == -INFINITY ? 0.0f : kBias - s.m[r][y]; }
+  if (s.far) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        if (far_scores(s.m[r][y])) {
+#pragma unroll
+          for (int k = 0; k < F::kUnits; ++k)
+#pragma unroll
+            for (int x = y; x < 4; x += 2) c[k][r][x] = from_far(c[k][r][x], f[r][y], s.m[r][y]);
+          f[r][y] = 1.0f;
+          less[r][y] = kBias;
+        }
   }
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    float less[2];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) less[y] = s.m[r][y] == -INFINITY ? 0.0f : kBias - s.m[r][y];
+  for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int k = 0; k < F::kUnits; ++k)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        w8[k][r][x] = transpose8(as_u32(__floats2half2_rn(exp2_fast(fmaf(c[k][r][2 * x], s.f[r][0], less[0])),
-                                                          exp2_fast(fmaf(c[k][r][2 * x + 1], s.f[r][1], less[1])))));
-  }
+        w8[k][r][x] = transpose8(as_u32(__floats2half2_rn(exp2_fast(fmaf(c[k][r][2 * x], f[r][0], less[r][0])),
+                                                          exp2_fast(fmaf(c[k][r][2 * x + 1], f[r][1], less[r][1])))));
 }
 
 // Values of a tile of which some row does not see all, before they are decoded.

@@ -172,13 +172,20 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 constexpr float kBias = 7.0f, kSlack = 8.0f;      // weights are 2^(x - m + 7); m is raised once x exceeds it by more than 8
 
+// A weight's exponent is fma(sum, f, 7 - m), with one rounding.  m itself is rounded, to a multiple of 1 from 2^23 on: then the exact
+// product may lie so far above or below it that every weight of the row overflows or vanishes.  From 2^22 on products are rounded as m
+// was, before m is taken off them.
+__device__ __forceinline__ bool far_scores(float m) { return fabsf(m) >= 0x1p22f && m != -INFINITY; }
+__device__ __forceinline__ float from_far(float sum, float f, float m) { return __fsub_rn(__fmul_rn(sum, f), m); }
+
 // A row of queries times a power of two (and the scale's sign), its largest element in [256, 512): fp16 holds 2^-33 of it.
-// `up`: that factor; `f`: a score is f times the sum of products, in units of log2, and f is above zero.
+// `up`: that factor; `f`: a score is f times the sum of products, in units of log2; f is above zero, and at most 2^96, with which no score
+// overflows (a sum is below 2^30) and any two that differ are too far apart for both to count.
 __device__ __forceinline__ void row_factors(float top, bool odd, float scale_log2, float& up, float& f) {
   const int e = top > 0.0f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -110), 119) : 0;
   up = odd ? __uint_as_float(0x7fc00000u)
            : __uint_as_float((static_cast<uint32_t>(127 - e) << 23) | (__float_as_uint(scale_log2) & 0x80000000u));
-  f = fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * fabsf(scale_log2), 1.2e-38f);
+  f = fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(127 + e) << 23) * fabsf(scale_log2), 1.2e-38f), 0x1p96f);
 }
 
 }  // namespace tempo
