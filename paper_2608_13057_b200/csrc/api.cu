@@ -755,6 +755,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.groups = reinterpret_cast<unsigned int*>(ws + L.off_groups);
   p.stats = reinterpret_cast<float*>(ws + L.off_stats); p.part = reinterpret_cast<float*>(ws + L.off_out);
   p.wait_ns = kDefaultWaitNs;
+  p.idle_ns = 4096 * kDefaultWaitNs;                     // 10^9 tiles, the most of a call, take 14 s on 148 SMs
   return launch_attend(p, a->max_q, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
 }
 

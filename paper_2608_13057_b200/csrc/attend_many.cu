@@ -354,6 +354,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     const int begin = snapped(p, before, runs, blockIdx.x, n_runs, total, start), end = snapped(p, before, runs, blockIdx.x + 1, n_runs, total, behind);
     volatile int* abort_at = &abort_flag;
     const auto wait = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.wait_ns); };
+    // The softmax waits for scores and joins as long as a call may take: while items have one row tile its second warpgroup has nothing to
+    // do until the next item, or until a cut one is joined, and that is the whole run of the first one.  The roles that feed it, and the
+    // issuer for its weights, wait within the ordinary limit at every tile: where anything stalls, one of theirs ends and ends these.
+    const auto wait_softmax = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.idle_ns); };
 
     // 512 threads of 128 registers at launch: 256 of 64 and 256 of 192
     if (warp < 8) {
@@ -507,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       const auto sync_softmax = [&]() {                // a barrier of the softmax warps whose wait ends like any other
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(bars.joined));
-        return wait(bars.joined, joins++ & 1);
+        return wait_softmax(bars.joined, joins++ & 1);
       };
       bool fine = true;
       Row mine;
@@ -536,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
           bool far = false;                            // far_scores of some row of the warp, from step i on
           int i = 0;
           for (; i < steps; ++i) {
-            fine = wait(bars.s_full[x], done & 1);
+            fine = wait_softmax(bars.s_full[x], done & 1);
             if (!fine) break;
             ++done;
             tc_fence_after();
@@ -587,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
           // of the other one: two chunks of 2048 over 6144 tokens take 502 us, with both ways in one loop 517, without this one 492.
           for (bool first = true; far && i < steps; ++i, first = false) {
             if (!first) {
-              fine = wait(bars.s_full[x], done & 1);
+              fine = wait_softmax(bars.s_full[x], done & 1);
               if (!fine) break;
               ++done;
               tc_fence_after();

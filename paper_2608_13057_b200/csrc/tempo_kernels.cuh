@@ -272,7 +272,7 @@ struct AttendParams {
   unsigned int* groups;      // and of a group among them, by the place of its first part
   float* stats;              // [CTA][2][rows][2]: maximum and sum of a part of an item
   float* part;               // [CTA][2][rows][D]
-  unsigned long long wait_ns;
+  unsigned long long wait_ns, idle_ns;
 };
 cudaError_t launch_attend(AttendParams p, int max_q, int D, int num_sms, cudaStream_t stream);
 cudaError_t launch_attend_many(const AttendParams& p, int D, int num_sms, cudaStream_t stream);
