@@ -457,6 +457,8 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), addresses and pitches 16-byte aligned
  *   (TEMPO_ERR_ALIGN; with 32 bytes prompts are read and written in fewer accesses); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
  *   max_q [host] is the most queries of a sequence: a hint for the choice of kernels, any value gives the same result within rounding.
+ *   tempo_attend_padded takes n_valid i32 [1] too (or NULL): rows from it on are neither read nor written, whatever q_start says of
+ *   them; a sequence that it cuts has its other rows' results as if it did not.
  *   Rows before q_start[0] and from q_start[B] on are left as they are.  Hq is a multiple of Hkv; B <= 1024.
  *   workspace  tempo_attend_workspace_bytes, 256-byte aligned, ZEROED once by the caller; every call that completes leaves it
  *        ready for the next.  It serves any call of the same D.  Calls that may overlap on the GPU need one each.  After
@@ -476,6 +478,9 @@ int tempo_attend_workspace_bytes(const tempo_cache* shape /*[host]*/, int32_t Hq
 int tempo_attend(const tempo_attention* args, const tempo_cache* shape, const void* q_bf16, const void* cache,
                  const int32_t* page_table, const int32_t* lens, const int32_t* q_start, void* out_bf16, uint32_t* status,
                  void* workspace, void* stream);
+int tempo_attend_padded(const tempo_attention* args, const tempo_cache* shape, const void* q_bf16, const void* cache,
+                        const int32_t* page_table, const int32_t* lens, const int32_t* q_start, const int32_t* n_valid, void* out_bf16,
+                        uint32_t* status, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

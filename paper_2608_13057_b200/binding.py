@@ -50,6 +50,7 @@ EXPORTS = (
     "tempo_packed_weight_bytes_bf16", "tempo_pack_weights_bf16", "tempo_permute_pad_bf16", "tempo_grouped_ffn_bf16",
     "tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_workspace_bytes", "tempo_few_ffn", "tempo_few_ffn_bf16",
     "tempo_cache_bytes", "tempo_qk_rotate", "tempo_kv_append", "tempo_kv_read", "tempo_attend_workspace_bytes", "tempo_attend",
+    "tempo_attend_padded",
 )
 
 
@@ -301,7 +302,7 @@ if not isinstance(_marshal, _NoMarshal):
     _marshal.bind(TempoError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
                                 ("tempo_norm_in", "tempo_norm_out", "tempo_route", "tempo_few_ffn", "tempo_few_ffn_bf16",
                                  "tempo_few_workspace_bytes", "tempo_packed_weight_bytes", "tempo_packed_weight_bytes_bf16",
-                                 "tempo_qk_rotate", "tempo_kv_append", "tempo_kv_read", "tempo_attend", "tempo_cache_bytes",
+                                 "tempo_qk_rotate", "tempo_kv_append", "tempo_kv_read", "tempo_attend_padded", "tempo_cache_bytes",
                                  "tempo_attend_workspace_bytes")))
 
 
@@ -399,14 +400,15 @@ def tempo_attend_workspace_bytes(cache_shape: TempoCache, Hq: int) -> int:
     return out.value
 
 
-def tempo_attend(cache_shape, q, cache, page_table, lens, out, status, workspace, scale=None, q_start=None, max_q=1):
+def tempo_attend(cache_shape, q, cache, page_table, lens, out, status, workspace, scale=None, q_start=None, max_q=1,
+                 n_valid=None):
     """out[i] = attention of q[i] over its sequence's cached tokens, up to its own.
 
     q, out bf16 [T, Hq, D]; page_table i32 [B, pages], lens i32 [B]; q_start i32 [B + 1]: the queries of sequence b are rows
     q_start[b] to q_start[b + 1] - 1, its newest tokens (None: one query per sequence).  scale: None is D ** -0.5.  max_q: the
-    most queries of a sequence, for the choice of kernels."""
+    most queries of a sequence, for the choice of kernels.  n_valid i32 [1]: rows behind it are neither read nor written (None: all)."""
     rc = _marshal.attend(ctypes.addressof(cache_shape), q, cache, page_table, lens, out, status, workspace,
-                         cache_shape.D ** -0.5 if scale is None else scale, q_start, max_q)
+                         cache_shape.D ** -0.5 if scale is None else scale, q_start, max_q, n_valid)
     if rc:
         _check(rc, "tempo_attend")
 

@@ -723,8 +723,9 @@ int tempo_attend_workspace_bytes(const tempo_cache* c, int32_t Hq, size_t* bytes
   return TEMPO_OK;
 }
 
-int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, const void* cache, const int32_t* page_table,
-                 const int32_t* lens, const int32_t* q_start, void* out, uint32_t* status, void* workspace, void* stream) {
+int tempo_attend_padded(const tempo_attention* a, const tempo_cache* c, const void* q, const void* cache, const int32_t* page_table,
+                        const int32_t* lens, const int32_t* q_start, const int32_t* n_valid, void* out, uint32_t* status,
+                        void* workspace, void* stream) {
   const int rc = check_cache(c);
   if (rc != TEMPO_OK) return rc;
   if (a == nullptr || !q || !cache || !page_table || !lens || !out || !status || !workspace) return TEMPO_ERR_NULL;
@@ -736,7 +737,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
       static_cast<long long>(a->T) * (a->Hq / c->Hkv) > 0x7fffff00ll)
     return TEMPO_ERR_UNSUPPORTED;
   if (!vectors8(q, a->ld_q, a->hd_q) || !vectors8(out, a->ld_out, a->hd_out) || !aligned(cache, 16) || !aligned(page_table, 4) ||
-      !aligned(lens, 4) || !aligned(q_start, 4) || !aligned(status, 4) || !aligned(workspace, 256))
+      !aligned(lens, 4) || !aligned(q_start, 4) || !aligned(n_valid, 4) || !aligned(status, 4) || !aligned(workspace, 256))
     return TEMPO_ERR_ALIGN;
   const int sms = min(sm_count(), kAttendMaxSms);
   if (sms <= 0) return TEMPO_ERR_CUDA;
@@ -747,7 +748,7 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.max_pages = a->max_pages; p.page_size = c->page_size; p.n_pages = c->n_pages;
   while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
   p.q = static_cast<const __nv_bfloat16*>(q); p.cache = static_cast<const uint8_t*>(cache);
-  p.page_table = page_table; p.lens = lens; p.q_start = q_start; p.out = static_cast<__nv_bfloat16*>(out);
+  p.page_table = page_table; p.lens = lens; p.q_start = q_start; p.n_valid = n_valid; p.out = static_cast<__nv_bfloat16*>(out);
   p.ld_q = a->ld_q; p.hd_q = a->hd_q; p.ld_out = a->ld_out; p.hd_out = a->hd_out;
   p.wide = aligned(q, 32) && a->ld_q % 16 == 0 && a->hd_q % 16 == 0 && aligned(out, 32) && a->ld_out % 16 == 0 && a->hd_out % 16 == 0;
   p.scale_log2 = a->scale * 1.4426950408889634f; p.status = status;
@@ -757,6 +758,11 @@ int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, 
   p.wait_ns = kDefaultWaitNs;
   p.idle_ns = 4096 * kDefaultWaitNs;                     // 10^9 tiles, the most of a call, take 14 s on 148 SMs
   return launch_attend(p, a->max_q, c->D, sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TEMPO_OK : TEMPO_ERR_CUDA;
+}
+
+int tempo_attend(const tempo_attention* a, const tempo_cache* c, const void* q, const void* cache, const int32_t* page_table,
+                 const int32_t* lens, const int32_t* q_start, void* out, uint32_t* status, void* workspace, void* stream) {
+  return tempo_attend_padded(a, c, q, cache, page_table, lens, q_start, nullptr, out, status, workspace, stream);
 }
 
 }  // extern "C"

@@ -33,11 +33,11 @@ namespace {
 // The kernel's form for items of 8 NR rows.  Warps: as many as have their registers without a spill, which would go to L2 (shared memory
 // leaves no L1): 16 rows and 12 warps took 88 us where 8 take 64 (64 x 8192); 8 rows and 12 warps 57, 16 warps 61, 8 warps 61
 // (2 x 131072), for D = 64 16 warps 22.5 and 12 warps 27 (37 x 2999).
-template <int D_, int NR_>
+template <int D_, int NR_, bool PADDED>
 struct Few {
   static constexpr int D = D_, NR = NR_, kRows = 8 * NR;
   static constexpr int kWarps = NR == 2 ? 8 : D == 128 ? 12 : 16, kTile = 64, kUnits = kTile / kUnit;
-  using Tiles = Cut<kRows, kTile>;
+  using Tiles = Cut<kRows, kTile, PADDED>;
   using Item = typename Tiles::Item;
   static constexpr int kStageBytes = 2 * kUnits * CacheUnit<D>::kBytes;   // the keys of its units, then the values
   static constexpr int kRing = kWarps * kStageBytes;
@@ -641,9 +641,9 @@ __global__ void __launch_bounds__(F::kWarps * 32, 1) attend_kernel(const __grid_
   }
 }
 
-template <int D, int NR>
+template <int D, int NR, bool PADDED>
 cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
-  using F = Few<D, NR>;
+  using F = Few<D, NR, PADDED>;
   static_assert(F::kBefore + (kAttendMaxB + 1) * 4 + 1024 <= 227 * 1024, "shared memory of one SM");
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = smem_limit_once(attend_kernel<F>, F::bytes(kAttendMaxB), done);
@@ -652,9 +652,13 @@ cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t st
 }
 
 // Items of 8 rows where no sequence has more: half the products of items of 16, and registers for 16 warps instead of 12.
+template <int D, bool PADDED>
+cudaError_t launch_attend_as(const AttendParams& p, int64_t rows, int num_sms, cudaStream_t stream) {
+  return rows <= 8 ? launch_attend_as<D, 1, PADDED>(p, num_sms, stream) : launch_attend_as<D, 2, PADDED>(p, num_sms, stream);
+}
 template <int D>
 cudaError_t launch_attend_as(const AttendParams& p, int64_t rows, int num_sms, cudaStream_t stream) {
-  return rows <= 8 ? launch_attend_as<D, 1>(p, num_sms, stream) : launch_attend_as<D, 2>(p, num_sms, stream);
+  return p.n_valid == nullptr ? launch_attend_as<D, false>(p, rows, num_sms, stream) : launch_attend_as<D, true>(p, rows, num_sms, stream);
 }
 
 }  // namespace

@@ -10,7 +10,8 @@
 
 namespace tempo {
 
-template <int ROWS, int TILE>
+// PADDED: with n_valid, in kernels of their own (in the others its lines cost a prompt 1 to 2 %).
+template <int ROWS, int TILE, bool PADDED>
 struct Cut {
   static constexpr int kRows = ROWS, kTile = TILE;
   static constexpr bool kMany = ROWS == kAttendManyRows;
@@ -21,7 +22,8 @@ struct Cut {
     int len, q0, n;             // tokens in the cache, first query row and queries of the sequence
   };
 
-  // A sequence; one that is the other kernel's has no queries here.
+  // A sequence; one that is the other kernel's has no queries here.  Rows from n_valid on are not there, nor are the tokens that they
+  // stand for: its other queries see what they see with them.
   static __device__ __forceinline__ void span_of(const AttendParams& p, int b, int& len, int& q0, int& n, bool tell = false) {
     const int given = p.lens[b];
     len = min(max(given, 0), p.max_pages << p.page_shift);
@@ -30,6 +32,11 @@ struct Cut {
     q0 = min(max(from, 0), p.T);
     n = max(min(max(to, 0), p.T) - q0, 0);
     if (tell && (len != given || q0 != from || q0 + n != to)) atomicOr(p.status, TEMPO_STATUS_BAD_INDEX);
+    if constexpr (PADDED) {
+      const int cut = min(max(q0 + n - max(*p.n_valid, 0), 0), n);
+      n -= cut;
+      len = max(len - cut, 0);
+    }
     if ((n * p.group <= p.rows_few || len <= p.len_few) == kMany) n = 0;
   }
 

@@ -28,8 +28,6 @@ constexpr int kThreads = 512;                         // four warpgroups: loader
 constexpr int kKeys = 128, kRowTile = 128, kRows = 2 * kRowTile;
 static_assert(kRows == kAttendManyRows, "the workspace is sized for it");
 constexpr int kDecoders = 6;                          // warps 2 to 7
-using Tiles = Cut<kRows, kKeys>;
-using Item = Tiles::Item;
 
 template <int D>
 struct ManySmem {
@@ -49,7 +47,9 @@ struct Bars {
 };
 
 // A CTA's run as pieces of items, the same in every role.
+template <class Tiles>
 struct Pieces {
+  using Item = typename Tiles::Item;
   Item it;
   int x, end;
   bool first;
@@ -73,7 +73,8 @@ constexpr int kLeast = 4, kSnap = 3;
 
 // Where run r begins, and in which item: its equal share of the tiles, or the border of an item that is near.  So an item [b, e) is cut
 // at the equal shares in (b + kSnap, e - kSnap), and nowhere else.
-__device__ __forceinline__ int snapped(const AttendParams& p, const int* before, const Runs& runs, int r, int n_runs, int total, Item& it) {
+template <class Tiles>
+__device__ __forceinline__ int snapped(const AttendParams& p, const int* before, const Runs& runs, int r, int n_runs, int total, typename Tiles::Item& it) {
   const int x = r >= n_runs ? total : runs.begin(r);
   if (x == total) return total;
   it = Tiles::item_at(p, before, x);
@@ -225,7 +226,7 @@ __device__ __forceinline__ void store32(void* dst, const uint32_t (&v)[8]) {
 }
 
 // This thread's row of queries into its row tile, as fp16 in the order of the decoded keys.
-template <int D>
+template <int D, class Item>
 __device__ __forceinline__ Row load_row(const AttendParams& p, const Item& it, int r, uint32_t tile, int row_in_tile) {
   Row o;
   const int row = it.row0 + r, qi = row / p.group, head = it.h * p.group + row - qi * p.group;
@@ -305,9 +306,11 @@ __device__ __forceinline__ void rescale(uint32_t o_at, float k) {
 template <int D>
 __device__ __noinline__ void rescale_far(uint32_t o_at, float k) { rescale<D>(o_at, k); }
 
-template <int D>
+template <int D, bool PADDED>
 __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_constant__ AttendParams p) {
   extern __shared__ uint8_t smem_raw[];
+  using Tiles = Cut<kRows, kKeys, PADDED>;
+  using Item = typename Tiles::Item;
   using S = ManySmem<D>;
   using U = CacheUnit<D>;
   __shared__ Bars bars;
@@ -340,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
   }
   pdl_wait();
   tc_fence_before();
-  const int total = Tiles::count_tiles<kThreads / 32>(p, before, warp_sum, false);      // also orders what is set up above
+  const int total = Tiles::template count_tiles<kThreads / 32>(p, before, warp_sum, false);      // also orders what is set up above
   tc_fence_after();
   const uint32_t tmem = s_tmem;
 
@@ -351,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
   if (works) {
     const Runs runs(total, n_runs);
     Item start, behind;                                // the items that the run begins in, and that the next one begins in
-    const int begin = snapped(p, before, runs, blockIdx.x, n_runs, total, start), end = snapped(p, before, runs, blockIdx.x + 1, n_runs, total, behind);
+    const int begin = snapped<Tiles>(p, before, runs, blockIdx.x, n_runs, total, start), end = snapped<Tiles>(p, before, runs, blockIdx.x + 1, n_runs, total, behind);
     volatile int* abort_at = &abort_flag;
     const auto wait = [&](uint64_t& b, uint32_t parity) { return mbar_wait_warp(smem_u32(&b), parity, abort_at, p.wait_ns); };
     // The softmax waits for scores and joins as long as a call may take: while items have one row tile its second warpgroup has nothing to
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     // 512 threads of 128 registers at launch: 256 of 64 and 256 of 192
     if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    Pieces pc(start, begin, end, before);
+    Pieces<Tiles> pc(start, begin, end, before);
     if (warp == 0) {
       // ---- loader: keys, then values of each tile; lanes 0 to 7 a unit each
       const size_t head_bytes = static_cast<size_t>(p.page_size / kUnit) * U::kBytes;
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
     }
     } else {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-      Pieces pc(start, begin, end, before);
+      Pieces<Tiles> pc(start, begin, end, before);
       // ---- softmax: warpgroup x on row tile x, thread by row
       const int x = (warp - 8) >> 2, row = (warp & 3) * 32 + lane, r = x * kRowTile + row;
       const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
       };
       bool fine = true;
       Row mine;
-      const auto load = [&](const Pieces& c) {
+      const auto load = [&](const Pieces<Tiles>& c) {
         if (x == 1 && !c.two(p.group)) return;
         mine = load_row<D>(p, c.it, r, q_tile, row);
         fence_async_smem();
@@ -759,26 +762,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_many_kernel(const __grid_c
 }
 
 // The warps' split of registers draws on those that the block was launched with: with fewer of them it would wait for good.
-template <int D>
+template <int D, bool PADDED>
 bool registers_suffice() {
   cudaFuncAttributes a;
-  return cudaFuncGetAttributes(&a, attend_many_kernel<D>) == cudaSuccess && a.numRegs * kThreads >= 256 * 64 + 256 * 192;
+  return cudaFuncGetAttributes(&a, attend_many_kernel<D, PADDED>) == cudaSuccess && a.numRegs * kThreads >= 256 * 64 + 256 * 192;
 }
 
-template <int D>
+template <int D, bool PADDED>
 cudaError_t launch_as(const AttendParams& p, int num_sms, cudaStream_t stream) {
-  static const bool fits = registers_suffice<D>();
+  static const bool fits = registers_suffice<D, PADDED>();
   if (!fits) return cudaErrorInvalidConfiguration;
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = smem_limit_once(attend_many_kernel<D>, ManySmem<D>::bytes(kAttendMaxB), done);
+  const cudaError_t e = smem_limit_once(attend_many_kernel<D, PADDED>, ManySmem<D>::bytes(kAttendMaxB), done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend_many_kernel<D>, dim3(num_sms), dim3(kThreads), ManySmem<D>::bytes(p.B), stream, p);
+  return launch_pdl(attend_many_kernel<D, PADDED>, dim3(num_sms), dim3(kThreads), ManySmem<D>::bytes(p.B), stream, p);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_many(const AttendParams& p, int D, int num_sms, cudaStream_t stream) {
-  return D == 64 ? launch_as<64>(p, num_sms, stream) : launch_as<128>(p, num_sms, stream);
+  if (p.n_valid == nullptr) return D == 64 ? launch_as<64, false>(p, num_sms, stream) : launch_as<128, false>(p, num_sms, stream);
+  return D == 64 ? launch_as<64, true>(p, num_sms, stream) : launch_as<128, true>(p, num_sms, stream);
 }
 
 }  // namespace tempo

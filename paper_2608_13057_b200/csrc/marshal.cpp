@@ -25,7 +25,7 @@ decltype(&tempo_packed_weight_bytes) g_packed_bytes[2] = {nullptr, nullptr};
 decltype(&tempo_qk_rotate) g_qk_rotate = nullptr;
 decltype(&tempo_kv_append) g_kv_append = nullptr;
 decltype(&tempo_kv_read) g_kv_read = nullptr;
-decltype(&tempo_attend) g_attend = nullptr;
+decltype(&tempo_attend_padded) g_attend = nullptr;
 decltype(&tempo_cache_bytes) g_cache_bytes = nullptr;
 decltype(&tempo_attend_workspace_bytes) g_attend_bytes = nullptr;
 
@@ -405,9 +405,9 @@ PyObject* kv_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
-// (cache shape address, q, cache, page_table, lens, out, status, workspace, scale, q_start, max_q)
+// (cache shape address, q, cache, page_table, lens, out, status, workspace, scale, q_start, max_q, n_valid)
 PyObject* attend(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  return guarded(n, 11, [&]() -> int {
+  return guarded(n, 12, [&]() -> int {
     const tempo_cache* c = cache_at(v[0]);
     tempo_attention a{};
     a.scale = number(v[8]);
@@ -421,6 +421,7 @@ PyObject* attend(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* status = word(v[6], "status");
     void* workspace = addr(v[7], at::kByte, "workspace");
     void* q_start = addr(v[9], at::kInt, "q_start");
+    void* n_valid = word(v[11], "n_valid");
     if (table == nullptr || lens == nullptr) refuse("page_table and lens: expected tensors");
     const at::Tensor& pt = THPVariable_Unpack(v[3]);
     if (pt.dim() != 2 || pt.size(0) > INT32_MAX || pt.size(1) > INT32_MAX) refuse("page_table: expected shape [sequences, pages], got ", pt.sizes());
@@ -433,7 +434,7 @@ PyObject* attend(PyObject*, PyObject* const* v, Py_ssize_t n) {
     size_t bytes = 0;
     if (g_attend_bytes(c, Hq, &bytes) == TEMPO_OK) holds(v[7], static_cast<int64_t>(bytes), "workspace");
     return g_attend(&a, c, q.at, cache, static_cast<const int32_t*>(table), static_cast<const int32_t*>(lens),
-                    static_cast<const int32_t*>(q_start), out.at, static_cast<uint32_t*>(status), workspace, stream);
+                    static_cast<const int32_t*>(q_start), static_cast<const int32_t*>(n_valid), out.at, static_cast<uint32_t*>(status), workspace, stream);
   });
 }
 

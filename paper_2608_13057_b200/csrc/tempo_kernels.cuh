@@ -264,6 +264,7 @@ struct AttendParams {
   const int32_t* page_table;
   const int32_t* lens;
   const int32_t* q_start;
+  const int32_t* n_valid;
   __nv_bfloat16* out;
   size_t ld_q, hd_q, ld_out, hd_out;
   float scale_log2;          // scale * log2(e)

@@ -140,8 +140,8 @@ class Attention:
         qkv bf16 [T, (Hq + 2 Hkv) * D]: a projection's rows (queries, keys, values); out bf16 [T, Hq, D] or [T, Hq * D].
         positions, slots i32 [T]: of the rotation, and where in the cache (page * page_size + offset; below zero: not appended).
         page_table i32 [B, pages], lens i32 [B]: the sequences with this batch's tokens; q_start i32 [B + 1]: their rows (None: one
-        each), max_q the most of one.  n_valid i32 [1]: rows behind it are not appended.  Enqueues kernels only: the call can be
-        captured in a CUDA graph."""
+        each), max_q the most of one.  n_valid i32 [1]: rows behind it are neither appended nor read, and their rows of out stay as
+        they are.  Enqueues kernels only: the call can be captured in a CUDA graph."""
         T = qkv.shape[0]
         if T > self.q.shape[0]:
             raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.q.shape[0]}")
@@ -151,7 +151,7 @@ class Attention:
         B.tempo_kv_append(self.shape, k, v, slots, self.cache, self.status, k_w=self.k_w, q=q, q_w=self.q_w, q_out=turned, eps=self.eps,
                           interleaved=self.interleaved, n_valid=n_valid, **turn)
         B.tempo_attend(self.shape, turned, self.cache, page_table, lens, out.view(T, self.Hq, self.D), self.status, self.workspace,
-                       scale=self.scale, q_start=q_start, max_q=max_q)
+                       scale=self.scale, q_start=q_start, max_q=max_q, n_valid=n_valid)
         return out
 
     def read(self, slots):
