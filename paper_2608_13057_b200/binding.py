@@ -400,13 +400,18 @@ def tempo_attend_workspace_bytes(cache_shape: TempoCache, Hq: int) -> int:
     return out.value
 
 
-def tempo_attend(cache_shape, q, cache, page_table, lens, out, status, workspace, scale=None, q_start=None, max_q=1,
+def tempo_attend(cache_shape, q, cache, page_table, lens, out, status, workspace, scale=None, q_start=None, max_q=None,
                  n_valid=None):
     """out[i] = attention of q[i] over its sequence's cached tokens, up to its own.
 
     q, out bf16 [T, Hq, D]; page_table i32 [B, pages], lens i32 [B]; q_start i32 [B + 1]: the queries of sequence b are rows
     q_start[b] to q_start[b + 1] - 1, its newest tokens (None: one query per sequence).  scale: None is D ** -0.5.  max_q: the
-    most queries of a sequence, for the choice of kernels.  n_valid i32 [1]: rows behind it are neither read nor written (None: all)."""
+    most queries of a sequence, for the choice of kernels (None: 1 without q_start, else as many as one has if each has one at
+    least; any value gives the same result within rounding, but prompts under a max_q of 1 take several times as long).  n_valid i32 [1]: rows behind it are neither read nor written (None: all)."""
+    if max_q is None:
+        max_q = 1
+        if q_start is not None and all(isinstance(t, torch.Tensor) and t.dim() for t in (q, page_table)):
+            max_q = max(1, q.shape[0] - page_table.shape[0] + 1)
     rc = _marshal.attend(ctypes.addressof(cache_shape), q, cache, page_table, lens, out, status, workspace,
                          cache_shape.D ** -0.5 if scale is None else scale, q_start, max_q, n_valid)
     if rc:

@@ -134,14 +134,14 @@ class Attention:
         self.q = torch.empty(max_tokens, Hq, D, dtype=torch.bfloat16, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
-    def forward(self, qkv, positions, slots, page_table, lens, out, q_start=None, max_q=1, n_valid=None):
+    def forward(self, qkv, positions, slots, page_table, lens, out, q_start=None, max_q=None, n_valid=None):
         """out = attention of this batch's tokens, which are appended to the cache first.
 
         qkv bf16 [T, (Hq + 2 Hkv) * D]: a projection's rows (queries, keys, values); out bf16 [T, Hq, D] or [T, Hq * D].
         positions, slots i32 [T]: of the rotation, and where in the cache (page * page_size + offset; below zero: not appended).
         page_table i32 [B, pages], lens i32 [B]: the sequences with this batch's tokens; q_start i32 [B + 1]: their rows (None: one
-        each), max_q the most of one.  n_valid i32 [1]: rows behind it are neither appended nor read, and their rows of out stay as
-        they are.  Enqueues kernels only: the call can be captured in a CUDA graph."""
+        each), max_q the most of one (None: 1 without q_start, else by the sizes).  n_valid i32 [1]: rows behind it are neither
+        appended nor read, and their rows of out stay as they are.  Enqueues kernels only: the call can be captured in a CUDA graph."""
         T = qkv.shape[0]
         if T > self.q.shape[0]:
             raise B.TempoError(f"a batch of {T} tokens exceeds the layer's {self.q.shape[0]}")
