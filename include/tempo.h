@@ -419,6 +419,7 @@ int tempo_cache_bytes(const tempo_cache* shape /*[host]*/, size_t* bytes /*[host
  *   tempo_kv_read     rows of the cache back as fp16, exactly: k[i], v[i] = token slots[i]
  * norm(x) = x / sqrt(mean(x^2) + eps) over the D elements of a head, whatever their size (squares may leave the range of 32 bits);
  * without q_w (k_w) that operand is not normed.
+ * cos_sin may have any finite entries, not only those of angles (a factor that scales the scores of long contexts among them).
  * rot turns the pairs (i, i + rot/2), or with `interleaved` (2i, 2i+1), i < rot/2, of the first `rot` elements by
  * (cos, sin) = cos_sin[position, i], cos_sin[position, rot/2 + i]; the others pass.  rot = 0: no rotation, no table.
  *   q, q' bf16 [T, Hq, D], k, k', v bf16 [T, Hkv, D]: heads of D contiguous elements at row and head pitches ld_*, hd_*
@@ -453,9 +454,13 @@ int tempo_kv_read(const tempo_cache* shape, const void* cache, const int32_t* sl
  *     out[i, h] = sum_t softmax_t(scale * <q[i, h], K[t, h / (Hq / Hkv)]>) V[t, h / (Hq / Hkv)]
  * A query that sees no token gets zeros.  K and V enter as they are (fp16 products, sums in 32 bits), and so does q where it lies
  * within 2^-25 of its head's largest element (within 2^-33 of that largest below); softmax weights are rounded to fp16 before they
- * meet V, and statistics are in 32 bits.  A query that is not finite makes its own head's output NaN.
+ * meet V, and statistics are in 32 bits.  The denominator is the sum of the rounded weights in the kernel for few queries and of the
+ * unrounded ones in the one for many, so that results differ within that rounding by which of them a sequence goes to (its rows and
+ * length, the batch's rows, max_q).  Scores may have any size that scale and q give.  A query that is not finite makes its own
+ * head's output NaN.
  *   q, out bf16 [T, Hq, D], heads of D contiguous elements at pitches ld_*, hd_* (elements), addresses and pitches 16-byte aligned
- *   (TEMPO_ERR_ALIGN; with 32 bytes prompts are read and written in fewer accesses); page_table i32 [B, max_pages], lens i32 [B]; q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
+ *   (TEMPO_ERR_ALIGN; with 32 bytes prompts are read and written in fewer accesses); page_table i32 [B, max_pages], lens i32 [B];
+ *   q_start i32 [B+1], rising, or NULL: one query per sequence (T = B).
  *   max_q [host] is the most queries of a sequence: a hint for the choice of kernels, any value gives the same result within rounding.
  *   tempo_attend_padded takes n_valid i32 [1] too (or NULL): rows from it on are neither read nor written, whatever q_start says of
  *   them; a sequence that it cuts has its other rows' results as if it did not.

@@ -12,11 +12,12 @@
 // a clock where the SM has 128.  Keys and values are the 16-row operand, so that 8 queries cost half the products of 16.  The order
 // of a sum over d or t is free: a lane's 16-byte load is what it needs, of keys 32 neighbouring elements (one group: one scale) of a
 // token, of values 16 neighbouring elements of two tokens side by side in a word's halves.
-// What bounds it: 64 sequences of up to 8192 tokens (16 rows; 193 MB) take 64.2 us, 46 % of a copy's rate, of which about 12 are
-// start and end; 16 tokens of a head cost a scheduler 330 instructions in 650 clocks with its two warps, 129 of them on the pipe of
-// logic, 121 on the one of fp16 sums, 34 matrix instructions of 8 clocks.  2 sequences of 131072 (4 rows; 245 MB) 58.4 us, 64 %:
-// 289 instructions, 17 matrix instructions.  One sequence of 1500: 9.7 us, a chain of latencies (tiles counted 1, queries and first
-// page 2, one tile 2.5, merges 1, arrival and join 2.5 us).
+// What bounds it: 64 sequences of up to 8192 tokens (16 rows; 193 MB) take 64.9 us, 45 % of a copy's rate, of which about 12 are
+// start and end; 16 tokens of a head cost a scheduler 321 instructions in 670 clocks, 119 of them on the pipe of logic, 127 on the one
+// of fp16 sums, 34 matrix instructions of 8 clocks: with its two warps it waits for results half of the time.  2 sequences of 131072
+// (4 rows; 245 MB) 57.7 us, 65 %: 286 instructions, 17 matrix instructions, in 440 clocks of a scheduler's three warps, of which this mix
+// of instructions alone takes 370.  One sequence of 1500: 9.9 us, a chain of latencies (tiles counted 1, queries and first page 2, one
+// tile 2.5, merges 1, arrival and join 2.5 us).
 //
 // Work is dealt in tiles of 64 tokens: the tiles of all items in one row, cut into equal runs, one for each warp of the launch,
 // whatever the lengths.  A warp streams its run through a tile of shared memory of its own (16-byte asynchronous copies: a bulk copy
@@ -651,7 +652,7 @@ cudaError_t launch_attend_as(const AttendParams& p, int num_sms, cudaStream_t st
   return launch_pdl(attend_kernel<F>, dim3(num_sms), dim3(F::kWarps * 32), F::bytes(p.B), stream, p);
 }
 
-// Items of 8 rows where no sequence has more: half the products of items of 16, and registers for 16 warps instead of 12.
+// Items of 8 rows where no sequence has more: half the products of items of 16, and registers for 12 warps (16 with D = 64) instead of 8.
 template <int D, bool PADDED>
 cudaError_t launch_attend_as(const AttendParams& p, int64_t rows, int num_sms, cudaStream_t stream) {
   return rows <= 8 ? launch_attend_as<D, 1, PADDED>(p, num_sms, stream) : launch_attend_as<D, 2, PADDED>(p, num_sms, stream);

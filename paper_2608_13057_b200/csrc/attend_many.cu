@@ -14,7 +14,7 @@
 // What bounds it: a step of 256 rows and 128 keys takes 2900 to 3600 clocks.  Its products alone, with the operands as they lie, take
 // 2460 (2048 at the nominal rate; Q K^T with both operands in shared memory reads 128 bytes a clock, all that there is), its
 // exponentials 2048 on the special-function units, and the softmax and decoding instructions 1400 of a scheduler's slots.  Two
-// chunks of 2048 queries over 6144 tokens, 64 heads of 128: 492 us, 1012 TFLOP/s, of which the row tiles' starts and ends are
+// chunks of 2048 queries over 6144 tokens, 64 heads of 128: 504 us, 989 TFLOP/s, of which the row tiles' starts and ends are
 // about 70 us.  Left out because they were slower (2 x 32768 tokens, 256 queries each, 339 us now): a quarter of the
 // exponentials as polynomials on the FMA pipe 408 against 369, two threads to a row 436 against 369.
 #include "attend_common.cuh"

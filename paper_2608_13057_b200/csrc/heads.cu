@@ -5,13 +5,13 @@
 // A head is held by D / 8 neighbouring lanes, eight elements each, so every operand is read once and every result written once.
 // Queries: a lane has both elements of its pairs, so that nothing is exchanged but the sum of squares, and weights, cos and sin
 // are multiplied once for all heads of a token that a group of lanes takes (one while there are few warps: latency; up to all).  Bound
-// by the bytes for a prompt, 8192 tokens of 64 + 4 heads of 128 in 54 to 55 us, 80 % of a copy's rate; by one launch and one
+// by the bytes for a prompt, 8192 tokens of 64 + 4 heads of 128 in 56.4 us, 78 % of a copy's rate; by one launch and one
 // load-sum-load-store chain for a token, 2.0 us.  Rotations of other lengths than multiples of 8 and rows at odd addresses go element by
-// element, the other ones through shared memory: 1200 tokens of 24 + 8 heads with 90 of 128 elements turned 12.9 us, all 128 6.7.
+// element, the other ones through shared memory: 1200 tokens of 24 + 8 heads with 90 of 128 elements turned 13.4 us, all 128 7.5.
 // Keys on their way into the cache: a code is the formula's in 64 bits also next to a border between two codes, whatever order a sum
 // is taken in, so that a cache filled here equals one filled elsewhere.  They are computed in 32 bits with a bound of their error, and
 // a warp in which any element lies within it of a border does all of its own again in 64.  4096 rows of 4 heads beside 64 heads of
-// queries, appended and read back: 39.9 us; all in 64 bits 44.5 us.
+// queries, appended and read back: 39.6 us; all in 64 bits 44.5 us.
 #include "cache.cuh"
 
 namespace tempo {

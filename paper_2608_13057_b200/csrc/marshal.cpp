@@ -1,7 +1,7 @@
 // Python module _marshal: argument marshalling of the calls whose kernels take a few microseconds (the norms, the router,
-// the few-token layer, the attention half of a layer).  It checks tensors and calls the C entry points, nothing else; the Python wrappers in binding.py
-// document the arguments.  The addresses of the C functions and the exception class come from binding.py at import, so the
-// library that is called is the one it loaded.
+// the few-token layer, the attention half of a layer).  It checks tensors and calls the C entry points, nothing else; the
+// Python wrappers in binding.py document the arguments.  The addresses of the C functions and the exception class come from
+// binding.py at import, so the library that is called is the one it loaded.
 #include <Python.h>
 
 #include <c10/cuda/CUDAFunctions.h>

@@ -120,7 +120,7 @@ class Attention:
     scale                of the scores; None: D ** -0.5
 
     A layer has one query buffer and one workspace: its calls must follow one another on one stream (or be ordered by events).
-    `status` collects the STATUS_* bits of every call.
+    `status` collects the STATUS_* bits of every call; after STATUS_TIMEOUT `workspace` has to be zeroed.
     """
 
     def __init__(self, n_pages, page_size, Hq, Hkv, D, max_tokens, cos_sin=None, q_w=None, k_w=None, eps=1e-6, interleaved=False,
